@@ -9,6 +9,7 @@
  *   3. hdf_lm_head_argmax  draft logits z_k and greedy draft tokens (Sec. 2.3)
  *   4. hdf_accept          greedy verification: longest agreeing prefix (Sec. 1, Sec. 3.4)
  *      (hdf_sample_tokens, hdf_accept_sample: the same at temperature T > 0;
+ *       hdf_sample_truncated, hdf_accept_truncated: with top-k, top-p and min-p as well;
  *       hdf_advance_context: the committed positions become the next round's context)
  *
  * Conventions shared by every call:
@@ -481,6 +482,105 @@ hdf_status hdf_kl_forward(const void* H_pos, int m, const float* gamma, float ep
                           int d, int vocab, hdf_dtype dtype, const float* student_logits,
                           int64_t ld, int B, const int32_t* labels, int n_seq, int P,
                           float temperature, float alpha, float* kl, float* ce, float* loss,
+                          void* ws, size_t ws_bytes, hdf_stream_t stream);
+
+/* ------------------------------------------------------------------------------
+ * 7. Truncated distributions: draws and verification with temperature, top-k, top-p and
+ * min-p (serving settings of every request), and a row's top logits.
+ *
+ * A row's entries are ordered by logit, largest first, ties to the lowest token.  -inf masks an
+ * entry (a NaN is masked too): it has no place in the order.  With m the greatest logit and
+ * w_v = exp((z_v - m) / T), the kept entries are the first n of the order:
+ *     n_k = top_k (all unmasked entries where 0 or more than there are)
+ *     n_p = the fewest of those n_k whose weights sum to at least top_p times the sum of all
+ *           n_k weights (n_k where top_p >= 1)
+ *     n_m = the entries with w_v >= min(min_p, 1)
+ *     n   = min(n_k, n_p, n_m); 1 at T = 0 (greedy); 0 where every entry is masked
+ * and the truncated distribution is the softmax at temperature T over them (one entry of
+ * probability 1 at T = 0).  A draw with the uniform u is the lowest token whose running sum of kept
+ * weights, in token order, exceeds u times their sum.  Sums and the weights in them are 64-bit.
+ * ----------------------------------------------------------------------------*/
+/* Settings, one value for every row or one a sequence.  Row r takes entry r / rows_per_seq of an
+ * array (device); where an array is NULL, the value beside it holds for all rows.  In arrays a
+ * temperature <= 0 or NaN is greedy, top_k <= 0, top_p >= 1 and min_p <= 0 (or NaN) are off,
+ * top_p <= 0 keeps the first entry. */
+typedef struct {
+  float temperature; /* >= 0, finite; 0 = greedy */
+  int top_k;         /* >= 0; 0 = off            */
+  float top_p;       /* >= 0; >= 1 = off         */
+  float min_p;       /* 0 <= min_p <= 1; 0 = off */
+  const float* temperatures;
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  int rows_per_seq; /* >= 1 */
+} hdf_truncation;
+
+/* Workspace bytes of hdf_sample_truncated (0 where none is needed, and on invalid arguments). */
+size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype);
+/* logits    rows x vocab dtype, row r at logits + r*ld; any alignment of their element
+ * params    host pointer
+ * uniforms  [rows] fp32 in [0, 1) (values outside are clamped), or NULL (no draws)
+ * tokens    [rows] int32 (out; with uniforms): the draw, -1 where every entry is masked
+ * kept      [rows] int32 (out): n
+ * cut_logit, cut_index  [rows] fp32, int32 (out): the last kept entry, so that v is kept iff
+ *           z_v > cut_logit or (z_v == cut_logit and v <= cut_index); -inf and -1 where every
+ *           unmasked entry is kept
+ * lse       [rows] fp64 (out): log of the sum of exp(z_v / T) over the kept entries (0 at T = 0,
+ *           -inf where n = 0), so that the truncated log-probability of v is z_v / T - lse
+ * ws, ws_bytes  at least hdf_sample_truncated_workspace(...) bytes, 256-byte aligned; its contents
+ *           on entry do not matter.
+ * Limits: 0 <= rows <= 65535, 1 <= vocab <= 2^20, ld >= vocab; logits below +inf. */
+hdf_status hdf_sample_truncated(const void* logits, int64_t rows, int vocab, int64_t ld,
+                                hdf_dtype dtype, const hdf_truncation* params,
+                                const float* uniforms, int32_t* tokens, int32_t* kept,
+                                float* cut_logit, int32_t* cut_index, double* lse, void* ws,
+                                size_t ws_bytes, hdf_stream_t stream);
+
+/* Workspace bytes of hdf_accept_truncated (0 on invalid arguments); the type is the target
+ * logits'. */
+size_t hdf_accept_truncated_workspace(int n_seq, int K, int vocab, hdf_dtype target_dtype);
+/* Speculative verification (section 5's rule) between truncated distributions, p_i the target's
+ * and q_i the drafter's, both under the sequence's settings:
+ *     draft x_i is accepted iff u_i q_i(x_i) < p_i(x_i), in order (u_i = uniforms[s][i]);
+ *     after n acceptances the next token is drawn with uniforms[s][K] from max(0, p_n - q_n) (from
+ *     p_n where that is zero throughout), after K from p_K.
+ * draft, draft_stride, ld   as hdf_accept_sample; a draft outside [0, vocab) is rejected
+ * draft_logits   draft_dtype, the rows the drafts were drawn from
+ * draft_cut_logit, draft_cut_index, draft_lse  [same rows]: their truncation under the same
+ *                settings (hdf_sample_truncated's outputs)
+ * target_logits  [n_seq][K+1][vocab] target_dtype, as hdf_accept_sample
+ * params         host pointer; the arrays hold an entry a sequence (rows_per_seq is not read)
+ * uniforms       [n_seq][K+1] fp32 in [0, 1)
+ * accept_len, next_anchor, commit_offsets, commit_tokens  as hdf_accept; the committed tokens are
+ *                the accepted drafts and the drawn token (-1 from a row masked throughout)
+ * ws, ws_bytes   at least hdf_accept_truncated_workspace(...) bytes, 256-byte aligned; its
+ *                contents on entry do not matter.
+ * Limits: 0 <= K <= 1024, 0 <= n_seq * (K + 1) <= 65535, 1 <= vocab <= 2^20. */
+hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const void* draft_logits,
+                                hdf_dtype draft_dtype, int64_t ld, const float* draft_cut_logit,
+                                const int32_t* draft_cut_index, const double* draft_lse,
+                                const void* target_logits, hdf_dtype target_dtype, int n_seq,
+                                int K, int vocab, const hdf_truncation* params,
+                                const float* uniforms, int32_t* accept_len, int32_t* next_anchor,
+                                int32_t* commit_offsets, int32_t* commit_tokens, void* ws,
+                                size_t ws_bytes, hdf_stream_t stream);
+
+/* Workspace bytes of hdf_top_logits (0 where none is needed, and on invalid arguments). */
+size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype);
+/* The first K entries of every row's order, and what the others weigh: a teacher's distribution
+ * as it is stored for distillation.
+ * logits   as hdf_sample_truncated
+ * ids      [rows][K] int32 (out): the tokens, -1 past the unmasked entries
+ * values   [rows][K] fp32 (out): their logits, -inf past the unmasked entries
+ * rest     [rows] fp32 (out, may be NULL): log of the sum of exp(z_v / T) over the unlisted
+ *          entries, -inf where there are none
+ * ws, ws_bytes  at least hdf_top_logits_workspace(...) bytes, 256-byte aligned; its contents on
+ *          entry do not matter.
+ * Limits: 0 <= rows <= 65535, 1 <= vocab <= 2^20, ld >= vocab, 1 <= K <= 1024,
+ *         0 < temperature < inf; logits below +inf. */
+hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,
+                          int K, float temperature, int32_t* ids, float* values, float* rest,
                           void* ws, size_t ws_bytes, hdf_stream_t stream);
 
 #ifdef __cplusplus

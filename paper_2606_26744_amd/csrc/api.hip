@@ -930,6 +930,155 @@ hdf_status hdf_accept_keys(void* ws, int n_seq, int B, int32_t* argmax, float* m
   return ok();
 }
 
+// ---------------------------------------------------------- truncated distributions
+}  // extern "C"
+
+namespace {
+
+constexpr int kMaxTruncVocab = 1 << 20;   // columns of an entry's 52-bit key
+
+hdf_status check_truncation(const char* fn, const hdf_truncation* p) {
+  if (p == nullptr) return fail(HDF_E_INVALID, "%s: null params", fn);
+  if (p->temperatures == nullptr && !(p->temperature >= 0.f && p->temperature < INFINITY))
+    return fail(HDF_E_INVALID, "%s: temperature must be finite and not negative", fn);
+  if (p->top_ks == nullptr && p->top_k < 0) return fail(HDF_E_INVALID, "%s: top_k < 0", fn);
+  if (p->top_ps == nullptr && !(p->top_p >= 0.f))
+    return fail(HDF_E_INVALID, "%s: top_p must not be negative", fn);
+  if (p->min_ps == nullptr && !(p->min_p >= 0.f && p->min_p <= 1.f))
+    return fail(HDF_E_INVALID, "%s: min_p outside [0, 1]", fn);
+  return HDF_OK;
+}
+
+hdf_status check_rows(const char* fn, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,
+                      const void* logits) {
+  if (dtype != HDF_F32 && dtype != HDF_BF16) return fail(HDF_E_INVALID, "%s: bad dtype", fn);
+  if (rows < 0 || vocab < 1 || ld < vocab)
+    return fail(HDF_E_INVALID, "%s: rows=%lld vocab=%d ld=%lld", fn, static_cast<long long>(rows),
+                vocab, static_cast<long long>(ld));
+  if (rows > 65535) return fail(HDF_E_UNSUPPORTED, "%s: more than 65535 rows", fn);
+  if (vocab > kMaxTruncVocab) return fail(HDF_E_UNSUPPORTED, "%s: vocab above 2^20", fn);
+  if (rows > 0 && logits == nullptr) return fail(HDF_E_INVALID, "%s: null logits", fn);
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == HDF_BF16 ? 1u : 3u)) != 0)
+    return fail(HDF_E_INVALID, "%s: logits must be aligned to their element", fn);
+  return HDF_OK;
+}
+
+hdf_status check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return HDF_OK;
+  if (ws == nullptr || ws_bytes < need)
+    return fail(HDF_E_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws_bytes);
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return fail(HDF_E_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  return HDF_OK;
+}
+
+void set_truncation(hdf::CutArgs& a, const hdf_truncation& p) {
+  a.t = p.temperature; a.k = p.top_k; a.p = p.top_p; a.mp = p.min_p;
+  a.ts = p.temperatures; a.ks = p.top_ks; a.ps = p.top_ps; a.mps = p.min_ps;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype) { return 0; }
+
+hdf_status hdf_sample_truncated(const void* logits, int64_t rows, int vocab, int64_t ld,
+                                hdf_dtype dtype, const hdf_truncation* params,
+                                const float* uniforms, int32_t* tokens, int32_t* kept,
+                                float* cut_logit, int32_t* cut_index, double* lse, void* ws,
+                                size_t ws_bytes, hdf_stream_t stream) {
+  hdf_status st = check_rows("sample_truncated", rows, vocab, ld, dtype, logits);
+  if (st == HDF_OK) st = check_truncation("sample_truncated", params);
+  if (st != HDF_OK) return st;
+  if (params->rows_per_seq < 1) return fail(HDF_E_INVALID, "sample_truncated: rows_per_seq < 1");
+  if (rows == 0) return ok();
+  if (kept == nullptr || cut_logit == nullptr || cut_index == nullptr || lse == nullptr ||
+      (uniforms == nullptr) != (tokens == nullptr))
+    return fail(HDF_E_INVALID, "sample_truncated: null pointer");
+  st = check_ws("sample_truncated", ws, ws_bytes, hdf_sample_truncated_workspace(rows, vocab, dtype));
+  if (st != HDF_OK) return st;
+  hdf::CutArgs a{};
+  a.z = logits; a.rows = rows; a.ld = ld; a.V = vocab; a.per = params->rows_per_seq;
+  set_truncation(a, *params);
+  a.u = uniforms; a.tok = tokens; a.kept = kept; a.cut_logit = cut_logit; a.cut_index = cut_index;
+  a.lse = lse;
+  const hipError_t e = hdf::launch_truncate(dtype == HDF_BF16, a,
+                                            reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "sample_truncated launch");
+  return ok();
+}
+
+size_t hdf_accept_truncated_workspace(int n_seq, int K, int vocab, hdf_dtype target_dtype) {
+  if (n_seq < 0 || K < 0 || K > 1024 || vocab < 1 || vocab > kMaxTruncVocab ||
+      int64_t(n_seq) * (K + 1) > 65535 || (target_dtype != HDF_F32 && target_dtype != HDF_BF16))
+    return 0;
+  return hdf::accept_truncated_ws_bytes(target_dtype == HDF_BF16, n_seq, K, vocab);
+}
+
+hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const void* draft_logits,
+                                hdf_dtype draft_dtype, int64_t ld, const float* draft_cut_logit,
+                                const int32_t* draft_cut_index, const double* draft_lse,
+                                const void* target_logits, hdf_dtype target_dtype, int n_seq,
+                                int K, int vocab, const hdf_truncation* params,
+                                const float* uniforms, int32_t* accept_len, int32_t* next_anchor,
+                                int32_t* commit_offsets, int32_t* commit_tokens, void* ws,
+                                size_t ws_bytes, hdf_stream_t stream) {
+  if (n_seq < 0) return fail(HDF_E_INVALID, "accept_truncated: n_seq < 0");
+  if (K < 0 || K > 1024) return fail(HDF_E_INVALID, "accept_truncated: K=%d outside [0, 1024]", K);
+  if (draft_stride < K) return fail(HDF_E_INVALID, "accept_truncated: draft_stride < K");
+  hdf_status st = check_rows("accept_truncated", int64_t(n_seq) * (K + 1), vocab, vocab,
+                             target_dtype, target_logits);
+  if (st == HDF_OK && K > 0)
+    st = check_rows("accept_truncated", n_seq > 0 ? 1 : 0, vocab, ld, draft_dtype, draft_logits);
+  if (st == HDF_OK) st = check_truncation("accept_truncated", params);
+  if (st != HDF_OK) return st;
+  if (n_seq == 0) return ok();
+  if ((K > 0 && (draft == nullptr || draft_cut_logit == nullptr || draft_cut_index == nullptr ||
+                 draft_lse == nullptr)) ||
+      uniforms == nullptr || accept_len == nullptr || next_anchor == nullptr)
+    return fail(HDF_E_INVALID, "accept_truncated: null pointer");
+  st = check_ws("accept_truncated", ws, ws_bytes,
+                hdf_accept_truncated_workspace(n_seq, K, vocab, target_dtype));
+  if (st != HDF_OK) return st;
+  hdf::CutArgs c{};
+  c.z = target_logits; c.rows = int64_t(n_seq) * (K + 1); c.ld = vocab; c.V = vocab; c.per = K + 1;
+  set_truncation(c, *params);
+  hdf::VerifyArgs a{};
+  a.draft = draft; a.stride = draft_stride; a.K = K; a.V = vocab; a.dz = draft_logits; a.ld = ld;
+  a.d_logit = draft_cut_logit; a.d_index = draft_cut_index; a.d_lse = draft_lse;
+  a.tz = target_logits; a.t = params->temperature; a.ts = params->temperatures; a.u = uniforms;
+  a.acc = accept_len; a.anchor = next_anchor; a.offs = commit_offsets; a.toks = commit_tokens;
+  const hipError_t e =
+      hdf::launch_accept_truncated(K > 0 && draft_dtype == HDF_BF16, target_dtype == HDF_BF16, a, c,
+                                   n_seq, ws, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "accept_truncated launch");
+  return ok();
+}
+
+size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype) { return 0; }
+
+hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,
+                          int K, float temperature, int32_t* ids, float* values, float* rest,
+                          void* ws, size_t ws_bytes, hdf_stream_t stream) {
+  hdf_status st = check_rows("top_logits", rows, vocab, ld, dtype, logits);
+  if (st != HDF_OK) return st;
+  if (K < 1 || K > 1024) return fail(HDF_E_INVALID, "top_logits: K=%d outside [1, 1024]", K);
+  if (!(temperature > 0.f) || !(temperature < INFINITY))
+    return fail(HDF_E_INVALID, "top_logits: temperature must be positive and finite");
+  if (rows == 0) return ok();
+  if (ids == nullptr || values == nullptr) return fail(HDF_E_INVALID, "top_logits: null pointer");
+  st = check_ws("top_logits", ws, ws_bytes, hdf_top_logits_workspace(rows, vocab, K, dtype));
+  if (st != HDF_OK) return st;
+  hdf::CutArgs a{};
+  a.z = logits; a.rows = rows; a.ld = ld; a.V = vocab; a.per = 1; a.t = temperature;
+  a.K = K; a.ids = ids; a.vals = values; a.rest = rest;
+  const hipError_t e = hdf::launch_top_logits(dtype == HDF_BF16, a,
+                                              reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "top_logits launch");
+  return ok();
+}
+
 // ---------------------------------------------------------- LM head without a workspace
 // For callers that cannot allocate: the per-row argmax keys live in this file-scope device
 // array (one copy per GPU, held until the process ends) instead of a workspace.  In host

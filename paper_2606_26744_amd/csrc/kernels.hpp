@@ -212,6 +212,56 @@ hipError_t launch_accept_sample(const int32_t* draft, int draft_stride, const fl
                                 uint64_t stream, int32_t* acc, int32_t* anchor, int32_t* offs,
                                 int32_t* toks, void* ws, hipStream_t s);
 
+// ---------------------------------------------------------------- truncated rows (trunc.hip)
+struct CutArgs {
+  const void* z;             // rows of V logits, stride ld
+  int64_t rows, ld;
+  int V;
+  // Truncation: row r takes entry r / per of an array, or the value where the array is NULL.
+  int per;
+  float t, p, mp;            // temperature, top_p, min_p
+  int k;                     // top_k
+  const float *ts, *ps, *mps;
+  const int32_t* ks;
+  const float* u;            // [rows] uniforms
+  int32_t* tok;              // [rows] draws, or NULL (no draw)
+  int32_t* kept;
+  float* cut_logit;
+  int32_t* cut_index;
+  double* lse;
+  // Top logits (at temperature t).
+  int K;
+  int32_t* ids;              // [rows][K]
+  float* vals;
+  float* rest;               // [rows], or NULL
+};
+hipError_t launch_truncate(bool bf16, const CutArgs& a, hipStream_t s);
+hipError_t launch_top_logits(bool bf16, const CutArgs& a, hipStream_t s);
+
+struct VerifyArgs {
+  const int32_t* draft;      // draft i of sequence s at s * stride + i, and so the rows below
+  int stride, K, V;
+  const void* dz;            // draft logits, row stride ld
+  int64_t ld;
+  const float* d_logit;      // their truncation
+  const int32_t* d_index;
+  const double* d_lse;
+  const void* tz;            // target logits [n_seq][K+1][V]
+  const float* t_logit;      // their truncation (set by the launch)
+  const int32_t* t_index;
+  const double* t_lse;
+  float t;
+  const float* ts;           // [n_seq] or NULL
+  const float* u;            // [n_seq][K+1]
+  int32_t* n_buf;            // [n_seq] accepted drafts, and the parts' sums (set by the launch)
+  double* sums;
+  int32_t *acc, *anchor, *offs, *toks;
+};
+size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V);
+// c: the truncation of the target rows (its outputs are set by the launch).
+hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs a, CutArgs c,
+                                   int n_seq, void* ws, hipStream_t s);
+
 // ---------------------------------------------------------------- KL forward (kl.hip)
 size_t kl_ws_bytes(int n_seq, int B, int P, int d, int V, bool bf16);
 hipError_t launch_kl_forward(bool bf16, const void* H_pos, int m, const float* gamma, float eps,

@@ -1,0 +1,142 @@
+// Rows of logits of either type, their order and their weights: shared by the truncated draws
+// and the distillation (trunc.hip, distill.hip).
+#pragma once
+
+#include "common.hpp"
+
+namespace hdf {
+
+// A row of V logits read 16 bytes at a time.  Rows start at any element (odd vocabularies, strides,
+// views): vector j holds columns j * N - shift .. + N - 1 and is aligned; the first and the last,
+// which reach past the row, are read element by element.
+template <typename T>
+struct LogitRow {
+  static constexpr int N = 16 / int(sizeof(T));
+  const T* p;
+  int V, shift;
+
+  __device__ __forceinline__ LogitRow(const T* row, int V_) : p(row), V(V_) {
+    shift = int((reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (N - 1));
+  }
+  __device__ __forceinline__ int vectors() const { return (V + shift + N - 1) / N; }
+  __device__ __forceinline__ int column(int j) const { return j * N - shift; }
+  // Vector j as fp32; columns outside the row and NaN are -inf, -0 is +0 (they are equal logits).
+  __device__ __forceinline__ void load(int j, float x[N]) const {
+    const int c = column(j);
+    if (c >= 0 && c + N <= V) {
+      const u32x4 v = ld16(p + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 2) {
+          x[2 * e] = lo_bf(v[e]);
+          x[2 * e + 1] = hi_bf(v[e]);
+        } else {
+          x[e] = __uint_as_float(v[e]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        x[e] = -INFINITY;
+        if (c + e >= 0 && c + e < V) {
+          if constexpr (sizeof(T) == 2)
+            x[e] = bf2f(p[c + e]);
+          else
+            x[e] = p[c + e];
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = fmaxf(x[e], -INFINITY) + 0.f;
+  }
+  __device__ __forceinline__ float at(int c) const {
+    if constexpr (sizeof(T) == 2)
+      return fmaxf(bf2f(p[c]), -INFINITY) + 0.f;
+    else
+      return fmaxf(p[c], -INFINITY) + 0.f;
+  }
+};
+
+// The order of a row's entries (largest value first, ties to the lowest column) as 52-bit keys,
+// greater for an earlier entry: the value's order key over the complement of the column.
+constexpr int kColumnBits = 20;
+constexpr uint32_t kColumnMask = (1u << kColumnBits) - 1;   // columns 0 .. 2^20 - 1
+
+__device__ __forceinline__ uint64_t entry_key(float z, int c) {
+  return (uint64_t(f32_order_key(z)) << kColumnBits) | (kColumnMask - uint32_t(c));
+}
+__device__ __forceinline__ float entry_logit(uint64_t k) {
+  return f32_from_order_key(uint32_t(k >> kColumnBits));
+}
+__device__ __forceinline__ int entry_column(uint64_t k) {
+  return int(kColumnMask - (uint32_t(k) & kColumnMask));
+}
+
+// 2^t in 64 bits for t <= 0 (and the few ulps above it that rounding leaves): 2^n times the
+// exponential series of f ln 2, |f| <= 1/2, whose first dropped term is 0.35^12 / 12! = 6e-15.
+// Which entry a draw or a cut falls on is decided by sums of these; with 32-bit exponentials one
+// row in a few thousand fell on a neighbour.
+__device__ __forceinline__ double exp2_64(double t) {
+  t = fmax(t, -1100.);   // below the least double; also what an infinite difference gives
+  const double n = rint(t);
+  const double x = (t - n) * 0.69314718055994530942;
+  double p = 1. / 39916800.;
+  p = fma(p, x, 1. / 3628800.);
+  p = fma(p, x, 1. / 362880.);
+  p = fma(p, x, 1. / 40320.);
+  p = fma(p, x, 1. / 5040.);
+  p = fma(p, x, 1. / 720.);
+  p = fma(p, x, 1. / 120.);
+  p = fma(p, x, 1. / 24.);
+  p = fma(p, x, 1. / 6.);
+  p = fma(p, x, 0.5);
+  p = fma(p, x, 1.);
+  p = fma(p, x, 1.);
+  return ldexp(p, int(n));
+}
+
+// Weight e^((z - m) / T) of an entry, c2 = log2(e) / T, m >= z (both may be +inf: weight 1);
+// 0 for a masked one.
+__device__ __forceinline__ double entry_weight(float z, float m, double c2) {
+  if (z == -INFINITY) return 0.;
+  return z == m ? 1. : exp2_64((double(z) - double(m)) * c2);
+}
+
+// Sums over a workgroup of W waves in a fixed order; every thread gets the result.  `sh` holds W
+// values and is free again when the next barrier has passed.
+template <int W, typename X, typename F>
+__device__ __forceinline__ X block_fold(X v, X* sh, F f) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, kWave));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  X t = sh[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) t = f(t, sh[w]);
+  __syncthreads();
+  return t;
+}
+
+// Inclusive running sum over the workgroup's threads, in their order; `total` gets the whole.
+template <int W, typename X>
+__device__ __forceinline__ X block_scan(X v, X* sh, X& total) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const X y = __shfl_up(v, o, kWave);
+    if (lane >= o) v += y;
+  }
+  if (lane == 63) sh[wid] = v;
+  __syncthreads();
+  X before = X(0), all = X(0);
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w == wid) before = all;
+    all += sh[w];
+  }
+  __syncthreads();
+  total = all;
+  return before + v;
+}
+
+}  // namespace hdf

@@ -7,9 +7,10 @@ no fallback: if the library is missing, loading fails loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -30,7 +31,10 @@ EXPORTS = ("hdf_last_error", "hdf_version", "hdf_hc_reduce", "hdf_rope_table",
            "hdf_sample_workspace", "hdf_sample_tokens", "hdf_accept_sample_workspace",
            "hdf_accept_sample", "hdf_kl_forward_workspace", "hdf_kl_forward",
            "hdf_advance_context", "hdf_kv_write_rows", "hdf_kv_read_rows",
-           "hdf_lm_head_argmax_noalloc", "hdf_lm_head_argmax_keys", "hdf_accept_keys")
+           "hdf_lm_head_argmax_noalloc", "hdf_lm_head_argmax_keys", "hdf_accept_keys",
+           "hdf_sample_truncated_workspace", "hdf_sample_truncated",
+           "hdf_accept_truncated_workspace", "hdf_accept_truncated",
+           "hdf_top_logits_workspace", "hdf_top_logits")
 
 
 class HdfError(RuntimeError):
@@ -42,6 +46,14 @@ class HdfError(RuntimeError):
 class ReduceParams(ctypes.Structure):
     _fields_ = [("eps", ctypes.c_float), ("gate_scale", ctypes.c_float),
                 ("gate_offset", ctypes.c_float), ("per_path_norm", ctypes.c_int)]
+
+
+class TruncationParams(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
+                ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p),
+                ("rows_per_seq", ctypes.c_int)]
 
 
 class Drafter(ctypes.Structure):
@@ -131,6 +143,21 @@ def lib() -> ctypes.CDLL:
     L.hdf_kl_forward.restype = _I
     L.hdf_kl_forward.argtypes = [_P, _I, _P, _F, _P, _I, _I, _I, _P, _I64, _I, _P, _I, _I, _F, _F,
                                  _P, _P, _P, _P, _SZ, _P]
+    L.hdf_sample_truncated_workspace.restype = _SZ
+    L.hdf_sample_truncated_workspace.argtypes = [_I64, _I, _I]
+    L.hdf_sample_truncated.restype = _I
+    L.hdf_sample_truncated.argtypes = [_P, _I64, _I, _I64, _I, ctypes.POINTER(TruncationParams), _P,
+                                       _P, _P, _P, _P, _P, _P, _SZ, _P]
+    L.hdf_accept_truncated_workspace.restype = _SZ
+    L.hdf_accept_truncated_workspace.argtypes = [_I, _I, _I, _I]
+    L.hdf_accept_truncated.restype = _I
+    L.hdf_accept_truncated.argtypes = [_P, _I, _P, _I, _I64, _P, _P, _P, _P, _I, _I, _I, _I,
+                                       ctypes.POINTER(TruncationParams), _P, _P, _P, _P, _P, _P,
+                                       _SZ, _P]
+    L.hdf_top_logits_workspace.restype = _SZ
+    L.hdf_top_logits_workspace.argtypes = [_I64, _I, _I, _I]
+    L.hdf_top_logits.restype = _I
+    L.hdf_top_logits.argtypes = [_P, _I64, _I, _I64, _I, _I, _F, _P, _P, _P, _P, _SZ, _P]
     _lib = L
     return L
 
@@ -361,6 +388,189 @@ def kl_forward(H_pos: torch.Tensor, w_lm: "PackedWeight", student_logits: torch.
                                 _ptr(kl), _ptr(ce), _ptr(loss), _ptr(ws), ws.numel(),
                                 _stream(stream)))
     return kl, ce, loss
+
+
+# --------------------------------------------------------------- truncated distributions
+
+class Truncation(NamedTuple):
+    """The cut of every row: entries kept, the last kept entry (-inf, -1 where every unmasked
+    one is), and the kept entries' log-sum-exp at the row's temperature."""
+    kept: torch.Tensor        # [rows] int32
+    cut_logit: torch.Tensor   # [rows] fp32
+    cut_index: torch.Tensor   # [rows] int32
+    lse: torch.Tensor         # [rows] fp64
+
+
+def _place(t: torch.Tensor, stream):
+    """Makes the tensor's device, and the given stream, current: outputs and workspaces are then
+    allocated for the stream that uses them, and nothing is launched on another device."""
+    if not t.is_cuda:
+        raise ValueError("libhdf takes device tensors")
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        return torch.cuda.stream(stream)
+    if t.device.index != torch.cuda.current_device():
+        return torch.cuda.device(t.device)
+    return contextlib.nullcontext()
+
+
+def _same_device(t: torch.Tensor, *others):
+    for o in others:
+        if o is not None and (not o.is_cuda or o.device != t.device):
+            raise ValueError("all tensors must be on one device")
+
+
+def _rows_of(t: torch.Tensor, what: str):
+    """(rows, columns, row stride) of a matrix of logits with unit column stride."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [rows, vocab] with unit column stride")
+    rows, V = t.shape
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), V)
+    if ld < V:
+        raise ValueError(f"{what} must not have overlapping rows")
+    return rows, V, ld
+
+
+def _scratch(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
+    if ws is None or ws.numel() * ws.element_size() < need:
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=like.device)
+    _same_device(like, ws)
+    return ws
+
+
+def _truncation_params(like, n, rows_per_seq, temperature, top_k, top_p, min_p):
+    """The C struct of settings that are numbers or tensors of one entry a sequence."""
+    p = TruncationParams(1.0, 0, 1.0, 0.0, None, None, None, None, rows_per_seq)
+    for value, one, many, dtype in (
+            (temperature, "temperature", "temperatures", torch.float32),
+            (top_k, "top_k", "top_ks", torch.int32), (top_p, "top_p", "top_ps", torch.float32),
+            (min_p, "min_p", "min_ps", torch.float32)):
+        if torch.is_tensor(value):
+            _typed(value, dtype, n, one)
+            _dev(value)
+            _same_device(like, value)
+            setattr(p, many, value.data_ptr())
+        elif value is not None:
+            setattr(p, one, value)
+    return p
+
+
+def sample_truncated(logits: torch.Tensor, uniforms: Optional[torch.Tensor] = None, *,
+                     temperature: Union[float, torch.Tensor] = 1.0,
+                     top_k: Union[int, torch.Tensor] = 0, top_p: Union[float, torch.Tensor] = 1.0,
+                     min_p: Union[float, torch.Tensor] = 0.0, rows_per_seq: int = 1,
+                     out=None, ws: Optional[torch.Tensor] = None, stream=None):
+    """hdf_sample_truncated: logits [rows, vocab] fp32 or bf16 (any row stride), uniforms [rows]
+    fp32 in [0, 1) or None -> (tokens [rows] int32 or None, Truncation).  Each setting is a number
+    or a tensor of one entry a sequence, a sequence being rows_per_seq consecutive rows.  out: a
+    preallocated (tokens, Truncation)."""
+    rows, V, ld = _rows_of(logits, "logits")
+    if rows_per_seq < 1:
+        raise ValueError("rows_per_seq must be positive")
+    p = _truncation_params(logits, -(-rows // rows_per_seq), rows_per_seq, temperature, top_k,
+                           top_p, min_p)
+    with _place(logits, stream):
+        if out is None:
+            i32 = dict(dtype=torch.int32, device=logits.device)
+            tok = torch.empty(rows, **i32) if uniforms is not None else None
+            cut = Truncation(torch.empty(rows, **i32),
+                             torch.empty(rows, dtype=torch.float32, device=logits.device),
+                             torch.empty(rows, **i32),
+                             torch.empty(rows, dtype=torch.float64, device=logits.device))
+        else:
+            tok, cut = out[0], Truncation(*out[1])
+            tok = tok if uniforms is not None else None
+        _typed(uniforms, torch.float32, rows, "uniforms")
+        _typed(tok, torch.int32, rows, "tokens")
+        for t, dtype, what in zip(cut, (torch.int32, torch.float32, torch.int32, torch.float64),
+                                  Truncation._fields):
+            _typed(t, dtype, rows, what)
+        _dev(uniforms, tok, *cut)
+        _same_device(logits, uniforms, tok, *cut)
+        dt = _dt(logits)
+        ws = _scratch(ws, int(lib().hdf_sample_truncated_workspace(rows, V, dt)), logits)
+        _check(lib().hdf_sample_truncated(
+            _ptr(logits), rows, V, ld, dt, ctypes.byref(p), _ptr(uniforms), _ptr(tok),
+            _ptr(cut.kept), _ptr(cut.cut_logit), _ptr(cut.cut_index), _ptr(cut.lse), _ptr(ws),
+            ws.numel() * ws.element_size(), _stream()))
+    return tok, cut
+
+
+def accept_truncated(draft: torch.Tensor, draft_logits: torch.Tensor, draft_cut,
+                     target_logits: torch.Tensor, uniforms: torch.Tensor, *, K: int,
+                     draft_stride: int, ld: Optional[int] = None,
+                     temperature: Union[float, torch.Tensor] = 1.0,
+                     top_k: Union[int, torch.Tensor] = 0, top_p: Union[float, torch.Tensor] = 1.0,
+                     min_p: Union[float, torch.Tensor] = 0.0, out=None,
+                     ws: Optional[torch.Tensor] = None, stream=None):
+    """hdf_accept_truncated.  draft, draft_logits and draft_cut (a Truncation) are views that start
+    at the first sequence's first draft: draft i of sequence s is element s*draft_stride + i and
+    row s*draft_stride + i (of a block's outputs: tokens[1:], logits[1:] and so on, with
+    draft_stride = B and K = B - 1); target_logits [n_seq, K+1, vocab], uniforms [n_seq, K+1]
+    fp32.  Each setting is a number or a tensor of one entry a sequence.  Returns (accept_len,
+    next_anchor, commit_offsets, commit_tokens); out: the same, preallocated."""
+    if target_logits.dim() != 3 or target_logits.shape[1] != K + 1:
+        raise ValueError("target_logits must be [n_seq, K+1, vocab]")
+    n_seq, _, V = target_logits.shape
+    need = (n_seq - 1) * draft_stride + K if n_seq > 0 and K > 0 else 0
+    d_rows, d_V, d_ld = _rows_of(draft_logits, "draft_logits")
+    if need and (d_rows < need or d_V != V or (ld is not None and ld != d_ld and d_rows > 1)):
+        raise ValueError("draft_logits must hold a row of the target's vocabulary for every draft, "
+                         "ld apart")
+    cut = Truncation(*draft_cut)
+    _typed(draft, torch.int32, need, "draft")
+    for t, dtype, what in zip(cut[1:], (torch.float32, torch.int32, torch.float64),
+                              Truncation._fields[1:]):
+        _typed(t, dtype, need, what)
+    _typed(uniforms, torch.float32, n_seq * (K + 1), "uniforms")
+    p = _truncation_params(target_logits, n_seq, 1, temperature, top_k, top_p, min_p)
+    with _place(target_logits, stream):
+        if out is None:
+            i32 = dict(dtype=torch.int32, device=target_logits.device)
+            out = (torch.empty(n_seq, **i32), torch.empty(n_seq, **i32),
+                   torch.empty(n_seq + 1, **i32), torch.empty(max(1, n_seq * (K + 1)), **i32))
+        acc, anc, offs, toks = out
+        for t, k, what in ((acc, n_seq, "accept_len"), (anc, n_seq, "next_anchor"),
+                           (offs, n_seq + 1, "commit_offsets"),
+                           (toks, n_seq * (K + 1), "commit_tokens")):
+            _typed(t, torch.int32, k, what)
+        _dev(draft, *cut[1:], target_logits, uniforms, acc, anc, offs, toks)
+        _same_device(target_logits, draft, draft_logits, *cut[1:], uniforms, acc, anc, offs, toks)
+        dt = _dt(target_logits)
+        ws = _scratch(ws, int(lib().hdf_accept_truncated_workspace(n_seq, K, V, dt)), target_logits)
+        _check(lib().hdf_accept_truncated(
+            _ptr(draft), draft_stride, _ptr(draft_logits), _dt(draft_logits), d_ld,
+            _ptr(cut.cut_logit), _ptr(cut.cut_index), _ptr(cut.lse), _ptr(target_logits), dt, n_seq,
+            K, V, ctypes.byref(p), _ptr(uniforms), _ptr(acc), _ptr(anc), _ptr(offs), _ptr(toks),
+            _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    return acc, anc, offs, toks
+
+
+def top_logits(logits: torch.Tensor, K: int, *, temperature: float = 1.0, want_rest: bool = True,
+               out=None, ws: Optional[torch.Tensor] = None, stream=None):
+    """hdf_top_logits: logits [rows, vocab] fp32 or bf16 (any row stride) -> (ids [rows, K] int32,
+    values [rows, K] fp32, rest [rows] fp32 or None): the K largest logits of every row in order,
+    and the log-sum-exp of the others at the temperature.  out: the same, preallocated."""
+    rows, V, ld = _rows_of(logits, "logits")
+    with _place(logits, stream):
+        if out is None:
+            dev = logits.device
+            out = (torch.empty((rows, max(K, 0)), dtype=torch.int32, device=dev),
+                   torch.empty((rows, max(K, 0)), dtype=torch.float32, device=dev),
+                   torch.empty(rows, dtype=torch.float32, device=dev) if want_rest else None)
+        ids, values, rest = out
+        _typed(ids, torch.int32, rows * K, "ids")
+        _typed(values, torch.float32, rows * K, "values")
+        _typed(rest, torch.float32, rows, "rest")
+        _dev(ids, values, rest)
+        _same_device(logits, ids, values, rest)
+        dt = _dt(logits)
+        ws = _scratch(ws, int(lib().hdf_top_logits_workspace(rows, V, K, dt)), logits)
+        _check(lib().hdf_top_logits(_ptr(logits), rows, V, ld, dt, K, float(temperature), _ptr(ids),
+                                    _ptr(values), _ptr(rest), _ptr(ws),
+                                    ws.numel() * ws.element_size(), _stream()))
+    return ids, values, rest
 
 
 # ----------------------------------------------------------------------------- weights
