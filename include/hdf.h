@@ -12,6 +12,9 @@
  *       hdf_sample_truncated, hdf_accept_truncated: with top-k, top-p and min-p as well;
  *       hdf_advance_context: the committed positions become the next round's context)
  *
+ * For training: hdf_kl_forward, and hdf_distill_forward / hdf_distill_backward against a teacher's
+ * stored top logits (hdf_top_logits).
+ *
  * Conventions shared by every call:
  *   - Tensor arguments are DEVICE pointers unless marked "host".  Tensors are dense,
  *     row-major, caller-allocated and caller-owned.  The library never allocates or
@@ -582,6 +585,61 @@ size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype)
 hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,
                           int K, float temperature, int32_t* ids, float* values, float* rest,
                           void* ws, size_t ws_bytes, hdf_stream_t stream);
+
+/* ------------------------------------------------------------------------------
+ * 8. Distillation from a teacher's stored top logits, forward and backward (section 6's
+ * objective with the teacher's distribution read instead of computed, and its gradient).
+ *
+ * For slot k = 1..P of block s the teacher's distribution p is over its K listed tokens and,
+ * where teacher_rest is given, one bucket of all others:
+ *     p = softmax(t_1 / T, ..., t_K / T [, rest])
+ * (rest is at temperature T already, as hdf_top_logits stores it).  A listed id outside
+ * [0, vocab) or equal to an earlier one of the row is no entry.  q = softmax(z / T), z the
+ * student's logits of the slot, and q_rest the sum of q over the unlisted tokens:
+ *     kl[s][k-1] = sum_i p_i (log p_i - log q_i) [+ p_rest (log p_rest - log q_rest)]
+ *     ce[s][k-1] = -log softmax(z)[labels[s][k-1]]    (k = 1..B-1; 0 where the label is outside
+ *                                                      [0, vocab): the slot has none)
+ *     loss = { L_KL = T^2/P * mean_s sum_k kl, L_CE = mean of ce over the labelled slots,
+ *              L_CE + alpha L_KL }
+ * A slot whose teacher has no entry of finite logit has kl = 0 and no gradient.  A masked (-inf)
+ * student logit has gradient 0 where it is not listed; one that the teacher gives mass makes kl
+ * infinite.  A NaN among a slot's student or teacher logits makes its losses and gradients NaN.
+ * Sums are 64-bit, losses rounded once.
+ * ----------------------------------------------------------------------------*/
+/* Bytes of the record that the forward pass leaves for the backward (0 on invalid arguments). */
+size_t hdf_distill_saved_bytes(int n_seq, int B, int P, int K);
+/* Workspace bytes of hdf_distill_forward (0 on invalid arguments). */
+size_t hdf_distill_workspace(int n_seq, int B, int vocab, hdf_dtype dtype);
+/* student_logits  dtype, slot k of block s at row s*B + k, row stride ld, any alignment of the
+ *                 element
+ * teacher_ids     [n_seq][P][K] int32; teacher_logits [n_seq][P][K] fp32
+ * teacher_rest    [n_seq][P] fp32 or NULL (p over the listed tokens alone)
+ * labels          [n_seq][B-1] int32 or NULL (no ce; L_CE = 0)
+ * kl              [n_seq][P] fp32 (out); ce [n_seq][B-1] fp32 (out, NULL without labels);
+ * loss            [3] fp32 (out)
+ * saved           hdf_distill_saved_bytes(...) bytes (out), 256-byte aligned
+ * ws, ws_bytes    at least hdf_distill_workspace(...) bytes, 256-byte aligned; its contents on
+ *                 entry do not matter.
+ * Limits: 2 <= B <= 1025; 1 <= P <= B-1; 1 <= K <= 1024; n_seq * B <= 65535; 1 <= vocab <= 2^20;
+ *         2^-100 <= temperature <= 2^100. */
+hdf_status hdf_distill_forward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
+                               int n_seq, int B, int P, const int32_t* teacher_ids,
+                               const float* teacher_logits, const float* teacher_rest, int K,
+                               const int32_t* labels, float temperature, float alpha, float* kl,
+                               float* ce, float* loss, void* saved, void* ws, size_t ws_bytes,
+                               hdf_stream_t stream);
+/* Gradient of grad_loss . loss + grad_kl . kl + grad_ce . ce with regard to every student logit.
+ * The arguments that the forward pass had too are the same; saved is what it left.
+ * grad_loss [3], grad_kl [n_seq][P], grad_ce [n_seq][B-1]  fp32, each may be NULL (zeros)
+ * d_logits  dtype (out), rows as student_logits', row stride ldd; every row's vocab columns are
+ *           written (zeros where a slot has no loss, slot 0 among them)
+ * Gradients are formed in fp32 and rounded once. */
+hdf_status hdf_distill_backward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
+                                int n_seq, int B, int P, const int32_t* teacher_ids, int K,
+                                const int32_t* labels, float temperature, float alpha,
+                                const void* saved, const float* grad_loss, const float* grad_kl,
+                                const float* grad_ce, void* d_logits, int64_t ldd,
+                                hdf_stream_t stream);
 
 #ifdef __cplusplus
 }

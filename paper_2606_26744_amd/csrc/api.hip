@@ -1079,6 +1079,101 @@ hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t l
   return ok();
 }
 
+// ---------------------------------------------------------- distillation from top logits
+}  // extern "C"
+
+namespace {
+
+bool distill_shape_ok(int n_seq, int B, int P, int K, int vocab) {
+  return n_seq >= 0 && B >= 2 && B <= 1025 && P >= 1 && P <= B - 1 && K >= 1 && K <= 1024 &&
+         vocab >= 1 && vocab <= kMaxTruncVocab && int64_t(n_seq) * B <= 65535;
+}
+
+hdf_status check_distill(const char* fn, const void* z, int64_t ld, hdf_dtype dtype, int vocab,
+                         int n_seq, int B, int P, const int32_t* ids, int K, float T, float alpha) {
+  if (n_seq < 0) return fail(HDF_E_INVALID, "%s: n_seq < 0", fn);
+  if (B < 2 || B > 1025) return fail(HDF_E_INVALID, "%s: B=%d outside [2, 1025]", fn, B);
+  if (P < 1 || P > B - 1) return fail(HDF_E_INVALID, "%s: P=%d outside [1, B-1]", fn, P);
+  if (K < 1 || K > 1024) return fail(HDF_E_INVALID, "%s: K=%d outside [1, 1024]", fn, K);
+  const hdf_status st = check_rows(fn, int64_t(n_seq) * B, vocab, ld, dtype, z);
+  if (st != HDF_OK) return st;
+  if (!(T >= 7.8886091e-31f && T <= 1.2676506e30f))
+    return fail(HDF_E_INVALID, "%s: temperature outside [2^-100, 2^100]", fn);
+  if (!(alpha > -INFINITY && alpha < INFINITY)) return fail(HDF_E_INVALID, "%s: alpha must be finite", fn);
+  if (n_seq > 0 && ids == nullptr) return fail(HDF_E_INVALID, "%s: null teacher_ids", fn);
+  return HDF_OK;
+}
+
+hdf::DistArgs distill_args(const void* z, int64_t ld, int vocab, int n_seq, int B, int P,
+                           const int32_t* ids, int K, const int32_t* labels, float T, float alpha) {
+  hdf::DistArgs a{};
+  a.z = z; a.ld = ld; a.V = vocab; a.n_seq = n_seq; a.B = B; a.P = P; a.K = K; a.ids = ids;
+  a.labels = labels; a.t = T; a.c2 = float(1.4426950408889634 / double(T)); a.alpha = alpha;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hdf_distill_saved_bytes(int n_seq, int B, int P, int K) {
+  return distill_shape_ok(n_seq, B, P, K, 1) ? hdf::distill_saved_bytes(n_seq, B, P, K) : 0;
+}
+
+size_t hdf_distill_workspace(int n_seq, int B, int vocab, hdf_dtype dtype) {
+  if (!distill_shape_ok(n_seq, B, 1, 1, vocab) || (dtype != HDF_F32 && dtype != HDF_BF16)) return 0;
+  return hdf::distill_ws_bytes(dtype == HDF_BF16, n_seq, B, vocab);
+}
+
+hdf_status hdf_distill_forward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
+                               int n_seq, int B, int P, const int32_t* teacher_ids,
+                               const float* teacher_logits, const float* teacher_rest, int K,
+                               const int32_t* labels, float temperature, float alpha, float* kl,
+                               float* ce, float* loss, void* saved, void* ws, size_t ws_bytes,
+                               hdf_stream_t stream) {
+  hdf_status st = check_distill("distill_forward", student_logits, ld, dtype, vocab, n_seq, B, P,
+                                teacher_ids, K, temperature, alpha);
+  if (st != HDF_OK || n_seq == 0) return st == HDF_OK ? ok() : st;
+  if (teacher_logits == nullptr || kl == nullptr || loss == nullptr || saved == nullptr ||
+      (labels == nullptr) != (ce == nullptr))
+    return fail(HDF_E_INVALID, "distill_forward: null pointer");
+  if ((reinterpret_cast<uintptr_t>(saved) & 255u) != 0)
+    return fail(HDF_E_INVALID, "distill_forward: saved must be 256-byte aligned");
+  st = check_ws("distill_forward", ws, ws_bytes, hdf_distill_workspace(n_seq, B, vocab, dtype));
+  if (st != HDF_OK) return st;
+  hdf::DistArgs a = distill_args(student_logits, ld, vocab, n_seq, B, P, teacher_ids, K, labels,
+                                 temperature, alpha);
+  a.tl = teacher_logits; a.rest = teacher_rest; a.kl = kl; a.ce = ce; a.loss = loss;
+  const hipError_t e = hdf::launch_distill_forward(dtype == HDF_BF16, a, saved, ws,
+                                                   reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "distill_forward launch");
+  return ok();
+}
+
+hdf_status hdf_distill_backward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
+                                int n_seq, int B, int P, const int32_t* teacher_ids, int K,
+                                const int32_t* labels, float temperature, float alpha,
+                                const void* saved, const float* grad_loss, const float* grad_kl,
+                                const float* grad_ce, void* d_logits, int64_t ldd,
+                                hdf_stream_t stream) {
+  hdf_status st = check_distill("distill_backward", student_logits, ld, dtype, vocab, n_seq, B, P,
+                                teacher_ids, K, temperature, alpha);
+  if (st == HDF_OK) st = check_rows("distill_backward", int64_t(n_seq) * B, vocab, ldd, dtype, d_logits);
+  if (st != HDF_OK || n_seq == 0) return st == HDF_OK ? ok() : st;
+  if (saved == nullptr) return fail(HDF_E_INVALID, "distill_backward: null saved");
+  if ((reinterpret_cast<uintptr_t>(saved) & 255u) != 0)
+    return fail(HDF_E_INVALID, "distill_backward: saved must be 256-byte aligned");
+  if (d_logits == student_logits)
+    return fail(HDF_E_INVALID, "distill_backward: d_logits must not be the logits");
+  hdf::DistArgs a = distill_args(student_logits, ld, vocab, n_seq, B, P, teacher_ids, K, labels,
+                                 temperature, alpha);
+  const hdf::DistGrad g{grad_loss, grad_kl, grad_ce, d_logits, ldd};
+  const hipError_t e = hdf::launch_distill_backward(dtype == HDF_BF16, a, g, saved,
+                                                    reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "distill_backward launch");
+  return ok();
+}
+
 // ---------------------------------------------------------- LM head without a workspace
 // For callers that cannot allocate: the per-row argmax keys live in this file-scope device
 // array (one copy per GPU, held until the process ends) instead of a workspace.  In host

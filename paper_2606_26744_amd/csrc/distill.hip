@@ -1,0 +1,409 @@
+// Distillation from a teacher's stored top logits, forward and backward.  For draft slot k <= P of
+// a block, p is the softmax at temperature T over the teacher's listed tokens S and, if given, the
+// bucket of all others (whose log-sum-exp was stored with them); q = softmax(z / T) the student's:
+//     kl = sum_S p_i (log p_i - log q_i) + p_r (log p_r - log q_r),   q_r = sum_{v not in S} q_v
+//     T dkl/dz_v = q_v - p_v in S,   q_v (1 - p_r / q_r) outside (q_v without the bucket)
+//     ce = log sum_v e^z_v - z_label,   dce/dz_v = softmax(z)_v - [v = label]
+// Forward: one pass over the logits, whose workgroups keep a part of a row in registers between its
+// greatest value and the sums; the rows' losses; their means.  Backward: one pass that forms every
+// gradient from the row's statistics and then overwrites the few listed tokens'.
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace hdf {
+
+constexpr int kDistThreads = 256;
+constexpr int kDistWaves = kDistThreads / kWave;
+constexpr int kDistElems = 32;                              // of a part, a thread
+constexpr int kDistPart = kDistThreads * kDistElems;        // columns of a part
+constexpr int kMaxTop = 1024;                               // K at most
+constexpr int kHashSlots = 2 * kMaxTop;
+
+// What a part of a row adds: its greatest logit m and, relative to it, the sums of e^((z - m) / T)
+// over all columns and over the unlisted ones, and of e^(z - m).
+struct DistPart {
+  float m;
+  double st, out, s1;
+};
+
+// A supervised slot's statistics for the backward pass.
+struct DistRow {
+  float m, inv_t, inv_1;   // greatest logit; one over the sums at temperatures T and 1
+  float outside;           // 1 - p_r / q_r, the factor of unlisted tokens (1 without the bucket)
+  int kl, ce;              // whether the slot has either loss
+};
+
+// Saved between the passes: the number of labelled slots, the slots' statistics, p of the listed
+// tokens (-1: no token, or one that stood before it in the list).
+struct DistSaved {
+  int* labelled;
+  DistRow* rows;
+  float* p;
+};
+static size_t al256(size_t x) { return (x + 255) / 256 * 256; }
+static DistSaved saved_of(void* saved, int n_seq, int B) {
+  char* s = static_cast<char*>(saved);
+  return {reinterpret_cast<int*>(s), reinterpret_cast<DistRow*>(s + 256),
+          reinterpret_cast<float*>(s + 256 + al256(size_t(n_seq) * (B - 1) * sizeof(DistRow)))};
+}
+size_t distill_saved_bytes(int n_seq, int B, int P, int K) {
+  return 256 + al256(size_t(n_seq) * (B - 1) * sizeof(DistRow)) + al256(size_t(n_seq) * P * K * 4);
+}
+
+static int dist_parts(bool bf16, int V) {
+  const int N = bf16 ? 8 : 4;
+  return ((V + 2 * N - 2) / N * N + kDistPart - 1) / kDistPart;
+}
+size_t distill_ws_bytes(bool bf16, int n_seq, int B, int V) {
+  return al256(size_t(n_seq) * (B - 1) * dist_parts(bf16, V) * sizeof(DistPart));
+}
+
+// Workgroup (part, slot): the slots are k = 1 .. slots of every block.
+template <typename T>
+__global__ void __launch_bounds__(kDistThreads)
+distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
+  constexpr int N = LogitRow<T>::N, G = kDistElems / N;
+  __shared__ uint32_t listed[kDistPart / 32];
+  __shared__ float shf[kDistWaves];
+  __shared__ double shd[kDistWaves];
+  const int part = blockIdx.x;
+  const int64_t i = blockIdx.y, s = i / slots;
+  const int k = int(i - s * slots) + 1;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + (s * a.B + k) * a.ld, a.V);
+  const int j0 = part * (kDistPart / N), nv = r.vectors();
+  const bool soft = k <= a.P, bucket = soft && a.rest != nullptr;
+  float x[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int j = j0 + g * kDistThreads + int(threadIdx.x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+    if (j < nv) r.load_raw(j, x[g]);
+  }
+  if (bucket) {
+    for (int w = threadIdx.x; w < kDistPart / 32; w += kDistThreads) listed[w] = 0;
+    __syncthreads();
+    const int32_t* ids = a.ids + (s * a.P + k - 1) * a.K;
+    const int c0 = r.column(j0);
+    for (int t = threadIdx.x; t < a.K; t += kDistThreads) {
+      const int id = ids[t];
+      const int b = id - c0;
+      if (id >= 0 && id < a.V && b >= 0 && b < kDistPart) atomicOr(&listed[b >> 5], 1u << (b & 31));
+    }
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, x[g][e]);
+  m = block_fold<kDistWaves>(m, shf, [](float u, float v) { return fmaxf(u, v); });
+  const float ref = m == -INFINITY ? 0.f : m;
+  float st = 0.f, out = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int b = (g * kDistThreads + int(threadIdx.x)) * N;
+    const uint32_t in = bucket ? listed[b >> 5] >> (b & 31) : 0u;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float d = x[g][e] - ref;
+      if (soft) {
+        const float w = __builtin_amdgcn_exp2f(d * a.c2);
+        st += w;
+        out += (in >> e) & 1u ? 0.f : w;
+      }
+      if (a.labels != nullptr && !(soft && a.t == 1.f)) s1 += __builtin_amdgcn_exp2f(d * 1.44269504f);
+    }
+  }
+  auto add = [](double u, double v) { return u + v; };
+  DistPart o;
+  o.m = m;
+  o.st = block_fold<kDistWaves>(double(st), shd, add);
+  o.out = block_fold<kDistWaves>(double(out), shd, add);
+  o.s1 = soft && a.t == 1.f ? o.st : block_fold<kDistWaves>(double(s1), shd, add);
+  if (threadIdx.x == 0) parts[i * gridDim.x + part] = o;
+}
+
+// One workgroup a slot: the parts joined, the teacher's distribution, the losses.
+template <typename T>
+__global__ void __launch_bounds__(kDistThreads)
+distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, int n_parts,
+                   DistSaved sv) {
+  __shared__ int hash_id[kHashSlots], hash_at[kHashSlots];
+  __shared__ double sh[kDistWaves];
+  const int64_t i = blockIdx.x, s = i / slots;
+  const int k = int(i - s * slots) + 1, tid = threadIdx.x;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + (s * a.B + k) * a.ld, a.V);
+  auto add = [](double u, double v) { return u + v; };
+  auto most = [](double u, double v) { return fmax(u, v); };
+  const DistPart* pt = parts + i * n_parts;
+  double m = -INFINITY;
+  for (int j = tid; j < n_parts; j += kDistThreads) m = fmax(m, double(pt[j].m));
+  m = block_fold<kDistWaves>(m, sh, most);
+  const double ref = m == -INFINITY ? 0. : m;
+  const double c2 = 1.4426950408889634074 / double(a.t);
+  double st = 0., out = 0., s1 = 0.;
+  for (int j = tid; j < n_parts; j += kDistThreads) {
+    const DistPart o = pt[j];
+    const double d = o.m == -INFINITY ? -INFINITY : double(o.m) - ref;
+    st += o.st * exp2_64(d * c2);
+    out += o.out * exp2_64(d * c2);
+    s1 += o.s1 * exp2_64(d * 1.4426950408889634074);
+  }
+  st = block_fold<kDistWaves>(st, sh, add);
+  out = block_fold<kDistWaves>(out, sh, add);
+  s1 = block_fold<kDistWaves>(s1, sh, add);
+  // A row masked throughout has no softmax: its factors are 0, as its exponentials.
+  DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), 1.f, 0, 0};
+
+  if (k <= a.P) {
+    const int64_t q = s * a.P + k - 1;
+    const int32_t* ids = a.ids + q * a.K;
+    const float* tl = a.tl + q * a.K;
+    float* ps = sv.p + q * a.K;
+    // A token's first place in the list holds: a table of tokens with their least place.
+    for (int h = tid; h < kHashSlots; h += kDistThreads) {
+      hash_id[h] = -1;
+      hash_at[h] = kMaxTop;
+    }
+    __syncthreads();
+    auto find = [&](int id) {
+      uint32_t h = (uint32_t(id) * 2654435761u) >> 21;   // 11 bits: kHashSlots
+      for (;;) {
+        const int was = atomicCAS(&hash_id[h], -1, id);
+        if (was == -1 || was == id) return int(h);
+        h = (h + 1) & (kHashSlots - 1);
+      }
+    };
+    for (int t = tid; t < a.K; t += kDistThreads) {
+      const int id = ids[t];
+      if (id >= 0 && id < a.V) atomicMin(&hash_at[find(id)], t);
+    }
+    __syncthreads();
+    const double inv_t = 1. / double(a.t);
+    const double lr = a.rest != nullptr ? double(a.rest[q]) : -INFINITY;
+    auto holds = [&](int t) {
+      const int id = ids[t];
+      return id >= 0 && id < a.V && hash_at[find(id)] == t;
+    };
+    double top = tid == 0 ? lr : -INFINITY, bad = tid == 0 && lr != lr ? lr : 0.;
+    for (int t = tid; t < a.K; t += kDistThreads)
+      if (holds(t)) {
+        const double l = double(tl[t]) * inv_t;
+        top = fmax(top, l);
+        bad += l != l ? l : 0.;
+      }
+    top = block_fold<kDistWaves>(top, sh, most);
+    bad = block_fold<kDistWaves>(bad, sh, add);
+    double kl = 0.;
+    if (top > -INFINITY || bad != 0.) {   // a teacher with some mass, or with a NaN to pass on
+      const double er = lr == -INFINITY ? 0. : exp(lr - top);
+      double sum = tid == 0 ? er : 0.;
+      for (int t = tid; t < a.K; t += kDistThreads)
+        if (holds(t)) sum += exp(double(tl[t]) * inv_t - top);
+      sum = block_fold<kDistWaves>(sum, sh, add);
+      const double log_sum = log(sum), log_st = log(st);
+      for (int t = tid; t < a.K; t += kDistThreads) {
+        float stored = -1.f;
+        if (holds(t)) {
+          const double l = double(tl[t]) * inv_t - top, p = exp(l) / sum;
+          const double z = double(r.raw(ids[t]));
+          const double lq = z == -INFINITY ? -INFINITY : (z - ref) * inv_t - log_st;
+          kl += p == 0. ? 0. : p * (l - log_sum - lq);
+          stored = float(p);
+        }
+        ps[t] = stored;
+      }
+      if (tid == 0 && er != 0.) {
+        const double p = er / sum;
+        const double lq = out == 0. ? -INFINITY : log(out) - log_st;
+        kl += p * (lr - top - log_sum - lq);
+        if (out != 0.) row.outside = float(1. - p * st / out);
+      }
+      kl = block_fold<kDistWaves>(kl, sh, add) + bad;
+      row.kl = 1;
+    } else {
+      for (int t = tid; t < a.K; t += kDistThreads) ps[t] = -1.f;
+    }
+    if (tid == 0) a.kl[q] = float(kl);
+  }
+  if (tid != 0) return;
+  if (a.labels != nullptr) {
+    const int64_t q = s * (a.B - 1) + k - 1;
+    const int label = a.labels[q];
+    double ce = 0.;
+    if (label >= 0 && label < a.V) {
+      const double z = double(r.raw(label));
+      ce = z == -INFINITY ? INFINITY : ref + log(s1) - z;
+      row.ce = 1;
+    }
+    a.ce[q] = float(ce);
+  }
+  sv.rows[s * (a.B - 1) + k - 1] = row;
+}
+
+// loss = { L_KL = T^2 / P * mean over blocks of the sum of kl, L_CE = mean ce of the labelled
+// slots, L_CE + alpha L_KL }.
+constexpr int kLossThreads = 1024;
+
+__global__ void __launch_bounds__(kLossThreads)
+distill_loss_kernel(DistArgs a, DistSaved sv) {
+  constexpr int W = kLossThreads / kWave;
+  __shared__ double sh[W];
+  auto add = [](double u, double v) { return u + v; };
+  double kl = 0., ce = 0., n = 0.;
+  for (int i = threadIdx.x; i < a.n_seq * a.P; i += kLossThreads) kl += double(a.kl[i]);
+  if (a.labels != nullptr)
+    for (int i = threadIdx.x; i < a.n_seq * (a.B - 1); i += kLossThreads) {
+      ce += double(a.ce[i]);
+      n += a.labels[i] >= 0 && a.labels[i] < a.V ? 1. : 0.;
+    }
+  kl = block_fold<W>(kl, sh, add);
+  ce = block_fold<W>(ce, sh, add);
+  n = block_fold<W>(n, sh, add);
+  if (threadIdx.x == 0) {
+    const double l_kl = double(a.t) * double(a.t) / a.P * kl / a.n_seq;
+    const double l_ce = n > 0. ? ce / n : 0.;
+    *sv.labelled = int(n);
+    a.loss[0] = float(l_kl);
+    a.loss[1] = float(l_ce);
+    a.loss[2] = float(l_ce + double(a.alpha) * l_kl);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_grad(T* p, float v) {
+  if constexpr (sizeof(T) == 2)
+    *p = __builtin_bit_cast(uint16_t, __bf16(v));
+  else
+    *p = v;
+}
+
+// Workgroup (part, row): the gradients of a part of a row; rows without a loss get zeros.
+template <typename T>
+__global__ void __launch_bounds__(kDistThreads)
+distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
+  constexpr int N = LogitRow<T>::N, G = kDistElems / N;
+  __shared__ int label_done;
+  const int part = blockIdx.x, tid = threadIdx.x;
+  const int64_t row = blockIdx.y, s = row / a.B;
+  const int k = int(row - s * a.B);
+  const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
+  T* d = static_cast<T*>(g.d) + row * g.ld;
+  const bool vec = LogitRow<T>(d, a.V).shift == r.shift;
+  const int j0 = part * (kDistPart / N), nv = r.vectors();
+  // Weights of the slot's losses: the means' upstream gradients and the losses' own.
+  float wk = 0.f, wc = 0.f;
+  DistRow st{0.f, 0.f, 0.f, 1.f, 0, 0};
+  int label = -1;
+  if (k >= 1) {
+    const int64_t q = s * (a.B - 1) + k - 1;
+    const float g0 = g.loss != nullptr ? g.loss[0] + a.alpha * g.loss[2] : 0.f;
+    const float g1 = g.loss != nullptr ? g.loss[1] + g.loss[2] : 0.f;
+    const bool labels = a.labels != nullptr && *sv.labelled > 0;
+    if (k <= a.P || labels) st = sv.rows[q];
+    if (k <= a.P && st.kl) {
+      wk = g0 * a.t / (float(a.P) * float(a.n_seq));
+      if (g.kl != nullptr) wk += g.kl[s * a.P + k - 1] / a.t;
+    }
+    if (labels && st.ce) {
+      wc = g1 / float(*sv.labelled);
+      if (g.ce != nullptr) wc += g.ce[q];
+      label = a.labels[q];
+    }
+  }
+  const bool soft = wk != 0.f, hard = wc != 0.f;
+  const float ct = wk * st.inv_t, co = ct * st.outside, c1 = wc * st.inv_1;
+  auto at_t = [&](float x) { return soft ? __builtin_amdgcn_exp2f((x - st.m) * a.c2) : 0.f; };
+  auto at_1 = [&](float x) { return hard ? __builtin_amdgcn_exp2f((x - st.m) * 1.44269504f) : 0.f; };
+  float x[G][N];
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    const int j = j0 + h * kDistThreads + tid;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[h][e] = -INFINITY;
+    if ((soft || hard) && j < nv) r.load_raw(j, x[h]);
+  }
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    const int j = j0 + h * kDistThreads + tid;
+    if (j >= nv) continue;
+    T o[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float et = at_t(x[h][e]);
+      const float e1 = hard && soft && a.t == 1.f ? et : at_1(x[h][e]);
+      store_grad(&o[e], (soft ? et * co : 0.f) + (hard ? e1 * c1 : 0.f));
+    }
+    const int c = r.column(j);
+    if (vec && c >= 0 && c + N <= a.V) {
+      u32x4 q;
+      __builtin_memcpy(&q, o, 16);
+      st16(d + c, q);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (c + e >= 0 && c + e < a.V) d[c + e] = o[e];
+    }
+  }
+  if (!soft && !hard) return;
+  // The listed tokens and the label of this part, over what was just stored.
+  if (tid == 0) label_done = 0;
+  __syncthreads();
+  const int c0 = max(r.column(j0), 0), c1_ = min(r.column(j0) + kDistPart, a.V);
+  if (soft) {
+    const int64_t q = s * a.P + k - 1;
+    for (int t = tid; t < a.K; t += kDistThreads) {
+      const int id = a.ids[q * a.K + t];
+      const float p = sv.p[q * a.K + t];
+      if (id < c0 || id >= c1_ || p == -1.f) continue;
+      const float z = r.raw(id);
+      float v = at_t(z) * ct - wk * p;
+      if (hard) v += at_1(z) * c1;
+      if (id == label) {
+        v -= wc;
+        label_done = 1;
+      }
+      store_grad(d + id, v);
+    }
+  }
+  __syncthreads();
+  if (tid == 0 && hard && !label_done && label >= c0 && label < c1_) {
+    const float z = r.raw(label);
+    store_grad(d + label, (soft ? at_t(z) * co : 0.f) + at_1(z) * c1 - wc);
+  }
+}
+
+template <typename T>
+static hipError_t forward(const DistArgs& a, const DistSaved& sv, int n_parts, DistPart* parts,
+                          hipStream_t s) {
+  const int slots = a.labels != nullptr ? a.B - 1 : a.P;
+  const unsigned rows = unsigned(a.n_seq) * slots;
+  hipLaunchKernelGGL((distill_part_kernel<T>), dim3(n_parts, rows), dim3(kDistThreads), 0, s, a, slots, parts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((distill_row_kernel<T>), dim3(rows), dim3(kDistThreads), 0, s, a, slots, parts, n_parts, sv);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, s, a, sv);
+  return hipGetLastError();
+}
+
+hipError_t launch_distill_forward(bool bf16, const DistArgs& a, void* saved, void* ws, hipStream_t s) {
+  const DistSaved sv = saved_of(saved, a.n_seq, a.B);
+  const int n_parts = dist_parts(bf16, a.V);
+  DistPart* parts = static_cast<DistPart*>(ws);
+  return bf16 ? forward<bf16_t>(a, sv, n_parts, parts, s) : forward<float>(a, sv, n_parts, parts, s);
+}
+
+hipError_t launch_distill_backward(bool bf16, const DistArgs& a, const DistGrad& g, const void* saved,
+                                   hipStream_t s) {
+  const DistSaved sv = saved_of(const_cast<void*>(saved), a.n_seq, a.B);
+  const dim3 grid(dist_parts(bf16, a.V), unsigned(a.n_seq) * a.B);
+  if (bf16)
+    hipLaunchKernelGGL((distill_grad_kernel<bf16_t>), grid, dim3(kDistThreads), 0, s, a, g, sv);
+  else
+    hipLaunchKernelGGL((distill_grad_kernel<float>), grid, dim3(kDistThreads), 0, s, a, g, sv);
+  return hipGetLastError();
+}
+
+}  // namespace hdf

@@ -262,6 +262,29 @@ size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V);
 hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs a, CutArgs c,
                                    int n_seq, void* ws, hipStream_t s);
 
+// ---------------------------------------------------------------- distillation (distill.hip)
+struct DistArgs {
+  const void* z;             // student logits, slot k of block s at row s * B + k, stride ld
+  int64_t ld;
+  int V, n_seq, B, P, K;
+  const int32_t* ids;        // [n_seq][P][K]
+  const float* tl;           // [n_seq][P][K]
+  const float* rest;         // [n_seq][P] or NULL
+  const int32_t* labels;     // [n_seq][B-1] or NULL
+  float t, c2, alpha;        // temperature, log2(e) / temperature
+  float *kl, *ce, *loss;
+};
+struct DistGrad {
+  const float *loss, *kl, *ce;   // upstream gradients, each may be NULL
+  void* d;                       // gradients, row stride ld
+  int64_t ld;
+};
+size_t distill_saved_bytes(int n_seq, int B, int P, int K);
+size_t distill_ws_bytes(bool bf16, int n_seq, int B, int V);
+hipError_t launch_distill_forward(bool bf16, const DistArgs& a, void* saved, void* ws, hipStream_t s);
+hipError_t launch_distill_backward(bool bf16, const DistArgs& a, const DistGrad& g, const void* saved,
+                                   hipStream_t s);
+
 // ---------------------------------------------------------------- KL forward (kl.hip)
 size_t kl_ws_bytes(int n_seq, int B, int P, int d, int V, bool bf16);
 hipError_t launch_kl_forward(bool bf16, const void* H_pos, int m, const float* gamma, float eps,

@@ -8,7 +8,8 @@ namespace hdf {
 
 // A row of V logits read 16 bytes at a time.  Rows start at any element (odd vocabularies, strides,
 // views): vector j holds columns j * N - shift .. + N - 1 and is aligned; the first and the last,
-// which reach past the row, are read element by element.
+// which reach past the row, are read element by element.  `load_raw` and `raw` give the values as
+// they are, `load` and `at` those of a row to choose from: NaN is -inf (masked), -0 is +0.
 template <typename T>
 struct LogitRow {
   static constexpr int N = 16 / int(sizeof(T));
@@ -20,8 +21,8 @@ struct LogitRow {
   }
   __device__ __forceinline__ int vectors() const { return (V + shift + N - 1) / N; }
   __device__ __forceinline__ int column(int j) const { return j * N - shift; }
-  // Vector j as fp32; columns outside the row and NaN are -inf, -0 is +0 (they are equal logits).
-  __device__ __forceinline__ void load(int j, float x[N]) const {
+  // Vector j as fp32; columns outside the row are -inf.
+  __device__ __forceinline__ void load_raw(int j, float x[N]) const {
     const int c = column(j);
     if (c >= 0 && c + N <= V) {
       const u32x4 v = ld16(p + c);
@@ -36,25 +37,21 @@ struct LogitRow {
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        x[e] = -INFINITY;
-        if (c + e >= 0 && c + e < V) {
-          if constexpr (sizeof(T) == 2)
-            x[e] = bf2f(p[c + e]);
-          else
-            x[e] = p[c + e];
-        }
-      }
+      for (int e = 0; e < N; ++e) x[e] = c + e >= 0 && c + e < V ? raw(c + e) : -INFINITY;
     }
+  }
+  __device__ __forceinline__ void load(int j, float x[N]) const {
+    load_raw(j, x);
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = fmaxf(x[e], -INFINITY) + 0.f;
   }
-  __device__ __forceinline__ float at(int c) const {
+  __device__ __forceinline__ float raw(int c) const {
     if constexpr (sizeof(T) == 2)
-      return fmaxf(bf2f(p[c]), -INFINITY) + 0.f;
+      return bf2f(p[c]);
     else
-      return fmaxf(p[c], -INFINITY) + 0.f;
+      return p[c];
   }
+  __device__ __forceinline__ float at(int c) const { return fmaxf(raw(c), -INFINITY) + 0.f; }
 };
 
 // The order of a row's entries (largest value first, ties to the lowest column) as 52-bit keys,

@@ -34,7 +34,8 @@ EXPORTS = ("hdf_last_error", "hdf_version", "hdf_hc_reduce", "hdf_rope_table",
            "hdf_lm_head_argmax_noalloc", "hdf_lm_head_argmax_keys", "hdf_accept_keys",
            "hdf_sample_truncated_workspace", "hdf_sample_truncated",
            "hdf_accept_truncated_workspace", "hdf_accept_truncated",
-           "hdf_top_logits_workspace", "hdf_top_logits")
+           "hdf_top_logits_workspace", "hdf_top_logits", "hdf_distill_saved_bytes",
+           "hdf_distill_workspace", "hdf_distill_forward", "hdf_distill_backward")
 
 
 class HdfError(RuntimeError):
@@ -158,6 +159,16 @@ def lib() -> ctypes.CDLL:
     L.hdf_top_logits_workspace.argtypes = [_I64, _I, _I, _I]
     L.hdf_top_logits.restype = _I
     L.hdf_top_logits.argtypes = [_P, _I64, _I, _I64, _I, _I, _F, _P, _P, _P, _P, _SZ, _P]
+    L.hdf_distill_saved_bytes.restype = _SZ
+    L.hdf_distill_saved_bytes.argtypes = [_I, _I, _I, _I]
+    L.hdf_distill_workspace.restype = _SZ
+    L.hdf_distill_workspace.argtypes = [_I, _I, _I, _I]
+    L.hdf_distill_forward.restype = _I
+    L.hdf_distill_forward.argtypes = [_P, _I64, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _F, _F, _P,
+                                      _P, _P, _P, _P, _SZ, _P]
+    L.hdf_distill_backward.restype = _I
+    L.hdf_distill_backward.argtypes = [_P, _I64, _I, _I, _I, _I, _I, _P, _I, _P, _F, _F, _P, _P, _P,
+                                       _P, _P, _I64, _P]
     _lib = L
     return L
 
@@ -571,6 +582,90 @@ def top_logits(logits: torch.Tensor, K: int, *, temperature: float = 1.0, want_r
                                     _ptr(values), _ptr(rest), _ptr(ws),
                                     ws.numel() * ws.element_size(), _stream()))
     return ids, values, rest
+
+
+# ------------------------------------------------------- distillation from top logits
+
+def _distill_shapes(student_logits, teacher_ids, labels, B):
+    rows, V, ld = _rows_of(student_logits, "student_logits")
+    if teacher_ids.dim() != 3:
+        raise ValueError("teacher_ids must be [n_seq, P, K]")
+    n_seq, P, K = teacher_ids.shape
+    if rows != n_seq * B:
+        raise ValueError("student_logits must hold B rows a block")
+    _typed(teacher_ids, torch.int32, n_seq * P * K, "teacher_ids")
+    _typed(labels, torch.int32, n_seq * (B - 1), "labels")
+    _dev(teacher_ids, labels)
+    _same_device(student_logits, teacher_ids, labels)
+    return n_seq, P, K, V, ld
+
+
+def distill_forward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
+                    teacher_logits: torch.Tensor, teacher_rest: Optional[torch.Tensor] = None,
+                    labels: Optional[torch.Tensor] = None, *, B: int, temperature: float = 1.0,
+                    alpha: float = 0.1, out=None, ws: Optional[torch.Tensor] = None, stream=None):
+    """hdf_distill_forward: student_logits [n_seq*B, vocab] fp32 or bf16 (any row stride),
+    teacher_ids int32 and teacher_logits fp32 [n_seq, P, K] with teacher_rest fp32 [n_seq, P] or
+    None (top_logits' outputs), labels int32 [n_seq, B-1] or None -> (kl [n_seq, P], ce
+    [n_seq, B-1] or None, loss [3] = L_KL, L_CE, L_CE + alpha L_KL, saved); `saved` is what
+    distill_backward takes.  out: the same, preallocated."""
+    n_seq, P, K, V, ld = _distill_shapes(student_logits, teacher_ids, labels, B)
+    _typed(teacher_logits, torch.float32, n_seq * P * K, "teacher_logits")
+    _typed(teacher_rest, torch.float32, n_seq * P, "teacher_rest")
+    with _place(student_logits, stream):
+        dt = _dt(student_logits)
+        need = int(lib().hdf_distill_saved_bytes(n_seq, B, P, K))
+        if out is None:
+            f32 = dict(dtype=torch.float32, device=student_logits.device)
+            out = (torch.empty((n_seq, P), **f32),
+                   torch.empty((n_seq, B - 1), **f32) if labels is not None else None,
+                   torch.zeros(3, **f32) if n_seq == 0 else torch.empty(3, **f32),
+                   torch.empty(max(need, 1), dtype=torch.uint8, device=student_logits.device))
+        kl, ce, loss, saved = out
+        _typed(kl, torch.float32, n_seq * P, "kl")
+        _typed(ce, torch.float32, n_seq * (B - 1), "ce")
+        _typed(loss, torch.float32, 3, "loss")
+        _typed(saved, torch.uint8, need, "saved")
+        _dev(teacher_logits, teacher_rest, kl, ce, loss, saved)
+        _same_device(student_logits, teacher_logits, teacher_rest, kl, ce, loss, saved)
+        ws = _scratch(ws, int(lib().hdf_distill_workspace(n_seq, B, V, dt)), student_logits)
+        _check(lib().hdf_distill_forward(
+            _ptr(student_logits), ld, dt, V, n_seq, B, P, _ptr(teacher_ids), _ptr(teacher_logits),
+            _ptr(teacher_rest), K, _ptr(labels), float(temperature), float(alpha), _ptr(kl),
+            _ptr(ce) if labels is not None else None, _ptr(loss), _ptr(saved), _ptr(ws),
+            ws.numel() * ws.element_size(), _stream()))
+    return kl, ce, loss, saved
+
+
+def distill_backward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
+                     labels: Optional[torch.Tensor], saved: torch.Tensor, *, B: int,
+                     temperature: float = 1.0, alpha: float = 0.1,
+                     grad_loss: Optional[torch.Tensor] = None,
+                     grad_kl: Optional[torch.Tensor] = None,
+                     grad_ce: Optional[torch.Tensor] = None,
+                     d_logits: Optional[torch.Tensor] = None, stream=None):
+    """hdf_distill_backward: the gradient [n_seq*B, vocab], in the logits' type, of grad_loss .
+    loss + grad_kl . kl + grad_ce . ce (fp32 tensors of the forward outputs' shapes, or None);
+    the other arguments as the forward pass had them."""
+    n_seq, P, K, V, ld = _distill_shapes(student_logits, teacher_ids, labels, B)
+    _typed(grad_loss, torch.float32, 3, "grad_loss")
+    _typed(grad_kl, torch.float32, n_seq * P, "grad_kl")
+    _typed(grad_ce, torch.float32, n_seq * (B - 1), "grad_ce")
+    _typed(saved, torch.uint8, int(lib().hdf_distill_saved_bytes(n_seq, B, P, K)), "saved")
+    with _place(student_logits, stream):
+        if d_logits is None:
+            d_logits = torch.empty((n_seq * B, V), dtype=student_logits.dtype,
+                                   device=student_logits.device)
+        d_rows, d_V, ldd = _rows_of(d_logits, "d_logits")
+        if (d_rows, d_V, d_logits.dtype) != (n_seq * B, V, student_logits.dtype):
+            raise ValueError("d_logits must have the shape and the type of student_logits")
+        _dev(saved, grad_loss, grad_kl, grad_ce)
+        _same_device(student_logits, saved, grad_loss, grad_kl, grad_ce, d_logits)
+        _check(lib().hdf_distill_backward(
+            _ptr(student_logits), ld, _dt(student_logits), V, n_seq, B, P, _ptr(teacher_ids), K,
+            _ptr(labels), float(temperature), float(alpha), _ptr(saved), _ptr(grad_loss),
+            _ptr(grad_kl), _ptr(grad_ce), _ptr(d_logits), ldd, _stream()))
+    return d_logits
 
 
 # ----------------------------------------------------------------------------- weights
