@@ -131,3 +131,61 @@ def drafter_step_sampled(handle: hdf.DrafterHandle, bufs: StepBuffers, sbufs: Sa
         ws=sbufs.accept_ws, stream=stream)
     return {"hidden": bufs.hidden, "logits": sbufs.logits, "tokens": sbufs.tokens,
             "accept_len": acc, "next_anchor": anc, "commit_offsets": offs, "commit_tokens": toks}
+
+
+class TruncatedStepBuffers:
+    """Extra device buffers of a step whose tokens are drawn from truncated distributions: fp32
+    logits [n_seq*B][V], draws and cuts of every slot, the verification's outputs, workspaces."""
+
+    def __init__(self, handle: hdf.DrafterHandle, n_seq: int, B: int, device="cuda"):
+        M, V = n_seq * B, handle.V
+        i32 = dict(dtype=torch.int32, device=device)
+        self.logits = torch.empty((M, V), dtype=torch.float32, device=device)
+        self.tokens = torch.empty(M, **i32)
+        self.cut = hdf.Truncation(torch.empty(M, **i32),
+                                  torch.empty(M, dtype=torch.float32, device=device),
+                                  torch.empty(M, **i32),
+                                  torch.empty(M, dtype=torch.float64, device=device))
+        self.accept = (torch.empty(n_seq, **i32), torch.empty(n_seq, **i32),
+                       torch.empty(n_seq + 1, **i32), torch.empty(M, **i32))
+        L, f32 = hdf.lib(), hdf.HDF_F32
+        # One workspace: the draws have run before the verification starts.  16-bit target logits
+        # need no more than 32-bit ones.
+        need = max(int(L.hdf_sample_truncated_workspace(M, V, f32)),
+                   int(L.hdf_accept_truncated_workspace(n_seq, B - 1, V, f32)),
+                   int(L.hdf_accept_truncated_workspace(n_seq, B - 1, V, hdf.HDF_BF16)))
+        self.ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+
+
+def drafter_step_truncated(handle: hdf.DrafterHandle, bufs: StepBuffers,
+                           tbufs: TruncatedStepBuffers, *, H_new: torch.Tensor, W_g: torch.Tensor,
+                           b_g: torch.Tensor, new_offsets: torch.Tensor, ctx_len: torch.Tensor,
+                           max_ctx: int, kv_offsets: torch.Tensor, kv_k: torch.Tensor,
+                           kv_vt: torch.Tensor, tokens: torch.Tensor, target_logits: torch.Tensor,
+                           draft_uniforms: torch.Tensor, accept_uniforms: torch.Tensor,
+                           temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                           reduce_kw: Optional[dict] = None, stream=None):
+    """The step under serving settings: reduce -> draft block -> LM head (logits kept) -> draws of
+    every slot from its truncated distribution -> speculative verification against target_logits
+    [n_seq, B, V] (fp32 or bf16; rows as in drafter_step_sampled) truncated alike.  temperature,
+    top_k, top_p and min_p are numbers or tensors of one entry a sequence; draft_uniforms
+    [n_seq*B] and accept_uniforms [n_seq, B] are the round's random numbers in [0, 1)."""
+    kw = dict(reduce_kw or {})
+    kw.setdefault("eps", handle.eps)
+    hdf.hc_reduce(H_new, W_g, b_g, Y=bufs.Y, stream=stream, **kw)
+    handle.draft_block(ctx_len=ctx_len, max_ctx=max_ctx, y_new=bufs.Y, new_offsets=new_offsets,
+                       kv_offsets=kv_offsets, kv_k=kv_k, kv_vt=kv_vt, tokens=tokens,
+                       hidden=bufs.hidden, ws=bufs.ws, stream=stream)
+    hdf.lm_head_argmax(bufs.hidden, handle.w_lm, ws=bufs.lm_ws, out=(bufs.argmax, bufs.max_logit),
+                       logits_out=tbufs.logits, stream=stream)
+    B = tokens.shape[1]
+    cuts = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+    hdf.sample_truncated(tbufs.logits, draft_uniforms, rows_per_seq=B,
+                         out=(tbufs.tokens, tbufs.cut), ws=tbufs.ws, stream=stream, **cuts)
+    acc, anc, offs, toks = hdf.accept_truncated(
+        tbufs.tokens[1:], tbufs.logits[1:], hdf.Truncation(*(x[1:] for x in tbufs.cut)),
+        target_logits, accept_uniforms, K=B - 1, draft_stride=B, out=tbufs.accept, ws=tbufs.ws,
+        stream=stream, **cuts)
+    return {"hidden": bufs.hidden, "logits": tbufs.logits, "tokens": tbufs.tokens,
+            "truncation": tbufs.cut, "accept_len": acc, "next_anchor": anc, "commit_offsets": offs,
+            "commit_tokens": toks}
