@@ -519,7 +519,8 @@ typedef struct {
   int rows_per_seq; /* >= 1 */
 } hdf_truncation;
 
-/* Workspace bytes of hdf_sample_truncated (0 where none is needed, and on invalid arguments). */
+/* Workspace bytes of hdf_sample_truncated (0 on invalid arguments); a workspace for more rows
+ * serves fewer. */
 size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype);
 /* logits    rows x vocab dtype, row r at logits + r*ld; any alignment of their element
  * params    host pointer
@@ -569,7 +570,8 @@ hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const vo
                                 int32_t* commit_offsets, int32_t* commit_tokens, void* ws,
                                 size_t ws_bytes, hdf_stream_t stream);
 
-/* Workspace bytes of hdf_top_logits (0 where none is needed, and on invalid arguments). */
+/* Workspace bytes of hdf_top_logits (0 on invalid arguments); a workspace for more rows serves
+ * fewer. */
 size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype);
 /* The first K entries of every row's order, and what the others weigh: a teacher's distribution
  * as it is stored for distillation.

@@ -981,7 +981,12 @@ void set_truncation(hdf::CutArgs& a, const hdf_truncation& p) {
 
 extern "C" {
 
-size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype) { return 0; }
+size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype) {
+  if (rows < 0 || rows > 65535 || vocab < 1 || vocab > kMaxTruncVocab ||
+      (dtype != HDF_F32 && dtype != HDF_BF16))
+    return 0;
+  return hdf::cut_ws_bytes(dtype == HDF_BF16, rows, vocab);
+}
 
 hdf_status hdf_sample_truncated(const void* logits, int64_t rows, int vocab, int64_t ld,
                                 hdf_dtype dtype, const hdf_truncation* params,
@@ -1003,7 +1008,7 @@ hdf_status hdf_sample_truncated(const void* logits, int64_t rows, int vocab, int
   set_truncation(a, *params);
   a.u = uniforms; a.tok = tokens; a.kept = kept; a.cut_logit = cut_logit; a.cut_index = cut_index;
   a.lse = lse;
-  const hipError_t e = hdf::launch_truncate(dtype == HDF_BF16, a,
+  const hipError_t e = hdf::launch_truncate(dtype == HDF_BF16, a, ws,
                                             reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "sample_truncated launch");
   return ok();
@@ -1056,7 +1061,9 @@ hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const vo
   return ok();
 }
 
-size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype) { return 0; }
+size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype) {
+  return K >= 1 && K <= 1024 ? hdf_sample_truncated_workspace(rows, vocab, dtype) : 0;
+}
 
 hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,
                           int K, float temperature, int32_t* ids, float* values, float* rest,
@@ -1073,7 +1080,7 @@ hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t l
   hdf::CutArgs a{};
   a.z = logits; a.rows = rows; a.ld = ld; a.V = vocab; a.per = 1; a.t = temperature;
   a.K = K; a.ids = ids; a.vals = values; a.rest = rest;
-  const hipError_t e = hdf::launch_top_logits(dtype == HDF_BF16, a,
+  const hipError_t e = hdf::launch_top_logits(dtype == HDF_BF16, a, ws,
                                               reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "top_logits launch");
   return ok();

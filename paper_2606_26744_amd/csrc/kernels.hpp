@@ -216,6 +216,7 @@ hipError_t launch_accept_sample(const int32_t* draft, int draft_stride, const fl
 struct CutArgs {
   const void* z;             // rows of V logits, stride ld
   int64_t rows, ld;
+  int64_t row0;              // first row of the launch (set by it)
   int V;
   // Truncation: row r takes entry r / per of an array, or the value where the array is NULL.
   int per;
@@ -235,8 +236,10 @@ struct CutArgs {
   float* vals;
   float* rest;               // [rows], or NULL
 };
-hipError_t launch_truncate(bool bf16, const CutArgs& a, hipStream_t s);
-hipError_t launch_top_logits(bool bf16, const CutArgs& a, hipStream_t s);
+// Workspace bytes of the next two: their first launch's lists and sums.
+size_t cut_ws_bytes(bool bf16, int64_t rows, int V);
+hipError_t launch_truncate(bool bf16, const CutArgs& a, void* ws, hipStream_t s);
+hipError_t launch_top_logits(bool bf16, const CutArgs& a, void* ws, hipStream_t s);
 
 struct VerifyArgs {
   const int32_t* draft;      // draft i of sequence s at s * stride + i, and so the rows below

@@ -16,18 +16,75 @@ namespace hdf {
 constexpr int kCutThreads = 1024;
 constexpr int kCutWaves = kCutThreads / kWave;
 constexpr int kBins = 2 * kCutThreads;
-constexpr int kListMax = kCutThreads;          // entries sorted at once
+constexpr int kListMax = 2 * kCutThreads;      // entries sorted at once
 constexpr int kAhead = 4;                      // vectors a thread loads before it uses them
 constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
 constexpr double kMassUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 
+// First launch: workgroup (row, chunk) keeps a chunk of a row in registers, lists its greatest
+// entries and sums up the others.  Second launch: a workgroup a row sorts the lists; where they hold
+// all that decides the cut, the row is not read again.
+constexpr int kHeadThreads = 512;
+constexpr int kHeadWaves = kHeadThreads / kWave;
+constexpr int kHeadBins = kHeadThreads;
+constexpr int kMaxChunks = 66;
+
+struct HeadStat {
+  float best;        // greatest value, its lowest column
+  int32_t best_col;
+  float floor;       // greatest unlisted value (-inf: none)
+  uint32_t valid;    // unmasked entries, listed ones
+  uint32_t listed;
+  uint32_t pad;
+  double rest;       // sum of e^((z - floor) / T) over the unlisted entries
+};
+
+struct HeadArgs {
+  int chunks, cap, vectors;   // of a row; entries a chunk may list; vectors of a chunk
+  uint64_t* list;             // [rows][chunks][cap]
+  HeadStat* stats;            // [rows][chunks]
+};
+
+// A row's settings.
+struct RowSettings {
+  float t, top_p, min_p;
+  int top_k;
+  bool greedy;
+  double inv_t, c2;
+};
+template <bool TOP>
+__device__ __forceinline__ RowSettings settings_of(const CutArgs& a, int64_t row) {
+  RowSettings s;
+  const int64_t i = TOP ? 0 : row / a.per;
+  s.t = !TOP && a.ts != nullptr ? a.ts[i] : a.t;
+  s.greedy = !(s.t > 0.f);
+  s.top_k = TOP ? a.K : a.ks != nullptr ? a.ks[i] : a.k;
+  s.top_p = TOP ? 1.f : a.ps != nullptr ? a.ps[i] : a.p;
+  s.min_p = TOP ? 0.f : a.mps != nullptr ? a.mps[i] : a.mp;
+  if (!TOP && s.top_k >= a.V) s.top_k = 0;
+  s.inv_t = s.greedy ? 1. : 1. / double(s.t);
+  s.c2 = 1.4426950408889634074 * s.inv_t;
+  return s;
+}
+// Entries that a chunk may list: all of a row's lists fit the sort.  With top_k a chunk need not
+// list more than that (and some, since whole bins are listed).
+__device__ __forceinline__ int list_cap(const RowSettings& s, int max_cap) {
+  if (s.greedy || (s.top_k <= 0 && !(s.top_p < 1.f) && !(s.min_p > 0.f))) return 0;
+  return s.top_k > 0 ? int(fmin(double(max_cap), 1.25 * s.top_k + 16.)) : max_cap;
+}
+
 struct CutShared {
   union {
     struct {
-      uint64_t mass[kBins];
-      uint32_t count[kBins];
       uint64_t list[kListMax];
+      union {
+        struct {
+          uint64_t mass[kBins];
+          uint32_t count[kBins];
+        };
+        double weight[kListMax];
+      };
     };
     double group[kCutWaves][kMaxGroups];
   };
@@ -36,51 +93,71 @@ struct CutShared {
     uint64_t u[kCutWaves];
     uint32_t i[kCutWaves];
   } red;
-  uint64_t before;
-  uint32_t n;
+  uint64_t before, best;
+  double rest, sum;
+  float floor;
+  uint32_t n, valid;
   int pick, last;
+  int offset[kMaxChunks + 1];   // of the chunks' lists
 };
 
-// Calls f(group, value, column) for every unmasked entry of the row; group g is the g-th run of
-// kCutThreads vectors, and after(g) follows a group's entries with all lanes together.
+// Calls f(group, value, column) for every unmasked entry of vectors j0 .. j1-1 of the row; group g
+// is the g-th run of kCutThreads of them, and after(g) follows a group's entries with all lanes
+// together.
 template <typename T, typename F, typename G>
-__device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f, G after) {
+__device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1, F f, G after) {
   constexpr int N = LogitRow<T>::N;
-  const int nv = r.vectors();
-  for (int b = 0; b < nv; b += kAhead * kCutThreads) {
+  for (int b = 0; j0 + b < j1; b += kAhead * kCutThreads) {
     float x[kAhead][N];
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
-      const int j = b + q * kCutThreads + int(threadIdx.x);
+      const int j = j0 + b + q * kCutThreads + int(threadIdx.x);
 #pragma unroll
       for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
-      if (j < nv) r.load(j, x[q]);
+      if (j < j1) r.load(j, x[q]);
     }
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
       const int g = b / kCutThreads + q;
-      const int c = r.column(g * kCutThreads + int(threadIdx.x));
+      const int c = r.column(j0 + g * kCutThreads + int(threadIdx.x));
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (x[q][e] > -INFINITY) f(g, x[q][e], c + e);
-      if (g * kCutThreads < nv) after(g);
+      if (j0 + g * kCutThreads < j1) after(g);
     }
   }
 }
 template <typename T, typename F>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
-  each_entry(r, f, [](int) {});
+  each_entry(r, 0, r.vectors(), f, [](int) {});
 }
 
-// The list's first n entries (n <= kListMax) from the greatest key down.
+// The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
+// exchanges within 64 entries stay in a wave's registers.
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
-  int P = 2;
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  int P = 64;
   while (P < n) P *= 2;
   for (int i = threadIdx.x; i < P; i += kCutThreads)
     if (i >= n) list[i] = 0;
   __syncthreads();
-  for (int size = 2; size <= P; size *= 2)
-    for (int d = size / 2; d > 0; d /= 2) {
+  auto in_waves = [&](int from, int to) {   // sizes from .. to, their exchanges of up to 32 apart
+    for (int s = wid; s * 64 < P; s += kCutWaves) {
+      const int i = s * 64 + lane;
+      uint64_t k = list[i];
+      for (int size = from; size <= to; size *= 2)
+        for (int d = size / 2 < 32 ? size / 2 : 32; d > 0; d /= 2) {
+          const uint64_t o = __shfl_xor(k, d, kWave);
+          const bool greater = ((lane & d) == 0) == ((i & size) == 0);
+          k = (o > k) == greater ? o : k;
+        }
+      list[i] = k;
+    }
+    __syncthreads();
+  };
+  in_waves(2, 64);
+  for (int size = 128; size <= P; size *= 2) {
+    for (int d = size / 2; d >= 64; d /= 2) {
       const int i = 2 * d * (int(threadIdx.x) / d) + int(threadIdx.x) % d;
       if (i + d < P) {
         const uint64_t a = list[i], b = list[i + d];
@@ -91,6 +168,8 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
       }
       __syncthreads();
     }
+    in_waves(size, size);
+  }
 }
 
 // First-level bin of a value below the row's greatest one: 64 bins a unit of (m - z) / T, so
@@ -187,11 +266,13 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
       sort_list(sh.list, n);
       int at;
       if (BY_MASS) {
-        const uint64_t k = sh.list[threadIdx.x];
-        const double w = int(threadIdx.x) < n ? entry_weight(entry_logit(k), m, c2) : 0.;
+        const int i = 2 * threadIdx.x;
+        const double w0 = i < n ? entry_weight(entry_logit(sh.list[i]), m, c2) : 0.;
+        const double w1 = i + 1 < n ? entry_weight(entry_logit(sh.list[i + 1]), m, c2) : 0.;
         double all;
-        const double sum = block_scan<kCutWaves>(w, sh.red.d, all);
-        if (int(threadIdx.x) < n && above + sum >= target) atomicMin(&sh.pick, int(threadIdx.x));
+        const double sum = block_scan<kCutWaves>(w0 + w1, sh.red.d, all);
+        if (i < n && above + (sum - w1) >= target) atomicMin(&sh.pick, i);
+        if (i + 1 < n && above + sum >= target) atomicMin(&sh.pick, i + 1);
         __syncthreads();
         at = min(sh.pick, n - 1);
       } else {
@@ -220,181 +301,501 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
   }
 }
 
+// The weights of a row's kept entries (keys >= cut) among vectors j0 .. j1-1, a group and wave a
+// sum in sh.group; returns their whole, `run` this thread's group's running sum and `mine` its own.
+template <typename T>
+__device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int j1, uint64_t cut,
+                                              float m, double c2, CutShared& sh, uint32_t& kept,
+                                              uint64_t& low, double& run, double& mine) {
+  kept = 0;
+  low = kKeyTop;
+  double s = 0.;
+  each_entry(
+      r, j0, j1,
+      [&](int, float z, int c) {
+        const uint64_t k = entry_key(z, c);
+        if (k < cut) return;
+        low = k < low ? k : low;
+        ++kept;
+        s += entry_weight(z, m, c2);
+      },
+      [&](int g) {
+        const double w = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) sh.group[threadIdx.x >> 6][g] = w;
+        s = 0.;
+      });
+  __syncthreads();
+  const int groups = (j1 - j0 + kCutThreads - 1) / kCutThreads;
+  mine = 0.;
+  if (int(threadIdx.x) < groups)
+    for (int w = 0; w < kCutWaves; ++w) mine += sh.group[w][threadIdx.x];
+  double all;
+  run = block_scan<kCutWaves>(mine, sh.red.d, all);
+  return all;
+}
+
+// The draw among the kept entries of vectors j0 .. j1-1, after kept_masses: the group in which
+// `base` and the running sum pass the target, then the entry; the last one where rounding leaves
+// none.
+template <typename T>
+__device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
+                                          double c2, double base, double target, double run,
+                                          double mine, CutShared& sh) {
+  if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = 0;
+  __syncthreads();
+  if (mine > 0.) {
+    if (base + run > target) atomicMin(&sh.pick, int(threadIdx.x));
+    atomicMax(&sh.last, int(threadIdx.x));
+  }
+  __syncthreads();
+  const int g = min(sh.pick, sh.last);
+  __syncthreads();
+  if (int(threadIdx.x) == g) sh.sum = base + (run - mine);
+  if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = -1;
+  __syncthreads();
+  const int j = j0 + g * kCutThreads + int(threadIdx.x), c = r.column(j);
+  float x[LogitRow<T>::N];
+  double own = 0., all;
+#pragma unroll
+  for (int e = 0; e < LogitRow<T>::N; ++e) x[e] = -INFINITY;
+  if (j < j1) {
+    r.load(j, x);
+#pragma unroll
+    for (int e = 0; e < LogitRow<T>::N; ++e) {
+      if (!(x[e] > -INFINITY && entry_key(x[e], c + e) >= cut)) {
+        x[e] = -INFINITY;
+        continue;
+      }
+      own += entry_weight(x[e], m, c2);
+      atomicMax(&sh.last, c + e);
+    }
+  }
+  const double upto = sh.sum + block_scan<kCutWaves>(own, sh.red.d, all);
+  if (own > 0. && upto > target) atomicMin(&sh.pick, int(threadIdx.x));
+  __syncthreads();
+  const int who = sh.pick;
+  __syncthreads();
+  if (int(threadIdx.x) == who) {
+    double before = upto - own;
+    int tok = -1;
+#pragma unroll
+    for (int e = 0; e < LogitRow<T>::N; ++e) {
+      const double w = entry_weight(x[e], m, c2);
+      if (w > 0. && (tok < 0 || before <= target)) tok = c + e;
+      before += w;
+    }
+    sh.last = tok;
+  }
+  __syncthreads();
+  return sh.last;
+}
+
+// A chunk of a row: E entries a thread.
+template <typename T, int E, bool TOP>
+__global__ void __launch_bounds__(kHeadThreads)
+row_head_kernel(CutArgs a, HeadArgs h) {
+  constexpr int N = LogitRow<T>::N, G = E / N;
+  __shared__ uint32_t count[kHeadBins];
+  __shared__ union {
+    double d[kHeadWaves];
+    float f[kHeadWaves];
+    uint32_t i[kHeadWaves];
+  } red;
+  __shared__ int best_col;
+  const int64_t at = blockIdx.x / h.chunks, row = a.row0 + at;   // in the launch, in the call
+  const int chunk = int(blockIdx.x - at * h.chunks), tid = threadIdx.x;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
+  const int j0 = chunk * G * kHeadThreads, nv = r.vectors();
+  float x[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int j = j0 + g * kHeadThreads + tid;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+    if (j < nv) r.load(j, x[g]);
+  }
+  const RowSettings s = settings_of<TOP>(a, row);
+  const int cap = list_cap(s, h.cap);
+  auto col = [&](int g, int e) { return r.column(j0 + g * kHeadThreads + tid) + e; };
+  auto add = [](auto u, auto v) { return u + v; };
+  auto most = [](float u, float v) { return fmaxf(u, v); };
+  auto least = [](float u, float v) { return fminf(u, v); };
+
+  count[tid] = 0;
+  if (tid == 0) best_col = a.V;
+  float top = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = fmaxf(top, x[g][e]);
+  const float m = block_fold<kHeadWaves>(top, red.f, most);
+  uint32_t valid = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      valid += x[g][e] > -INFINITY;
+      if (top == m && x[g][e] == m) atomicMin(&best_col, col(g, e));
+    }
+  valid = block_fold<kHeadWaves>(valid, red.i, add);
+
+  // The list.  The least of the threads' greatest values leaves one entry a thread above it, so the
+  // first ones of the order are all there; a histogram between it and the chunk's greatest value
+  // tells how many bins' entries fit.  Values far below the greatest (masks by the type's lowest
+  // value) would widen the bins: they are left to the second launch.
+  float lo = INFINITY, scale = 0.f;
+  int bins = 0;
+  uint32_t listed = 0, mine = 0, before = 0;
+  if (cap > 0 && m > -INFINITY) {
+    const float far = m - 64.f * fmaxf(s.greedy ? 1.f : s.t, 1.f);
+    lo = block_fold<kHeadWaves>(top > far ? top : INFINITY, red.f, least);
+    scale = float(kHeadBins) / (m - lo);
+    auto bin = [&](float z) { return z == m ? 0 : int(fminf((m - z) * scale, float(kHeadBins - 1))); };
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (x[g][e] >= lo) atomicAdd(&count[bin(x[g][e])], 1u);
+    __syncthreads();
+    uint32_t all;
+    const uint32_t upto = block_scan<kHeadWaves>(count[tid], red.i, all);
+    const bool fits = upto <= uint32_t(cap);
+    bins = int(block_fold<kHeadWaves>(uint32_t(fits), red.i, add));
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) mine += x[g][e] >= lo && bin(x[g][e]) < bins;
+    before = block_scan<kHeadWaves>(mine, red.i, listed) - mine;
+    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
+    if (mine > 0) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (x[g][e] >= lo && bin(x[g][e]) < bins) {
+            list[before++] = entry_key(x[g][e], col(g, e));
+            x[g][e] = -INFINITY;   // what stays is unlisted
+          }
+    }
+  }
+  float floor = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; ++e) floor = fmaxf(floor, x[g][e]);
+  floor = block_fold<kHeadWaves>(floor, red.f, most);
+  // The unlisted entries' weights, where the row's cut or draw needs them: in 64 bits there, in 32
+  // for the rest of the top logits, whose logarithm is stored in 32.
+  double rest = 0.;
+  const bool sums = TOP ? a.rest != nullptr : !s.greedy && s.top_k <= 0 && (s.top_p < 1.f || cap == 0);
+  if (sums && floor > -INFINITY) {
+    if constexpr (TOP) {
+      const float c2 = float(s.c2);
+      float f = 0.f;
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          f += x[g][e] == floor ? 1.f : __builtin_amdgcn_exp2f((x[g][e] - floor) * c2);
+      rest = double(f);
+    } else {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e) rest += entry_weight(x[g][e], floor, s.c2);
+    }
+    rest = block_fold<kHeadWaves>(rest, red.d, add);
+  }
+  if (tid == 0)
+    h.stats[at * h.chunks + chunk] = HeadStat{m, best_col, floor, valid, listed, 0u, rest};
+}
+
 // One row a workgroup.  TOP: the first K entries and the log-sum-exp of the others; else the
 // truncation and the draw.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kCutThreads)
-row_cut_kernel(CutArgs a) {
+row_cut_kernel(CutArgs a, HeadArgs h) {
   __shared__ CutShared sh;
-  const int64_t row = blockIdx.x;
+  const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
-  const int64_t si = TOP ? 0 : row / a.per;
-  const float t = a.ts != nullptr ? a.ts[si] : a.t;
-  const bool greedy = !(t > 0.f);
-  const double inv_t = greedy ? 1. : 1. / double(t);
-  const double c2 = 1.4426950408889634074 * inv_t;
-  const float scale = float(64. * inv_t);
+  const RowSettings s = settings_of<TOP>(a, row);
+  const float scale = float(64. * s.inv_t);
+  const HeadStat* hs = h.stats + at * h.chunks;
+  auto add = [](auto u, auto v) { return u + v; };
 
-  uint64_t best = 0;
-  uint32_t valid = 0;
-  each_entry(r, [&](int, float z, int c) {
-    const uint64_t k = entry_key(z, c);
-    best = k > best ? k : best;
-    ++valid;
-  });
-  best = block_fold<kCutWaves>(best, sh.red.u, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-  valid = block_fold<kCutWaves>(valid, sh.red.i, [](uint32_t x, uint32_t y) { return x + y; });
-  const float m = entry_logit(best);
+  // The chunks together, by the first wave.
+  if (wid == 0) {
+    uint64_t best = 0;
+    uint32_t valid = 0;
+    float floor = -INFINITY;
+    int run = 0;
+    for (int c0 = 0; c0 < h.chunks; c0 += 64) {
+      const int c = c0 + lane;
+      int n = 0;
+      if (c < h.chunks) {
+        const HeadStat st = hs[c];
+        if (st.valid > 0) {
+          const uint64_t k = entry_key(st.best, st.best_col);
+          best = k > best ? k : best;
+        }
+        valid += st.valid;
+        floor = fmaxf(floor, st.floor);
+        n = int(st.listed);
+      }
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += y;
+      }
+      if (c < h.chunks) sh.offset[c] = run + upto - n;
+      run += __shfl(upto, 63, kWave);
+    }
+    valid = wave_sum(valid);
+    floor = wave_max(floor);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const uint64_t y = __shfl_xor(best, o, kWave);
+      best = y > best ? y : best;
+    }
+    if (lane == 0) {
+      sh.best = best;
+      sh.valid = valid;
+      sh.floor = floor;
+      sh.offset[h.chunks] = run;
+    }
+  }
+  __syncthreads();
+  const uint64_t best = sh.best;
+  const uint32_t valid = sh.valid;
+  const float m = entry_logit(best), floor = sh.floor;
+  const int listed = sh.offset[h.chunks];
+
+  if (!TOP && (valid == 0 || s.greedy)) {
+    if (tid == 0) {
+      if (a.tok != nullptr) a.tok[row] = valid != 0 ? entry_column(best) : -1;
+      a.kept[row] = valid != 0 ? 1 : 0;
+      a.cut_logit[row] = valid > 1 ? m : -INFINITY;
+      a.cut_index[row] = valid > 1 ? entry_column(best) : -1;
+      a.lse[row] = valid != 0 ? 0. : -INFINITY;
+    }
+    return;
+  }
+
+  // The lists in order; the first `sure` of them are the row's first ones (every unlisted entry's
+  // value is at most `floor`).
+  for (int c = wid; c < h.chunks; c += kCutWaves) {
+    const int o = sh.offset[c], n = sh.offset[c + 1] - o;
+    const uint64_t* list = h.list + (at * h.chunks + c) * h.cap;
+    for (int i = lane; i < n; i += 64) sh.list[o + i] = list[i];
+  }
+  __syncthreads();
+  if (listed > 0) sort_list(sh.list, listed);
+  uint32_t sure = 0;
+  for (int i = tid; i < listed; i += kCutThreads) sure += entry_logit(sh.list[i]) > floor;
+  sure = block_fold<kCutWaves>(sure, sh.red.i, add);
+  const bool whole = sure == valid;   // nothing is unlisted
 
   if constexpr (TOP) {
     const int K = a.K;
     const int n = int(min(uint32_t(K), valid));
-    uint64_t cut = 0;
-    if (valid > uint32_t(K)) cut = select_entry<false>(r, double(K), 0, m, c2, scale, sh);
-    if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
-    uint64_t next = 0;   // the first entry past the list
-    each_entry(r, [&](int, float z, int c) {
-      const uint64_t k = entry_key(z, c);
-      if (k >= cut)
-        sh.list[atomicAdd(&sh.n, 1u)] = k;
-      else
-        next = k > next ? k : next;
-    });
-    __syncthreads();
-    sort_list(sh.list, n);
-    for (int i = threadIdx.x; i < K; i += kCutThreads) {
+    const bool quick = sure >= uint32_t(n);
+    if (!quick) {
+      const uint64_t cut =
+          valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, m, s.c2, scale, sh) : 0;
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      uint64_t next = 0;   // the first entry past the list
+      each_entry(r, [&](int, float z, int c) {
+        const uint64_t k = entry_key(z, c);
+        if (k >= cut)
+          sh.list[atomicAdd(&sh.n, 1u)] = k;
+        else
+          next = k > next ? k : next;
+      });
+      __syncthreads();
+      sort_list(sh.list, n);
+      if (a.rest != nullptr) {
+        next = block_fold<kCutWaves>(next, sh.red.u,
+                                     [](uint64_t u, uint64_t v) { return u > v ? u : v; });
+        const float top = entry_logit(next);
+        double sum = 0.;
+        if (next != 0)
+          each_entry(r, [&](int, float z, int c) {
+            if (entry_key(z, c) < cut) sum += entry_weight(z, top, s.c2);
+          });
+        sum = block_fold<kCutWaves>(sum, sh.red.d, add);
+        if (tid == 0)
+          a.rest[row] = next != 0 ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
+      }
+    } else if (a.rest != nullptr) {
+      const float after = listed > n ? entry_logit(sh.list[n]) : -INFINITY;
+      const float top = fmaxf(floor, after);
+      double sum = 0.;
+      if (top > -INFINITY) {
+        for (int i = n + tid; i < listed; i += kCutThreads)
+          sum += entry_weight(entry_logit(sh.list[i]), top, s.c2);
+        if (tid < h.chunks) sum += hs[tid].rest * entry_weight(hs[tid].floor, top, s.c2);
+      }
+      sum = block_fold<kCutWaves>(sum, sh.red.d, add);
+      if (tid == 0)
+        a.rest[row] = top > -INFINITY ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
+    }
+    for (int i = tid; i < K; i += kCutThreads) {
       const uint64_t k = sh.list[i < n ? i : 0];
       a.ids[row * K + i] = i < n ? entry_column(k) : -1;
       a.vals[row * K + i] = i < n ? entry_logit(k) : -INFINITY;
     }
-    if (a.rest == nullptr) return;
-    next = block_fold<kCutWaves>(next, sh.red.u, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-    const float top = entry_logit(next);
-    double s = 0.;
-    if (next != 0)
-      each_entry(r, [&](int, float z, int c) {
-        if (entry_key(z, c) < cut) s += entry_weight(z, top, c2);
-      });
-    s = block_fold<kCutWaves>(s, sh.red.d, [](double x, double y) { return x + y; });
-    if (threadIdx.x == 0)
-      a.rest[row] = next != 0 ? float(double(top) * inv_t + log(s)) : -INFINITY;
   } else {
-    if (valid == 0 || greedy) {
-      if (threadIdx.x == 0) {
-        if (a.tok != nullptr) a.tok[row] = valid != 0 ? entry_column(best) : -1;
-        a.kept[row] = valid != 0 ? 1 : 0;
-        a.cut_logit[row] = valid > 1 ? m : -INFINITY;
-        a.cut_index[row] = valid > 1 ? entry_column(best) : -1;
-        a.lse[row] = valid != 0 ? 0. : -INFINITY;
+    const bool has_k = s.top_k > 0 && uint32_t(s.top_k) < valid;
+    const bool has_p = s.top_p < 1.f, has_m = s.min_p > 0.f;
+    const double least_w = has_m ? fmin(double(s.min_p), 1.) : 0.;
+    uint32_t kept = valid;
+    uint64_t low = 0;
+    double mass;
+    const double u = a.u != nullptr ? fmin(fmax(double(a.u[row]), 0.), 1.) : 0.;
+    int tok = -1;
+    if (s.top_k <= 0 && !has_p && !has_m) {
+      // Everything is kept: the chunks' sums are the masses, and only the chunk drawn is read.
+      const double w = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].floor, m, s.c2) : 0.;
+      const double run = block_scan<kCutWaves>(w, sh.red.d, mass);
+      if (a.tok != nullptr) {
+        const double target = u * mass;
+        if (tid == 0) sh.pick = kCutThreads, sh.last = 0;
+        __syncthreads();
+        if (w > 0.) {
+          if (run > target) atomicMin(&sh.pick, tid);
+          atomicMax(&sh.last, tid);
+        }
+        __syncthreads();
+        const int c = min(sh.pick, sh.last);
+        __syncthreads();
+        if (tid == c) sh.sum = run - w;
+        __syncthreads();
+        const double base = sh.sum;
+        const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
+        uint32_t n;
+        uint64_t l;
+        double grun, gmine;
+        kept_masses(r, j0, j1, 0, m, s.c2, sh, n, l, grun, gmine);
+        tok = draw_entry(r, j0, j1, 0, m, s.c2, base, target, grun, gmine, sh);
       }
-      return;
+    } else {
+      // Running sums over the sorted lists, two entries a thread.
+      const int i0 = 2 * tid;
+      double w[2];
+      uint32_t above = 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        w[e] = i0 + e < listed ? entry_weight(entry_logit(sh.list[i0 + e]), m, s.c2) : 0.;
+        above += uint32_t(i0 + e) < sure && w[e] >= least_w;
+      }
+      double all;
+      const double upto = block_scan<kCutWaves>(w[0] + w[1], sh.red.d, all);
+      const uint32_t n_m = has_m ? block_fold<kCutWaves>(above, sh.red.i, add) : valid;
+      const uint32_t n_k = has_k ? uint32_t(s.top_k) : valid;
+      auto sum_at = [&](uint32_t n) {   // of the first n entries, n >= 1
+        if (uint32_t(i0) == ((n - 1) & ~1u)) sh.sum = (n & 1u) != 0 ? upto - w[1] : upto;
+        __syncthreads();
+        const double v = sh.sum;
+        __syncthreads();
+        return v;
+      };
+      // Without top_k the unlisted entries' sum is known; a top_k of more than the unmasked entries
+      // comes without it.
+      bool quick = has_k ? n_k <= sure : s.top_k <= 0 || whole;
+      uint32_t n = n_k;
+      if (quick && has_p) {
+        double zk;
+        if (has_k) {
+          zk = sum_at(n_k);
+        } else {
+          double rest = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].floor, m, s.c2) : 0.;
+          rest = block_fold<kCutWaves>(rest, sh.red.d, add);
+          zk = all + rest;
+        }
+        const double target = fmax(double(s.top_p) * zk, 1e-300);
+        if (tid == 0) sh.pick = kListMax;
+        __syncthreads();
+        if (uint32_t(i0) < sure && upto - w[1] >= target) atomicMin(&sh.pick, i0);
+        if (uint32_t(i0) + 1 < sure && upto >= target) atomicMin(&sh.pick, i0 + 1);
+        __syncthreads();
+        const uint32_t n_p = uint32_t(sh.pick) + 1;
+        __syncthreads();
+        n = n_p <= sure ? min(n, n_p) : n;
+      }
+      if (has_m && (n_m < sure || whole)) n = min(n, n_m);
+      quick = quick && n <= sure;
+      if (quick) {
+        kept = n;
+        low = sh.list[n - 1];
+        mass = sum_at(n);
+        if (a.tok != nullptr) {
+          // In token order: columns with their places as keys, the weights beside them.
+          const double target = u * mass;
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (uint32_t(i0 + e) < n) {
+              const uint64_t k = sh.list[i0 + e];
+              sh.weight[i0 + e] = w[e];
+              sh.list[i0 + e] = ((k & kColumnMask) << 12) | uint64_t(i0 + e);
+            }
+          __syncthreads();
+          sort_list(sh.list, int(n));
+          double v[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            v[e] = uint32_t(i0 + e) < n ? sh.weight[sh.list[i0 + e] & 4095u] : 0.;
+          const double run = block_scan<kCutWaves>(v[0] + v[1], sh.red.d, all);
+          if (tid == 0) sh.pick = kListMax, sh.last = 0;
+          __syncthreads();
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (v[e] > 0.) {
+              if ((e == 0 ? run - v[1] : run) > target) atomicMin(&sh.pick, i0 + e);
+              atomicMax(&sh.last, i0 + e);
+            }
+          __syncthreads();
+          tok = int(kColumnMask - uint32_t(sh.list[min(sh.pick, sh.last)] >> 12));
+        }
+      } else {
+        // The lists do not reach the cut: the row is read again.
+        uint64_t cut = 0;
+        if (has_k) cut = select_entry<false>(r, double(n_k), 0, m, s.c2, scale, sh);
+        if (has_p) {
+          double zk = 0.;
+          each_entry(r, [&](int, float z, int c) {
+            if (entry_key(z, c) >= cut) zk += entry_weight(z, m, s.c2);
+          });
+          zk = block_fold<kCutWaves>(zk, sh.red.d, add);
+          // A target of 0 is reached by the first entry, not before it.
+          const uint64_t k = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), cut, m, s.c2,
+                                                scale, sh);
+          cut = k > cut ? k : cut;
+        }
+        if (has_m) {
+          const uint64_t k = uint64_t(least_value_key(m, [&](float z) {
+                               return entry_weight(z, m, s.c2) >= least_w;
+                             })) << kColumnBits;
+          cut = k > cut ? k : cut;
+        }
+        double run, mine;
+        mass = kept_masses(r, 0, r.vectors(), cut, m, s.c2, sh, kept, low, run, mine);
+        kept = block_fold<kCutWaves>(kept, sh.red.i, add);
+        low = block_fold<kCutWaves>(low, sh.red.u,
+                                    [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+        if (a.tok != nullptr)
+          tok = draw_entry(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass, run, mine, sh);
+      }
     }
-    const int top_k = a.ks != nullptr ? a.ks[si] : a.k;
-    const float top_p = a.ps != nullptr ? a.ps[si] : a.p;
-    const float min_p = a.mps != nullptr ? a.mps[si] : a.mp;
-    uint64_t cut = 0;
-    if (top_k > 0 && uint32_t(top_k) < valid)
-      cut = select_entry<false>(r, double(top_k), 0, m, c2, scale, sh);
-    if (top_p < 1.f) {
-      double s = 0.;
-      each_entry(r, [&](int, float z, int c) {
-        if (entry_key(z, c) >= cut) s += entry_weight(z, m, c2);
-      });
-      s = block_fold<kCutWaves>(s, sh.red.d, [](double x, double y) { return x + y; });
-      // A target of 0 is reached by the first entry, not before it.
-      const double target = fmax(double(top_p) * s, 1e-300);
-      const uint64_t k = select_entry<true>(r, target, cut, m, c2, scale, sh);
-      cut = k > cut ? k : cut;
-    }
-    if (min_p > 0.f) {
-      const double least = fmin(double(min_p), 1.);
-      const uint64_t k = uint64_t(least_value_key(m, [&](float z) {
-                           return entry_weight(z, m, c2) >= least;
-                         })) << kColumnBits;
-      cut = k > cut ? k : cut;
-    }
-
-    // The kept entries: how many, the last of them, their weights' sums a group and wave.
-    uint32_t kept = 0;
-    uint64_t low = kKeyTop;
-    double s = 0.;
-    auto keeps = [&](float z, int c) { return entry_key(z, c) >= cut; };
-    each_entry(
-        r,
-        [&](int, float z, int c) {
-          if (!keeps(z, c)) return;
-          const uint64_t k = entry_key(z, c);
-          low = k < low ? k : low;
-          ++kept;
-          s += entry_weight(z, m, c2);
-        },
-        [&](int g) {
-          const double w = wave_sum(s);
-          if ((threadIdx.x & 63) == 0) sh.group[threadIdx.x >> 6][g] = w;
-          s = 0.;
-        });
-    __syncthreads();
-    kept = block_fold<kCutWaves>(kept, sh.red.i, [](uint32_t x, uint32_t y) { return x + y; });
-    low = block_fold<kCutWaves>(low, sh.red.u, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
-    const int groups = (r.vectors() + kCutThreads - 1) / kCutThreads;
-    double gs = 0., mass;
-    if (int(threadIdx.x) < groups)
-      for (int w = 0; w < kCutWaves; ++w) gs += sh.group[w][threadIdx.x];
-    const double run = block_scan<kCutWaves>(gs, sh.red.d, mass);
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
       const bool every = kept == valid;
       a.kept[row] = int32_t(kept);
       a.cut_logit[row] = every ? -INFINITY : entry_logit(low);
       a.cut_index[row] = every ? -1 : entry_column(low);
-      a.lse[row] = double(m) * inv_t + log(mass);
-    }
-    if (a.tok == nullptr) return;
-    // The draw: the group in which the running sum passes the target, then the entry.
-    const double target = fmin(fmax(double(a.u[row]), 0.), 1.) * mass;
-    if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = 0;
-    __syncthreads();
-    if (int(threadIdx.x) < groups && gs > 0.) {
-      if (run > target) atomicMin(&sh.pick, int(threadIdx.x));
-      atomicMax(&sh.last, int(threadIdx.x));
-    }
-    __syncthreads();
-    const int g = min(sh.pick, sh.last);
-    __syncthreads();
-    if (int(threadIdx.x) == g) sh.group[0][0] = run - gs;
-    if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = -1;
-    __syncthreads();
-    const double base = sh.group[0][0];
-    float x[LogitRow<T>::N];
-    const int j = g * kCutThreads + int(threadIdx.x), c = r.column(j);
-    double mine = 0., all;
-    if (j < r.vectors()) {
-      r.load(j, x);
-#pragma unroll
-      for (int e = 0; e < LogitRow<T>::N; ++e) {
-        const bool k = x[e] > -INFINITY && keeps(x[e], c + e);
-        x[e] = k ? x[e] : -INFINITY;
-        mine += entry_weight(x[e], m, c2);
-        if (k) atomicMax(&sh.last, c + e);
-      }
-    }
-    const double upto = base + block_scan<kCutWaves>(mine, sh.red.d, all);
-    if (mine > 0. && upto > target) atomicMin(&sh.pick, int(threadIdx.x));
-    __syncthreads();
-    if (sh.pick < kCutThreads) {
-      if (int(threadIdx.x) == sh.pick) {
-        double before = upto - mine;
-        int tok = -1;
-#pragma unroll
-        for (int e = 0; e < LogitRow<T>::N; ++e) {
-          const double w = entry_weight(x[e], m, c2);
-          before += w;
-          if (w > 0. && (tok < 0 || before - w <= target)) tok = c + e;
-        }
-        a.tok[row] = tok;
-      }
-    } else if (threadIdx.x == 0) {
-      a.tok[row] = sh.last;
+      a.lse[row] = double(m) * s.inv_t + log(mass);
+      if (a.tok != nullptr) a.tok[row] = tok;
     }
   }
 }
@@ -617,23 +1018,64 @@ verify_pick_kernel(VerifyArgs a, int parts) {
       a.toks[ahead + i] = i < n ? a.draft[int64_t(s) * a.stride + i] : token;
 }
 
-template <bool TOP>
-static hipError_t launch_cut(bool bf16, const CutArgs& a, hipStream_t s) {
-  if (bf16)
-    hipLaunchKernelGGL((row_cut_kernel<bf16_t, TOP>), dim3(unsigned(a.rows)), dim3(kCutThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((row_cut_kernel<float, TOP>), dim3(unsigned(a.rows)), dim3(kCutThreads), 0, s, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_truncate(bool bf16, const CutArgs& a, hipStream_t s) {
-  return launch_cut<false>(bf16, a, s);
-}
-hipError_t launch_top_logits(bool bf16, const CutArgs& a, hipStream_t s) {
-  return launch_cut<true>(bf16, a, s);
-}
-
 static size_t al256(size_t x) { return (x + 255) / 256 * 256; }
+
+// The first launch's chunks: 16384 columns each, or 4096 where those would leave CUs idle (and the
+// lists of so many chunks still hold enough).
+struct HeadPlan {
+  int chunks, elems;
+};
+static HeadPlan head_plan(bool bf16, int64_t rows, int V) {
+  const int N = bf16 ? 8 : 4, span = (V + 2 * N - 2) / N * N;
+  const int large = (span + 32 * kHeadThreads - 1) / (32 * kHeadThreads);
+  const int small = (span + 8 * kHeadThreads - 1) / (8 * kHeadThreads);
+  if (rows * large < device_cu_count() && small <= 64) return {small, 8};
+  return {large, 32};
+}
+// Rows of one pair of launches; more run in turns over the same workspace.
+constexpr int64_t kCutRows = 4096;
+
+size_t cut_ws_bytes(bool bf16, int64_t rows, int V) {
+  const int64_t n = rows < kCutRows ? rows : kCutRows;
+  // The lists of a row hold kListMax entries whatever its chunks; small chunks are more.
+  const HeadPlan one = head_plan(bf16, 0, V), many = head_plan(bf16, kCutRows, V);
+  const size_t chunks = size_t(one.chunks > many.chunks ? one.chunks : many.chunks);
+  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * chunks * sizeof(HeadStat));
+}
+
+template <typename T, bool TOP>
+static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
+  for (int64_t r0 = 0; r0 < all.rows; r0 += kCutRows) {
+    CutArgs a = all;
+    a.rows = all.rows - r0 < kCutRows ? all.rows - r0 : kCutRows;
+    a.row0 = r0;
+    const HeadPlan pl = head_plan(sizeof(T) == 2, a.rows, a.V);
+    HeadArgs h;
+    h.chunks = pl.chunks;
+    h.cap = kListMax / pl.chunks;
+    h.vectors = pl.elems * kHeadThreads / LogitRow<T>::N;
+    h.list = static_cast<uint64_t*>(ws);
+    h.stats = reinterpret_cast<HeadStat*>(static_cast<char*>(ws) + al256(size_t(a.rows) * kListMax * 8));
+    const dim3 grid(unsigned(a.rows) * pl.chunks);
+    if (pl.elems == 8)
+      hipLaunchKernelGGL((row_head_kernel<T, 8, TOP>), grid, dim3(kHeadThreads), 0, s, a, h);
+    else
+      hipLaunchKernelGGL((row_head_kernel<T, 32, TOP>), grid, dim3(kHeadThreads), 0, s, a, h);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((row_cut_kernel<T, TOP>), dim3(unsigned(a.rows)), dim3(kCutThreads), 0, s, a, h);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_truncate(bool bf16, const CutArgs& a, void* ws, hipStream_t s) {
+  return bf16 ? launch_cut<bf16_t, false>(a, ws, s) : launch_cut<float, false>(a, ws, s);
+}
+hipError_t launch_top_logits(bool bf16, const CutArgs& a, void* ws, hipStream_t s) {
+  return bf16 ? launch_cut<bf16_t, true>(a, ws, s) : launch_cut<float, true>(a, ws, s);
+}
 
 // Parts of a target row: 256 vectors each, of its least vectors and one for a row that starts
 // inside one.
@@ -644,7 +1086,7 @@ static int verify_parts(bool bf16, int V) {
 
 size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V) {
   const size_t rows = size_t(n_seq) * (K + 1);
-  return al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
+  return cut_ws_bytes(bf16, int64_t(rows), V) + al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
          al256(size_t(n_seq) * verify_parts(bf16, V) * 16);
 }
 
@@ -676,7 +1118,7 @@ hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs
   a.t_logit = c.cut_logit;
   a.t_index = c.cut_index;
   a.t_lse = c.lse;
-  const hipError_t e = launch_truncate(target_bf16, c, s);
+  const hipError_t e = launch_truncate(target_bf16, c, take(cut_ws_bytes(target_bf16, int64_t(rows), a.V)), s);
   if (e != hipSuccess) return e;
   if (draft_bf16)
     return target_bf16 ? launch_verify<bf16_t, bf16_t>(a, n_seq, parts, s)
