@@ -985,7 +985,7 @@ size_t hdf_sample_truncated_workspace(int64_t rows, int vocab, hdf_dtype dtype) 
   if (rows < 0 || rows > 65535 || vocab < 1 || vocab > kMaxTruncVocab ||
       (dtype != HDF_F32 && dtype != HDF_BF16))
     return 0;
-  return hdf::cut_ws_bytes(dtype == HDF_BF16, rows, vocab);
+  return hdf::cut_ws_bytes(dtype == HDF_BF16, rows, vocab, false);
 }
 
 hdf_status hdf_sample_truncated(const void* logits, int64_t rows, int vocab, int64_t ld,
@@ -1062,7 +1062,8 @@ hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const vo
 }
 
 size_t hdf_top_logits_workspace(int64_t rows, int vocab, int K, hdf_dtype dtype) {
-  return K >= 1 && K <= 1024 ? hdf_sample_truncated_workspace(rows, vocab, dtype) : 0;
+  if (hdf_sample_truncated_workspace(rows, vocab, dtype) == 0 || K < 1 || K > 1024) return 0;
+  return hdf::cut_ws_bytes(dtype == HDF_BF16, rows, vocab, true);
 }
 
 hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t ld, hdf_dtype dtype,

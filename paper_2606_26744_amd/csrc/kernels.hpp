@@ -236,8 +236,8 @@ struct CutArgs {
   float* vals;
   float* rest;               // [rows], or NULL
 };
-// Workspace bytes of the next two: their first launch's lists and sums.
-size_t cut_ws_bytes(bool bf16, int64_t rows, int V);
+// Workspace bytes of the next two (top: of the second): their first launch's lists and sums.
+size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top);
 hipError_t launch_truncate(bool bf16, const CutArgs& a, void* ws, hipStream_t s);
 hipError_t launch_top_logits(bool bf16, const CutArgs& a, void* ws, hipStream_t s);
 

@@ -9,7 +9,7 @@ namespace hdf {
 // A row of V logits read 16 bytes at a time.  Rows start at any element (odd vocabularies, strides,
 // views): vector j holds columns j * N - shift .. + N - 1 and is aligned; the first and the last,
 // which reach past the row, are read element by element.  `load_raw` and `raw` give the values as
-// they are, `load` and `at` those of a row to choose from: NaN is -inf (masked), -0 is +0.
+// they are, `load` and `at` those of a row to choose from: NaN is -inf (masked).
 template <typename T>
 struct LogitRow {
   static constexpr int N = 16 / int(sizeof(T));
@@ -43,7 +43,7 @@ struct LogitRow {
   __device__ __forceinline__ void load(int j, float x[N]) const {
     load_raw(j, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = fmaxf(x[e], -INFINITY) + 0.f;
+    for (int e = 0; e < N; ++e) x[e] = fmaxf(x[e], -INFINITY);
   }
   __device__ __forceinline__ float raw(int c) const {
     if constexpr (sizeof(T) == 2)
@@ -51,16 +51,17 @@ struct LogitRow {
     else
       return p[c];
   }
-  __device__ __forceinline__ float at(int c) const { return fmaxf(raw(c), -INFINITY) + 0.f; }
+  __device__ __forceinline__ float at(int c) const { return fmaxf(raw(c), -INFINITY); }
 };
 
 // The order of a row's entries (largest value first, ties to the lowest column) as 52-bit keys,
-// greater for an earlier entry: the value's order key over the complement of the column.
+// greater for an earlier entry: the value's order key (-0 as +0: they are equal logits) over the
+// complement of the column.
 constexpr int kColumnBits = 20;
 constexpr uint32_t kColumnMask = (1u << kColumnBits) - 1;   // columns 0 .. 2^20 - 1
 
 __device__ __forceinline__ uint64_t entry_key(float z, int c) {
-  return (uint64_t(f32_order_key(z)) << kColumnBits) | (kColumnMask - uint32_t(c));
+  return (uint64_t(f32_order_key(z + 0.f)) << kColumnBits) | (kColumnMask - uint32_t(c));
 }
 __device__ __forceinline__ float entry_logit(uint64_t k) {
   return f32_from_order_key(uint32_t(k >> kColumnBits));

@@ -17,40 +17,53 @@ constexpr int kCutThreads = 1024;
 constexpr int kCutWaves = kCutThreads / kWave;
 constexpr int kBins = 2 * kCutThreads;
 constexpr int kListMax = 2 * kCutThreads;      // entries sorted at once
-constexpr int kAhead = 4;                      // vectors a thread loads before it uses them
+constexpr int kAhead = 16;                     // entries a thread loads before it uses them
 constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
 constexpr double kMassUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 
 // First launch: workgroup (row, chunk) keeps a chunk of a row in registers, lists its greatest
-// entries and sums up the others.  Second launch: a workgroup a row sorts the lists; where they hold
-// all that decides the cut, the row is not read again.
+// entries and, where the cut depends on the others, sums them up: in a histogram of weights for a
+// nucleus (top_p without top_k), in one sum otherwise.  Second launch: a workgroup a row finds how
+// far down the order the cut lies and sorts the listed entries up to there; a cut below the lists
+// takes one more pass over the row.
 constexpr int kHeadThreads = 512;
 constexpr int kHeadWaves = kHeadThreads / kWave;
-constexpr int kHeadBins = kHeadThreads;
 constexpr int kMaxChunks = 66;
+
+// The nucleus histogram: bins of 1/16 octave of weight.  Entry z has t = 16 z log2(e) / T, bin
+// n = rint(t) and within it the weight 2^((t - n) / 16), 0.978 .. 1.022, as a multiple of 2^-48;
+// integers, so that the sums do not depend on their order.  1024 bins from the chunk's greatest
+// entry down; entries more than 62 octaves below it weigh nothing.
+constexpr int kMassBins = 1024;
 
 struct HeadStat {
   float best;        // greatest value, its lowest column
   int32_t best_col;
-  float floor;       // greatest unlisted value (-inf: none)
+  float floor;       // every entry >= floor is listed (-inf: all are)
+  float near;        // a value that at least `few` entries reach (HeadArgs)
   uint32_t valid;    // unmasked entries, listed ones
   uint32_t listed;
-  uint32_t pad;
-  double rest;       // sum of e^((z - floor) / T) over the unlisted entries
+  int32_t top_bin;   // bin of the greatest value, and how many bins from it down are stored
+  int32_t bins;      // (-1: values beyond the bins' range)
+  float rest_ref;    // rest: sum of e^((z - rest_ref) / T) over the unlisted entries
+  float pad;
+  double rest;
 };
 
 struct HeadArgs {
   int chunks, cap, vectors;   // of a row; entries a chunk may list; vectors of a chunk
   uint64_t* list;             // [rows][chunks][cap]
   HeadStat* stats;            // [rows][chunks]
+  uint64_t* mass;             // [rows][chunks][kMassBins]
+  int32_t* pending;           // [rows] rows left to the third launch, or NULL
 };
 
 // A row's settings.
 struct RowSettings {
   float t, top_p, min_p;
   int top_k;
-  bool greedy;
+  bool greedy, nucleus, open;
   double inv_t, c2;
 };
 template <bool TOP>
@@ -63,18 +76,38 @@ __device__ __forceinline__ RowSettings settings_of(const CutArgs& a, int64_t row
   s.top_p = TOP ? 1.f : a.ps != nullptr ? a.ps[i] : a.p;
   s.min_p = TOP ? 0.f : a.mps != nullptr ? a.mps[i] : a.mp;
   if (!TOP && s.top_k >= a.V) s.top_k = 0;
+  s.nucleus = !s.greedy && s.top_k <= 0 && s.top_p < 1.f;
+  s.open = !s.greedy && s.top_k <= 0 && !s.nucleus && !(s.min_p > 0.f);
   s.inv_t = s.greedy ? 1. : 1. / double(s.t);
   s.c2 = 1.4426950408889634074 * s.inv_t;
   return s;
 }
-// Entries that a chunk may list: all of a row's lists fit the sort.  With top_k a chunk need not
-// list more than that (and some, since whole bins are listed).
-__device__ __forceinline__ int list_cap(const RowSettings& s, int max_cap) {
-  if (s.greedy || (s.top_k <= 0 && !(s.top_p < 1.f) && !(s.min_p > 0.f))) return 0;
-  return s.top_k > 0 ? int(fmin(double(max_cap), 1.25 * s.top_k + 16.)) : max_cap;
+
+// Bin of a value and the weight within it (a multiple of 2^-48 in the low bits).  The magic
+// constants round to an integer in the low bits of the sum; the series is that of 2^(g / 16),
+// |g| <= 1/2, whose first dropped term is 0.022^7 / 7! = 4e-16.
+__device__ __forceinline__ int weight_bin(float z, double k16) {
+  const double t = fma(double(z), k16, 6755399441055744.);   // 1.5 * 2^52
+  return int(uint32_t(__builtin_bit_cast(uint64_t, t)));
+}
+__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, int& n) {
+  const double t = fma(double(z), k16, 6755399441055744.);
+  n = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
+  const double g = fma(double(z), k16, -(t - 6755399441055744.));
+  constexpr double c = 0.69314718055994530942 / 16.;
+  double p = c * c * c * c * c * c / 720.;
+  p = fma(p, g, c * c * c * c * c / 120.);
+  p = fma(p, g, c * c * c * c / 24.);
+  p = fma(p, g, c * c * c / 6.);
+  p = fma(p, g, c * c / 2.);
+  p = fma(p, g, c);
+  p = fma(p, g, 17.);   // 16 + 1: a unit of 16's last place is 2^-48
+  return __builtin_bit_cast(uint64_t, p) - 0x4030000000000000ull;
 }
 
+template <int NT>
 struct CutShared {
+  static constexpr int W = NT / kWave;
   union {
     struct {
       uint64_t list[kListMax];
@@ -86,19 +119,20 @@ struct CutShared {
         double weight[kListMax];
       };
     };
-    double group[kCutWaves][kMaxGroups];
+    double group[W][kMaxGroups];
   };
+  double chunk[kMaxChunks];
   union {
-    double d[kCutWaves];
-    uint64_t u[kCutWaves];
-    uint32_t i[kCutWaves];
+    double d[W];
+    uint64_t u[W];
+    uint32_t i[W];
+    float f[W];
   } red;
   uint64_t before, best;
-  double rest, sum;
-  float floor;
-  uint32_t n, valid;
-  int pick, last;
-  int offset[kMaxChunks + 1];   // of the chunks' lists
+  double sum;
+  float floor, near;
+  uint32_t n, valid, listed;
+  int pick, last, top_bin, bins;
 };
 
 // Calls f(group, value, column) for every unmasked entry of vectors j0 .. j1-1 of the row; group g
@@ -106,18 +140,18 @@ struct CutShared {
 // together.
 template <typename T, typename F, typename G>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1, F f, G after) {
-  constexpr int N = LogitRow<T>::N;
-  for (int b = 0; j0 + b < j1; b += kAhead * kCutThreads) {
-    float x[kAhead][N];
+  constexpr int N = LogitRow<T>::N, Q = kAhead / N;
+  for (int b = 0; j0 + b < j1; b += Q * kCutThreads) {
+    float x[Q][N];
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
+    for (int q = 0; q < Q; ++q) {
       const int j = j0 + b + q * kCutThreads + int(threadIdx.x);
 #pragma unroll
       for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
       if (j < j1) r.load(j, x[q]);
     }
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
+    for (int q = 0; q < Q; ++q) {
       const int g = b / kCutThreads + q;
       const int c = r.column(j0 + g * kCutThreads + int(threadIdx.x));
 #pragma unroll
@@ -134,15 +168,15 @@ __device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
 
 // The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
 // exchanges within 64 entries stay in a wave's registers.
+template <int NT>
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   int P = 64;
   while (P < n) P *= 2;
-  for (int i = threadIdx.x; i < P; i += kCutThreads)
-    if (i >= n) list[i] = 0;
+  for (int i = n + int(threadIdx.x); i < P; i += NT) list[i] = 0;
   __syncthreads();
   auto in_waves = [&](int from, int to) {   // sizes from .. to, their exchanges of up to 32 apart
-    for (int s = wid; s * 64 < P; s += kCutWaves) {
+    for (int s = wid; s * 64 < P; s += NT / kWave) {
       const int i = s * 64 + lane;
       uint64_t k = list[i];
       for (int size = from; size <= to; size *= 2)
@@ -158,8 +192,8 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   in_waves(2, 64);
   for (int size = 128; size <= P; size *= 2) {
     for (int d = size / 2; d >= 64; d /= 2) {
-      const int i = 2 * d * (int(threadIdx.x) / d) + int(threadIdx.x) % d;
-      if (i + d < P) {
+      for (int t = threadIdx.x; t < P / 2; t += NT) {
+        const int i = 2 * d * (t / d) + t % d;
         const uint64_t a = list[i], b = list[i + d];
         if ((a < b) == ((i & size) == 0)) {
           list[i] = b;
@@ -202,13 +236,18 @@ __device__ __forceinline__ uint32_t least_value_key(float m, F holds) {
 // Key of the entry with which the running sum, in order, of ones (BY_MASS false) or weights over
 // the entries with keys >= floor reaches `target`; the last of them if rounding leaves none.
 // Histograms of 2048 bins over ever smaller ranges of the order, until a bin's entries fit the
-// list: the first by value, further ones by key, where the last range is one key.
+// list: the first by value, further ones by key, where the last range is one key.  A caller that
+// knows the range of keys and the sum `above` it starts there (lo > 0).
 template <bool BY_MASS, typename T>
 __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t floor, float m,
-                                 double c2, float scale, CutShared& sh) {
-  double above = 0.;
-  uint64_t lo = 0, hi = kKeyTop;
-  int shift = -1, bin = 0;   // shift -1: the bins by value
+                                 double c2, float scale, CutShared<kCutThreads>& sh, uint64_t lo = 0,
+                                 uint64_t hi = kKeyTop, double above = 0.) {
+  auto shift_of = [&]() {
+    int sh_ = 0;
+    while (((hi - lo) >> sh_) >= uint64_t(kBins)) ++sh_;
+    return sh_;
+  };
+  int shift = lo > 0 ? shift_of() : -1, bin = 0;   // shift -1: the bins by value
   for (;;) {
     for (int b = threadIdx.x; b < kBins; b += kCutThreads) {
       sh.count[b] = 0;
@@ -263,7 +302,7 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
       });
       __syncthreads();
       const int n = int(sh.n);
-      sort_list(sh.list, n);
+      sort_list<kCutThreads>(sh.list, n);
       int at;
       if (BY_MASS) {
         const int i = 2 * threadIdx.x;
@@ -295,8 +334,7 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
       const uint64_t l = hi - ((uint64_t(1) << shift) - 1);
       lo = l > lo ? l : lo;
     }
-    shift = 0;
-    while (((hi - lo) >> shift) >= uint64_t(kBins)) ++shift;
+    shift = shift_of();
     __syncthreads();
   }
 }
@@ -305,7 +343,8 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
 // sum in sh.group; returns their whole, `run` this thread's group's running sum and `mine` its own.
 template <typename T>
 __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int j1, uint64_t cut,
-                                              float m, double c2, CutShared& sh, uint32_t& kept,
+                                              float m, double c2, CutShared<kCutThreads>& sh,
+                                              uint32_t& kept,
                                               uint64_t& low, double& run, double& mine) {
   kept = 0;
   low = kKeyTop;
@@ -340,7 +379,7 @@ __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int 
 template <typename T>
 __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
                                           double c2, double base, double target, double run,
-                                          double mine, CutShared& sh) {
+                                          double mine, CutShared<kCutThreads>& sh) {
   if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = 0;
   __syncthreads();
   if (mine > 0.) {
@@ -395,15 +434,18 @@ template <typename T, int E, bool TOP>
 __global__ void __launch_bounds__(kHeadThreads)
 row_head_kernel(CutArgs a, HeadArgs h) {
   constexpr int N = LogitRow<T>::N, G = E / N;
-  __shared__ uint32_t count[kHeadBins];
+  __shared__ unsigned long long mass[kMassBins];
+  __shared__ uint32_t count[kHeadThreads];
   __shared__ union {
     double d[kHeadWaves];
     float f[kHeadWaves];
     uint32_t i[kHeadWaves];
   } red;
+  __shared__ uint32_t wave_n[2][kHeadWaves];
   __shared__ int best_col;
   const int64_t at = blockIdx.x / h.chunks, row = a.row0 + at;   // in the launch, in the call
   const int chunk = int(blockIdx.x - at * h.chunks), tid = threadIdx.x;
+  const int lane = tid & 63, wid = tid >> 6;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const int j0 = chunk * G * kHeadThreads, nv = r.vectors();
   float x[G][N];
@@ -415,13 +457,25 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     if (j < nv) r.load(j, x[g]);
   }
   const RowSettings s = settings_of<TOP>(a, row);
-  const int cap = list_cap(s, h.cap);
   auto col = [&](int g, int e) { return r.column(j0 + g * kHeadThreads + tid) + e; };
   auto add = [](auto u, auto v) { return u + v; };
   auto most = [](float u, float v) { return fmaxf(u, v); };
   auto least = [](float u, float v) { return fminf(u, v); };
+  // Entries for which `of` holds, over the workgroup: counted by the scalar unit.
+  auto count_of = [&](int which, auto of) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) n += uint32_t(__popcll(__ballot(of(x[g][e]))));
+    if (lane == 0) wave_n[which][wid] = n;
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kHeadWaves; ++w) all += wave_n[which][w];
+    return all;
+  };
 
-  count[tid] = 0;
   if (tid == 0) best_col = a.V;
   float top = -INFINITY;
 #pragma unroll
@@ -429,148 +483,232 @@ row_head_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll
     for (int e = 0; e < N; ++e) top = fmaxf(top, x[g][e]);
   const float m = block_fold<kHeadWaves>(top, red.f, most);
-  uint32_t valid = 0;
+  if (top == m && m > -INFINITY) {
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      valid += x[g][e] > -INFINITY;
-      if (top == m && x[g][e] == m) atomicMin(&best_col, col(g, e));
-    }
-  valid = block_fold<kHeadWaves>(valid, red.i, add);
-
-  // The list.  The least of the threads' greatest values leaves one entry a thread above it, so the
-  // first ones of the order are all there; a histogram between it and the chunk's greatest value
-  // tells how many bins' entries fit.  Values far below the greatest (masks by the type's lowest
-  // value) would widen the bins: they are left to the second launch.
-  float lo = INFINITY, scale = 0.f;
-  int bins = 0;
-  uint32_t listed = 0, mine = 0, before = 0;
-  if (cap > 0 && m > -INFINITY) {
-    const float far = m - 64.f * fmaxf(s.greedy ? 1.f : s.t, 1.f);
-    lo = block_fold<kHeadWaves>(top > far ? top : INFINITY, red.f, least);
-    scale = float(kHeadBins) / (m - lo);
-    auto bin = [&](float z) { return z == m ? 0 : int(fminf((m - z) * scale, float(kHeadBins - 1))); };
-#pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int g = G - 1; g >= 0; --g)
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (x[g][e] >= lo) atomicAdd(&count[bin(x[g][e])], 1u);
+        if (x[g][e] == m) atomicMin(&best_col, col(g, e));
+  }
+  const uint32_t valid = count_of(0, [](float z) { return z > -INFINITY; });
+
+  // The list: all entries >= lo, lo a thread's greatest value such that `want` threads reach it; so
+  // at least `want` entries do, and hardly more unless the great ones crowd into few threads (then
+  // fewer threads are asked for).  A histogram of the 512 greatest values finds it.  Values far
+  // below the chunk's greatest (masks by the type's lowest value) would widen its bins: they take
+  // no part.  near: the same for the few entries a chunk has to contribute on the average.
+  float lo = INFINITY, near = INFINITY;
+  uint32_t listed = 0;
+  if (!s.greedy && !s.open && valid > 0) {
+    const float far = m - 64.f * fmaxf(s.t, 1.f);
+    const bool in = top > far;
+    const float low = block_fold<kHeadWaves>(in ? top : INFINITY, red.f, least);
+    const float scale = float(kHeadThreads) / (m - low);
+    const int mine = top == m ? 0 : int(fminf((m - top) * scale, float(kHeadThreads - 1)));
+    int want = s.top_k > 0 ? int(fminf(float(s.top_k) + 4.f, float(kHeadThreads))) : h.cap;
+    const int most_wanted = 2 * h.cap / 3 > 0 ? 2 * h.cap / 3 : 1;
+    want = want < most_wanted ? want : most_wanted;
+    const int few = s.top_k > 0 ? (s.top_k + h.chunks - 1) / h.chunks : 1;
+    count[tid] = 0;
+    __syncthreads();
+    if (in) atomicAdd(&count[mine], 1u);
     __syncthreads();
     uint32_t all;
     const uint32_t upto = block_scan<kHeadWaves>(count[tid], red.i, all);
-    const bool fits = upto <= uint32_t(cap);
-    bins = int(block_fold<kHeadWaves>(uint32_t(fits), red.i, add));
+    count[tid] = upto;
+    __syncthreads();
+    const uint32_t first = in && mine > 0 ? count[mine - 1] : 0u;   // threads in the bins before
+    near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
+    if (valid <= uint32_t(h.cap)) {
+      lo = -3.402823466e38f;
+      listed = valid;
+    } else {
+      for (; want > 0; want /= 2) {
+        lo = block_fold<kHeadWaves>(in && first < uint32_t(want) ? top : INFINITY, red.f, least);
+        const float v = lo;
+        listed = count_of(1, [&](float z) { return z >= v; });
+        if (listed <= uint32_t(h.cap)) break;
+        __syncthreads();
+      }
+      if (want == 0) {
+        lo = INFINITY;
+        listed = 0;
+      }
+    }
+    if (listed > 0) {
+      if (listed == valid) count_of(1, [&](float z) { return z >= lo; });
+      uint32_t before = 0;
+      for (int w = 0; w < wid; ++w) before += wave_n[1][w];
+      uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+      for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int e = 0; e < N; ++e) mine += x[g][e] >= lo && bin(x[g][e]) < bins;
-    before = block_scan<kHeadWaves>(mine, red.i, listed) - mine;
-    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
-    if (mine > 0) {
+        for (int e = 0; e < N; ++e) {
+          const bool is = x[g][e] >= lo;
+          const unsigned long long who = __ballot(is);
+          if (who != 0ull) {
+            const uint32_t k = __popcll(who & ((1ull << lane) - 1));
+            if (is) list[before + k] = entry_key(x[g][e], col(g, e));
+            before += uint32_t(__popcll(who));
+          }
+        }
+    }
+  }
+
+  HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0.f, 0.f, 0.};
+  if (s.nucleus && valid > 0) {
+    const double k16 = 16. * s.c2;
+    const float range = float(992. / k16);   // 62 octaves
+    if (fabs(double(m)) * k16 < 1e9 && range < INFINITY) {
+      for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
+      __syncthreads();
+      const float end = m - range;
+      st.top_bin = weight_bin(m, k16);
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (x[g][e] >= lo && bin(x[g][e]) < bins) {
-            list[before++] = entry_key(x[g][e], col(g, e));
-            x[g][e] = -INFINITY;   // what stays is unlisted
+          if (x[g][e] >= end && x[g][e] > -INFINITY) {
+            int n;
+            const uint64_t w = weight_in_bin(x[g][e], k16, n);
+            const int b = st.top_bin - n;
+            if (b >= 0 && b < kMassBins) atomicAdd(&mass[b], static_cast<unsigned long long>(w));
           }
+      __syncthreads();
+      uint32_t end_bin = 0;
+      for (int b = tid; b < kMassBins; b += kHeadThreads)
+        if (mass[b] != 0) end_bin = uint32_t(b) + 1;
+      end_bin = block_fold<kHeadWaves>(end_bin, red.i, [](uint32_t u, uint32_t v) { return u > v ? u : v; });
+      uint64_t* out = h.mass + (at * h.chunks + chunk) * kMassBins;
+      for (int b = tid; b < int(end_bin); b += kHeadThreads) out[b] = mass[b];
+      st.bins = int(end_bin);
+    } else {
+      st.bins = -1;
     }
-  }
-  float floor = -INFINITY;
+  } else if (TOP && a.rest != nullptr && valid > listed) {
+    // The others of the top logits: 32-bit exponentials, as their logarithm is stored in 32 bits.
+    // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.
+    const float c2 = float(s.c2);
+    for (int turn = 0; turn < 2; ++turn) {
+      st.rest_ref = lo;
+      if (turn == 1 || !(lo < INFINITY)) {
+        float g_top = -INFINITY;
 #pragma unroll
-  for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < N; ++e) floor = fmaxf(floor, x[g][e]);
-  floor = block_fold<kHeadWaves>(floor, red.f, most);
-  // The unlisted entries' weights, where the row's cut or draw needs them: in 64 bits there, in 32
-  // for the rest of the top logits, whose logarithm is stored in 32.
-  double rest = 0.;
-  const bool sums = TOP ? a.rest != nullptr : !s.greedy && s.top_k <= 0 && (s.top_p < 1.f || cap == 0);
-  if (sums && floor > -INFINITY) {
-    if constexpr (TOP) {
-      const float c2 = float(s.c2);
+          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e] >= lo ? -INFINITY : x[g][e]);
+        st.rest_ref = block_fold<kHeadWaves>(g_top, red.f, most);
+      }
       float f = 0.f;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          f += x[g][e] == floor ? 1.f : __builtin_amdgcn_exp2f((x[g][e] - floor) * c2);
-      rest = double(f);
-    } else {
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int e = 0; e < N; ++e) rest += entry_weight(x[g][e], floor, s.c2);
+        for (int e = 0; e < N; ++e) {
+          const float d = x[g][e] == st.rest_ref ? 0.f : (x[g][e] - st.rest_ref) * c2;
+          const float w = __builtin_amdgcn_exp2f(d);
+          f += x[g][e] >= lo ? 0.f : w;
+        }
+      st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
+      if (st.rest > 1e-25 || !(lo < INFINITY)) break;
     }
-    rest = block_fold<kHeadWaves>(rest, red.d, add);
+  } else if (!TOP && s.open && valid > 0) {
+    double sum = 0.;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum += entry_weight(x[g][e], m, s.c2);
+    st.rest_ref = m;
+    st.rest = block_fold<kHeadWaves>(sum, red.d, add);
   }
-  if (tid == 0)
-    h.stats[at * h.chunks + chunk] = HeadStat{m, best_col, floor, valid, listed, 0u, rest};
+  if (tid == 0) h.stats[at * h.chunks + chunk] = st;
+}
+
+// First place, in the order of places 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes)
+// the target, n where none does; `sum_to` gets the sum of the first n_sum of them.
+template <int NT, bool STRICT, typename F>
+__device__ __forceinline__ int reach(int n, double target, int n_sum, double& sum_to,
+                                     CutShared<NT>& sh, F w) {
+  if (threadIdx.x == 0) sh.pick = n;
+  double before = 0.;
+  for (int b = 0; b < n; b += NT) {
+    const int i = b + int(threadIdx.x);
+    const double v = i < n ? w(i) : 0.;
+    double all;
+    const double run = before + block_scan<CutShared<NT>::W>(v, sh.red.d, all);
+    if (i < n && (STRICT ? v > 0. && run > target : run >= target)) atomicMin(&sh.pick, i);
+    if (i == n_sum - 1) sh.sum = run;
+    before += all;
+  }
+  __syncthreads();
+  const int at = sh.pick;
+  sum_to = n_sum > 0 ? sh.sum : 0.;
+  __syncthreads();
+  return at;
 }
 
 // One row a workgroup.  TOP: the first K entries and the log-sum-exp of the others; else the
-// truncation and the draw.
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kCutThreads)
+// truncation and the draw.  LISTS: only rows whose cut lies within the lists; the others are marked
+// as pending.
+template <typename T, bool TOP, int NT, bool LISTS>
+__global__ void __launch_bounds__(NT)
 row_cut_kernel(CutArgs a, HeadArgs h) {
-  __shared__ CutShared sh;
+  using Shared = CutShared<NT>;
+  constexpr int W = Shared::W;
+  __shared__ Shared sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  if (!LISTS && h.pending != nullptr && h.pending[at] == 0) return;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const RowSettings s = settings_of<TOP>(a, row);
   const float scale = float(64. * s.inv_t);
   const HeadStat* hs = h.stats + at * h.chunks;
   auto add = [](auto u, auto v) { return u + v; };
+  auto most64 = [](uint64_t u, uint64_t v) { return u > v ? u : v; };
 
   // The chunks together, by the first wave.
   if (wid == 0) {
     uint64_t best = 0;
-    uint32_t valid = 0;
-    float floor = -INFINITY;
-    int run = 0;
-    for (int c0 = 0; c0 < h.chunks; c0 += 64) {
-      const int c = c0 + lane;
-      int n = 0;
-      if (c < h.chunks) {
-        const HeadStat st = hs[c];
-        if (st.valid > 0) {
-          const uint64_t k = entry_key(st.best, st.best_col);
-          best = k > best ? k : best;
-        }
-        valid += st.valid;
-        floor = fmaxf(floor, st.floor);
-        n = int(st.listed);
-      }
-      int upto = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += y;
-      }
-      if (c < h.chunks) sh.offset[c] = run + upto - n;
-      run += __shfl(upto, 63, kWave);
+    uint32_t valid = 0, listed = 0;
+    float floor = -INFINITY, near = INFINITY;
+    int top_bin = -2147483647, bins = 0;
+    for (int c = lane; c < h.chunks; c += 64) {
+      const HeadStat st = hs[c];
+      if (st.valid == 0) continue;
+      const uint64_t k = entry_key(st.best, st.best_col);
+      best = k > best ? k : best;
+      valid += st.valid;
+      listed += st.listed;
+      floor = fmaxf(floor, st.floor);
+      near = fminf(near, st.near);
+      top_bin = st.bins > 0 ? max(top_bin, st.top_bin) : top_bin;
+      bins = st.bins < 0 ? -1 : bins;
     }
     valid = wave_sum(valid);
+    listed = wave_sum(listed);
     floor = wave_max(floor);
+    near = -wave_max(-near);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t y = __shfl_xor(best, o, kWave);
-      best = y > best ? y : best;
+      best = most64(best, __shfl_xor(best, o, kWave));
+      top_bin = max(top_bin, __shfl_xor(top_bin, o, kWave));
+      bins = min(bins, __shfl_xor(bins, o, kWave));
     }
     if (lane == 0) {
       sh.best = best;
       sh.valid = valid;
+      sh.listed = listed;
       sh.floor = floor;
-      sh.offset[h.chunks] = run;
+      sh.near = near;
+      sh.top_bin = top_bin;
+      sh.bins = bins;
     }
   }
   __syncthreads();
   const uint64_t best = sh.best;
-  const uint32_t valid = sh.valid;
+  const uint32_t valid = sh.valid, listed = sh.listed;
   const float m = entry_logit(best), floor = sh.floor;
-  const int listed = sh.offset[h.chunks];
+  const bool whole = listed == valid;   // nothing is unlisted
+  if (LISTS && tid == 0) h.pending[at] = 0;
 
   if (!TOP && (valid == 0 || s.greedy)) {
     if (tid == 0) {
@@ -583,66 +721,87 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     return;
   }
 
-  // The lists in order; the first `sure` of them are the row's first ones (every unlisted entry's
-  // value is at most `floor`).
-  for (int c = wid; c < h.chunks; c += kCutWaves) {
-    const int o = sh.offset[c], n = sh.offset[c + 1] - o;
-    const uint64_t* list = h.list + (at * h.chunks + c) * h.cap;
-    for (int i = lane; i < n; i += 64) sh.list[o + i] = list[i];
-  }
-  __syncthreads();
-  if (listed > 0) sort_list(sh.list, listed);
-  uint32_t sure = 0;
-  for (int i = tid; i < listed; i += kCutThreads) sure += entry_logit(sh.list[i]) > floor;
-  sure = block_fold<kCutWaves>(sure, sh.red.i, add);
-  const bool whole = sure == valid;   // nothing is unlisted
+  // Calls f(key) for every listed entry, a wave a chunk.
+  auto each_listed = [&](auto f) {
+    for (int c = wid; c < h.chunks; c += W) {
+      const int n = int(hs[c].listed);
+      const uint64_t* list = h.list + (at * h.chunks + c) * h.cap;
+      for (int i = lane; i < n; i += 64) f(list[i]);
+    }
+  };
+  // The listed entries of value >= t, sorted; all of the row's where t >= floor.
+  auto gather = [&](float t) {
+    __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    each_listed([&](uint64_t k) {
+      if (entry_logit(k) >= t) sh.list[atomicAdd(&sh.n, 1u)] = k;
+    });
+    __syncthreads();
+    const int n = int(sh.n);
+    __syncthreads();
+    return n;
+  };
 
   if constexpr (TOP) {
     const int K = a.K;
     const int n = int(min(uint32_t(K), valid));
-    const bool quick = sure >= uint32_t(n);
-    if (!quick) {
-      const uint64_t cut =
-          valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, m, s.c2, scale, sh) : 0;
-      if (tid == 0) sh.n = 0;
-      __syncthreads();
-      uint64_t next = 0;   // the first entry past the list
-      each_entry(r, [&](int, float z, int c) {
-        const uint64_t k = entry_key(z, c);
-        if (k >= cut)
-          sh.list[atomicAdd(&sh.n, 1u)] = k;
-        else
-          next = k > next ? k : next;
-      });
-      __syncthreads();
-      sort_list(sh.list, n);
+    int have = gather(fmaxf(floor, sh.near));
+    if (have < n && sh.near > floor) have = gather(floor);
+    if (have < n) {
+      if constexpr (LISTS) {
+        if (tid == 0) h.pending[at] = 1;
+        return;
+      } else {
+        const uint64_t cut =
+            valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, m, s.c2, scale, sh) : 0;
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        uint64_t next = 0;   // the first entry past the list
+        each_entry(r, [&](int, float z, int c) {
+          const uint64_t k = entry_key(z, c);
+          if (k >= cut)
+            sh.list[atomicAdd(&sh.n, 1u)] = k;
+          else
+            next = k > next ? k : next;
+        });
+        __syncthreads();
+        sort_list<NT>(sh.list, n);
+        if (a.rest != nullptr) {
+          next = block_fold<W>(next, sh.red.u, most64);
+          const float top = entry_logit(next);
+          double sum = 0.;
+          if (next != 0)
+            each_entry(r, [&](int, float z, int c) {
+              if (entry_key(z, c) < cut) sum += entry_weight(z, top, s.c2);
+            });
+          sum = block_fold<W>(sum, sh.red.d, add);
+          if (tid == 0)
+            a.rest[row] = next != 0 ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
+        }
+      }
+    } else {
+      sort_list<NT>(sh.list, have);
       if (a.rest != nullptr) {
-        next = block_fold<kCutWaves>(next, sh.red.u,
-                                     [](uint64_t u, uint64_t v) { return u > v ? u : v; });
-        const float top = entry_logit(next);
+        const uint64_t last = n > 0 ? sh.list[n - 1] : 0;
+        uint64_t next = 0;
+        float ref = -INFINITY;
+        each_listed([&](uint64_t k) { next = k < last ? most64(next, k) : next; });
+        if (tid < h.chunks && hs[tid].rest > 0.) ref = hs[tid].rest_ref;
+        ref = fmaxf(ref, next != 0 ? entry_logit(next) : -INFINITY);
+        ref = block_fold<W>(ref, sh.red.f, [](float u, float v) { return fmaxf(u, v); });
         double sum = 0.;
-        if (next != 0)
-          each_entry(r, [&](int, float z, int c) {
-            if (entry_key(z, c) < cut) sum += entry_weight(z, top, s.c2);
-          });
-        sum = block_fold<kCutWaves>(sum, sh.red.d, add);
+        each_listed([&](uint64_t k) {
+          if (k < last) sum += entry_weight(entry_logit(k), ref, s.c2);
+        });
+        if (tid < h.chunks && hs[tid].rest > 0.)
+          sum += hs[tid].rest * entry_weight(hs[tid].rest_ref, ref, s.c2);
+        sum = block_fold<W>(sum, sh.red.d, add);
         if (tid == 0)
-          a.rest[row] = next != 0 ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
+          a.rest[row] = ref > -INFINITY ? float(double(ref) * s.inv_t + log(sum)) : -INFINITY;
       }
-    } else if (a.rest != nullptr) {
-      const float after = listed > n ? entry_logit(sh.list[n]) : -INFINITY;
-      const float top = fmaxf(floor, after);
-      double sum = 0.;
-      if (top > -INFINITY) {
-        for (int i = n + tid; i < listed; i += kCutThreads)
-          sum += entry_weight(entry_logit(sh.list[i]), top, s.c2);
-        if (tid < h.chunks) sum += hs[tid].rest * entry_weight(hs[tid].floor, top, s.c2);
-      }
-      sum = block_fold<kCutWaves>(sum, sh.red.d, add);
-      if (tid == 0)
-        a.rest[row] = top > -INFINITY ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
     }
-    for (int i = tid; i < K; i += kCutThreads) {
+    for (int i = tid; i < K; i += NT) {
       const uint64_t k = sh.list[i < n ? i : 0];
       a.ids[row * K + i] = i < n ? entry_column(k) : -1;
       a.vals[row * K + i] = i < n ? entry_logit(k) : -INFINITY;
@@ -653,14 +812,78 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     const double least_w = has_m ? fmin(double(s.min_p), 1.) : 0.;
     uint32_t kept = valid;
     uint64_t low = 0;
-    double mass;
+    double mass = 0.;
     const double u = a.u != nullptr ? fmin(fmax(double(a.u[row]), 0.), 1.) : 0.;
     int tok = -1;
-    if (s.top_k <= 0 && !has_p && !has_m) {
+
+    // The nucleus' border bin: the histograms joined, their running sum against top_p of the whole.
+    const double k16 = 16. * s.c2;
+    const bool binned = s.nucleus && sh.bins == 0;
+    double zk = 0., above = 0.;   // relative to the greatest entry: the whole, the bins above it
+    int border = 0;
+    const int top_bin = sh.top_bin;
+    auto bin_weight = [&](int b) { return exp2_64(-double(b) / 16.); };
+    // Weight of the top bin's middle relative to the greatest entry's.
+    const double unit =
+        binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * 3.552713678800501e-15 : 0.;   // 2^-48
+    auto mass_at = [&](int c, int b) -> uint64_t {   // of chunk c in the row's bin b
+      const int i = b - (top_bin - hs[c].top_bin);
+      return i >= 0 && i < hs[c].bins ? h.mass[(at * h.chunks + c) * kMassBins + i] : 0ull;
+    };
+    if (binned) {
+      constexpr int PER = kMassBins / NT;
+      double v[PER], sum = 0.;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const int b = PER * tid + e;
+        double n = 0.;
+        for (int c = 0; c < h.chunks; ++c)
+          if (hs[c].valid > 0) n += double(mass_at(c, b));
+        v[e] = n * bin_weight(b) * unit;
+        sum += v[e];
+      }
+      const double run = block_scan<W>(sum, sh.red.d, zk);
+      if (tid == 0) sh.pick = kMassBins, sh.last = 0;
+      __syncthreads();
+      const double target = fmax(double(s.top_p) * zk, 1e-300);
+      double upto = run - sum;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        upto += v[e];
+        if (v[e] > 0.) {
+          if (upto >= target) atomicMin(&sh.pick, PER * tid + e);
+          atomicMax(&sh.last, PER * tid + e);
+        }
+      }
+      __syncthreads();
+      border = min(sh.pick, sh.last);
+      upto = run - sum;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        if (PER * tid + e == border) sh.sum = upto;
+        upto += v[e];
+      }
+      __syncthreads();
+      above = sh.sum;
+      __syncthreads();
+    }
+    // Least value of bin b or a greater one.
+    auto bin_edge = [&](int b) {
+      return f32_from_order_key(least_value_key(m, [&](float z) {   // far values have no bin
+        return double(z) * k16 > double(top_bin) - 2048. && weight_bin(z, k16) >= top_bin - b;
+      }));
+    };
+
+    if (s.open) {
       // Everything is kept: the chunks' sums are the masses, and only the chunk drawn is read.
-      const double w = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].floor, m, s.c2) : 0.;
-      const double run = block_scan<kCutWaves>(w, sh.red.d, mass);
-      if (a.tok != nullptr) {
+      const double w = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].rest_ref, m, s.c2) : 0.;
+      const double run = block_scan<W>(w, sh.red.d, mass);
+      if constexpr (LISTS) {
+        if (a.tok != nullptr) {
+          if (tid == 0) h.pending[at] = 1;
+          return;
+        }
+      } else if (a.tok != nullptr) {
         const double target = u * mass;
         if (tid == 0) sh.pick = kCutThreads, sh.last = 0;
         __syncthreads();
@@ -682,111 +905,180 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         tok = draw_entry(r, j0, j1, 0, m, s.c2, base, target, grun, gmine, sh);
       }
     } else {
-      // Running sums over the sorted lists, two entries a thread.
-      const int i0 = 2 * tid;
-      double w[2];
-      uint32_t above = 0;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        w[e] = i0 + e < listed ? entry_weight(entry_logit(sh.list[i0 + e]), m, s.c2) : 0.;
-        above += uint32_t(i0 + e) < sure && w[e] >= least_w;
+      // How far down the cut can lie, and whether the lists reach it.
+      float t = floor;
+      bool quick;
+      if (has_k)
+        t = fmaxf(floor, sh.near), quick = true;
+      else if (binned)
+        t = bin_edge(border), quick = t >= floor;
+      else if (s.top_k <= 0 && !has_p)
+        t = f32_from_order_key(least_value_key(
+            m, [&](float z) { return entry_weight(z, m, s.c2) >= least_w; })),
+        quick = t >= floor;
+      else
+        quick = whole;
+      int have = quick ? gather(t) : 0;
+      if (has_k && have < s.top_k) {
+        if (t > floor) have = gather(floor);
+        quick = have >= s.top_k;
       }
-      double all;
-      const double upto = block_scan<kCutWaves>(w[0] + w[1], sh.red.d, all);
-      const uint32_t n_m = has_m ? block_fold<kCutWaves>(above, sh.red.i, add) : valid;
-      const uint32_t n_k = has_k ? uint32_t(s.top_k) : valid;
-      auto sum_at = [&](uint32_t n) {   // of the first n entries, n >= 1
-        if (uint32_t(i0) == ((n - 1) & ~1u)) sh.sum = (n & 1u) != 0 ? upto - w[1] : upto;
-        __syncthreads();
-        const double v = sh.sum;
-        __syncthreads();
-        return v;
-      };
-      // Without top_k the unlisted entries' sum is known; a top_k of more than the unmasked entries
-      // comes without it.
-      bool quick = has_k ? n_k <= sure : s.top_k <= 0 || whole;
-      uint32_t n = n_k;
-      if (quick && has_p) {
-        double zk;
-        if (has_k) {
-          zk = sum_at(n_k);
-        } else {
-          double rest = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].floor, m, s.c2) : 0.;
-          rest = block_fold<kCutWaves>(rest, sh.red.d, add);
-          zk = all + rest;
-        }
-        const double target = fmax(double(s.top_p) * zk, 1e-300);
-        if (tid == 0) sh.pick = kListMax;
-        __syncthreads();
-        if (uint32_t(i0) < sure && upto - w[1] >= target) atomicMin(&sh.pick, i0);
-        if (uint32_t(i0) + 1 < sure && upto >= target) atomicMin(&sh.pick, i0 + 1);
-        __syncthreads();
-        const uint32_t n_p = uint32_t(sh.pick) + 1;
-        __syncthreads();
-        n = n_p <= sure ? min(n, n_p) : n;
-      }
-      if (has_m && (n_m < sure || whole)) n = min(n, n_m);
-      quick = quick && n <= sure;
       if (quick) {
-        kept = n;
-        low = sh.list[n - 1];
-        mass = sum_at(n);
-        if (a.tok != nullptr) {
-          // In token order: columns with their places as keys, the weights beside them.
-          const double target = u * mass;
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (uint32_t(i0 + e) < n) {
-              const uint64_t k = sh.list[i0 + e];
-              sh.weight[i0 + e] = w[e];
-              sh.list[i0 + e] = ((k & kColumnMask) << 12) | uint64_t(i0 + e);
-            }
-          __syncthreads();
-          sort_list(sh.list, int(n));
-          double v[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            v[e] = uint32_t(i0 + e) < n ? sh.weight[sh.list[i0 + e] & 4095u] : 0.;
-          const double run = block_scan<kCutWaves>(v[0] + v[1], sh.red.d, all);
-          if (tid == 0) sh.pick = kListMax, sh.last = 0;
-          __syncthreads();
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (v[e] > 0.) {
-              if ((e == 0 ? run - v[1] : run) > target) atomicMin(&sh.pick, i0 + e);
-              atomicMax(&sh.last, i0 + e);
-            }
-          __syncthreads();
-          tok = int(kColumnMask - uint32_t(sh.list[min(sh.pick, sh.last)] >> 12));
+        sort_list<NT>(sh.list, have);
+        auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
+        int n = has_k ? s.top_k : have;
+        if (has_p) {
+          double sum;
+          if (!binned) reach<NT, false>(n, 1e300, n, zk, sh, weight);   // of all n
+          const int p = reach<NT, false>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
+          n = min(n, p + 1);
         }
+        if (has_m) {
+          uint32_t c = 0;
+          for (int i = tid; i < n; i += NT) c += weight(i) >= least_w;
+          n = int(block_fold<W>(c, sh.red.i, add));
+        }
+        kept = uint32_t(n);
+        low = sh.list[n - 1];
+        __syncthreads();
+        // In token order: columns with their places as keys, the weights beside them.
+        for (int i = tid; i < n; i += NT) {
+          const uint64_t k = sh.list[i];
+          sh.weight[i] = entry_weight(entry_logit(k), m, s.c2);
+          sh.list[i] = ((k & kColumnMask) << 12) | uint64_t(i);
+        }
+        __syncthreads();
+        sort_list<NT>(sh.list, n);
+        auto in_order = [&](int i) { return sh.weight[sh.list[i] & 4095u]; };
+        reach<NT, true>(n, 1e300, n, mass, sh, in_order);
+        if (a.tok != nullptr) {
+          double sum;
+          int i = reach<NT, true>(n, u * mass, 0, sum, sh, in_order);
+          if (i == n) {   // the last with a weight
+            if (tid == 0) sh.last = 0;
+            __syncthreads();
+            for (int q = tid; q < n; q += NT)
+              if (in_order(q) > 0.) atomicMax(&sh.last, q);
+            __syncthreads();
+            i = sh.last;
+          }
+          tok = int(kColumnMask - uint32_t(sh.list[i] >> 12));
+        }
+      } else if constexpr (LISTS) {
+        if (tid == 0) h.pending[at] = 1;
+        return;
       } else {
         // The lists do not reach the cut: the row is read again.
         uint64_t cut = 0;
-        if (has_k) cut = select_entry<false>(r, double(n_k), 0, m, s.c2, scale, sh);
-        if (has_p) {
-          double zk = 0.;
+        uint64_t cut_m = 0;
+        if (has_m)
+          cut_m = uint64_t(least_value_key(m, [&](float z) {
+                    return entry_weight(z, m, s.c2) >= least_w;
+                  })) << kColumnBits;
+        bool done = false;
+        if (binned) {
+          // The border bin's entries, and how many lie above it.
+          const float end = bin_edge(border);
+          const float over = border > 0 ? bin_edge(border - 1) : INFINITY;
+          __syncthreads();
+          if (tid == 0) sh.n = 0;
+          __syncthreads();
+          uint32_t greater = 0;
           each_entry(r, [&](int, float z, int c) {
-            if (entry_key(z, c) >= cut) zk += entry_weight(z, m, s.c2);
+            if (border > 0 && z >= over) {
+              ++greater;
+            } else if (z >= end) {
+              const uint32_t i = atomicAdd(&sh.n, 1u);
+              if (i < uint32_t(kListMax)) sh.list[i] = entry_key(z, c);
+            }
           });
-          zk = block_fold<kCutWaves>(zk, sh.red.d, add);
-          // A target of 0 is reached by the first entry, not before it.
-          const uint64_t k = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), cut, m, s.c2,
-                                                scale, sh);
-          cut = k > cut ? k : cut;
+          greater = block_fold<W>(greater, sh.red.i, add);
+          const uint32_t in = sh.n;
+          __syncthreads();
+          if (in <= uint32_t(kListMax) && in > 0) {
+            sort_list<NT>(sh.list, int(in));
+            auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
+            double sum;
+            const int p = reach<NT, false>(int(in), fmax(double(s.top_p) * zk, 1e-300) - above, 0, sum,
+                                           sh, weight);
+            const int n = min(p + 1, int(in));
+            cut = sh.list[n - 1];
+            if (cut_m <= cut) {
+              done = true;
+              kept = greater + uint32_t(n);
+              low = cut;
+              {
+                // The chunks' masses: their bins above the border, and their part of its entries.
+                for (int c = wid; c < h.chunks; c += W) {
+                  double w = 0.;
+                  if (hs[c].valid > 0)
+                    for (int b = lane; b < border; b += 64)
+                      w += double(mass_at(c, b)) * bin_weight(b) * unit;
+                  for (int i = lane; i < n; i += 64) {
+                    const uint64_t k = sh.list[i];
+                    const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
+                    if (j / h.vectors == c) w += entry_weight(entry_logit(k), m, s.c2);
+                  }
+                  w = wave_sum(w);
+                  if (lane == 0) sh.chunk[c] = w;
+                }
+                __syncthreads();
+                const double w = tid < h.chunks ? sh.chunk[tid] : 0.;
+                const double run = block_scan<W>(w, sh.red.d, mass);
+                if (a.tok != nullptr) {
+                  const double target = u * mass;
+                  if (tid == 0) sh.pick = kCutThreads, sh.last = 0;
+                  __syncthreads();
+                  if (w > 0.) {
+                    if (run > target) atomicMin(&sh.pick, tid);
+                    atomicMax(&sh.last, tid);
+                  }
+                  __syncthreads();
+                  const int c = min(sh.pick, sh.last);
+                  __syncthreads();
+                  if (tid == c) sh.sum = run - w;
+                  __syncthreads();
+                  const double base = sh.sum;
+                  const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
+                  uint32_t k;
+                  uint64_t l;
+                  double grun, gmine;
+                  kept_masses(r, j0, j1, cut, m, s.c2, sh, k, l, grun, gmine);
+                  tok = draw_entry(r, j0, j1, cut, m, s.c2, base, target, grun, gmine, sh);
+                }
+              }
+            }
+          }
         }
-        if (has_m) {
-          const uint64_t k = uint64_t(least_value_key(m, [&](float z) {
-                               return entry_weight(z, m, s.c2) >= least_w;
-                             })) << kColumnBits;
-          cut = k > cut ? k : cut;
+        if (!done && binned && cut == 0 && sh.n > uint32_t(kListMax)) {
+          // A border bin of many entries: the cut among them.
+          const uint64_t end = entry_key(bin_edge(border), a.V - 1);
+          const uint64_t over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
+          __syncthreads();
+          cut = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), 0, m, s.c2, scale, sh, end,
+                                   over, above);
         }
-        double run, mine;
-        mass = kept_masses(r, 0, r.vectors(), cut, m, s.c2, sh, kept, low, run, mine);
-        kept = block_fold<kCutWaves>(kept, sh.red.i, add);
-        low = block_fold<kCutWaves>(low, sh.red.u,
-                                    [](uint64_t x, uint64_t y) { return x < y ? x : y; });
-        if (a.tok != nullptr)
-          tok = draw_entry(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass, run, mine, sh);
+        if (!done) {
+          const bool known = cut != 0;   // but for min_p
+          if (has_k) cut = select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh);
+          if (has_p && !known) {
+            double all = 0.;
+            each_entry(r, [&](int, float z, int c) {
+              if (entry_key(z, c) >= cut) all += entry_weight(z, m, s.c2);
+            });
+            all = block_fold<W>(all, sh.red.d, add);
+            // A target of 0 is reached by the first entry, not before it.
+            cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2,
+                                                 scale, sh));
+          }
+          cut = most64(cut, cut_m);
+          double run, mine;
+          mass = kept_masses(r, 0, r.vectors(), cut, m, s.c2, sh, kept, low, run, mine);
+          kept = block_fold<W>(kept, sh.red.i, add);
+          low = block_fold<W>(low, sh.red.u, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+          if (a.tok != nullptr)
+            tok = draw_entry(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass, run, mine, sh);
+        }
       }
     }
     if (tid == 0) {
@@ -1032,38 +1324,68 @@ static HeadPlan head_plan(bool bf16, int64_t rows, int V) {
   if (rows * large < device_cu_count() && small <= 64) return {small, 8};
   return {large, 32};
 }
-// Rows of one pair of launches; more run in turns over the same workspace.
-constexpr int64_t kCutRows = 4096;
+// Rows of one group of launches; more run in turns over the same workspace.
+constexpr int64_t kCutChunks = 8192;
+static int64_t cut_rows(bool bf16, int64_t rows, int V) {
+  const int64_t most = kCutChunks / head_plan(bf16, kCutChunks, V).chunks;
+  return rows < most ? rows : most;
+}
+// Above this many rows the lists are handled by small workgroups, four to a CU, and a third launch
+// takes the rows that they leave; up to it one launch of large ones does both.
+constexpr int64_t kCombinedRows = 256;
+constexpr int kListThreads = 256;
 
-size_t cut_ws_bytes(bool bf16, int64_t rows, int V) {
-  const int64_t n = rows < kCutRows ? rows : kCutRows;
-  // The lists of a row hold kListMax entries whatever its chunks; small chunks are more.
-  const HeadPlan one = head_plan(bf16, 0, V), many = head_plan(bf16, kCutRows, V);
-  const size_t chunks = size_t(one.chunks > many.chunks ? one.chunks : many.chunks);
-  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * chunks * sizeof(HeadStat));
+size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
+  const int64_t n = cut_rows(bf16, rows, V);
+  // The lists of a row hold kListMax entries whatever its chunks.  Small chunks are more of them, but
+  // only of few rows.
+  int64_t chunks = n * head_plan(bf16, kCutChunks, V).chunks;
+  const int64_t few = n < device_cu_count() ? n : device_cu_count();
+  const HeadPlan fine = head_plan(bf16, 0, V);
+  const int64_t fine_chunks = few * fine.chunks;
+  chunks = chunks > fine_chunks ? chunks : fine_chunks;
+  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * 4) + al256(size_t(chunks) * sizeof(HeadStat)) +
+         (top ? 0 : al256(size_t(chunks) * kMassBins * 8));
 }
 
 template <typename T, bool TOP>
 static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
-  for (int64_t r0 = 0; r0 < all.rows; r0 += kCutRows) {
+  const bool bf16 = sizeof(T) == 2;
+  const int64_t most = cut_rows(bf16, all.rows, all.V);
+  for (int64_t r0 = 0; r0 < all.rows; r0 += most) {
     CutArgs a = all;
-    a.rows = all.rows - r0 < kCutRows ? all.rows - r0 : kCutRows;
+    a.rows = all.rows - r0 < most ? all.rows - r0 : most;
     a.row0 = r0;
-    const HeadPlan pl = head_plan(sizeof(T) == 2, a.rows, a.V);
+    const HeadPlan pl = head_plan(bf16, a.rows, a.V);
+    char* p = static_cast<char*>(ws);
+    auto take = [&](size_t bytes) {
+      char* q = p;
+      p += al256(bytes);
+      return q;
+    };
     HeadArgs h;
     h.chunks = pl.chunks;
     h.cap = kListMax / pl.chunks;
     h.vectors = pl.elems * kHeadThreads / LogitRow<T>::N;
-    h.list = static_cast<uint64_t*>(ws);
-    h.stats = reinterpret_cast<HeadStat*>(static_cast<char*>(ws) + al256(size_t(a.rows) * kListMax * 8));
-    const dim3 grid(unsigned(a.rows) * pl.chunks);
+    h.list = reinterpret_cast<uint64_t*>(take(size_t(a.rows) * kListMax * 8));
+    h.pending = reinterpret_cast<int32_t*>(take(size_t(a.rows) * 4));
+    h.stats = reinterpret_cast<HeadStat*>(take(size_t(a.rows) * pl.chunks * sizeof(HeadStat)));
+    h.mass = reinterpret_cast<uint64_t*>(p);
+    const dim3 grid(unsigned(a.rows) * pl.chunks), rows(unsigned(a.rows));
     if (pl.elems == 8)
       hipLaunchKernelGGL((row_head_kernel<T, 8, TOP>), grid, dim3(kHeadThreads), 0, s, a, h);
     else
       hipLaunchKernelGGL((row_head_kernel<T, 32, TOP>), grid, dim3(kHeadThreads), 0, s, a, h);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((row_cut_kernel<T, TOP>), dim3(unsigned(a.rows)), dim3(kCutThreads), 0, s, a, h);
+    if (a.rows > kCombinedRows) {
+      hipLaunchKernelGGL((row_cut_kernel<T, TOP, kListThreads, true>), rows, dim3(kListThreads), 0, s, a, h);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    } else {
+      h.pending = nullptr;
+    }
+    hipLaunchKernelGGL((row_cut_kernel<T, TOP, kCutThreads, false>), rows, dim3(kCutThreads), 0, s, a, h);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -1086,7 +1408,7 @@ static int verify_parts(bool bf16, int V) {
 
 size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V) {
   const size_t rows = size_t(n_seq) * (K + 1);
-  return cut_ws_bytes(bf16, int64_t(rows), V) + al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
+  return cut_ws_bytes(bf16, int64_t(rows), V, false) + al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
          al256(size_t(n_seq) * verify_parts(bf16, V) * 16);
 }
 
@@ -1118,7 +1440,7 @@ hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs
   a.t_logit = c.cut_logit;
   a.t_index = c.cut_index;
   a.t_lse = c.lse;
-  const hipError_t e = launch_truncate(target_bf16, c, take(cut_ws_bytes(target_bf16, int64_t(rows), a.V)), s);
+  const hipError_t e = launch_truncate(target_bf16, c, take(cut_ws_bytes(target_bf16, int64_t(rows), a.V, false)), s);
   if (e != hipSuccess) return e;
   if (draft_bf16)
     return target_bf16 ? launch_verify<bf16_t, bf16_t>(a, n_seq, parts, s)

@@ -41,13 +41,13 @@ def _value(x, r, per):
     return x if not torch.is_tensor(x) else x[r // per].item()
 
 
-def _check_draws(z, u=None, per=1, **kw):
+def _check_draws(z, u=None, per=1, rows=None, **kw):
+    """rows: those to compare (all)."""
     tok, cut = hdf.sample_truncated(z, u, rows_per_seq=per, **kw)
     torch.cuda.synchronize()
-    zn = _np(z)
-    for r in range(z.shape[0]):
+    for r in range(z.shape[0]) if rows is None else rows:
         s = {k: _value(v, r, per) for k, v in kw.items()}
-        n, cl, ci, lse, p = tr.truncate(zn[r], **s)
+        n, cl, ci, lse, p = tr.truncate(_np(z[r]), **s)
         assert int(cut.kept[r]) == n, (r, s)
         assert float(cut.cut_logit[r]) == cl and int(cut.cut_index[r]) == ci, (r, s)
         got = float(cut.lse[r])
@@ -164,6 +164,57 @@ def test_many_equal_entries():
     for kw in (dict(), dict(top_p=0.5), dict(top_k=30001), dict(top_k=1), dict(min_p=1.0),
                dict(top_k=50000, top_p=0.25), dict(temperature=1e-4, top_p=0.7)):
         _check_draws(z, _u(6, 2), **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_nuclei_wider_than_the_lists(dtype):
+    """Thousands of kept entries, cuts in bins of a few and of thousands of entries, with and without
+    min_p above or below them."""
+    z = _logits(3, 200003, 41, dtype, "flat")
+    z[2, :150000] = -np.inf
+    for kw in (dict(temperature=1.5, top_p=0.5), dict(temperature=3.0, top_p=0.9),
+               dict(temperature=1.0, top_p=0.999), dict(temperature=30.0, top_p=0.3),
+               dict(top_p=0.9, min_p=0.001), dict(top_p=0.9, min_p=0.02), dict(min_p=0.01),
+               dict(top_k=70000, top_p=0.6), dict(top_k=5000, min_p=0.03)):
+        _check_draws(z, _u(3, 5), **kw)
+
+
+def test_many_rows():
+    """More rows than one launch of large workgroups takes: lists in small ones, the rest after."""
+    n, V = 300, 6007
+    z = _logits(n, V, 17)
+    z[100:200] = _logits(100, V, 18, kind="flat")
+    z[7] = -np.inf
+    z[8] = 1.0
+    g = torch.Generator().manual_seed(3)
+
+    def pick(values, dtype):
+        return torch.tensor(values, dtype=dtype)[torch.randint(0, len(values), (n // 3,), generator=g)
+                                                 ].to(DEV)
+    _check_draws(z, _u(n, 2), per=3, temperature=pick([0.0, 0.7, 1.0, 1.5], torch.float32),
+                 top_k=pick([0, 0, 10, 200, 4000], torch.int32),
+                 top_p=pick([1.0, 0.9, 0.99, 0.5], torch.float32),
+                 min_p=pick([0.0, 0.0, 0.05], torch.float32))
+    _check_draws(z, None, top_p=0.8)
+    ids, values, rest = hdf.top_logits(z, 40)
+    for r in range(n):
+        i, v, s = tr.top_logits(_np(z[r]), 40)
+        assert ids[r].tolist() == i.tolist() and _np(values[r]).tolist() == v.tolist(), r
+        assert float(rest[r]) == s or abs(float(rest[r]) - s) <= 2e-7 * max(1.0, abs(s)), r
+
+
+def test_rows_in_several_groups_of_launches():
+    """So many long rows that they run in turns over one workspace."""
+    V, n = 1 << 20, 131
+    z = torch.randn(n, V, generator=torch.Generator(DEV).manual_seed(3), device=DEV,
+                    dtype=torch.float32).mul_(2).to(torch.bfloat16)
+    rows = (0, 1, 125, 126, 127, 130)
+    _check_draws(z, _u(n, 1), rows=rows, temperature=0.8, top_p=0.7)
+    _check_draws(z, _u(n, 2), rows=rows, top_k=30)
+    ids, values, _ = hdf.top_logits(z, 17)
+    for r in rows:
+        i, v, _ = tr.top_logits(_np(z[r]), 17)
+        assert ids[r].tolist() == i.tolist()
 
 
 def test_uniforms_at_and_past_the_ends():
