@@ -70,26 +70,34 @@ __device__ __forceinline__ int entry_column(uint64_t k) {
   return int(kColumnMask - (uint32_t(k) & kColumnMask));
 }
 
+// a * b + k with k the same for all lanes: a scalar operand.  (The compiler would copy k into the
+// result first, two moves a product, and take three times as long over a series.)
+__device__ __forceinline__ double fma_k(double a, double b, double k) {
+  double d;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(k));
+  return d;
+}
+
 // 2^t in 64 bits for t <= 0 (and the few ulps above it that rounding leaves): 2^n times the
 // exponential series of f ln 2, |f| <= 1/2, whose first dropped term is 0.35^12 / 12! = 6e-15.
 // Which entry a draw or a cut falls on is decided by sums of these; with 32-bit exponentials one
-// row in a few thousand fell on a neighbour.
+// row in a few thousand would fall on a neighbour.
 __device__ __forceinline__ double exp2_64(double t) {
   t = fmax(t, -1100.);   // below the least double; also what an infinite difference gives
   const double n = rint(t);
   const double x = (t - n) * 0.69314718055994530942;
   double p = 1. / 39916800.;
-  p = fma(p, x, 1. / 3628800.);
-  p = fma(p, x, 1. / 362880.);
-  p = fma(p, x, 1. / 40320.);
-  p = fma(p, x, 1. / 5040.);
-  p = fma(p, x, 1. / 720.);
-  p = fma(p, x, 1. / 120.);
-  p = fma(p, x, 1. / 24.);
-  p = fma(p, x, 1. / 6.);
-  p = fma(p, x, 0.5);
-  p = fma(p, x, 1.);
-  p = fma(p, x, 1.);
+  p = fma_k(p, x, 1. / 3628800.);
+  p = fma_k(p, x, 1. / 362880.);
+  p = fma_k(p, x, 1. / 40320.);
+  p = fma_k(p, x, 1. / 5040.);
+  p = fma_k(p, x, 1. / 720.);
+  p = fma_k(p, x, 1. / 120.);
+  p = fma_k(p, x, 1. / 24.);
+  p = fma_k(p, x, 1. / 6.);
+  p = fma_k(p, x, 0.5);
+  p = fma_k(p, x, 1.);
+  p = fma_k(p, x, 1.);
   return ldexp(p, int(n));
 }
 

@@ -96,12 +96,12 @@ __device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, int& n) {
   const double g = fma(double(z), k16, -(t - 6755399441055744.));
   constexpr double c = 0.69314718055994530942 / 16.;
   double p = c * c * c * c * c * c / 720.;
-  p = fma(p, g, c * c * c * c * c / 120.);
-  p = fma(p, g, c * c * c * c / 24.);
-  p = fma(p, g, c * c * c / 6.);
-  p = fma(p, g, c * c / 2.);
-  p = fma(p, g, c);
-  p = fma(p, g, 17.);   // 16 + 1: a unit of 16's last place is 2^-48
+  p = fma_k(p, g, c * c * c * c * c / 120.);
+  p = fma_k(p, g, c * c * c * c / 24.);
+  p = fma_k(p, g, c * c * c / 6.);
+  p = fma_k(p, g, c * c / 2.);
+  p = fma_k(p, g, c);
+  p = fma_k(p, g, 17.);   // 16 + 1: a unit of 16's last place is 2^-48
   return __builtin_bit_cast(uint64_t, p) - 0x4030000000000000ull;
 }
 
@@ -122,6 +122,11 @@ struct CutShared {
     double group[W][kMaxGroups];
   };
   double chunk[kMaxChunks];
+  struct {
+    int listed, top_bin, bins;
+    float rest_ref;
+    double rest;
+  } part[kMaxChunks];   // of the chunks' statistics
   union {
     double d[W];
     uint64_t u[W];
@@ -484,11 +489,12 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     for (int e = 0; e < N; ++e) top = fmaxf(top, x[g][e]);
   const float m = block_fold<kHeadWaves>(top, red.f, most);
   if (top == m && m > -INFINITY) {
+    int first = a.V;
 #pragma unroll
     for (int g = G - 1; g >= 0; --g)
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (x[g][e] == m) atomicMin(&best_col, col(g, e));
+      for (int e = N - 1; e >= 0; --e) first = x[g][e] == m ? col(g, e) : first;
+    atomicMin(&best_col, first);
   }
   const uint32_t valid = count_of(0, [](float z) { return z > -INFINITY; });
 
@@ -548,7 +554,10 @@ row_head_kernel(CutArgs a, HeadArgs h) {
           const unsigned long long who = __ballot(is);
           if (who != 0ull) {
             const uint32_t k = __popcll(who & ((1ull << lane) - 1));
-            if (is) list[before + k] = entry_key(x[g][e], col(g, e));
+            if (is) {
+              list[before + k] = entry_key(x[g][e], col(g, e));
+              if constexpr (TOP) x[g][e] = -INFINITY;   // what stays is unlisted
+            }
             before += uint32_t(__popcll(who));
           }
         }
@@ -568,12 +577,11 @@ row_head_kernel(CutArgs a, HeadArgs h) {
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (x[g][e] >= end && x[g][e] > -INFINITY) {
-            int n;
-            const uint64_t w = weight_in_bin(x[g][e], k16, n);
-            const int b = st.top_bin - n;
-            if (b >= 0 && b < kMassBins) atomicAdd(&mass[b], static_cast<unsigned long long>(w));
-          }
+        {
+          int n;   // of top_bin - 993 .. top_bin
+          const uint64_t w = weight_in_bin(fmaxf(x[g][e], end), k16, n);
+          if (x[g][e] >= end) atomicAdd(&mass[st.top_bin - n], static_cast<unsigned long long>(w));
+        }
       __syncthreads();
       uint32_t end_bin = 0;
       for (int b = tid; b < kMassBins; b += kHeadThreads)
@@ -588,7 +596,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   } else if (TOP && a.rest != nullptr && valid > listed) {
     // The others of the top logits: 32-bit exponentials, as their logarithm is stored in 32 bits.
     // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.
-    const float c2 = float(s.c2);
+    const float c2 = fminf(float(s.c2), 3e38f);
     for (int turn = 0; turn < 2; ++turn) {
       st.rest_ref = lo;
       if (turn == 1 || !(lo < INFINITY)) {
@@ -596,18 +604,14 @@ row_head_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e] >= lo ? -INFINITY : x[g][e]);
+          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e]);
         st.rest_ref = block_fold<kHeadWaves>(g_top, red.f, most);
       }
       float f = 0.f;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float d = x[g][e] == st.rest_ref ? 0.f : (x[g][e] - st.rest_ref) * c2;
-          const float w = __builtin_amdgcn_exp2f(d);
-          f += x[g][e] >= lo ? 0.f : w;
-        }
+        for (int e = 0; e < N; ++e) f += __builtin_amdgcn_exp2f((x[g][e] - st.rest_ref) * c2);
       st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
       if (st.rest > 1e-25 || !(lo < INFINITY)) break;
     }
@@ -673,6 +677,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     int top_bin = -2147483647, bins = 0;
     for (int c = lane; c < h.chunks; c += 64) {
       const HeadStat st = hs[c];
+      sh.part[c] = {int(st.listed), st.top_bin, st.bins, st.rest_ref, st.rest};
       if (st.valid == 0) continue;
       const uint64_t k = entry_key(st.best, st.best_col);
       best = k > best ? k : best;
@@ -721,22 +726,25 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     return;
   }
 
-  // Calls f(key) for every listed entry, a wave a chunk.
-  auto each_listed = [&](auto f) {
-    for (int c = wid; c < h.chunks; c += W) {
-      const int n = int(hs[c].listed);
-      const uint64_t* list = h.list + (at * h.chunks + c) * h.cap;
-      for (int i = lane; i < n; i += 64) f(list[i]);
+  // The listed entries, all in flight together: this thread's places of the row's lists.
+  constexpr int LISTED = kListMax / NT;
+  uint64_t mine[LISTED];
+  {
+    const uint64_t* list = h.list + at * h.chunks * h.cap;
+#pragma unroll
+    for (int q = 0; q < LISTED; ++q) {
+      const int i = q * NT + tid, c = i / h.cap;
+      mine[q] = c < h.chunks && i - c * h.cap < sh.part[c].listed ? list[i] : 0ull;
     }
-  };
-  // The listed entries of value >= t, sorted; all of the row's where t >= floor.
+  }
+  // Those of value >= t into the list; all of the row's where t >= floor.
   auto gather = [&](float t) {
     __syncthreads();
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    each_listed([&](uint64_t k) {
-      if (entry_logit(k) >= t) sh.list[atomicAdd(&sh.n, 1u)] = k;
-    });
+#pragma unroll
+    for (int q = 0; q < LISTED; ++q)
+      if (mine[q] != 0 && entry_logit(mine[q]) >= t) sh.list[atomicAdd(&sh.n, 1u)] = mine[q];
     __syncthreads();
     const int n = int(sh.n);
     __syncthreads();
@@ -786,16 +794,17 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         const uint64_t last = n > 0 ? sh.list[n - 1] : 0;
         uint64_t next = 0;
         float ref = -INFINITY;
-        each_listed([&](uint64_t k) { next = k < last ? most64(next, k) : next; });
-        if (tid < h.chunks && hs[tid].rest > 0.) ref = hs[tid].rest_ref;
+#pragma unroll
+        for (int q = 0; q < LISTED; ++q) next = mine[q] < last ? most64(next, mine[q]) : next;
+        if (tid < h.chunks && sh.part[tid].rest > 0.) ref = sh.part[tid].rest_ref;
         ref = fmaxf(ref, next != 0 ? entry_logit(next) : -INFINITY);
         ref = block_fold<W>(ref, sh.red.f, [](float u, float v) { return fmaxf(u, v); });
         double sum = 0.;
-        each_listed([&](uint64_t k) {
-          if (k < last) sum += entry_weight(entry_logit(k), ref, s.c2);
-        });
-        if (tid < h.chunks && hs[tid].rest > 0.)
-          sum += hs[tid].rest * entry_weight(hs[tid].rest_ref, ref, s.c2);
+#pragma unroll
+        for (int q = 0; q < LISTED; ++q)
+          if (mine[q] != 0 && mine[q] < last) sum += entry_weight(entry_logit(mine[q]), ref, s.c2);
+        if (tid < h.chunks && sh.part[tid].rest > 0.)
+          sum += sh.part[tid].rest * entry_weight(sh.part[tid].rest_ref, ref, s.c2);
         sum = block_fold<W>(sum, sh.red.d, add);
         if (tid == 0)
           a.rest[row] = ref > -INFINITY ? float(double(ref) * s.inv_t + log(sum)) : -INFINITY;
@@ -827,8 +836,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     const double unit =
         binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * 3.552713678800501e-15 : 0.;   // 2^-48
     auto mass_at = [&](int c, int b) -> uint64_t {   // of chunk c in the row's bin b
-      const int i = b - (top_bin - hs[c].top_bin);
-      return i >= 0 && i < hs[c].bins ? h.mass[(at * h.chunks + c) * kMassBins + i] : 0ull;
+      const int i = b - (top_bin - sh.part[c].top_bin);
+      return i >= 0 && i < sh.part[c].bins ? h.mass[(at * h.chunks + c) * kMassBins + i] : 0ull;
     };
     if (binned) {
       constexpr int PER = kMassBins / NT;
@@ -837,8 +846,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       for (int e = 0; e < PER; ++e) {
         const int b = PER * tid + e;
         double n = 0.;
-        for (int c = 0; c < h.chunks; ++c)
-          if (hs[c].valid > 0) n += double(mass_at(c, b));
+#pragma unroll 8
+        for (int c = 0; c < h.chunks; ++c) n += double(mass_at(c, b));
         v[e] = n * bin_weight(b) * unit;
         sum += v[e];
       }
@@ -876,7 +885,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
 
     if (s.open) {
       // Everything is kept: the chunks' sums are the masses, and only the chunk drawn is read.
-      const double w = tid < h.chunks ? hs[tid].rest * entry_weight(hs[tid].rest_ref, m, s.c2) : 0.;
+      const double w =
+          tid < h.chunks ? sh.part[tid].rest * entry_weight(sh.part[tid].rest_ref, m, s.c2) : 0.;
       const double run = block_scan<W>(w, sh.red.d, mass);
       if constexpr (LISTS) {
         if (a.tok != nullptr) {
@@ -1011,9 +1021,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
                 // The chunks' masses: their bins above the border, and their part of its entries.
                 for (int c = wid; c < h.chunks; c += W) {
                   double w = 0.;
-                  if (hs[c].valid > 0)
-                    for (int b = lane; b < border; b += 64)
-                      w += double(mass_at(c, b)) * bin_weight(b) * unit;
+                  for (int b = lane; b < border; b += 64)
+                    w += double(mass_at(c, b)) * bin_weight(b) * unit;
                   for (int i = lane; i < n; i += 64) {
                     const uint64_t k = sh.list[i];
                     const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
