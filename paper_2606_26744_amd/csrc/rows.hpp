@@ -21,20 +21,28 @@ struct LogitRow {
   }
   __device__ __forceinline__ int vectors() const { return (V + shift + N - 1) / N; }
   __device__ __forceinline__ int column(int j) const { return j * N - shift; }
+  // Whether vectors j .. j + n - 1 lie within the row.
+  __device__ __forceinline__ bool inside(int j, int n) const {
+    return column(j) >= 0 && column(j + n) <= V;
+  }
+  // Vector j, which lies within the row.
+  __device__ __forceinline__ void load_inside(int j, float x[N]) const {
+    const u32x4 v = ld16(p + column(j));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 2) {
+        x[2 * e] = lo_bf(v[e]);
+        x[2 * e + 1] = hi_bf(v[e]);
+      } else {
+        x[e] = __uint_as_float(v[e]);
+      }
+    }
+  }
   // Vector j as fp32; columns outside the row are -inf.
   __device__ __forceinline__ void load_raw(int j, float x[N]) const {
     const int c = column(j);
     if (c >= 0 && c + N <= V) {
-      const u32x4 v = ld16(p + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2) {
-          x[2 * e] = lo_bf(v[e]);
-          x[2 * e + 1] = hi_bf(v[e]);
-        } else {
-          x[e] = __uint_as_float(v[e]);
-        }
-      }
+      load_inside(j, x);
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e) x[e] = c + e >= 0 && c + e < V ? raw(c + e) : -INFINITY;
@@ -108,12 +116,56 @@ __device__ __forceinline__ double entry_weight(float z, float m, double c2) {
   return z == m ? 1. : exp2_64((double(z) - double(m)) * c2);
 }
 
-// Sums over a workgroup of W waves in a fixed order; every thread gets the result.  `sh` holds W
-// values and is free again when the next barrier has passed.
+// Another lane's value within the row of 16 (a DPP move; 64-bit values in two).
+template <int CTRL, int ROWS, typename X>
+__device__ __forceinline__ X dpp(X v) {
+  constexpr int D = sizeof(X) / 4;
+  int w[D];
+  __builtin_memcpy(w, &v, sizeof(X));
+#pragma unroll
+  for (int i = 0; i < D; ++i) w[i] = __builtin_amdgcn_update_dpp(0, w[i], CTRL, ROWS, 0xf, true);
+  __builtin_memcpy(&v, w, sizeof(X));
+  return v;
+}
+template <typename X>
+__device__ __forceinline__ X read_lane(X v, int lane) {
+  constexpr int D = sizeof(X) / 4;
+  int w[D];
+  __builtin_memcpy(w, &v, sizeof(X));
+#pragma unroll
+  for (int i = 0; i < D; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
+  __builtin_memcpy(&v, w, sizeof(X));
+  return v;
+}
+
+// All lanes' values under f (commutative, associative but for rounding), the same to every lane:
+// within rows of 16 by moves between lanes, then the four rows.  The whole wave takes part.
+template <typename X, typename F>
+__device__ __forceinline__ X wave_fold(X v, F f) {
+  v = f(v, dpp<0xB1, 0xf>(v));    // lanes 1 apart
+  v = f(v, dpp<0x4E, 0xf>(v));    // 2 apart
+  v = f(v, dpp<0x141, 0xf>(v));   // mirrored in 8
+  v = f(v, dpp<0x140, 0xf>(v));   // mirrored in 16
+  return f(f(read_lane(v, 0), read_lane(v, 16)), f(read_lane(v, 32), read_lane(v, 48)));
+}
+
+// Inclusive running sum over a wave's lanes.
+template <typename X>
+__device__ __forceinline__ X wave_scan(X v) {
+  v += dpp<0x111, 0xf>(v);   // from 1, 2, 4, 8 lanes before in the row, zero past its start
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);   // the last lane of rows 0 and 2 to rows 1 and 3
+  v += dpp<0x143, 0xc>(v);   // lane 31 to rows 2 and 3
+  return v;
+}
+
+// f over a workgroup of W waves in a fixed order; every thread gets the result.  `sh` holds W values
+// and is free again on return.
 template <int W, typename X, typename F>
 __device__ __forceinline__ X block_fold(X v, X* sh, F f) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, kWave));
+  v = wave_fold(v, f);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   X t = sh[0];
@@ -127,11 +179,7 @@ __device__ __forceinline__ X block_fold(X v, X* sh, F f) {
 template <int W, typename X>
 __device__ __forceinline__ X block_scan(X v, X* sh, X& total) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const X y = __shfl_up(v, o, kWave);
-    if (lane >= o) v += y;
-  }
+  v = wave_scan(v);
   if (lane == 63) sh[wid] = v;
   __syncthreads();
   X before = X(0), all = X(0);

@@ -17,7 +17,6 @@ constexpr int kCutThreads = 1024;
 constexpr int kCutWaves = kCutThreads / kWave;
 constexpr int kBins = 2 * kCutThreads;
 constexpr int kListMax = 2 * kCutThreads;      // entries sorted at once
-constexpr int kAhead = 16;                     // entries a thread loads before it uses them
 constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
 constexpr double kMassUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
@@ -30,6 +29,7 @@ constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 constexpr int kHeadThreads = 512;
 constexpr int kHeadWaves = kHeadThreads / kWave;
 constexpr int kMaxChunks = 66;
+constexpr float kLeast = -3.402823466e38f;   // the least finite value
 
 // The nucleus histogram: bins of 1/16 octave of weight.  Entry z has t = 16 z log2(e) / T, bin
 // n = rint(t) and within it the weight 2^((t - n) / 16), 0.978 .. 1.022, as a multiple of 2^-48;
@@ -46,17 +46,18 @@ struct HeadStat {
   uint32_t listed;
   int32_t top_bin;   // bin of the greatest value, and how many bins from it down are stored
   int32_t bins;      // (-1: values beyond the bins' range)
-  float rest_ref;    // rest: sum of e^((z - rest_ref) / T) over the unlisted entries
-  float pad;
+  double rest_ref;   // rest: sum of e^((z - rest_ref) / T) over the unlisted entries
   double rest;
 };
+
+struct CutNote;   // what one phase of a row's cut leaves for the next
 
 struct HeadArgs {
   int chunks, cap, vectors;   // of a row; entries a chunk may list; vectors of a chunk
   uint64_t* list;             // [rows][chunks][cap]
   HeadStat* stats;            // [rows][chunks]
   uint64_t* mass;             // [rows][chunks][kMassBins]
-  int32_t* pending;           // [rows] rows left to the third launch, or NULL
+  CutNote* notes;             // [rows]
 };
 
 // A row's settings.
@@ -105,7 +106,7 @@ __device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, int& n) {
   return __builtin_bit_cast(uint64_t, p) - 0x4030000000000000ull;
 }
 
-template <int NT>
+template <int NT, bool SEARCH = true>
 struct CutShared {
   static constexpr int W = NT / kWave;
   union {
@@ -113,8 +114,8 @@ struct CutShared {
       uint64_t list[kListMax];
       union {
         struct {
-          uint64_t mass[kBins];
-          uint32_t count[kBins];
+          uint64_t mass[SEARCH ? kBins : 1];
+          uint32_t count[SEARCH ? kBins : 1];
         };
         double weight[kListMax];
       };
@@ -124,8 +125,7 @@ struct CutShared {
   double chunk[kMaxChunks];
   struct {
     int listed, top_bin, bins;
-    float rest_ref;
-    double rest;
+    double rest_ref, rest;
   } part[kMaxChunks];   // of the chunks' statistics
   union {
     double d[W];
@@ -141,34 +141,39 @@ struct CutShared {
 };
 
 // Calls f(group, value, column) for every unmasked entry of vectors j0 .. j1-1 of the row; group g
-// is the g-th run of kCutThreads of them, and after(g) follows a group's entries with all lanes
-// together.
-template <typename T, typename F, typename G>
+// is the g-th run of NT of them, and after(g) follows a group's entries with all lanes together.  A
+// thread has AHEAD entries in flight.
+template <int NT, int AHEAD, typename T, typename F, typename G>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1, F f, G after) {
-  constexpr int N = LogitRow<T>::N, Q = kAhead / N;
-  for (int b = 0; j0 + b < j1; b += Q * kCutThreads) {
+  constexpr int N = LogitRow<T>::N, Q = AHEAD / N;
+  for (int b = 0; j0 + b < j1; b += Q * NT) {
     float x[Q][N];
+    if (j0 + b + Q * NT <= j1 && r.inside(j0 + b, Q * NT)) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const int j = j0 + b + q * kCutThreads + int(threadIdx.x);
+      for (int q = 0; q < Q; ++q) r.load_inside(j0 + b + q * NT + int(threadIdx.x), x[q]);
+    } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
-      if (j < j1) r.load(j, x[q]);
+      for (int q = 0; q < Q; ++q) {
+        const int j = j0 + b + q * NT + int(threadIdx.x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
+        if (j < j1) r.load_raw(j, x[q]);
+      }
     }
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int g = b / kCutThreads + q;
-      const int c = r.column(j0 + g * kCutThreads + int(threadIdx.x));
+      const int g = b / NT + q;
+      const int c = r.column(j0 + g * NT + int(threadIdx.x));
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (x[q][e] > -INFINITY) f(g, x[q][e], c + e);
-      if (j0 + g * kCutThreads < j1) after(g);
+        if (x[q][e] > -INFINITY) f(g, x[q][e], c + e);   // false for NaN
+      if (j0 + g * NT < j1) after(g);
     }
   }
 }
 template <typename T, typename F>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
-  each_entry(r, 0, r.vectors(), f, [](int) {});
+  each_entry<kCutThreads, 16>(r, 0, r.vectors(), f, [](int) {});
 }
 
 // The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
@@ -346,15 +351,15 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
 
 // The weights of a row's kept entries (keys >= cut) among vectors j0 .. j1-1, a group and wave a
 // sum in sh.group; returns their whole, `run` this thread's group's running sum and `mine` its own.
-template <typename T>
+template <int NT, bool S, typename T>
 __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int j1, uint64_t cut,
-                                              float m, double c2, CutShared<kCutThreads>& sh,
+                                              float m, double c2, CutShared<NT, S>& sh,
                                               uint32_t& kept,
                                               uint64_t& low, double& run, double& mine) {
   kept = 0;
   low = kKeyTop;
   double s = 0.;
-  each_entry(
+  each_entry<NT, 16>(
       r, j0, j1,
       [&](int, float z, int c) {
         const uint64_t k = entry_key(z, c);
@@ -369,23 +374,23 @@ __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int 
         s = 0.;
       });
   __syncthreads();
-  const int groups = (j1 - j0 + kCutThreads - 1) / kCutThreads;
+  const int groups = (j1 - j0 + NT - 1) / NT;
   mine = 0.;
   if (int(threadIdx.x) < groups)
-    for (int w = 0; w < kCutWaves; ++w) mine += sh.group[w][threadIdx.x];
+    for (int w = 0; w < NT / kWave; ++w) mine += sh.group[w][threadIdx.x];
   double all;
-  run = block_scan<kCutWaves>(mine, sh.red.d, all);
+  run = block_scan<NT / kWave>(mine, sh.red.d, all);
   return all;
 }
 
 // The draw among the kept entries of vectors j0 .. j1-1, after kept_masses: the group in which
 // `base` and the running sum pass the target, then the entry; the last one where rounding leaves
 // none.
-template <typename T>
+template <int NT, bool S, typename T>
 __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
                                           double c2, double base, double target, double run,
-                                          double mine, CutShared<kCutThreads>& sh) {
-  if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = 0;
+                                          double mine, CutShared<NT, S>& sh) {
+  if (threadIdx.x == 0) sh.pick = NT, sh.last = 0;
   __syncthreads();
   if (mine > 0.) {
     if (base + run > target) atomicMin(&sh.pick, int(threadIdx.x));
@@ -395,9 +400,9 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
   const int g = min(sh.pick, sh.last);
   __syncthreads();
   if (int(threadIdx.x) == g) sh.sum = base + (run - mine);
-  if (threadIdx.x == 0) sh.pick = kCutThreads, sh.last = -1;
+  if (threadIdx.x == 0) sh.pick = NT, sh.last = -1;
   __syncthreads();
-  const int j = j0 + g * kCutThreads + int(threadIdx.x), c = r.column(j);
+  const int j = j0 + g * NT + int(threadIdx.x), c = r.column(j);
   float x[LogitRow<T>::N];
   double own = 0., all;
 #pragma unroll
@@ -414,7 +419,7 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
       atomicMax(&sh.last, c + e);
     }
   }
-  const double upto = sh.sum + block_scan<kCutWaves>(own, sh.red.d, all);
+  const double upto = sh.sum + block_scan<NT / kWave>(own, sh.red.d, all);
   if (own > 0. && upto > target) atomicMin(&sh.pick, int(threadIdx.x));
   __syncthreads();
   const int who = sh.pick;
@@ -432,6 +437,13 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
   }
   __syncthreads();
   return sh.last;
+}
+
+// The greatest of three values, none of them NaN.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
 }
 
 // A chunk of a row: E entries a thread.
@@ -454,12 +466,17 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const int j0 = chunk * G * kHeadThreads, nv = r.vectors();
   float x[G][N];
+  if (r.inside(j0, G * kHeadThreads)) {   // all but a row's first and last chunk
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int j = j0 + g * kHeadThreads + tid;
+    for (int g = 0; g < G; ++g) r.load_inside(j0 + g * kHeadThreads + tid, x[g]);
+  } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
-    if (j < nv) r.load(j, x[g]);
+    for (int g = 0; g < G; ++g) {
+      const int j = j0 + g * kHeadThreads + tid;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+      if (j < nv) r.load_raw(j, x[g]);
+    }
   }
   const RowSettings s = settings_of<TOP>(a, row);
   auto col = [&](int g, int e) { return r.column(j0 + g * kHeadThreads + tid) + e; };
@@ -467,27 +484,40 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   auto most = [](float u, float v) { return fmaxf(u, v); };
   auto least = [](float u, float v) { return fminf(u, v); };
   // Entries for which `of` holds, over the workgroup: counted by the scalar unit.
-  auto count_of = [&](int which, auto of) {
+  auto count_of = [&](auto of) {
     uint32_t n = 0;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < N; ++e) n += uint32_t(__popcll(__ballot(of(x[g][e]))));
-    if (lane == 0) wave_n[which][wid] = n;
+    if (lane == 0) wave_n[1][wid] = n;
     __syncthreads();
     uint32_t all = 0;
 #pragma unroll
-    for (int w = 0; w < kHeadWaves; ++w) all += wave_n[which][w];
+    for (int w = 0; w < kHeadWaves; ++w) all += wave_n[1][w];
     return all;
   };
 
-  if (tid == 0) best_col = a.V;
+  // Unmasked entries (NaN is masked: no comparison holds for it), the greatest one.
+  uint32_t live = 0;
   float top = -INFINITY;
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < N; ++e) top = fmaxf(top, x[g][e]);
+    for (int e = 0; e < N; e += 2) {
+      // (A ballot of "> -inf" comes out as "unequal or NaN" here: the least value instead.)
+      const bool is0 = x[g][e] >= kLeast, is1 = x[g][e + 1] >= kLeast;
+      live += uint32_t(__popcll(__ballot(is0))) + uint32_t(__popcll(__ballot(is1)));
+      x[g][e] = is0 ? x[g][e] : -INFINITY;
+      x[g][e + 1] = is1 ? x[g][e + 1] : -INFINITY;
+      top = max3(top, x[g][e], x[g][e + 1]);
+    }
+  if (tid == 0) best_col = a.V;
+  if (lane == 0) wave_n[0][wid] = live;
   const float m = block_fold<kHeadWaves>(top, red.f, most);
+  uint32_t valid = 0;
+#pragma unroll
+  for (int w = 0; w < kHeadWaves; ++w) valid += wave_n[0][w];
   if (top == m && m > -INFINITY) {
     int first = a.V;
 #pragma unroll
@@ -496,7 +526,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
       for (int e = N - 1; e >= 0; --e) first = x[g][e] == m ? col(g, e) : first;
     atomicMin(&best_col, first);
   }
-  const uint32_t valid = count_of(0, [](float z) { return z > -INFINITY; });
+  __syncthreads();
 
   // The list: all entries >= lo, lo a thread's greatest value such that `want` threads reach it; so
   // at least `want` entries do, and hardly more unless the great ones crowd into few threads (then
@@ -526,13 +556,13 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     const uint32_t first = in && mine > 0 ? count[mine - 1] : 0u;   // threads in the bins before
     near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
     if (valid <= uint32_t(h.cap)) {
-      lo = -3.402823466e38f;
+      lo = kLeast;
       listed = valid;
     } else {
       for (; want > 0; want /= 2) {
         lo = block_fold<kHeadWaves>(in && first < uint32_t(want) ? top : INFINITY, red.f, least);
         const float v = lo;
-        listed = count_of(1, [&](float z) { return z >= v; });
+        listed = count_of([&](float z) { return z >= v; });
         if (listed <= uint32_t(h.cap)) break;
         __syncthreads();
       }
@@ -542,7 +572,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
       }
     }
     if (listed > 0) {
-      if (listed == valid) count_of(1, [&](float z) { return z >= lo; });
+      if (listed == valid) count_of([&](float z) { return z >= lo; });
       uint32_t before = 0;
       for (int w = 0; w < wid; ++w) before += wave_n[1][w];
       uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
@@ -564,7 +594,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     }
   }
 
-  HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0.f, 0.f, 0.};
+  HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0., 0.};
   if (s.nucleus && valid > 0) {
     const double k16 = 16. * s.c2;
     const float range = float(992. / k16);   // 62 octaves
@@ -595,23 +625,27 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     }
   } else if (TOP && a.rest != nullptr && valid > listed) {
     // The others of the top logits: 32-bit exponentials, as their logarithm is stored in 32 bits.
-    // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.
+    // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.  The
+    // reference is what the rounded product of lo and log2(e) / T stands for, so that an entry
+    // costs one product, rounded once.
     const float c2 = fminf(float(s.c2), 3e38f);
     for (int turn = 0; turn < 2; ++turn) {
-      st.rest_ref = lo;
+      float ref = lo;
       if (turn == 1 || !(lo < INFINITY)) {
         float g_top = -INFINITY;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
           for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e]);
-        st.rest_ref = block_fold<kHeadWaves>(g_top, red.f, most);
+        ref = block_fold<kHeadWaves>(g_top, red.f, most);
       }
+      const float k = fmaxf(fminf(ref * c2, 3e38f), -3e38f);
       float f = 0.f;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e) f += __builtin_amdgcn_exp2f((x[g][e] - st.rest_ref) * c2);
+        for (int e = 0; e < N; ++e) f += __builtin_amdgcn_exp2f(fmaf(x[g][e], c2, -k));
+      st.rest_ref = double(k) / double(c2);
       st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
       if (st.rest > 1e-25 || !(lo < INFINITY)) break;
     }
@@ -621,7 +655,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < N; ++e) sum += entry_weight(x[g][e], m, s.c2);
-    st.rest_ref = m;
+    st.rest_ref = double(m);
     st.rest = block_fold<kHeadWaves>(sum, red.d, add);
   }
   if (tid == 0) h.stats[at * h.chunks + chunk] = st;
@@ -629,16 +663,16 @@ row_head_kernel(CutArgs a, HeadArgs h) {
 
 // First place, in the order of places 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes)
 // the target, n where none does; `sum_to` gets the sum of the first n_sum of them.
-template <int NT, bool STRICT, typename F>
+template <int NT, bool STRICT, bool S, typename F>
 __device__ __forceinline__ int reach(int n, double target, int n_sum, double& sum_to,
-                                     CutShared<NT>& sh, F w) {
+                                     CutShared<NT, S>& sh, F w) {
   if (threadIdx.x == 0) sh.pick = n;
   double before = 0.;
   for (int b = 0; b < n; b += NT) {
     const int i = b + int(threadIdx.x);
     const double v = i < n ? w(i) : 0.;
     double all;
-    const double run = before + block_scan<CutShared<NT>::W>(v, sh.red.d, all);
+    const double run = before + block_scan<NT / kWave>(v, sh.red.d, all);
     if (i < n && (STRICT ? v > 0. && run > target : run >= target)) atomicMin(&sh.pick, i);
     if (i == n_sum - 1) sh.sum = run;
     before += all;
@@ -650,24 +684,41 @@ __device__ __forceinline__ int reach(int n, double target, int n_sum, double& su
   return at;
 }
 
+// A row's share of the second launch's work.  With few rows one launch of large workgroups does all
+// of it; with many the lists are handled by small ones, several to a CU, and two more launches take
+// what those leave: the rows that need one more pass, and those that need the search.
+enum CutPhase { kAll, kLists, kBorder, kSearch };
+enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
+
+// Between the phases: a nucleus' border bin, the weights above it and in the whole.
+struct CutNote {
+  double whole, above;
+  int32_t border, left;
+};
+
 // One row a workgroup.  TOP: the first K entries and the log-sum-exp of the others; else the
-// truncation and the draw.  LISTS: only rows whose cut lies within the lists; the others are marked
-// as pending.
-template <typename T, bool TOP, int NT, bool LISTS>
+// truncation and the draw.
+template <typename T, bool TOP, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
 row_cut_kernel(CutArgs a, HeadArgs h) {
-  using Shared = CutShared<NT>;
+  constexpr bool LISTS = PHASE == kAll || PHASE == kLists, BORDER = PHASE == kAll || PHASE == kBorder,
+                 SEARCH = PHASE == kAll || PHASE == kSearch;
+  using Shared = CutShared<NT, SEARCH>;
   constexpr int W = Shared::W;
   __shared__ Shared sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  if (!LISTS && h.pending != nullptr && h.pending[at] == 0) return;
+  CutNote* note = h.notes + at;
+  if (PHASE == kBorder && note->left != kLeftBorder) return;
+  if (PHASE == kSearch && note->left != kLeftSearch) return;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const RowSettings s = settings_of<TOP>(a, row);
   const float scale = float(64. * s.inv_t);
-  const HeadStat* hs = h.stats + at * h.chunks;
   auto add = [](auto u, auto v) { return u + v; };
   auto most64 = [](uint64_t u, uint64_t v) { return u > v ? u : v; };
+  auto leave = [&](int left) {
+    if (tid == 0) note->left = left;
+  };
 
   // The chunks together, by the first wave.
   if (wid == 0) {
@@ -675,29 +726,29 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     uint32_t valid = 0, listed = 0;
     float floor = -INFINITY, near = INFINITY;
     int top_bin = -2147483647, bins = 0;
-    for (int c = lane; c < h.chunks; c += 64) {
-      const HeadStat st = hs[c];
-      sh.part[c] = {int(st.listed), st.top_bin, st.bins, st.rest_ref, st.rest};
-      if (st.valid == 0) continue;
-      const uint64_t k = entry_key(st.best, st.best_col);
-      best = k > best ? k : best;
-      valid += st.valid;
-      listed += st.listed;
-      floor = fmaxf(floor, st.floor);
-      near = fminf(near, st.near);
-      top_bin = st.bins > 0 ? max(top_bin, st.top_bin) : top_bin;
-      bins = st.bins < 0 ? -1 : bins;
+    const HeadStat* hs = h.stats + at * h.chunks;
+    for (int c0 = 0; c0 < h.chunks; c0 += 64) {
+      if (c0 + lane < h.chunks) {
+        const HeadStat st = hs[c0 + lane];
+        sh.part[c0 + lane] = {int(st.listed), st.top_bin, st.bins, st.rest_ref, st.rest};
+        if (st.valid != 0) {
+          best = most64(best, entry_key(st.best, st.best_col));
+          valid += st.valid;
+          listed += st.listed;
+          floor = fmaxf(floor, st.floor);
+          near = fminf(near, st.near);
+          top_bin = st.bins > 0 ? max(top_bin, st.top_bin) : top_bin;
+          bins = st.bins < 0 ? -1 : bins;
+        }
+      }
     }
-    valid = wave_sum(valid);
-    listed = wave_sum(listed);
-    floor = wave_max(floor);
-    near = -wave_max(-near);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      best = most64(best, __shfl_xor(best, o, kWave));
-      top_bin = max(top_bin, __shfl_xor(top_bin, o, kWave));
-      bins = min(bins, __shfl_xor(bins, o, kWave));
-    }
+    best = wave_fold(best, most64);
+    valid = wave_fold(valid, add);
+    listed = wave_fold(listed, add);
+    floor = wave_fold(floor, [](float u, float v) { return fmaxf(u, v); });
+    near = wave_fold(near, [](float u, float v) { return fminf(u, v); });
+    top_bin = wave_fold(top_bin, [](int u, int v) { return max(u, v); });
+    bins = wave_fold(bins, [](int u, int v) { return min(u, v); });
     if (lane == 0) {
       sh.best = best;
       sh.valid = valid;
@@ -713,9 +764,9 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   const uint32_t valid = sh.valid, listed = sh.listed;
   const float m = entry_logit(best), floor = sh.floor;
   const bool whole = listed == valid;   // nothing is unlisted
-  if (LISTS && tid == 0) h.pending[at] = 0;
+  if (PHASE == kLists) leave(kDone);
 
-  if (!TOP && (valid == 0 || s.greedy)) {
+  if (!TOP && LISTS && (valid == 0 || s.greedy)) {
     if (tid == 0) {
       if (a.tok != nullptr) a.tok[row] = valid != 0 ? entry_column(best) : -1;
       a.kept[row] = valid != 0 ? 1 : 0;
@@ -727,14 +778,16 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   }
 
   // The listed entries, all in flight together: this thread's places of the row's lists.
-  constexpr int LISTED = kListMax / NT;
+  constexpr int LISTED = LISTS ? kListMax / NT : 1;
   uint64_t mine[LISTED];
-  {
+  if constexpr (LISTS) {
     const uint64_t* list = h.list + at * h.chunks * h.cap;
 #pragma unroll
     for (int q = 0; q < LISTED; ++q) {
       const int i = q * NT + tid, c = i / h.cap;
-      mine[q] = c < h.chunks && i - c * h.cap < sh.part[c].listed ? list[i] : 0ull;
+      const bool is = c < h.chunks && i - c * h.cap < sh.part[c].listed;
+      mine[q] = list[is ? i : 0];
+      mine[q] = is ? mine[q] : 0ull;
     }
   }
   // Those of value >= t into the list; all of the row's where t >= floor.
@@ -754,13 +807,38 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   if constexpr (TOP) {
     const int K = a.K;
     const int n = int(min(uint32_t(K), valid));
-    int have = gather(fmaxf(floor, sh.near));
-    if (have < n && sh.near > floor) have = gather(floor);
-    if (have < n) {
-      if constexpr (LISTS) {
-        if (tid == 0) h.pending[at] = 1;
+    bool done = false;
+    if constexpr (LISTS) {
+      int have = gather(fmaxf(floor, sh.near));
+      if (have < n && sh.near > floor) have = gather(floor);
+      if (have >= n) {
+        done = true;
+        sort_list<NT>(sh.list, have);
+        if (a.rest != nullptr) {
+          const uint64_t last = n > 0 ? sh.list[n - 1] : 0;
+          uint64_t next = 0;
+#pragma unroll
+          for (int q = 0; q < LISTED; ++q) next = mine[q] < last ? most64(next, mine[q]) : next;
+          double ref = next != 0 ? double(entry_logit(next)) : -INFINITY;
+          const bool rest = tid < h.chunks && sh.part[tid].rest > 0.;
+          if (rest) ref = fmax(ref, sh.part[tid].rest_ref);
+          ref = block_fold<W>(ref, sh.red.d, [](double u, double v) { return fmax(u, v); });
+          double sum = 0.;
+#pragma unroll
+          for (int q = 0; q < LISTED; ++q)
+            if (mine[q] != 0 && mine[q] < last)
+              sum += exp2_64((double(entry_logit(mine[q])) - ref) * s.c2);
+          if (rest) sum += sh.part[tid].rest * exp2_64((sh.part[tid].rest_ref - ref) * s.c2);
+          sum = block_fold<W>(sum, sh.red.d, add);
+          if (tid == 0) a.rest[row] = sum > 0. ? float(ref * s.inv_t + log(sum)) : -INFINITY;
+        }
+      } else if (PHASE == kLists) {
+        leave(kLeftSearch);
         return;
-      } else {
+      }
+    }
+    if constexpr (SEARCH) {
+      if (!done) {
         const uint64_t cut =
             valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, m, s.c2, scale, sh) : 0;
         if (tid == 0) sh.n = 0;
@@ -788,27 +866,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
             a.rest[row] = next != 0 ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
         }
       }
-    } else {
-      sort_list<NT>(sh.list, have);
-      if (a.rest != nullptr) {
-        const uint64_t last = n > 0 ? sh.list[n - 1] : 0;
-        uint64_t next = 0;
-        float ref = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < LISTED; ++q) next = mine[q] < last ? most64(next, mine[q]) : next;
-        if (tid < h.chunks && sh.part[tid].rest > 0.) ref = sh.part[tid].rest_ref;
-        ref = fmaxf(ref, next != 0 ? entry_logit(next) : -INFINITY);
-        ref = block_fold<W>(ref, sh.red.f, [](float u, float v) { return fmaxf(u, v); });
-        double sum = 0.;
-#pragma unroll
-        for (int q = 0; q < LISTED; ++q)
-          if (mine[q] != 0 && mine[q] < last) sum += entry_weight(entry_logit(mine[q]), ref, s.c2);
-        if (tid < h.chunks && sh.part[tid].rest > 0.)
-          sum += sh.part[tid].rest * entry_weight(sh.part[tid].rest_ref, ref, s.c2);
-        sum = block_fold<W>(sum, sh.red.d, add);
-        if (tid == 0)
-          a.rest[row] = ref > -INFINITY ? float(double(ref) * s.inv_t + log(sum)) : -INFINITY;
-      }
     }
     for (int i = tid; i < K; i += NT) {
       const uint64_t k = sh.list[i < n ? i : 0];
@@ -819,11 +876,61 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     const bool has_k = s.top_k > 0 && uint32_t(s.top_k) < valid;
     const bool has_p = s.top_p < 1.f, has_m = s.min_p > 0.f;
     const double least_w = has_m ? fmin(double(s.min_p), 1.) : 0.;
-    uint32_t kept = valid;
-    uint64_t low = 0;
-    double mass = 0.;
     const double u = a.u != nullptr ? fmin(fmax(double(a.u[row]), 0.), 1.) : 0.;
-    int tok = -1;
+    auto write = [&](uint32_t kept, uint64_t low, double mass, int tok) {
+      if (tid != 0) return;
+      const bool every = kept == valid;
+      a.kept[row] = int32_t(kept);
+      a.cut_logit[row] = every ? -INFINITY : entry_logit(low);
+      a.cut_index[row] = every ? -1 : entry_column(low);
+      a.lse[row] = double(m) * s.inv_t + log(mass);
+      if (a.tok != nullptr) a.tok[row] = tok;
+    };
+    // Least value of weight min_p.
+    auto value_of_min_p = [&]() {
+      return f32_from_order_key(
+          least_value_key(m, [&](float z) { return entry_weight(z, m, s.c2) >= least_w; }));
+    };
+    // The draw when the chunks' masses are known (thread c has chunk c's): only the chunk that the
+    // running sum passes the target in is read.
+    auto draw_in_chunks = [&](double w, double run, double mass, uint64_t cut) {
+      const double target = u * mass;
+      if (tid == 0) sh.pick = NT, sh.last = 0;
+      __syncthreads();
+      if (w > 0.) {
+        if (run > target) atomicMin(&sh.pick, tid);
+        atomicMax(&sh.last, tid);
+      }
+      __syncthreads();
+      const int c = min(sh.pick, sh.last);
+      __syncthreads();
+      if (tid == c) sh.sum = run - w;
+      __syncthreads();
+      const double base = sh.sum;
+      const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
+      uint32_t n;
+      uint64_t l;
+      double grun, gmine;
+      kept_masses<NT, SEARCH>(r, j0, j1, cut, m, s.c2, sh, n, l, grun, gmine);
+      return draw_entry<NT, SEARCH>(r, j0, j1, cut, m, s.c2, base, target, grun, gmine, sh);
+    };
+
+    if (s.open) {
+      // Everything is kept: the chunks' sums are the masses.
+      const bool is = tid < h.chunks && sh.part[tid].rest > 0.;
+      const double w = is ? sh.part[tid].rest * exp2_64((sh.part[tid].rest_ref - double(m)) * s.c2) : 0.;
+      double mass;
+      const double run = block_scan<W>(w, sh.red.d, mass);
+      if constexpr (PHASE == kLists) {
+        if (a.tok != nullptr)
+          leave(kLeftBorder);
+        else
+          write(valid, 0, mass, -1);
+      } else if constexpr (BORDER) {
+        write(valid, 0, mass, a.tok != nullptr ? draw_in_chunks(w, run, mass, 0) : -1);
+      }
+      return;
+    }
 
     // The nucleus' border bin: the histograms joined, their running sum against top_p of the whole.
     const double k16 = 16. * s.c2;
@@ -832,49 +939,62 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     int border = 0;
     const int top_bin = sh.top_bin;
     auto bin_weight = [&](int b) { return exp2_64(-double(b) / 16.); };
-    // Weight of the top bin's middle relative to the greatest entry's.
+    // 2^-48 of the top bin's middle, relative to the greatest entry's weight.
     const double unit =
-        binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * 3.552713678800501e-15 : 0.;   // 2^-48
-    auto mass_at = [&](int c, int b) -> uint64_t {   // of chunk c in the row's bin b
+        binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * 3.552713678800501e-15 : 0.;
+    const uint64_t* masses = h.mass + at * h.chunks * kMassBins;
+    auto mass_at = [&](int c, int b) -> double {   // of chunk c in the row's bin b
       const int i = b - (top_bin - sh.part[c].top_bin);
-      return i >= 0 && i < sh.part[c].bins ? h.mass[(at * h.chunks + c) * kMassBins + i] : 0ull;
+      const bool is = i >= 0 && i < sh.part[c].bins;
+      const uint64_t n = masses[int64_t(c) * kMassBins + (is ? i : 0)];   // loaded in any case
+      return is ? double(n) : 0.;
     };
-    if (binned) {
-      constexpr int PER = kMassBins / NT;
-      double v[PER], sum = 0.;
+    if constexpr (LISTS) {
+      if (binned) {
+        constexpr int PER = kMassBins / NT;
+        double v[PER], sum = 0.;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const int b = PER * tid + e;
-        double n = 0.;
+        for (int e = 0; e < PER; ++e) v[e] = 0.;
 #pragma unroll 8
-        for (int c = 0; c < h.chunks; ++c) n += double(mass_at(c, b));
-        v[e] = n * bin_weight(b) * unit;
-        sum += v[e];
-      }
-      const double run = block_scan<W>(sum, sh.red.d, zk);
-      if (tid == 0) sh.pick = kMassBins, sh.last = 0;
-      __syncthreads();
-      const double target = fmax(double(s.top_p) * zk, 1e-300);
-      double upto = run - sum;
+        for (int c = 0; c < h.chunks; ++c) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        upto += v[e];
-        if (v[e] > 0.) {
-          if (upto >= target) atomicMin(&sh.pick, PER * tid + e);
-          atomicMax(&sh.last, PER * tid + e);
+          for (int e = 0; e < PER; ++e) v[e] += mass_at(c, PER * tid + e);
         }
-      }
-      __syncthreads();
-      border = min(sh.pick, sh.last);
-      upto = run - sum;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        if (PER * tid + e == border) sh.sum = upto;
-        upto += v[e];
+        for (int e = 0; e < PER; ++e) {
+          v[e] *= bin_weight(PER * tid + e) * unit;
+          sum += v[e];
+        }
+        const double run = block_scan<W>(sum, sh.red.d, zk);
+        if (tid == 0) sh.pick = kMassBins, sh.last = 0;
+        __syncthreads();
+        const double target = fmax(double(s.top_p) * zk, 1e-300);
+        double upto = run - sum;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          upto += v[e];
+          if (v[e] > 0.) {
+            if (upto >= target) atomicMin(&sh.pick, PER * tid + e);
+            atomicMax(&sh.last, PER * tid + e);
+          }
+        }
+        __syncthreads();
+        border = min(sh.pick, sh.last);
+        upto = run - sum;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          if (PER * tid + e == border) sh.sum = upto;
+          upto += v[e];
+        }
+        __syncthreads();
+        above = sh.sum;
+        __syncthreads();
+        if (PHASE == kLists && tid == 0) note->whole = zk, note->above = above, note->border = border;
       }
-      __syncthreads();
-      above = sh.sum;
-      __syncthreads();
+    } else if (binned) {
+      zk = note->whole;
+      above = note->above;
+      border = note->border;
     }
     // Least value of bin b or a greater one.
     auto bin_edge = [&](int b) {
@@ -883,38 +1003,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       }));
     };
 
-    if (s.open) {
-      // Everything is kept: the chunks' sums are the masses, and only the chunk drawn is read.
-      const double w =
-          tid < h.chunks ? sh.part[tid].rest * entry_weight(sh.part[tid].rest_ref, m, s.c2) : 0.;
-      const double run = block_scan<W>(w, sh.red.d, mass);
-      if constexpr (LISTS) {
-        if (a.tok != nullptr) {
-          if (tid == 0) h.pending[at] = 1;
-          return;
-        }
-      } else if (a.tok != nullptr) {
-        const double target = u * mass;
-        if (tid == 0) sh.pick = kCutThreads, sh.last = 0;
-        __syncthreads();
-        if (w > 0.) {
-          if (run > target) atomicMin(&sh.pick, tid);
-          atomicMax(&sh.last, tid);
-        }
-        __syncthreads();
-        const int c = min(sh.pick, sh.last);
-        __syncthreads();
-        if (tid == c) sh.sum = run - w;
-        __syncthreads();
-        const double base = sh.sum;
-        const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
-        uint32_t n;
-        uint64_t l;
-        double grun, gmine;
-        kept_masses(r, j0, j1, 0, m, s.c2, sh, n, l, grun, gmine);
-        tok = draw_entry(r, j0, j1, 0, m, s.c2, base, target, grun, gmine, sh);
-      }
-    } else {
+    if constexpr (LISTS) {
       // How far down the cut can lie, and whether the lists reach it.
       float t = floor;
       bool quick;
@@ -923,9 +1012,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       else if (binned)
         t = bin_edge(border), quick = t >= floor;
       else if (s.top_k <= 0 && !has_p)
-        t = f32_from_order_key(least_value_key(
-            m, [&](float z) { return entry_weight(z, m, s.c2) >= least_w; })),
-        quick = t >= floor;
+        t = value_of_min_p(), quick = t >= floor;
       else
         quick = whole;
       int have = quick ? gather(t) : 0;
@@ -939,8 +1026,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         int n = has_k ? s.top_k : have;
         if (has_p) {
           double sum;
-          if (!binned) reach<NT, false>(n, 1e300, n, zk, sh, weight);   // of all n
-          const int p = reach<NT, false>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
+          if (!binned) reach<NT, false, SEARCH>(n, 1e300, n, zk, sh, weight);   // of all n
+          const int p = reach<NT, false, SEARCH>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
           n = min(n, p + 1);
         }
         if (has_m) {
@@ -948,8 +1035,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           for (int i = tid; i < n; i += NT) c += weight(i) >= least_w;
           n = int(block_fold<W>(c, sh.red.i, add));
         }
-        kept = uint32_t(n);
-        low = sh.list[n - 1];
+        const uint64_t low = sh.list[n - 1];
         __syncthreads();
         // In token order: columns with their places as keys, the weights beside them.
         for (int i = tid; i < n; i += NT) {
@@ -960,10 +1046,12 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         __syncthreads();
         sort_list<NT>(sh.list, n);
         auto in_order = [&](int i) { return sh.weight[sh.list[i] & 4095u]; };
-        reach<NT, true>(n, 1e300, n, mass, sh, in_order);
+        double mass;
+        int tok = -1;
+        reach<NT, true, SEARCH>(n, 1e300, n, mass, sh, in_order);
         if (a.tok != nullptr) {
           double sum;
-          int i = reach<NT, true>(n, u * mass, 0, sum, sh, in_order);
+          int i = reach<NT, true, SEARCH>(n, u * mass, 0, sum, sh, in_order);
           if (i == n) {   // the last with a weight
             if (tid == 0) sh.last = 0;
             __syncthreads();
@@ -974,129 +1062,108 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           }
           tok = int(kColumnMask - uint32_t(sh.list[i] >> 12));
         }
-      } else if constexpr (LISTS) {
-        if (tid == 0) h.pending[at] = 1;
+        write(uint32_t(n), low, mass, tok);
         return;
-      } else {
-        // The lists do not reach the cut: the row is read again.
-        uint64_t cut = 0;
-        uint64_t cut_m = 0;
-        if (has_m)
-          cut_m = uint64_t(least_value_key(m, [&](float z) {
-                    return entry_weight(z, m, s.c2) >= least_w;
-                  })) << kColumnBits;
-        bool done = false;
-        if (binned) {
-          // The border bin's entries, and how many lie above it.
-          const float end = bin_edge(border);
-          const float over = border > 0 ? bin_edge(border - 1) : INFINITY;
-          __syncthreads();
-          if (tid == 0) sh.n = 0;
-          __syncthreads();
-          uint32_t greater = 0;
-          each_entry(r, [&](int, float z, int c) {
-            if (border > 0 && z >= over) {
-              ++greater;
-            } else if (z >= end) {
-              const uint32_t i = atomicAdd(&sh.n, 1u);
-              if (i < uint32_t(kListMax)) sh.list[i] = entry_key(z, c);
-            }
-          });
-          greater = block_fold<W>(greater, sh.red.i, add);
-          const uint32_t in = sh.n;
-          __syncthreads();
-          if (in <= uint32_t(kListMax) && in > 0) {
-            sort_list<NT>(sh.list, int(in));
-            auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
-            double sum;
-            const int p = reach<NT, false>(int(in), fmax(double(s.top_p) * zk, 1e-300) - above, 0, sum,
-                                           sh, weight);
-            const int n = min(p + 1, int(in));
-            cut = sh.list[n - 1];
-            if (cut_m <= cut) {
-              done = true;
-              kept = greater + uint32_t(n);
-              low = cut;
-              {
-                // The chunks' masses: their bins above the border, and their part of its entries.
-                for (int c = wid; c < h.chunks; c += W) {
-                  double w = 0.;
-                  for (int b = lane; b < border; b += 64)
-                    w += double(mass_at(c, b)) * bin_weight(b) * unit;
-                  for (int i = lane; i < n; i += 64) {
-                    const uint64_t k = sh.list[i];
-                    const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
-                    if (j / h.vectors == c) w += entry_weight(entry_logit(k), m, s.c2);
-                  }
-                  w = wave_sum(w);
-                  if (lane == 0) sh.chunk[c] = w;
-                }
-                __syncthreads();
-                const double w = tid < h.chunks ? sh.chunk[tid] : 0.;
-                const double run = block_scan<W>(w, sh.red.d, mass);
-                if (a.tok != nullptr) {
-                  const double target = u * mass;
-                  if (tid == 0) sh.pick = kCutThreads, sh.last = 0;
-                  __syncthreads();
-                  if (w > 0.) {
-                    if (run > target) atomicMin(&sh.pick, tid);
-                    atomicMax(&sh.last, tid);
-                  }
-                  __syncthreads();
-                  const int c = min(sh.pick, sh.last);
-                  __syncthreads();
-                  if (tid == c) sh.sum = run - w;
-                  __syncthreads();
-                  const double base = sh.sum;
-                  const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
-                  uint32_t k;
-                  uint64_t l;
-                  double grun, gmine;
-                  kept_masses(r, j0, j1, cut, m, s.c2, sh, k, l, grun, gmine);
-                  tok = draw_entry(r, j0, j1, cut, m, s.c2, base, target, grun, gmine, sh);
-                }
-              }
-            }
-          }
-        }
-        if (!done && binned && cut == 0 && sh.n > uint32_t(kListMax)) {
-          // A border bin of many entries: the cut among them.
-          const uint64_t end = entry_key(bin_edge(border), a.V - 1);
-          const uint64_t over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
-          __syncthreads();
-          cut = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), 0, m, s.c2, scale, sh, end,
-                                   over, above);
-        }
-        if (!done) {
-          const bool known = cut != 0;   // but for min_p
-          if (has_k) cut = select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh);
-          if (has_p && !known) {
-            double all = 0.;
-            each_entry(r, [&](int, float z, int c) {
-              if (entry_key(z, c) >= cut) all += entry_weight(z, m, s.c2);
-            });
-            all = block_fold<W>(all, sh.red.d, add);
-            // A target of 0 is reached by the first entry, not before it.
-            cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2,
-                                                 scale, sh));
-          }
-          cut = most64(cut, cut_m);
-          double run, mine;
-          mass = kept_masses(r, 0, r.vectors(), cut, m, s.c2, sh, kept, low, run, mine);
-          kept = block_fold<W>(kept, sh.red.i, add);
-          low = block_fold<W>(low, sh.red.u, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
-          if (a.tok != nullptr)
-            tok = draw_entry(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass, run, mine, sh);
-        }
+      }
+      if (PHASE == kLists) {
+        leave(binned ? kLeftBorder : kLeftSearch);
+        return;
       }
     }
-    if (tid == 0) {
-      const bool every = kept == valid;
-      a.kept[row] = int32_t(kept);
-      a.cut_logit[row] = every ? -INFINITY : entry_logit(low);
-      a.cut_index[row] = every ? -1 : entry_column(low);
-      a.lse[row] = double(m) * s.inv_t + log(mass);
-      if (a.tok != nullptr) a.tok[row] = tok;
+
+    // The lists do not reach the cut: the row is read again.
+    uint64_t cut = 0;
+    const uint64_t cut_m =
+        has_m ? uint64_t(f32_order_key(value_of_min_p() + 0.f)) << kColumnBits : 0;
+    if constexpr (BORDER) {
+      if (binned) {
+        // The border bin's entries, and how many lie above it.
+        const float end = bin_edge(border);
+        const float over = border > 0 ? bin_edge(border - 1) : INFINITY;
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        uint32_t greater = 0;
+        each_entry<NT, 32>(
+            r, 0, r.vectors(),
+            [&](int, float z, int c) {
+              if (z >= over && border > 0) {
+                ++greater;
+              } else if (z >= end) {
+                const uint32_t i = atomicAdd(&sh.n, 1u);
+                if (i < uint32_t(kListMax)) sh.list[i] = entry_key(z, c);
+              }
+            },
+            [](int) {});
+        greater = block_fold<W>(greater, sh.red.i, add);
+        const uint32_t in = sh.n;
+        __syncthreads();
+        if (in <= uint32_t(kListMax) && in > 0) {
+          sort_list<NT>(sh.list, int(in));
+          auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
+          double sum;
+          const int p = reach<NT, false, SEARCH>(int(in), fmax(double(s.top_p) * zk, 1e-300) - above, 0, sum, sh,
+                                         weight);
+          const int n = min(p + 1, int(in));
+          cut = sh.list[n - 1];
+          if (cut_m <= cut) {
+            // The chunks' masses: their bins above the border, and their part of its entries.
+            for (int c = wid; c < h.chunks; c += W) {
+              double w = 0.;
+              for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
+              for (int i = lane; i < n; i += 64) {
+                const uint64_t k = sh.list[i];
+                const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
+                if (j / h.vectors == c) w += entry_weight(entry_logit(k), m, s.c2);
+              }
+              w = wave_fold(w, add);
+              if (lane == 0) sh.chunk[c] = w;
+            }
+            __syncthreads();
+            const double w = tid < h.chunks ? sh.chunk[tid] : 0.;
+            double mass;
+            const double run = block_scan<W>(w, sh.red.d, mass);
+            const int tok = a.tok != nullptr ? draw_in_chunks(w, run, mass, cut) : -1;
+            write(greater + uint32_t(n), cut, mass, tok);
+            if (PHASE == kBorder) leave(kDone);
+            return;
+          }
+        }
+      }
+      if (PHASE == kBorder) {
+        leave(kLeftSearch);
+        return;
+      }
+    }
+    if constexpr (SEARCH) {
+      if (has_k) cut = select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh);
+      if (binned) {
+        // A border bin of many entries: the cut among them.
+        const uint64_t end = entry_key(bin_edge(border), a.V - 1);
+        const uint64_t over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
+        cut = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), 0, m, s.c2, scale, sh, end,
+                                 over, above);
+      } else if (has_p) {
+        double all = 0.;
+        each_entry(r, [&](int, float z, int c) {
+          if (entry_key(z, c) >= cut) all += entry_weight(z, m, s.c2);
+        });
+        all = block_fold<W>(all, sh.red.d, add);
+        // A target of 0 is reached by the first entry, not before it.
+        cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2,
+                                             scale, sh));
+      }
+      cut = most64(cut, cut_m);
+      double run, mine_w;
+      uint32_t kept;
+      uint64_t low;
+      const double mass = kept_masses<NT, SEARCH>(r, 0, r.vectors(), cut, m, s.c2, sh, kept, low, run, mine_w);
+      kept = block_fold<W>(kept, sh.red.i, add);
+      low = block_fold<W>(low, sh.red.u, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+      const int tok = a.tok != nullptr ? draw_entry<NT, SEARCH>(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass,
+                                                        run, mine_w, sh)
+                                       : -1;
+      write(kept, low, mass, tok);
     }
   }
 }
@@ -1339,10 +1406,9 @@ static int64_t cut_rows(bool bf16, int64_t rows, int V) {
   const int64_t most = kCutChunks / head_plan(bf16, kCutChunks, V).chunks;
   return rows < most ? rows : most;
 }
-// Above this many rows the lists are handled by small workgroups, four to a CU, and a third launch
-// takes the rows that they leave; up to it one launch of large ones does both.
+// Above this many rows (a workgroup a CU) the second launch's phases run apart.
 constexpr int64_t kCombinedRows = 256;
-constexpr int kListThreads = 256;
+constexpr int kListThreads = 256, kBorderThreads = 512;
 
 size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
   const int64_t n = cut_rows(bf16, rows, V);
@@ -1353,7 +1419,7 @@ size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
   const HeadPlan fine = head_plan(bf16, 0, V);
   const int64_t fine_chunks = few * fine.chunks;
   chunks = chunks > fine_chunks ? chunks : fine_chunks;
-  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * 4) + al256(size_t(chunks) * sizeof(HeadStat)) +
+  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * sizeof(CutNote)) + al256(size_t(chunks) * sizeof(HeadStat)) +
          (top ? 0 : al256(size_t(chunks) * kMassBins * 8));
 }
 
@@ -1377,7 +1443,7 @@ static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
     h.cap = kListMax / pl.chunks;
     h.vectors = pl.elems * kHeadThreads / LogitRow<T>::N;
     h.list = reinterpret_cast<uint64_t*>(take(size_t(a.rows) * kListMax * 8));
-    h.pending = reinterpret_cast<int32_t*>(take(size_t(a.rows) * 4));
+    h.notes = reinterpret_cast<CutNote*>(take(size_t(a.rows) * sizeof(CutNote)));
     h.stats = reinterpret_cast<HeadStat*>(take(size_t(a.rows) * pl.chunks * sizeof(HeadStat)));
     h.mass = reinterpret_cast<uint64_t*>(p);
     const dim3 grid(unsigned(a.rows) * pl.chunks), rows(unsigned(a.rows));
@@ -1387,14 +1453,19 @@ static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
       hipLaunchKernelGGL((row_head_kernel<T, 32, TOP>), grid, dim3(kHeadThreads), 0, s, a, h);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.rows > kCombinedRows) {
-      hipLaunchKernelGGL((row_cut_kernel<T, TOP, kListThreads, true>), rows, dim3(kListThreads), 0, s, a, h);
+    if (a.rows <= kCombinedRows) {
+      hipLaunchKernelGGL((row_cut_kernel<T, TOP, kCutThreads, kAll>), rows, dim3(kCutThreads), 0, s, a, h);
+    } else {
+      hipLaunchKernelGGL((row_cut_kernel<T, TOP, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
-    } else {
-      h.pending = nullptr;
+      if constexpr (!TOP) {
+        hipLaunchKernelGGL((row_cut_kernel<T, TOP, kBorderThreads, kBorder>), rows, dim3(kBorderThreads), 0, s, a, h);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
+      hipLaunchKernelGGL((row_cut_kernel<T, TOP, kCutThreads, kSearch>), rows, dim3(kCutThreads), 0, s, a, h);
     }
-    hipLaunchKernelGGL((row_cut_kernel<T, TOP, kCutThreads, false>), rows, dim3(kCutThreads), 0, s, a, h);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
