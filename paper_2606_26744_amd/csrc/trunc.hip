@@ -446,6 +446,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// bits * 2 + (x >= lo), which is false for NaN.
+__device__ __forceinline__ uint32_t push_at_least(uint32_t bits, float x, float lo) {
+  uint32_t d;
+  asm("v_cmp_ge_f32 vcc, %2, %3\n\tv_addc_co_u32 %0, vcc, %1, %1, vcc"
+      : "=v"(d)
+      : "v"(bits), "v"(x), "v"(lo)
+      : "vcc");
+  return d;
+}
+
 // A chunk of a row: E entries a thread.
 template <typename T, int E, bool TOP>
 __global__ void __launch_bounds__(kHeadThreads)
@@ -458,7 +468,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     float f[kHeadWaves];
     uint32_t i[kHeadWaves];
   } red;
-  __shared__ uint32_t wave_n[2][kHeadWaves];
+  __shared__ uint32_t wave_n[kHeadWaves];
   __shared__ int best_col;
   const int64_t at = blockIdx.x / h.chunks, row = a.row0 + at;   // in the launch, in the call
   const int chunk = int(blockIdx.x - at * h.chunks), tid = threadIdx.x;
@@ -483,21 +493,6 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   auto add = [](auto u, auto v) { return u + v; };
   auto most = [](float u, float v) { return fmaxf(u, v); };
   auto least = [](float u, float v) { return fminf(u, v); };
-  // Entries for which `of` holds, over the workgroup: counted by the scalar unit.
-  auto count_of = [&](auto of) {
-    uint32_t n = 0;
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int e = 0; e < N; ++e) n += uint32_t(__popcll(__ballot(of(x[g][e]))));
-    if (lane == 0) wave_n[1][wid] = n;
-    __syncthreads();
-    uint32_t all = 0;
-#pragma unroll
-    for (int w = 0; w < kHeadWaves; ++w) all += wave_n[1][w];
-    return all;
-  };
-
   // Unmasked entries (NaN is masked: no comparison holds for it), the greatest one.
   uint32_t live = 0;
   float top = -INFINITY;
@@ -513,11 +508,11 @@ row_head_kernel(CutArgs a, HeadArgs h) {
       top = max3(top, x[g][e], x[g][e + 1]);
     }
   if (tid == 0) best_col = a.V;
-  if (lane == 0) wave_n[0][wid] = live;
+  if (lane == 0) wave_n[wid] = live;
   const float m = block_fold<kHeadWaves>(top, red.f, most);
   uint32_t valid = 0;
 #pragma unroll
-  for (int w = 0; w < kHeadWaves; ++w) valid += wave_n[0][w];
+  for (int w = 0; w < kHeadWaves; ++w) valid += wave_n[w];
   if (top == m && m > -INFINITY) {
     int first = a.V;
 #pragma unroll
@@ -555,42 +550,31 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     __syncthreads();
     const uint32_t first = in && mine > 0 ? count[mine - 1] : 0u;   // threads in the bins before
     near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
-    if (valid <= uint32_t(h.cap)) {
-      lo = kLeast;
-      listed = valid;
-    } else {
-      for (; want > 0; want /= 2) {
-        lo = block_fold<kHeadWaves>(in && first < uint32_t(want) ? top : INFINITY, red.f, least);
-        const float v = lo;
-        listed = count_of([&](float z) { return z >= v; });
-        if (listed <= uint32_t(h.cap)) break;
-        __syncthreads();
-      }
-      if (want == 0) {
-        lo = INFINITY;
-        listed = 0;
-      }
-    }
-    if (listed > 0) {
-      if (listed == valid) count_of([&](float z) { return z >= lo; });
-      uint32_t before = 0;
-      for (int w = 0; w < wid; ++w) before += wave_n[1][w];
-      uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
+    const bool every = valid <= uint32_t(h.cap);
+    uint32_t bits = 0, before = 0;   // this thread's listed entries, the first one's bit the highest
+    for (; want > 0; want /= 2) {
+      lo = every ? kLeast
+                 : block_fold<kHeadWaves>(in && first < uint32_t(want) ? top : INFINITY, red.f, least);
+      bits = 0;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const bool is = x[g][e] >= lo;
-          const unsigned long long who = __ballot(is);
-          if (who != 0ull) {
-            const uint32_t k = __popcll(who & ((1ull << lane) - 1));
-            if (is) {
-              list[before + k] = entry_key(x[g][e], col(g, e));
-              if constexpr (TOP) x[g][e] = -INFINITY;   // what stays is unlisted
-            }
-            before += uint32_t(__popcll(who));
-          }
-        }
+        for (int e = 0; e < N; ++e) bits = push_at_least(bits, x[g][e], lo);
+      const uint32_t n = __popc(bits);
+      before = block_scan<kHeadWaves>(n, red.i, listed) - n;
+      if (listed <= uint32_t(h.cap)) break;
+    }
+    if (want == 0) {
+      lo = INFINITY;
+      listed = bits = 0;
+    }
+    // Few threads have more than one or two: their values are read again, not picked from registers.
+    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap + before;
+    while (bits != 0) {
+      const int q = E - __ffs(bits);
+      bits &= bits - 1;
+      const int c = r.column(j0 + q / N * kHeadThreads + tid) + q % N;
+      *list++ = entry_key(r.raw(c), c);
     }
   }
 
@@ -636,7 +620,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e]);
+          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e] < lo ? x[g][e] : -INFINITY);
         ref = block_fold<kHeadWaves>(g_top, red.f, most);
       }
       const float k = fmaxf(fminf(ref * c2, 3e38f), -3e38f);
@@ -644,7 +628,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e) f += __builtin_amdgcn_exp2f(fmaf(x[g][e], c2, -k));
+        for (int e = 0; e < N; ++e) f += x[g][e] < lo ? __builtin_amdgcn_exp2f(fmaf(x[g][e], c2, -k)) : 0.f;
       st.rest_ref = double(k) / double(c2);
       st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
       if (st.rest > 1e-25 || !(lo < INFINITY)) break;
@@ -1003,47 +987,105 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       }));
     };
 
+    const uint64_t cut_m =
+        has_m ? uint64_t(f32_order_key(value_of_min_p() + 0.f)) << kColumnBits : 0;
+    uint64_t cut = 0;
+    // Among the border bin's n entries in the list, sorted: the first to reach the target.
+    auto cut_of_border = [&](int n, int& kept) {
+      sort_list<NT>(sh.list, n);
+      double sum;
+      const int p = reach<NT, false, SEARCH>(
+          n, fmax(double(s.top_p) * zk, 1e-300) - above, 0, sum, sh,
+          [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); });
+      kept = min(p + 1, n);
+      return sh.list[kept - 1];
+    };
+    const float border_end = binned ? bin_edge(border) : 0.f;
+    const float border_over = binned && border > 0 ? bin_edge(border - 1) : INFINITY;
+
     if constexpr (LISTS) {
-      // How far down the cut can lie, and whether the lists reach it.
-      float t = floor;
+      // The cut, where the lists hold all that lies above it.
       bool quick;
-      if (has_k)
-        t = fmaxf(floor, sh.near), quick = true;
-      else if (binned)
-        t = bin_edge(border), quick = t >= floor;
-      else if (s.top_k <= 0 && !has_p)
-        t = value_of_min_p(), quick = t >= floor;
-      else
-        quick = whole;
-      int have = quick ? gather(t) : 0;
-      if (has_k && have < s.top_k) {
-        if (t > floor) have = gather(floor);
+      if (has_k) {
+        int have = gather(fmaxf(floor, sh.near));
+        if (have < s.top_k && sh.near > floor) have = gather(floor);
         quick = have >= s.top_k;
+        if (quick) {
+          sort_list<NT>(sh.list, have);
+          auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
+          int n = s.top_k;
+          if (has_p) {
+            double sum;
+            reach<NT, false, SEARCH>(n, 1e300, n, zk, sh, weight);   // of all n
+            const int p =
+                reach<NT, false, SEARCH>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
+            n = min(n, p + 1);
+          }
+          cut = sh.list[n - 1];
+        }
+      } else if (binned) {
+        quick = border_end >= floor;
+        if (quick) {
+          __syncthreads();
+          if (tid == 0) sh.n = 0;
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < LISTED; ++q) {
+            const float z = entry_logit(mine[q]);
+            if (mine[q] != 0 && z >= border_end && (z < border_over || border == 0))
+              sh.list[atomicAdd(&sh.n, 1u)] = mine[q];
+          }
+          __syncthreads();
+          const int n = int(sh.n);
+          __syncthreads();
+          int k;
+          cut = cut_of_border(n, k);
+        }
+      } else {
+        // min_p alone; a nucleus or a top_k of all that is left, with everything listed.
+        quick = whole || (!has_p && s.top_k <= 0 && entry_logit(cut_m) >= floor);
+        if (quick && has_p) {
+          const int n = gather(floor);
+          sort_list<NT>(sh.list, n);
+          auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
+          double sum;
+          reach<NT, false, SEARCH>(n, 1e300, n, zk, sh, weight);
+          const int p =
+              reach<NT, false, SEARCH>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
+          cut = sh.list[min(p, n - 1)];
+        }
       }
       if (quick) {
-        sort_list<NT>(sh.list, have);
-        auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
-        int n = has_k ? s.top_k : have;
-        if (has_p) {
-          double sum;
-          if (!binned) reach<NT, false, SEARCH>(n, 1e300, n, zk, sh, weight);   // of all n
-          const int p = reach<NT, false, SEARCH>(n, fmax(double(s.top_p) * zk, 1e-300), 0, sum, sh, weight);
-          n = min(n, p + 1);
-        }
-        if (has_m) {
-          uint32_t c = 0;
-          for (int i = tid; i < n; i += NT) c += weight(i) >= least_w;
-          n = int(block_fold<W>(c, sh.red.i, add));
-        }
-        const uint64_t low = sh.list[n - 1];
+        // The kept entries in token order: columns with their places as keys, the weights beside
+        // them.
         __syncthreads();
-        // In token order: columns with their places as keys, the weights beside them.
-        for (int i = tid; i < n; i += NT) {
-          const uint64_t k = sh.list[i];
-          sh.weight[i] = entry_weight(entry_logit(k), m, s.c2);
-          sh.list[i] = ((k & kColumnMask) << 12) | uint64_t(i);
-        }
+        if (tid == 0) sh.n = 0;
         __syncthreads();
+        cut = most64(cut, cut_m);
+        uint64_t low = kKeyTop;
+        uint32_t many = 0;
+#pragma unroll
+        for (int q = 0; q < LISTED; ++q)
+          if (mine[q] != 0 && mine[q] >= cut) {
+            low = mine[q] < low ? mine[q] : low;
+            ++many;
+          }
+        many = block_fold<W>(many, sh.red.i, add);
+        // (A nucleus of many is left to the next phase, which need not sort it.)
+        if (PHASE == kLists && binned && many > 2 * NT) {
+          leave(kLeftBorder);
+          return;
+        }
+        low = block_fold<W>(low, sh.red.u, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+#pragma unroll
+        for (int q = 0; q < LISTED; ++q)
+          if (mine[q] != 0 && mine[q] >= cut) {
+            const uint32_t i = atomicAdd(&sh.n, 1u);
+            sh.list[i] = ((mine[q] & kColumnMask) << 12) | uint64_t(i);
+            sh.weight[i] = entry_weight(entry_logit(mine[q]), m, s.c2);
+          }
+        __syncthreads();
+        const int n = int(many);
         sort_list<NT>(sh.list, n);
         auto in_order = [&](int i) { return sh.weight[sh.list[i] & 4095u]; };
         double mass;
@@ -1072,40 +1114,51 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     }
 
     // The lists do not reach the cut: the row is read again.
-    uint64_t cut = 0;
-    const uint64_t cut_m =
-        has_m ? uint64_t(f32_order_key(value_of_min_p() + 0.f)) << kColumnBits : 0;
     if constexpr (BORDER) {
       if (binned) {
         // The border bin's entries, and how many lie above it.
-        const float end = bin_edge(border);
-        const float over = border > 0 ? bin_edge(border - 1) : INFINITY;
         __syncthreads();
         if (tid == 0) sh.n = 0;
         __syncthreads();
         uint32_t greater = 0;
-        each_entry<NT, 32>(
-            r, 0, r.vectors(),
-            [&](int, float z, int c) {
-              if (z >= over && border > 0) {
-                ++greater;
-              } else if (z >= end) {
-                const uint32_t i = atomicAdd(&sh.n, 1u);
-                if (i < uint32_t(kListMax)) sh.list[i] = entry_key(z, c);
-              }
-            },
-            [](int) {});
-        greater = block_fold<W>(greater, sh.red.i, add);
+        constexpr int N = LogitRow<T>::N, Q = 32 / N;
+        const int nv = r.vectors();
+        for (int b = 0; b < nv; b += Q * NT) {
+          float x[Q][N];
+          if (r.inside(b, Q * NT)) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) r.load_inside(b + q * NT + tid, x[q]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+#pragma unroll
+              for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
+              if (b + q * NT + tid < nv) r.load_raw(b + q * NT + tid, x[q]);
+            }
+          }
+          uint32_t bits = 0;   // of the border bin, the first entry's bit the highest
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const bool over = x[q][e] >= border_over;
+              greater += uint32_t(__popcll(__ballot(over)));
+              bits = 2 * bits + uint32_t(x[q][e] >= border_end && !over);
+            }
+          while (bits != 0) {
+            const int q = 32 - __ffs(bits);
+            bits &= bits - 1;
+            const int c = r.column(b + q / N * NT + tid) + q % N;
+            const uint32_t i = atomicAdd(&sh.n, 1u);
+            if (i < uint32_t(kListMax)) sh.list[i] = entry_key(r.raw(c), c);
+          }
+        }
+        greater = block_fold<W>(lane == 0 ? greater : 0u, sh.red.i, add);
         const uint32_t in = sh.n;
         __syncthreads();
         if (in <= uint32_t(kListMax) && in > 0) {
-          sort_list<NT>(sh.list, int(in));
-          auto weight = [&](int i) { return entry_weight(entry_logit(sh.list[i]), m, s.c2); };
-          double sum;
-          const int p = reach<NT, false, SEARCH>(int(in), fmax(double(s.top_p) * zk, 1e-300) - above, 0, sum, sh,
-                                         weight);
-          const int n = min(p + 1, int(in));
-          cut = sh.list[n - 1];
+          int n;
+          cut = cut_of_border(int(in), n);
           if (cut_m <= cut) {
             // The chunks' masses: their bins above the border, and their part of its entries.
             for (int c = wid; c < h.chunks; c += W) {
@@ -1113,7 +1166,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
               for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
               for (int i = lane; i < n; i += 64) {
                 const uint64_t k = sh.list[i];
-                const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
+                const int j = (entry_column(k) + r.shift) / N;
                 if (j / h.vectors == c) w += entry_weight(entry_logit(k), m, s.c2);
               }
               w = wave_fold(w, add);
@@ -1125,7 +1178,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
             const double run = block_scan<W>(w, sh.red.d, mass);
             const int tok = a.tok != nullptr ? draw_in_chunks(w, run, mass, cut) : -1;
             write(greater + uint32_t(n), cut, mass, tok);
-            if (PHASE == kBorder) leave(kDone);
             return;
           }
         }
@@ -1136,11 +1188,11 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       }
     }
     if constexpr (SEARCH) {
-      if (has_k) cut = select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh);
+      cut = has_k ? select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh) : 0;
       if (binned) {
         // A border bin of many entries: the cut among them.
-        const uint64_t end = entry_key(bin_edge(border), a.V - 1);
-        const uint64_t over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
+        const uint64_t end = entry_key(border_end, a.V - 1);
+        const uint64_t over = border > 0 ? entry_key(border_over, kColumnMask) - 1 : kKeyTop;
         cut = select_entry<true>(r, fmax(double(s.top_p) * zk, 1e-300), 0, m, s.c2, scale, sh, end,
                                  over, above);
       } else if (has_p) {
