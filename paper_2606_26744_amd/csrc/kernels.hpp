@@ -212,7 +212,7 @@ hipError_t launch_accept_sample(const int32_t* draft, int draft_stride, const fl
                                 uint64_t stream, int32_t* acc, int32_t* anchor, int32_t* offs,
                                 int32_t* toks, void* ws, hipStream_t s);
 
-// ---------------------------------------------------------------- truncated rows (trunc.hip)
+// ---------------------------------------------------------------- truncated rows (row_head.hip, row_cut.hip, verify.hip)
 struct CutArgs {
   const void* z;             // rows of V logits, stride ld
   int64_t rows, ld;

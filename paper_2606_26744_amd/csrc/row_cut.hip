@@ -1,0 +1,1047 @@
+// Second launch of a row's cut (row_cut.hpp): a workgroup a row.  Its code runs once a row, mostly on
+// the way to the next memory access or barrier, so it is kept short: the same few loops for all
+// settings, nothing unrolled that memory does not need in flight.  (139 KB of unrolled code took
+// 60 us a row of instruction fetches where it takes 20.)
+#include "row_cut.hpp"
+
+namespace hdf {
+
+constexpr int kCutThreads = 1024;
+constexpr int kCutWaves = kCutThreads / kWave;
+constexpr int kBins = 2 * kCutThreads;
+constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
+constexpr double kSearchUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
+constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
+
+template <int NT, bool SEARCH>
+struct CutShared {
+  static constexpr int W = NT / kWave;
+  union {
+    struct {
+      uint64_t list[kListMax];
+      union {
+        struct {
+          uint64_t mass[SEARCH ? kBins : 1];
+          uint32_t count[SEARCH ? kBins : 1];
+        };
+        double weight[kListMax];
+      };
+    };
+    double group[W][kMaxGroups];
+  };
+  double chunk[kMaxChunks];
+  struct {
+    int listed, top_bin, bins;
+    double rest_ref, rest;
+  } part[kMaxChunks];   // of the chunks' statistics
+  union {
+    double d[W];
+    uint64_t u[W];
+    uint32_t i[W];
+    float f[W];
+  } red;
+  uint64_t before, best;
+  double sum;
+  float floor, near;
+  uint32_t n, valid, listed;
+  int pick, last, top_bin, bins;
+};
+
+// Calls f(value, column) for every unmasked entry of vectors j0 .. j1-1 of the row and after(g) with
+// all lanes together behind the g-th run of NT of them; the next run's loads are in flight.
+template <int NT, typename T, typename F, typename G>
+__device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1, F f, G after) {
+  constexpr int N = LogitRow<T>::N;
+  float x[N], y[N];
+  auto load = [&](int g, float v[N]) {
+    const int j = j0 + g * NT + int(threadIdx.x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = -INFINITY;
+    if (j < j1) r.load_raw(j, v);
+  };
+  const int groups = (j1 - j0 + NT - 1) / NT;
+  load(0, x);
+#pragma unroll 1
+  for (int g = 0; g < groups; ++g) {
+    load(g + 1, y);
+    const int c = r.column(j0 + g * NT + int(threadIdx.x));
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if (x[e] > -INFINITY) f(x[e], c + e);   // false for NaN
+      x[e] = y[e];
+    }
+    after(g);
+  }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
+  each_entry<kCutThreads>(r, 0, r.vectors(), f, [](int) {});
+}
+
+// The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
+// exchanges within 64 entries stay in a wave's registers.
+template <int NT>
+__device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  int P = 64;
+  while (P < n) P *= 2;
+  for (int i = n + int(threadIdx.x); i < P; i += NT) list[i] = 0;
+  __syncthreads();
+  auto in_waves = [&](int from, int to) {   // sizes from .. to, their exchanges of up to 32 apart
+    for (int s = wid; s * 64 < P; s += NT / kWave) {
+      const int i = s * 64 + lane;
+      uint64_t k = list[i];
+      for (int size = from; size <= to; size *= 2)
+        for (int d = size / 2 < 32 ? size / 2 : 32; d > 0; d /= 2) {
+          const uint64_t o = __shfl_xor(k, d, kWave);
+          const bool greater = ((lane & d) == 0) == ((i & size) == 0);
+          k = (o > k) == greater ? o : k;
+        }
+      list[i] = k;
+    }
+    __syncthreads();
+  };
+  in_waves(2, 64);
+  for (int size = 128; size <= P; size *= 2) {
+    for (int d = size / 2; d >= 64; d /= 2) {
+      for (int t = threadIdx.x; t < P / 2; t += NT) {
+        const int i = 2 * d * (t / d) + t % d;
+        const uint64_t a = list[i], b = list[i + d];
+        if ((a < b) == ((i & size) == 0)) {
+          list[i] = b;
+          list[i + d] = a;
+        }
+      }
+      __syncthreads();
+    }
+    in_waves(size, size);
+  }
+}
+
+// Least order key of a value in (-inf, m] for which `holds` is true, which it is from there on and
+// for m: each wave for itself, 64 candidates a round.
+template <typename F>
+__device__ __forceinline__ uint32_t least_value_key(float m, F holds) {
+  uint32_t l = 0x007FFFFFu, h = f32_order_key(m);   // the key of -inf: not among the candidates
+  while (h - l > 1) {
+    const uint32_t step = (h - l - 1) / 64 + 1;
+    const uint64_t k = uint64_t(l) + uint64_t(step) * ((threadIdx.x & 63) + 1);
+    const bool in = k < h && holds(f32_from_order_key(uint32_t(k)));
+    const unsigned long long is = __ballot(in);
+    // Lanes past h count as true: the first true one bounds the answer from above.
+    const unsigned long long past = __ballot(k >= h);
+    const unsigned long long any = is | past;
+    const int f = any != 0ull ? __ffsll(static_cast<long long>(any)) - 1 : 64;
+    const uint64_t up = uint64_t(l) + uint64_t(step) * (f + 1);
+    l += step * uint32_t(f);
+    h = up < h ? uint32_t(up) : h;
+  }
+  return h;
+}
+
+// First-level bin of a value below the row's greatest one: 64 bins a unit of (m - z) / T, so
+// monotone in the value.
+__device__ __forceinline__ int value_bin(float z, float m, float scale) {
+  return z == m ? 0 : int(fminf((m - z) * scale, float(kBins - 1)));
+}
+
+// Key of the entry with which the running sum, in order, of ones (BY_MASS false) or weights over
+// the entries with keys >= floor reaches `target`; the last of them if rounding leaves none.
+// Histograms of 2048 bins over ever smaller ranges of the order, until a bin's entries fit the
+// list: the first by value, further ones by key, where the last range is one key.  A caller that
+// knows the range of keys and the sum `above` it starts there (lo > 0).
+template <bool BY_MASS, typename T>
+__device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t floor, float m,
+                                 double c2, float scale, CutShared<kCutThreads, true>& sh, uint64_t lo = 0,
+                                 uint64_t hi = kKeyTop, double above = 0.) {
+  auto shift_of = [&]() {
+    int sh_ = 0;
+    while (((hi - lo) >> sh_) >= uint64_t(kBins)) ++sh_;
+    return sh_;
+  };
+  int shift = lo > 0 ? shift_of() : -1, bin = 0;   // shift -1: the bins by value
+  for (;;) {
+    for (int b = threadIdx.x; b < kBins; b += kCutThreads) {
+      sh.count[b] = 0;
+      sh.mass[b] = 0;
+    }
+    if (threadIdx.x == 0) sh.pick = -1, sh.last = 0;
+    __syncthreads();
+    auto bin_of = [&](float z, uint64_t k) {
+      return shift < 0 ? value_bin(z, m, scale) : int((hi - k) >> shift);
+    };
+    each_entry(r, [&](float z, int c) {
+      const uint64_t k = entry_key(z, c);
+      if (k < floor || k < lo || k > hi) return;
+      const int b = bin_of(z, k);
+      atomicAdd(&sh.count[b], 1u);
+      if (BY_MASS)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
+                  static_cast<unsigned long long>(entry_weight(z, m, c2) / kSearchUnit + 0.5));
+    });
+    __syncthreads();
+    const int b0 = 2 * threadIdx.x;
+    const uint64_t v0 = BY_MASS ? sh.mass[b0] : sh.count[b0];
+    const uint64_t v1 = BY_MASS ? sh.mass[b0 + 1] : sh.count[b0 + 1];
+    uint64_t whole;
+    const uint64_t at1 = block_scan<kCutWaves>(v0 + v1, sh.red.u, whole);
+    const double unit = BY_MASS ? kSearchUnit : 1.;
+    auto reached = [&](uint64_t s) { return above + double(s) * unit >= target; };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t after = h == 0 ? at1 - v1 : at1, before = after - (h == 0 ? v0 : v1);
+      if (reached(after) && !reached(before)) {
+        sh.pick = b0 + h;
+        sh.before = before;
+      }
+      if (sh.count[b0 + h] != 0) atomicMax(&sh.last, b0 + h);
+    }
+    __syncthreads();
+    if (sh.pick < 0 && int(threadIdx.x) == sh.last / 2) {
+      sh.before = (sh.last & 1) ? at1 - v1 : at1 - v1 - v0;
+    }
+    bin = sh.pick < 0 ? sh.last : sh.pick;
+    __syncthreads();
+    above += double(sh.before) * unit;
+    const uint32_t here = sh.count[bin];
+    if (threadIdx.x == 0) sh.n = 0, sh.pick = kListMax;
+    __syncthreads();
+    if (here <= uint32_t(kListMax)) {
+      each_entry(r, [&](float z, int c) {
+        const uint64_t k = entry_key(z, c);
+        if (k < floor || k < lo || k > hi || bin_of(z, k) != bin) return;
+        sh.list[atomicAdd(&sh.n, 1u)] = k;
+      });
+      __syncthreads();
+      const int n = int(sh.n);
+      sort_list<kCutThreads>(sh.list, n);
+      int at;
+      if (BY_MASS) {
+        const int i = 2 * threadIdx.x;
+        const double w0 = i < n ? entry_weight(entry_logit(sh.list[i]), m, c2) : 0.;
+        const double w1 = i + 1 < n ? entry_weight(entry_logit(sh.list[i + 1]), m, c2) : 0.;
+        double all;
+        const double sum = block_scan<kCutWaves>(w0 + w1, sh.red.d, all);
+        if (i < n && above + (sum - w1) >= target) atomicMin(&sh.pick, i);
+        if (i + 1 < n && above + sum >= target) atomicMin(&sh.pick, i + 1);
+        __syncthreads();
+        at = min(sh.pick, n - 1);
+      } else {
+        at = min(max(int(target - above) - 1, 0), n - 1);
+      }
+      const uint64_t k = sh.list[at];
+      __syncthreads();
+      return k;
+    }
+    if (shift < 0) {
+      // The bin's range of keys: value_bin falls as keys rise.
+      auto least = [&](int b) {
+        return uint64_t(least_value_key(m, [&](float z) { return value_bin(z, m, scale) <= b; }))
+               << kColumnBits;
+      };
+      lo = least(bin);
+      hi = bin == 0 ? kKeyTop : least(bin - 1) - 1;
+    } else {
+      hi -= uint64_t(bin) << shift;
+      const uint64_t l = hi - ((uint64_t(1) << shift) - 1);
+      lo = l > lo ? l : lo;
+    }
+    shift = shift_of();
+    __syncthreads();
+  }
+}
+
+// The weights of a row's kept entries (those before or at `cut` in the order) among vectors
+// j0 .. j1-1, a sum a group and wave in sh.group; returns their whole, `run` this thread's group's
+// running sum and `mine` its own.  COUNT: also how many, and the last one's key, of this thread.
+template <int NT, bool COUNT, bool S, typename T>
+__device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int j1, uint64_t cut,
+                                              float m, double c2, CutShared<NT, S>& sh, double& run,
+                                              double& mine, uint32_t* kept = nullptr,
+                                              uint64_t* low = nullptr) {
+  double s = 0.;
+  const float cz = entry_logit(cut);
+  const int cc = entry_column(cut);
+  each_entry<NT>(
+      r, j0, j1,
+      [&](float z, int c) {
+        if (cut != 0 && !(z > cz || (z == cz && c <= cc))) return;
+        if constexpr (COUNT) {
+          const uint64_t k = entry_key(z, c);
+          *low = k < *low ? k : *low;
+          ++*kept;
+        }
+        s += entry_weight(z, m, c2);
+      },
+      [&](int g) {
+        s = wave_fold(s, [](double u, double v) { return u + v; });
+        if ((threadIdx.x & 63) == 0) sh.group[threadIdx.x >> 6][g] = s;
+        s = 0.;
+      });
+  __syncthreads();
+  const int groups = (j1 - j0 + NT - 1) / NT;
+  mine = 0.;
+  if (int(threadIdx.x) < groups)
+    for (int w = 0; w < NT / kWave; ++w) mine += sh.group[w][threadIdx.x];
+  double all;
+  run = block_scan<NT / kWave>(mine, sh.red.d, all);
+  return all;
+}
+
+// The draw among the kept entries of vectors j0 .. j1-1, after kept_masses: the group in which
+// `base` and the running sum pass the target, then the entry; the last one where rounding leaves
+// none.
+template <int NT, bool S, typename T>
+__device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
+                                          double c2, double base, double target, double run,
+                                          double mine, CutShared<NT, S>& sh) {
+  if (threadIdx.x == 0) sh.pick = NT, sh.last = 0;
+  __syncthreads();
+  if (mine > 0.) {
+    if (base + run > target) atomicMin(&sh.pick, int(threadIdx.x));
+    atomicMax(&sh.last, int(threadIdx.x));
+  }
+  __syncthreads();
+  const int g = min(sh.pick, sh.last);
+  __syncthreads();
+  if (int(threadIdx.x) == g) sh.sum = base + (run - mine);
+  if (threadIdx.x == 0) sh.pick = NT, sh.last = -1;
+  __syncthreads();
+  const int j = j0 + g * NT + int(threadIdx.x), c = r.column(j);
+  const float cz = entry_logit(cut);
+  const int cc = entry_column(cut);
+  constexpr int N = LogitRow<T>::N;
+  float x[N];
+  double w[N], own = 0., all;
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+  if (j < j1) r.load(j, x);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const bool is = x[e] > -INFINITY && (cut == 0 || x[e] > cz || (x[e] == cz && c + e <= cc));
+    w[e] = entry_weight(is ? x[e] : -INFINITY, m, c2);
+    own += w[e];
+    if (is) atomicMax(&sh.last, c + e);
+  }
+  const double upto = sh.sum + block_scan<NT / kWave>(own, sh.red.d, all);
+  if (own > 0. && upto > target) atomicMin(&sh.pick, int(threadIdx.x));
+  __syncthreads();
+  const int who = sh.pick;
+  __syncthreads();
+  if (int(threadIdx.x) == who) {
+    double before = upto - own;
+    int tok = -1;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if (w[e] > 0. && (tok < 0 || before <= target)) tok = c + e;
+      before += w[e];
+    }
+    sh.last = tok;
+  }
+  __syncthreads();
+  return sh.last;
+}
+
+// First place, among 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes) `from` times the
+// sum of the first n_sum of them, or `target` where n_sum is 0; n where none does.  `sum` gets the
+// sum.
+template <int NT, bool STRICT, bool S, typename F>
+__device__ __forceinline__ int reach(int n, int n_sum, double from, double target, double& sum,
+                                     CutShared<NT, S>& sh, F w) {
+  int at = n;
+#pragma unroll 1
+  for (int pass = n_sum > 0 ? 0 : 1; pass < 2; ++pass) {   // the sum, then the place
+    if (threadIdx.x == 0) sh.pick = n;
+    const int m = pass == 0 ? n_sum : n;
+    double before = 0.;
+#pragma unroll 1
+    for (int b = 0; b < m; b += NT) {
+      const int i = b + int(threadIdx.x);
+      const double v = i < m ? w(i) : 0.;
+      double all;
+      const double run = before + block_scan<NT / kWave>(v, sh.red.d, all);
+      if (pass == 1 && i < m && (STRICT ? v > 0. && run > target : run >= target))
+        atomicMin(&sh.pick, i);
+      before += all;
+    }
+    __syncthreads();
+    at = sh.pick;
+    if (pass == 0) {
+      sum = before;
+      target = STRICT ? from * sum : fmax(from * sum, 1e-300);   // 0 is reached by the first, not before
+    }
+    __syncthreads();
+  }
+  return at;
+}
+
+// A row's share of the second launch's work.  With few rows one launch of large workgroups does all
+// of it; with many the lists are handled by small ones, several to a CU, and two more launches take
+// what those leave: the rows that need one more pass, and those that need the search.
+enum CutPhase { kAll, kLists, kBorder, kSearch };
+enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
+
+// The chunks' statistics joined, by the first wave.
+template <int NT, bool S>
+__device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, CutShared<NT, S>& sh) {
+  auto add = [](uint32_t u, uint32_t v) { return u + v; };
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    uint64_t best = 0;
+    uint32_t valid = 0, listed = 0;
+    float floor = -INFINITY, near = INFINITY;
+    int top_bin = -2147483647, bins = 0;
+#pragma unroll 1
+    for (int c = lane; c < chunks; c += 64) {
+      const HeadStat st = hs[c];
+      sh.part[c] = {int(st.listed), st.top_bin, st.bins, st.rest_ref, st.rest};
+      if (st.valid == 0) continue;
+      const uint64_t k = entry_key(st.best, st.best_col);
+      best = k > best ? k : best;
+      valid += st.valid;
+      listed += st.listed;
+      floor = fmaxf(floor, st.floor);
+      near = fminf(near, st.near);
+      top_bin = st.bins > 0 ? max(top_bin, st.top_bin) : top_bin;
+      bins = st.bins < 0 ? -1 : bins;
+    }
+    best = wave_fold(best, [](uint64_t u, uint64_t v) { return u > v ? u : v; });
+    valid = wave_fold(valid, add);
+    listed = wave_fold(listed, add);
+    floor = wave_fold(floor, [](float u, float v) { return fmaxf(u, v); });
+    near = wave_fold(near, [](float u, float v) { return fminf(u, v); });
+    top_bin = wave_fold(top_bin, [](int u, int v) { return max(u, v); });
+    bins = wave_fold(bins, [](int u, int v) { return min(u, v); });
+    if (lane == 0) {
+      sh.best = best;
+      sh.valid = valid;
+      sh.listed = listed;
+      sh.floor = floor;
+      sh.near = near;
+      sh.top_bin = top_bin;
+      sh.bins = bins;
+    }
+  }
+  __syncthreads();
+}
+
+// This thread's places of a row's lists, all in flight together; 0 past a chunk's list.
+template <int NT, bool S>
+__device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, const CutShared<NT, S>& sh,
+                                            uint64_t mine[kListMax / NT]) {
+  const uint64_t* list = h.list + at * h.chunks * h.cap;
+#pragma unroll
+  for (int q = 0; q < kListMax / NT; ++q) {
+    const int i = q * NT + int(threadIdx.x), c = i / h.cap;
+    const bool is = c < h.chunks && i - c * h.cap < sh.part[c].listed;
+    mine[q] = list[is ? i : 0];
+    mine[q] = is ? mine[q] : 0ull;
+  }
+}
+// The listed entries of value >= t and < over into the list; how many.
+template <int NT, bool S>
+__device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float t, float over,
+                                      CutShared<NT, S>& sh) {
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kListMax / NT; ++q) {
+    const float z = entry_logit(mine[q]);
+    if (mine[q] != 0 && z >= t && (z < over || over == INFINITY))
+      sh.list[atomicAdd(&sh.n, 1u)] = mine[q];
+  }
+  __syncthreads();
+  const int n = int(sh.n);
+  __syncthreads();
+  return n;
+}
+
+// The first K entries of a row and the log-sum-exp of the others.
+template <typename T, int NT, CutPhase PHASE>
+__global__ void __launch_bounds__(NT)
+row_top_kernel(CutArgs a, HeadArgs h) {
+  constexpr bool LISTS = PHASE != kSearch, SEARCH = PHASE != kLists;
+  constexpr int W = NT / kWave;
+  __shared__ CutShared<NT, SEARCH> sh;
+  const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
+  const int tid = threadIdx.x, K = a.K;
+  if (PHASE == kSearch && h.notes[at].left != kLeftSearch) return;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
+  const RowSettings s = settings_of<true>(a, row);
+  auto add = [](double u, double v) { return u + v; };
+  auto most64 = [](uint64_t u, uint64_t v) { return u > v ? u : v; };
+  join_chunks(h.stats + at * h.chunks, h.chunks, sh);
+  const uint32_t valid = sh.valid;
+  const int n = int(min(uint32_t(K), valid));
+  int have = 0;
+  bool done = false;
+  if constexpr (LISTS) {
+    uint64_t mine[kListMax / NT];
+    load_listed(h, at, sh, mine);
+    const float floor = sh.floor;
+    // As far down as the chunks' shares go (every entry >= floor is listed), or to the floor.
+    float t = fmaxf(floor, sh.near);
+#pragma unroll 1
+    for (;;) {
+      have = gather(mine, t, INFINITY, sh);
+      if (have >= n || t <= floor) break;
+      t = floor;
+    }
+    done = have >= n;
+    if (PHASE == kLists && tid == 0) h.notes[at].left = done ? kDone : kLeftSearch;
+    if (done) {
+      sort_list<NT>(sh.list, have);
+      if (a.rest != nullptr) {
+        const uint64_t last = n > 0 ? sh.list[n - 1] : 0;
+        double ref = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kListMax / NT; ++q)
+          if (mine[q] != 0 && mine[q] < last) ref = fmax(ref, double(entry_logit(mine[q])));
+        const bool rest = tid < h.chunks && sh.part[tid].rest > 0.;
+        if (rest) ref = fmax(ref, sh.part[tid].rest_ref);
+        ref = block_fold<W>(ref, sh.red.d, [](double u, double v) { return fmax(u, v); });
+        double sum = rest ? sh.part[tid].rest * exp2_64((sh.part[tid].rest_ref - ref) * s.c2) : 0.;
+#pragma unroll
+        for (int q = 0; q < kListMax / NT; ++q)
+          if (mine[q] != 0 && mine[q] < last)
+            sum += exp2_64((double(entry_logit(mine[q])) - ref) * s.c2);
+        sum = block_fold<W>(sum, sh.red.d, add);
+        if (tid == 0) a.rest[row] = sum > 0. ? float(ref * s.inv_t + log(sum)) : -INFINITY;
+      }
+    } else if (PHASE == kLists) {
+      return;
+    }
+  }
+  if constexpr (SEARCH) {
+    if (!done) {
+      const uint64_t cut = valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, entry_logit(sh.best),
+                                                                     s.c2, float(64. * s.inv_t), sh)
+                                               : 0;
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      uint64_t next = 0;   // the first entry past the list
+      each_entry(r, [&](float z, int c) {
+        const uint64_t k = entry_key(z, c);
+        if (k >= cut)
+          sh.list[atomicAdd(&sh.n, 1u)] = k;
+        else
+          next = k > next ? k : next;
+      });
+      __syncthreads();
+      sort_list<NT>(sh.list, n);
+      if (a.rest != nullptr) {
+        next = block_fold<W>(next, sh.red.u, most64);
+        const float top = entry_logit(next);
+        double sum = 0.;
+        if (next != 0)
+          each_entry(r, [&](float z, int c) {
+            if (entry_key(z, c) < cut) sum += entry_weight(z, top, s.c2);
+          });
+        sum = block_fold<W>(sum, sh.red.d, add);
+        if (tid == 0)
+          a.rest[row] = next != 0 ? float(double(top) * s.inv_t + log(sum)) : -INFINITY;
+      }
+    }
+  }
+  for (int i = tid; i < K; i += NT) {
+    const uint64_t k = sh.list[i < n ? i : 0];
+    a.ids[row * K + i] = i < n ? entry_column(k) : -1;
+    a.vals[row * K + i] = i < n ? entry_logit(k) : -INFINITY;
+  }
+}
+
+// A row's truncation and draw.
+template <typename T, int NT, CutPhase PHASE>
+__global__ void __launch_bounds__(NT)
+row_cut_kernel(CutArgs a, HeadArgs h) {
+  constexpr bool LISTS = PHASE == kAll || PHASE == kLists, BORDER = PHASE == kAll || PHASE == kBorder,
+                 SEARCH = PHASE == kAll || PHASE == kSearch;
+  constexpr int W = NT / kWave, PER = kMassBins / NT, LISTED = kListMax / NT;
+  // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
+  // whose masses the histograms hold, one chunk is read instead.
+  constexpr int kInOrder = 512;
+  __shared__ CutShared<NT, SEARCH> sh;
+  const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  CutNote* note = h.notes + at;
+  if (PHASE == kBorder && note->left != kLeftBorder) return;
+  if (PHASE == kSearch && note->left != kLeftSearch) return;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
+  const RowSettings s = settings_of<false>(a, row);
+  auto add = [](auto u, auto v) { return u + v; };
+  auto most64 = [](uint64_t u, uint64_t v) { return u > v ? u : v; };
+  auto least64 = [](uint64_t u, uint64_t v) { return u < v ? u : v; };
+  auto leave = [&](int left) {
+    if (tid == 0) note->left = left;
+  };
+  join_chunks(h.stats + at * h.chunks, h.chunks, sh);
+  const uint64_t best = sh.best;
+  const uint32_t valid = sh.valid, listed = sh.listed;
+  const float m = entry_logit(best), floor = sh.floor;
+  const int top_bin = sh.top_bin;
+  const bool whole = listed == valid;   // nothing is unlisted
+  const bool binned = s.binned && sh.bins == 0;
+  if (PHASE == kLists) leave(kDone);
+
+  if (LISTS && (valid == 0 || s.greedy)) {
+    if (tid == 0) {
+      if (a.tok != nullptr) a.tok[row] = valid != 0 ? entry_column(best) : -1;
+      a.kept[row] = valid != 0 ? 1 : 0;
+      a.cut_logit[row] = valid > 1 ? m : -INFINITY;
+      a.cut_index[row] = valid > 1 ? entry_column(best) : -1;
+      a.lse[row] = valid != 0 ? 0. : -INFINITY;
+    }
+    return;
+  }
+  const bool has_k = s.top_k > 0 && uint32_t(s.top_k) < valid;
+  const bool has_p = s.top_p < 1.f, has_m = s.min_p > 0.f;
+  const double u = a.u != nullptr ? fmin(fmax(double(a.u[row]), 0.), 1.) : 0.;
+  auto write = [&](uint32_t kept, uint64_t low, double mass, int tok) {
+    if (tid != 0) return;
+    const bool every = kept == valid;
+    a.kept[row] = int32_t(kept);
+    a.cut_logit[row] = every ? -INFINITY : entry_logit(low);
+    a.cut_index[row] = every ? -1 : entry_column(low);
+    a.lse[row] = double(m) * s.inv_t + log(mass);
+    if (a.tok != nullptr) a.tok[row] = tok;
+  };
+
+  uint64_t mine[LISTED];
+  if constexpr (LISTS) load_listed(h, at, sh, mine);
+
+  // Least value of weight min_p, as the key of its last possible entry.
+  uint64_t cut_m = 0;
+  if (has_m) {
+    const double least = fmin(double(s.min_p), 1.);
+    const uint32_t k = least_value_key(m, [&](float z) { return entry_weight(z, m, s.c2) >= least; });
+    cut_m = uint64_t(f32_order_key(f32_from_order_key(k) + 0.f)) << kColumnBits;
+  }
+
+  // A cut by weight: the histograms joined.  The border bin is that of top_p's cut or of min_p's.
+  const double k16 = 16. * s.c2;
+  double whole_w = 0., above = 0.;   // relative to the greatest entry: the whole, the bins above
+  int border = 0;
+  bool by_p = false;   // whether top_p's cut lies in it
+  auto bin_weight = [&](int b) { return exp2_64(-double(b) / 16.); };
+  // 2^-48 of the top bin's middle, relative to the greatest entry's weight.
+  const double unit = binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * kMassUnit : 0.;
+  const uint64_t* masses = h.mass + at * h.chunks * kMassBins;
+  auto mass_at = [&](int c, int b) -> double {   // of chunk c in the row's bin b
+    const int i = b - (top_bin - sh.part[c].top_bin);
+    const bool is = i >= 0 && i < sh.part[c].bins;
+    const uint64_t n = masses[int64_t(c) * kMassBins + (is ? i : 0)];   // loaded in any case
+    return is ? double(n) : 0.;
+  };
+  if constexpr (LISTS) {
+    if (binned) {
+      double v[PER], sum = 0.;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) v[e] = 0.;
+      constexpr int AHEAD = 8 / (PER > 1 ? 2 : 1);   // chunks whose loads are in flight together
+#pragma unroll 1
+      for (int c0 = 0; c0 < h.chunks; c0 += AHEAD) {
+        double x[AHEAD][PER];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+          for (int e = 0; e < PER; ++e) x[i][e] = mass_at(min(c0 + i, h.chunks - 1), PER * tid + e);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+          for (int e = 0; e < PER; ++e) v[e] += c0 + i < h.chunks ? x[i][e] : 0.;
+      }
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        v[e] *= bin_weight(PER * tid + e) * unit;
+        sum += v[e];
+      }
+      const double run = block_scan<W>(sum, sh.red.d, whole_w);
+      if (tid == 0) sh.pick = kMassBins, sh.last = 0;
+      __syncthreads();
+      const double target = has_p ? fmax(double(s.top_p) * whole_w, 1e-300) : INFINITY;
+      double upto = run - sum;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        upto += v[e];
+        if (v[e] > 0.) {
+          if (upto >= target) atomicMin(&sh.pick, PER * tid + e);
+          atomicMax(&sh.last, PER * tid + e);
+        }
+      }
+      __syncthreads();
+      border = min(sh.pick, sh.last);
+      by_p = has_p;
+      if (has_m) {
+        const int b = min(top_bin - weight_bin(entry_logit(cut_m), k16), kMassBins - 1);
+        by_p = has_p && border <= b;
+        border = min(border, b);
+      }
+      upto = run - sum;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        if (PER * tid + e == border) sh.sum = upto;
+        upto += v[e];
+      }
+      __syncthreads();
+      above = sh.sum;
+      __syncthreads();
+      if (PHASE == kLists && tid == 0)
+        note->whole = whole_w, note->above = above, note->border = border, note->by_p = by_p;
+    }
+  } else if (binned) {
+    whole_w = note->whole;
+    above = note->above;
+    border = note->border;
+    by_p = note->by_p != 0;
+  }
+  // Least value of bin b or a greater one.
+  auto bin_edge = [&](int b) {
+    return f32_from_order_key(least_value_key(m, [&](float z) {   // far values have no bin
+      return double(z) * k16 > double(top_bin) - 2048. && weight_bin(z, k16) >= top_bin - b;
+    }));
+  };
+
+  uint64_t cut = 0;
+  if (binned || PHASE == kBorder || (LISTS && (has_k || whole))) {
+    // The entries that the cut lies among, sorted; `greater` more lie above them.
+    float end = 0.f, over = INFINITY;
+    uint32_t greater = 0;
+    int n = 0;
+    bool from_lists = !binned;
+#pragma unroll 1
+    for (;;) {
+      if (binned && !s.open) {
+        end = bin_edge(border);
+        over = border > 0 ? bin_edge(border - 1) : INFINITY;
+        from_lists = LISTS && end >= floor;
+      } else if (binned) {
+        break;   // nothing is cut
+      }
+      if (LISTS && from_lists) {
+        float t = binned ? end : has_k ? fmaxf(floor, sh.near) : floor;
+#pragma unroll 1
+        for (;;) {
+          n = gather(mine, t, over, sh);
+          if (!has_k || n >= s.top_k || t <= floor) break;
+          t = floor;
+        }
+      } else if (BORDER && binned) {
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        greater = 0;
+        constexpr int N = LogitRow<T>::N, Q = 32 / N;
+        const int nv = r.vectors();
+#pragma unroll 1
+        for (int b = 0; b < nv; b += Q * NT) {
+          float x[Q][N];
+          if (r.inside(b, Q * NT)) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) r.load_inside(b + q * NT + tid, x[q]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+#pragma unroll
+              for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
+              if (b + q * NT + tid < nv) r.load_raw(b + q * NT + tid, x[q]);
+            }
+          }
+          uint32_t bits = 0;   // of the border bin, the first entry's bit the highest
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const bool up = x[q][e] >= over;
+              greater += uint32_t(__popcll(__ballot(up)));
+              bits = 2 * bits + uint32_t(x[q][e] >= end && !up);
+            }
+          while (bits != 0) {
+            const int q = 32 - __ffs(bits);
+            bits &= bits - 1;
+            const int c = r.column(b + q / N * NT + tid) + q % N;
+            const uint32_t i = atomicAdd(&sh.n, 1u);
+            if (i < uint32_t(kListMax)) sh.list[i] = entry_key(r.raw(c), c);
+          }
+        }
+        greater = block_fold<W>(lane == 0 ? greater : 0u, sh.red.i, add);
+        n = int(sh.n);
+        __syncthreads();
+      } else {
+        break;
+      }
+      if (n == 0 || n > kListMax || (has_k && n < s.top_k)) break;
+      sort_list<NT>(sh.list, n);
+      for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
+      __syncthreads();
+      int k = has_k ? s.top_k : n;
+      if (binned ? by_p : has_p) {
+        double sum;
+        const int p = reach<NT, false>(k, binned ? 0 : k, double(s.top_p),
+                                       fmax(double(s.top_p) * whole_w, 1e-300) - above, sum, sh,
+                                       [&](int i) { return sh.weight[i]; });
+        k = min(k, p + 1);
+      }
+      if (cut_m != 0) {
+        uint32_t c = 0;
+        for (int i = tid; i < k; i += NT) c += sh.list[i] >= cut_m;
+        k = int(block_fold<W>(c, sh.red.i, add));
+      }
+      if (k > 0) {
+        cut = sh.list[k - 1];
+        greater += uint32_t(k);
+        break;
+      }
+      // min_p's cut lies above all of its bin's entries: the last bin before with any.
+      if (tid == 0) sh.last = 0;
+      __syncthreads();
+      for (int b = tid; b < border; b += NT) {
+        double any = 0.;
+        for (int c = 0; c < h.chunks; ++c) any += mass_at(c, b);
+        if (any > 0.) atomicMax(&sh.last, b);
+      }
+      __syncthreads();
+      border = sh.last;
+      by_p = false;
+      __syncthreads();
+    }
+
+    if constexpr (LISTS) {
+      if (from_lists && cut != 0) {
+        // All kept entries are listed: in token order, columns with their places as keys, the
+        // weights beside them.
+        uint32_t many = 0;
+        uint64_t low = kKeyTop;
+#pragma unroll
+        for (int q = 0; q < LISTED; ++q)
+          if (mine[q] != 0 && mine[q] >= cut) {
+            low = least64(low, mine[q]);
+            ++many;
+          }
+        many = block_fold<W>(many, sh.red.i, add);
+        greater = many;
+        if (!binned || many <= uint32_t(kInOrder)) {
+          low = block_fold<W>(low, sh.red.u, least64);
+          if (tid == 0) sh.n = 0;
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < LISTED; ++q)
+            if (mine[q] != 0 && mine[q] >= cut) {
+              const uint32_t i = atomicAdd(&sh.n, 1u);
+              sh.list[i] = ((mine[q] & kColumnMask) << 12) | uint64_t(i);
+              sh.weight[i] = double(entry_logit(mine[q]));
+            }
+          __syncthreads();
+          const int k = int(many);
+          for (int i = tid; i < k; i += NT) sh.weight[i] = entry_weight(float(sh.weight[i]), m, s.c2);
+          sort_list<NT>(sh.list, k);
+          double mass;
+          int i = reach<NT, true>(k, k, u, 0., mass, sh,
+                                  [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
+          if (i == k) {   // the last with a weight
+            if (tid == 0) sh.last = 0;
+            __syncthreads();
+            for (int q = tid; q < k; q += NT)
+              if (sh.weight[sh.list[q] & 4095u] > 0.) atomicMax(&sh.last, q);
+            __syncthreads();
+            i = sh.last;
+          }
+          write(many, low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
+          return;
+        }
+      }
+      if (PHASE == kLists) {
+        leave(binned ? kLeftBorder : kLeftSearch);
+        return;
+      }
+    }
+    if constexpr (BORDER) {
+      if (binned && (cut != 0 || s.open)) {
+        // The chunks' masses: their bins above the border, and their part of its entries.
+        if (s.open) border = kMassBins, greater = valid, n = 0;
+#pragma unroll 1
+        for (int c = wid; c < h.chunks; c += W) {
+          double w = 0.;
+#pragma unroll 2
+          for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
+#pragma unroll 1
+          for (int i = lane; i < n; i += 64) {
+            const uint64_t k = sh.list[i];
+            const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
+            if (k >= cut && j / h.vectors == c) w += sh.weight[i];
+          }
+          w = wave_fold(w, add);
+          if (lane == 0) sh.chunk[c] = w;
+        }
+        __syncthreads();
+        // The draw: only the chunk that the running sum passes the target in is read.
+        const double w = tid < h.chunks ? sh.chunk[tid] : 0.;
+        double mass;
+        const double run = block_scan<W>(w, sh.red.d, mass);
+        int tok = -1;
+        if (a.tok != nullptr) {
+          const double target = u * mass;
+          if (tid == 0) sh.pick = NT, sh.last = 0;
+          __syncthreads();
+          if (w > 0.) {
+            if (run > target) atomicMin(&sh.pick, tid);
+            atomicMax(&sh.last, tid);
+          }
+          __syncthreads();
+          const int c = min(sh.pick, sh.last);
+          __syncthreads();
+          if (tid == c) sh.sum = run - w;
+          __syncthreads();
+          const double base = sh.sum;
+          const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
+          double grun, gmine;
+          kept_masses<NT, false>(r, j0, j1, cut, m, s.c2, sh, grun, gmine);
+          tok = draw_entry<NT>(r, j0, j1, cut, m, s.c2, base, target, grun, gmine, sh);
+        }
+        write(greater, cut, mass, tok);
+        return;
+      }
+      if (PHASE == kBorder) {
+        leave(kLeftSearch);
+        return;
+      }
+    }
+  } else if (PHASE == kLists) {
+    leave(kLeftSearch);
+    return;
+  }
+  if constexpr (SEARCH) {
+    // Neither the lists nor the histograms tell: counts of very many entries, values beyond the
+    // bins, border bins of more entries than are sorted.
+    const float scale = float(64. * s.inv_t);
+    cut = has_k ? select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh) : 0;
+    if (binned ? by_p : has_p) {
+      uint64_t end = 0, over = kKeyTop;
+      double all = whole_w;
+      if (binned) {
+        end = entry_key(bin_edge(border), a.V - 1);
+        over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
+      } else {
+        all = 0.;
+        each_entry(r, [&](float z, int c) {
+          if (entry_key(z, c) >= cut) all += entry_weight(z, m, s.c2);
+        });
+        all = block_fold<W>(all, sh.red.d, add);
+      }
+      // A target of 0 is reached by the first entry, not before it.
+      cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2, scale,
+                                           sh, end, over, binned ? above : 0.));
+    }
+    cut = most64(cut, cut_m);
+    double run, own;
+    uint32_t kept = 0;
+    uint64_t low = kKeyTop;
+    const double mass =
+        kept_masses<NT, true>(r, 0, r.vectors(), cut, m, s.c2, sh, run, own, &kept, &low);
+    kept = block_fold<W>(kept, sh.red.i, add);
+    low = block_fold<W>(low, sh.red.u, least64);
+    const int tok = a.tok != nullptr ? draw_entry<NT>(r, 0, r.vectors(), cut, m, s.c2, 0., u * mass, run,
+                                                      own, sh)
+                                     : -1;
+    write(kept, low, mass, tok);
+  }
+}
+
+static size_t al256(size_t x) { return (x + 255) / 256 * 256; }
+
+// The first launch's chunks: 16384 columns each, or 4096 where those would leave CUs idle (and the
+// lists of so many chunks still hold enough).
+struct HeadPlan {
+  int chunks, elems;
+};
+static HeadPlan head_plan(bool bf16, int64_t rows, int V) {
+  const int N = bf16 ? 8 : 4, span = (V + 2 * N - 2) / N * N;
+  const int large = (span + 32 * kHeadThreads - 1) / (32 * kHeadThreads);
+  const int small = (span + 8 * kHeadThreads - 1) / (8 * kHeadThreads);
+  if (rows * large < device_cu_count() && small <= 64) return {small, 8};
+  return {large, 32};
+}
+// Rows of one group of launches; more run in turns over the same workspace.
+constexpr int64_t kCutChunks = 8192;
+static int64_t cut_rows(bool bf16, int64_t rows, int V) {
+  const int64_t most = kCutChunks / head_plan(bf16, kCutChunks, V).chunks;
+  return rows < most ? rows : most;
+}
+// Above this many rows (a workgroup a CU) the second launch's phases run apart.
+constexpr int64_t kCombinedRows = 256;
+constexpr int kListThreads = 256, kBorderThreads = 512;
+
+size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
+  const int64_t n = cut_rows(bf16, rows, V);
+  // The lists of a row hold kListMax entries whatever its chunks.  Small chunks are more of them, but
+  // only of few rows.
+  int64_t chunks = n * head_plan(bf16, kCutChunks, V).chunks;
+  const int64_t few = n < device_cu_count() ? n : device_cu_count();
+  const HeadPlan fine = head_plan(bf16, 0, V);
+  const int64_t fine_chunks = few * fine.chunks;
+  chunks = chunks > fine_chunks ? chunks : fine_chunks;
+  return al256(size_t(n) * kListMax * 8) + al256(size_t(n) * sizeof(CutNote)) + al256(size_t(chunks) * sizeof(HeadStat)) +
+         (top ? 0 : al256(size_t(chunks) * kMassBins * 8));
+}
+
+template <typename T, bool TOP>
+static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
+  const bool bf16 = sizeof(T) == 2;
+  const int64_t most = cut_rows(bf16, all.rows, all.V);
+  for (int64_t r0 = 0; r0 < all.rows; r0 += most) {
+    CutArgs a = all;
+    a.rows = all.rows - r0 < most ? all.rows - r0 : most;
+    a.row0 = r0;
+    const HeadPlan pl = head_plan(bf16, a.rows, a.V);
+    char* p = static_cast<char*>(ws);
+    auto take = [&](size_t bytes) {
+      char* q = p;
+      p += al256(bytes);
+      return q;
+    };
+    HeadArgs h;
+    h.chunks = pl.chunks;
+    h.cap = kListMax / pl.chunks;
+    h.vectors = pl.elems * kHeadThreads / LogitRow<T>::N;
+    h.list = reinterpret_cast<uint64_t*>(take(size_t(a.rows) * kListMax * 8));
+    h.notes = reinterpret_cast<CutNote*>(take(size_t(a.rows) * sizeof(CutNote)));
+    h.stats = reinterpret_cast<HeadStat*>(take(size_t(a.rows) * pl.chunks * sizeof(HeadStat)));
+    h.mass = reinterpret_cast<uint64_t*>(p);
+    hipError_t e = launch_row_head(bf16, TOP, pl.elems == 8, a, h, s);
+    if (e != hipSuccess) return e;
+    const dim3 rows(unsigned(a.rows)), one(kCutThreads);
+    const bool apart = a.rows > kCombinedRows;
+    if constexpr (TOP) {
+      if (apart) {
+        hipLaunchKernelGGL((row_top_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kSearch>), rows, one, 0, s, a, h);
+      } else {
+        hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kAll>), rows, one, 0, s, a, h);
+      }
+    } else if (apart) {
+      hipLaunchKernelGGL((row_cut_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((row_cut_kernel<T, kBorderThreads, kBorder>), rows, dim3(kBorderThreads), 0, s, a, h);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kSearch>), rows, one, 0, s, a, h);
+    } else {
+      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kAll>), rows, one, 0, s, a, h);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_truncate(bool bf16, const CutArgs& a, void* ws, hipStream_t s) {
+  return bf16 ? launch_cut<bf16_t, false>(a, ws, s) : launch_cut<float, false>(a, ws, s);
+}
+hipError_t launch_top_logits(bool bf16, const CutArgs& a, void* ws, hipStream_t s) {
+  return bf16 ? launch_cut<bf16_t, true>(a, ws, s) : launch_cut<float, true>(a, ws, s);
+}
+
+}  // namespace hdf

@@ -1,0 +1,111 @@
+// Rows of logits cut to the head of their distribution: truncated draws (temperature, top-k,
+// top-p, min-p) and a row's top logits.
+//
+// The entries of a row are ordered by value, ties to the lowest column; masked ones (-inf) have
+// no place.  With m the greatest and w_v = e^((z_v - m) / T), the kept entries are the first
+//     n = min(n_k, n_p, n_m):  n_k = top_k;  n_p = the fewest of those whose weights sum to top_p
+//     of the first n_k entries' sum;  n_m = those with w_v >= min_p.
+// The draw is the lowest column whose running sum of kept weights, in column order, passes
+// u times their whole.  Sums are 64-bit throughout: a cut or a draw falls between neighbours that
+// may be 1e-6 of the whole apart.
+//
+// First launch (row_head.hip): workgroup (row, chunk) keeps a chunk of a row in registers, lists
+// its greatest entries and, where the cut is not a count of entries, sums the weights up in a
+// histogram.  Second launch (row_cut.hip): a workgroup a row finds how far down the order the cut
+// lies; a cut below the lists takes one more pass over the row.
+#pragma once
+
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace hdf {
+
+constexpr int kHeadThreads = 512;
+constexpr int kListMax = 2048;               // listed entries of a row; entries sorted at once
+constexpr int kMaxChunks = 66;
+constexpr float kLeast = -3.402823466e38f;   // the least finite value
+
+// The histogram: bins of 1/16 octave of weight.  Entry z has t = 16 z log2(e) / T, bin n = rint(t)
+// and within it the weight 2^((t - n) / 16), 0.978 .. 1.022, as a multiple of 2^-48; integers, so
+// that the sums do not depend on their order.  1024 bins from the chunk's greatest entry down;
+// entries more than 62 octaves below it weigh nothing.
+constexpr int kMassBins = 1024;
+constexpr double kMassUnit = 1.0 / 281474976710656.0;   // 2^-48
+
+struct HeadStat {
+  float best;        // greatest value, its lowest column
+  int32_t best_col;
+  float floor;       // every entry >= floor is listed (-inf: all are)
+  float near;        // a value that the chunk's share of the top_k entries reaches
+  uint32_t valid;    // unmasked entries, listed ones
+  uint32_t listed;
+  int32_t top_bin;   // bin of the greatest value, and how many bins from it down are stored
+  int32_t bins;      // (-1: values beyond the bins' range)
+  double rest_ref;   // of top logits: rest = the sum of e^((z - rest_ref) / T) over the unlisted
+  double rest;
+};
+
+// Between the phases of a row's cut: a nucleus' border bin, the weights above it and in the whole.
+struct CutNote {
+  double whole, above;
+  int32_t border, by_p, left;
+};
+
+struct HeadArgs {
+  int chunks, cap, vectors;   // of a row; entries a chunk may list; vectors of a chunk
+  uint64_t* list;             // [rows][chunks][cap]
+  HeadStat* stats;            // [rows][chunks]
+  uint64_t* mass;             // [rows][chunks][kMassBins]
+  CutNote* notes;             // [rows]
+};
+
+// A row's settings.
+struct RowSettings {
+  float t, top_p, min_p;
+  int top_k;
+  bool greedy, binned;   // binned: the cut, or the draw, goes by weight and not by count
+  bool open;             // nothing is cut
+  double inv_t, c2;
+};
+template <bool TOP>
+__device__ __forceinline__ RowSettings settings_of(const CutArgs& a, int64_t row) {
+  RowSettings s;
+  const int64_t i = TOP ? 0 : row / a.per;
+  s.t = !TOP && a.ts != nullptr ? a.ts[i] : a.t;
+  s.greedy = !(s.t > 0.f);
+  s.top_k = TOP ? a.K : a.ks != nullptr ? a.ks[i] : a.k;
+  s.top_p = TOP ? 1.f : a.ps != nullptr ? a.ps[i] : a.p;
+  s.min_p = TOP ? 0.f : a.mps != nullptr ? a.mps[i] : a.mp;
+  if (!TOP && s.top_k >= a.V) s.top_k = 0;
+  s.binned = !s.greedy && s.top_k <= 0;
+  s.open = s.binned && !(s.top_p < 1.f) && !(s.min_p > 0.f);
+  s.inv_t = s.greedy ? 1. : 1. / double(s.t);
+  s.c2 = 1.4426950408889634074 * s.inv_t;
+  return s;
+}
+
+// Bin of a value and the weight within it (a multiple of 2^-48 in the low bits).  The magic
+// constants round to an integer in the low bits of the sum; the series is that of 2^(g / 16),
+// |g| <= 1/2, whose first dropped term is 0.022^7 / 7! = 4e-16.
+__device__ __forceinline__ int weight_bin(float z, double k16) {
+  const double t = fma(double(z), k16, 6755399441055744.);   // 1.5 * 2^52
+  return int(uint32_t(__builtin_bit_cast(uint64_t, t)));
+}
+__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, int& n) {
+  const double t = fma(double(z), k16, 6755399441055744.);
+  n = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
+  const double g = fma(double(z), k16, -(t - 6755399441055744.));
+  constexpr double c = 0.69314718055994530942 / 16.;
+  double p = c * c * c * c * c * c / 720.;
+  p = fma_k(p, g, c * c * c * c * c / 120.);
+  p = fma_k(p, g, c * c * c * c / 24.);
+  p = fma_k(p, g, c * c * c / 6.);
+  p = fma_k(p, g, c * c / 2.);
+  p = fma_k(p, g, c);
+  p = fma_k(p, g, 17.);   // 16 + 1: a unit of 16's last place is 2^-48
+  return __builtin_bit_cast(uint64_t, p) - 0x4030000000000000ull;
+}
+
+hipError_t launch_row_head(bool bf16, bool top, bool small, const CutArgs& a, const HeadArgs& h, hipStream_t s);
+
+}  // namespace hdf

@@ -1,0 +1,224 @@
+// First launch of a row's cut (row_cut.hpp).
+#include "row_cut.hpp"
+
+namespace hdf {
+
+constexpr int kHeadWaves = kHeadThreads / kWave;
+
+// The greatest of three values, none of them NaN.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+// bits * 2 + (x >= lo), which is false for NaN.
+__device__ __forceinline__ uint32_t push_at_least(uint32_t bits, float x, float lo) {
+  uint32_t d;
+  asm("v_cmp_ge_f32 vcc, %2, %3\n\tv_addc_co_u32 %0, vcc, %1, %1, vcc"
+      : "=v"(d)
+      : "v"(bits), "v"(x), "v"(lo)
+      : "vcc");
+  return d;
+}
+
+// A chunk of a row: E entries a thread.
+template <typename T, int E, bool TOP>
+__global__ void __launch_bounds__(kHeadThreads)
+row_head_kernel(CutArgs a, HeadArgs h) {
+  constexpr int N = LogitRow<T>::N, G = E / N;
+  __shared__ unsigned long long mass[kMassBins];
+  __shared__ uint32_t count[kHeadThreads];
+  __shared__ union {
+    double d[kHeadWaves];
+    float f[kHeadWaves];
+    uint32_t i[kHeadWaves];
+  } red;
+  __shared__ uint32_t wave_n[kHeadWaves];
+  __shared__ int best_col;
+  const int64_t at = blockIdx.x / h.chunks, row = a.row0 + at;   // in the launch, in the call
+  const int chunk = int(blockIdx.x - at * h.chunks), tid = threadIdx.x;
+  const int lane = tid & 63, wid = tid >> 6;
+  const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
+  const int j0 = chunk * G * kHeadThreads, nv = r.vectors();
+  float x[G][N];
+  if (r.inside(j0, G * kHeadThreads)) {   // all but a row's first and last chunk
+#pragma unroll
+    for (int g = 0; g < G; ++g) r.load_inside(j0 + g * kHeadThreads + tid, x[g]);
+  } else {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int j = j0 + g * kHeadThreads + tid;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+      if (j < nv) r.load_raw(j, x[g]);
+    }
+  }
+  const RowSettings s = settings_of<TOP>(a, row);
+  auto col = [&](int g, int e) { return r.column(j0 + g * kHeadThreads + tid) + e; };
+  auto add = [](auto u, auto v) { return u + v; };
+  auto most = [](float u, float v) { return fmaxf(u, v); };
+  auto least = [](float u, float v) { return fminf(u, v); };
+  // Unmasked entries (NaN is masked: no comparison holds for it), the greatest one.
+  uint32_t live = 0;
+  float top = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      // (A ballot of "> -inf" comes out as "unequal or NaN" here: the least value instead.)
+      const bool is0 = x[g][e] >= kLeast, is1 = x[g][e + 1] >= kLeast;
+      live += uint32_t(__popcll(__ballot(is0))) + uint32_t(__popcll(__ballot(is1)));
+      x[g][e] = is0 ? x[g][e] : -INFINITY;
+      x[g][e + 1] = is1 ? x[g][e + 1] : -INFINITY;
+      top = max3(top, x[g][e], x[g][e + 1]);
+    }
+  if (tid == 0) best_col = a.V;
+  if (lane == 0) wave_n[wid] = live;
+  const float m = block_fold<kHeadWaves>(top, red.f, most);
+  uint32_t valid = 0;
+#pragma unroll
+  for (int w = 0; w < kHeadWaves; ++w) valid += wave_n[w];
+  if (top == m && m > -INFINITY) {
+    int first = a.V;
+#pragma unroll
+    for (int g = G - 1; g >= 0; --g)
+#pragma unroll
+      for (int e = N - 1; e >= 0; --e) first = x[g][e] == m ? col(g, e) : first;
+    atomicMin(&best_col, first);
+  }
+  __syncthreads();
+
+  // The list: all entries >= lo, lo a thread's greatest value such that `want` threads reach it; so
+  // at least `want` entries do, and hardly more unless the great ones crowd into few threads (then
+  // fewer threads are asked for).  A histogram of the 512 greatest values finds it.  Values far
+  // below the chunk's greatest (masks by the type's lowest value) would widen its bins: they take
+  // no part.  near: the same for the few entries a chunk has to contribute on the average.
+  float lo = INFINITY, near = INFINITY;
+  uint32_t listed = 0;
+  if (!s.greedy && !s.open && valid > 0) {
+    const float far = m - 64.f * fmaxf(s.t, 1.f);
+    const bool in = top > far;
+    const float low = block_fold<kHeadWaves>(in ? top : INFINITY, red.f, least);
+    const float scale = float(kHeadThreads) / (m - low);
+    const int mine = top == m ? 0 : int(fminf((m - top) * scale, float(kHeadThreads - 1)));
+    int want = s.top_k > 0 ? int(fminf(float(s.top_k) + 4.f, float(kHeadThreads))) : h.cap;
+    const int most_wanted = 2 * h.cap / 3 > 0 ? 2 * h.cap / 3 : 1;
+    want = want < most_wanted ? want : most_wanted;
+    const int few = s.top_k > 0 ? (s.top_k + h.chunks - 1) / h.chunks : 1;
+    count[tid] = 0;
+    __syncthreads();
+    if (in) atomicAdd(&count[mine], 1u);
+    __syncthreads();
+    uint32_t all;
+    const uint32_t upto = block_scan<kHeadWaves>(count[tid], red.i, all);
+    count[tid] = upto;
+    __syncthreads();
+    const uint32_t first = in && mine > 0 ? count[mine - 1] : 0u;   // threads in the bins before
+    near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
+    const bool every = valid <= uint32_t(h.cap);
+    uint32_t bits = 0, before = 0;   // this thread's listed entries, the first one's bit the highest
+    for (; want > 0; want /= 2) {
+      lo = every ? kLeast
+                 : block_fold<kHeadWaves>(in && first < uint32_t(want) ? top : INFINITY, red.f, least);
+      bits = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e) bits = push_at_least(bits, x[g][e], lo);
+      const uint32_t n = __popc(bits);
+      before = block_scan<kHeadWaves>(n, red.i, listed) - n;
+      if (listed <= uint32_t(h.cap)) break;
+    }
+    if (want == 0) {
+      lo = INFINITY;
+      listed = bits = 0;
+    }
+    // Few threads have more than one or two: their values are read again, not picked from registers.
+    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap + before;
+    while (bits != 0) {
+      const int q = E - __ffs(bits);
+      bits &= bits - 1;
+      const int c = r.column(j0 + q / N * kHeadThreads + tid) + q % N;
+      *list++ = entry_key(r.raw(c), c);
+    }
+  }
+
+  HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0., 0.};
+  if (s.binned && valid > 0) {
+    const double k16 = 16. * s.c2;
+    const float range = float(992. / k16);   // 62 octaves
+    if (fabs(double(m)) * k16 < 1e9 && range < INFINITY) {
+      for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
+      __syncthreads();
+      const float end = m - range;
+      st.top_bin = weight_bin(m, k16);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+        {
+          int n;   // of top_bin - 993 .. top_bin
+          const uint64_t w = weight_in_bin(fmaxf(x[g][e], end), k16, n);
+          if (x[g][e] >= end) atomicAdd(&mass[st.top_bin - n], static_cast<unsigned long long>(w));
+        }
+      __syncthreads();
+      uint32_t end_bin = 0;
+      for (int b = tid; b < kMassBins; b += kHeadThreads)
+        if (mass[b] != 0) end_bin = uint32_t(b) + 1;
+      end_bin = block_fold<kHeadWaves>(end_bin, red.i, [](uint32_t u, uint32_t v) { return u > v ? u : v; });
+      uint64_t* out = h.mass + (at * h.chunks + chunk) * kMassBins;
+      for (int b = tid; b < int(end_bin); b += kHeadThreads) out[b] = mass[b];
+      st.bins = int(end_bin);
+    } else {
+      st.bins = -1;
+    }
+  } else if (TOP && a.rest != nullptr && valid > listed) {
+    // The others of the top logits: 32-bit exponentials, as their logarithm is stored in 32 bits.
+    // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.  The
+    // reference is what the rounded product of lo and log2(e) / T stands for, so that an entry
+    // costs one product, rounded once.
+    const float c2 = fminf(float(s.c2), 3e38f);
+    for (int turn = 0; turn < 2; ++turn) {
+      float ref = lo;
+      if (turn == 1 || !(lo < INFINITY)) {
+        float g_top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e] < lo ? x[g][e] : -INFINITY);
+        ref = block_fold<kHeadWaves>(g_top, red.f, most);
+      }
+      const float k = fmaxf(fminf(ref * c2, 3e38f), -3e38f);
+      float f = 0.f;
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e) f += x[g][e] < lo ? __builtin_amdgcn_exp2f(fmaf(x[g][e], c2, -k)) : 0.f;
+      st.rest_ref = double(k) / double(c2);
+      st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
+      if (st.rest > 1e-25 || !(lo < INFINITY)) break;
+    }
+  }
+  if (tid == 0) h.stats[at * h.chunks + chunk] = st;
+}
+
+template <typename T>
+static hipError_t launch_head(bool top, bool small, const CutArgs& a, const HeadArgs& h, hipStream_t s) {
+  const dim3 grid(unsigned(a.rows) * h.chunks), wg(kHeadThreads);
+  if (top && small)
+    hipLaunchKernelGGL((row_head_kernel<T, 8, true>), grid, wg, 0, s, a, h);
+  else if (top)
+    hipLaunchKernelGGL((row_head_kernel<T, 32, true>), grid, wg, 0, s, a, h);
+  else if (small)
+    hipLaunchKernelGGL((row_head_kernel<T, 8, false>), grid, wg, 0, s, a, h);
+  else
+    hipLaunchKernelGGL((row_head_kernel<T, 32, false>), grid, wg, 0, s, a, h);
+  return hipGetLastError();
+}
+
+hipError_t launch_row_head(bool bf16, bool top, bool small, const CutArgs& a, const HeadArgs& h, hipStream_t s) {
+  return bf16 ? launch_head<bf16_t>(top, small, a, h, s) : launch_head<float>(top, small, a, h, s);
+}
+
+}  // namespace hdf

@@ -1,5 +1,5 @@
 // Rows of logits of either type, their order and their weights: shared by the truncated draws
-// and the distillation (trunc.hip, distill.hip).
+// and the distillation (row_cut.hip, verify.hip, distill.hip).
 #pragma once
 
 #include "common.hpp"

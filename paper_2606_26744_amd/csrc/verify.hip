@@ -1,0 +1,275 @@
+// Speculative verification between truncated distributions: draft x_i of a sequence is accepted if
+// u_i q_i(x_i) < p_i(x_i), p and q the truncated distributions of the target's and the drafter's
+// row; after n acceptances the next token is drawn from max(0, p_n - q_n) by its running sum in
+// column order (from p_n where that is zero throughout, or after K acceptances).  The target rows
+// are truncated first (row_cut.hip); the draw reads one row, or two, a sequence.
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace hdf {
+
+constexpr int kVerifyThreads = 256;    // one vector of a part each
+constexpr int kVerifyWaves = kVerifyThreads / kWave;
+
+// Probability of an entry under a row's truncation; lse2 = lse * log2(e).
+struct RowCut {
+  float logit;
+  int index;
+  double lse2;
+};
+__device__ __forceinline__ double cut_prob(const RowCut& k, float z, int c, bool greedy, double c2) {
+  if (!(z > k.logit || (z == k.logit && c <= k.index)) || z == -INFINITY) return 0.;
+  return greedy ? 1. : exp2_64(double(z) * c2 - k.lse2);
+}
+
+template <typename TD, typename TT>
+struct VerifyRows {
+  const VerifyArgs& a;
+  int s;
+  bool greedy;
+  double c2;
+  __device__ VerifyRows(const VerifyArgs& a_, int s_) : a(a_), s(s_) {
+    const float t = a.ts != nullptr ? a.ts[s] : a.t;
+    greedy = !(t > 0.f);
+    c2 = greedy ? 0. : 1.4426950408889634074 / double(t);
+  }
+  __device__ const TT* target(int i) const {
+    return static_cast<const TT*>(a.tz) + (int64_t(s) * (a.K + 1) + i) * a.V;
+  }
+  __device__ const TD* draft(int i) const {
+    return static_cast<const TD*>(a.dz) + (int64_t(s) * a.stride + i) * a.ld;
+  }
+  __device__ RowCut target_cut(int i) const {
+    const int64_t r = int64_t(s) * (a.K + 1) + i;
+    return {a.t_logit[r], a.t_index[r], a.t_lse[r] * 1.4426950408889634074};
+  }
+  __device__ RowCut draft_cut(int i) const {
+    const int64_t r = int64_t(s) * a.stride + i;
+    return {a.d_logit[r], a.d_index[r], a.d_lse[r] * 1.4426950408889634074};
+  }
+  // Weights of the next token's draw in vector j of target row n: the residual w and the target's
+  // own p.
+  __device__ void weights(int n, int j, double w[LogitRow<TT>::N], double p[LogitRow<TT>::N]) const {
+    constexpr int N = LogitRow<TT>::N;
+    const LogitRow<TT> t(target(n), a.V);
+    const LogitRow<TD> d(n < a.K ? draft(n) : nullptr, a.V);
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = p[e] = 0.;
+    if (j >= t.vectors()) return;
+    t.load(j, x);
+    const RowCut tc = target_cut(n), dc = n < a.K ? draft_cut(n) : tc;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int c = t.column(j) + e;
+      p[e] = cut_prob(tc, x[e], c, greedy, c2);
+      w[e] = p[e];
+      if (n < a.K && p[e] > 0.) w[e] = fmax(p[e] - cut_prob(dc, d.at(c), c, greedy, c2), 0.);
+    }
+  }
+};
+
+// Workgroup (part, sequence): the sequence's decisions (each workgroup makes them for itself: a
+// launch between would cost more than the few dependent loads), then the sums of both weights over
+// 256 vectors of row n.
+template <typename TD, typename TT>
+__global__ void __launch_bounds__(kVerifyThreads)
+verify_sum_kernel(VerifyArgs a) {
+  __shared__ int decided;
+  __shared__ double sh[kVerifyWaves];
+  const int s = blockIdx.y, part = blockIdx.x;
+  const VerifyRows<TD, TT> v(a, s);
+  if (threadIdx.x < 64) {
+    int n = a.K;
+    for (int c0 = 0; c0 < a.K; c0 += 64) {
+      const int i = c0 + int(threadIdx.x);
+      bool reject = false;
+      if (i < a.K) {
+        const int x = a.draft[int64_t(s) * a.stride + i];
+        double p = 0., q = 0.;
+        if (x >= 0 && x < a.V) {
+          p = cut_prob(v.target_cut(i), LogitRow<TT>(v.target(i), a.V).at(x), x, v.greedy, v.c2);
+          q = cut_prob(v.draft_cut(i), LogitRow<TD>(v.draft(i), a.V).at(x), x, v.greedy, v.c2);
+        }
+        reject = !(double(a.u[int64_t(s) * (a.K + 1) + i]) * q < p);
+      }
+      const unsigned long long miss = __ballot(reject);
+      if (miss != 0ull) {
+        n = c0 + __ffsll(static_cast<long long>(miss)) - 1;
+        break;
+      }
+    }
+    if (threadIdx.x == 0) {
+      decided = n;
+      if (part == 0) a.n_buf[s] = n;
+    }
+  }
+  __syncthreads();
+  double w[LogitRow<TT>::N], p[LogitRow<TT>::N], sw = 0., sp = 0.;
+  v.weights(decided, part * kVerifyThreads + int(threadIdx.x), w, p);
+#pragma unroll
+  for (int e = 0; e < LogitRow<TT>::N; ++e) {
+    sw += w[e];
+    sp += p[e];
+  }
+  auto add = [](double x, double y) { return x + y; };
+  sw = block_fold<kVerifyWaves>(sw, sh, add);
+  sp = block_fold<kVerifyWaves>(sp, sh, add);
+  if (threadIdx.x == 0) {
+    double* o = a.sums + (int64_t(s) * gridDim.x + part) * 2;
+    o[0] = sw;
+    o[1] = sp;
+  }
+}
+
+// One workgroup a sequence: the part in which the running sum passes u times the whole, the entry
+// within it, and the sequence's commits behind those of the sequences before it.
+template <typename TD, typename TT>
+__global__ void __launch_bounds__(kVerifyThreads)
+verify_pick_kernel(VerifyArgs a, int parts) {
+  __shared__ double sh[kVerifyWaves];
+  __shared__ int shi[kVerifyWaves];
+  __shared__ double base;
+  __shared__ int pick, last, token;
+  const int s = blockIdx.x, tid = threadIdx.x;
+  const VerifyRows<TD, TT> v(a, s);
+  const int n = a.n_buf[s];
+  const double* sums = a.sums + int64_t(s) * parts * 2;
+  auto add = [](auto x, auto y) { return x + y; };
+  double sw = 0., sp = 0.;
+  for (int i = tid; i < parts; i += kVerifyThreads) {
+    sw += sums[2 * i];
+    sp += sums[2 * i + 1];
+  }
+  sw = block_fold<kVerifyWaves>(sw, sh, add);
+  sp = block_fold<kVerifyWaves>(sp, sh, add);
+  const int which = sw > 0. ? 0 : 1;
+  const double target = fmin(fmax(double(a.u[int64_t(s) * (a.K + 1) + a.K]), 0.), 1.) *
+                        (which == 0 ? sw : sp);
+  if (tid == 0) pick = parts, last = 0, token = -1, base = 0.;
+  __syncthreads();
+  double before = 0.;   // of the parts ahead of this round's
+  for (int b = 0; b < parts; b += kVerifyThreads) {
+    const int i = b + tid;
+    const double mine = i < parts ? sums[2 * i + which] : 0.;
+    double all;
+    const double run = before + block_scan<kVerifyWaves>(mine, sh, all);
+    if (mine > 0.) {
+      if (run > target) atomicMin(&pick, i);
+      atomicMax(&last, i);
+    }
+    __syncthreads();
+    const bool found = pick < parts;
+    if (found || b + kVerifyThreads >= parts) {
+      if (i == (found ? pick : last)) base = run - mine;
+    }
+    before += all;
+    __syncthreads();
+    if (found) break;
+  }
+  const int part = pick < parts ? pick : last;
+  // `last` may lie in an earlier round than the final one: its base is then not the one stored.
+  // The draw below takes the part's last entry in that case, whatever the base.
+  const bool tail = pick >= parts;
+  __syncthreads();
+  if (tid == 0) pick = kVerifyThreads, last = -1;
+  __syncthreads();
+  double w[LogitRow<TT>::N], p[LogitRow<TT>::N], mine = 0., all;
+  const int j = part * kVerifyThreads + tid;
+  v.weights(n, j, w, p);
+  const int c = LogitRow<TT>(v.target(n), a.V).column(j);
+#pragma unroll
+  for (int e = 0; e < LogitRow<TT>::N; ++e) {
+    w[e] = which == 0 ? w[e] : p[e];
+    mine += w[e];
+    if (w[e] > 0.) atomicMax(&last, c + e);
+  }
+  const double upto = base + block_scan<kVerifyWaves>(mine, sh, all);
+  if (!tail && mine > 0. && upto > target) atomicMin(&pick, tid);
+  __syncthreads();
+  if (pick < kVerifyThreads) {
+    if (tid == pick) {
+      double sum = upto - mine;
+      int tok = -1;
+#pragma unroll
+      for (int e = 0; e < LogitRow<TT>::N; ++e) {
+        sum += w[e];
+        if (w[e] > 0. && (tok < 0 || sum - w[e] <= target)) tok = c + e;
+      }
+      token = tok;
+    }
+  } else if (tid == 0) {
+    token = last;
+  }
+  int ahead = 0;
+  if (a.offs != nullptr || a.toks != nullptr) {
+    for (int i = tid; i < s; i += kVerifyThreads) ahead += a.n_buf[i] + 1;
+    ahead = block_fold<kVerifyWaves>(ahead, shi, add);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a.acc[s] = n;
+    a.anchor[s] = token;
+    if (a.offs != nullptr) {
+      a.offs[s] = ahead;
+      if (s == int(gridDim.x) - 1) a.offs[s + 1] = ahead + n + 1;
+    }
+  }
+  if (a.toks != nullptr)
+    for (int i = tid; i <= n; i += kVerifyThreads)
+      a.toks[ahead + i] = i < n ? a.draft[int64_t(s) * a.stride + i] : token;
+}
+
+static size_t al256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Parts of a target row: 256 vectors each, of its least vectors and one for a row that starts
+// inside one.
+static int verify_parts(bool bf16, int V) {
+  const int N = bf16 ? 8 : 4;
+  return ((V + 2 * N - 2) / N + kVerifyThreads - 1) / kVerifyThreads;
+}
+
+size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V) {
+  const size_t rows = size_t(n_seq) * (K + 1);
+  return cut_ws_bytes(bf16, int64_t(rows), V, false) + al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
+         al256(size_t(n_seq) * verify_parts(bf16, V) * 16);
+}
+
+template <typename TD, typename TT>
+static hipError_t launch_verify(const VerifyArgs& a, int n_seq, int parts, hipStream_t s) {
+  hipLaunchKernelGGL((verify_sum_kernel<TD, TT>), dim3(parts, n_seq), dim3(kVerifyThreads), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((verify_pick_kernel<TD, TT>), dim3(n_seq), dim3(kVerifyThreads), 0, s, a, parts);
+  return hipGetLastError();
+}
+
+hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs a, CutArgs c,
+                                   int n_seq, void* ws, hipStream_t s) {
+  const size_t rows = size_t(n_seq) * (a.K + 1);
+  char* p = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) {
+    char* q = p;
+    p += al256(bytes);
+    return q;
+  };
+  c.lse = reinterpret_cast<double*>(take(rows * 8));
+  c.cut_logit = reinterpret_cast<float*>(take(rows * 4));
+  c.cut_index = reinterpret_cast<int32_t*>(take(rows * 4));
+  c.kept = reinterpret_cast<int32_t*>(take(rows * 4));
+  a.n_buf = reinterpret_cast<int32_t*>(take(size_t(n_seq) * 4));
+  const int parts = verify_parts(target_bf16, a.V);
+  a.sums = reinterpret_cast<double*>(take(size_t(n_seq) * parts * 16));
+  a.t_logit = c.cut_logit;
+  a.t_index = c.cut_index;
+  a.t_lse = c.lse;
+  const hipError_t e = launch_truncate(target_bf16, c, take(cut_ws_bytes(target_bf16, int64_t(rows), a.V, false)), s);
+  if (e != hipSuccess) return e;
+  if (draft_bf16)
+    return target_bf16 ? launch_verify<bf16_t, bf16_t>(a, n_seq, parts, s)
+                       : launch_verify<bf16_t, float>(a, n_seq, parts, s);
+  return target_bf16 ? launch_verify<float, bf16_t>(a, n_seq, parts, s)
+                     : launch_verify<float, float>(a, n_seq, parts, s);
+}
+
+}  // namespace hdf
