@@ -194,8 +194,8 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
         sh.pick = b0 + h;
         sh.before = before;
       }
-      if (sh.count[b0 + h] != 0) atomicMax(&sh.last, b0 + h);
     }
+    note_last((sh.count[b0] | sh.count[b0 + 1]) != 0, sh.count[b0 + 1] != 0 ? b0 + 1 : b0, &sh.last);
     __syncthreads();
     if (sh.pick < 0 && int(threadIdx.x) == sh.last / 2) {
       sh.before = (sh.last & 1) ? at1 - v1 : at1 - v1 - v0;
@@ -222,8 +222,8 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
         const double w1 = i + 1 < n ? entry_weight(entry_logit(sh.list[i + 1]), m, c2) : 0.;
         double all;
         const double sum = block_scan<kCutWaves>(w0 + w1, sh.red.d, all);
-        if (i < n && above + (sum - w1) >= target) atomicMin(&sh.pick, i);
-        if (i + 1 < n && above + sum >= target) atomicMin(&sh.pick, i + 1);
+        const bool is0 = i < n && above + (sum - w1) >= target;
+        note_first(is0 || (i + 1 < n && above + sum >= target), is0 ? i : i + 1, &sh.pick);
         __syncthreads();
         at = min(sh.pick, n - 1);
       } else {
@@ -297,10 +297,8 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
                                           double mine, CutShared<NT, S>& sh) {
   if (threadIdx.x == 0) sh.pick = NT, sh.last = 0;
   __syncthreads();
-  if (mine > 0.) {
-    if (base + run > target) atomicMin(&sh.pick, int(threadIdx.x));
-    atomicMax(&sh.last, int(threadIdx.x));
-  }
+  note_first(mine > 0. && base + run > target, threadIdx.x, &sh.pick);
+  note_last(mine > 0., threadIdx.x, &sh.last);
   __syncthreads();
   const int g = min(sh.pick, sh.last);
   __syncthreads();
@@ -316,15 +314,17 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = -INFINITY;
   if (j < j1) r.load(j, x);
+  int end = -1;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     const bool is = x[e] > -INFINITY && (cut == 0 || x[e] > cz || (x[e] == cz && c + e <= cc));
     w[e] = entry_weight(is ? x[e] : -INFINITY, m, c2);
     own += w[e];
-    if (is) atomicMax(&sh.last, c + e);
+    end = is ? c + e : end;
   }
+  note_last(end >= 0, end, &sh.last);
   const double upto = sh.sum + block_scan<NT / kWave>(own, sh.red.d, all);
-  if (own > 0. && upto > target) atomicMin(&sh.pick, int(threadIdx.x));
+  note_first(own > 0. && upto > target, threadIdx.x, &sh.pick);
   __syncthreads();
   const int who = sh.pick;
   __syncthreads();
@@ -360,8 +360,8 @@ __device__ __forceinline__ int reach(int n, int n_sum, double from, double targe
       const double v = i < m ? w(i) : 0.;
       double all;
       const double run = before + block_scan<NT / kWave>(v, sh.red.d, all);
-      if (pass == 1 && i < m && (STRICT ? v > 0. && run > target : run >= target))
-        atomicMin(&sh.pick, i);
+      if (pass == 1)
+        note_first(i < m && (STRICT ? v > 0. && run > target : run >= target), i, &sh.pick);
       before += all;
     }
     __syncthreads();
@@ -375,10 +375,12 @@ __device__ __forceinline__ int reach(int n, int n_sum, double from, double targe
   return at;
 }
 
-// A row's share of the second launch's work.  With few rows one launch of large workgroups does all
-// of it; with many the lists are handled by small ones, several to a CU, and two more launches take
-// what those leave: the rows that need one more pass, and those that need the search.
-enum CutPhase { kAll, kLists, kBorder, kSearch };
+// The second launch's work in phases, a launch each.  The lists are handled by small workgroups: a
+// large one's waves take turns at the same few instructions (1024 threads took 16 us for a row with
+// top_k that 256 take X us for).  What those leave, the rows that need one more pass and those that
+// need the search, large ones take after, in one launch, or with many rows in two, of which the
+// first needs fewer registers.
+enum CutPhase { kLists, kRest, kBorder, kSearch };
 enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
 
 // The chunks' statistics joined, by the first wave.
@@ -461,7 +463,7 @@ __device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float 
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
 row_top_kernel(CutArgs a, HeadArgs h) {
-  constexpr bool LISTS = PHASE != kSearch, SEARCH = PHASE != kLists;
+  constexpr bool LISTS = PHASE == kLists, SEARCH = !LISTS;
   constexpr int W = NT / kWave;
   __shared__ CutShared<NT, SEARCH> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
@@ -489,7 +491,7 @@ row_top_kernel(CutArgs a, HeadArgs h) {
       t = floor;
     }
     done = have >= n;
-    if (PHASE == kLists && tid == 0) h.notes[at].left = done ? kDone : kLeftSearch;
+    if (tid == 0) h.notes[at].left = done ? kDone : kLeftSearch;
     if (done) {
       sort_list<NT>(sh.list, have);
       if (a.rest != nullptr) {
@@ -509,12 +511,12 @@ row_top_kernel(CutArgs a, HeadArgs h) {
         sum = block_fold<W>(sum, sh.red.d, add);
         if (tid == 0) a.rest[row] = sum > 0. ? float(ref * s.inv_t + log(sum)) : -INFINITY;
       }
-    } else if (PHASE == kLists) {
+    } else {
       return;
     }
   }
   if constexpr (SEARCH) {
-    if (!done) {
+    {
       const uint64_t cut = valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, entry_logit(sh.best),
                                                                      s.c2, float(64. * s.inv_t), sh)
                                                : 0;
@@ -555,8 +557,8 @@ row_top_kernel(CutArgs a, HeadArgs h) {
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
 row_cut_kernel(CutArgs a, HeadArgs h) {
-  constexpr bool LISTS = PHASE == kAll || PHASE == kLists, BORDER = PHASE == kAll || PHASE == kBorder,
-                 SEARCH = PHASE == kAll || PHASE == kSearch;
+  constexpr bool LISTS = PHASE == kLists, BORDER = PHASE == kRest || PHASE == kBorder,
+                 SEARCH = PHASE == kRest || PHASE == kSearch;
   constexpr int W = NT / kWave, PER = kMassBins / NT, LISTED = kListMax / NT;
   // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
   // whose masses the histograms hold, one chunk is read instead.
@@ -567,6 +569,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   CutNote* note = h.notes + at;
   if (PHASE == kBorder && note->left != kLeftBorder) return;
   if (PHASE == kSearch && note->left != kLeftSearch) return;
+  if (PHASE == kRest && note->left == kDone) return;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const RowSettings s = settings_of<false>(a, row);
   auto add = [](auto u, auto v) { return u + v; };
@@ -661,14 +664,15 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       __syncthreads();
       const double target = has_p ? fmax(double(s.top_p) * whole_w, 1e-300) : INFINITY;
       double upto = run - sum;
+      int first = -1, last = -1;
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         upto += v[e];
-        if (v[e] > 0.) {
-          if (upto >= target) atomicMin(&sh.pick, PER * tid + e);
-          atomicMax(&sh.last, PER * tid + e);
-        }
+        last = v[e] > 0. ? PER * tid + e : last;
+        first = first < 0 && v[e] > 0. && upto >= target ? PER * tid + e : first;
       }
+      note_first(first >= 0, first, &sh.pick);
+      note_last(last >= 0, last, &sh.last);
       __syncthreads();
       border = min(sh.pick, sh.last);
       by_p = has_p;
@@ -703,7 +707,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   };
 
   uint64_t cut = 0;
-  if (binned || PHASE == kBorder || (LISTS && (has_k || whole))) {
+  if (LISTS ? binned || has_k || whole : BORDER && binned) {
     // The entries that the cut lies among, sorted; `greater` more lie above them.
     float end = 0.f, over = INFINITY;
     uint32_t greater = 0;
@@ -770,8 +774,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       } else {
         break;
       }
-      if (n == 0 || n > kListMax || (has_k && n < s.top_k)) break;
-      sort_list<NT>(sh.list, n);
+      if (n > kListMax || (has_k && n < s.top_k)) break;
+      if (n > 0) sort_list<NT>(sh.list, n);
       for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
       __syncthreads();
       int k = has_k ? s.top_k : n;
@@ -792,13 +796,14 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         greater += uint32_t(k);
         break;
       }
-      // min_p's cut lies above all of its bin's entries: the last bin before with any.
+      // min_p's cut lies above all of its bin's entries, if it has any: the last bin before that has.
       if (tid == 0) sh.last = 0;
       __syncthreads();
-      for (int b = tid; b < border; b += NT) {
+      for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
+        const int b = b0 + tid;
         double any = 0.;
-        for (int c = 0; c < h.chunks; ++c) any += mass_at(c, b);
-        if (any > 0.) atomicMax(&sh.last, b);
+        for (int c = 0; b < border && c < h.chunks; ++c) any += mass_at(c, b);
+        note_last(any > 0., b, &sh.last);
       }
       __syncthreads();
       border = sh.last;
@@ -841,8 +846,10 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           if (i == k) {   // the last with a weight
             if (tid == 0) sh.last = 0;
             __syncthreads();
-            for (int q = tid; q < k; q += NT)
-              if (sh.weight[sh.list[q] & 4095u] > 0.) atomicMax(&sh.last, q);
+            for (int q0 = 0; q0 < k; q0 += NT) {
+              const int q = q0 + tid;
+              note_last(q < k && sh.weight[sh.list[q < k ? q : 0] & 4095u] > 0., q, &sh.last);
+            }
             __syncthreads();
             i = sh.last;
           }
@@ -862,7 +869,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll 1
         for (int c = wid; c < h.chunks; c += W) {
           double w = 0.;
-#pragma unroll 2
           for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
 #pragma unroll 1
           for (int i = lane; i < n; i += 64) {
@@ -883,10 +889,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           const double target = u * mass;
           if (tid == 0) sh.pick = NT, sh.last = 0;
           __syncthreads();
-          if (w > 0.) {
-            if (run > target) atomicMin(&sh.pick, tid);
-            atomicMax(&sh.last, tid);
-          }
+          note_first(w > 0. && run > target, tid, &sh.pick);
+          note_last(w > 0., tid, &sh.last);
           __syncthreads();
           const int c = min(sh.pick, sh.last);
           __syncthreads();
@@ -967,8 +971,8 @@ static int64_t cut_rows(bool bf16, int64_t rows, int V) {
   const int64_t most = kCutChunks / head_plan(bf16, kCutChunks, V).chunks;
   return rows < most ? rows : most;
 }
-// Above this many rows (a workgroup a CU) the second launch's phases run apart.
-constexpr int64_t kCombinedRows = 256;
+// Above this many rows (a large workgroup a CU) the rest is two launches.
+constexpr int64_t kRestRows = 256;
 constexpr int kListThreads = 256, kBorderThreads = 512;
 
 size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
@@ -1009,27 +1013,22 @@ static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
     h.mass = reinterpret_cast<uint64_t*>(p);
     hipError_t e = launch_row_head(bf16, TOP, pl.elems == 8, a, h, s);
     if (e != hipSuccess) return e;
-    const dim3 rows(unsigned(a.rows)), one(kCutThreads);
-    const bool apart = a.rows > kCombinedRows;
+    const dim3 rows(unsigned(a.rows)), lists(kListThreads), large(kCutThreads);
+    if constexpr (TOP)
+      hipLaunchKernelGGL((row_top_kernel<T, kListThreads, kLists>), rows, lists, 0, s, a, h);
+    else
+      hipLaunchKernelGGL((row_cut_kernel<T, kListThreads, kLists>), rows, lists, 0, s, a, h);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if constexpr (TOP) {
-      if (apart) {
-        hipLaunchKernelGGL((row_top_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kSearch>), rows, one, 0, s, a, h);
-      } else {
-        hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kAll>), rows, one, 0, s, a, h);
-      }
-    } else if (apart) {
-      hipLaunchKernelGGL((row_cut_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kSearch>), rows, large, 0, s, a, h);
+    } else if (a.rows <= kRestRows) {
+      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kRest>), rows, large, 0, s, a, h);
+    } else {
       hipLaunchKernelGGL((row_cut_kernel<T, kBorderThreads, kBorder>), rows, dim3(kBorderThreads), 0, s, a, h);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kSearch>), rows, one, 0, s, a, h);
-    } else {
-      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kAll>), rows, one, 0, s, a, h);
+      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kSearch>), rows, large, 0, s, a, h);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -161,6 +161,22 @@ __device__ __forceinline__ X wave_scan(X v) {
   return v;
 }
 
+// Least (greatest) i of the lanes for which c holds into *dst, one atomic a wave; i rises with the
+// lane.  (A wave's 64 atomics of different values to one word are done one by one: 45 thousand cycles
+// for the eight entries a thread of a draw.)
+__device__ __forceinline__ void note_first(bool c, int i, int* dst) {
+  const unsigned long long m = __ballot(c);
+  if (m == 0ull) return;
+  const int v = read_lane(i, __ffsll(static_cast<long long>(m)) - 1);
+  if ((threadIdx.x & 63) == 0) atomicMin(dst, v);
+}
+__device__ __forceinline__ void note_last(bool c, int i, int* dst) {
+  const unsigned long long m = __ballot(c);
+  if (m == 0ull) return;
+  const int v = read_lane(i, 63 - __clzll(static_cast<long long>(m)));
+  if ((threadIdx.x & 63) == 0) atomicMax(dst, v);
+}
+
 // f over a workgroup of W waves in a fixed order; every thread gets the result.  `sh` holds W values
 // and is free again on return.
 template <int W, typename X, typename F>

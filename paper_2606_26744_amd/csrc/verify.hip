@@ -154,10 +154,8 @@ verify_pick_kernel(VerifyArgs a, int parts) {
     const double mine = i < parts ? sums[2 * i + which] : 0.;
     double all;
     const double run = before + block_scan<kVerifyWaves>(mine, sh, all);
-    if (mine > 0.) {
-      if (run > target) atomicMin(&pick, i);
-      atomicMax(&last, i);
-    }
+    note_first(mine > 0. && run > target, i, &pick);
+    note_last(mine > 0., i, &last);
     __syncthreads();
     const bool found = pick < parts;
     if (found || b + kVerifyThreads >= parts) {
@@ -178,14 +176,16 @@ verify_pick_kernel(VerifyArgs a, int parts) {
   const int j = part * kVerifyThreads + tid;
   v.weights(n, j, w, p);
   const int c = LogitRow<TT>(v.target(n), a.V).column(j);
+  int end = -1;
 #pragma unroll
   for (int e = 0; e < LogitRow<TT>::N; ++e) {
     w[e] = which == 0 ? w[e] : p[e];
     mine += w[e];
-    if (w[e] > 0.) atomicMax(&last, c + e);
+    end = w[e] > 0. ? c + e : end;
   }
+  note_last(end >= 0, end, &last);
   const double upto = base + block_scan<kVerifyWaves>(mine, sh, all);
-  if (!tail && mine > 0. && upto > target) atomicMin(&pick, tid);
+  note_first(!tail && mine > 0. && upto > target, tid, &pick);
   __syncthreads();
   if (pick < kVerifyThreads) {
     if (tid == pick) {
