@@ -84,26 +84,33 @@ __device__ __forceinline__ RowSettings settings_of(const CutArgs& a, int64_t row
   return s;
 }
 
-// Bin of a value and the weight within it (a multiple of 2^-48 in the low bits).  The magic
-// constants round to an integer in the low bits of the sum; the series is that of 2^(g / 16),
-// |g| <= 1/2, whose first dropped term is 0.022^7 / 7! = 4e-16.
+// Bin of a value: the magic constant, 1.5 * 2^52, rounds to an integer in the low bits of the sum.
+constexpr double kRound = 6755399441055744.;
 __device__ __forceinline__ int weight_bin(float z, double k16) {
-  const double t = fma(double(z), k16, 6755399441055744.);   // 1.5 * 2^52
-  return int(uint32_t(__builtin_bit_cast(uint64_t, t)));
+  return int(uint32_t(__builtin_bit_cast(uint64_t, fma_k(double(z), k16, kRound))));
 }
-__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, int& n) {
-  const double t = fma(double(z), k16, 6755399441055744.);
+// Bin and the weight within it as a multiple of 2^-48: the series of 2^(g / 16), |g| <= 1/2, whose
+// first dropped term is 0.022^7 / 7! = 4e-16, with all coefficients times 2^(48 - 1074), so that the
+// result is subnormal and its bits are the integer.  c6: mass_coefficient(), kept in registers by
+// the caller.
+constexpr double kLog16 = 0.69314718055994530942 / 16.;
+constexpr double kBits = 0x1p-1026;
+__device__ __forceinline__ double mass_coefficient() {
+  double c = kLog16 * kLog16 * kLog16 * kLog16 * kLog16 * kLog16 / 720. * kBits;
+  asm volatile("" : "+v"(c));   // not copied anew for every entry
+  return c;
+}
+__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, double c6, int& n) {
+  const double t = fma_k(double(z), k16, kRound);
   n = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
-  const double g = fma(double(z), k16, -(t - 6755399441055744.));
-  constexpr double c = 0.69314718055994530942 / 16.;
-  double p = c * c * c * c * c * c / 720.;
-  p = fma_k(p, g, c * c * c * c * c / 120.);
-  p = fma_k(p, g, c * c * c * c / 24.);
-  p = fma_k(p, g, c * c * c / 6.);
-  p = fma_k(p, g, c * c / 2.);
-  p = fma_k(p, g, c);
-  p = fma_k(p, g, 17.);   // 16 + 1: a unit of 16's last place is 2^-48
-  return __builtin_bit_cast(uint64_t, p) - 0x4030000000000000ull;
+  const double g = fma(double(z), k16, kRound - t);
+  double p = fma_k(c6, g, kLog16 * kLog16 * kLog16 * kLog16 * kLog16 / 120. * kBits);
+  p = fma_k(p, g, kLog16 * kLog16 * kLog16 * kLog16 / 24. * kBits);
+  p = fma_k(p, g, kLog16 * kLog16 * kLog16 / 6. * kBits);
+  p = fma_k(p, g, kLog16 * kLog16 / 2. * kBits);
+  p = fma_k(p, g, kLog16 * kBits);
+  p = fma_k(p, g, kBits);
+  return __builtin_bit_cast(uint64_t, p);
 }
 
 hipError_t launch_row_head(bool bf16, bool top, bool small, const CutArgs& a, const HeadArgs& h, hipStream_t s);

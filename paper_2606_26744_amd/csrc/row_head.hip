@@ -5,10 +5,16 @@ namespace hdf {
 
 constexpr int kHeadWaves = kHeadThreads / kWave;
 
-// The greatest of three values, none of them NaN.
+// The greatest of three or two values, none of them NaN.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+__device__ __forceinline__ float max2(float a, float b) {
+  float d;
+  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
   return d;
 }
 
@@ -148,19 +154,23 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   if (s.binned && valid > 0) {
     const double k16 = 16. * s.c2;
     const float range = float(992. / k16);   // 62 octaves
-    if (fabs(double(m)) * k16 < 1e9 && range < INFINITY) {
+    if (fabs(double(m)) * k16 < 8e6 && range < INFINITY) {   // bins of 24 bits
       for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
       __syncthreads();
       const float end = m - range;
-      st.top_bin = weight_bin(m, k16);
+      const double c6 = mass_coefficient();
+      const int top_bin = weight_bin(m, k16);
+      st.top_bin = top_bin;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < N; ++e)
         {
           int n;   // of top_bin - 993 .. top_bin
-          const uint64_t w = weight_in_bin(fmaxf(x[g][e], end), k16, n);
-          if (x[g][e] >= end) atomicAdd(&mass[st.top_bin - n], static_cast<unsigned long long>(w));
+          const uint64_t w = weight_in_bin(max2(x[g][e], end), k16, c6, n);
+          auto* bin = reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(mass) +
+                                                            __mul24(top_bin - n, 8));
+          if (x[g][e] >= end) atomicAdd(bin, static_cast<unsigned long long>(w));
         }
       __syncthreads();
       uint32_t end_bin = 0;

@@ -184,9 +184,19 @@ __device__ __forceinline__ X block_fold(X v, X* sh, F f) {
   v = wave_fold(v, f);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  X t = sh[0];
+  X t;
+  if constexpr (W == 4 || W == 8 || W == 16) {   // a lane a wave, and as within rows of 16
+    t = sh[threadIdx.x & (W - 1)];
+    t = f(t, dpp<0xB1, 0xf>(t));
+    t = f(t, dpp<0x4E, 0xf>(t));
+    if constexpr (W > 4) t = f(t, dpp<0x141, 0xf>(t));
+    if constexpr (W > 8) t = f(t, dpp<0x140, 0xf>(t));
+    t = read_lane(t, 0);   // one order of the sum for all
+  } else {
+    t = sh[0];
 #pragma unroll
-  for (int w = 1; w < W; ++w) t = f(t, sh[w]);
+    for (int w = 1; w < W; ++w) t = f(t, sh[w]);
+  }
   __syncthreads();
   return t;
 }
