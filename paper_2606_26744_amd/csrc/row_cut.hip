@@ -13,10 +13,17 @@ constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
 constexpr double kSearchUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 
-template <int NT, bool SEARCH>
+// Entries of a border bin that are held at once.
+constexpr int kBorderMax = 4096;
+
+template <int NT, bool SEARCH, bool BORDER>
 struct CutShared {
   static constexpr int W = NT / kWave;
   union {
+    struct {
+      uint64_t border[BORDER ? kBorderMax : 1];
+      unsigned long long fine[BORDER ? NT : 1];
+    };
     struct {
       uint64_t list[kListMax];
       union {
@@ -29,7 +36,10 @@ struct CutShared {
     };
     double group[W][kMaxGroups];
   };
-  double chunk[kMaxChunks];
+  union {
+    double chunk[kMaxChunks];
+    unsigned long long chunk_n[kMaxChunks];
+  };
   struct {
     int listed, top_bin, bins;
     double rest_ref, rest;
@@ -42,7 +52,7 @@ struct CutShared {
   } red;
   uint64_t before, best;
   double sum;
-  float floor, near;
+  float floor, near, edge[2];
   uint32_t n, valid, listed;
   int pick, last, top_bin, bins;
 };
@@ -150,9 +160,9 @@ __device__ __forceinline__ int value_bin(float z, float m, float scale) {
 // Histograms of 2048 bins over ever smaller ranges of the order, until a bin's entries fit the
 // list: the first by value, further ones by key, where the last range is one key.  A caller that
 // knows the range of keys and the sum `above` it starts there (lo > 0).
-template <bool BY_MASS, typename T>
+template <bool BY_MASS, typename T, typename Shared>
 __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t floor, float m,
-                                 double c2, float scale, CutShared<kCutThreads, true>& sh, uint64_t lo = 0,
+                                 double c2, float scale, Shared& sh, uint64_t lo = 0,
                                  uint64_t hi = kKeyTop, double above = 0.) {
   auto shift_of = [&]() {
     int sh_ = 0;
@@ -254,9 +264,9 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
 // The weights of a row's kept entries (those before or at `cut` in the order) among vectors
 // j0 .. j1-1, a sum a group and wave in sh.group; returns their whole, `run` this thread's group's
 // running sum and `mine` its own.  COUNT: also how many, and the last one's key, of this thread.
-template <int NT, bool COUNT, bool S, typename T>
+template <int NT, bool COUNT, typename Shared, typename T>
 __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int j1, uint64_t cut,
-                                              float m, double c2, CutShared<NT, S>& sh, double& run,
+                                              float m, double c2, Shared& sh, double& run,
                                               double& mine, uint32_t* kept = nullptr,
                                               uint64_t* low = nullptr) {
   double s = 0.;
@@ -291,10 +301,10 @@ __device__ __forceinline__ double kept_masses(const LogitRow<T>& r, int j0, int 
 // The draw among the kept entries of vectors j0 .. j1-1, after kept_masses: the group in which
 // `base` and the running sum pass the target, then the entry; the last one where rounding leaves
 // none.
-template <int NT, bool S, typename T>
+template <int NT, typename Shared, typename T>
 __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
                                           double c2, double base, double target, double run,
-                                          double mine, CutShared<NT, S>& sh) {
+                                          double mine, Shared& sh) {
   if (threadIdx.x == 0) sh.pick = NT, sh.last = 0;
   __syncthreads();
   note_first(mine > 0. && base + run > target, threadIdx.x, &sh.pick);
@@ -345,9 +355,9 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
 // First place, among 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes) `from` times the
 // sum of the first n_sum of them, or `target` where n_sum is 0; n where none does.  `sum` gets the
 // sum.
-template <int NT, bool STRICT, bool S, typename F>
+template <int NT, bool STRICT, typename Shared, typename F>
 __device__ __forceinline__ int reach(int n, int n_sum, double from, double target, double& sum,
-                                     CutShared<NT, S>& sh, F w) {
+                                     Shared& sh, F w) {
   int at = n;
 #pragma unroll 1
   for (int pass = n_sum > 0 ? 0 : 1; pass < 2; ++pass) {   // the sum, then the place
@@ -384,8 +394,8 @@ enum CutPhase { kLists, kRest, kBorder, kSearch };
 enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
 
 // The chunks' statistics joined, by the first wave.
-template <int NT, bool S>
-__device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, CutShared<NT, S>& sh) {
+template <typename Shared>
+__device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, Shared& sh) {
   auto add = [](uint32_t u, uint32_t v) { return u + v; };
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
@@ -428,8 +438,8 @@ __device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, CutS
 }
 
 // This thread's places of a row's lists, all in flight together; 0 past a chunk's list.
-template <int NT, bool S>
-__device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, const CutShared<NT, S>& sh,
+template <int NT, typename Shared>
+__device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, const Shared& sh,
                                             uint64_t mine[kListMax / NT]) {
   const uint64_t* list = h.list + at * h.chunks * h.cap;
 #pragma unroll
@@ -441,9 +451,9 @@ __device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, const
   }
 }
 // The listed entries of value >= t and < over into the list; how many.
-template <int NT, bool S>
+template <int NT, typename Shared>
 __device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float t, float over,
-                                      CutShared<NT, S>& sh) {
+                                      Shared& sh) {
   __syncthreads();
   if (threadIdx.x == 0) sh.n = 0;
   __syncthreads();
@@ -463,9 +473,9 @@ __device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float 
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
 row_top_kernel(CutArgs a, HeadArgs h) {
-  constexpr bool LISTS = PHASE == kLists, SEARCH = !LISTS;
+  constexpr bool LISTS = PHASE == kLists, SEARCH = !LISTS, BORDER = false;
   constexpr int W = NT / kWave;
-  __shared__ CutShared<NT, SEARCH> sh;
+  __shared__ CutShared<NT, SEARCH, BORDER> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, K = a.K;
   if (PHASE == kSearch && h.notes[at].left != kLeftSearch) return;
@@ -480,13 +490,13 @@ row_top_kernel(CutArgs a, HeadArgs h) {
   bool done = false;
   if constexpr (LISTS) {
     uint64_t mine[kListMax / NT];
-    load_listed(h, at, sh, mine);
+    load_listed<NT>(h, at, sh, mine);
     const float floor = sh.floor;
     // As far down as the chunks' shares go (every entry >= floor is listed), or to the floor.
     float t = fmaxf(floor, sh.near);
 #pragma unroll 1
     for (;;) {
-      have = gather(mine, t, INFINITY, sh);
+      have = gather<NT>(mine, t, INFINITY, sh);
       if (have >= n || t <= floor) break;
       t = floor;
     }
@@ -553,6 +563,108 @@ row_top_kernel(CutArgs a, HeadArgs h) {
   }
 }
 
+// The row's entries with end <= z < over, up to kBorderMax of them, in sh.border: how many there are.
+// greater: how many lie above.
+template <int NT, typename T, typename Shared>
+__device__ __forceinline__ int border_entries(const LogitRow<T>& r, float end, float over,
+                                              uint32_t& greater, Shared& sh) {
+  constexpr int N = LogitRow<T>::N, Q = 32 / N;
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  uint32_t up = 0;
+  const int nv = r.vectors();
+#pragma unroll 1
+  for (int b = 0; b < nv; b += Q * NT) {
+    float x[Q][N];
+    if (r.inside(b, Q * NT)) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) r.load_inside(b + q * NT + tid, x[q]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
+        if (b + q * NT + tid < nv) r.load_raw(b + q * NT + tid, x[q]);
+      }
+    }
+    uint32_t bits = 0;   // of the border bin, the first entry's bit the highest
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const bool is = x[q][e] >= over;
+        up += uint32_t(__popcll(__ballot(is)));
+        bits = 2 * bits + uint32_t(x[q][e] >= end && !is);
+      }
+    const uint32_t own = __popc(bits), upto = wave_scan(own);
+    uint32_t at = 0;
+    if (lane == 63) at = atomicAdd(&sh.n, upto);
+    at = read_lane(at, 63) + upto - own;
+    while (bits != 0) {
+      const int q = 32 - __ffs(bits);
+      bits &= bits - 1;
+      const int c = r.column(b + q / N * NT + tid) + q % N;
+      if (at < uint32_t(kBorderMax)) sh.border[at] = entry_key(r.raw(c), c);
+      ++at;
+    }
+  }
+  greater = block_fold<NT / kWave>(lane == 0 ? up : 0u, sh.red.i,
+                                   [](uint32_t u, uint32_t v) { return u + v; });
+  return int(sh.n);
+}
+
+// Key, among the n border entries, all of one bin, at which `above` and the running sum of their
+// weights in the order, times w_bin, reach the target; the last one if rounding leaves none.  Masses
+// over ever smaller ranges of keys; sorting the entries instead took three times as long.
+template <int NT, typename Shared>
+__device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi, double k16, double above,
+                                                 double w_bin, double target, Shared& sh) {
+  const int tid = threadIdx.x;
+  const double c5 = mass_coefficient();
+  uint64_t base = 0;
+#pragma unroll 1
+  while (lo < hi) {
+    int shift = 0;
+    while (((hi - lo) >> shift) >= uint64_t(NT)) ++shift;
+    sh.fine[tid] = 0;
+    if (tid == 0) sh.pick = NT, sh.last = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) {
+      const uint64_t k = sh.border[i];
+      int bin;
+      if (k >= lo && k <= hi)
+        atomicAdd(&sh.fine[(hi - k) >> shift],
+                  static_cast<unsigned long long>(weight_in_bin(entry_logit(k), k16, c5, bin)));
+    }
+    __syncthreads();
+    const uint64_t own = sh.fine[tid];
+    uint64_t all;
+    const uint64_t upto = base + block_scan<NT / kWave>(own, sh.red.u, all);
+    note_first(own > 0 && above + double(upto) * w_bin >= target, tid, &sh.pick);
+    note_last(own > 0, tid, &sh.last);
+    __syncthreads();
+    const int at = min(sh.pick, sh.last);
+    if (tid == at) sh.before = upto - own;
+    hi -= uint64_t(at) << shift;
+    const uint64_t least = hi - ((uint64_t(1) << shift) - 1);
+    lo = least > lo ? least : lo;
+    // The range that its entries take.
+    uint64_t first = 0, last = kKeyTop;
+    for (int i = tid; i < n; i += NT) {
+      const uint64_t k = sh.border[i];
+      const bool in = k >= lo && k <= hi;
+      first = in && k > first ? k : first;
+      last = in && k < last ? k : last;
+    }
+    hi = block_fold<NT / kWave>(first, sh.red.u, [](uint64_t u, uint64_t v) { return u > v ? u : v; });
+    lo = block_fold<NT / kWave>(last, sh.red.u, [](uint64_t u, uint64_t v) { return u < v ? u : v; });
+    base = sh.before;
+  }
+  __syncthreads();
+  return hi;
+}
+
 // A row's truncation and draw.
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
@@ -563,7 +675,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
   // whose masses the histograms hold, one chunk is read instead.
   constexpr int kInOrder = 512;
-  __shared__ CutShared<NT, SEARCH> sh;
+  __shared__ CutShared<NT, SEARCH, BORDER> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   CutNote* note = h.notes + at;
@@ -611,14 +723,16 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   };
 
   uint64_t mine[LISTED];
-  if constexpr (LISTS) load_listed(h, at, sh, mine);
+  if constexpr (LISTS) load_listed<NT>(h, at, sh, mine);
 
   // Least value of weight min_p, as the key of its last possible entry.
   uint64_t cut_m = 0;
-  if (has_m) {
+  if (has_m && (LISTS || !binned)) {
     const double least = fmin(double(s.min_p), 1.);
     const uint32_t k = least_value_key(m, [&](float z) { return entry_weight(z, m, s.c2) >= least; });
     cut_m = uint64_t(f32_order_key(f32_from_order_key(k) + 0.f)) << kColumnBits;
+  } else if (has_m) {
+    cut_m = note->cut_m;
   }
 
   // A cut by weight: the histograms joined.  The border bin is that of top_p's cut or of min_p's.
@@ -691,7 +805,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       above = sh.sum;
       __syncthreads();
       if (PHASE == kLists && tid == 0)
-        note->whole = whole_w, note->above = above, note->border = border, note->by_p = by_p;
+        note->whole = whole_w, note->above = above, note->border = border, note->by_p = by_p,
+        note->cut_m = cut_m;
     }
   } else if (binned) {
     whole_w = note->whole;
@@ -699,90 +814,62 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     border = note->border;
     by_p = note->by_p != 0;
   }
-  // Least value of bin b or a greater one.
-  auto bin_edge = [&](int b) {
-    return f32_from_order_key(least_value_key(m, [&](float z) {   // far values have no bin
-      return double(z) * k16 > double(top_bin) - 2048. && weight_bin(z, k16) >= top_bin - b;
-    }));
+  // The least values of the border bin and of the bin before: end <= z < over.
+  float end = 0.f, over = INFINITY;
+  auto find_edges = [&]() {
+    if (wid < 2) {
+      const int b = border - wid;
+      const float z = b < 0 ? INFINITY : f32_from_order_key(least_value_key(m, [&](float z) {
+        return double(z) * k16 > double(top_bin) - 2048. && weight_bin(z, k16) >= top_bin - b;
+      }));   // (far values have no bin)
+      if (lane == 0) sh.edge[wid] = z;
+    }
+    __syncthreads();
+    end = sh.edge[0];
+    over = sh.edge[1];
+    __syncthreads();
   };
+  // min_p's cut may lie above all of its bin's entries, if it has any: the last bin before that has.
+  auto bin_before = [&]() {
+    if (tid == 0) sh.last = 0;
+    __syncthreads();
+    for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
+      const int b = b0 + tid;
+      double any = 0.;
+      for (int c = 0; b < border && c < h.chunks; ++c) any += mass_at(c, b);
+      note_last(any > 0., b, &sh.last);
+    }
+    __syncthreads();
+    border = sh.last;
+    by_p = false;
+    __syncthreads();
+    find_edges();
+  };
+  const double target_p = fmax(double(s.top_p) * whole_w, 1e-300);   // 0 is reached by the first
 
   uint64_t cut = 0;
-  if (LISTS ? binned || has_k || whole : BORDER && binned) {
-    // The entries that the cut lies among, sorted; `greater` more lie above them.
-    float end = 0.f, over = INFINITY;
-    uint32_t greater = 0;
-    int n = 0;
-    bool from_lists = !binned;
+  if constexpr (LISTS) {
+    if (binned && !s.open) find_edges();
+    // The entries that the cut lies among, if they are listed, sorted.
+    bool from_lists = binned ? !s.open && end >= floor : has_k || whole;
 #pragma unroll 1
-    for (;;) {
-      if (binned && !s.open) {
-        end = bin_edge(border);
-        over = border > 0 ? bin_edge(border - 1) : INFINITY;
-        from_lists = LISTS && end >= floor;
-      } else if (binned) {
-        break;   // nothing is cut
+    while (from_lists && cut == 0) {
+      float t = binned ? end : has_k ? fmaxf(floor, sh.near) : floor;
+      int n;
+#pragma unroll 1
+      for (;;) {
+        n = gather<NT>(mine, t, over, sh);
+        if (!has_k || n >= s.top_k || t <= floor) break;
+        t = floor;
       }
-      if (LISTS && from_lists) {
-        float t = binned ? end : has_k ? fmaxf(floor, sh.near) : floor;
-#pragma unroll 1
-        for (;;) {
-          n = gather(mine, t, over, sh);
-          if (!has_k || n >= s.top_k || t <= floor) break;
-          t = floor;
-        }
-      } else if (BORDER && binned) {
-        __syncthreads();
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        greater = 0;
-        constexpr int N = LogitRow<T>::N, Q = 32 / N;
-        const int nv = r.vectors();
-#pragma unroll 1
-        for (int b = 0; b < nv; b += Q * NT) {
-          float x[Q][N];
-          if (r.inside(b, Q * NT)) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) r.load_inside(b + q * NT + tid, x[q]);
-          } else {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-#pragma unroll
-              for (int e = 0; e < N; ++e) x[q][e] = -INFINITY;
-              if (b + q * NT + tid < nv) r.load_raw(b + q * NT + tid, x[q]);
-            }
-          }
-          uint32_t bits = 0;   // of the border bin, the first entry's bit the highest
-#pragma unroll
-          for (int q = 0; q < Q; ++q)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              const bool up = x[q][e] >= over;
-              greater += uint32_t(__popcll(__ballot(up)));
-              bits = 2 * bits + uint32_t(x[q][e] >= end && !up);
-            }
-          while (bits != 0) {
-            const int q = 32 - __ffs(bits);
-            bits &= bits - 1;
-            const int c = r.column(b + q / N * NT + tid) + q % N;
-            const uint32_t i = atomicAdd(&sh.n, 1u);
-            if (i < uint32_t(kListMax)) sh.list[i] = entry_key(r.raw(c), c);
-          }
-        }
-        greater = block_fold<W>(lane == 0 ? greater : 0u, sh.red.i, add);
-        n = int(sh.n);
-        __syncthreads();
-      } else {
-        break;
-      }
-      if (n > kListMax || (has_k && n < s.top_k)) break;
+      if (has_k && n < s.top_k) break;
       if (n > 0) sort_list<NT>(sh.list, n);
       for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
       __syncthreads();
       int k = has_k ? s.top_k : n;
       if (binned ? by_p : has_p) {
         double sum;
-        const int p = reach<NT, false>(k, binned ? 0 : k, double(s.top_p),
-                                       fmax(double(s.top_p) * whole_w, 1e-300) - above, sum, sh,
+        const int p = reach<NT, false>(k, binned ? 0 : k, double(s.top_p), target_p - above, sum, sh,
                                        [&](int i) { return sh.weight[i]; });
         k = min(k, p + 1);
       }
@@ -791,91 +878,109 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         for (int i = tid; i < k; i += NT) c += sh.list[i] >= cut_m;
         k = int(block_fold<W>(c, sh.red.i, add));
       }
-      if (k > 0) {
+      if (k > 0)
         cut = sh.list[k - 1];
-        greater += uint32_t(k);
-        break;
-      }
-      // min_p's cut lies above all of its bin's entries, if it has any: the last bin before that has.
-      if (tid == 0) sh.last = 0;
-      __syncthreads();
-      for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
-        const int b = b0 + tid;
-        double any = 0.;
-        for (int c = 0; b < border && c < h.chunks; ++c) any += mass_at(c, b);
-        note_last(any > 0., b, &sh.last);
-      }
-      __syncthreads();
-      border = sh.last;
-      by_p = false;
-      __syncthreads();
+      else
+        bin_before();
     }
-
-    if constexpr (LISTS) {
-      if (from_lists && cut != 0) {
-        // All kept entries are listed: in token order, columns with their places as keys, the
-        // weights beside them.
-        uint32_t many = 0;
-        uint64_t low = kKeyTop;
+    if (cut != 0) {
+      // All kept entries are listed: in token order, columns with their places as keys, the weights
+      // beside them.
+      uint32_t many = 0;
+      uint64_t low = kKeyTop;
+#pragma unroll
+      for (int q = 0; q < LISTED; ++q)
+        if (mine[q] != 0 && mine[q] >= cut) {
+          low = least64(low, mine[q]);
+          ++many;
+        }
+      many = block_fold<W>(many, sh.red.i, add);
+      if (!binned || many <= uint32_t(kInOrder)) {
+        low = block_fold<W>(low, sh.red.u, least64);
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
 #pragma unroll
         for (int q = 0; q < LISTED; ++q)
           if (mine[q] != 0 && mine[q] >= cut) {
-            low = least64(low, mine[q]);
-            ++many;
+            const uint32_t i = atomicAdd(&sh.n, 1u);
+            sh.list[i] = ((mine[q] & kColumnMask) << 12) | uint64_t(i);
+            sh.weight[i] = double(entry_logit(mine[q]));
           }
-        many = block_fold<W>(many, sh.red.i, add);
-        greater = many;
-        if (!binned || many <= uint32_t(kInOrder)) {
-          low = block_fold<W>(low, sh.red.u, least64);
-          if (tid == 0) sh.n = 0;
+        __syncthreads();
+        const int k = int(many);
+        for (int i = tid; i < k; i += NT) sh.weight[i] = entry_weight(float(sh.weight[i]), m, s.c2);
+        sort_list<NT>(sh.list, k);
+        double mass;
+        int i = reach<NT, true>(k, k, u, 0., mass, sh,
+                                [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
+        if (i == k) {   // the last with a weight
+          if (tid == 0) sh.last = 0;
           __syncthreads();
-#pragma unroll
-          for (int q = 0; q < LISTED; ++q)
-            if (mine[q] != 0 && mine[q] >= cut) {
-              const uint32_t i = atomicAdd(&sh.n, 1u);
-              sh.list[i] = ((mine[q] & kColumnMask) << 12) | uint64_t(i);
-              sh.weight[i] = double(entry_logit(mine[q]));
-            }
-          __syncthreads();
-          const int k = int(many);
-          for (int i = tid; i < k; i += NT) sh.weight[i] = entry_weight(float(sh.weight[i]), m, s.c2);
-          sort_list<NT>(sh.list, k);
-          double mass;
-          int i = reach<NT, true>(k, k, u, 0., mass, sh,
-                                  [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
-          if (i == k) {   // the last with a weight
-            if (tid == 0) sh.last = 0;
-            __syncthreads();
-            for (int q0 = 0; q0 < k; q0 += NT) {
-              const int q = q0 + tid;
-              note_last(q < k && sh.weight[sh.list[q < k ? q : 0] & 4095u] > 0., q, &sh.last);
-            }
-            __syncthreads();
-            i = sh.last;
+          for (int q0 = 0; q0 < k; q0 += NT) {
+            const int q = q0 + tid;
+            note_last(q < k && sh.weight[sh.list[q < k ? q : 0] & 4095u] > 0., q, &sh.last);
           }
-          write(many, low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
-          return;
+          __syncthreads();
+          i = sh.last;
         }
-      }
-      if (PHASE == kLists) {
-        leave(binned ? kLeftBorder : kLeftSearch);
+        write(many, low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
         return;
       }
     }
-    if constexpr (BORDER) {
-      if (binned && (cut != 0 || s.open)) {
-        // The chunks' masses: their bins above the border, and their part of its entries.
-        if (s.open) border = kMassBins, greater = valid, n = 0;
+    if (tid == 0) {
+      note->border = border, note->by_p = by_p, note->end = end, note->over = over;
+      note->left = binned ? kLeftBorder : kLeftSearch;
+    }
+  }
+  if constexpr (BORDER) {
+    if (binned) {
+      uint32_t greater = valid;
+      int n = 0;
+      end = note->end;
+      over = note->over;
+      const bool fits = s.open || [&]() {
+        for (;;) {
+          n = border_entries<NT>(r, end, over, greater, sh);
+          if (n > kBorderMax) return false;
+          cut = cut_m;
+          if (by_p)
+            cut = most64(cut, border_entry<NT>(n, uint64_t(f32_order_key(end)) << kColumnBits,
+                                               uint64_t(f32_order_key(over)) << kColumnBits, k16, above,
+                                               bin_weight(border) * unit, target_p, sh));
+          uint64_t low = kKeyTop;
+          uint32_t kept = 0;
+          for (int i = tid; i < n; i += NT) {
+            const uint64_t k = sh.border[i];
+            kept += k >= cut;
+            low = k >= cut && k < low ? k : low;
+          }
+          kept = block_fold<W>(kept, sh.red.i, add);
+          cut = block_fold<W>(low, sh.red.u, least64);
+          greater += kept;
+          if (kept > 0) return true;
+          bin_before();
+        }
+      }();
+      if (fits) {
+        // The chunks' masses: their part of the border's entries, their bins above it.
+        if (s.open) border = kMassBins;
+        for (int c = tid; c < h.chunks; c += NT) sh.chunk_n[c] = 0;
+        __syncthreads();
+        const double c5 = mass_coefficient();
+        for (int i = tid; i < n; i += NT) {
+          const uint64_t k = sh.border[i];
+          const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
+          int b;
+          if (k >= cut)
+            atomicAdd(&sh.chunk_n[j / h.vectors],
+                      static_cast<unsigned long long>(weight_in_bin(entry_logit(k), k16, c5, b)));
+        }
+        __syncthreads();
+        const double w_last = n > 0 ? bin_weight(border) * unit : 0.;
 #pragma unroll 1
         for (int c = wid; c < h.chunks; c += W) {
-          double w = 0.;
+          double w = lane == 0 ? double(sh.chunk_n[c]) * w_last : 0.;
           for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
-#pragma unroll 1
-          for (int i = lane; i < n; i += 64) {
-            const uint64_t k = sh.list[i];
-            const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
-            if (k >= cut && j / h.vectors == c) w += sh.weight[i];
-          }
           w = wave_fold(w, add);
           if (lane == 0) sh.chunk[c] = w;
         }
@@ -905,14 +1010,11 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         write(greater, cut, mass, tok);
         return;
       }
-      if (PHASE == kBorder) {
-        leave(kLeftSearch);
-        return;
-      }
     }
-  } else if (PHASE == kLists) {
-    leave(kLeftSearch);
-    return;
+    if (PHASE == kBorder) {
+      leave(kLeftSearch);
+      return;
+    }
   }
   if constexpr (SEARCH) {
     // Neither the lists nor the histograms tell: counts of very many entries, values beyond the
@@ -920,11 +1022,11 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     const float scale = float(64. * s.inv_t);
     cut = has_k ? select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh) : 0;
     if (binned ? by_p : has_p) {
-      uint64_t end = 0, over = kKeyTop;
+      uint64_t from = 0, to = kKeyTop;
       double all = whole_w;
       if (binned) {
-        end = entry_key(bin_edge(border), a.V - 1);
-        over = border > 0 ? entry_key(bin_edge(border - 1), kColumnMask) - 1 : kKeyTop;
+        from = entry_key(note->end, a.V - 1);
+        to = border > 0 ? (uint64_t(f32_order_key(note->over)) << kColumnBits) - 1 : kKeyTop;
       } else {
         all = 0.;
         each_entry(r, [&](float z, int c) {
@@ -934,7 +1036,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       }
       // A target of 0 is reached by the first entry, not before it.
       cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2, scale,
-                                           sh, end, over, binned ? above : 0.));
+                                           sh, from, to, binned ? above : 0.));
     }
     cut = most64(cut, cut_m);
     double run, own;

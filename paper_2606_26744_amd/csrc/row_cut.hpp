@@ -27,9 +27,9 @@ constexpr float kLeast = -3.402823466e38f;   // the least finite value
 
 // The histogram: bins of 1/16 octave of weight.  Entry z has t = 16 z log2(e) / T, bin n = rint(t)
 // and within it the weight 2^((t - n) / 16), 0.978 .. 1.022, as a multiple of 2^-48; integers, so
-// that the sums do not depend on their order.  1024 bins from the chunk's greatest entry down;
-// entries more than 62 octaves below it weigh nothing.
-constexpr int kMassBins = 1024;
+// that the sums do not depend on their order.  Bins from the chunk's greatest entry down; entries
+// of the last 40, more than 61 octaves below it, weigh nothing.
+constexpr int kMassBins = 1024, kKeptBins = 984;
 constexpr double kMassUnit = 1.0 / 281474976710656.0;   // 2^-48
 
 struct HeadStat {
@@ -45,9 +45,12 @@ struct HeadStat {
   double rest;
 };
 
-// Between the phases of a row's cut: a nucleus' border bin, the weights above it and in the whole.
+// Between the phases of a row's cut: a nucleus' border bin, the weights above it and in the whole,
+// the bin's values end <= z < over; the last key that min_p keeps.
 struct CutNote {
   double whole, above;
+  uint64_t cut_m;
+  float end, over;
   int32_t border, by_p, left;
 };
 
@@ -89,27 +92,28 @@ constexpr double kRound = 6755399441055744.;
 __device__ __forceinline__ int weight_bin(float z, double k16) {
   return int(uint32_t(__builtin_bit_cast(uint64_t, fma_k(double(z), k16, kRound))));
 }
-// Bin and the weight within it as a multiple of 2^-48: the series of 2^(g / 16), |g| <= 1/2, whose
-// first dropped term is 0.022^7 / 7! = 4e-16, with all coefficients times 2^(48 - 1074), so that the
-// result is subnormal and its bits are the integer.  c6: mass_coefficient(), kept in registers by
-// the caller.
-constexpr double kLog16 = 0.69314718055994530942 / 16.;
+// Bin and the weight within it as a multiple of 2^-48: the series of 2^(g / 16), |g| <= 1/2, to the
+// sixth power, with g^6 replaced by 3/8 g^4 - 9/256 g^2 + 1/2048, from which it differs by
+// T_6(2g) / 2048: 5e-15 of the weight at the most, and of alternating sign.  All coefficients are
+// times 2^(48 - 1074), so that the result is subnormal and its bits are the integer.  c5:
+// mass_coefficient(), kept in registers by the caller.
 constexpr double kBits = 0x1p-1026;
+constexpr double kLog16 = 0.69314718055994530942 / 16., kLog16_2 = kLog16 * kLog16;
+constexpr double kMass6 = kLog16_2 * kLog16_2 * kLog16_2 / 720.;
 __device__ __forceinline__ double mass_coefficient() {
-  double c = kLog16 * kLog16 * kLog16 * kLog16 * kLog16 * kLog16 / 720. * kBits;
+  double c = kLog16_2 * kLog16_2 * kLog16 / 120. * kBits;
   asm volatile("" : "+v"(c));   // not copied anew for every entry
   return c;
 }
-__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, double c6, int& n) {
+__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, double c5, int& n) {
   const double t = fma_k(double(z), k16, kRound);
   n = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
   const double g = fma(double(z), k16, kRound - t);
-  double p = fma_k(c6, g, kLog16 * kLog16 * kLog16 * kLog16 * kLog16 / 120. * kBits);
-  p = fma_k(p, g, kLog16 * kLog16 * kLog16 * kLog16 / 24. * kBits);
-  p = fma_k(p, g, kLog16 * kLog16 * kLog16 / 6. * kBits);
-  p = fma_k(p, g, kLog16 * kLog16 / 2. * kBits);
+  double p = fma_k(c5, g, (kLog16_2 * kLog16_2 / 24. + kMass6 * 0.375) * kBits);
+  p = fma_k(p, g, kLog16_2 * kLog16 / 6. * kBits);
+  p = fma_k(p, g, (kLog16_2 / 2. - kMass6 * 0.03515625) * kBits);
   p = fma_k(p, g, kLog16 * kBits);
-  p = fma_k(p, g, kBits);
+  p = fma_k(p, g, (1. + kMass6 / 2048.) * kBits);
   return __builtin_bit_cast(uint64_t, p);
 }
 

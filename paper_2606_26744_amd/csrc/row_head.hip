@@ -18,6 +18,14 @@ __device__ __forceinline__ float max2(float a, float b) {
   return d;
 }
 
+// a * B + c of 24-bit a; B an inline constant.
+template <int B>
+__device__ __forceinline__ int mad24(int a, int c) {
+  int d;
+  asm("v_mad_i32_i24 %0, %1, %2, %3" : "=v"(d) : "v"(a), "n"(B), "v"(c));
+  return d;
+}
+
 // bits * 2 + (x >= lo), which is false for NaN.
 __device__ __forceinline__ uint32_t push_at_least(uint32_t bits, float x, float lo) {
   uint32_t d;
@@ -67,18 +75,23 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   auto least = [](float u, float v) { return fminf(u, v); };
   // Unmasked entries (NaN is masked: no comparison holds for it), the greatest one.
   uint32_t live = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      // (A ballot of "> -inf" comes out as "unequal or NaN" here: the least value instead.)
+      live += uint32_t(__popcll(__ballot(x[g][e] >= kLeast)));
+  if (live != uint32_t(kWave * E)) {   // of this wave
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[g][e] = x[g][e] >= kLeast ? x[g][e] : -INFINITY;
+  }
   float top = -INFINITY;
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      // (A ballot of "> -inf" comes out as "unequal or NaN" here: the least value instead.)
-      const bool is0 = x[g][e] >= kLeast, is1 = x[g][e + 1] >= kLeast;
-      live += uint32_t(__popcll(__ballot(is0))) + uint32_t(__popcll(__ballot(is1)));
-      x[g][e] = is0 ? x[g][e] : -INFINITY;
-      x[g][e + 1] = is1 ? x[g][e + 1] : -INFINITY;
-      top = max3(top, x[g][e], x[g][e + 1]);
-    }
+    for (int e = 0; e < N; e += 2) top = max3(top, x[g][e], x[g][e + 1]);
   if (tid == 0) best_col = a.V;
   if (lane == 0) wave_n[wid] = live;
   const float m = block_fold<kHeadWaves>(top, red.f, most);
@@ -153,28 +166,29 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0., 0.};
   if (s.binned && valid > 0) {
     const double k16 = 16. * s.c2;
-    const float range = float(992. / k16);   // 62 octaves
-    if (fabs(double(m)) * k16 < 8e6 && range < INFINITY) {   // bins of 24 bits
+    // Masked and far entries go to the last bins, which are not kept, all lanes to different ones:
+    // cheaper than leaving them out.  (A bin is at least half a unit in the last place of m wide.)
+    const float step = float(double(s.t) * kLog16);   // a bin's width
+    const float end = m - step * float(kKeptBins + 4 + (lane & 31));
+    if (fabs(double(m)) * k16 < 8e6 && m - step * float(kMassBins - 1) >= kLeast) {
       for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
       __syncthreads();
-      const float end = m - range;
-      const double c6 = mass_coefficient();
+      const double c5 = mass_coefficient();
       const int top_bin = weight_bin(m, k16);
       st.top_bin = top_bin;
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-        {
-          int n;   // of top_bin - 993 .. top_bin
-          const uint64_t w = weight_in_bin(max2(x[g][e], end), k16, c6, n);
+        for (int e = 0; e < N; ++e) {
+          int n;   // of 24 bits, top_bin - 1023 .. top_bin
+          const uint64_t w = weight_in_bin(max2(x[g][e], end), k16, c5, n);
           auto* bin = reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(mass) +
-                                                            __mul24(top_bin - n, 8));
-          if (x[g][e] >= end) atomicAdd(bin, static_cast<unsigned long long>(w));
+                                                            mad24<-8>(n, 8 * top_bin));
+          atomicAdd(bin, static_cast<unsigned long long>(w));
         }
       __syncthreads();
       uint32_t end_bin = 0;
-      for (int b = tid; b < kMassBins; b += kHeadThreads)
+      for (int b = tid; b < kKeptBins; b += kHeadThreads)
         if (mass[b] != 0) end_bin = uint32_t(b) + 1;
       end_bin = block_fold<kHeadWaves>(end_bin, red.i, [](uint32_t u, uint32_t v) { return u > v ? u : v; });
       uint64_t* out = h.mass + (at * h.chunks + chunk) * kMassBins;

@@ -208,14 +208,26 @@ __device__ __forceinline__ X block_scan(X v, X* sh, X& total) {
   v = wave_scan(v);
   if (lane == 63) sh[wid] = v;
   __syncthreads();
-  X before = X(0), all = X(0);
+  X before = X(0);
+  if constexpr (W == 4 || W == 8 || W == 16) {   // a lane a wave, and as within rows of 16
+    X t = sh[lane & (W - 1)];
+    t += dpp<0x111, 0xf>(t);
+    t += dpp<0x112, 0xf>(t);
+    if constexpr (W > 4) t += dpp<0x114, 0xf>(t);
+    if constexpr (W > 8) t += dpp<0x118, 0xf>(t);
+    const int w = __builtin_amdgcn_readfirstlane(wid);
+    if (w > 0) before = read_lane(t, w - 1);
+    total = read_lane(t, W - 1);
+  } else {
+    X all = X(0);
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    if (w == wid) before = all;
-    all += sh[w];
+    for (int w = 0; w < W; ++w) {
+      if (w == wid) before = all;
+      all += sh[w];
+    }
+    total = all;
   }
   __syncthreads();
-  total = all;
   return before + v;
 }
 
