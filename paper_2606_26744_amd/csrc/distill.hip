@@ -19,11 +19,11 @@ constexpr int kDistPart = kDistThreads * kDistElems;        // columns of a part
 constexpr int kMaxTop = 1024;                               // K at most
 constexpr int kHashSlots = 2 * kMaxTop;
 
-// What a part of a row adds: its greatest logit m and, relative to it, the sums of e^((z - m) / T)
-// over all columns and over the unlisted ones, and of e^(z - m).
+// What a part of a row adds: its greatest logit m; the sums of e^((z - mt) / T) over all columns and
+// over the unlisted ones, and of e^(z - m1), mt and m1 being m but for rounding.
 struct DistPart {
   float m;
-  double st, out, s1;
+  double mt, m1, st, out, s1;
 };
 
 // A supervised slot's statistics for the backward pass.
@@ -95,31 +95,63 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < N; ++e) m = fmaxf(m, x[g][e]);
+    for (int e = 0; e < N; e += 2) m = max3(m, x[g][e], x[g][e + 1]);
   m = block_fold<kDistWaves>(m, shf, [](float u, float v) { return fmaxf(u, v); });
-  const float ref = m == -INFINITY ? 0.f : m;
-  float st = 0.f, out = 0.f, s1 = 0.f;
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int b = (g * kDistThreads + int(threadIdx.x)) * N;
-    const uint32_t in = bucket ? listed[b >> 5] >> (b & 31) : 0u;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float d = x[g][e] - ref;
-      if (soft) {
-        const float w = __builtin_amdgcn_exp2f(d * a.c2);
-        st += w;
-        out += (in >> e) & 1u ? 0.f : w;
-      }
-      if (a.labels != nullptr && !(soft && a.t == 1.f)) s1 += __builtin_amdgcn_exp2f(d * 1.44269504f);
-    }
-  }
-  auto add = [](double u, double v) { return u + v; };
+  // An exponential costs one product, rounded once: 2^(z c - b), b the rounded product of m and c,
+  // so relative to b / c.  Where that rounding is no small part of an octave (rows of the type's
+  // lowest value), z - m first.
   DistPart o;
   o.m = m;
-  o.st = block_fold<kDistWaves>(double(st), shd, add);
+  float ref = m == -INFINITY ? 0.f : m;
+  const float log2e = 1.44269504f, c_most = fmaxf(soft ? a.c2 : 0.f, log2e);
+  if (!(fabsf(ref) * c_most < 1e6f)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[g][e] -= ref;
+    o.mt = o.m1 = double(ref);
+    ref = 0.f;
+  } else {
+    o.mt = double(ref * a.c2) / double(a.c2);
+    o.m1 = double(ref * log2e) / double(log2e);
+  }
+  const bool hard = a.labels != nullptr && !(soft && a.t == 1.f);
+  float s1 = 0.f;
+  if (hard) {
+    const float b = ref * log2e;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s1 += __builtin_amdgcn_exp2f(fmaf(x[g][e], log2e, -b));
+  }
+  float in = 0.f, out = 0.f;   // over the listed (with the bucket) and the other columns
+  if (soft) {
+    const float b = ref * a.c2;
+    auto weight = [&](float z) { return __builtin_amdgcn_exp2f(fmaf(z, a.c2, -b)); };
+    if (bucket) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int at = (g * kDistThreads + int(threadIdx.x)) * N;
+        const uint32_t is = listed[at >> 5] >> (at & 31) & ((1u << N) - 1);
+        if (is != 0) {   // few
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if ((is >> e) & 1u) {
+              in += weight(x[g][e]);
+              x[g][e] = -INFINITY;
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < N; ++e) out += weight(x[g][e]);
+  }
+  auto add = [](double u, double v) { return u + v; };
   o.out = block_fold<kDistWaves>(double(out), shd, add);
-  o.s1 = soft && a.t == 1.f ? o.st : block_fold<kDistWaves>(double(s1), shd, add);
+  o.st = o.out + (bucket ? block_fold<kDistWaves>(double(in), shd, add) : 0.);
+  o.s1 = hard ? block_fold<kDistWaves>(double(s1), shd, add) : o.st;
   if (threadIdx.x == 0) parts[i * gridDim.x + part] = o;
 }
 
@@ -144,10 +176,12 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
   double st = 0., out = 0., s1 = 0.;
   for (int j = tid; j < n_parts; j += kDistThreads) {
     const DistPart o = pt[j];
-    const double d = o.m == -INFINITY ? -INFINITY : double(o.m) - ref;
-    st += o.st * exp2_64(d * c2);
-    out += o.out * exp2_64(d * c2);
-    s1 += o.s1 * exp2_64(d * 1.4426950408889634074);
+    const double wt = exp2_64(o.m == -INFINITY ? -INFINITY : (o.mt - ref) * c2);
+    st += o.st * wt;
+    out += o.out * wt;
+    s1 += a.t == 1.f && k <= a.P
+              ? o.s1 * wt
+              : o.s1 * exp2_64(o.m == -INFINITY ? -INFINITY : (o.m1 - ref) * 1.4426950408889634074);
   }
   st = block_fold<kDistWaves>(st, sh, add);
   out = block_fold<kDistWaves>(out, sh, add);

@@ -33,7 +33,7 @@ constexpr int kMassBins = 1024, kKeptBins = 984;
 constexpr double kMassUnit = 1.0 / 281474976710656.0;   // 2^-48
 
 struct HeadStat {
-  float best;        // greatest value, its lowest column
+  float best;        // greatest value, its lowest column (of greedy rows)
   int32_t best_col;
   float floor;       // every entry >= floor is listed (-inf: all are)
   float near;        // a value that the chunk's share of the top_k entries reaches

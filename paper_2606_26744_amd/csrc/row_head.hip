@@ -5,19 +5,6 @@ namespace hdf {
 
 constexpr int kHeadWaves = kHeadThreads / kWave;
 
-// The greatest of three or two values, none of them NaN.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-  return d;
-}
-
-__device__ __forceinline__ float max2(float a, float b) {
-  float d;
-  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
-  return d;
-}
-
 // a * B + c of 24-bit a; B an inline constant.
 template <int B>
 __device__ __forceinline__ int mad24(int a, int c) {
@@ -49,7 +36,8 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     uint32_t i[kHeadWaves];
   } red;
   __shared__ uint32_t wave_n[kHeadWaves];
-  __shared__ int best_col;
+  __shared__ int best_col, end_bin;
+  __shared__ uint16_t picked[kHeadThreads / kWave][kWave];
   const int64_t at = blockIdx.x / h.chunks, row = a.row0 + at;   // in the launch, in the call
   const int chunk = int(blockIdx.x - at * h.chunks), tid = threadIdx.x;
   const int lane = tid & 63, wid = tid >> 6;
@@ -92,21 +80,23 @@ row_head_kernel(CutArgs a, HeadArgs h) {
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int e = 0; e < N; e += 2) top = max3(top, x[g][e], x[g][e + 1]);
-  if (tid == 0) best_col = a.V;
+  if (tid == 0) best_col = a.V, end_bin = 0;
   if (lane == 0) wave_n[wid] = live;
   const float m = block_fold<kHeadWaves>(top, red.f, most);
   uint32_t valid = 0;
 #pragma unroll
   for (int w = 0; w < kHeadWaves; ++w) valid += wave_n[w];
-  if (top == m && m > -INFINITY) {
-    int first = a.V;
+  if (s.greedy) {
+    if (top == m && m > -INFINITY) {
+      int first = a.V;
 #pragma unroll
-    for (int g = G - 1; g >= 0; --g)
+      for (int g = G - 1; g >= 0; --g)
 #pragma unroll
-      for (int e = N - 1; e >= 0; --e) first = x[g][e] == m ? col(g, e) : first;
-    atomicMin(&best_col, first);
+        for (int e = N - 1; e >= 0; --e) first = x[g][e] == m ? col(g, e) : first;
+      atomicMin(&best_col, first);
+    }
+    __syncthreads();
   }
-  __syncthreads();
 
   // The list: all entries >= lo, lo a thread's greatest value such that `want` threads reach it; so
   // at least `want` entries do, and hardly more unless the great ones crowd into few threads (then
@@ -134,7 +124,8 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     count[tid] = upto;
     __syncthreads();
     const uint32_t first = in && mine > 0 ? count[mine - 1] : 0u;   // threads in the bins before
-    near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
+    if (s.top_k > 0)
+      near = block_fold<kHeadWaves>(in && first < uint32_t(few) ? top : INFINITY, red.f, least);
     const bool every = valid <= uint32_t(h.cap);
     uint32_t bits = 0, before = 0;   // this thread's listed entries, the first one's bit the highest
     for (; want > 0; want /= 2) {
@@ -151,19 +142,37 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     }
     if (want == 0) {
       lo = INFINITY;
-      listed = bits = 0;
+      listed = bits = before = 0;   // of the last attempt
     }
-    // Few threads have more than one or two: their values are read again, not picked from registers.
-    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap + before;
-    while (bits != 0) {
-      const int q = E - __ffs(bits);
-      bits &= bits - 1;
-      const int c = r.column(j0 + q / N * kHeadThreads + tid) + q % N;
-      *list++ = entry_key(r.raw(c), c);
+    // Few of a wave's entries are listed: brought together, a lane takes one, whose value is read
+    // again, not picked from registers.
+    uint64_t* list = h.list + (at * h.chunks + chunk) * h.cap;
+    const uint32_t wave0 = read_lane(before, 0);
+    const uint32_t in_wave = read_lane(before + uint32_t(__popc(bits)), kWave - 1) - wave0;
+#pragma unroll 1
+    for (uint32_t b0 = 0; b0 < in_wave; b0 += kWave) {
+      uint32_t i = before - wave0 - b0;
+      while (bits != 0 && i < uint32_t(kWave)) {
+        const int q = E - __ffs(bits);
+        bits &= bits - 1;
+        picked[wid][i++] = uint16_t(q * kWave + lane);
+      }
+      before = wave0 + b0 + i;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      if (b0 + lane < in_wave) {
+        const int p = picked[wid][lane], q = p / kWave;
+        const int c = r.column(j0 + q / N * kHeadThreads + wid * kWave + p % kWave) + q % N;
+        list[wave0 + b0 + lane] = entry_key(r.raw(c), c);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
   }
 
-  HeadStat st{m, best_col, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0., 0.};
+  HeadStat st{m, s.greedy ? best_col : 0, valid == listed ? -INFINITY : lo, near, valid, listed, 0, 0, 0., 0.};
   if (s.binned && valid > 0) {
     const double k16 = 16. * s.c2;
     // Masked and far entries go to the last bins, which are not kept, all lanes to different ones:
@@ -187,13 +196,15 @@ row_head_kernel(CutArgs a, HeadArgs h) {
           atomicAdd(bin, static_cast<unsigned long long>(w));
         }
       __syncthreads();
-      uint32_t end_bin = 0;
-      for (int b = tid; b < kKeptBins; b += kHeadThreads)
-        if (mass[b] != 0) end_bin = uint32_t(b) + 1;
-      end_bin = block_fold<kHeadWaves>(end_bin, red.i, [](uint32_t u, uint32_t v) { return u > v ? u : v; });
+      for (int b0 = 0; b0 < kKeptBins; b0 += kHeadThreads) {   // whole waves
+        const int b = b0 + tid;
+        note_last(b < kKeptBins && mass[b < kKeptBins ? b : 0] != 0, b + 1, &end_bin);
+      }
+      __syncthreads();
+      const int bins = end_bin;
       uint64_t* out = h.mass + (at * h.chunks + chunk) * kMassBins;
-      for (int b = tid; b < int(end_bin); b += kHeadThreads) out[b] = mass[b];
-      st.bins = int(end_bin);
+      for (int b = tid; b < bins; b += kHeadThreads) out[b] = mass[b];
+      st.bins = bins;
     } else {
       st.bins = -1;
     }

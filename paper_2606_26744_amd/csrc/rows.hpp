@@ -78,6 +78,19 @@ __device__ __forceinline__ int entry_column(uint64_t k) {
   return int(kColumnMask - (uint32_t(k) & kColumnMask));
 }
 
+// The greatest of three or two values, none of them NaN.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+__device__ __forceinline__ float max2(float a, float b) {
+  float d;
+  asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+
 // a * b + k with k the same for all lanes: a scalar operand.  (The compiler would copy k into the
 // result first, two moves a product, and take three times as long over a series.)
 __device__ __forceinline__ double fma_k(double a, double b, double k) {
