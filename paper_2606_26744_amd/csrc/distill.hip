@@ -10,6 +10,8 @@
 #include "kernels.hpp"
 #include "rows.hpp"
 
+#include <type_traits>
+
 namespace hdf {
 
 constexpr int kDistThreads = 256;
@@ -64,8 +66,7 @@ __global__ void __launch_bounds__(kDistThreads)
 distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
   constexpr int N = LogitRow<T>::N, G = kDistElems / N;
   __shared__ uint32_t listed[kDistPart / 32];
-  __shared__ float shf[kDistWaves];
-  __shared__ double shd[kDistWaves];
+  __shared__ float shf[kDistWaves], sums[kDistWaves][3];
   const int part = blockIdx.x;
   const int64_t i = blockIdx.y, s = i / slots;
   const int k = int(i - s * slots) + 1;
@@ -73,12 +74,17 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
   const int j0 = part * (kDistPart / N), nv = r.vectors();
   const bool soft = k <= a.P, bucket = soft && a.rest != nullptr;
   float x[G][N];
+  if (r.inside(j0, G * kDistThreads)) {   // all but a row's first and last part
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int j = j0 + g * kDistThreads + int(threadIdx.x);
+    for (int g = 0; g < G; ++g) r.load_inside(j0 + g * kDistThreads + int(threadIdx.x), x[g]);
+  } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
-    if (j < nv) r.load_raw(j, x[g]);
+    for (int g = 0; g < G; ++g) {
+      const int j = j0 + g * kDistThreads + int(threadIdx.x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+      if (j < nv) r.load_raw(j, x[g]);
+    }
   }
   if (bucket) {
     for (int w = threadIdx.x; w < kDistPart / 32; w += kDistThreads) listed[w] = 0;
@@ -100,34 +106,36 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
   // An exponential costs one product, rounded once: 2^(z c - b), b the rounded product of m and c,
   // so relative to b / c.  Where that rounding is no small part of an octave (rows of the type's
   // lowest value), z - m first.
-  DistPart o;
-  o.m = m;
-  float ref = m == -INFINITY ? 0.f : m;
-  const float log2e = 1.44269504f, c_most = fmaxf(soft ? a.c2 : 0.f, log2e);
-  if (!(fabsf(ref) * c_most < 1e6f)) {
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[g][e] -= ref;
-    o.mt = o.m1 = double(ref);
-    ref = 0.f;
-  } else {
-    o.mt = double(ref * a.c2) / double(a.c2);
-    o.m1 = double(ref * log2e) / double(log2e);
-  }
+  const float ref = m == -INFINITY ? 0.f : m, log2e = 1.44269504f;
+  const bool far = !(fabsf(ref) * fmaxf(soft ? a.c2 : 0.f, log2e) < 1e6f);
   const bool hard = a.labels != nullptr && !(soft && a.t == 1.f);
-  float s1 = 0.f;
-  if (hard) {
-    const float b = ref * log2e;
+  // Over the whole row at T = 1, the unlisted and the listed (with the bucket) columns: 32-bit sums
+  // of N values, then of few of those and over the wave, at most 15 additions in a row; 64-bit
+  // beyond.
+  float sum[3] = {0.f, 0.f, 0.f};
+  auto weight = [&](bool is_far, float z, float c, float b) {
+    return __builtin_amdgcn_exp2f(is_far ? (z - ref) * c : fmaf(z, c, -b));
+  };
+  auto exps_of = [&](auto is_far, float c) __attribute__((always_inline)) {
+    const float b = ref * c;
+    float v[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g) {
+      v[g] = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s1 += __builtin_amdgcn_exp2f(fmaf(x[g][e], log2e, -b));
-  }
-  float in = 0.f, out = 0.f;   // over the listed (with the bucket) and the other columns
+      for (int e = 0; e < N; ++e) v[g] += weight(decltype(is_far)::value, x[g][e], c, b);
+    }
+#pragma unroll
+    for (int d = 1; d < G; d *= 2)
+#pragma unroll
+      for (int g = 0; g < G; g += 2 * d) v[g] += v[g + d];
+    return v[0];
+  };
+  auto exps = [&](float c) __attribute__((always_inline)) {
+    return far ? exps_of(std::true_type(), c) : exps_of(std::false_type(), c);
+  };
+  if (hard) sum[0] = exps(log2e);
   if (soft) {
-    const float b = ref * a.c2;
-    auto weight = [&](float z) { return __builtin_amdgcn_exp2f(fmaf(z, a.c2, -b)); };
     if (bucket) {
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -137,22 +145,34 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
 #pragma unroll
           for (int e = 0; e < N; ++e)
             if ((is >> e) & 1u) {
-              in += weight(x[g][e]);
+              sum[2] += weight(far, x[g][e], a.c2, ref * a.c2);
               x[g][e] = -INFINITY;
             }
         }
       }
     }
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int e = 0; e < N; ++e) out += weight(x[g][e]);
+    sum[1] = exps(a.c2);
   }
-  auto add = [](double u, double v) { return u + v; };
-  o.out = block_fold<kDistWaves>(double(out), shd, add);
-  o.st = o.out + (bucket ? block_fold<kDistWaves>(double(in), shd, add) : 0.);
-  o.s1 = hard ? block_fold<kDistWaves>(double(s1), shd, add) : o.st;
-  if (threadIdx.x == 0) parts[i * gridDim.x + part] = o;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const float t = wave_fold(sum[i], [](float u, float v) { return u + v; });
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6][i] = t;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double t[3] = {0., 0., 0.};
+#pragma unroll
+  for (int w = 0; w < kDistWaves; ++w)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) t[i] += double(sums[w][i]);
+  DistPart o;
+  o.m = m;
+  o.mt = far ? double(ref) : double(ref * a.c2) / double(a.c2);
+  o.m1 = far ? double(ref) : double(ref * log2e) / double(log2e);
+  o.out = t[1];
+  o.st = t[1] + t[2];
+  o.s1 = hard ? t[0] : o.st;
+  parts[i * gridDim.x + part] = o;
 }
 
 // One workgroup a slot: the parts joined, the teacher's distribution, the losses.
@@ -345,38 +365,73 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
       label = a.labels[q];
     }
   }
-  const bool soft = wk != 0.f, hard = wc != 0.f;
+  const bool soft = wk != 0.f, hard = wc != 0.f, one = a.t == 1.f;
+  const float log2e = 1.44269504f;
   const float ct = wk * st.inv_t, co = ct * st.outside, c1 = wc * st.inv_1;
   auto at_t = [&](float x) { return soft ? __builtin_amdgcn_exp2f((x - st.m) * a.c2) : 0.f; };
-  auto at_1 = [&](float x) { return hard ? __builtin_amdgcn_exp2f((x - st.m) * 1.44269504f) : 0.f; };
+  auto at_1 = [&](float x) { return hard ? __builtin_amdgcn_exp2f((x - st.m) * log2e) : 0.f; };
   float x[G][N];
+  const bool inside = r.inside(j0, G * kDistThreads);   // all but a row's first and last part
+  if (inside && (soft || hard)) {
 #pragma unroll
-  for (int h = 0; h < G; ++h) {
-    const int j = j0 + h * kDistThreads + tid;
+    for (int h = 0; h < G; ++h) r.load_inside(j0 + h * kDistThreads + tid, x[h]);
+  } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[h][e] = -INFINITY;
-    if ((soft || hard) && j < nv) r.load_raw(j, x[h]);
-  }
+    for (int h = 0; h < G; ++h) {
+      const int j = j0 + h * kDistThreads + tid;
 #pragma unroll
-  for (int h = 0; h < G; ++h) {
-    const int j = j0 + h * kDistThreads + tid;
-    if (j >= nv) continue;
-    T o[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float et = at_t(x[h][e]);
-      const float e1 = hard && soft && a.t == 1.f ? et : at_1(x[h][e]);
-      store_grad(&o[e], (soft ? et * co : 0.f) + (hard ? e1 * c1 : 0.f));
+      for (int e = 0; e < N; ++e) x[h][e] = -INFINITY;
+      if ((soft || hard) && j < nv) r.load_raw(j, x[h]);
     }
-    const int c = r.column(j);
-    if (vec && c >= 0 && c + N <= a.V) {
+  }
+  // As in the forward pass, an exponential costs one product where z c is not too far out; what
+  // rounding adds to the product of m and c goes into the factor.
+  const bool far = !(fabsf(st.m) * fmaxf(soft ? a.c2 : 0.f, log2e) < 1e6f);
+  auto sums = [&](auto is_far, auto two, float c, float k, float k1) __attribute__((always_inline)) {
+    constexpr bool FAR = decltype(is_far)::value;
+    const float b = st.m * c, b1 = st.m * log2e;
+    if (!FAR) {
+      k *= __builtin_amdgcn_exp2f(-fmaf(st.m, c, -b));
+      k1 *= __builtin_amdgcn_exp2f(-fmaf(st.m, log2e, -b1));
+    }
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float z = x[h][e], d = z - st.m;
+        float v = __builtin_amdgcn_exp2f(FAR ? d * c : fmaf(z, c, -b)) * k;
+        if (decltype(two)::value)
+          v = fmaf(__builtin_amdgcn_exp2f(FAR ? d * log2e : fmaf(z, log2e, -b1)), k1, v);
+        x[h][e] = v;
+      }
+  };
+  const bool two = soft && hard && !one;
+  const float c = soft ? a.c2 : log2e, k1 = hard ? c1 : 0.f, kt = (soft ? co : 0.f) + (two ? 0.f : k1);
+  if (two && far)
+    sums(std::true_type(), std::true_type(), c, kt, k1);
+  else if (two)
+    sums(std::false_type(), std::true_type(), c, kt, k1);
+  else if (far)
+    sums(std::true_type(), std::false_type(), c, kt, 0.f);
+  else
+    sums(std::false_type(), std::false_type(), c, kt, 0.f);   // zeros where there is no loss
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    const int j = j0 + h * kDistThreads + tid, c = r.column(j);
+    if (vec && (inside || (j < nv && c >= 0 && c + N <= a.V))) {
       u32x4 q;
-      __builtin_memcpy(&q, o, 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 2)
+          q[e] = pack_bf2(x[h][2 * e], x[h][2 * e + 1]);
+        else
+          q[e] = __float_as_uint(x[h][e]);
+      }
       st16(d + c, q);
-    } else {
+    } else if (j < nv) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (c + e >= 0 && c + e < a.V) d[c + e] = o[e];
+        if (c + e >= 0 && c + e < a.V) store_grad(d + c + e, x[h][e]);
     }
   }
   if (!soft && !hard) return;
