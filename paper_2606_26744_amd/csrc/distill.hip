@@ -19,7 +19,6 @@ constexpr int kDistWaves = kDistThreads / kWave;
 constexpr int kDistElems = 32;                              // of a part, a thread
 constexpr int kDistPart = kDistThreads * kDistElems;        // columns of a part
 constexpr int kMaxTop = 1024;                               // K at most
-constexpr int kHashSlots = 2 * kMaxTop;
 
 // What a part of a row adds: its greatest logit m; the sums of e^((z - mt) / T) over all columns and
 // over the unlisted ones, and of e^(z - m1), mt and m1 being m but for rounding.
@@ -175,94 +174,143 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts) {
   parts[i * gridDim.x + part] = o;
 }
 
-// One workgroup a slot: the parts joined, the teacher's distribution, the losses.
-template <typename T>
-__global__ void __launch_bounds__(kDistThreads)
+// Values of all waves folded at once, f[i] into v[i]: one barrier, so `sh` is not to be written again
+// before the next one.
+template <int W, int N, typename F>
+__device__ __forceinline__ void fold_all(double (&v)[N], double (&sh)[W][N], F f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = wave_fold(v[i], [&](double x, double y) { return f(i, x, y); });
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6][i] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = sh[0][i];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v[i] = f(i, v[i], sh[w][i]);
+  }
+}
+
+// One workgroup a slot: the parts joined, the teacher's distribution, the losses.  A matter of
+// latency: all loads but the listed logits' go out first, and five barriers separate its steps.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT)
 distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, int n_parts,
                    DistSaved sv) {
-  __shared__ int hash_id[kHashSlots], hash_at[kHashSlots];
-  __shared__ double sh[kDistWaves];
+  constexpr int Q = 4, W = NT / kWave;   // listed tokens of a thread, at most
+  __shared__ int hash_id[2 * Q * NT], hash_at[2 * Q * NT];
+  __shared__ double sh3[W][3], sh4[W][4], sh1[W][1];
   const int64_t i = blockIdx.x, s = i / slots;
   const int k = int(i - s * slots) + 1, tid = threadIdx.x;
   const LogitRow<T> r(static_cast<const T*>(a.z) + (s * a.B + k) * a.ld, a.V);
-  auto add = [](double u, double v) { return u + v; };
-  auto most = [](double u, double v) { return fmax(u, v); };
-  const DistPart* pt = parts + i * n_parts;
-  double m = -INFINITY;
-  for (int j = tid; j < n_parts; j += kDistThreads) m = fmax(m, double(pt[j].m));
-  m = block_fold<kDistWaves>(m, sh, most);
-  const double ref = m == -INFINITY ? 0. : m;
-  const double c2 = 1.4426950408889634074 / double(a.t);
-  double st = 0., out = 0., s1 = 0.;
-  for (int j = tid; j < n_parts; j += kDistThreads) {
-    const DistPart o = pt[j];
-    const double wt = exp2_64(o.m == -INFINITY ? -INFINITY : (o.mt - ref) * c2);
-    st += o.st * wt;
-    out += o.out * wt;
-    s1 += a.t == 1.f && k <= a.P
-              ? o.s1 * wt
-              : o.s1 * exp2_64(o.m == -INFINITY ? -INFINITY : (o.m1 - ref) * 1.4426950408889634074);
-  }
-  st = block_fold<kDistWaves>(st, sh, add);
-  out = block_fold<kDistWaves>(out, sh, add);
-  s1 = block_fold<kDistWaves>(s1, sh, add);
-  // A row masked throughout has no softmax: its factors are 0, as its exponentials.
-  DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), 1.f, 0, 0};
-
-  if (k <= a.P) {
-    const int64_t q = s * a.P + k - 1;
+  const bool soft = k <= a.P;
+  const int64_t q = s * a.P + k - 1;
+  int id[Q], slot[Q];
+  double l[Q], z[Q];   // the teacher's logits over T, the student's
+  double lr = -INFINITY;
+  const double inv_t = 1. / double(a.t);
+  if (soft) {
     const int32_t* ids = a.ids + q * a.K;
     const float* tl = a.tl + q * a.K;
-    float* ps = sv.p + q * a.K;
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      const int t = e * NT + tid;
+      id[e] = t < a.K ? ids[t] : -1;
+      l[e] = t < a.K ? double(tl[t]) * inv_t : -INFINITY;
+      if (id[e] >= a.V) id[e] = -1;
+    }
+    if (a.rest != nullptr) lr = double(a.rest[q]);
+  }
+  const DistPart* pt = parts + i * n_parts;
+  DistPart first;
+  first.m = -INFINITY;
+  if (tid < n_parts) first = pt[tid];
+  double label_z = 0.;
+  int label = -1;
+  if (a.labels != nullptr) {
+    label = a.labels[s * (a.B - 1) + k - 1];
+    if (label >= 0 && label < a.V) label_z = double(r.raw(label));
+  }
+  double v[3] = {-INFINITY, -INFINITY, 0.};   // greatest logit, the teacher's; its NaNs
+  v[0] = double(first.m);
+  for (int j = tid + NT; j < n_parts; j += NT) v[0] = fmax(v[0], double(pt[j].m));
+  int mask = 127;   // of the hash table: at least twice as many slots as tokens
+  if (soft) {
+#pragma unroll
+    for (int e = 0; e < Q; ++e) z[e] = id[e] >= 0 ? double(r.raw(id[e])) : 0.;
     // A token's first place in the list holds: a table of tokens with their least place.
-    for (int h = tid; h < kHashSlots; h += kDistThreads) {
+    while (mask + 1 < 2 * a.K) mask = 2 * mask + 1;
+    for (int h = tid; h <= mask; h += NT) {
       hash_id[h] = -1;
       hash_at[h] = kMaxTop;
     }
     __syncthreads();
-    auto find = [&](int id) {
-      uint32_t h = (uint32_t(id) * 2654435761u) >> 21;   // 11 bits: kHashSlots
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      if (id[e] < 0) continue;
+      uint32_t h = (uint32_t(id[e]) * 2654435761u) >> 20 & uint32_t(mask);
       for (;;) {
-        const int was = atomicCAS(&hash_id[h], -1, id);
-        if (was == -1 || was == id) return int(h);
-        h = (h + 1) & (kHashSlots - 1);
+        const int was = atomicCAS(&hash_id[h], -1, id[e]);
+        if (was == -1 || was == id[e]) break;
+        h = (h + 1) & uint32_t(mask);
       }
-    };
-    for (int t = tid; t < a.K; t += kDistThreads) {
-      const int id = ids[t];
-      if (id >= 0 && id < a.V) atomicMin(&hash_at[find(id)], t);
+      slot[e] = int(h);
+      atomicMin(&hash_at[h], e * NT + tid);
     }
     __syncthreads();
-    const double inv_t = 1. / double(a.t);
-    const double lr = a.rest != nullptr ? double(a.rest[q]) : -INFINITY;
-    auto holds = [&](int t) {
-      const int id = ids[t];
-      return id >= 0 && id < a.V && hash_at[find(id)] == t;
-    };
-    double top = tid == 0 ? lr : -INFINITY, bad = tid == 0 && lr != lr ? lr : 0.;
-    for (int t = tid; t < a.K; t += kDistThreads)
-      if (holds(t)) {
-        const double l = double(tl[t]) * inv_t;
-        top = fmax(top, l);
-        bad += l != l ? l : 0.;
-      }
-    top = block_fold<kDistWaves>(top, sh, most);
-    bad = block_fold<kDistWaves>(bad, sh, add);
-    double kl = 0.;
-    if (top > -INFINITY || bad != 0.) {   // a teacher with some mass, or with a NaN to pass on
-      const double er = lr == -INFINITY ? 0. : exp(lr - top);
-      double sum = tid == 0 ? er : 0.;
-      for (int t = tid; t < a.K; t += kDistThreads)
-        if (holds(t)) sum += exp(double(tl[t]) * inv_t - top);
-      sum = block_fold<kDistWaves>(sum, sh, add);
+    v[1] = tid == 0 ? lr : -INFINITY;
+    v[2] = tid == 0 && lr != lr ? lr : 0.;
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      if (id[e] >= 0 && hash_at[slot[e]] != e * NT + tid) id[e] = -1;
+      if (id[e] < 0) continue;
+      v[1] = fmax(v[1], l[e]);
+      v[2] += l[e] != l[e] ? l[e] : 0.;
+    }
+  }
+  fold_all(v, sh3, [](int e, double x, double y) { return e < 2 ? fmax(x, y) : x + y; });
+  const double ref = v[0] == -INFINITY ? 0. : v[0], top = v[1], bad = v[2];
+  const bool taught = soft && (top > -INFINITY || bad != 0.);   // some mass, or a NaN to pass on
+  const double c2 = 1.4426950408889634074 / double(a.t);
+  double u[4] = {0., 0., 0., 0.};   // st, out, s1; the teacher's sum
+  auto join = [&](const DistPart& o) {
+    if (o.m == -INFINITY && o.st == o.st && o.s1 == o.s1) return;
+    const double wt = exp2_64((o.mt - ref) * c2);
+    u[0] += o.st * wt;
+    u[1] += o.out * wt;
+    u[2] += soft && a.t == 1.f ? o.s1 * wt : o.s1 * exp2_64((o.m1 - ref) * 1.4426950408889634074);
+  };
+  if (tid < n_parts) join(first);
+  for (int j = tid + NT; j < n_parts; j += NT) join(pt[j]);
+  const double er = lr == -INFINITY || !taught ? 0. : exp(lr - top);
+  double w[Q];
+  if (taught) {
+    u[3] = tid == 0 ? er : 0.;
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      w[e] = id[e] >= 0 ? exp(l[e] - top) : 0.;
+      u[3] += w[e];
+    }
+  }
+  fold_all(u, sh4, [](int, double x, double y) { return x + y; });
+  const double st = u[0], out = u[1], s1 = u[2], sum = u[3];
+  // A row masked throughout has no softmax: its factors are 0, as its exponentials.
+  DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), 1.f, 0, 0};
+  if (soft) {
+    float* ps = sv.p + q * a.K;
+    double kl[1] = {0.};
+    if (taught) {
       const double log_sum = log(sum), log_st = log(st);
-      for (int t = tid; t < a.K; t += kDistThreads) {
+#pragma unroll
+      for (int e = 0; e < Q; ++e) {
+        const int t = e * NT + tid;
+        if (t >= a.K) continue;
         float stored = -1.f;
-        if (holds(t)) {
-          const double l = double(tl[t]) * inv_t - top, p = exp(l) / sum;
-          const double z = double(r.raw(ids[t]));
-          const double lq = z == -INFINITY ? -INFINITY : (z - ref) * inv_t - log_st;
-          kl += p == 0. ? 0. : p * (l - log_sum - lq);
+        if (id[e] >= 0) {
+          const double p = w[e] / sum;
+          const double lq = z[e] == -INFINITY ? -INFINITY : (z[e] - ref) * inv_t - log_st;
+          kl[0] += p == 0. ? 0. : p * (l[e] - top - log_sum - lq);
           stored = float(p);
         }
         ps[t] = stored;
@@ -270,27 +318,24 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
       if (tid == 0 && er != 0.) {
         const double p = er / sum;
         const double lq = out == 0. ? -INFINITY : log(out) - log_st;
-        kl += p * (lr - top - log_sum - lq);
+        kl[0] += p * (lr - top - log_sum - lq);
         if (out != 0.) row.outside = float(1. - p * st / out);
       }
-      kl = block_fold<kDistWaves>(kl, sh, add) + bad;
       row.kl = 1;
     } else {
-      for (int t = tid; t < a.K; t += kDistThreads) ps[t] = -1.f;
+      for (int t = tid; t < a.K; t += NT) ps[t] = -1.f;
     }
-    if (tid == 0) a.kl[q] = float(kl);
+    fold_all(kl, sh1, [](int, double x, double y) { return x + y; });
+    if (tid == 0) a.kl[q] = float(kl[0] + bad);
   }
   if (tid != 0) return;
   if (a.labels != nullptr) {
-    const int64_t q = s * (a.B - 1) + k - 1;
-    const int label = a.labels[q];
     double ce = 0.;
     if (label >= 0 && label < a.V) {
-      const double z = double(r.raw(label));
-      ce = z == -INFINITY ? INFINITY : ref + log(s1) - z;
+      ce = label_z == -INFINITY ? INFINITY : ref + log(s1) - label_z;
       row.ce = 1;
     }
-    a.ce[q] = float(ce);
+    a.ce[s * (a.B - 1) + k - 1] = float(ce);
   }
   sv.rows[s * (a.B - 1) + k - 1] = row;
 }
@@ -301,19 +346,16 @@ constexpr int kLossThreads = 1024;
 
 __global__ void __launch_bounds__(kLossThreads)
 distill_loss_kernel(DistArgs a, DistSaved sv) {
-  constexpr int W = kLossThreads / kWave;
-  __shared__ double sh[W];
-  auto add = [](double u, double v) { return u + v; };
-  double kl = 0., ce = 0., n = 0.;
-  for (int i = threadIdx.x; i < a.n_seq * a.P; i += kLossThreads) kl += double(a.kl[i]);
+  __shared__ double sh[kLossThreads / kWave][3];
+  double v[3] = {0., 0., 0.};   // kl, ce; labelled slots
+  for (int i = threadIdx.x; i < a.n_seq * a.P; i += kLossThreads) v[0] += double(a.kl[i]);
   if (a.labels != nullptr)
     for (int i = threadIdx.x; i < a.n_seq * (a.B - 1); i += kLossThreads) {
-      ce += double(a.ce[i]);
-      n += a.labels[i] >= 0 && a.labels[i] < a.V ? 1. : 0.;
+      v[1] += double(a.ce[i]);
+      v[2] += a.labels[i] >= 0 && a.labels[i] < a.V ? 1. : 0.;
     }
-  kl = block_fold<W>(kl, sh, add);
-  ce = block_fold<W>(ce, sh, add);
-  n = block_fold<W>(n, sh, add);
+  fold_all(v, sh, [](int, double x, double y) { return x + y; });
+  const double kl = v[0], ce = v[1], n = v[2];
   if (threadIdx.x == 0) {
     const double l_kl = double(a.t) * double(a.t) / a.P * kl / a.n_seq;
     const double l_ce = n > 0. ? ce / n : 0.;
@@ -470,7 +512,10 @@ static hipError_t forward(const DistArgs& a, const DistSaved& sv, int n_parts, D
   hipLaunchKernelGGL((distill_part_kernel<T>), dim3(n_parts, rows), dim3(kDistThreads), 0, s, a, slots, parts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((distill_row_kernel<T>), dim3(rows), dim3(kDistThreads), 0, s, a, slots, parts, n_parts, sv);
+  if (a.K <= kMaxTop / 4)   // one wave
+    hipLaunchKernelGGL((distill_row_kernel<T, 64>), dim3(rows), dim3(64), 0, s, a, slots, parts, n_parts, sv);
+  else
+    hipLaunchKernelGGL((distill_row_kernel<T, 256>), dim3(rows), dim3(256), 0, s, a, slots, parts, n_parts, sv);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, s, a, sv);
