@@ -4,6 +4,8 @@
 // 60 us a row of instruction fetches where it takes 20.)
 #include "row_cut.hpp"
 
+#include <type_traits>
+
 namespace hdf {
 
 constexpr int kCutThreads = 1024;
@@ -50,11 +52,12 @@ struct CutShared {
     uint32_t i[W];
     float f[W];
   } red;
+  double run[kWave];
   uint64_t before, best;
   double sum;
   float floor, near, edge[2];
   uint32_t n, valid, listed;
-  int pick, last, top_bin, bins;
+  int pick, last, last_m, top_bin, bins, span;   // span: of the bins of all chunks
 };
 
 // Calls f(value, column) for every unmasked entry of vectors j0 .. j1-1 of the row and after(g) with
@@ -88,6 +91,18 @@ __device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
   each_entry<kCutThreads>(r, 0, r.vectors(), f, [](int) {});
 }
 
+// Exchanges of a bitonic sort within a wave, FROM, FROM / 2 .. 1 lanes apart, the greater key to the
+// lower lane where `down`.
+template <int FROM>
+__device__ __forceinline__ uint64_t wave_merge(uint64_t k, bool down) {
+  const uint64_t o = lane_xor<FROM>(k);
+  k = (o > k) == (((threadIdx.x & FROM) == 0) == down) ? o : k;
+  if constexpr (FROM > 1)
+    return wave_merge<FROM / 2>(k, down);
+  else
+    return k;
+}
+
 // The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
 // exchanges within 64 entries stay in a wave's registers.
 template <int NT>
@@ -97,25 +112,24 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   while (P < n) P *= 2;
   for (int i = n + int(threadIdx.x); i < P; i += NT) list[i] = 0;
   __syncthreads();
-  auto in_waves = [&](int from, int to) {   // sizes from .. to, their exchanges of up to 32 apart
-    for (int s = wid; s * 64 < P; s += NT / kWave) {
-      const int i = s * 64 + lane;
-      uint64_t k = list[i];
-      for (int size = from; size <= to; size *= 2)
-        for (int d = size / 2 < 32 ? size / 2 : 32; d > 0; d /= 2) {
-          const uint64_t o = __shfl_xor(k, d, kWave);
-          const bool greater = ((lane & d) == 0) == ((i & size) == 0);
-          k = (o > k) == greater ? o : k;
-        }
-      list[i] = k;
-    }
-    __syncthreads();
-  };
-  in_waves(2, 64);
+#pragma unroll 1
+  for (int s = wid; s * 64 < P; s += NT / kWave) {
+    uint64_t k = list[s * 64 + lane];
+    k = wave_merge<1>(k, (lane & 2) == 0);
+    k = wave_merge<2>(k, (lane & 4) == 0);
+    k = wave_merge<4>(k, (lane & 8) == 0);
+    k = wave_merge<8>(k, (lane & 16) == 0);
+    k = wave_merge<16>(k, (lane & 32) == 0);
+    k = wave_merge<32>(k, (s & 1) == 0);
+    list[s * 64 + lane] = k;
+  }
+  __syncthreads();
+#pragma unroll 1
   for (int size = 128; size <= P; size *= 2) {
+#pragma unroll 1
     for (int d = size / 2; d >= 64; d /= 2) {
       for (int t = threadIdx.x; t < P / 2; t += NT) {
-        const int i = 2 * d * (t / d) + t % d;
+        const int i = 2 * t - (t & (d - 1));
         const uint64_t a = list[i], b = list[i + d];
         if ((a < b) == ((i & size) == 0)) {
           list[i] = b;
@@ -124,7 +138,10 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
       }
       __syncthreads();
     }
-    in_waves(size, size);
+#pragma unroll 1
+    for (int s = wid; s * 64 < P; s += NT / kWave)
+      list[s * 64 + lane] = wave_merge<32>(list[s * 64 + lane], (s * 64 & size) == 0);
+    __syncthreads();
   }
 }
 
@@ -147,6 +164,17 @@ __device__ __forceinline__ uint32_t least_value_key(float m, F holds) {
     h = up < h ? uint32_t(up) : h;
   }
   return h;
+}
+
+// The same where an estimate is at hand: the 64 values around it first.
+template <typename F>
+__device__ __forceinline__ uint32_t least_value_key(float m, float near, F holds) {
+  const uint32_t h = f32_order_key(m), k = f32_order_key(near) - 32 + (threadIdx.x & 63);
+  const bool in = k >= h || (k > 0x007FFFFFu && holds(f32_from_order_key(k)));
+  const unsigned long long is = __ballot(in);
+  if (is != 0ull && (is & 1ull) == 0ull)
+    return read_lane(k, __ffsll(static_cast<long long>(is)) - 1);
+  return least_value_key(m, holds);
 }
 
 // First-level bin of a value below the row's greatest one: 64 bins a unit of (m - z) / T, so
@@ -353,35 +381,33 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
 }
 
 // First place, among 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes) `from` times the
-// sum of the first n_sum of them, or `target` where n_sum is 0; n where none does.  `sum` gets the
-// sum.
+// whole sum, or `target` where from is negative; n where none does.  `sum` gets the whole,
+// sh.last the last place with a weight.
 template <int NT, bool STRICT, typename Shared, typename F>
-__device__ __forceinline__ int reach(int n, int n_sum, double from, double target, double& sum,
-                                     Shared& sh, F w) {
-  int at = n;
+__device__ __forceinline__ int reach(int n, double from, double target, double& sum, Shared& sh, F w) {
+  const bool once = n <= NT;   // the sum and the place of one scan
 #pragma unroll 1
-  for (int pass = n_sum > 0 ? 0 : 1; pass < 2; ++pass) {   // the sum, then the place
-    if (threadIdx.x == 0) sh.pick = n;
-    const int m = pass == 0 ? n_sum : n;
+  for (int pass = from >= 0. && !once ? 0 : 1; pass < 2; ++pass) {   // the sum, then the place
+    if (threadIdx.x == 0) sh.pick = n, sh.last = 0;
     double before = 0.;
 #pragma unroll 1
-    for (int b = 0; b < m; b += NT) {
+    for (int b = 0; b < n; b += NT) {
       const int i = b + int(threadIdx.x);
-      const double v = i < m ? w(i) : 0.;
+      const double v = i < n ? w(i) : 0.;
       double all;
       const double run = before + block_scan<NT / kWave>(v, sh.red.d, all);
-      if (pass == 1)
-        note_first(i < m && (STRICT ? v > 0. && run > target : run >= target), i, &sh.pick);
       before += all;
+      if (from >= 0. && (once || pass == 0))   // 0 is reached by the first, not before
+        target = STRICT ? from * before : fmax(from * before, 1e-300);
+      if (pass == 1) {
+        note_first(i < n && (STRICT ? v > 0. && run > target : run >= target), i, &sh.pick);
+        note_last(v > 0., i, &sh.last);
+      }
     }
     __syncthreads();
-    at = sh.pick;
-    if (pass == 0) {
-      sum = before;
-      target = STRICT ? from * sum : fmax(from * sum, 1e-300);   // 0 is reached by the first, not before
-    }
-    __syncthreads();
+    sum = before;
   }
+  const int at = sh.pick;
   return at;
 }
 
@@ -424,7 +450,13 @@ __device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, Shar
     near = wave_fold(near, [](float u, float v) { return fminf(u, v); });
     top_bin = wave_fold(top_bin, [](int u, int v) { return max(u, v); });
     bins = wave_fold(bins, [](int u, int v) { return min(u, v); });
+    int span = 0;
+#pragma unroll 1
+    for (int c = lane; c < chunks; c += 64)
+      if (sh.part[c].bins > 0) span = max(span, top_bin - sh.part[c].top_bin + sh.part[c].bins);
+    span = wave_fold(span, [](int u, int v) { return max(u, v); });
     if (lane == 0) {
+      sh.span = span;
       sh.best = best;
       sh.valid = valid;
       sh.listed = listed;
@@ -437,36 +469,44 @@ __device__ __forceinline__ void join_chunks(const HeadStat* hs, int chunks, Shar
   __syncthreads();
 }
 
-// This thread's places of a row's lists, all in flight together; 0 past a chunk's list.
-template <int NT, typename Shared>
-__device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, const Shared& sh,
-                                            uint64_t mine[kListMax / NT]) {
+// This thread's places of a row's lists, all in flight together; only_listed() masks those past a
+// chunk's list, once the chunks' statistics are known.
+template <int NT>
+__device__ __forceinline__ void load_listed(const HeadArgs& h, int64_t at, uint64_t mine[kListMax / NT]) {
   const uint64_t* list = h.list + at * h.chunks * h.cap;
 #pragma unroll
   for (int q = 0; q < kListMax / NT; ++q) {
-    const int i = q * NT + int(threadIdx.x), c = i / h.cap;
-    const bool is = c < h.chunks && i - c * h.cap < sh.part[c].listed;
-    mine[q] = list[is ? i : 0];
+    const int i = q * NT + int(threadIdx.x);
+    mine[q] = list[i < h.chunks * h.cap ? i : 0];
+  }
+}
+template <int NT, typename Shared>
+__device__ __forceinline__ void only_listed(const HeadArgs& h, const Shared& sh, uint64_t mine[kListMax / NT]) {
+#pragma unroll
+  for (int q = 0; q < kListMax / NT; ++q) {
+    const uint32_t i = q * NT + threadIdx.x, c = i / uint32_t(h.cap);
+    const bool is = c < uint32_t(h.chunks) && int(i - c * h.cap) < sh.part[c < uint32_t(h.chunks) ? c : 0].listed;
     mine[q] = is ? mine[q] : 0ull;
   }
 }
-// The listed entries of value >= t and < over into the list; how many.
+// The listed entries of value >= t into the list; how many.
 template <int NT, typename Shared>
-__device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float t, float over,
-                                      Shared& sh) {
+__device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float t, Shared& sh) {
   __syncthreads();
   if (threadIdx.x == 0) sh.n = 0;
   __syncthreads();
+  uint32_t own = 0;
 #pragma unroll
-  for (int q = 0; q < kListMax / NT; ++q) {
-    const float z = entry_logit(mine[q]);
-    if (mine[q] != 0 && z >= t && (z < over || over == INFINITY))
-      sh.list[atomicAdd(&sh.n, 1u)] = mine[q];
-  }
+  for (int q = 0; q < kListMax / NT; ++q) own += mine[q] != 0 && entry_logit(mine[q]) >= t;
+  const uint32_t upto = wave_scan(own);
+  uint32_t at = 0;
+  if ((threadIdx.x & 63) == 63) at = atomicAdd(&sh.n, upto);
+  at = read_lane(at, 63) + upto - own;
+#pragma unroll
+  for (int q = 0; q < kListMax / NT; ++q)
+    if (mine[q] != 0 && entry_logit(mine[q]) >= t) sh.list[at++] = mine[q];
   __syncthreads();
-  const int n = int(sh.n);
-  __syncthreads();
-  return n;
+  return int(sh.n);
 }
 
 // The first K entries of a row and the log-sum-exp of the others.
@@ -483,20 +523,21 @@ row_top_kernel(CutArgs a, HeadArgs h) {
   const RowSettings s = settings_of<true>(a, row);
   auto add = [](double u, double v) { return u + v; };
   auto most64 = [](uint64_t u, uint64_t v) { return u > v ? u : v; };
+  uint64_t mine[kListMax / NT];
+  if constexpr (LISTS) load_listed<NT>(h, at, mine);
   join_chunks(h.stats + at * h.chunks, h.chunks, sh);
   const uint32_t valid = sh.valid;
   const int n = int(min(uint32_t(K), valid));
   int have = 0;
   bool done = false;
   if constexpr (LISTS) {
-    uint64_t mine[kListMax / NT];
-    load_listed<NT>(h, at, sh, mine);
+    only_listed<NT>(h, sh, mine);
     const float floor = sh.floor;
     // As far down as the chunks' shares go (every entry >= floor is listed), or to the floor.
     float t = fmaxf(floor, sh.near);
 #pragma unroll 1
     for (;;) {
-      have = gather<NT>(mine, t, INFINITY, sh);
+      have = gather<NT>(mine, t, sh);
       if (have >= n || t <= floor) break;
       t = floor;
     }
@@ -564,7 +605,7 @@ row_top_kernel(CutArgs a, HeadArgs h) {
 }
 
 // The row's entries with end <= z < over, up to kBorderMax of them, in sh.border: how many there are.
-// greater: how many lie above.
+// greater: how many lie above.  First their columns, then the values of all at once.
 template <int NT, typename T, typename Shared>
 __device__ __forceinline__ int border_entries(const LogitRow<T>& r, float end, float over,
                                               uint32_t& greater, Shared& sh) {
@@ -604,14 +645,19 @@ __device__ __forceinline__ int border_entries(const LogitRow<T>& r, float end, f
     while (bits != 0) {
       const int q = 32 - __ffs(bits);
       bits &= bits - 1;
-      const int c = r.column(b + q / N * NT + tid) + q % N;
-      if (at < uint32_t(kBorderMax)) sh.border[at] = entry_key(r.raw(c), c);
+      if (at < uint32_t(kBorderMax)) sh.border[at] = uint64_t(r.column(b + q / N * NT + tid) + q % N);
       ++at;
     }
   }
   greater = block_fold<NT / kWave>(lane == 0 ? up : 0u, sh.red.i,
                                    [](uint32_t u, uint32_t v) { return u + v; });
-  return int(sh.n);
+  const int n = int(sh.n);
+  for (int i = tid; i < min(n, kBorderMax); i += NT) {
+    const int c = int(sh.border[i]);
+    sh.border[i] = entry_key(r.raw(c), c);
+  }
+  __syncthreads();
+  return n;
 }
 
 // Key, among the n border entries, all of one bin, at which `above` and the running sum of their
@@ -621,7 +667,7 @@ template <int NT, typename Shared>
 __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi, double k16, double above,
                                                  double w_bin, double target, Shared& sh) {
   const int tid = threadIdx.x;
-  const double c5 = mass_coefficient();
+  const double c5 = mass_coefficient(kBits);
   uint64_t base = 0;
 #pragma unroll 1
   while (lo < hi) {
@@ -665,9 +711,88 @@ __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi
   return hi;
 }
 
+// The draw among a row's kept entries of vectors j0 .. j1-1 (a chunk's), up to 32 entries for each of
+// 512 threads: the entry at which `base` and the running sum pass the target, the last one where
+// rounding leaves none.  table: the weights of the bins' middles; from `end` down entries have none.
+// The chunk stays in registers; its runs of 64 vectors, a sum each, are gone through by every wave,
+// the run's entries by the wave that holds them.
+template <int NT, typename T, typename Shared>
+__device__ __forceinline__ int draw_binned(const LogitRow<T>& r, int j0, int j1, uint64_t cut, double k16,
+                                           int top_bin, float end, const double* table, double base,
+                                           double target, Shared& sh) {
+  constexpr int N = LogitRow<T>::N, G = 32 * kHeadThreads / N / NT, W = NT / kWave;
+  static_assert(G * W <= kWave);
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const float cz = entry_logit(cut);
+  const int cc = entry_column(cut);
+  float x[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[g][e] = -INFINITY;
+    if (j0 + g * NT + tid < j1) r.load_raw(j0 + g * NT + tid, x[g]);
+  }
+  const double c5 = mass_coefficient(1.);
+  auto weight = [&](float z, int c) __attribute__((always_inline)) {
+    int n;
+    const double p = bin_series<false>(fmaxf(z, end), k16, c5, n) * table[top_bin - n];
+    return z > end && (cut == 0 || z > cz || (z == cz && c <= cc)) ? p : 0.;
+  };
+  auto add = [](double u, double v) { return u + v; };
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int c = r.column(j0 + g * NT + tid);
+    double s = 0.;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += weight(x[g][e], c + e);
+    s = wave_fold(s, add);
+    if (lane == 0) sh.run[g * W + wid] = s;
+  }
+  __syncthreads();
+  const double v = lane < G * W ? sh.run[lane] : 0., run = base + wave_scan(v);
+  const unsigned long long any = __ballot(v > 0.), past = __ballot(v > 0. && run > target);
+  const int at = past != 0ull ? __ffsll(static_cast<long long>(past)) - 1
+                              : any != 0ull ? 63 - __clzll(static_cast<long long>(any)) : 0;
+  if (wid == at % W) {
+    const double before = read_lane(run, at) - read_lane(v, at);
+    float y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = x[0][e];
+#pragma unroll
+    for (int g = 1; g < G; ++g)
+      if (at / W == g) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = x[g][e];
+      }
+    const int c = r.column(j0 + at / W * NT + tid);
+    double w[N], own = 0.;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      w[e] = weight(y[e], c + e);
+      own += w[e];
+    }
+    const double upto = before + wave_scan(own);
+    const unsigned long long some = __ballot(own > 0.), over = __ballot(own > 0. && upto > target);
+    const int who = over != 0ull ? __ffsll(static_cast<long long>(over)) - 1
+                                 : 63 - __clzll(static_cast<long long>(some | 1ull));
+    if (lane == who) {
+      double sum = upto - own;
+      int tok = -1;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (w[e] > 0. && (tok < 0 || sum <= target)) tok = c + e;
+        sum += w[e];
+      }
+      sh.last = tok;
+    }
+  }
+  __syncthreads();
+  return sh.last;
+}
+
 // A row's truncation and draw.
 template <typename T, int NT, CutPhase PHASE>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, PHASE == kBorder ? 8 : 1)
 row_cut_kernel(CutArgs a, HeadArgs h) {
   constexpr bool LISTS = PHASE == kLists, BORDER = PHASE == kRest || PHASE == kBorder,
                  SEARCH = PHASE == kRest || PHASE == kSearch;
@@ -690,6 +815,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   auto leave = [&](int left) {
     if (tid == 0) note->left = left;
   };
+  uint64_t mine[LISTED];
+  if (LISTS && !s.greedy && !s.open) load_listed<NT>(h, at, mine);
   join_chunks(h.stats + at * h.chunks, h.chunks, sh);
   const uint64_t best = sh.best;
   const uint32_t valid = sh.valid, listed = sh.listed;
@@ -722,14 +849,15 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     if (a.tok != nullptr) a.tok[row] = tok;
   };
 
-  uint64_t mine[LISTED];
-  if constexpr (LISTS) load_listed<NT>(h, at, sh, mine);
+  if constexpr (LISTS) only_listed<NT>(h, sh, mine);
 
   // Least value of weight min_p, as the key of its last possible entry.
   uint64_t cut_m = 0;
   if (has_m && (LISTS || !binned)) {
     const double least = fmin(double(s.min_p), 1.);
-    const uint32_t k = least_value_key(m, [&](float z) { return entry_weight(z, m, s.c2) >= least; });
+    const uint32_t k = least_value_key(m, float(double(m) + log(least) / s.inv_t), [&](float z) {
+      return entry_weight(z, m, s.c2) >= least;
+    });
     cut_m = uint64_t(f32_order_key(f32_from_order_key(k) + 0.f)) << kColumnBits;
   } else if (has_m) {
     cut_m = note->cut_m;
@@ -751,60 +879,66 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     return is ? double(n) : 0.;
   };
   if constexpr (LISTS) {
-    if (binned) {
-      double v[PER], sum = 0.;
+    // P consecutive bins a thread, of sixteen loads in flight together.
+    auto join_masses = [&](auto bins_each) __attribute__((always_inline)) {
+      constexpr int P = decltype(bins_each)::value, AHEAD = 16 / P;
+      double v[P], sum = 0.;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) v[e] = 0.;
-      constexpr int AHEAD = 8 / (PER > 1 ? 2 : 1);   // chunks whose loads are in flight together
+      for (int e = 0; e < P; ++e) v[e] = 0.;
 #pragma unroll 1
       for (int c0 = 0; c0 < h.chunks; c0 += AHEAD) {
-        double x[AHEAD][PER];
+        double x[AHEAD][P];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-          for (int e = 0; e < PER; ++e) x[i][e] = mass_at(min(c0 + i, h.chunks - 1), PER * tid + e);
+          for (int e = 0; e < P; ++e) x[i][e] = mass_at(min(c0 + i, h.chunks - 1), P * tid + e);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-          for (int e = 0; e < PER; ++e) v[e] += c0 + i < h.chunks ? x[i][e] : 0.;
+          for (int e = 0; e < P; ++e) v[e] += c0 + i < h.chunks ? x[i][e] : 0.;
       }
+      if (tid == 0) sh.pick = kMassBins, sh.last = 0, sh.last_m = 0;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        v[e] *= bin_weight(PER * tid + e) * unit;
+      for (int e = 0; e < P; ++e) {
+        v[e] *= bin_weight(P * tid + e) * unit;
         sum += v[e];
       }
       const double run = block_scan<W>(sum, sh.red.d, whole_w);
-      if (tid == 0) sh.pick = kMassBins, sh.last = 0;
-      __syncthreads();
       const double target = has_p ? fmax(double(s.top_p) * whole_w, 1e-300) : INFINITY;
+      // min_p's bin: the last one with entries up to that of its least value.
+      const int bin_m = has_m ? min(top_bin - weight_bin(entry_logit(cut_m), k16), kMassBins - 1) : -1;
       double upto = run - sum;
-      int first = -1, last = -1;
+      int first = -1, last = -1, last_m = -1;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
+      for (int e = 0; e < P; ++e) {
+        const int b = P * tid + e;
         upto += v[e];
-        last = v[e] > 0. ? PER * tid + e : last;
-        first = first < 0 && v[e] > 0. && upto >= target ? PER * tid + e : first;
+        last = v[e] > 0. ? b : last;
+        last_m = v[e] > 0. && b <= bin_m ? b : last_m;
+        first = first < 0 && v[e] > 0. && upto >= target ? b : first;
       }
       note_first(first >= 0, first, &sh.pick);
       note_last(last >= 0, last, &sh.last);
+      if (has_m) note_last(last_m >= 0, last_m, &sh.last_m);
       __syncthreads();
       border = min(sh.pick, sh.last);
-      by_p = has_p;
-      if (has_m) {
-        const int b = min(top_bin - weight_bin(entry_logit(cut_m), k16), kMassBins - 1);
-        by_p = has_p && border <= b;
-        border = min(border, b);
-      }
+      by_p = has_p && (!has_m || border <= sh.last_m);
+      if (has_m) border = min(border, sh.last_m);
       upto = run - sum;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        if (PER * tid + e == border) sh.sum = upto;
+      for (int e = 0; e < P; ++e) {
+        if (P * tid + e == border) sh.sum = upto;
         upto += v[e];
       }
       __syncthreads();
       above = sh.sum;
-      __syncthreads();
-      if (PHASE == kLists && tid == 0)
+    };
+    if (binned) {
+      if (sh.span <= 2 * NT)
+        join_masses(std::integral_constant<int, 2>());
+      else
+        join_masses(std::integral_constant<int, PER>());
+      if (tid == 0)
         note->whole = whole_w, note->above = above, note->border = border, note->by_p = by_p,
         note->cut_m = cut_m;
     }
@@ -819,7 +953,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   auto find_edges = [&]() {
     if (wid < 2) {
       const int b = border - wid;
-      const float z = b < 0 ? INFINITY : f32_from_order_key(least_value_key(m, [&](float z) {
+      const float near = float((double(top_bin - b) - 0.5) * (double(s.t) * kLog16));
+      const float z = b < 0 ? INFINITY : f32_from_order_key(least_value_key(m, near, [&](float z) {
         return double(z) * k16 > double(top_bin) - 2048. && weight_bin(z, k16) >= top_bin - b;
       }));   // (far values have no bin)
       if (lane == 0) sh.edge[wid] = z;
@@ -850,26 +985,28 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   uint64_t cut = 0;
   if constexpr (LISTS) {
     if (binned && !s.open) find_edges();
-    // The entries that the cut lies among, if they are listed, sorted.
+    // The kept entries and those that the cut lies among, if they are listed, sorted.  Under a cut by
+    // weight only a few: of more, whose masses the histograms hold, one chunk is read instead.
     bool from_lists = binned ? !s.open && end >= floor : has_k || whole;
+    int k = 0;
 #pragma unroll 1
-    while (from_lists && cut == 0) {
+    while (from_lists && k == 0) {
       float t = binned ? end : has_k ? fmaxf(floor, sh.near) : floor;
       int n;
 #pragma unroll 1
       for (;;) {
-        n = gather<NT>(mine, t, over, sh);
+        n = gather<NT>(mine, t, sh);
         if (!has_k || n >= s.top_k || t <= floor) break;
         t = floor;
       }
-      if (has_k && n < s.top_k) break;
-      if (n > 0) sort_list<NT>(sh.list, n);
+      if ((has_k && n < s.top_k) || (binned && n > kInOrder)) break;
+      sort_list<NT>(sh.list, n);
       for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
       __syncthreads();
-      int k = has_k ? s.top_k : n;
+      k = has_k ? s.top_k : n;
       if (binned ? by_p : has_p) {
         double sum;
-        const int p = reach<NT, false>(k, binned ? 0 : k, double(s.top_p), target_p - above, sum, sh,
+        const int p = reach<NT, false>(k, binned ? -1. : double(s.top_p), target_p, sum, sh,
                                        [&](int i) { return sh.weight[i]; });
         k = min(k, p + 1);
       }
@@ -878,54 +1015,20 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         for (int i = tid; i < k; i += NT) c += sh.list[i] >= cut_m;
         k = int(block_fold<W>(c, sh.red.i, add));
       }
-      if (k > 0)
-        cut = sh.list[k - 1];
-      else
-        bin_before();
+      if (k == 0) bin_before();
     }
-    if (cut != 0) {
-      // All kept entries are listed: in token order, columns with their places as keys, the weights
-      // beside them.
-      uint32_t many = 0;
-      uint64_t low = kKeyTop;
-#pragma unroll
-      for (int q = 0; q < LISTED; ++q)
-        if (mine[q] != 0 && mine[q] >= cut) {
-          low = least64(low, mine[q]);
-          ++many;
-        }
-      many = block_fold<W>(many, sh.red.i, add);
-      if (!binned || many <= uint32_t(kInOrder)) {
-        low = block_fold<W>(low, sh.red.u, least64);
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < LISTED; ++q)
-          if (mine[q] != 0 && mine[q] >= cut) {
-            const uint32_t i = atomicAdd(&sh.n, 1u);
-            sh.list[i] = ((mine[q] & kColumnMask) << 12) | uint64_t(i);
-            sh.weight[i] = double(entry_logit(mine[q]));
-          }
-        __syncthreads();
-        const int k = int(many);
-        for (int i = tid; i < k; i += NT) sh.weight[i] = entry_weight(float(sh.weight[i]), m, s.c2);
-        sort_list<NT>(sh.list, k);
-        double mass;
-        int i = reach<NT, true>(k, k, u, 0., mass, sh,
-                                [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
-        if (i == k) {   // the last with a weight
-          if (tid == 0) sh.last = 0;
-          __syncthreads();
-          for (int q0 = 0; q0 < k; q0 += NT) {
-            const int q = q0 + tid;
-            note_last(q < k && sh.weight[sh.list[q < k ? q : 0] & 4095u] > 0., q, &sh.last);
-          }
-          __syncthreads();
-          i = sh.last;
-        }
-        write(many, low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
-        return;
-      }
+    if (k > 0) {
+      // In token order: columns with the weights' places as keys.
+      const uint64_t low = sh.list[k - 1];
+      __syncthreads();
+      for (int i = tid; i < k; i += NT) sh.list[i] = ((sh.list[i] & kColumnMask) << 12) | uint64_t(i);
+      __syncthreads();
+      sort_list<NT>(sh.list, k);
+      double mass;
+      int i = reach<NT, true>(k, u, 0., mass, sh, [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
+      if (i == k) i = sh.last;   // rounding left none: the last with a weight
+      write(uint32_t(k), low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
+      return;
     }
     if (tid == 0) {
       note->border = border, note->by_p = by_p, note->end = end, note->over = over;
@@ -966,7 +1069,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         if (s.open) border = kMassBins;
         for (int c = tid; c < h.chunks; c += NT) sh.chunk_n[c] = 0;
         __syncthreads();
-        const double c5 = mass_coefficient();
+        const double c5 = mass_coefficient(kBits);
         for (int i = tid; i < n; i += NT) {
           const uint64_t k = sh.border[i];
           const int j = (entry_column(k) + r.shift) / LogitRow<T>::N;
@@ -976,11 +1079,22 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
                       static_cast<unsigned long long>(weight_in_bin(entry_logit(k), k16, c5, b)));
         }
         __syncthreads();
-        const double w_last = n > 0 ? bin_weight(border) * unit : 0.;
+        // Weights of the bins' middles, relative to the greatest entry's, over the border's entries.
+        double* table = reinterpret_cast<double*>(sh.border);
+        for (int b = tid; b < kMassBins; b += NT)
+          table[b] = b < kKeptBins ? bin_weight(b) * (unit / kMassUnit) : 0.;
+        __syncthreads();
 #pragma unroll 1
         for (int c = wid; c < h.chunks; c += W) {
-          double w = lane == 0 ? double(sh.chunk_n[c]) * w_last : 0.;
-          for (int b = lane; b < border; b += 64) w += mass_at(c, b) * bin_weight(b) * unit;
+          double w = lane == 0 && n > 0 ? double(sh.chunk_n[c]) * (table[border] * kMassUnit) : 0.;
+#pragma unroll 1
+          for (int b0 = lane; b0 < border; b0 += 256) {
+            double v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = b0 + 64 * i < border ? mass_at(c, b0 + 64 * i) : 0.;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w += v[i] * (table[min(b0 + 64 * i, kMassBins - 1)] * kMassUnit);
+          }
           w = wave_fold(w, add);
           if (lane == 0) sh.chunk[c] = w;
         }
@@ -998,14 +1112,11 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           note_last(w > 0., tid, &sh.last);
           __syncthreads();
           const int c = min(sh.pick, sh.last);
-          __syncthreads();
           if (tid == c) sh.sum = run - w;
           __syncthreads();
-          const double base = sh.sum;
           const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
-          double grun, gmine;
-          kept_masses<NT, false>(r, j0, j1, cut, m, s.c2, sh, grun, gmine);
-          tok = draw_entry<NT>(r, j0, j1, cut, m, s.c2, base, target, grun, gmine, sh);
+          const float far = m - float(double(s.t) * kLog16) * float(kKeptBins + 4);
+          tok = draw_binned<NT>(r, j0, j1, cut, k16, top_bin, far, table, sh.sum, target, sh);
         }
         write(greater, cut, mass, tok);
         return;

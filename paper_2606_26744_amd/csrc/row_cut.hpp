@@ -92,29 +92,33 @@ constexpr double kRound = 6755399441055744.;
 __device__ __forceinline__ int weight_bin(float z, double k16) {
   return int(uint32_t(__builtin_bit_cast(uint64_t, fma_k(double(z), k16, kRound))));
 }
-// Bin and the weight within it as a multiple of 2^-48: the series of 2^(g / 16), |g| <= 1/2, to the
-// sixth power, with g^6 replaced by 3/8 g^4 - 9/256 g^2 + 1/2048, from which it differs by
-// T_6(2g) / 2048: 5e-15 of the weight at the most, and of alternating sign.  All coefficients are
-// times 2^(48 - 1074), so that the result is subnormal and its bits are the integer.  c5:
-// mass_coefficient(), kept in registers by the caller.
+// Bin and the weight within it: the series of 2^(g / 16), |g| <= 1/2, to the sixth power, with g^6
+// replaced by 3/8 g^4 - 9/256 g^2 + 1/2048, from which it differs by T_6(2g) / 2048: 5e-15 of the
+// weight at the most, and of alternating sign.  SCALE 2^(48 - 1074) makes the result subnormal and
+// its bits the weight as a multiple of 2^-48.  c5: mass_coefficient(), kept in registers by the
+// caller.
 constexpr double kBits = 0x1p-1026;
 constexpr double kLog16 = 0.69314718055994530942 / 16., kLog16_2 = kLog16 * kLog16;
 constexpr double kMass6 = kLog16_2 * kLog16_2 * kLog16_2 / 720.;
-__device__ __forceinline__ double mass_coefficient() {
-  double c = kLog16_2 * kLog16_2 * kLog16 / 120. * kBits;
+__device__ __forceinline__ double mass_coefficient(double scale) {
+  double c = kLog16_2 * kLog16_2 * kLog16 / 120. * scale;
   asm volatile("" : "+v"(c));   // not copied anew for every entry
   return c;
 }
-__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, double c5, int& n) {
+template <bool BITS>
+__device__ __forceinline__ double bin_series(float z, double k16, double c5, int& n) {
+  constexpr double S = BITS ? kBits : 1.;
   const double t = fma_k(double(z), k16, kRound);
   n = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
   const double g = fma(double(z), k16, kRound - t);
-  double p = fma_k(c5, g, (kLog16_2 * kLog16_2 / 24. + kMass6 * 0.375) * kBits);
-  p = fma_k(p, g, kLog16_2 * kLog16 / 6. * kBits);
-  p = fma_k(p, g, (kLog16_2 / 2. - kMass6 * 0.03515625) * kBits);
-  p = fma_k(p, g, kLog16 * kBits);
-  p = fma_k(p, g, (1. + kMass6 / 2048.) * kBits);
-  return __builtin_bit_cast(uint64_t, p);
+  double p = fma_k(c5, g, (kLog16_2 * kLog16_2 / 24. + kMass6 * 0.375) * S);
+  p = fma_k(p, g, kLog16_2 * kLog16 / 6. * S);
+  p = fma_k(p, g, (kLog16_2 / 2. - kMass6 * 0.03515625) * S);
+  p = fma_k(p, g, kLog16 * S);
+  return fma_k(p, g, (1. + kMass6 / 2048.) * S);
+}
+__device__ __forceinline__ uint64_t weight_in_bin(float z, double k16, double c5, int& n) {
+  return __builtin_bit_cast(uint64_t, bin_series<true>(z, k16, c5, n));
 }
 
 hipError_t launch_row_head(bool bf16, bool top, bool small, const CutArgs& a, const HeadArgs& h, hipStream_t s);

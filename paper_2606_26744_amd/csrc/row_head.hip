@@ -182,7 +182,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     if (fabs(double(m)) * k16 < 8e6 && m - step * float(kMassBins - 1) >= kLeast) {
       for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
       __syncthreads();
-      const double c5 = mass_coefficient();
+      const double c5 = mass_coefficient(kBits);
       const int top_bin = weight_bin(m, k16);
       st.top_bin = top_bin;
 #pragma unroll

@@ -25,9 +25,10 @@ struct LogitRow {
   __device__ __forceinline__ bool inside(int j, int n) const {
     return column(j) >= 0 && column(j + n) <= V;
   }
-  // Vector j, which lies within the row.
-  __device__ __forceinline__ void load_inside(int j, float x[N]) const {
-    const u32x4 v = ld16(p + column(j));
+  // Vector j, which lies within the row: its bits, and as fp32.
+  __device__ __forceinline__ u32x4 bits_inside(int j) const { return ld16(p + column(j)); }
+  __device__ __forceinline__ void load_inside(int j, float x[N]) const { unpack(bits_inside(j), x); }
+  static __device__ __forceinline__ void unpack(u32x4 v, float x[N]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (sizeof(T) == 2) {
@@ -149,6 +150,27 @@ __device__ __forceinline__ X read_lane(X v, int lane) {
   for (int i = 0; i < D; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
   __builtin_memcpy(&v, w, sizeof(X));
   return v;
+}
+
+// The value of the lane D apart (D a power of two): moves between lanes, no shared memory.
+template <int D>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
+  if constexpr (D == 1) return dpp<0xB1, 0xf>(v);
+  if constexpr (D == 2) return dpp<0x4E, 0xf>(v);
+  if constexpr (D == 4) return dpp<0x1B, 0xf>(dpp<0x141, 0xf>(v));   // 7 apart, then 3
+  if constexpr (D == 8) return dpp<0x128, 0xf>(v);                   // turned by 8 of 16
+  if constexpr (D >= 16) {   // rows, or halves, change places between two copies
+    uint32_t w[2];
+    __builtin_memcpy(w, &v, 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const auto p = D == 16 ? __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false)
+                             : __builtin_amdgcn_permlane32_swap(w[i], w[i], false, false);
+      w[i] = (threadIdx.x & D) != 0 ? p[0] : p[1];
+    }
+    __builtin_memcpy(&v, w, 8);
+    return v;
+  }
 }
 
 // All lanes' values under f (commutative, associative but for rounding), the same to every lane:
