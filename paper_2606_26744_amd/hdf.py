@@ -412,23 +412,28 @@ class Truncation(NamedTuple):
     lse: torch.Tensor         # [rows] fp64
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _place(t: torch.Tensor, stream):
     """Makes the tensor's device, and the given stream, current: outputs and workspaces are then
     allocated for the stream that uses them, and nothing is launched on another device."""
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0:
         raise ValueError("libhdf takes device tensors")
     if stream is not None:
         if stream.device != t.device:
             raise ValueError("the stream belongs to another device than the tensors")
         return torch.cuda.stream(stream)
-    if t.device.index != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         return torch.cuda.device(t.device)
-    return contextlib.nullcontext()
+    return _HERE
 
 
 def _same_device(t: torch.Tensor, *others):
+    device = t.get_device()
     for o in others:
-        if o is not None and (not o.is_cuda or o.device != t.device):
+        if o is not None and o.get_device() != device:
             raise ValueError("all tensors must be on one device")
 
 
@@ -450,21 +455,23 @@ def _scratch(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch
     return ws
 
 
-def _truncation_params(like, n, rows_per_seq, temperature, top_k, top_p, min_p):
-    """The C struct of settings that are numbers or tensors of one entry a sequence."""
-    p = TruncationParams(1.0, 0, 1.0, 0.0, None, None, None, None, rows_per_seq)
-    for value, one, many, dtype in (
-            (temperature, "temperature", "temperatures", torch.float32),
-            (top_k, "top_k", "top_ks", torch.int32), (top_p, "top_p", "top_ps", torch.float32),
-            (min_p, "min_p", "min_ps", torch.float32)):
-        if torch.is_tensor(value):
-            _typed(value, dtype, n, one)
+_SETTINGS = (("temperature", "temperatures", torch.float32), ("top_k", "top_ks", torch.int32),
+             ("top_p", "top_ps", torch.float32), ("min_p", "min_ps", torch.float32))
+
+
+def _truncation_params(like, n, rows_per_seq, *values):
+    """The C struct of settings (in _SETTINGS' order) that are numbers or tensors of one entry a
+    sequence."""
+    one, many = [1.0, 0, 1.0, 0.0], [None] * 4
+    for i, value in enumerate(values):
+        if isinstance(value, torch.Tensor):
+            _typed(value, _SETTINGS[i][2], n, _SETTINGS[i][0])
             _dev(value)
             _same_device(like, value)
-            setattr(p, many, value.data_ptr())
+            many[i] = value.data_ptr()
         elif value is not None:
-            setattr(p, one, value)
-    return p
+            one[i] = value
+    return TruncationParams(*one, *many, rows_per_seq)
 
 
 def sample_truncated(logits: torch.Tensor, uniforms: Optional[torch.Tensor] = None, *,
@@ -482,23 +489,25 @@ def sample_truncated(logits: torch.Tensor, uniforms: Optional[torch.Tensor] = No
     p = _truncation_params(logits, -(-rows // rows_per_seq), rows_per_seq, temperature, top_k,
                            top_p, min_p)
     with _place(logits, stream):
+        _typed(uniforms, torch.float32, rows, "uniforms")
+        _dev(uniforms)
+        _same_device(logits, uniforms)
         if out is None:
-            i32 = dict(dtype=torch.int32, device=logits.device)
-            tok = torch.empty(rows, **i32) if uniforms is not None else None
-            cut = Truncation(torch.empty(rows, **i32),
-                             torch.empty(rows, dtype=torch.float32, device=logits.device),
-                             torch.empty(rows, **i32),
-                             torch.empty(rows, dtype=torch.float64, device=logits.device))
+            device, i32 = logits.device, torch.int32
+            tok = torch.empty(rows, dtype=i32, device=device) if uniforms is not None else None
+            cut = Truncation(torch.empty(rows, dtype=i32, device=device),
+                             torch.empty(rows, dtype=torch.float32, device=device),
+                             torch.empty(rows, dtype=i32, device=device),
+                             torch.empty(rows, dtype=torch.float64, device=device))
         else:
             tok, cut = out[0], Truncation(*out[1])
             tok = tok if uniforms is not None else None
-        _typed(uniforms, torch.float32, rows, "uniforms")
-        _typed(tok, torch.int32, rows, "tokens")
-        for t, dtype, what in zip(cut, (torch.int32, torch.float32, torch.int32, torch.float64),
-                                  Truncation._fields):
-            _typed(t, dtype, rows, what)
-        _dev(uniforms, tok, *cut)
-        _same_device(logits, uniforms, tok, *cut)
+            _typed(tok, torch.int32, rows, "tokens")
+            for t, dtype, what in zip(cut, (torch.int32, torch.float32, torch.int32, torch.float64),
+                                      Truncation._fields):
+                _typed(t, dtype, rows, what)
+            _dev(tok, *cut)
+            _same_device(logits, tok, *cut)
         dt = _dt(logits)
         ws = _scratch(ws, int(lib().hdf_sample_truncated_workspace(rows, V, dt)), logits)
         _check(lib().hdf_sample_truncated(
