@@ -579,12 +579,13 @@ def top_logits(logits: torch.Tensor, K: int, *, temperature: float = 1.0, want_r
             out = (torch.empty((rows, max(K, 0)), dtype=torch.int32, device=dev),
                    torch.empty((rows, max(K, 0)), dtype=torch.float32, device=dev),
                    torch.empty(rows, dtype=torch.float32, device=dev) if want_rest else None)
+        else:
+            _typed(out[0], torch.int32, rows * K, "ids")
+            _typed(out[1], torch.float32, rows * K, "values")
+            _typed(out[2], torch.float32, rows, "rest")
+            _dev(*out)
+            _same_device(logits, *out)
         ids, values, rest = out
-        _typed(ids, torch.int32, rows * K, "ids")
-        _typed(values, torch.float32, rows * K, "values")
-        _typed(rest, torch.float32, rows, "rest")
-        _dev(ids, values, rest)
-        _same_device(logits, ids, values, rest)
         dt = _dt(logits)
         ws = _scratch(ws, int(lib().hdf_top_logits_workspace(rows, V, K, dt)), logits)
         _check(lib().hdf_top_logits(_ptr(logits), rows, V, ld, dt, K, float(temperature), _ptr(ids),
@@ -623,6 +624,8 @@ def distill_forward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
     _typed(teacher_rest, torch.float32, n_seq * P, "teacher_rest")
     with _place(student_logits, stream):
         dt = _dt(student_logits)
+        _dev(teacher_logits, teacher_rest)
+        _same_device(student_logits, teacher_logits, teacher_rest)
         need = int(lib().hdf_distill_saved_bytes(n_seq, B, P, K))
         if out is None:
             f32 = dict(dtype=torch.float32, device=student_logits.device)
@@ -630,13 +633,14 @@ def distill_forward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
                    torch.empty((n_seq, B - 1), **f32) if labels is not None else None,
                    torch.zeros(3, **f32) if n_seq == 0 else torch.empty(3, **f32),
                    torch.empty(max(need, 1), dtype=torch.uint8, device=student_logits.device))
+        else:
+            _typed(out[0], torch.float32, n_seq * P, "kl")
+            _typed(out[1], torch.float32, n_seq * (B - 1), "ce")
+            _typed(out[2], torch.float32, 3, "loss")
+            _typed(out[3], torch.uint8, need, "saved")
+            _dev(*out)
+            _same_device(student_logits, *out)
         kl, ce, loss, saved = out
-        _typed(kl, torch.float32, n_seq * P, "kl")
-        _typed(ce, torch.float32, n_seq * (B - 1), "ce")
-        _typed(loss, torch.float32, 3, "loss")
-        _typed(saved, torch.uint8, need, "saved")
-        _dev(teacher_logits, teacher_rest, kl, ce, loss, saved)
-        _same_device(student_logits, teacher_logits, teacher_rest, kl, ce, loss, saved)
         ws = _scratch(ws, int(lib().hdf_distill_workspace(n_seq, B, V, dt)), student_logits)
         _check(lib().hdf_distill_forward(
             _ptr(student_logits), ld, dt, V, n_seq, B, P, _ptr(teacher_ids), _ptr(teacher_logits),
@@ -662,14 +666,14 @@ def distill_backward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
     _typed(grad_ce, torch.float32, n_seq * (B - 1), "grad_ce")
     _typed(saved, torch.uint8, int(lib().hdf_distill_saved_bytes(n_seq, B, P, K)), "saved")
     with _place(student_logits, stream):
+        _dev(saved, grad_loss, grad_kl, grad_ce)
+        _same_device(student_logits, saved, grad_loss, grad_kl, grad_ce, d_logits)
         if d_logits is None:
             d_logits = torch.empty((n_seq * B, V), dtype=student_logits.dtype,
                                    device=student_logits.device)
         d_rows, d_V, ldd = _rows_of(d_logits, "d_logits")
         if (d_rows, d_V, d_logits.dtype) != (n_seq * B, V, student_logits.dtype):
             raise ValueError("d_logits must have the shape and the type of student_logits")
-        _dev(saved, grad_loss, grad_kl, grad_ce)
-        _same_device(student_logits, saved, grad_loss, grad_kl, grad_ce, d_logits)
         _check(lib().hdf_distill_backward(
             _ptr(student_logits), ld, _dt(student_logits), V, n_seq, B, P, _ptr(teacher_ids), K,
             _ptr(labels), float(temperature), float(alpha), _ptr(saved), _ptr(grad_loss),
