@@ -35,7 +35,7 @@ def slot_kl(z, ids, values, rest=None, T=1.0):
     if p is None:
         return 0.0, np.zeros_like(z)
     q = _softmax(z / T)
-    lq = z / T - z.max() / T - np.log(np.exp((z - z.max()) / T).sum())
+    lq = (z - z.max()) / T - np.log(np.exp((z - z.max()) / T).sum())
     inside = np.zeros(z.shape[0], dtype=bool)
     inside[toks] = True
     kl = sum(pi * (np.log(pi) - lq[t]) for t, pi in zip(toks, p) if pi > 0)
@@ -61,7 +61,7 @@ def slot_ce(z, label):
     q = _softmax(z)
     g = q.copy()
     g[label] -= 1
-    return float(z.max() + np.log(np.exp(z - z.max()).sum()) - z[label]), g
+    return float((z.max() - z[label]) + np.log(np.exp(z - z.max()).sum())), g
 
 
 def distill(student, ids, values, rest, labels, B, T, alpha, g_loss=(0, 0, 0), g_kl=None, g_ce=None):

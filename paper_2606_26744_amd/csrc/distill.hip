@@ -332,7 +332,7 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
   if (a.labels != nullptr) {
     double ce = 0.;
     if (label >= 0 && label < a.V) {
-      ce = label_z == -INFINITY ? INFINITY : ref + log(s1) - label_z;
+      ce = label_z == -INFINITY ? INFINITY : (ref - label_z) + log(s1);
       row.ce = 1;
     }
     a.ce[s * (a.B - 1) + k - 1] = float(ce);

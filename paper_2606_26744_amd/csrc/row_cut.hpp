@@ -80,7 +80,8 @@ __device__ __forceinline__ RowSettings settings_of(const CutArgs& a, int64_t row
   s.top_p = TOP ? 1.f : a.ps != nullptr ? a.ps[i] : a.p;
   s.min_p = TOP ? 0.f : a.mps != nullptr ? a.mps[i] : a.mp;
   if (!TOP && s.top_k >= a.V) s.top_k = 0;
-  s.binned = !s.greedy && s.top_k <= 0;
+  // (A min_p below the bins' 61 octaves goes by the search.)
+  s.binned = !s.greedy && s.top_k <= 0 && !(s.min_p > 0.f && s.min_p < 1e-18f);
   s.open = s.binned && !(s.top_p < 1.f) && !(s.min_p > 0.f);
   s.inv_t = s.greedy ? 1. : 1. / double(s.t);
   s.c2 = 1.4426950408889634074 * s.inv_t;

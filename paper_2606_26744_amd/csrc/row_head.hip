@@ -179,7 +179,7 @@ row_head_kernel(CutArgs a, HeadArgs h) {
     // cheaper than leaving them out.  (A bin is at least half a unit in the last place of m wide.)
     const float step = float(double(s.t) * kLog16);   // a bin's width
     const float end = m - step * float(kKeptBins + 4 + (lane & 31));
-    if (fabs(double(m)) * k16 < 8e6 && m - step * float(kMassBins - 1) >= kLeast) {
+    if (fabs(double(m)) * k16 < 8e6 && step > 1e-37f && m - step * float(kMassBins - 1) >= kLeast) {
       for (int b = tid; b < kMassBins; b += kHeadThreads) mass[b] = 0;
       __syncthreads();
       const double c5 = mass_coefficient(kBits);

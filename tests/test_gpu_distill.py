@@ -199,6 +199,29 @@ def test_masked_students():
     _check(c, B)
 
 
+@pytest.mark.parametrize("T", [1.0, 0.5])
+def test_students_far_from_zero(T):
+    """Rows of the type's lowest value throughout, and rows whose greatest logit is so large that its
+    product with log2(e) / T rounds to no small part of an octave: differences of logits are what
+    counts."""
+    n, B, P, K, V = 1, 6, 5, 12, 3001
+    c = _case(n, B, P, K, V, 14, T=T)
+    z = c["z"]
+    z[1] = torch.finfo(torch.float32).min
+    z[2] += 2.0 ** 19
+    z[3] = (z[3] - 4) * 2.0 ** 20 * T
+    z[4] -= 2.0 ** 17
+    z[5] = 1e30
+    c["ids"][0, 2] = z[3].topk(K).indices.int()   # the others are beyond any sum
+    c["rest"][0, 2] = -np.inf
+    _check(c, B, T)
+
+
+@pytest.mark.parametrize("K", [63, 64, 65, 255, 256, 257, 700])
+def test_list_lengths(K):
+    _check(_case(2, 3, 2, K, 2003, K), 3)
+
+
 def test_student_that_gives_a_listed_token_no_mass():
     c = _case(1, 3, 2, 5, 400, 3)
     c["z"][1, c["ids"][0, 0, 2].long()] = -np.inf

@@ -203,6 +203,45 @@ def test_many_rows():
         assert float(rest[r]) == s or abs(float(rest[r]) - s) <= 2e-7 * max(1.0, abs(s)), r
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [3, 259])
+def test_borders_of_many_entries(n, dtype):
+    """A nucleus' border falls among a few, some thousand (more than a row's lists hold) and more
+    entries than are held at once, of distinct values and of ties, in few rows and in many."""
+    V = 60013
+    z = _logits(n, V, 51, dtype, "flat")
+    z[1] = (z[1] * 4).round() / 4
+    rows = (0, 1, n - 1)
+    for kw in (dict(temperature=1.5, top_p=0.95), dict(temperature=3.0, top_p=0.5),
+               dict(temperature=12.0, top_p=0.7), dict(temperature=3.0, min_p=0.4),
+               dict(temperature=3.0, top_p=0.6, min_p=0.37), dict(top_p=0.999, min_p=1e-6)):
+        _check_draws(z, _u(n, 12), rows=rows, **kw)
+
+
+@pytest.mark.parametrize("n", [2, 258])
+def test_weights_far_below_the_greatest(n):
+    """Entries many octaves below a row's greatest: kept by a tiny min_p, weightless in a draw;
+    temperatures so low that any other entry weighs nothing; a greatest value of zero, of the least
+    and of the greatest magnitude."""
+    V = 9001
+    z = _logits(n, V, 61, kind="flat")
+    rows = (0, 1, n - 1)
+    for kw in (dict(temperature=0.05, min_p=1e-20), dict(temperature=0.05, min_p=1e-17),
+               dict(temperature=0.05, top_p=0.999999), dict(temperature=0.02),
+               dict(temperature=0.03, min_p=1e-38, top_p=0.9)):
+        _check_draws(z, _u(n, 3), rows=rows, **kw)
+    top = z - z.max(1, keepdim=True).values
+    for T in (1e-42, 1e-38, 1e-30):
+        for kw in (dict(top_p=0.9), dict(), dict(min_p=0.5), dict(top_k=3)):
+            _check_draws(top, _u(n, 4), rows=rows, temperature=T, **kw)
+    for scale in (1e-38, 1e30):
+        for kw in (dict(top_p=0.9), dict(), dict(min_p=0.5)):
+            _check_draws(z * scale, _u(n, 5), rows=rows, temperature=scale, **kw)
+    inf = torch.full((n,), float("inf"), device=DEV)
+    _, cut = hdf.sample_truncated(z, _u(n, 6), temperature=inf, min_p=1.0)
+    assert (cut.kept == V).all()   # all weigh the same
+
+
 def test_rows_in_several_groups_of_launches():
     """So many long rows that they run in turns over one workspace."""
     V, n = 1 << 20, 131
