@@ -103,6 +103,17 @@ __device__ __forceinline__ uint64_t wave_merge(uint64_t k, bool down) {
     return k;
 }
 
+// The wave's keys from the greatest down.
+__device__ __forceinline__ uint64_t wave_sort(uint64_t k, bool down = true) {
+  const uint32_t lane = threadIdx.x & 63;
+  k = wave_merge<1>(k, (lane & 2) == 0);
+  k = wave_merge<2>(k, (lane & 4) == 0);
+  k = wave_merge<4>(k, (lane & 8) == 0);
+  k = wave_merge<8>(k, (lane & 16) == 0);
+  k = wave_merge<16>(k, (lane & 32) == 0);
+  return wave_merge<32>(k, down);
+}
+
 // The list's first n entries (n <= kListMax) from the greatest key down: a bitonic sort whose
 // exchanges within 64 entries stay in a wave's registers.
 template <int NT>
@@ -113,16 +124,8 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   for (int i = n + int(threadIdx.x); i < P; i += NT) list[i] = 0;
   __syncthreads();
 #pragma unroll 1
-  for (int s = wid; s * 64 < P; s += NT / kWave) {
-    uint64_t k = list[s * 64 + lane];
-    k = wave_merge<1>(k, (lane & 2) == 0);
-    k = wave_merge<2>(k, (lane & 4) == 0);
-    k = wave_merge<4>(k, (lane & 8) == 0);
-    k = wave_merge<8>(k, (lane & 16) == 0);
-    k = wave_merge<16>(k, (lane & 32) == 0);
-    k = wave_merge<32>(k, (s & 1) == 0);
-    list[s * 64 + lane] = k;
-  }
+  for (int s = wid; s * 64 < P; s += NT / kWave)
+    list[s * 64 + lane] = wave_sort(list[s * 64 + lane], (s & 1) == 0);
   __syncthreads();
 #pragma unroll 1
   for (int size = 128; size <= P; size *= 2) {
@@ -691,10 +694,31 @@ __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi
     note_last(own > 0, tid, &sh.last);
     __syncthreads();
     const int at = min(sh.pick, sh.last);
+    const bool few = sh.fine[at] < (uint64_t(62) << 48);   // fewer than 64: they weigh 0.978 at least
     if (tid == at) sh.before = upto - own;
     hi -= uint64_t(at) << shift;
     const uint64_t least = hi - ((uint64_t(1) << shift) - 1);
     lo = least > lo ? least : lo;
+    if (few) {   // every wave sorts and sums them for itself
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      base = sh.before;
+      for (int i = tid; i < n; i += NT) {
+        const uint64_t k = sh.border[i];
+        if (k >= lo && k <= hi) sh.fine[atomicAdd(&sh.n, 1u)] = k;
+      }
+      __syncthreads();
+      const int lane = tid & 63;
+      uint64_t k = wave_sort(lane < int(sh.n) ? sh.fine[lane] : 0ull);
+      int bin;
+      const uint64_t w = k != 0 ? weight_in_bin(entry_logit(k), k16, c5, bin) : 0ull;
+      const unsigned long long some = __ballot(k != 0);
+      const unsigned long long past = __ballot(k != 0 && above + double(base + wave_scan(w)) * w_bin >= target);
+      k = read_lane(k, past != 0ull ? __ffsll(static_cast<long long>(past)) - 1
+                                    : 63 - __clzll(static_cast<long long>(some | 1ull)));
+      __syncthreads();
+      return k;
+    }
     // The range that its entries take.
     uint64_t first = 0, last = kKeyTop;
     for (int i = tid; i < n; i += NT) {
