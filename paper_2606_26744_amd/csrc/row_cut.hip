@@ -8,10 +8,7 @@
 
 namespace hdf {
 
-constexpr int kCutThreads = 1024;
-constexpr int kCutWaves = kCutThreads / kWave;
-constexpr int kBins = 2 * kCutThreads;
-constexpr int kMaxGroups = (1 << kColumnBits) / (4 * kCutThreads) + 1;
+constexpr int kBins = 2048;   // of the search
 constexpr double kSearchUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 
@@ -36,7 +33,7 @@ struct CutShared {
         double weight[kListMax];
       };
     };
-    double group[W][kMaxGroups];
+    double group[W][(1 << kColumnBits) / (4 * NT) + 1];
   };
   union {
     double chunk[kMaxChunks];
@@ -86,9 +83,9 @@ __device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1,
     after(g);
   }
 }
-template <typename T, typename F>
+template <int NT, typename T, typename F>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, F f) {
-  each_entry<kCutThreads>(r, 0, r.vectors(), f, [](int) {});
+  each_entry<NT>(r, 0, r.vectors(), f, [](int) {});
 }
 
 // Exchanges of a bitonic sort within a wave, FROM, FROM / 2 .. 1 lanes apart, the greater key to the
@@ -191,10 +188,11 @@ __device__ __forceinline__ int value_bin(float z, float m, float scale) {
 // Histograms of 2048 bins over ever smaller ranges of the order, until a bin's entries fit the
 // list: the first by value, further ones by key, where the last range is one key.  A caller that
 // knows the range of keys and the sum `above` it starts there (lo > 0).
-template <bool BY_MASS, typename T, typename Shared>
+template <int NT, bool BY_MASS, typename T, typename Shared>
 __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t floor, float m,
                                  double c2, float scale, Shared& sh, uint64_t lo = 0,
                                  uint64_t hi = kKeyTop, double above = 0.) {
+  constexpr int W = NT / kWave, PER = kBins / NT, LISTED = kListMax / NT;
   auto shift_of = [&]() {
     int sh_ = 0;
     while (((hi - lo) >> sh_) >= uint64_t(kBins)) ++sh_;
@@ -202,16 +200,16 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
   };
   int shift = lo > 0 ? shift_of() : -1, bin = 0;   // shift -1: the bins by value
   for (;;) {
-    for (int b = threadIdx.x; b < kBins; b += kCutThreads) {
+    for (int b = threadIdx.x; b < kBins; b += NT) {
       sh.count[b] = 0;
       sh.mass[b] = 0;
     }
-    if (threadIdx.x == 0) sh.pick = -1, sh.last = 0;
+    if (threadIdx.x == 0) sh.pick = sh.last = 0, sh.before = 0;
     __syncthreads();
     auto bin_of = [&](float z, uint64_t k) {
       return shift < 0 ? value_bin(z, m, scale) : int((hi - k) >> shift);
     };
-    each_entry(r, [&](float z, int c) {
+    each_entry<NT>(r, [&](float z, int c) {
       const uint64_t k = entry_key(z, c);
       if (k < floor || k < lo || k > hi) return;
       const int b = bin_of(z, k);
@@ -221,50 +219,62 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
                   static_cast<unsigned long long>(entry_weight(z, m, c2) / kSearchUnit + 0.5));
     });
     __syncthreads();
-    const int b0 = 2 * threadIdx.x;
-    const uint64_t v0 = BY_MASS ? sh.mass[b0] : sh.count[b0];
-    const uint64_t v1 = BY_MASS ? sh.mass[b0 + 1] : sh.count[b0 + 1];
-    uint64_t whole;
-    const uint64_t at1 = block_scan<kCutWaves>(v0 + v1, sh.red.u, whole);
+    const int b0 = PER * threadIdx.x;
+    uint64_t own = 0, whole;
+    int end = -1;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      own += BY_MASS ? sh.mass[b0 + e] : sh.count[b0 + e];
+      end = sh.count[b0 + e] != 0 ? b0 + e : end;
+    }
+    const uint64_t upto = block_scan<W>(own, sh.red.u, whole);
+    note_last(end >= 0, end, &sh.last);
+    __syncthreads();
     const double unit = BY_MASS ? kSearchUnit : 1.;
     auto reached = [&](uint64_t s) { return above + double(s) * unit >= target; };
+    const bool none = !reached(whole);
+    uint64_t after = upto - own;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint64_t after = h == 0 ? at1 - v1 : at1, before = after - (h == 0 ? v0 : v1);
-      if (reached(after) && !reached(before)) {
-        sh.pick = b0 + h;
+    for (int e = 0; e < PER; ++e) {
+      const uint64_t before = after;
+      after += BY_MASS ? sh.mass[b0 + e] : sh.count[b0 + e];
+      if (none ? b0 + e == sh.last : after > before && reached(after) && (before == 0 || !reached(before))) {
+        sh.pick = b0 + e;
         sh.before = before;
       }
     }
-    note_last((sh.count[b0] | sh.count[b0 + 1]) != 0, sh.count[b0 + 1] != 0 ? b0 + 1 : b0, &sh.last);
     __syncthreads();
-    if (sh.pick < 0 && int(threadIdx.x) == sh.last / 2) {
-      sh.before = (sh.last & 1) ? at1 - v1 : at1 - v1 - v0;
-    }
-    bin = sh.pick < 0 ? sh.last : sh.pick;
-    __syncthreads();
+    bin = sh.pick;
     above += double(sh.before) * unit;
     const uint32_t here = sh.count[bin];
+    __syncthreads();
     if (threadIdx.x == 0) sh.n = 0, sh.pick = kListMax;
     __syncthreads();
     if (here <= uint32_t(kListMax)) {
-      each_entry(r, [&](float z, int c) {
+      each_entry<NT>(r, [&](float z, int c) {
         const uint64_t k = entry_key(z, c);
         if (k < floor || k < lo || k > hi || bin_of(z, k) != bin) return;
         sh.list[atomicAdd(&sh.n, 1u)] = k;
       });
       __syncthreads();
       const int n = int(sh.n);
-      sort_list<kCutThreads>(sh.list, n);
+      sort_list<NT>(sh.list, n);
       int at;
       if (BY_MASS) {
-        const int i = 2 * threadIdx.x;
-        const double w0 = i < n ? entry_weight(entry_logit(sh.list[i]), m, c2) : 0.;
-        const double w1 = i + 1 < n ? entry_weight(entry_logit(sh.list[i + 1]), m, c2) : 0.;
-        double all;
-        const double sum = block_scan<kCutWaves>(w0 + w1, sh.red.d, all);
-        const bool is0 = i < n && above + (sum - w1) >= target;
-        note_first(is0 || (i + 1 < n && above + sum >= target), is0 ? i : i + 1, &sh.pick);
+        const int i0 = LISTED * threadIdx.x;
+        double own_w = 0., all;
+#pragma unroll 1
+        for (int e = 0; e < LISTED; ++e)
+          own_w += i0 + e < n ? entry_weight(entry_logit(sh.list[i0 + e]), m, c2) : 0.;
+        double run = above + (block_scan<W>(own_w, sh.red.d, all) - own_w);
+        int first = -1;
+#pragma unroll 1
+        for (int e = 0; e < LISTED; ++e)
+          if (i0 + e < n) {
+            run += entry_weight(entry_logit(sh.list[i0 + e]), m, c2);
+            first = first < 0 && run >= target ? i0 + e : first;
+          }
+        note_first(first >= 0, first, &sh.pick);
         __syncthreads();
         at = min(sh.pick, n - 1);
       } else {
@@ -414,12 +424,11 @@ __device__ __forceinline__ int reach(int n, double from, double target, double& 
   return at;
 }
 
-// The second launch's work in phases, a launch each.  The lists are handled by small workgroups: a
-// large one's waves take turns at the same few instructions (1024 threads took 16 us for a row with
-// top_k that 256 take X us for).  What those leave, the rows that need one more pass and those that
-// need the search, large ones take after, in one launch, or with many rows in two, of which the
-// first needs fewer registers.
-enum CutPhase { kLists, kRest, kBorder, kSearch };
+// The second launch's work in phases.  Of few rows one launch does it all, in small workgroups: a
+// large one's waves take turns at the same few instructions.  Of many rows those that the lists do
+// not settle are left to further launches of larger workgroups: one more pass, with few enough
+// registers for many rows at a time, and the search.
+enum CutPhase { kAll, kLists, kBorder, kSearch };
 enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
 
 // The chunks' statistics joined, by the first wave.
@@ -516,9 +525,9 @@ __device__ __forceinline__ int gather(const uint64_t mine[kListMax / NT], float 
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT)
 row_top_kernel(CutArgs a, HeadArgs h) {
-  constexpr bool LISTS = PHASE == kLists, SEARCH = !LISTS, BORDER = false;
+  constexpr bool LISTS = PHASE != kSearch, SEARCH = PHASE != kLists;
   constexpr int W = NT / kWave;
-  __shared__ CutShared<NT, SEARCH, BORDER> sh;
+  __shared__ CutShared<NT, SEARCH, false> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, K = a.K;
   if (PHASE == kSearch && h.notes[at].left != kLeftSearch) return;
@@ -545,7 +554,7 @@ row_top_kernel(CutArgs a, HeadArgs h) {
       t = floor;
     }
     done = have >= n;
-    if (tid == 0) h.notes[at].left = done ? kDone : kLeftSearch;
+    if (PHASE == kLists && tid == 0) h.notes[at].left = done ? kDone : kLeftSearch;
     if (done) {
       sort_list<NT>(sh.list, have);
       if (a.rest != nullptr) {
@@ -565,19 +574,20 @@ row_top_kernel(CutArgs a, HeadArgs h) {
         sum = block_fold<W>(sum, sh.red.d, add);
         if (tid == 0) a.rest[row] = sum > 0. ? float(ref * s.inv_t + log(sum)) : -INFINITY;
       }
-    } else {
+    } else if (PHASE == kLists) {
       return;
     }
   }
   if constexpr (SEARCH) {
-    {
-      const uint64_t cut = valid > uint32_t(K) ? select_entry<false>(r, double(K), 0, entry_logit(sh.best),
+    if (!done) {
+      __syncthreads();
+      const uint64_t cut = valid > uint32_t(K) ? select_entry<NT, false>(r, double(K), 0, entry_logit(sh.best),
                                                                      s.c2, float(64. * s.inv_t), sh)
                                                : 0;
       if (tid == 0) sh.n = 0;
       __syncthreads();
       uint64_t next = 0;   // the first entry past the list
-      each_entry(r, [&](float z, int c) {
+      each_entry<NT>(r, [&](float z, int c) {
         const uint64_t k = entry_key(z, c);
         if (k >= cut)
           sh.list[atomicAdd(&sh.n, 1u)] = k;
@@ -591,7 +601,7 @@ row_top_kernel(CutArgs a, HeadArgs h) {
         const float top = entry_logit(next);
         double sum = 0.;
         if (next != 0)
-          each_entry(r, [&](float z, int c) {
+          each_entry<NT>(r, [&](float z, int c) {
             if (entry_key(z, c) < cut) sum += entry_weight(z, top, s.c2);
           });
         sum = block_fold<W>(sum, sh.red.d, add);
@@ -818,8 +828,8 @@ __device__ __forceinline__ int draw_binned(const LogitRow<T>& r, int j0, int j1,
 template <typename T, int NT, CutPhase PHASE>
 __global__ void __launch_bounds__(NT, PHASE == kBorder ? 8 : 1)
 row_cut_kernel(CutArgs a, HeadArgs h) {
-  constexpr bool LISTS = PHASE == kLists, BORDER = PHASE == kRest || PHASE == kBorder,
-                 SEARCH = PHASE == kRest || PHASE == kSearch;
+  constexpr bool LISTS = PHASE == kAll || PHASE == kLists, BORDER = PHASE == kAll || PHASE == kBorder,
+                 SEARCH = PHASE == kAll || PHASE == kSearch;
   constexpr int W = NT / kWave, PER = kMassBins / NT, LISTED = kListMax / NT;
   // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
   // whose masses the histograms hold, one chunk is read instead.
@@ -830,7 +840,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   CutNote* note = h.notes + at;
   if (PHASE == kBorder && note->left != kLeftBorder) return;
   if (PHASE == kSearch && note->left != kLeftSearch) return;
-  if (PHASE == kRest && note->left == kDone) return;
   const LogitRow<T> r(static_cast<const T*>(a.z) + row * a.ld, a.V);
   const RowSettings s = settings_of<false>(a, row);
   auto add = [](auto u, auto v) { return u + v; };
@@ -891,6 +900,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   const double k16 = 16. * s.c2;
   double whole_w = 0., above = 0.;   // relative to the greatest entry: the whole, the bins above
   int border = 0;
+  float end = 0.f, over = INFINITY;   // the values of the border bin: end <= z < over
   bool by_p = false;   // whether top_p's cut lies in it
   auto bin_weight = [&](int b) { return exp2_64(-double(b) / 16.); };
   // 2^-48 of the top bin's middle, relative to the greatest entry's weight.
@@ -962,7 +972,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         join_masses(std::integral_constant<int, 2>());
       else
         join_masses(std::integral_constant<int, PER>());
-      if (tid == 0)
+      if (PHASE == kLists && tid == 0)
         note->whole = whole_w, note->above = above, note->border = border, note->by_p = by_p,
         note->cut_m = cut_m;
     }
@@ -971,9 +981,10 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     above = note->above;
     border = note->border;
     by_p = note->by_p != 0;
+    end = note->end;
+    over = note->over;
   }
   // The least values of the border bin and of the bin before: end <= z < over.
-  float end = 0.f, over = INFINITY;
   auto find_edges = [&]() {
     if (wid < 2) {
       const int b = border - wid;
@@ -1054,17 +1065,16 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       write(uint32_t(k), low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
       return;
     }
-    if (tid == 0) {
+    if (PHASE == kLists && tid == 0) {
       note->border = border, note->by_p = by_p, note->end = end, note->over = over;
       note->left = binned ? kLeftBorder : kLeftSearch;
     }
   }
+  if (PHASE == kAll) __syncthreads();
   if constexpr (BORDER) {
     if (binned) {
       uint32_t greater = valid;
       int n = 0;
-      end = note->end;
-      over = note->over;
       const bool fits = s.open || [&]() {
         for (;;) {
           n = border_entries<NT>(r, end, over, greater, sh);
@@ -1155,22 +1165,22 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     // Neither the lists nor the histograms tell: counts of very many entries, values beyond the
     // bins, border bins of more entries than are sorted.
     const float scale = float(64. * s.inv_t);
-    cut = has_k ? select_entry<false>(r, double(s.top_k), 0, m, s.c2, scale, sh) : 0;
+    cut = has_k ? select_entry<NT, false>(r, double(s.top_k), 0, m, s.c2, scale, sh) : 0;
     if (binned ? by_p : has_p) {
       uint64_t from = 0, to = kKeyTop;
       double all = whole_w;
       if (binned) {
-        from = entry_key(note->end, a.V - 1);
-        to = border > 0 ? (uint64_t(f32_order_key(note->over)) << kColumnBits) - 1 : kKeyTop;
+        from = entry_key(end, a.V - 1);
+        to = border > 0 ? (uint64_t(f32_order_key(over)) << kColumnBits) - 1 : kKeyTop;
       } else {
         all = 0.;
-        each_entry(r, [&](float z, int c) {
+        each_entry<NT>(r, [&](float z, int c) {
           if (entry_key(z, c) >= cut) all += entry_weight(z, m, s.c2);
         });
         all = block_fold<W>(all, sh.red.d, add);
       }
       // A target of 0 is reached by the first entry, not before it.
-      cut = most64(cut, select_entry<true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2, scale,
+      cut = most64(cut, select_entry<NT, true>(r, fmax(double(s.top_p) * all, 1e-300), cut, m, s.c2, scale,
                                            sh, from, to, binned ? above : 0.));
     }
     cut = most64(cut, cut_m);
@@ -1208,9 +1218,13 @@ static int64_t cut_rows(bool bf16, int64_t rows, int V) {
   const int64_t most = kCutChunks / head_plan(bf16, kCutChunks, V).chunks;
   return rows < most ? rows : most;
 }
-// Above this many rows (a large workgroup a CU) the rest is two launches.
-constexpr int64_t kRestRows = 256;
-constexpr int kListThreads = 256, kBorderThreads = 512;
+constexpr int kListThreads = 256, kBorderThreads = 512, kSearchThreads = 1024;
+constexpr int kAllThreads = 512;
+// Whether one launch does all: up to a row a CU, whose running sums a workgroup's threads hold.
+constexpr int64_t kAllRows = 256;
+static bool all_at_once(bool bf16, int64_t rows, int V) {
+  return rows <= kAllRows && V <= kAllThreads * kAllThreads * (bf16 ? 8 : 4) - 16;
+}
 
 size_t cut_ws_bytes(bool bf16, int64_t rows, int V, bool top) {
   const int64_t n = cut_rows(bf16, rows, V);
@@ -1250,22 +1264,22 @@ static hipError_t launch_cut(const CutArgs& all, void* ws, hipStream_t s) {
     h.mass = reinterpret_cast<uint64_t*>(p);
     hipError_t e = launch_row_head(bf16, TOP, pl.elems == 8, a, h, s);
     if (e != hipSuccess) return e;
-    const dim3 rows(unsigned(a.rows)), lists(kListThreads), large(kCutThreads);
-    if constexpr (TOP)
-      hipLaunchKernelGGL((row_top_kernel<T, kListThreads, kLists>), rows, lists, 0, s, a, h);
-    else
-      hipLaunchKernelGGL((row_cut_kernel<T, kListThreads, kLists>), rows, lists, 0, s, a, h);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if constexpr (TOP) {
-      hipLaunchKernelGGL((row_top_kernel<T, kCutThreads, kSearch>), rows, large, 0, s, a, h);
-    } else if (a.rows <= kRestRows) {
-      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kRest>), rows, large, 0, s, a, h);
+    const dim3 rows{unsigned(a.rows)};
+    if (all_at_once(bf16, a.rows, a.V)) {
+      if constexpr (TOP)
+        hipLaunchKernelGGL((row_top_kernel<T, kAllThreads, kAll>), rows, dim3(kAllThreads), 0, s, a, h);
+      else
+        hipLaunchKernelGGL((row_cut_kernel<T, kAllThreads, kAll>), rows, dim3(kAllThreads), 0, s, a, h);
+    } else if constexpr (TOP) {
+      hipLaunchKernelGGL((row_top_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL((row_top_kernel<T, kSearchThreads, kSearch>), rows, dim3(kSearchThreads), 0, s, a, h);
     } else {
+      hipLaunchKernelGGL((row_cut_kernel<T, kListThreads, kLists>), rows, dim3(kListThreads), 0, s, a, h);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
       hipLaunchKernelGGL((row_cut_kernel<T, kBorderThreads, kBorder>), rows, dim3(kBorderThreads), 0, s, a, h);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((row_cut_kernel<T, kCutThreads, kSearch>), rows, large, 0, s, a, h);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL((row_cut_kernel<T, kSearchThreads, kSearch>), rows, dim3(kSearchThreads), 0, s, a, h);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
