@@ -58,29 +58,42 @@ struct CutShared {
 };
 
 // Calls f(value, column) for every unmasked entry of vectors j0 .. j1-1 of the row and after(g) with
-// all lanes together behind the g-th run of NT of them; the next run's loads are in flight.
+// all lanes together behind the g-th run of NT of them; the loads of the next runs, 16 entries a
+// thread, are in flight.
 template <int NT, typename T, typename F, typename G>
 __device__ __forceinline__ void each_entry(const LogitRow<T>& r, int j0, int j1, F f, G after) {
-  constexpr int N = LogitRow<T>::N;
-  float x[N], y[N];
-  auto load = [&](int g, float v[N]) {
-    const int j = j0 + g * NT + int(threadIdx.x);
+  constexpr int N = LogitRow<T>::N, Q = 16 / N;
+  float x[Q][N], y[Q][N];
+  auto load = [&](int g, float v[Q][N]) {
+    const int first = j0 + g * NT;
+    if (r.inside(first, Q * NT) && first + Q * NT <= j1) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = -INFINITY;
-    if (j < j1) r.load_raw(j, v);
+      for (int q = 0; q < Q; ++q) r.load_inside(first + q * NT + int(threadIdx.x), v[q]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int j = first + q * NT + int(threadIdx.x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[q][e] = -INFINITY;
+        if (j < j1) r.load_raw(j, v[q]);
+      }
+    }
   };
   const int groups = (j1 - j0 + NT - 1) / NT;
   load(0, x);
 #pragma unroll 1
-  for (int g = 0; g < groups; ++g) {
-    load(g + 1, y);
-    const int c = r.column(j0 + g * NT + int(threadIdx.x));
+  for (int g0 = 0; g0 < groups; g0 += Q) {
+    load(g0 + Q, y);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      if (x[e] > -INFINITY) f(x[e], c + e);   // false for NaN
-      x[e] = y[e];
+    for (int q = 0; q < Q; ++q) {
+      const int g = g0 + q, c = r.column(j0 + g * NT + int(threadIdx.x));
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (x[q][e] > -INFINITY) f(x[q][e], c + e);   // false for NaN
+        x[q][e] = y[q][e];
+      }
+      if (g < groups) after(g);
     }
-    after(g);
   }
 }
 template <int NT, typename T, typename F>
