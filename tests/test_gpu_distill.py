@@ -217,6 +217,20 @@ def test_students_far_from_zero(T):
     _check(c, B, T)
 
 
+@pytest.mark.parametrize("n", [32, 33, 70])
+def test_means_over_few_and_many_slots(n):
+    """Slots that one launch counts and more, over a workspace of arbitrary contents, used again."""
+    B, P, K, V = 9, 8, 70, 301
+    c = _case(n, B, P, K, V, n)
+    _check(c, B)
+    ws = torch.full((hdf.lib().hdf_distill_workspace(n, B, V, 0),), 255, dtype=torch.uint8, device=DEV)
+    args = (c["z"], c["ids"], c["val"], c["rest"], c["lab"])
+    want = hdf.distill_forward(*args, B=B)
+    for _ in range(3):
+        got = hdf.distill_forward(*args, B=B, ws=ws)
+        assert all(torch.equal(g, w) for g, w in zip(got[:3], want[:3]))
+
+
 @pytest.mark.parametrize("K", [63, 64, 65, 255, 256, 257, 700])
 def test_list_lengths(K):
     _check(_case(2, 3, 2, K, 2003, K), 3)

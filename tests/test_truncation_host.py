@@ -81,6 +81,18 @@ def test_accept_limits_and_workspace():
     assert sizes == sorted(sizes)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("V", [1, 100, 4097, 32003, 129280, 262145, 1 << 20])
+def test_workspaces_serve_fewer_rows(V, dtype):
+    """The need of every smaller call lies within the size that is reported for a larger one."""
+    L = hdf.lib()
+    rows = list(range(1, 300)) + list(range(300, 9000, 131)) + [65535]
+    for size in (lambda n: L.hdf_sample_truncated_workspace(n, V, dtype),
+                 lambda n: L.hdf_top_logits_workspace(n, V, 5, dtype)):
+        sizes = [size(n) for n in rows]
+        assert sizes[0] > 0 and sizes == sorted(sizes)
+
+
 def _top(rows=4, V=100, ld=100, dtype=0, K=5, T=1.0, logits=FAKE, ids=FAKE, values=FAKE):
     return _status(hdf.lib().hdf_top_logits(logits, rows, V, ld, dtype, K, T, ids, values, None,
                                             FAKE, 1 << 30, None))
