@@ -501,7 +501,8 @@ hdf_status hdf_kl_forward(const void* H_pos, int m, const float* gamma, float ep
  *     n   = min(n_k, n_p, n_m); 1 at T = 0 (greedy); 0 where every entry is masked
  * and the truncated distribution is the softmax at temperature T over them (one entry of
  * probability 1 at T = 0).  A draw with the uniform u is the lowest token whose running sum of kept
- * weights, in token order, exceeds u times their sum.  Sums and the weights in them are 64-bit.
+ * weights, in token order, exceeds u times their sum.  Sums and the weights in them are 64-bit (of
+ * weights below 2^-60, 2^-41 of the whole at most, a sum may hold nothing).
  * ----------------------------------------------------------------------------*/
 /* Settings, one value for every row or one a sequence.  Row r takes entry r / rows_per_seq of an
  * array (device); where an array is NULL, the value beside it holds for all rows.  In arrays a
@@ -606,7 +607,8 @@ hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t l
  * A slot whose teacher has no entry of finite logit has kl = 0 and no gradient.  A masked (-inf)
  * student logit has gradient 0 where it is not listed; one that the teacher gives mass makes kl
  * infinite.  A NaN among a slot's student or teacher logits makes its losses and gradients NaN.
- * Sums are 64-bit, losses rounded once.
+ * Sums are 32-bit within a wave, over at most 15 additions in a row, 64-bit beyond; losses are
+ * rounded once.
  * ----------------------------------------------------------------------------*/
 /* Bytes of the record that the forward pass leaves for the backward (0 on invalid arguments). */
 size_t hdf_distill_saved_bytes(int n_seq, int B, int P, int K);

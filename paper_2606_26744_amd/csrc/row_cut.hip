@@ -1,7 +1,10 @@
 // Second launch of a row's cut (row_cut.hpp): a workgroup a row.  Its code runs once a row, mostly on
 // the way to the next memory access or barrier, so it is kept short: the same few loops for all
-// settings, nothing unrolled that memory does not need in flight.  (139 KB of unrolled code took
-// 60 us a row of instruction fetches where it takes 20.)
+// settings, nothing unrolled that memory does not need in flight.  What bounds it is the latency of
+// those steps, 1 to 6 thousand cycles each, and for a nucleus beyond the lists the row's second pass.
+// Of 128 rows of 129280 fp32 logits it takes 9 us with top_k = 50, 18 us for a nucleus of 5 entries,
+// 46 us for one of 4000; of 1024 rows of 16 bits, a nucleus of 4600, 130 us (the second pass, 97, at
+// 2.7 TB/s).
 #include "row_cut.hpp"
 
 #include <type_traits>
@@ -437,10 +440,12 @@ __device__ __forceinline__ int reach(int n, double from, double target, double& 
   return at;
 }
 
-// The second launch's work in phases.  Of few rows one launch does it all, in small workgroups: a
-// large one's waves take turns at the same few instructions.  Of many rows those that the lists do
-// not settle are left to further launches of larger workgroups: one more pass, with few enough
-// registers for many rows at a time, and the search.
+// The second launch's work in phases.  Of few rows one launch does it all, 512 threads a row (128 rows
+// of 129280, a nucleus of 4000 entries 65 us in all, 81 with 256 threads, 62 with 1024; 60 rows of
+// 32003, one of 4 entries 21, 22 and 23 us; in three launches 78 and 24).  Of many rows those that the
+// lists do not settle are left to further launches of larger workgroups: one more pass, with few
+// enough registers for many rows at a time, and the search (lists by 256 threads a row: 1024 rows, a
+// nucleus of 5 entries 148 us in all, 153 by 512).
 enum CutPhase { kAll, kLists, kBorder, kSearch };
 enum { kDone = 0, kLeftBorder = 1, kLeftSearch = 2 };
 
@@ -980,7 +985,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       __syncthreads();
       above = sh.sum;
     };
-    if (binned) {
+    if (binned && !s.open) {
       if (sh.span <= 2 * NT)
         join_masses(std::integral_constant<int, 2>());
       else
@@ -1113,7 +1118,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       }();
       if (fits) {
         // The chunks' masses: their part of the border's entries, their bins above it.
-        if (s.open) border = kMassBins;
+        if (s.open) border = min(sh.span, kMassBins);
         for (int c = tid; c < h.chunks; c += NT) sh.chunk_n[c] = 0;
         __syncthreads();
         const double c5 = mass_coefficient(kBits);

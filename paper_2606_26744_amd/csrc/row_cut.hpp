@@ -12,7 +12,8 @@
 // First launch (row_head.hip): workgroup (row, chunk) keeps a chunk of a row in registers, lists
 // its greatest entries and, where the cut is not a count of entries, sums the weights up in a
 // histogram.  Second launch (row_cut.hip): a workgroup a row finds how far down the order the cut
-// lies; a cut below the lists takes one more pass over the row.
+// lies; a cut below the lists takes one more pass over the row.  (One workgroup a row for all of it,
+// going over the row again and again: 128 rows of 129280 228 us where the two take 45.)
 #pragma once
 
 #include "kernels.hpp"
@@ -28,7 +29,7 @@ constexpr float kLeast = -3.402823466e38f;   // the least finite value
 // The histogram: bins of 1/16 octave of weight.  Entry z has t = 16 z log2(e) / T, bin n = rint(t)
 // and within it the weight 2^((t - n) / 16), 0.978 .. 1.022, as a multiple of 2^-48; integers, so
 // that the sums do not depend on their order.  Bins from the chunk's greatest entry down; entries
-// of the last 40, more than 61 octaves below it, weigh nothing.
+// of the last 40, more than 61 octaves below it, weigh nothing (all 2^20 of a row 2^-41 of the whole).
 constexpr int kMassBins = 1024, kKeptBins = 984;
 constexpr double kMassUnit = 1.0 / 281474976710656.0;   // 2^-48
 
