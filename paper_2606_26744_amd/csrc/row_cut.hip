@@ -3,8 +3,8 @@
 // settings, nothing unrolled that memory does not need in flight.  What bounds it is the latency of
 // those steps, 1 to 6 thousand cycles each, and for a nucleus beyond the lists the row's second pass.
 // Of 128 rows of 129280 fp32 logits it takes 9 us with top_k = 50, 18 us for a nucleus of 5 entries,
-// 46 us for one of 4000; of 1024 rows of 16 bits, a nucleus of 4600, 130 us (the second pass, 97, at
-// 2.7 TB/s).
+// 46 us for one of 4000; of 1024 rows of 16 bits, a nucleus of 4600, 125 us (the second pass, 92, at
+// 2.9 TB/s).
 #include "row_cut.hpp"
 
 #include <type_traits>
