@@ -136,6 +136,17 @@ def test_every_alignment_of_logits_and_gradients(offset, dtype):
         assert (buf[mask] == 9.0).all()
 
 
+def test_rows_more_than_32_bits_apart():
+    """Logits and gradients whose offsets in elements pass 2^32."""
+    n, B, V, ld = 1, 3, 4003, 2 ** 31 + 8
+    c = _case(n, B, 2, 9, V, 3, torch.bfloat16)
+    z, d = (torch.as_strided(torch.empty(2 * ld + V, dtype=torch.bfloat16, device=DEV), (B, V), (ld, 1))
+            for _ in range(2))
+    z.copy_(c["z"])
+    c["z"] = z
+    _check(c, B, d_logits=d)
+
+
 def test_every_upstream_gradient():
     n, B, P = 3, 5, 2
     c = _case(n, B, P, 10, 5000, 2)

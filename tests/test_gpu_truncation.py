@@ -256,6 +256,17 @@ def test_rows_in_several_groups_of_launches():
         assert ids[r].tolist() == i.tolist()
 
 
+def test_rows_more_than_32_bits_apart():
+    """Rows whose offsets in elements pass 2^32."""
+    V, ld = 5003, 3 * 2 ** 30 + 1
+    buf = torch.empty(2 * ld + V, dtype=torch.bfloat16, device=DEV)
+    z = torch.as_strided(buf, (3, V), (ld, 1))
+    z.copy_(_logits(3, V, 9, torch.bfloat16))
+    for kw in (dict(top_p=0.9), dict(top_k=30), dict(temperature=3.0, top_p=0.9), dict()):
+        _check_draws(z, _u(3, 1), **kw)
+    _check_top(z, 20)
+
+
 def test_uniforms_at_and_past_the_ends():
     z = _logits(1, 5000, 2).repeat(6, 1)
     u = torch.tensor([0.0, 1 - 2.0 ** -24, 1.0, 7.0, -3.0, float("nan")], device=DEV)
