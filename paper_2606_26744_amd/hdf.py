@@ -463,11 +463,15 @@ def _truncation_params(like, n, rows_per_seq, *values):
     """The C struct of settings (in _SETTINGS' order) that are numbers or tensors of one entry a
     sequence."""
     one, many = [1.0, 0, 1.0, 0.0], [None] * 4
+    device = like.get_device()
     for i, value in enumerate(values):
         if isinstance(value, torch.Tensor):
-            _typed(value, _SETTINGS[i][2], n, _SETTINGS[i][0])
-            _dev(value)
-            _same_device(like, value)
+            name, _, dtype = _SETTINGS[i]
+            if (value.dtype != dtype or value.numel() < n or device < 0 or
+                    value.get_device() != device or not value.is_contiguous()):
+                _typed(value, dtype, n, name)
+                _dev(value)
+                _same_device(like, value)
             many[i] = value.data_ptr()
         elif value is not None:
             one[i] = value
@@ -493,11 +497,10 @@ def sample_truncated(logits: torch.Tensor, uniforms: Optional[torch.Tensor] = No
         _dev(uniforms)
         _same_device(logits, uniforms)
         if out is None:
-            device, i32 = logits.device, torch.int32
-            tok = torch.empty(rows, dtype=i32, device=device) if uniforms is not None else None
-            cut = Truncation(torch.empty(rows, dtype=i32, device=device),
-                             torch.empty(rows, dtype=torch.float32, device=device),
-                             torch.empty(rows, dtype=i32, device=device),
+            device = logits.device
+            tok, kept, index = torch.empty((3, rows), dtype=torch.int32, device=device).unbind(0)
+            tok = tok if uniforms is not None else None
+            cut = Truncation(kept, torch.empty(rows, dtype=torch.float32, device=device), index,
                              torch.empty(rows, dtype=torch.float64, device=device))
         else:
             tok, cut = out[0], Truncation(*out[1])
