@@ -848,8 +848,10 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
                  SEARCH = PHASE == kAll || PHASE == kSearch;
   constexpr int W = NT / kWave, PER = kMassBins / NT, LISTED = kListMax / NT;
   // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
-  // whose masses the histograms hold, one chunk is read instead.
-  constexpr int kInOrder = 512;
+  // whose masses the histograms hold, one chunk is read instead.  (The larger workgroup sorts more:
+  // 60 rows, a min_p that keeps 1400, 28 us by 512, 35 by 256; 1024 rows, a nucleus, 243 by 512, 235 by
+  // 256, 283 by 1536.)
+  constexpr int kInOrder = PHASE == kAll ? 512 : 256;
   __shared__ CutShared<NT, SEARCH, BORDER> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
