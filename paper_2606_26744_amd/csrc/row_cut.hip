@@ -410,13 +410,13 @@ __device__ __forceinline__ int draw_entry(const LogitRow<T>& r, int j0, int j1, 
 }
 
 // First place, among 0 .. n-1, whose running sum of w(i) reaches (STRICT: passes) `from` times the
-// whole sum, or `target` where from is negative; n where none does.  `sum` gets the whole,
-// sh.last the last place with a weight.
+// whole sum; n where none does.  `sum` gets the whole, sh.last the last place with a weight.
 template <int NT, bool STRICT, typename Shared, typename F>
-__device__ __forceinline__ int reach(int n, double from, double target, double& sum, Shared& sh, F w) {
+__device__ __forceinline__ int reach(int n, double from, double& sum, Shared& sh, F w) {
   const bool once = n <= NT;   // the sum and the place of one scan
+  double target = 0.;
 #pragma unroll 1
-  for (int pass = from >= 0. && !once ? 0 : 1; pass < 2; ++pass) {   // the sum, then the place
+  for (int pass = once ? 1 : 0; pass < 2; ++pass) {   // the sum, then the place
     if (threadIdx.x == 0) sh.pick = n, sh.last = 0;
     double before = 0.;
 #pragma unroll 1
@@ -426,7 +426,7 @@ __device__ __forceinline__ int reach(int n, double from, double target, double& 
       double all;
       const double run = before + block_scan<NT / kWave>(v, sh.red.d, all);
       before += all;
-      if (from >= 0. && (once || pass == 0))   // 0 is reached by the first, not before
+      if (once || pass == 0)   // 0 is reached by the first, not before
         target = STRICT ? from * before : fmax(from * before, 1e-300);
       if (pass == 1) {
         note_first(i < n && (STRICT ? v > 0. && run > target : run >= target), i, &sh.pick);
@@ -436,8 +436,7 @@ __device__ __forceinline__ int reach(int n, double from, double target, double& 
     __syncthreads();
     sum = before;
   }
-  const int at = sh.pick;
-  return at;
+  return sh.pick;
 }
 
 // The second launch's work in phases.  Of few rows one launch does it all, 512 threads a row (128 rows
@@ -691,12 +690,28 @@ __device__ __forceinline__ int border_entries(const LogitRow<T>& r, float end, f
   return n;
 }
 
+// Masses relative to the greatest entry's weight: integers of a bin over that of the greatest entry,
+// which is w0.  Correctly rounded, from two exact halves, so that n equal entries at the top weigh n
+// and a cut or a draw among them falls where their count says.
+struct TopWeight {
+  double w0, inv;
+  __device__ __forceinline__ double over(double hi, double lo) const {   // (2^32 hi + lo) / w0
+    const double s = fma(hi, 4294967296., lo), rest = lo - fma(hi, -4294967296., s);
+    const double q = s * inv;
+    return fma(fma(-q, w0, s) + rest, inv, q);
+  }
+  __device__ __forceinline__ double over(uint64_t n) const {
+    return over(double(uint32_t(n >> 32)), double(uint32_t(n)));
+  }
+};
+
 // Key, among the n border entries, all of one bin, at which `above` and the running sum of their
 // weights in the order, times w_bin, reach the target; the last one if rounding leaves none.  Masses
 // over ever smaller ranges of keys; sorting the entries instead took three times as long.
 template <int NT, typename Shared>
 __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi, double k16, double above,
-                                                 double w_bin, double target, Shared& sh) {
+                                                 const TopWeight& top, double w_bin, double target,
+                                                 Shared& sh) {
   const int tid = threadIdx.x;
   const double c5 = mass_coefficient(kBits);
   uint64_t base = 0;
@@ -718,7 +733,7 @@ __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi
     const uint64_t own = sh.fine[tid];
     uint64_t all;
     const uint64_t upto = base + block_scan<NT / kWave>(own, sh.red.u, all);
-    note_first(own > 0 && above + double(upto) * w_bin >= target, tid, &sh.pick);
+    note_first(own > 0 && above + top.over(upto) * w_bin >= target, tid, &sh.pick);
     note_last(own > 0, tid, &sh.last);
     __syncthreads();
     const int at = min(sh.pick, sh.last);
@@ -741,7 +756,8 @@ __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi
       int bin;
       const uint64_t w = k != 0 ? weight_in_bin(entry_logit(k), k16, c5, bin) : 0ull;
       const unsigned long long some = __ballot(k != 0);
-      const unsigned long long past = __ballot(k != 0 && above + double(base + wave_scan(w)) * w_bin >= target);
+      const double run = above + top.over(base + wave_scan(w)) * w_bin;
+      const unsigned long long past = __ballot(k != 0 && run >= target);
       k = read_lane(k, past != 0ull ? __ffsll(static_cast<long long>(past)) - 1
                                     : 63 - __clzll(static_cast<long long>(some | 1ull)));
       __syncthreads();
@@ -765,13 +781,14 @@ __device__ __forceinline__ uint64_t border_entry(int n, uint64_t lo, uint64_t hi
 
 // The draw among a row's kept entries of vectors j0 .. j1-1 (a chunk's, up to 64 runs of 64 a wave):
 // the entry at which `base` and the running sum pass the target, the last one where rounding leaves
-// none.  table: the weights of the bins' middles; from `end` down entries have none.  A sum a run,
+// none.  table: the weights of the bins' middles over the greatest entry's, which is 1 exactly; from
+// `end` down entries have none.  A sum a run,
 // gone through by every wave, then the run's entries by one.  A loop with D vectors in flight; all in
 // registers was 5 KB of code, run once: 13 thousand cycles for 4096 entries where this takes 9.
 template <int NT, int D, typename T, typename Shared>
-__device__ __forceinline__ int draw_binned(const LogitRow<T>& r, int j0, int j1, uint64_t cut, double k16,
-                                           int top_bin, float end, const double* table, double base,
-                                           double target, Shared& sh) {
+__device__ __forceinline__ int draw_binned(const LogitRow<T>& r, int j0, int j1, uint64_t cut, float m,
+                                           double k16, int top_bin, float end, const double* table,
+                                           double base, double target, Shared& sh) {
   constexpr int N = LogitRow<T>::N, W = NT / kWave;
   static_assert(32 * kHeadThreads / N / NT * W <= kWave);
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
@@ -792,7 +809,7 @@ __device__ __forceinline__ int draw_binned(const LogitRow<T>& r, int j0, int j1,
       const float z = x[e];
       const double p = bin_series<false>(fmaxf(z, end), k16, c5, n) * table[top_bin - n];
       const bool kept = z > end && (cut == 0 || z > cz || (z == cz && r.column(j) + e <= cc));
-      w[e] = kept ? p : 0.;
+      w[e] = kept ? z == m ? 1. : p : 0.;
       s += w[e];
     }
     return s;
@@ -921,25 +938,29 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   float end = 0.f, over = INFINITY;   // the values of the border bin: end <= z < over
   bool by_p = false;   // whether top_p's cut lies in it
   auto bin_weight = [&](int b) { return exp2_64(-double(b) / 16.); };
-  // 2^-48 of the top bin's middle, relative to the greatest entry's weight.
-  const double unit = binned ? exp2((double(top_bin) - double(m) * k16) / 16.) * kMassUnit : 0.;
+  TopWeight top{1., 1.};
+  if (binned) {
+    int n;
+    top.w0 = double(weight_in_bin(m, k16, mass_coefficient(kBits), n));
+    top.inv = 1. / top.w0;
+  }
   const uint64_t* masses = h.mass + at * h.chunks * kMassBins;
-  auto mass_at = [&](int c, int b) -> double {   // of chunk c in the row's bin b
+  auto mass_at = [&](int c, int b) -> uint64_t {   // of chunk c in the row's bin b
     const int i = b - (top_bin - sh.part[c].top_bin);
     const bool is = i >= 0 && i < sh.part[c].bins;
     const uint64_t n = masses[int64_t(c) * kMassBins + (is ? i : 0)];   // loaded in any case
-    return is ? double(n) : 0.;
+    return is ? n : 0ull;
   };
   if constexpr (LISTS) {
     // P consecutive bins a thread, of sixteen loads in flight together.
     auto join_masses = [&](auto bins_each) __attribute__((always_inline)) {
       constexpr int P = decltype(bins_each)::value, AHEAD = 16 / P;
-      double v[P], sum = 0.;
+      double v[P], lo[P], sum = 0.;   // high and low halves: exact sums
 #pragma unroll
-      for (int e = 0; e < P; ++e) v[e] = 0.;
+      for (int e = 0; e < P; ++e) v[e] = lo[e] = 0.;
 #pragma unroll 1
       for (int c0 = 0; c0 < h.chunks; c0 += AHEAD) {
-        double x[AHEAD][P];
+        uint64_t x[AHEAD][P];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
@@ -947,12 +968,16 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-          for (int e = 0; e < P; ++e) v[e] += c0 + i < h.chunks ? x[i][e] : 0.;
+          for (int e = 0; e < P; ++e) {
+            const uint64_t n = c0 + i < h.chunks ? x[i][e] : 0ull;
+            v[e] += double(uint32_t(n >> 32));
+            lo[e] += double(uint32_t(n));
+          }
       }
       if (tid == 0) sh.pick = kMassBins, sh.last = 0, sh.last_m = 0;
 #pragma unroll
       for (int e = 0; e < P; ++e) {
-        v[e] *= bin_weight(P * tid + e) * unit;
+        v[e] = top.over(v[e], lo[e]) * bin_weight(P * tid + e);
         sum += v[e];
       }
       const double run = block_scan<W>(sum, sh.red.d, whole_w);
@@ -1023,9 +1048,9 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     __syncthreads();
     for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
       const int b = b0 + tid;
-      double any = 0.;
-      for (int c = 0; b < border && c < h.chunks; ++c) any += mass_at(c, b);
-      note_last(any > 0., b, &sh.last);
+      uint64_t any = 0;
+      for (int c = 0; b < border && c < h.chunks; ++c) any |= mass_at(c, b);
+      note_last(any != 0, b, &sh.last);
     }
     __syncthreads();
     border = sh.last;
@@ -1057,10 +1082,20 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
       __syncthreads();
       k = has_k ? s.top_k : n;
-      if (binned ? by_p : has_p) {
+      if (binned && by_p) {   // as the histograms count them
+        static_assert(kInOrder <= NT);
+        int bin;
+        const float z = tid < n ? entry_logit(sh.list[tid]) : INFINITY;
+        const uint64_t own = z < over ? weight_in_bin(z, k16, mass_coefficient(kBits), bin) : 0ull;
+        uint64_t all;
+        if (tid == 0) sh.pick = n - 1;
+        const uint64_t run = block_scan<W>(own, sh.red.u, all);
+        note_first(own != 0 && above + top.over(run) * bin_weight(border) >= target_p, tid, &sh.pick);
+        __syncthreads();
+        k = min(k, sh.pick + 1);
+      } else if (!binned && has_p) {
         double sum;
-        const int p = reach<NT, false>(k, binned ? -1. : double(s.top_p), target_p, sum, sh,
-                                       [&](int i) { return sh.weight[i]; });
+        const int p = reach<NT, false>(k, double(s.top_p), sum, sh, [&](int i) { return sh.weight[i]; });
         k = min(k, p + 1);
       }
       if (cut_m != 0) {
@@ -1078,7 +1113,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
       __syncthreads();
       sort_list<NT>(sh.list, k);
       double mass;
-      int i = reach<NT, true>(k, u, 0., mass, sh, [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
+      int i = reach<NT, true>(k, u, mass, sh, [&](int q) { return sh.weight[sh.list[q] & 4095u]; });
       if (i == k) i = sh.last;   // rounding left none: the last with a weight
       write(uint32_t(k), low, mass, int(kColumnMask - uint32_t(sh.list[i] >> 12)));
       return;
@@ -1101,7 +1136,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           if (by_p)
             cut = most64(cut, border_entry<NT>(n, uint64_t(f32_order_key(end)) << kColumnBits,
                                                uint64_t(f32_order_key(over)) << kColumnBits, k16, above,
-                                               bin_weight(border) * unit, target_p, sh));
+                                               top, bin_weight(border), target_p, sh));
           uint64_t low = kKeyTop;
           uint32_t kept = 0;
           for (int i = tid; i < n; i += NT) {
@@ -1134,23 +1169,24 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         // Weights of the bins' middles, relative to the greatest entry's, over the border's entries.
         double* table = reinterpret_cast<double*>(sh.border);
         for (int b = tid; b < kMassBins; b += NT)
-          table[b] = b < kKeptBins ? bin_weight(b) * (unit / kMassUnit) : 0.;
+          table[b] = b < kKeptBins ? bin_weight(b) : 0.;
         __syncthreads();
 #pragma unroll 1
         for (int c = wid; c < h.chunks; c += W) {
-          double w = lane == 0 && n > 0 ? double(sh.chunk_n[c]) * (table[border] * kMassUnit) : 0.;
+          double w = lane == 0 && n > 0 ? top.over(sh.chunk_n[c]) * table[border] : 0.;
 #pragma unroll 1
           for (int b0 = lane; b0 < border; b0 += 256) {
-            double v[4];
+            uint64_t v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = b0 + 64 * i < border ? mass_at(c, b0 + 64 * i) : 0.;
+            for (int i = 0; i < 4; ++i) v[i] = b0 + 64 * i < border ? mass_at(c, b0 + 64 * i) : 0ull;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w += v[i] * (table[min(b0 + 64 * i, kMassBins - 1)] * kMassUnit);
+            for (int i = 0; i < 4; ++i) w += top.over(v[i]) * table[min(b0 + 64 * i, kMassBins - 1)];
           }
           w = wave_fold(w, add);
           if (lane == 0) sh.chunk[c] = w;
         }
         __syncthreads();
+        for (int b = tid; b < kMassBins; b += NT) table[b] *= top.inv / kMassUnit;   // for the draw
         // The draw: only the chunk that the running sum passes the target in is read.
         const double w = tid < h.chunks ? sh.chunk[tid] : 0.;
         double mass;
@@ -1168,7 +1204,8 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
           __syncthreads();
           const int j0 = c * h.vectors, j1 = min(r.vectors(), j0 + h.vectors);
           const float far = m - float(double(s.t) * kLog16) * float(kKeptBins + 4);
-          tok = draw_binned<NT, PHASE == kAll ? 4 : 2>(r, j0, j1, cut, k16, top_bin, far, table, sh.sum, target, sh);
+          tok = draw_binned<NT, PHASE == kAll ? 4 : 2>(r, j0, j1, cut, m, k16, top_bin, far, table,
+                                                           sh.sum, target, sh);
         }
         write(greater, cut, mass, tok);
         return;

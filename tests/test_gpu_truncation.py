@@ -4,6 +4,8 @@ Draws, cuts and identities are whole numbers and have to be equal: both sides su
 no row is built so that a cut falls within 1e-9 of a border unless its sums are exact.  The
 log-sum-exps are 64-bit: the kernels' exponentials drop less than 1e-14 of a term and the sums
 of V terms round by V * 2^-53 at most, so 1e-10 relative to max(1, |lse|) covers 2^17 columns."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -164,6 +166,35 @@ def test_many_equal_entries():
     for kw in (dict(), dict(top_p=0.5), dict(top_k=30001), dict(top_k=1), dict(min_p=1.0),
                dict(top_k=50000, top_p=0.25), dict(temperature=1e-4, top_p=0.7)):
         _check_draws(z, _u(6, 2), **kw)
+
+
+@pytest.mark.parametrize("V", [2, 56, 640, 4096, 8192, 32768, 131072])
+@pytest.mark.parametrize("n", [3, 258])
+def test_equal_entries_on_the_border(n, V):
+    """Rows of equal logits, alone, above ones that weigh nothing and among masked ones: a nucleus of
+    a dyadic share holds exactly that many, and a uniform on the border between two tokens takes the
+    second: n weights of one sum to n."""
+    z = torch.full((n, V), 3.7, device=DEV)
+    z[1, V // 2:] = -1e4
+    z[2, ::2] = -np.inf
+    z[2] -= 90.3
+    live = [np.arange(V), np.arange(V // 2), np.arange(1, V, 2)]   # the equal ones, as columns
+    for dtype in (torch.float32, torch.bfloat16):
+        x = z.to(dtype)
+        for T in (1.0, 0.7):
+            for kw in (dict(top_p=0.5), dict(top_p=0.25), dict(top_p=0.75), dict(min_p=1.0),
+                       dict(top_k=max(1, V // 4), top_p=0.5)):
+                for at in (0.5, 0.25, 3 / 128):
+                    tok, cut = hdf.sample_truncated(x, torch.full((n,), at, device=DEV), temperature=T,
+                                                    **kw)
+                    for r, cols in enumerate(live):
+                        # n weights of one sum to n: the first to pass u n is number floor(u n).
+                        most = min(len(cols), kw.get("top_k", V))
+                        want = math.ceil(most * kw.get("top_p", 1.0))
+                        assert int(cut.kept[r]) == want, (r, kw)
+                        assert int(tok[r]) == cols[math.floor(at * want)], (r, kw, at)
+                        every = want == (len(cols) if r != 1 else V)
+                        assert int(cut.cut_index[r]) == (-1 if every else cols[want - 1])
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
