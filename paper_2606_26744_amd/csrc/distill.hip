@@ -24,17 +24,20 @@ constexpr int kDistElems = 32;                              // of a part, a thre
 constexpr int kDistPart = kDistThreads * kDistElems;        // columns of a part
 constexpr int kMaxTop = 1024;                               // K at most
 
-// What a part of a row adds: its greatest logit m; the sums of e^((z - mt) / T) over all columns and
-// over the unlisted ones, and of e^(z - m1), mt and m1 being m but for rounding.
+// What a part of a row adds, with a bucket its unlisted columns alone (they may all lie hundreds of
+// octaves below the listed ones, and the bucket's gradient is spread by their softmax): the greatest
+// logit m, the sums of e^((z - mt) / T) and of e^(z - m1), mt and m1 being m but for rounding.
 struct DistPart {
   float m;
-  double mt, m1, st, out, s1;
+  double mt, m1, st, s1;
 };
 
 // A supervised slot's statistics for the backward pass.
 struct DistRow {
-  float m, inv_t, inv_1;   // greatest logit; one over the sums at temperatures T and 1
-  float outside;           // 1 - p_r / q_r, the factor of unlisted tokens (1 without the bucket)
+  float m, inv_t, inv_1;   // greatest logit; one over the sums at temperatures T and 1, relative to it
+  float mu, unlisted;      // the columns' greatest, with a bucket the unlisted ones'; relative to it,
+                           // 1 / (sum at T) less p_r / (unlisted sum)
+  float shift;             // e^(mu - m)
   int kl, ce;              // whether the slot has either loss
 };
 
@@ -69,7 +72,7 @@ __global__ void __launch_bounds__(kDistThreads)
 distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts, uint32_t* done) {
   constexpr int N = LogitRow<T>::N, G = kDistElems / N;
   __shared__ uint32_t listed[kDistPart / 32];
-  __shared__ float shf[kDistWaves], sums[kDistWaves][3];
+  __shared__ float shf[kDistWaves], sums[kDistWaves][2];
   const int part = blockIdx.x;
   const int64_t i = blockIdx.y, s = i / slots;
   const int k = int(i - s * slots) + 1;
@@ -100,6 +103,18 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts, uint32_
       if (id >= 0 && id < a.V && b >= 0 && b < kDistPart) atomicOr(&listed[b >> 5], 1u << (b & 31));
     }
   }
+  if (bucket) {
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int at = (g * kDistThreads + int(threadIdx.x)) * N;
+      const uint32_t is = listed[at >> 5] >> (at & 31) & ((1u << N) - 1);
+      if (is != 0) {   // few
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[g][e] = (is >> e) & 1u ? -INFINITY : x[g][e];
+      }
+    }
+  }
   float m = -INFINITY;
 #pragma unroll
   for (int g = 0; g < G; ++g)
@@ -112,10 +127,9 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts, uint32_
   const float ref = m == -INFINITY ? 0.f : m, log2e = 1.44269504f;
   const bool far = !(fabsf(ref) * fmaxf(soft ? a.c2 : 0.f, log2e) < 1e6f);
   const bool hard = a.labels != nullptr && !(soft && a.t == 1.f);
-  // Over the whole row at T = 1, the unlisted and the listed (with the bucket) columns: 32-bit sums
-  // of N values, then of few of those and over the wave, at most 15 additions in a row; 64-bit
-  // beyond.
-  float sum[3] = {0.f, 0.f, 0.f};
+  // At T = 1 and at T: 32-bit sums of N values, then of few of those and over the wave, at most 15
+  // additions in a row; 64-bit beyond.
+  float sum[2] = {0.f, 0.f};
   auto weight = [&](bool is_far, float z, float c, float b) {
     return __builtin_amdgcn_exp2f(is_far ? (z - ref) * c : fmaf(z, c, -b));
   };
@@ -138,43 +152,25 @@ distill_part_kernel(DistArgs a, int slots, DistPart* __restrict__ parts, uint32_
     return far ? exps_of(std::true_type(), c) : exps_of(std::false_type(), c);
   };
   if (hard) sum[0] = exps(log2e);
-  if (soft) {
-    if (bucket) {
+  if (soft) sum[1] = exps(a.c2);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const int at = (g * kDistThreads + int(threadIdx.x)) * N;
-        const uint32_t is = listed[at >> 5] >> (at & 31) & ((1u << N) - 1);
-        if (is != 0) {   // few
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if ((is >> e) & 1u) {
-              sum[2] += weight(far, x[g][e], a.c2, ref * a.c2);
-              x[g][e] = -INFINITY;
-            }
-        }
-      }
-    }
-    sum[1] = exps(a.c2);
-  }
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const float t = wave_fold(sum[i], [](float u, float v) { return u + v; });
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6][i] = t;
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
   if (part == 0 && i == 0) *done = 0;   // of the next launch
-  double t[3] = {0., 0., 0.};
+  double t[2] = {0., 0.};
 #pragma unroll
   for (int w = 0; w < kDistWaves; ++w)
 #pragma unroll
-    for (int i = 0; i < 3; ++i) t[i] += double(sums[w][i]);
+    for (int i = 0; i < 2; ++i) t[i] += double(sums[w][i]);
   DistPart o;
   o.m = m;
   o.mt = far ? double(ref) : double(ref * a.c2) / double(a.c2);
   o.m1 = far ? double(ref) : double(ref * log2e) / double(log2e);
-  o.out = t[1];
-  o.st = t[1] + t[2];
+  o.st = t[1];
   o.s1 = hard ? t[0] : o.st;
   parts[i * gridDim.x + part] = o;
 }
@@ -250,12 +246,12 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
                    DistSaved sv, uint32_t* done) {
   constexpr int Q = 4, W = NT / kWave;   // listed tokens of a thread, at most
   __shared__ int hash_id[2 * Q * NT], hash_at[2 * Q * NT];
-  __shared__ double sh3[W][3], sh4[W][4], sh1[W][1];
+  __shared__ double sh3[W][3], sh4[W][4], sh5[W][5], sh1[W][1];
   __shared__ uint32_t order;
   const int64_t i = blockIdx.x, s = i / slots;
   const int k = int(i - s * slots) + 1, tid = threadIdx.x;
   const LogitRow<T> r(static_cast<const T*>(a.z) + (s * a.B + k) * a.ld, a.V);
-  const bool soft = k <= a.P;
+  const bool soft = k <= a.P, bucket = soft && a.rest != nullptr, one = soft && a.t == 1.f;
   const int64_t q = s * a.P + k - 1;
   int id[Q], slot[Q];
   double l[Q], z[Q];   // the teacher's logits over T, the student's
@@ -274,7 +270,7 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
       l[e] = t < a.K ? double(tl[t]) * inv_t : -INFINITY;
       if (id[e] >= a.V) id[e] = -1;
     }
-    if (a.rest != nullptr) lr = double(a.rest[q]);
+    if (bucket) lr = double(a.rest[q]);
   }
   const DistPart* pt = parts + i * n_parts;
   DistPart first;
@@ -286,7 +282,8 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
     label = a.labels[s * (a.B - 1) + k - 1];
     if (label >= 0 && label < a.V) label_z = double(r.raw(label));
   }
-  double v[3] = {-INFINITY, -INFINITY, 0.};   // greatest logit, the teacher's; its NaNs
+  double v[4] = {-INFINITY, -INFINITY, 0., -INFINITY};   // greatest logit of the parts, the teacher's;
+                                                         // its NaNs; the greatest of all
   v[0] = double(first.m);
   for (int j = tid + NT; j < n_parts; j += NT) v[0] = fmax(v[0], double(pt[j].m));
   int mask = 127;   // of the hash table: at least twice as many slots as tokens
@@ -320,37 +317,53 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
       if (id[e] >= 0 && hash_at[slot[e]] != e * NT + tid) id[e] = -1;
       if (id[e] < 0) continue;
       v[1] = fmax(v[1], l[e]);
+      v[3] = fmax(v[3], z[e]);
       v[2] += l[e] != l[e] ? l[e] : 0.;
     }
   }
-  fold_all(v, sh3, [](int e, double x, double y) { return e < 2 ? fmax(x, y) : x + y; });
-  const double ref = v[0] == -INFINITY ? 0. : v[0], top = v[1], bad = v[2];
+  fold_all(v, sh4, [](int e, double x, double y) { return e != 2 ? fmax(x, y) : x + y; });
+  const double mu = v[0] == -INFINITY ? 0. : v[0], top = v[1], bad = v[2];
+  const double most = fmax(v[0], v[3]), ref = most == -INFINITY ? 0. : most;
   const bool taught = soft && (top > -INFINITY || bad != 0.);   // some mass, or a NaN to pass on
   const double c2 = 1.4426950408889634074 / double(a.t);
-  double u[4] = {0., 0., 0., 0.};   // st, out, s1; the teacher's sum
+  constexpr double log2e = 1.4426950408889634074;
+  // The parts' sums at T and at 1 (relative to mu), the teacher's, the listed tokens' (to the greatest).
+  double u[5] = {0., 0., 0., 0., 0.};
   auto join = [&](const DistPart& o) {
     if (o.m == -INFINITY && o.st == o.st && o.s1 == o.s1) return;
-    const double wt = exp2_64((o.mt - ref) * c2);
+    const double wt = exp2_64((o.mt - mu) * c2);
     u[0] += o.st * wt;
-    u[1] += o.out * wt;
-    u[2] += soft && a.t == 1.f ? o.s1 * wt : o.s1 * exp2_64((o.m1 - ref) * 1.4426950408889634074);
+    u[1] += one ? o.s1 * wt : o.s1 * exp2_64((o.m1 - mu) * log2e);
   };
   if (tid < n_parts) join(first);
   for (int j = tid + NT; j < n_parts; j += NT) join(pt[j]);
   const double er = lr == -INFINITY || !taught ? 0. : exp(lr - top);
   double w[Q];
   if (taught) {
-    u[3] = tid == 0 ? er : 0.;
+    u[2] = tid == 0 ? er : 0.;
 #pragma unroll
     for (int e = 0; e < Q; ++e) {
       w[e] = id[e] >= 0 ? exp(l[e] - top) : 0.;
-      u[3] += w[e];
+      u[2] += w[e];
     }
   }
-  fold_all(u, sh4, [](int, double x, double y) { return x + y; });
-  const double st = u[0], out = u[1], s1 = u[2], sum = u[3];
+  if (bucket) {
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      if (id[e] < 0 || z[e] == -INFINITY) continue;
+      const double nan = z[e] != z[e] ? z[e] : 0.;   // which the powers do not pass on
+      u[3] += exp2_64((z[e] - ref) * c2) + nan;
+      u[4] += exp2_64((z[e] - ref) * log2e) + nan;
+    }
+  }
+  fold_all(u, sh5, [](int, double x, double y) { return x + y; });
+  const double out = u[0], sum = u[2], to = (mu - ref) * inv_t;   // log of e^(mu / T) over e^(ref / T)
+  const double st = out * exp2_64((mu - ref) * c2) + u[3];
+  const double s1 = u[1] * exp2_64((mu - ref) * log2e) + u[4];
   // A row masked throughout has no softmax: its factors are 0, as its exponentials.
-  DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), 1.f, 0, 0};
+  DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), float(mu),
+              0.f, float(exp2_64((mu - ref) * log2e)), 0, 0};
+  double unlisted = st == 0. ? 0. : exp2_64((mu - ref) * c2) / st;
   if (soft) {
     float* ps = sv.p + q * a.K;
     double kl[1] = {0.};
@@ -371,9 +384,9 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
       }
       if (tid == 0 && er != 0.) {
         const double p = er / sum;
-        const double lq = out == 0. ? -INFINITY : log(out) - log_st;
+        const double lq = out == 0. ? -INFINITY : log(out) + to - log_st;
         kl[0] += p * (lr - top - log_sum - lq);
-        if (out != 0.) row.outside = float(1. - p * st / out);
+        if (out != 0.) unlisted -= p / out;
       }
       row.kl = 1;
     } else {
@@ -391,6 +404,7 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
       }
       put(a.ce + s * (a.B - 1) + k - 1, float(ce));
     }
+    row.unlisted = float(unlisted);
     sv.rows[s * (a.B - 1) + k - 1] = row;
     if (done != nullptr) {   // counted once they are in memory
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -425,7 +439,7 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
   const int j0 = part * (kDistPart / N), nv = r.vectors();
   // Weights of the slot's losses: the means' upstream gradients and the losses' own.
   float wk = 0.f, wc = 0.f;
-  DistRow st{0.f, 0.f, 0.f, 1.f, 0, 0};
+  DistRow st{0.f, 0.f, 0.f, 0.f, 0.f, 1.f, 0, 0};
   int label = -1;
   if (k >= 1) {
     const int64_t q = s * (a.B - 1) + k - 1;
@@ -445,7 +459,10 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
   }
   const bool soft = wk != 0.f, hard = wc != 0.f, one = a.t == 1.f;
   const float log2e = 1.44269504f;
-  const float ct = wk * st.inv_t, co = ct * st.outside, c1 = wc * st.inv_1;
+  const float ct = wk * st.inv_t, cu = wk * st.unlisted, c1 = wc * st.inv_1;
+  // What the columns' exponentials are relative to: with a bucket the greatest unlisted one (the
+  // listed ones are written after).
+  const float mu = soft ? st.mu : st.m, shift = soft ? st.shift : 1.f;
   auto at_t = [&](float x) { return soft ? __builtin_amdgcn_exp2f((x - st.m) * a.c2) : 0.f; };
   auto at_1 = [&](float x) { return hard ? __builtin_amdgcn_exp2f((x - st.m) * log2e) : 0.f; };
   float x[G][N];
@@ -464,27 +481,27 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
   }
   // As in the forward pass, an exponential costs one product where z c is not too far out; what
   // rounding adds to the product of m and c goes into the factor.
-  const bool far = !(fabsf(st.m) * fmaxf(soft ? a.c2 : 0.f, log2e) < 1e6f);
+  const bool far = !(fmaxf(fabsf(mu), fabsf(st.m)) * fmaxf(soft ? a.c2 : 0.f, log2e) < 1e6f);
   auto sums = [&](auto is_far, auto two, float c, float k, float k1) __attribute__((always_inline)) {
     constexpr bool FAR = decltype(is_far)::value;
-    const float b = st.m * c, b1 = st.m * log2e;
+    const float b = mu * c, b1 = st.m * log2e;
     if (!FAR) {
-      k *= __builtin_amdgcn_exp2f(-fmaf(st.m, c, -b));
+      k *= __builtin_amdgcn_exp2f(-fmaf(mu, c, -b));
       k1 *= __builtin_amdgcn_exp2f(-fmaf(st.m, log2e, -b1));
     }
 #pragma unroll
     for (int h = 0; h < G; ++h)
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float z = x[h][e], d = z - st.m;
-        float v = __builtin_amdgcn_exp2f(FAR ? d * c : fmaf(z, c, -b)) * k;
+        const float z = x[h][e];
+        float v = __builtin_amdgcn_exp2f(FAR ? (z - mu) * c : fmaf(z, c, -b)) * k;
         if (decltype(two)::value)
-          v = fmaf(__builtin_amdgcn_exp2f(FAR ? d * log2e : fmaf(z, log2e, -b1)), k1, v);
+          v = fmaf(__builtin_amdgcn_exp2f(FAR ? (z - st.m) * log2e : fmaf(z, log2e, -b1)), k1, v);
         x[h][e] = v;
       }
   };
   const bool two = soft && hard && !one;
-  const float c = soft ? a.c2 : log2e, k1 = hard ? c1 : 0.f, kt = (soft ? co : 0.f) + (two ? 0.f : k1);
+  const float c = soft ? a.c2 : log2e, k1 = hard ? c1 : 0.f, kt = (soft ? cu : 0.f) + (two ? 0.f : k1 * shift);
   if (two && far)
     sums(std::true_type(), std::true_type(), c, kt, k1);
   else if (two)
@@ -536,7 +553,8 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
   __syncthreads();
   if (tid == 0 && hard && !label_done && label >= c0 && label < c1_) {
     const float z = r.raw(label);
-    store_grad(d + label, (soft ? at_t(z) * co : 0.f) + at_1(z) * c1 - wc);
+    const float u = soft ? __builtin_amdgcn_exp2f((z - mu) * a.c2) * cu : 0.f;
+    store_grad(d + label, u + at_1(z) * c1 - wc);
   }
 }
 

@@ -228,6 +228,44 @@ def test_students_far_from_zero(T):
     _check(c, B, T)
 
 
+@pytest.mark.parametrize("T", [1.0, 0.125])
+def test_unlisted_columns_far_below_the_listed_ones(T):
+    """A student all of whose unlisted columns vanish beside the listed ones: the bucket's divergence
+    is finite, and its gradient is spread over them by their own softmax, by formula in 64 bits."""
+    n, B, P, K, V = 2, 4, 3, 6, 700
+    for dtype in (torch.float32, torch.bfloat16):
+        c = _case(n, B, P, K, V, 21, dtype, labels=False, T=T)
+        z = c["z"].view(n, B, V)
+        for s in range(n):
+            for k in range(1, P + 1):
+                z[s, k, c["ids"][s, k - 1].long()] += 200.0 * (s + 1)
+        c["rest"][:] = c["val"][:, :, 0] / T - 1.0       # a bucket of weight
+        kl, _, _, saved = hdf.distill_forward(c["z"], c["ids"], c["val"], c["rest"], B=B, temperature=T)
+        d = hdf.distill_backward(c["z"], c["ids"], None, saved, B=B, temperature=T,
+                                 grad_kl=torch.ones(n, P, device=DEV))
+        step = torch.finfo(dtype).eps / 2
+        for s in range(n):
+            for k in range(1, P + 1):
+                x = _np(z[s, k]) / T
+                toks, p, pr = od.teacher(c["ids"][s, k - 1].tolist(), _np(c["val"])[s, k - 1],
+                                         float(c["rest"][s, k - 1]), V, T)
+                want, grad = od.slot_kl(_np(z[s, k]), c["ids"][s, k - 1].tolist(),
+                                        _np(c["val"])[s, k - 1], float(c["rest"][s, k - 1]), T)
+                assert np.isfinite(want)
+                assert abs(float(kl[s, k - 1]) - want) <= 4 * REL + 2.0 ** -24 * abs(want)
+                inside = np.zeros(V, bool)
+                inside[toks] = True
+                far = np.where(inside, -np.inf, x)
+                spread = np.exp(far - far.max())
+                spread /= spread.sum()
+                grad = -pr * spread / T              # q itself is beyond 64 bits, or next to it
+                q = np.exp(x - x.max())
+                grad[inside] = ((q / q.sum())[inside] - p[np.argsort(toks)]) / T
+                got = _np(d.view(n, B, V)[s, k])
+                mag = np.where(inside, 2.0, pr * spread) / T
+                assert (np.abs(got - grad) <= GREL * mag * (1 + step) + step * np.abs(grad) + 1e-37).all()
+
+
 @pytest.mark.parametrize("n", [32, 33, 70])
 def test_means_over_few_and_many_slots(n):
     """Slots that one launch counts and more, over a workspace of arbitrary contents, used again."""
