@@ -1173,19 +1173,14 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         __syncthreads();
 #pragma unroll 1
         for (int c = wid; c < h.chunks; c += W) {
-          // (Exactly the top bin and the border's entries; the others' weights are no whole numbers.)
-          double w = 0.;
-          if (lane < 2) {
-            const uint64_t k = lane == 0 ? sh.chunk_n[c] : border > 0 ? mass_at(c, 0) : 0ull;
-            w = top.over(k) * (lane == 0 && n > 0 ? table[border] : 1.);
-          }
+          double w = lane == 0 && n > 0 ? top.over(sh.chunk_n[c]) * table[border] : 0.;
 #pragma unroll 1
-          for (int b0 = lane + 1; b0 < border; b0 += 256) {
+          for (int b0 = lane; b0 < border; b0 += 256) {
             uint64_t v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = b0 + 64 * i < border ? mass_at(c, b0 + 64 * i) : 0ull;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w += double(v[i]) * top.inv * table[min(b0 + 64 * i, kMassBins - 1)];
+            for (int i = 0; i < 4; ++i) w += top.over(v[i]) * table[min(b0 + 64 * i, kMassBins - 1)];
           }
           w = wave_fold(w, add);
           if (lane == 0) sh.chunk[c] = w;
