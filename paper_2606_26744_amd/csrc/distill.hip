@@ -322,8 +322,11 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
     }
   }
   fold_all(v, sh4, [](int e, double x, double y) { return e != 2 ? fmax(x, y) : x + y; });
-  const double mu = v[0] == -INFINITY ? 0. : v[0], top = v[1], bad = v[2];
+  const double top = v[1], bad = v[2];
   const double most = fmax(v[0], v[3]), ref = most == -INFINITY ? 0. : most;
+  // Without a column in the parts (all that are not listed are masked) the greatest of all: powers of
+  // mu - ref are then 1, where another value's could pass the range and make NaNs of zero sums.
+  const double mu = v[0] == -INFINITY ? ref : v[0];
   const bool taught = soft && (top > -INFINITY || bad != 0.);   // some mass, or a NaN to pass on
   const double c2 = 1.4426950408889634074 / double(a.t);
   constexpr double log2e = 1.4426950408889634074;
