@@ -419,10 +419,14 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
   if (order == gridDim.x - 1) distill_loss<NT, true>(a, sv, sh3);
 }
 
+// Rounded by the conversion instruction, which keeps a NaN of any bits one.
+__device__ __forceinline__ uint32_t bf16_bits(float v) {
+  return __builtin_bit_cast(uint16_t, __bf16(v));
+}
 template <typename T>
 __device__ __forceinline__ void store_grad(T* p, float v) {
   if constexpr (sizeof(T) == 2)
-    *p = __builtin_bit_cast(uint16_t, __bf16(v));
+    *p = bf16_t(bf16_bits(v));
   else
     *p = v;
 }
@@ -521,7 +525,7 @@ distill_grad_kernel(DistArgs a, DistGrad g, DistSaved sv) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (sizeof(T) == 2)
-          q[e] = pack_bf2(x[h][2 * e], x[h][2 * e + 1]);
+          q[e] = bf16_bits(x[h][2 * e]) | bf16_bits(x[h][2 * e + 1]) << 16;
         else
           q[e] = __float_as_uint(x[h][e]);
       }
