@@ -606,7 +606,8 @@ hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t l
  *              L_CE + alpha L_KL }
  * A slot whose teacher has no entry of finite logit has kl = 0 and no gradient.  A masked (-inf)
  * student logit has gradient 0 where it is not listed; one that the teacher gives mass makes kl
- * infinite.  A NaN among a slot's student or teacher logits makes its losses and gradients NaN.
+ * infinite.  A NaN or +inf among a slot's student logits makes its losses and all of its gradients
+ * NaN; among its teacher's, its kl and its gradients wherever kl has one.
  * Sums are 32-bit within a wave, over at most 15 additions in a row, 64-bit beyond; losses are
  * rounded once.
  * ----------------------------------------------------------------------------*/

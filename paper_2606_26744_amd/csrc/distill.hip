@@ -311,14 +311,14 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
     }
     __syncthreads();
     v[1] = tid == 0 ? lr : -INFINITY;
-    v[2] = tid == 0 && lr != lr ? lr : 0.;
+    v[2] = tid == 0 && lr != -INFINITY ? lr - lr : 0.;   // NaN of NaN and +inf, else 0
 #pragma unroll
     for (int e = 0; e < Q; ++e) {
       if (id[e] >= 0 && hash_at[slot[e]] != e * NT + tid) id[e] = -1;
       if (id[e] < 0) continue;
       v[1] = fmax(v[1], l[e]);
       v[3] = fmax(v[3], z[e]);
-      v[2] += l[e] != l[e] ? l[e] : 0.;
+      v[2] += l[e] != -INFINITY ? l[e] - l[e] : 0.;
     }
   }
   fold_all(v, sh4, [](int e, double x, double y) { return e != 2 ? fmax(x, y) : x + y; });
@@ -354,7 +354,7 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
 #pragma unroll
     for (int e = 0; e < Q; ++e) {
       if (id[e] < 0 || z[e] == -INFINITY) continue;
-      const double nan = z[e] != z[e] ? z[e] : 0.;   // which the powers do not pass on
+      const double nan = z[e] - z[e];   // of NaN and +inf, which the powers do not pass on; else 0
       u[3] += exp2_64((z[e] - ref) * c2) + nan;
       u[4] += exp2_64((z[e] - ref) * log2e) + nan;
     }
@@ -366,7 +366,7 @@ distill_row_kernel(DistArgs a, int slots, const DistPart* __restrict__ parts, in
   // A row masked throughout has no softmax: its factors are 0, as its exponentials.
   DistRow row{float(ref), st == 0. ? 0.f : float(1. / st), s1 == 0. ? 0.f : float(1. / s1), float(mu),
               0.f, float(exp2_64((mu - ref) * log2e)), 0, 0};
-  double unlisted = st == 0. ? 0. : exp2_64((mu - ref) * c2) / st;
+  double unlisted = (st == 0. ? 0. : exp2_64((mu - ref) * c2) / st) + bad;
   if (soft) {
     float* ps = sv.p + q * a.K;
     double kl[1] = {0.};

@@ -34,3 +34,23 @@ def test_nans_of_any_bits(bits, dtype):
         assert torch.isnan(d[B + 2]).all(), where
         others = [r for r in range(n * B) if r != B + 2]
         assert torch.isfinite(d[others]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["student listed", "student unlisted", "teacher"])
+def test_a_slot_with_one_is_not_a_number_throughout(where, value, rest, dtype):
+    n, B, P, V = 2, 4, 3, 701
+    c = base._case(n, B, P, 6, V, 5, dtype, rest=rest)
+    if where == "teacher":
+        c["val"][1, 1, 2] = value
+    else:
+        ids = c["ids"][1, 1].tolist()
+        c["z"][B + 2, ids[3] if where == "student listed" else
+               next(i for i in range(V) if i not in ids)] = value
+    kl, d = _grad(c, B, grad_kl=torch.ones(n, P, device=DEV))
+    assert torch.isnan(kl).view(-1).tolist() == [i == 4 for i in range(n * P)]
+    assert torch.isnan(d[B + 2]).all()
+    others = [r for r in range(n * B) if r != B + 2]
+    assert torch.isfinite(d[others]).all()
