@@ -550,6 +550,8 @@ size_t hdf_accept_truncated_workspace(int n_seq, int K, int vocab, hdf_dtype tar
  *     draft x_i is accepted iff u_i q_i(x_i) < p_i(x_i), in order (u_i = uniforms[s][i]);
  *     after n acceptances the next token is drawn with uniforms[s][K] from max(0, p_n - q_n) (from
  *     p_n where that is zero throughout), after K from p_K.
+ * Probabilities are taken from the log-sum-exps, to 2^-53 of those: 2^-27 at |lse| = 2^26, where T is
+ * about 1e-6.  Beyond, from the row itself, to 2^-40 whatever the temperature.
  * draft, draft_stride, ld   as hdf_accept_sample; a draft outside [0, vocab) is rejected
  * draft_logits   draft_dtype, the rows the drafts were drawn from
  * draft_cut_logit, draft_cut_index, draft_lse  [same rows]: their truncation under the same

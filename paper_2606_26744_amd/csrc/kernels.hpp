@@ -213,6 +213,20 @@ hipError_t launch_accept_sample(const int32_t* draft, int draft_stride, const fl
                                 int32_t* toks, void* ws, hipStream_t s);
 
 // ---------------------------------------------------------------- truncated rows (row_head.hip, row_cut.hip, verify.hip)
+// The drafts' rows of a verification: draft i of sequence s is row s * stride + i, entry s * K + i of
+// the outputs, which hold the greatest logit and the log-sum-exp relative to it of rows with far_lse().
+struct DraftRows {
+  const void* z;
+  bool bf16;
+  int64_t ld;
+  int stride, K;
+  int64_t n;                 // drafts of all sequences, 0 without a verification
+  const float* logit;
+  const int32_t* index;
+  const double* lse;
+  float* top;
+  double* log_sum;
+};
 struct CutArgs {
   const void* z;             // rows of V logits, stride ld
   int64_t rows, ld;
@@ -230,6 +244,10 @@ struct CutArgs {
   float* cut_logit;
   int32_t* cut_index;
   double* lse;
+  // Of a verification (else NULL): the greatest logits, the log-sum-exps relative to them.
+  float* top;
+  double* log_sum;
+  DraftRows drafts;
   // Top logits (at temperature t).
   int K;
   int32_t* ids;              // [rows][K]
@@ -253,10 +271,13 @@ struct VerifyArgs {
   const float* t_logit;      // their truncation (set by the launch)
   const int32_t* t_index;
   const double* t_lse;
+  const float *t_top, *d_top;    // of far rows: the greatest logit, the log-sum-exp relative to it
+  const double *t_log, *d_log;
   float t;
   const float* ts;           // [n_seq] or NULL
   const float* u;            // [n_seq][K+1]
-  int32_t* n_buf;            // [n_seq] accepted drafts, and the parts' sums (set by the launch)
+  int32_t* n_buf;            // [n_seq] accepted drafts, the cuts of the rows behind them, and the
+  void* cuts;                // parts' sums (set by the launch)
   double* sums;
   int32_t *acc, *anchor, *offs, *toks;
 };

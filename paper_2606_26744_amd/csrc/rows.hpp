@@ -130,6 +130,11 @@ __device__ __forceinline__ double entry_weight(float z, float m, double c2) {
   return z == m ? 1. : exp2_64((double(z) - double(m)) * c2);
 }
 
+// Whether a row's log-sum-exp is so far from 0 that its rounding, up to 2^-53 of it, is more than
+// 2^-27 of the probabilities that are taken from it: where T is about 1e-6 (or the logits are as
+// large).  At 2^53, T = 1e-14, nothing of them would be left.
+__device__ __forceinline__ bool far_lse(double lse) { return fabs(lse) > 67108864. && lse > -INFINITY; }
+
 // Another lane's value within the row of 16 (a DPP move; 64-bit values in two).
 template <int CTRL, int ROWS, typename X>
 __device__ __forceinline__ X dpp(X v) {

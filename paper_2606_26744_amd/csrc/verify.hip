@@ -13,15 +13,17 @@ namespace hdf {
 constexpr int kVerifyThreads = 256;    // one vector of a part each
 constexpr int kVerifyWaves = kVerifyThreads / kWave;
 
-// Probability of an entry under a row's truncation; lse2 = lse * log2(e).
+// A row's truncation: the probability of a kept entry is e^((z - ref) / T - lse).  ref = 0 and lse the
+// stored log-sum-exp, or, where that is far from 0 (far_lse), the row's greatest logit and the
+// log-sum-exp relative to it.
 struct RowCut {
   float logit;
   int index;
-  double lse2;
+  double ref, lse;
 };
-__device__ __forceinline__ double cut_prob(const RowCut& k, float z, int c, bool greedy, double c2) {
+__device__ __forceinline__ double cut_prob(const RowCut& k, float z, int c, bool greedy, double inv_t) {
   if (!(z > k.logit || (z == k.logit && c <= k.index)) || z == -INFINITY) return 0.;
-  return greedy ? 1. : exp2_64(double(z) * c2 - k.lse2);
+  return greedy ? 1. : exp2_64(fma(double(z) - k.ref, inv_t, -k.lse) * 1.4426950408889634074);
 }
 
 template <typename TD, typename TT>
@@ -29,44 +31,54 @@ struct VerifyRows {
   const VerifyArgs& a;
   int s;
   bool greedy;
-  double c2;
+  double inv_t;
   __device__ VerifyRows(const VerifyArgs& a_, int s_) : a(a_), s(s_) {
     const float t = a.ts != nullptr ? a.ts[s] : a.t;
     greedy = !(t > 0.f);
-    c2 = greedy ? 0. : 1.4426950408889634074 / double(t);
+    inv_t = greedy ? 0. : 1. / double(t);   // as the truncation took it: its rounding cancels
   }
-  __device__ const TT* target(int i) const {
-    return static_cast<const TT*>(a.tz) + (int64_t(s) * (a.K + 1) + i) * a.V;
+  __device__ LogitRow<TT> target(int i) const {
+    return {static_cast<const TT*>(a.tz) + (int64_t(s) * (a.K + 1) + i) * a.V, a.V};
   }
-  __device__ const TD* draft(int i) const {
-    return static_cast<const TD*>(a.dz) + (int64_t(s) * a.stride + i) * a.ld;
+  __device__ LogitRow<TD> draft(int i) const {
+    return {static_cast<const TD*>(a.dz) + (int64_t(s) * a.stride + i) * a.ld, a.V};
   }
   __device__ RowCut target_cut(int i) const {
     const int64_t r = int64_t(s) * (a.K + 1) + i;
-    return {a.t_logit[r], a.t_index[r], a.t_lse[r] * 1.4426950408889634074};
+    const double lse = a.t_lse[r];
+    const bool far = !greedy && far_lse(lse);
+    return {a.t_logit[r], a.t_index[r], far ? double(a.t_top[r]) : 0., far ? a.t_log[r] : lse};
   }
   __device__ RowCut draft_cut(int i) const {
-    const int64_t r = int64_t(s) * a.stride + i;
-    return {a.d_logit[r], a.d_index[r], a.d_lse[r] * 1.4426950408889634074};
+    const int64_t r = int64_t(s) * a.stride + i, e = int64_t(s) * a.K + i;
+    const double lse = a.d_lse[r];
+    const bool far = !greedy && far_lse(lse);
+    return {a.d_logit[r], a.d_index[r], far ? double(a.d_top[e]) : 0., far ? a.d_log[e] : lse};
   }
   // Weights of the next token's draw in vector j of target row n: the residual w and the target's
   // own p.
-  __device__ void weights(int n, int j, double w[LogitRow<TT>::N], double p[LogitRow<TT>::N]) const {
+  __device__ void weights(int n, int j, const RowCut& tc, const RowCut& dc, double w[LogitRow<TT>::N],
+                          double p[LogitRow<TT>::N]) const {
     constexpr int N = LogitRow<TT>::N;
-    const LogitRow<TT> t(target(n), a.V);
-    const LogitRow<TD> d(n < a.K ? draft(n) : nullptr, a.V);
+    const LogitRow<TT> t = target(n);
+    const LogitRow<TD> d = draft(n < a.K ? n : 0);
+    // Sums of equal rows that were taken in different orders differ by less than this, of the
+    // probabilities; stored ones do not differ.
+    const double least = tc.ref != 0. && dc.ref != 0. ? 0x1p-40 : 0.;
     float x[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) w[e] = p[e] = 0.;
     if (j >= t.vectors()) return;
     t.load(j, x);
-    const RowCut tc = target_cut(n), dc = n < a.K ? draft_cut(n) : tc;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const int c = t.column(j) + e;
-      p[e] = cut_prob(tc, x[e], c, greedy, c2);
+      p[e] = cut_prob(tc, x[e], c, greedy, inv_t);
       w[e] = p[e];
-      if (n < a.K && p[e] > 0.) w[e] = fmax(p[e] - cut_prob(dc, d.at(c), c, greedy, c2), 0.);
+      if (n < a.K && p[e] > 0.) {
+        w[e] = p[e] - cut_prob(dc, d.at(c), c, greedy, inv_t);
+        w[e] = w[e] > least * p[e] ? w[e] : 0.;
+      }
     }
   }
 };
@@ -90,8 +102,8 @@ verify_sum_kernel(VerifyArgs a) {
         const int x = a.draft[int64_t(s) * a.stride + i];
         double p = 0., q = 0.;
         if (x >= 0 && x < a.V) {
-          p = cut_prob(v.target_cut(i), LogitRow<TT>(v.target(i), a.V).at(x), x, v.greedy, v.c2);
-          q = cut_prob(v.draft_cut(i), LogitRow<TD>(v.draft(i), a.V).at(x), x, v.greedy, v.c2);
+          p = cut_prob(v.target_cut(i), v.target(i).at(x), x, v.greedy, v.inv_t);
+          q = cut_prob(v.draft_cut(i), v.draft(i).at(x), x, v.greedy, v.inv_t);
         }
         reject = !(double(a.u[int64_t(s) * (a.K + 1) + i]) * q < p);
       }
@@ -101,14 +113,19 @@ verify_sum_kernel(VerifyArgs a) {
         break;
       }
     }
-    if (threadIdx.x == 0) {
-      decided = n;
-      if (part == 0) a.n_buf[s] = n;
-    }
+    if (threadIdx.x == 0) decided = n;
   }
   __syncthreads();
+  const int n = decided;
+  const RowCut t = v.target_cut(n), d = n < a.K ? v.draft_cut(n) : t;
+  if (part == 0 && threadIdx.x == 0) {
+    a.n_buf[s] = n;
+    RowCut* cuts = static_cast<RowCut*>(a.cuts) + 2 * s;
+    cuts[0] = t;
+    cuts[1] = d;
+  }
   double w[LogitRow<TT>::N], p[LogitRow<TT>::N], sw = 0., sp = 0.;
-  v.weights(decided, part * kVerifyThreads + int(threadIdx.x), w, p);
+  v.weights(n, part * kVerifyThreads + int(threadIdx.x), t, d, w, p);
 #pragma unroll
   for (int e = 0; e < LogitRow<TT>::N; ++e) {
     sw += w[e];
@@ -136,6 +153,7 @@ verify_pick_kernel(VerifyArgs a, int parts) {
   const int s = blockIdx.x, tid = threadIdx.x;
   const VerifyRows<TD, TT> v(a, s);
   const int n = a.n_buf[s];
+  const RowCut t = static_cast<const RowCut*>(a.cuts)[2 * s], d = static_cast<const RowCut*>(a.cuts)[2 * s + 1];
   const double* sums = a.sums + int64_t(s) * parts * 2;
   auto add = [](auto x, auto y) { return x + y; };
   double sw = 0., sp = 0.;
@@ -176,8 +194,8 @@ verify_pick_kernel(VerifyArgs a, int parts) {
   __syncthreads();
   double w[LogitRow<TT>::N], p[LogitRow<TT>::N], mine = 0., all;
   const int j = part * kVerifyThreads + tid;
-  v.weights(n, j, w, p);
-  const int c = LogitRow<TT>(v.target(n), a.V).column(j);
+  v.weights(n, j, t, d, w, p);
+  const int c = v.target(n).column(j);
   int end = -1;
 #pragma unroll
   for (int e = 0; e < LogitRow<TT>::N; ++e) {
@@ -232,9 +250,9 @@ static int verify_parts(bool bf16, int V) {
 }
 
 size_t accept_truncated_ws_bytes(bool bf16, int n_seq, int K, int V) {
-  const size_t rows = size_t(n_seq) * (K + 1);
-  return cut_ws_bytes(bf16, int64_t(rows), V, false) + al256(rows * 8) + 3 * al256(rows * 4) + al256(size_t(n_seq) * 4) +
-         al256(size_t(n_seq) * verify_parts(bf16, V) * 16);
+  const size_t n = n_seq, rows = n * (K + 1), drafts = n * K;
+  return cut_ws_bytes(bf16, int64_t(rows), V, false) + 2 * al256(rows * 8) + 4 * al256(rows * 4) + al256(drafts * 8) +
+         al256(drafts * 4) + al256(n * 4) + al256(n * 2 * sizeof(RowCut)) + al256(n * verify_parts(bf16, V) * 16);
 }
 
 template <typename TD, typename TT>
@@ -248,7 +266,7 @@ static hipError_t launch_verify(const VerifyArgs& a, int n_seq, int parts, hipSt
 
 hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs a, CutArgs c,
                                    int n_seq, void* ws, hipStream_t s) {
-  const size_t rows = size_t(n_seq) * (a.K + 1);
+  const size_t rows = size_t(n_seq) * (a.K + 1), drafts = size_t(n_seq) * a.K;
   char* p = static_cast<char*>(ws);
   auto take = [&](size_t bytes) {
     char* q = p;
@@ -256,15 +274,24 @@ hipError_t launch_accept_truncated(bool draft_bf16, bool target_bf16, VerifyArgs
     return q;
   };
   c.lse = reinterpret_cast<double*>(take(rows * 8));
+  c.log_sum = reinterpret_cast<double*>(take(rows * 8));
+  c.top = reinterpret_cast<float*>(take(rows * 4));
   c.cut_logit = reinterpret_cast<float*>(take(rows * 4));
   c.cut_index = reinterpret_cast<int32_t*>(take(rows * 4));
   c.kept = reinterpret_cast<int32_t*>(take(rows * 4));
+  c.drafts = {a.dz, draft_bf16, a.ld, a.stride, a.K, int64_t(drafts), a.d_logit, a.d_index, a.d_lse,
+              reinterpret_cast<float*>(take(drafts * 4)), reinterpret_cast<double*>(take(drafts * 8))};
   a.n_buf = reinterpret_cast<int32_t*>(take(size_t(n_seq) * 4));
+  a.cuts = take(size_t(n_seq) * 2 * sizeof(RowCut));
   const int parts = verify_parts(target_bf16, a.V);
   a.sums = reinterpret_cast<double*>(take(size_t(n_seq) * parts * 16));
   a.t_logit = c.cut_logit;
   a.t_index = c.cut_index;
   a.t_lse = c.lse;
+  a.t_top = c.top;
+  a.t_log = c.log_sum;
+  a.d_top = c.drafts.top;
+  a.d_log = c.drafts.log_sum;
   const hipError_t e = launch_truncate(target_bf16, c, take(cut_ws_bytes(target_bf16, int64_t(rows), a.V, false)), s);
   if (e != hipSuccess) return e;
   if (draft_bf16)
