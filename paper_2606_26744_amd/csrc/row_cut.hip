@@ -12,7 +12,7 @@
 namespace hdf {
 
 constexpr int kBins = 2048;   // of the search
-constexpr double kSearchUnit = 1.0 / 8796093022208.0;   // 2^-43: sums of up to 2^20 weights fit 64 bits
+constexpr int kSearchBits = 43;   // of a weight: sums of up to 2^20 of them fit 64 bits
 constexpr uint64_t kKeyTop = (uint64_t(1) << (32 + kColumnBits)) - 1;
 
 // Entries of a border bin that are held at once.
@@ -194,9 +194,9 @@ __device__ __forceinline__ uint32_t least_value_key(float m, float near, F holds
 }
 
 // First-level bin of a value below the row's greatest one: 64 bins a unit of (m - z) / T, so
-// monotone in the value.
+// monotone in the value.  Halves: the difference of two finite values may not be one.
 __device__ __forceinline__ int value_bin(float z, float m, float scale) {
-  return z == m ? 0 : int(fminf((m - z) * scale, float(kBins - 1)));
+  return z == m ? 0 : int(fminf((0.5f * m - 0.5f * z) * (2.f * scale), float(kBins - 1)));
 }
 
 // Key of the entry with which the running sum, in order, of ones (BY_MASS false) or weights over
@@ -204,6 +204,10 @@ __device__ __forceinline__ int value_bin(float z, float m, float scale) {
 // Histograms of 2048 bins over ever smaller ranges of the order, until a bin's entries fit the
 // list: the first by value, further ones by key, where the last range is one key.  A caller that
 // knows the range of keys and the sum `above` it starts there (lo > 0).
+// A weight counts as a multiple of 2^-(43 + e), e the whole octaves by which all of its bin (of the
+// range, in those by key) stay below the row's greatest: to 2^-43 of itself, however light, down to
+// 2^-46 of the greatest; lighter ones, all in the last bin by value, to 2^-89.  Integers, so that a
+// bin's sum does not depend on its order; the bins' sums are added in 64-bit floating point.
 template <int NT, bool BY_MASS, typename T, typename Shared>
 __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t floor, float m,
                                  double c2, float scale, Shared& sh, uint64_t lo = 0,
@@ -214,16 +218,24 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
     while (((hi - lo) >> sh_) >= uint64_t(kBins)) ++sh_;
     return sh_;
   };
+  scale = fminf(scale, 1e38f);   // a finite one: no entry in a bin of lighter ones
+  auto octaves_of = [&]() {   // of the range; kKeyTop is no value's
+    return int(fmin((double(m) - double(fminf(entry_logit(hi), m))) * c2, 900.));
+  };
   int shift = lo > 0 ? shift_of() : -1, bin = 0;   // shift -1: the bins by value
+  int octaves = lo > 0 && BY_MASS ? octaves_of() : 0;
   for (;;) {
     for (int b = threadIdx.x; b < kBins; b += NT) {
       sh.count[b] = 0;
       sh.mass[b] = 0;
     }
-    if (threadIdx.x == 0) sh.pick = sh.last = 0, sh.before = 0;
+    if (threadIdx.x == 0) sh.pick = kBins, sh.last = 0;
     __syncthreads();
     auto bin_of = [&](float z, uint64_t k) {
       return shift < 0 ? value_bin(z, m, scale) : int((hi - k) >> shift);
+    };
+    auto bits_of = [&](int b) {   // log2(e) / 64 octaves a bin by value
+      return kSearchBits + (shift < 0 ? int(float(b) * 0.0225421f) : octaves);
     };
     each_entry<NT>(r, [&](float z, int c) {
       const uint64_t k = entry_key(z, c);
@@ -232,36 +244,38 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
       atomicAdd(&sh.count[b], 1u);
       if (BY_MASS)
         atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]),
-                  static_cast<unsigned long long>(entry_weight(z, m, c2) / kSearchUnit + 0.5));
+                  static_cast<unsigned long long>(ldexp(entry_weight(z, m, c2), bits_of(b)) + 0.5));
     });
     __syncthreads();
     const int b0 = PER * threadIdx.x;
-    uint64_t own = 0, whole;
+    auto sum_of = [&](int b) { return BY_MASS ? ldexp(double(sh.mass[b]), -bits_of(b)) : double(sh.count[b]); };
+    double own = 0., whole;
     int end = -1;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      own += BY_MASS ? sh.mass[b0 + e] : sh.count[b0 + e];
+      own += sum_of(b0 + e);
       end = sh.count[b0 + e] != 0 ? b0 + e : end;
     }
-    const uint64_t upto = block_scan<W>(own, sh.red.u, whole);
-    note_last(end >= 0, end, &sh.last);
-    __syncthreads();
-    const double unit = BY_MASS ? kSearchUnit : 1.;
-    auto reached = [&](uint64_t s) { return above + double(s) * unit >= target; };
-    const bool none = !reached(whole);
-    uint64_t after = upto - own;
+    const double before = above + (block_scan<W>(own, sh.red.d, whole) - own);
+    double upto = before;
+    int first = -1;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const uint64_t before = after;
-      after += BY_MASS ? sh.mass[b0 + e] : sh.count[b0 + e];
-      if (none ? b0 + e == sh.last : after > before && reached(after) && (before == 0 || !reached(before))) {
-        sh.pick = b0 + e;
-        sh.before = before;
-      }
+      const double v = sum_of(b0 + e);
+      upto += v;
+      first = first < 0 && v > 0. && upto >= target ? b0 + e : first;
+    }
+    note_first(first >= 0, first, &sh.pick);
+    note_last(end >= 0, end, &sh.last);
+    __syncthreads();
+    bin = min(sh.pick, sh.last);
+    if (int(threadIdx.x) == bin / PER) {
+      upto = before;
+      for (int b = b0; b < bin; ++b) upto += sum_of(b);
+      sh.sum = upto;
     }
     __syncthreads();
-    bin = sh.pick;
-    above += double(sh.before) * unit;
+    above = sh.sum;
     const uint32_t here = sh.count[bin];
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0, sh.pick = kListMax;
@@ -314,6 +328,7 @@ __device__ uint64_t select_entry(const LogitRow<T>& r, double target, uint64_t f
       lo = l > lo ? l : lo;
     }
     shift = shift_of();
+    if (BY_MASS) octaves = octaves_of();
     __syncthreads();
   }
 }
