@@ -639,7 +639,8 @@ hdf_status hdf_distill_forward(const void* student_logits, int64_t ld, hdf_dtype
  * The arguments that the forward pass had too are the same; saved is what it left.
  * grad_loss [3], grad_kl [n_seq][P], grad_ce [n_seq][B-1]  fp32, each may be NULL (zeros)
  * d_logits  dtype (out), rows as student_logits', row stride ldd; every row's vocab columns are
- *           written (zeros where a slot has no loss, slot 0 among them)
+ *           written (zeros where a slot has no loss, slot 0 among them).  No byte of its rows may be
+ *           one of student_logits' (interleaved rows are fine).
  * Gradients are formed in fp32 and rounded once. */
 hdf_status hdf_distill_backward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
                                 int n_seq, int B, int P, const int32_t* teacher_ids, int K,

@@ -1112,6 +1112,25 @@ hdf_status check_distill(const char* fn, const void* z, int64_t ld, hdf_dtype dt
   return HDF_OK;
 }
 
+// Whether any of the rows at a (stride lda elements) holds a byte of one of the rows at b; the rows of
+// either side lie apart, in rising order.
+bool rows_meet(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows, int vocab, int size) {
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t width = uintptr_t(vocab) * size;
+  auto start = [&](uintptr_t p, int64_t ld, int64_t r) { return p + uintptr_t(r) * uintptr_t(ld) * size; };
+  if (start(pa, lda, rows - 1) + width <= pb || start(pb, ldb, rows - 1) + width <= pa) return false;
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
+    const uintptr_t x = start(pa, lda, i), y = start(pb, ldb, j);
+    if (x + width <= y)
+      ++i;
+    else if (y + width <= x)
+      ++j;
+    else
+      return true;
+  }
+  return false;
+}
+
 hdf::DistArgs distill_args(const void* z, int64_t ld, int vocab, int n_seq, int B, int P,
                            const int32_t* ids, int K, const int32_t* labels, float T, float alpha) {
   hdf::DistArgs a{};
@@ -1171,8 +1190,8 @@ hdf_status hdf_distill_backward(const void* student_logits, int64_t ld, hdf_dtyp
   if (saved == nullptr) return fail(HDF_E_INVALID, "distill_backward: null saved");
   if ((reinterpret_cast<uintptr_t>(saved) & 255u) != 0)
     return fail(HDF_E_INVALID, "distill_backward: saved must be 256-byte aligned");
-  if (d_logits == student_logits)
-    return fail(HDF_E_INVALID, "distill_backward: d_logits must not be the logits");
+  if (rows_meet(student_logits, ld, d_logits, ldd, int64_t(n_seq) * B, vocab, dtype == HDF_BF16 ? 2 : 4))
+    return fail(HDF_E_INVALID, "distill_backward: d_logits must not share memory with the logits");
   hdf::DistArgs a = distill_args(student_logits, ld, vocab, n_seq, B, P, teacher_ids, K, labels,
                                  temperature, alpha);
   const hdf::DistGrad g{grad_loss, grad_kl, grad_ce, d_logits, ldd};
