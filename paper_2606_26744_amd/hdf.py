@@ -437,11 +437,22 @@ def _same_device(t: torch.Tensor, *others):
             raise ValueError("all tensors must be on one device")
 
 
+_INT_MAX = (1 << 31) - 1
+
+
+def _int32(value: int, what: str):
+    """ctypes cuts an integer to the low bits of its C type."""
+    if not -_INT_MAX <= value <= _INT_MAX:
+        raise ValueError(f"{what} must fit 32 bits")
+
+
 def _rows_of(t: torch.Tensor, what: str):
     """(rows, columns, row stride) of a matrix of logits with unit column stride."""
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what} must be [rows, vocab] with unit column stride")
     rows, V = t.shape
+    if rows > _INT_MAX or V > _INT_MAX:
+        raise ValueError(f"the rows and columns of {what} must fit 32 bits")
     ld = t.stride(0) if rows > 1 else max(t.stride(0), V)
     if ld < V:
         raise ValueError(f"{what} must not have overlapping rows")
@@ -474,6 +485,8 @@ def _truncation_params(like, n, rows_per_seq, *values):
                 _same_device(like, value)
             many[i] = value.data_ptr()
         elif value is not None:
+            if i == 1:
+                _int32(value, "top_k")
             one[i] = value
     return TruncationParams(*one, *many, rows_per_seq)
 
@@ -490,6 +503,7 @@ def sample_truncated(logits: torch.Tensor, uniforms: Optional[torch.Tensor] = No
     rows, V, ld = _rows_of(logits, "logits")
     if rows_per_seq < 1:
         raise ValueError("rows_per_seq must be positive")
+    _int32(rows_per_seq, "rows_per_seq")
     p = _truncation_params(logits, -(-rows // rows_per_seq), rows_per_seq, temperature, top_k,
                            top_p, min_p)
     with _place(logits, stream):
@@ -536,6 +550,8 @@ def accept_truncated(draft: torch.Tensor, draft_logits: torch.Tensor, draft_cut,
     if target_logits.dim() != 3 or target_logits.shape[1] != K + 1:
         raise ValueError("target_logits must be [n_seq, K+1, vocab]")
     n_seq, _, V = target_logits.shape
+    _int32(draft_stride, "draft_stride")
+    _int32(max(n_seq, V), "target_logits' sequences and columns")
     need = (n_seq - 1) * draft_stride + K if n_seq > 0 and K > 0 else 0
     d_rows, d_V, d_ld = _rows_of(draft_logits, "draft_logits")
     if need and (d_rows < need or d_V != V or (ld is not None and ld != d_ld and d_rows > 1)):
@@ -576,6 +592,7 @@ def top_logits(logits: torch.Tensor, K: int, *, temperature: float = 1.0, want_r
     values [rows, K] fp32, rest [rows] fp32 or None): the K largest logits of every row in order,
     and the log-sum-exp of the others at the temperature.  out: the same, preallocated."""
     rows, V, ld = _rows_of(logits, "logits")
+    _int32(K, "K")
     with _place(logits, stream):
         if out is None:
             dev = logits.device
