@@ -461,8 +461,10 @@ def _rows_of(t: torch.Tensor, what: str):
 
 def _scratch(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
     if ws is None or ws.numel() * ws.element_size() < need:
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=like.device)
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=like.device)
     _same_device(like, ws)
+    if not ws.is_contiguous():
+        raise ValueError("a workspace must be contiguous")
     return ws
 
 
