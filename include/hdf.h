@@ -563,7 +563,8 @@ size_t hdf_accept_truncated_workspace(int n_seq, int K, int vocab, hdf_dtype tar
  *                the accepted drafts and the drawn token (-1 from a row masked throughout)
  * ws, ws_bytes   at least hdf_accept_truncated_workspace(...) bytes, 256-byte aligned; its
  *                contents on entry do not matter.
- * Limits: 0 <= K <= 1024, 0 <= n_seq * (K + 1) <= 65535, 1 <= vocab <= 2^20. */
+ * Limits: 0 <= K <= 1024, 0 <= n_seq * (K + 1) <= 65535, 1 <= vocab <= 2^20; n_seq = 0 writes
+ *         nothing. */
 hdf_status hdf_accept_truncated(const int32_t* draft, int draft_stride, const void* draft_logits,
                                 hdf_dtype draft_dtype, int64_t ld, const float* draft_cut_logit,
                                 const int32_t* draft_cut_index, const double* draft_lse,
@@ -627,8 +628,8 @@ size_t hdf_distill_workspace(int n_seq, int B, int vocab, hdf_dtype dtype);
  * saved           hdf_distill_saved_bytes(...) bytes (out), 256-byte aligned
  * ws, ws_bytes    at least hdf_distill_workspace(...) bytes, 256-byte aligned; its contents on
  *                 entry do not matter.
- * Limits: 2 <= B <= 1025; 1 <= P <= B-1; 1 <= K <= 1024; n_seq * B <= 65535; 1 <= vocab <= 2^20;
- *         2^-100 <= temperature <= 2^100. */
+ * Limits: 2 <= B <= 1025; 1 <= P <= B-1; 1 <= K <= 1024; 0 <= n_seq * B <= 65535 (n_seq = 0 writes
+ *         nothing); 1 <= vocab <= 2^20; 2^-100 <= temperature <= 2^100. */
 hdf_status hdf_distill_forward(const void* student_logits, int64_t ld, hdf_dtype dtype, int vocab,
                                int n_seq, int B, int P, const int32_t* teacher_ids,
                                const float* teacher_logits, const float* teacher_rest, int K,

@@ -578,6 +578,8 @@ def accept_truncated(draft: torch.Tensor, draft_logits: torch.Tensor, draft_cut,
             _typed(t, torch.int32, k, what)
         _dev(draft, *cut[1:], target_logits, uniforms, acc, anc, offs, toks)
         _same_device(target_logits, draft, draft_logits, *cut[1:], uniforms, acc, anc, offs, toks)
+        if n_seq == 0 and offs is not None:   # the call writes nothing then
+            offs.view(-1)[:1].zero_()
         dt = _dt(target_logits)
         ws = _scratch(ws, int(lib().hdf_accept_truncated_workspace(n_seq, K, V, dt)), target_logits)
         _check(lib().hdf_accept_truncated(
@@ -653,7 +655,7 @@ def distill_forward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
             f32 = dict(dtype=torch.float32, device=student_logits.device)
             out = (torch.empty((n_seq, P), **f32),
                    torch.empty((n_seq, B - 1), **f32) if labels is not None else None,
-                   torch.zeros(3, **f32) if n_seq == 0 else torch.empty(3, **f32),
+                   torch.empty(3, **f32),
                    torch.empty(max(need, 1), dtype=torch.uint8, device=student_logits.device))
         else:
             _typed(out[0], torch.float32, n_seq * P, "kl")
@@ -663,6 +665,8 @@ def distill_forward(student_logits: torch.Tensor, teacher_ids: torch.Tensor,
             _dev(*out)
             _same_device(student_logits, *out)
         kl, ce, loss, saved = out
+        if n_seq == 0:   # the call writes nothing then
+            loss.view(-1)[:3].zero_()
         ws = _scratch(ws, int(lib().hdf_distill_workspace(n_seq, B, V, dt)), student_logits)
         _check(lib().hdf_distill_forward(
             _ptr(student_logits), ld, dt, V, n_seq, B, P, _ptr(teacher_ids), _ptr(teacher_logits),
