@@ -1097,22 +1097,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     over = sh.edge[1];
     __syncthreads();
   };
-  // min_p's cut may lie above all of its bin's entries, if it has any: the last bin before that has.
-  auto bin_before = [&]() {
-    if (tid == 0) sh.last = 0;
-    __syncthreads();
-    for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
-      const int b = b0 + tid;
-      uint64_t any = 0;
-      for (int c = 0; b < border && c < h.chunks; ++c) any |= mass_at(c, b);
-      note_last(any != 0, b, &sh.last);
-    }
-    __syncthreads();
-    border = sh.last;
-    by_p = false;
-    __syncthreads();
-    find_edges();
-  };
   const double target_p = fmax(double(s.top_p) * whole_w, 1e-300);   // 0 is reached by the first
 
   uint64_t cut = 0;
@@ -1120,19 +1104,18 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
     if (binned && !s.open) find_edges();
     // The kept entries and those that the cut lies among, if they are listed, sorted.  Under a cut by
     // weight only a few: of more, whose masses the histograms hold, one chunk is read instead.
-    bool from_lists = binned ? !s.open && end >= floor : has_k || whole;
-    int k = 0;
-#pragma unroll 1
-    while (from_lists && k == 0) {
+    int n = 0, k = 0;
+    if (binned ? !s.open && end >= floor : has_k || whole) {
       float t = binned ? end : has_k ? fmaxf(floor, sh.near) : floor;
-      int n;
 #pragma unroll 1
       for (;;) {
         n = gather<NT>(mine, t, sh);
         if (!has_k || n >= s.top_k || t <= floor) break;
         t = floor;
       }
-      if ((has_k && n < s.top_k) || (binned && n > kInOrder)) break;
+    }
+    // The greatest entry is among them and is kept.
+    if (n > 0 && !(has_k && n < s.top_k) && !(binned && n > kInOrder)) {
       sort_list<NT>(sh.list, n);
       for (int i = tid; i < n; i += NT) sh.weight[i] = entry_weight(entry_logit(sh.list[i]), m, s.c2);
       __syncthreads();
@@ -1158,7 +1141,6 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
         for (int i = tid; i < k; i += NT) c += sh.list[i] >= cut_m;
         k = int(block_fold<W>(c, sh.red.i, add));
       }
-      if (k == 0) bin_before();
     }
     if (k > 0) {
       // In token order: columns with the weights' places as keys.
@@ -1181,6 +1163,22 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   if (PHASE == kAll) __syncthreads();
   if constexpr (BORDER) {
     if (binned) {
+      // min_p's cut may lie above all of its bin's entries, if it has any: the last bin before that has.
+      auto bin_before = [&]() {
+        if (tid == 0) sh.last = 0;
+        __syncthreads();
+        for (int b0 = 0; b0 < border; b0 += NT) {   // whole waves
+          const int b = b0 + tid;
+          uint64_t any = 0;
+          for (int c = 0; b < border && c < h.chunks; ++c) any |= mass_at(c, b);
+          note_last(any != 0, b, &sh.last);
+        }
+        __syncthreads();
+        border = sh.last;
+        by_p = false;
+        __syncthreads();
+        find_edges();
+      };
       uint32_t greater = valid;
       int n = 0;
       const bool fits = s.open || [&]() {
