@@ -221,22 +221,16 @@ __device__ __forceinline__ void note_last(bool c, int i, int* dst) {
 // and is free again on return.
 template <int W, typename X, typename F>
 __device__ __forceinline__ X block_fold(X v, X* sh, F f) {
+  static_assert(W == 4 || W == 8 || W == 16);
   v = wave_fold(v, f);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  X t;
-  if constexpr (W == 4 || W == 8 || W == 16) {   // a lane a wave, and as within rows of 16
-    t = sh[threadIdx.x & (W - 1)];
-    t = f(t, dpp<0xB1, 0xf>(t));
-    t = f(t, dpp<0x4E, 0xf>(t));
-    if constexpr (W > 4) t = f(t, dpp<0x141, 0xf>(t));
-    if constexpr (W > 8) t = f(t, dpp<0x140, 0xf>(t));
-    t = read_lane(t, 0);   // one order of the sum for all
-  } else {
-    t = sh[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w) t = f(t, sh[w]);
-  }
+  X t = sh[threadIdx.x & (W - 1)];   // a lane a wave, and as within rows of 16
+  t = f(t, dpp<0xB1, 0xf>(t));
+  t = f(t, dpp<0x4E, 0xf>(t));
+  if constexpr (W > 4) t = f(t, dpp<0x141, 0xf>(t));
+  if constexpr (W > 8) t = f(t, dpp<0x140, 0xf>(t));
+  t = read_lane(t, 0);   // one order of the sum for all
   __syncthreads();
   return t;
 }
@@ -244,29 +238,20 @@ __device__ __forceinline__ X block_fold(X v, X* sh, F f) {
 // Inclusive running sum over the workgroup's threads, in their order; `total` gets the whole.
 template <int W, typename X>
 __device__ __forceinline__ X block_scan(X v, X* sh, X& total) {
+  static_assert(W == 4 || W == 8 || W == 16);
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   v = wave_scan(v);
   if (lane == 63) sh[wid] = v;
   __syncthreads();
+  X t = sh[lane & (W - 1)];   // a lane a wave, and as within rows of 16
+  t += dpp<0x111, 0xf>(t);
+  t += dpp<0x112, 0xf>(t);
+  if constexpr (W > 4) t += dpp<0x114, 0xf>(t);
+  if constexpr (W > 8) t += dpp<0x118, 0xf>(t);
+  const int w = __builtin_amdgcn_readfirstlane(wid);
   X before = X(0);
-  if constexpr (W == 4 || W == 8 || W == 16) {   // a lane a wave, and as within rows of 16
-    X t = sh[lane & (W - 1)];
-    t += dpp<0x111, 0xf>(t);
-    t += dpp<0x112, 0xf>(t);
-    if constexpr (W > 4) t += dpp<0x114, 0xf>(t);
-    if constexpr (W > 8) t += dpp<0x118, 0xf>(t);
-    const int w = __builtin_amdgcn_readfirstlane(wid);
-    if (w > 0) before = read_lane(t, w - 1);
-    total = read_lane(t, W - 1);
-  } else {
-    X all = X(0);
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      if (w == wid) before = all;
-      all += sh[w];
-    }
-    total = all;
-  }
+  if (w > 0) before = read_lane(t, w - 1);
+  total = read_lane(t, W - 1);
   __syncthreads();
   return before + v;
 }
