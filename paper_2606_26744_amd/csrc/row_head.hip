@@ -5,6 +5,8 @@
 // 8 serve where rows are few.
 #include "row_cut.hpp"
 
+#include <type_traits>
+
 namespace hdf {
 
 constexpr int kHeadWaves = kHeadThreads / kWave;
@@ -213,11 +215,13 @@ row_head_kernel(CutArgs a, HeadArgs h) {
       st.bins = -1;
     }
   } else if (TOP && a.rest != nullptr && valid > listed) {
-    // The others of the top logits: 32-bit exponentials, as their logarithm is stored in 32 bits.
-    // Relative to lo, which they stay below; where nearly all vanish so, to their greatest.  The
+    // The others of the top logits: 32-bit exponentials, each to 2^-23 and, by its exponent's rounding,
+    // 2^-24 of that at the most, 32 added in 32 bits; a logarithm off by 2e-6 at the worst, stored in 32
+    // bits.  Relative to lo, which they stay below; where nearly all vanish so, to their greatest.  The
     // reference is what the rounded product of lo and log2(e) / T stands for, so that an entry
-    // costs one product, rounded once.
-    const float c2 = fminf(float(s.c2), 3e38f);
+    // costs one product, rounded once; where that rounding is no small part of an octave, z - ref
+    // first, in 64 bits.
+    const float c2 = float(s.c2);
     for (int turn = 0; turn < 2; ++turn) {
       float ref = lo;
       if (turn == 1 || !(lo < INFINITY)) {
@@ -228,13 +232,22 @@ row_head_kernel(CutArgs a, HeadArgs h) {
           for (int e = 0; e < N; ++e) g_top = fmaxf(g_top, x[g][e] < lo ? x[g][e] : -INFINITY);
         ref = block_fold<kHeadWaves>(g_top, red.f, most);
       }
-      const float k = fmaxf(fminf(ref * c2, 3e38f), -3e38f);
-      float f = 0.f;
+      const bool far = !(fmax(fabs(double(ref)), 1e-32) * s.c2 < 1e6);   // c2 past 1e38 too
+      const float k = ref * c2;
+      auto others = [&](auto is_far) __attribute__((always_inline)) {
+        float f = 0.f;
 #pragma unroll
-      for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < N; ++e) f += x[g][e] < lo ? __builtin_amdgcn_exp2f(fmaf(x[g][e], c2, -k)) : 0.f;
-      st.rest_ref = double(k) / double(c2);
+          for (int e = 0; e < N; ++e) {
+            const float t = decltype(is_far)::value ? float((double(x[g][e]) - double(ref)) * s.c2)
+                                                    : fmaf(x[g][e], c2, -k);
+            f += x[g][e] < lo ? __builtin_amdgcn_exp2f(t) : 0.f;
+          }
+        return f;
+      };
+      const float f = far ? others(std::true_type()) : others(std::false_type());
+      st.rest_ref = far ? double(ref) : double(k) / double(c2);
       st.rest = block_fold<kHeadWaves>(double(f), red.d, add);
       if (st.rest > 1e-25 || !(lo < INFINITY)) break;
     }
