@@ -611,8 +611,9 @@ hdf_status hdf_top_logits(const void* logits, int64_t rows, int vocab, int64_t l
  * student logit has gradient 0 where it is not listed; one that the teacher gives mass makes kl
  * infinite.  A NaN or +inf among a slot's student logits makes its losses and all of its gradients
  * NaN; among its teacher's, its kl and its gradients wherever kl has one.
- * Sums are 32-bit within a wave, over at most 15 additions in a row, 64-bit beyond; losses are
- * rounded once.
+ * Sums are 32-bit within a wave, over at most 15 additions in a row, 64-bit beyond: right to 1.1e-6
+ * of themselves, their logarithms, and so kl and ce, to as much absolutely (kl holds two on either
+ * side of its difference); losses are rounded once.
  * ----------------------------------------------------------------------------*/
 /* Bytes of the record that the forward pass leaves for the backward (0 on invalid arguments). */
 size_t hdf_distill_saved_bytes(int n_seq, int B, int P, int K);

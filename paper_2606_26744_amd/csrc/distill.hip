@@ -8,9 +8,9 @@
 // greatest value and the sums; the rows' losses; their means.  Backward: one pass that forms every
 // gradient from the row's statistics and then overwrites the few listed tokens'.  Memory bounds both
 // of a large batch: 960 slots of 129280 16-bit logits 46 us forward alone (5.4 TB/s), 72 behind the
-// backward pass of the step before, whose gradients still have to leave the caches; backward 101 us
-// for 513 MB, 5.1 TB/s (a copy of the logits: 108).  Latency bounds a few dozen slots: 5 us the pass, 9
-// or 10 the losses and their means, 6 the gradients.
+// backward pass of the step before, whose gradients still have to leave the caches; backward 98 us
+// for 513 MB, 5.2 TB/s (a copy of the logits: 108).  Latency bounds a few dozen slots: 5 us the pass, 8
+// to 11 the losses and their means, 6 the gradients.
 #include "kernels.hpp"
 #include "rows.hpp"
 

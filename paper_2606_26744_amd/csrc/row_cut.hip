@@ -1,10 +1,10 @@
 // Second launch of a row's cut (row_cut.hpp): a workgroup a row.  Its code runs once a row, mostly on
 // the way to the next memory access or barrier, so it is kept short: the same few loops for all
 // settings, nothing unrolled that memory does not need in flight.  What bounds it is the latency of
-// those steps, 1 to 6 thousand cycles each, and for a nucleus beyond the lists the row's second pass.
-// Of 128 rows of 129280 fp32 logits it takes 9 us with top_k = 50, 18 us for a nucleus of 5 entries,
-// 46 us for one of 4000; of 1024 rows of 16 bits, a nucleus of 4600, 125 us (the second pass, 98, at
-// 2.7 TB/s).
+// those steps, 1 to 6 thousand cycles each, and for a nucleus beyond the lists the row's second pass,
+// 18 vector instructions an entry.  Of 128 rows of 129280 fp32 logits it takes 10 us with top_k = 50, 14
+// us for a nucleus of 5 entries, 42 us for one of 4000; of 1024 rows of 16 bits, a nucleus of 4600, 123
+// us (the second pass, 99, at 2.7 TB/s and 72% of the vector issue).
 #include "row_cut.hpp"
 
 #include <type_traits>
@@ -909,8 +909,7 @@ row_cut_kernel(CutArgs a, HeadArgs h) {
   // Kept entries that are brought into token order to draw among them; of more (of a cut by weight),
   // whose masses the histograms hold, one chunk is read instead.  An entry a thread, so at most NT.
   // (One launch, min_p: 60 rows of 32003 that keep up to 747, 28.5 us by 512, 35.7 by 256; 200 rows, up
-  // to 554, 40 by 512, 46 by 256.  Lists in workgroups of their own: 1024 rows, a nucleus, 235 by 256;
-  // 243 by 512, measured when a thread still took several.)
+  // to 554, 40 by 512, 46 by 256.)
   constexpr int kInOrder = PHASE == kAll ? 512 : 256;
   __shared__ CutShared<NT, SEARCH, BORDER> sh;
   const int64_t at = blockIdx.x, row = a.row0 + at;   // in the launch, in the call

@@ -1,7 +1,7 @@
-// First launch of a row's cut (row_cut.hpp).  Vector instructions bound it: of an entry of a nucleus
-// 11 for its bin and weight, 5 for the order, and as many again of a thread's share of the folds and
-// lists; 1024 rows of 129280 16-bit logits take 129 us at 87% of the issue slots (reading them alone,
-// greedy: 50), their top logits 97 at 92%.  32 entries a thread: 64 were no faster (half the waves),
+// First launch of a row's cut (row_cut.hpp).  Vector instructions bound it: of 27 an entry of a
+// nucleus 11 for its bin and weight, 5 for the order, the others a thread's share of the masks, folds and
+// lists; 1024 rows of 129280 16-bit logits take 130 us at 87% of the issue slots (reading them alone,
+// greedy: 50), the top logits of 960 99 at 93%.  32 entries a thread: 64 were no faster (half the waves),
 // 8 serve where rows are few.
 #include "row_cut.hpp"
 

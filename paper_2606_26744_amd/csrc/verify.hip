@@ -3,7 +3,7 @@
 // row; after n acceptances the next token is drawn from max(0, p_n - q_n) by its running sum in
 // column order (from p_n where that is zero throughout, or after K acceptances).  The target rows
 // are truncated first (row_cut.hip); the draw reads one row, or two, a sequence.  Latency bounds the
-// two launches, 7 us each for 8 sequences of 129280 logits, 6 for one of 32000: chains of dependent
+// two launches, 7 to 8 us each for 8 sequences of 129280 logits, 6 for one of 32000: chains of dependent
 // loads (draft, cut, logits; sums, part, entries) between barriers.
 #include "kernels.hpp"
 #include "rows.hpp"
