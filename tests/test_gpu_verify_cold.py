@@ -1,6 +1,6 @@
 """Verification at temperatures so low that logits over the temperature pass what a 64-bit
 log-sum-exp resolves: probabilities are those of the draws, ties at the top among them, and every
-decision equals the float64 oracle's.  Uniforms lie 1e-4 at least from the border of a decision
+decision equals the float64 oracle's.  Uniforms lie 5e-5 at least from the border of a decision
 between ties (n equal entries weigh 1 / n each)."""
 import numpy as np
 import pytest
@@ -33,7 +33,7 @@ def _rows(n, B, V, seed, dd, td):
 
 
 def _uniforms(n, B, seed):
-    """Multiples of 1/7 and 1/11, away from every m / k of small k."""
+    """Away from every quotient of two numbers up to 4."""
     g = torch.Generator().manual_seed(seed)
     return ((torch.randint(0, 500, (n, B), generator=g) + 0.37) / 500).to(DEV)
 
