@@ -236,6 +236,95 @@ hdf_status hdf_kv_read_rows(const void* kv_k, const void* kv_vt, int64_t kv_cap,
                             int64_t row0, int64_t n_rows, void* k_rows, void* v_rows,
                             hdf_stream_t stream);
 
+/* ------------------------------------------------------------------------------
+ * 4-bit KV cache: the cache of section 2 at about a quarter of its bytes, with row-major keys and
+ * values written to it and read from it, and the attention over it.
+ *
+ * An element is a code of 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times a scale:
+ *   keys    2^e for every 32 consecutive dims of a row's head, e the least integer with
+ *           a <= 7 * 2^e, a the greatest magnitude of the 32 (-125 <= e <= 125)
+ *   values  a bfloat16 s for a row's head, the least with a <= 6 * s (s >= 2^-126)
+ * An element becomes the nearest code of x / scale, ties to the even code (of 0 .. 7), 6 beyond
+ * it: the same codes whatever the kernels' order.  A key is off by scale (at most a / 3.5) or less,
+ * a value by s, half of that below 4 scales and a quarter below 2.  Where the 32 dims (keys) or the
+ * head (values) hold a NaN or an infinity, all of them become NaN.  4.25 bits an element of a key
+ * with its scale, 4.125 (head_dim 128) or 4.25 (64) of a value.
+ *
+ * The cache is one array of tiles, [n_layers][n_kv_heads][kv_cap/64][hdf_kv4_tile_bytes]: a tile
+ * holds keys and values of 64 rows of one head, with their scales, in the order of the attention
+ * kernel's operands (this library's own; csrc/kv4.hpp).  Rows, slots (kv_offsets) and pages
+ * (page_table, one page = one tile of every head) are those of the wider cache above.  Zero bytes
+ * are rows of zeros.
+ * ----------------------------------------------------------------------------*/
+/* Bytes of a tile (0: head_dim not in {64, 128}), and of a whole cache (0 on invalid arguments). */
+size_t hdf_kv4_tile_bytes(int head_dim);
+size_t hdf_kv4_cache_bytes(int n_layers, int n_kv_heads, int head_dim, int64_t kv_cap);
+
+/* hdf_kv_write_rows / hdf_kv_read_rows for this cache.  Row i of k_rows / v_rows (head h from
+ * column h*head_dim on, rows ld_k / ld_v elements apart) is cache row rows[i], or row0 + i when
+ * rows is NULL.  Either of k_rows, v_rows may be NULL to skip keys or values, not both; a write
+ * touches nothing else of the cache, a read nothing else of the outputs.  Writes to a row outside
+ * [0, kv_cap) (from `rows`) are skipped, reads of one return zeros.  A read rounds code * scale
+ * once to `dtype` (keys are exact in either type).
+ * A row may be named once in a write: of a row named twice the codes and scales of either may
+ * remain.  Writes to different rows may run at the same time on different streams only where the
+ * rows lie in different groups of 8 (8j .. 8j+7), whose values share words.
+ * Limits: head_dim in {64, 128}; kv_cap a positive multiple of 64 below 2^31; n_rows, row0 as
+ *         there; ld_k, ld_v >= n_kv_heads*head_dim and multiples of 16 bytes; layer >= 0 (not
+ *         checked against the cache); tensors 16-byte aligned. */
+hdf_status hdf_kv4_write_rows(const void* k_rows, int64_t ld_k, const void* v_rows, int64_t ld_v,
+                              int64_t n_rows, const int32_t* rows, int64_t row0, int layer,
+                              int n_kv_heads, int head_dim, hdf_dtype dtype, void* kv4,
+                              int64_t kv_cap, hdf_stream_t stream);
+hdf_status hdf_kv4_read_rows(const void* kv4, int64_t kv_cap, int layer, int n_kv_heads,
+                             int head_dim, hdf_dtype dtype, const int32_t* rows, int64_t row0,
+                             int64_t n_rows, void* k_rows, int64_t ld_k, void* v_rows,
+                             int64_t ld_v, hdf_stream_t stream);
+
+/* One layer of a 4-bit cache as the attention reads it: with kv_offsets (contiguous slots) or
+ * page_table, exactly one of them. */
+typedef struct {
+  const void* kv4;           /* the whole cache                                             */
+  int64_t kv_cap;            /* rows of it (64 * pages)                                     */
+  int layer;
+  const int32_t* kv_offsets; /* [n_seq+1] or NULL                                           */
+  const int32_t* page_table; /* [n_seq][max_pages] or NULL                                  */
+  int max_pages;             /* max_pages * 64 >= max_ctx                                   */
+} hdf_kv4_cache;
+
+/* Attention of a block of queries of every sequence over its cached context and, where given, the
+ * block's own keys and values (in `dtype`, not quantised).  For slot k of sequence s and query
+ * head h, which reads head j = h / (n_heads / n_kv_heads) of the keys and values:
+ *   x_t = scale * q . K_t   over the context positions t < ctx_len[s] and the block's slots
+ *                           t < block_len[s], with `causal` its slots t <= k only
+ *   out = sum_t softmax(x)_t V_t,   lse = log sum_t exp(x_t)
+ * with fp32 accumulation; bf16: probabilities carry 16 bits into the products; fp32: queries and
+ * probabilities all 24.  A slot with no key at all gets zeros and an lse of -inf.  B = 1 is the
+ * decoding of single tokens; without the block's keys, write a position to the cache before the
+ * query that should see it.
+ * q, k_blk, v_blk, out  row s*B + k, ld_* elements apart: [n_heads or n_kv_heads][head_dim]
+ *             contiguous, dtype; k_blk and v_blk may be NULL together (no keys of the block)
+ * ctx_len     [n_seq] int32, 0 .. max_ctx (larger ones count as max_ctx)
+ * block_len   [n_seq] int32, 0 .. B, or NULL (B): slots in use; the others' outputs are left as
+ *             they were
+ * cache       may be NULL with max_ctx = 0.  A page or slot outside the cache counts as absent:
+ *             its positions have no keys
+ * lse         [n_seq*B][n_heads] fp32 or NULL
+ * ws          hdf_block_attention_kv4_workspace(...) bytes (may be 0, then NULL), 256-byte aligned;
+ *             contents on entry do not matter.  The size serves smaller max_ctx too.
+ * Limits: head_dim in {64, 128}; 1 <= B <= 64; n_kv_heads divides n_heads; n_seq, n_kv_heads and
+ *         n_seq * ceil(n_heads / n_kv_heads * B / 16) below 65536; scale finite and positive; ld_*
+ *         multiples of 16 bytes; tensors 16-byte aligned. */
+size_t hdf_block_attention_kv4_workspace(int n_seq, int B, int n_heads, int n_kv_heads,
+                                         int head_dim, int max_ctx);
+hdf_status hdf_block_attention_kv4(const void* q, int64_t ld_q, const void* k_blk, int64_t ld_k,
+                                   const void* v_blk, int64_t ld_v, int n_seq, int B, int n_heads,
+                                   int n_kv_heads, int head_dim, hdf_dtype dtype,
+                                   const hdf_kv4_cache* cache, const int32_t* ctx_len, int max_ctx,
+                                   const int32_t* block_len, int causal, float scale, void* out,
+                                   int64_t ld_out, float* lse, void* ws, size_t ws_bytes,
+                                   hdf_stream_t stream);
+
 /* Workspace bytes hdf_draft_block needs for these sizes (0 on invalid arguments), and for the
  * same ones with fewer new rows: one workspace, sized by the largest n_new, serves all rounds. */
 size_t hdf_draft_block_workspace(const hdf_drafter* w, int n_seq, int B, int64_t n_new,

@@ -13,6 +13,7 @@
 
 #include "../../include/hdf.h"
 #include "kernels.hpp"
+#include "kv4.hpp"
 
 namespace {
 
@@ -555,6 +556,144 @@ hdf_status hdf_kv_read_rows(const void* kv_k, const void* kv_vt, int64_t kv_cap,
                                            rows, row0, n_heads, head_dim,
                                            reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "kv_read_rows launch");
+  return ok();
+}
+
+// ------------------------------------------------------------------ 4-bit cache
+size_t hdf_kv4_tile_bytes(int head_dim) {
+  return head_dim == 64 || head_dim == 128 ? size_t(hdf::kv4_tile_bytes(head_dim)) : 0;
+}
+
+size_t hdf_kv4_cache_bytes(int n_layers, int n_kv_heads, int head_dim, int64_t kv_cap) {
+  if (n_layers < 1 || n_kv_heads < 1 || kv_cap < 0 || kv_cap % 64 != 0 || kv_cap > INT32_MAX) return 0;
+  return size_t(n_layers) * size_t(n_kv_heads) * size_t(kv_cap / 64) * hdf_kv4_tile_bytes(head_dim);
+}
+
+// A layer's tiles.
+static char* kv4_layer(const void* kv4, int layer, int n_kv_heads, int head_dim, int64_t kv_cap) {
+  return static_cast<char*>(const_cast<void*>(kv4)) +
+         size_t(layer) * hdf_kv4_cache_bytes(1, n_kv_heads, head_dim, kv_cap);
+}
+
+// Rows of `width` elements ld apart: whole, and 16 bytes at a time.
+static bool rows_ld_ok(int64_t ld, int64_t width, size_t el) {
+  return ld >= width && ld <= INT64_MAX / 16 && (ld * int64_t(el)) % 16 == 0;
+}
+
+static hdf_status kv4_rows(const char* fn, bool write, void* kv4, int64_t kv_cap, int layer,
+                           int n_kv_heads, int head_dim, hdf_dtype dtype, const int32_t* rows,
+                           int64_t row0, int64_t n_rows, void* k, int64_t ld_k, void* v,
+                           int64_t ld_v, hdf_stream_t stream) {
+  if (row0 > INT32_MAX) return fail(HDF_E_INVALID, "%s: row0 beyond the cache", fn);
+  const hdf_status st =
+      kv_rows_check(fn, k != nullptr ? kv4 : nullptr, v != nullptr ? kv4 : nullptr, kv_cap, layer,
+                    n_kv_heads, head_dim, dtype, rows, row0, n_rows, k, v);
+  if (st != HDF_OK || n_rows == 0) return st == HDF_OK ? ok() : st;
+  const size_t el = dtype == HDF_BF16 ? 2 : 4;
+  const int64_t width = int64_t(n_kv_heads) * head_dim;
+  if ((k != nullptr && !rows_ld_ok(ld_k, width, el)) || (v != nullptr && !rows_ld_ok(ld_v, width, el)))
+    return fail(HDF_E_INVALID, "%s: rows must be n_kv_heads*head_dim apart or more, by 16 bytes", fn);
+  hdf::Kv4RowArgs a{};
+  a.tiles = kv4_layer(kv4, layer, n_kv_heads, head_dim, kv_cap);
+  a.cap = kv_cap;
+  a.k = k; a.v = v; a.ld_k = ld_k; a.ld_v = ld_v;
+  a.n = n_rows; a.rows = rows; a.row0 = row0; a.nh = n_kv_heads;
+  const hipError_t e = hdf::launch_kv4_rows(dtype == HDF_BF16, write, head_dim, a,
+                                            reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, fn);
+  return ok();
+}
+
+hdf_status hdf_kv4_write_rows(const void* k_rows, int64_t ld_k, const void* v_rows, int64_t ld_v,
+                              int64_t n_rows, const int32_t* rows, int64_t row0, int layer,
+                              int n_kv_heads, int head_dim, hdf_dtype dtype, void* kv4,
+                              int64_t kv_cap, hdf_stream_t stream) {
+  return kv4_rows("kv4_write_rows", true, kv4, kv_cap, layer, n_kv_heads, head_dim, dtype, rows, row0,
+                  n_rows, const_cast<void*>(k_rows), ld_k, const_cast<void*>(v_rows), ld_v, stream);
+}
+
+hdf_status hdf_kv4_read_rows(const void* kv4, int64_t kv_cap, int layer, int n_kv_heads,
+                             int head_dim, hdf_dtype dtype, const int32_t* rows, int64_t row0,
+                             int64_t n_rows, void* k_rows, int64_t ld_k, void* v_rows,
+                             int64_t ld_v, hdf_stream_t stream) {
+  return kv4_rows("kv4_read_rows", false, const_cast<void*>(kv4), kv_cap, layer, n_kv_heads, head_dim,
+                  dtype, rows, row0, n_rows, k_rows, ld_k, v_rows, ld_v, stream);
+}
+
+// Sizes of an attention call over the 4-bit cache.
+static hdf_status kv4_attn_shape(const char* fn, int n_seq, int B, int n_heads, int n_kv_heads,
+                                 int head_dim, int max_ctx) {
+  if (n_seq < 0 || max_ctx < 0) return fail(HDF_E_INVALID, "%s: negative size", fn);
+  if (B < 1 || B > 64) return fail(HDF_E_INVALID, "%s: B=%d outside [1, 64]", fn, B);
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0)
+    return fail(HDF_E_INVALID, "%s: n_kv_heads=%d does not divide n_heads=%d", fn, n_kv_heads, n_heads);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(HDF_E_UNSUPPORTED, "%s: head_dim %d not in {64, 128}", fn, head_dim);
+  const int64_t q_rows = int64_t(n_heads / n_kv_heads) * B;
+  if (n_seq > 65535 || n_kv_heads > 65535 || int64_t(n_seq) * ((q_rows + 15) / 16) > 65535)
+    return fail(HDF_E_UNSUPPORTED, "%s: more than 65535 sequences, heads or tiles of queries", fn);
+  return HDF_OK;
+}
+
+size_t hdf_block_attention_kv4_workspace(int n_seq, int B, int n_heads, int n_kv_heads,
+                                         int head_dim, int max_ctx) {
+  if (kv4_attn_shape("block_attention_kv4", n_seq, B, n_heads, n_kv_heads, head_dim, max_ctx) != HDF_OK)
+    return 0;
+  return hdf::kv4_attn_ws_bytes(n_seq, n_kv_heads, int64_t(n_heads / n_kv_heads) * B, head_dim, max_ctx);
+}
+
+hdf_status hdf_block_attention_kv4(const void* q, int64_t ld_q, const void* k_blk, int64_t ld_k,
+                                   const void* v_blk, int64_t ld_v, int n_seq, int B, int n_heads,
+                                   int n_kv_heads, int head_dim, hdf_dtype dtype,
+                                   const hdf_kv4_cache* cache, const int32_t* ctx_len, int max_ctx,
+                                   const int32_t* block_len, int causal, float scale, void* out,
+                                   int64_t ld_out, float* lse, void* ws, size_t ws_bytes,
+                                   hdf_stream_t stream) {
+  static const char* fn = "block_attention_kv4";
+  if (dtype != HDF_F32 && dtype != HDF_BF16) return fail(HDF_E_INVALID, "%s: bad dtype", fn);
+  const hdf_status st = kv4_attn_shape(fn, n_seq, B, n_heads, n_kv_heads, head_dim, max_ctx);
+  if (st != HDF_OK) return st;
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(HDF_E_INVALID, "%s: scale must be finite and positive", fn);
+  if (n_seq == 0) return ok();
+  if (q == nullptr || out == nullptr || ctx_len == nullptr) return fail(HDF_E_INVALID, "%s: null pointer", fn);
+  if ((k_blk == nullptr) != (v_blk == nullptr))
+    return fail(HDF_E_INVALID, "%s: keys of the block without values (or the reverse)", fn);
+  for (const void* p : {q, k_blk, v_blk, static_cast<const void*>(out)})
+    if (p != nullptr && !aligned16(p)) return fail(HDF_E_INVALID, "%s: tensors must be 16-byte aligned", fn);
+  const size_t el = dtype == HDF_BF16 ? 2 : 4;
+  const int64_t qw = int64_t(n_heads) * head_dim, kw = int64_t(n_kv_heads) * head_dim;
+  if (!rows_ld_ok(ld_q, qw, el) || !rows_ld_ok(ld_out, qw, el) ||
+      (k_blk != nullptr && (!rows_ld_ok(ld_k, kw, el) || !rows_ld_ok(ld_v, kw, el))))
+    return fail(HDF_E_INVALID, "%s: rows must be as far apart as they are long or more, by 16 bytes", fn);
+  hdf::Kv4AttnArgs a{};
+  if (max_ctx > 0) {
+    if (cache == nullptr || cache->kv4 == nullptr || !aligned16(cache->kv4))
+      return fail(HDF_E_INVALID, "%s: a context needs a cache, 16-byte aligned", fn);
+    if ((cache->kv_offsets == nullptr) == (cache->page_table == nullptr))
+      return fail(HDF_E_INVALID, "%s: give one of kv_offsets and page_table", fn);
+    if (cache->kv_cap <= 0 || cache->kv_cap % 64 != 0 || cache->kv_cap > INT32_MAX || cache->layer < 0)
+      return fail(HDF_E_INVALID, "%s: kv_cap must be a positive multiple of 64 below 2^31, layer >= 0", fn);
+    if (cache->page_table != nullptr && int64_t(cache->max_pages) * 64 < max_ctx)
+      return fail(HDF_E_INVALID, "%s: max_pages=%d cannot hold max_ctx=%d", fn, cache->max_pages, max_ctx);
+    a.tiles = kv4_layer(cache->kv4, cache->layer, n_kv_heads, head_dim, cache->kv_cap);
+    a.n_tiles = cache->kv_cap / 64;
+    a.kv_offsets = cache->kv_offsets;
+    a.page_table = cache->page_table; a.max_pages = cache->max_pages;
+  }
+  const size_t need = hdf_block_attention_kv4_workspace(n_seq, B, n_heads, n_kv_heads, head_dim, max_ctx);
+  if (need > 0 && (ws == nullptr || ws_bytes < need))
+    return fail(HDF_E_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws_bytes);
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return fail(HDF_E_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  a.q = q; a.ld_q = ld_q;
+  a.kb = k_blk; a.vb = v_blk; a.ld_kb = ld_k; a.ld_vb = ld_v;
+  a.ctx_len = ctx_len; a.max_ctx = max_ctx; a.block_len = block_len;
+  a.n_seq = n_seq; a.B = B; a.nh = n_heads; a.nkv = n_kv_heads; a.causal = causal != 0 ? 1 : 0;
+  a.scale_log2 = float(1.4426950408889634 * double(scale));
+  a.out = out; a.ld_out = ld_out; a.lse = lse;
+  const hipError_t e = hdf::launch_kv4_attention(dtype == HDF_BF16, head_dim, a, ws,
+                                                 reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, fn);
   return ok();
 }
 

@@ -324,6 +324,49 @@ hipError_t launch_kv_rows(bool bf16, bool write, void* kc, void* vc, int64_t cap
                           void* vrows, int64_t n, const int32_t* rows, int64_t row0, int nh,
                           int hd, hipStream_t s);
 
+// ---------------------------------------------------------------- 4-bit cache (kv4_rows.hip, kv4_attention.hip)
+struct Kv4RowArgs {
+  char* tiles;               // the layer's [nh][cap/64] tiles (kv4.hpp)
+  int64_t cap;
+  void *k, *v;               // row-major rows [n][ld], head h from column h * hd on; either may be NULL
+  int64_t ld_k, ld_v;
+  int64_t n;
+  const int32_t* rows;       // cache row of each (outside [0, cap): skipped, read as zeros), or NULL:
+  int64_t row0;              // row0 + i
+  int nh;
+  int64_t groups;            // set by the launch
+};
+// write: k, v are quantised into the cache; otherwise read back from it.
+hipError_t launch_kv4_rows(bool bf16, bool write, int hd, const Kv4RowArgs& a, hipStream_t s);
+
+struct Kv4AttnArgs {
+  const void* q;             // row s * B + k: [nh][hd], row stride ld_q
+  int64_t ld_q;
+  const char* tiles;         // the layer's [nkv][n_tiles] tiles
+  int64_t n_tiles;
+  const int32_t* ctx_len;    // [n_seq]
+  const int32_t* kv_offsets; // [n_seq+1], or
+  const int32_t* page_table; // [n_seq][max_pages]
+  int max_pages, max_ctx;
+  const void *kb, *vb;       // the block's keys and values, row s * B + k: [nkv][hd], or NULL
+  int64_t ld_kb, ld_vb;
+  const int32_t* block_len;  // [n_seq] or NULL (B)
+  int n_seq, B, nh, nkv, causal;
+  float scale_log2;          // log2(e) * softmax scale
+  int n_chunks, chunk_len;   // a multiple of 64
+  void* out;                 // row s * B + k: [nh][hd], row stride ld_out
+  int64_t ld_out;
+  float* lse;                // [n_seq * B][nh] or NULL
+  float* part_o;             // n_chunks > 1: [n_seq][nkv][n_chunks][G * B][hd]
+  float* part_ml;            // ... [2]
+};
+// Chunks of the context and their length for these sizes (n_heads / n_kv_heads * B query rows a
+// head of keys), and the workspace bytes of every call up to max_ctx.
+void kv4_attn_plan(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx, int* n_chunks, int* chunk_len);
+size_t kv4_attn_ws_bytes(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx);
+// ws: kv4_attn_ws_bytes (part_o, part_ml, the plan are set by the launch).
+hipError_t launch_kv4_attention(bool bf16, int hd, const Kv4AttnArgs& a, void* ws, hipStream_t s);
+
 // ---------------------------------------------------------------- attention (attention.hip)
 struct AttnArgs {
   const void* q;             // [n_seq][nh][B][hd]

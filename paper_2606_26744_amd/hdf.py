@@ -35,7 +35,9 @@ EXPORTS = ("hdf_last_error", "hdf_version", "hdf_hc_reduce", "hdf_rope_table",
            "hdf_sample_truncated_workspace", "hdf_sample_truncated",
            "hdf_accept_truncated_workspace", "hdf_accept_truncated",
            "hdf_top_logits_workspace", "hdf_top_logits", "hdf_distill_saved_bytes",
-           "hdf_distill_workspace", "hdf_distill_forward", "hdf_distill_backward")
+           "hdf_distill_workspace", "hdf_distill_forward", "hdf_distill_backward",
+           "hdf_kv4_tile_bytes", "hdf_kv4_cache_bytes", "hdf_kv4_write_rows", "hdf_kv4_read_rows",
+           "hdf_block_attention_kv4_workspace", "hdf_block_attention_kv4")
 
 
 class HdfError(RuntimeError):
@@ -70,6 +72,12 @@ class Drafter(ctypes.Structure):
                 ("w_down", ctypes.POINTER(ctypes.c_void_p)),
                 ("final_norm", ctypes.c_void_p), ("rope_cs", ctypes.c_void_p),
                 ("rope_max_pos", ctypes.c_int)]
+
+
+class Kv4Cache(ctypes.Structure):
+    _fields_ = [("kv4", ctypes.c_void_p), ("kv_cap", ctypes.c_int64), ("layer", ctypes.c_int),
+                ("kv_offsets", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("max_pages", ctypes.c_int)]
 
 
 _lib = None
@@ -169,6 +177,20 @@ def lib() -> ctypes.CDLL:
     L.hdf_distill_backward.restype = _I
     L.hdf_distill_backward.argtypes = [_P, _I64, _I, _I, _I, _I, _I, _P, _I, _P, _F, _F, _P, _P, _P,
                                        _P, _P, _I64, _P]
+    L.hdf_kv4_tile_bytes.restype = _SZ
+    L.hdf_kv4_tile_bytes.argtypes = [_I]
+    L.hdf_kv4_cache_bytes.restype = _SZ
+    L.hdf_kv4_cache_bytes.argtypes = [_I, _I, _I, _I64]
+    L.hdf_kv4_write_rows.restype = _I
+    L.hdf_kv4_write_rows.argtypes = [_P, _I64, _P, _I64, _I64, _P, _I64, _I, _I, _I, _I, _P, _I64, _P]
+    L.hdf_kv4_read_rows.restype = _I
+    L.hdf_kv4_read_rows.argtypes = [_P, _I64, _I, _I, _I, _I, _P, _I64, _I64, _P, _I64, _P, _I64, _P]
+    L.hdf_block_attention_kv4_workspace.restype = _SZ
+    L.hdf_block_attention_kv4_workspace.argtypes = [_I] * 6
+    L.hdf_block_attention_kv4.restype = _I
+    L.hdf_block_attention_kv4.argtypes = [_P, _I64, _P, _I64, _P, _I64, _I, _I, _I, _I, _I, _I,
+                                          ctypes.POINTER(Kv4Cache), _P, _I, _P, _I, _F, _P, _I64,
+                                          _P, _P, _SZ, _P]
     _lib = L
     return L
 
@@ -1037,3 +1059,193 @@ def kv_slot_offsets(ctx_lens: Sequence[int]) -> list:
     for t in ctx_lens:
         offs.append(offs[-1] + ((int(t) + 63) // 64) * 64)
     return offs
+
+
+# ------------------------------------------------------------------------- 4-bit cache
+
+def kv4_alloc(n_layers: int, n_kv_heads: int, head_dim: int, kv_cap: int,
+              device="cuda") -> torch.Tensor:
+    """A 4-bit KV cache of zeros: uint8 [n_layers, n_kv_heads, kv_cap/64, tile bytes], a tile
+    holding keys and values of 64 positions of one head with their scales (hdf.h)."""
+    if kv_cap % 64:
+        raise ValueError("kv_cap must be a multiple of 64")
+    tile = int(lib().hdf_kv4_tile_bytes(head_dim))
+    if tile == 0:
+        raise ValueError(f"head_dim {head_dim} not in (64, 128)")
+    return torch.zeros((n_layers, n_kv_heads, kv_cap // 64, tile), dtype=torch.uint8, device=device)
+
+
+def _kv4_dims(kv4: torch.Tensor):
+    """(n_layers, n_kv_heads, head_dim, kv_cap) of a cache tensor from kv4_alloc."""
+    if kv4.dtype != torch.uint8 or kv4.dim() != 4 or not kv4.is_contiguous():
+        raise ValueError("kv4 must be a contiguous uint8 [layers, heads, tiles, tile bytes] tensor")
+    L, nh, tiles, tile = kv4.shape
+    hd = _KV4_HEAD_DIMS.get(tile)
+    if hd is None:
+        hd = next((d for d in (64, 128) if int(lib().hdf_kv4_tile_bytes(d)) == tile), None)
+        if hd is None:
+            raise ValueError(f"tiles of {tile} bytes belong to no head_dim")
+        _KV4_HEAD_DIMS[tile] = hd
+    return L, nh, hd, tiles * 64
+
+
+_KV4_HEAD_DIMS = {}
+
+
+def _kv4_layer(layer: int, L: int):
+    if not 0 <= layer < L:
+        raise ValueError(f"layer {layer} outside [0, {L})")
+
+
+def _kv4_rows_arg(rows: Optional[torch.Tensor], n: int, row0: int):
+    if rows is not None and (rows.dtype != torch.int32 or rows.numel() != n or
+                             not rows.is_contiguous()):
+        raise ValueError("rows must be a contiguous int32 tensor with one entry per row")
+    if not 0 <= row0 <= _INT_MAX:
+        raise ValueError("row0 must be in [0, 2^31)")
+
+
+def _row_stride(t: Optional[torch.Tensor], n: int, width: int, what: str) -> int:
+    """Row stride of a [n, width] matrix with unit column stride."""
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [{n}, {width}] with unit column stride")
+    return t.stride(0) if n > 1 else max(t.stride(0), width)
+
+
+def kv4_write_rows(kv4: torch.Tensor, layer: int, k_rows: Optional[torch.Tensor],
+                   v_rows: Optional[torch.Tensor], *, row0: int = 0,
+                   rows: Optional[torch.Tensor] = None, stream=None):
+    """hdf_kv4_write_rows: row i of k_rows / v_rows [n, n_kv_heads*head_dim] (fp32 or bf16, any row
+    stride of whole 16 bytes) quantised into cache row rows[i] (int32 device tensor, each row named
+    once) or row0 + i of one layer.  Either of k_rows, v_rows may be None."""
+    L, nh, hd, cap = _kv4_dims(kv4)
+    src = k_rows if k_rows is not None else v_rows
+    if src is None:
+        raise ValueError("give keys or values")
+    n = src.shape[0]
+    _kv4_layer(layer, L)
+    _kv4_rows_arg(rows, n, row0)
+    ld_k = _row_stride(k_rows, n, nh * hd, "k_rows")
+    ld_v = _row_stride(v_rows, n, nh * hd, "v_rows")
+    if k_rows is not None and v_rows is not None and k_rows.dtype != v_rows.dtype:
+        raise ValueError("k_rows and v_rows must be of one type")
+    with _place(kv4, stream):
+        _same_device(kv4, k_rows, v_rows, rows)
+        _check(lib().hdf_kv4_write_rows(_ptr(k_rows), ld_k, _ptr(v_rows), ld_v, n, _ptr(rows), row0,
+                                        layer, nh, hd, _dt(src), _ptr(kv4), cap, _stream()))
+
+
+def kv4_read_rows(kv4: torch.Tensor, layer: int, n: int, *, row0: int = 0,
+                  rows: Optional[torch.Tensor] = None, dtype=torch.bfloat16, out=None, stream=None):
+    """hdf_kv4_read_rows: cache rows rows[i] (or row0 + i), i < n, of one layer as row-major (keys,
+    values), each [n, n_kv_heads*head_dim].  out: the same, preallocated (either may be None)."""
+    L, nh, hd, cap = _kv4_dims(kv4)
+    _kv4_layer(layer, L)
+    if not 0 <= n <= _INT_MAX:
+        raise ValueError("n must be in [0, 2^31)")
+    _kv4_rows_arg(rows, n, row0)
+    with _place(kv4, stream):
+        if out is None:
+            k = torch.empty((n, nh * hd), dtype=dtype, device=kv4.device)
+            out = k, torch.empty_like(k)
+        k, v = out
+        src = k if k is not None else v
+        if src is None or (k is not None and v is not None and k.dtype != v.dtype):
+            raise ValueError("out must hold keys or values, of one type")
+        ld_k, ld_v = _row_stride(k, n, nh * hd, "keys"), _row_stride(v, n, nh * hd, "values")
+        _same_device(kv4, k, v, rows)
+        _check(lib().hdf_kv4_read_rows(_ptr(kv4), cap, layer, nh, hd, _dt(src), _ptr(rows), row0, n,
+                                       _ptr(k), ld_k, _ptr(v), ld_v, _stream()))
+    return k, v
+
+
+def _block_stride(t: torch.Tensor, n_seq: int, B: int, what: str) -> int:
+    """Row stride of a [n_seq, B, heads, head_dim] tensor whose rows (s, k) hold their heads
+    contiguously and lie evenly, row s*B + k."""
+    _, _, H, hd = t.shape
+    s0, s1, s2, s3 = t.stride()
+    ok = (s3 == 1 or hd == 1) and (H == 1 or s2 == hd)
+    ld = s1 if B > 1 else s0 if n_seq > 1 else H * hd
+    if not ok or (B > 1 and n_seq > 1 and s0 != B * ld):
+        raise ValueError(f"{what} must hold a slot's heads contiguously and its slots evenly")
+    return ld
+
+
+def block_attention_kv4_workspace(n_seq: int, B: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                                  max_ctx: int) -> int:
+    """Bytes of hdf_block_attention_kv4's workspace (those of every smaller max_ctx too)."""
+    return int(lib().hdf_block_attention_kv4_workspace(n_seq, B, n_heads, n_kv_heads, head_dim,
+                                                       max_ctx))
+
+
+def block_attention_kv4(q: torch.Tensor, kv4: Optional[torch.Tensor], layer: int = 0, *,
+                        ctx_len: torch.Tensor, max_ctx: int,
+                        kv_offsets: Optional[torch.Tensor] = None,
+                        page_table: Optional[torch.Tensor] = None,
+                        k_blk: Optional[torch.Tensor] = None, v_blk: Optional[torch.Tensor] = None,
+                        block_len: Optional[torch.Tensor] = None, causal: bool = False,
+                        scale: Optional[float] = None, want_lse: bool = True, out=None,
+                        ws: Optional[torch.Tensor] = None, stream=None):
+    """hdf_block_attention_kv4: q [n_seq, B, n_heads, head_dim] fp32 or bf16 over the 4-bit cache
+    (kv_offsets [n_seq+1] or page_table [n_seq, max_pages], int32) and, where given, the block's
+    own k_blk, v_blk [n_seq, B, n_kv_heads, head_dim] -> (out like q, lse [n_seq, B, n_heads] fp32
+    or None).  ctx_len, block_len: int32 [n_seq]; scale: 1/sqrt(head_dim) if None; kv4 may be None
+    with max_ctx = 0.  q, k_blk, v_blk, out may be columns of wider rows.  out: a preallocated (out,
+    lse); outputs of slots from block_len on are left as they were."""
+    if q.dim() != 4:
+        raise ValueError("q must be [n_seq, B, n_heads, head_dim]")
+    n_seq, B, H, hd = q.shape
+    _int32(max(n_seq, H), "q's sequences and heads")
+    _int32(max_ctx, "max_ctx")
+    dt = _dt(q)
+    if (k_blk is None) != (v_blk is None):
+        raise ValueError("give k_blk and v_blk together")
+    if kv4 is not None:
+        L, nkv, hd_kv, cap = _kv4_dims(kv4)
+        _kv4_layer(layer, L)
+        if hd_kv != hd:
+            raise ValueError("q and the cache disagree in head_dim")
+    elif k_blk is not None:
+        nkv = k_blk.shape[2] if k_blk.dim() == 4 else 0
+    else:
+        nkv = H
+    for t, what in ((k_blk, "k_blk"), (v_blk, "v_blk")):
+        if t is not None and (t.dtype != q.dtype or t.shape != (n_seq, B, nkv, hd)):
+            raise ValueError(f"{what} must be [n_seq, B, n_kv_heads, head_dim] of q's type")
+    if kv4 is not None and max_ctx > 0:
+        if (kv_offsets is None) == (page_table is None):
+            raise ValueError("give exactly one of kv_offsets and page_table")
+        if page_table is not None and (page_table.dtype != torch.int32 or page_table.dim() != 2 or
+                                       page_table.shape[0] != n_seq):
+            raise ValueError("page_table must be an int32 [n_seq, max_pages] tensor")
+    _typed(ctx_len, torch.int32, n_seq, "ctx_len")
+    _typed(block_len, torch.int32, n_seq, "block_len")
+    _typed(kv_offsets, torch.int32, n_seq + 1, "kv_offsets")
+    scale = hd ** -0.5 if scale is None else float(scale)
+    with _place(q, stream):
+        if out is None:
+            out = (torch.empty((n_seq, B, H, hd), dtype=q.dtype, device=q.device),
+                   torch.empty((n_seq, B, H), dtype=torch.float32, device=q.device)
+                   if want_lse else None)
+        o, lse = out
+        if o.shape != q.shape or o.dtype != q.dtype:
+            raise ValueError("out must have the shape and the type of q")
+        _typed(lse, torch.float32, n_seq * B * H, "lse")
+        _dev(ctx_len, block_len, kv_offsets, page_table, lse)
+        _same_device(q, kv4, ctx_len, block_len, kv_offsets, page_table, k_blk, v_blk, o, lse)
+        lds = [_block_stride(t, n_seq, B, what) if t is not None else 0
+               for t, what in ((q, "q"), (k_blk, "k_blk"), (v_blk, "v_blk"), (o, "out"))]
+        cache = None
+        if kv4 is not None and max_ctx > 0:
+            cache = ctypes.byref(Kv4Cache(kv4.data_ptr(), cap, layer, _ptr(kv_offsets),
+                                          _ptr(page_table),
+                                          page_table.shape[1] if page_table is not None else 0))
+        need = block_attention_kv4_workspace(n_seq, B, H, nkv, hd, max_ctx) if nkv > 0 else 0
+        ws = _scratch(ws, need, q) if need else None
+        _check(lib().hdf_block_attention_kv4(
+            _ptr(q), lds[0], _ptr(k_blk), lds[1], _ptr(v_blk), lds[2], n_seq, B, H, nkv, hd, dt,
+            cache, _ptr(ctx_len), max_ctx, _ptr(block_len), int(causal), scale, _ptr(o), lds[3],
+            _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+    return o, lse

@@ -1,0 +1,175 @@
+"""GPU tests of hdf_block_attention_kv4 against the oracle over what the cache stands for.
+
+Bound of an output element, with A = sum p |v| (at least |out|):
+  a score is off by d <= (hd + 4) 2^-24 scale sum |q k| + 2^-22 (fp32 sums; the exponential and
+  its argument), its probability by a factor 1 + d, the ratio of sums by 2 d; a probability in two
+  bf16 terms keeps 2^-16 of itself (three: 2^-24, a query in three: 2^-24 more of its score); sums
+  over T keys in fp32, each at most T 2^-24; the result is rounded once, 2^-8 of itself (bf16) or
+  2^-24 (fp32).  What lies below fp32's least normal number, 2^-126, may be 0: a key's probability
+  relative to the greatest and the lower term it is split into, so 2 * 2^-126 max |v| a key.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4 as ref
+from paper_2606_26744_amd import hdf
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _np(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+class Case:
+    def __init__(self, ctx, B, H, nkv, hd, dtype, *, paged=True, block=True, fused=False, seed=0,
+                 layers=1, layer=0, spread=1.0):
+        g = torch.Generator().manual_seed(seed)
+        n = len(ctx)
+        self.ctx, self.B, self.H, self.nkv, self.hd, self.dtype, self.layer = ctx, B, H, nkv, hd, dtype, layer
+        tiles = [(t + 63) // 64 for t in ctx]
+        total = sum(tiles) + 2
+        order = torch.randperm(total, generator=g).tolist()
+        self.kv4 = hdf.kv4_alloc(layers, nkv, hd, 64 * total)
+        self.kv4.fill_(0xFF)            # rows that no sequence holds: NaN scales
+        self.max_ctx = max(max(ctx), 1)
+        width = max((self.max_ctx + 63) // 64, 1)
+        table, offs, at = np.full((n, width), -1, np.int32), [0], 0
+        self.k, self.v = [], []
+        for s, T in enumerate(ctx):
+            pages = order[at:at + tiles[s]] if paged else list(range(at, at + tiles[s]))
+            at += tiles[s]
+            table[s, :tiles[s]] = pages
+            offs.append(64 * at)
+            k = torch.randn(T, nkv, hd, generator=g) * spread
+            v = torch.randn(T, nkv, hd, generator=g) * torch.exp(torch.randn(T, nkv, 1, generator=g))
+            k, v = k.to(dtype), v.to(dtype)
+            if T:
+                hdf.kv4_write_rows(self.kv4, layer, k.view(T, -1).cuda(), v.view(T, -1).cuda(),
+                                   rows=hdf.paged_rows(pages, T, "cuda"))
+            self.k.append(ref.quantise_keys(_np(k)))
+            self.v.append(ref.quantise_values(_np(v)))
+        i32 = dict(dtype=torch.int32, device="cuda")
+        self.kw = dict(ctx_len=torch.tensor(ctx, **i32), max_ctx=self.max_ctx)
+        if paged:
+            self.kw["page_table"] = torch.from_numpy(table).cuda()
+        else:
+            self.kw["kv_offsets"] = torch.tensor(offs, **i32)
+        wide = (torch.randn(n, B, (H + 2 * nkv) * hd, generator=g) * spread).to(dtype).cuda()
+        cols = wide[..., :H * hd], wide[..., H * hd:(H + nkv) * hd], wide[..., (H + nkv) * hd:]
+        cols = [c if fused else c.contiguous() for c in cols]
+        self.q = cols[0].view(n, B, H, hd)
+        self.kb, self.vb = (c.view(n, B, nkv, hd) for c in cols[1:])
+        if block:
+            self.kw.update(k_blk=self.kb, v_blk=self.vb)
+        self.block = block
+
+    def check(self, out, lse, *, causal=False, blen=None, scale=None):
+        f32 = self.dtype == F32
+        for s, T in enumerate(self.ctx):
+            b = self.B if blen is None else blen[s]
+            kb, vb = (_np(self.kb[s, :b]), _np(self.vb[s, :b])) if self.block else (None, None)
+            o, l, mass, reach = ref.attend(_np(self.q[s, :b]), self.k[s], self.v[s], kb, vb,
+                                           causal=causal, scale=scale)
+            d = (self.hd + 4) * 2.0 ** -24 * reach + 2.0 ** -22 + (2.0 ** -24 * reach if f32 else 0)
+            N = T + self.B
+            tol = mass * (2 * d[..., None] + (2.0 ** -24 if f32 else 2.0 ** -16) + 2 * N * 2.0 ** -24)
+            tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
+            top = max([np.abs(x).max() for x in (self.v[s], vb) if x is not None and x.size] or [0.0])
+            tol += 2 * N * 2.0 ** -126 * top
+            err = np.abs(_np(out[s, :b]) - o)
+            assert (err <= tol).all(), (s, T, float((err - tol).max()), np.argwhere(err > tol)[:3])
+            if lse is not None:
+                got = _np(lse[s, :b])
+                fin = np.isfinite(l)
+                assert np.array_equal(got[~fin], l[~fin])
+                e = np.abs(got[fin] - l[fin])
+                bound = (d + N * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(l)))[fin]
+                assert (e <= bound).all(), (s, T, float((e - bound).max()))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,H,nkv", [(1, 4, 4), (16, 2, 2), (5, 6, 3), (16, 8, 2), (33, 2, 1), (1, 14, 2)])
+def test_blocks_over_ragged_contexts(hd, dtype, B, H, nkv):
+    print(f"[kv4 attention] hd={hd} {dtype} B={B} H={H}/{nkv}", flush=True)
+    c = Case([1, 64, 130, 0, 700], B, H, nkv, hd, dtype, fused=B == 5, seed=B + H)
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("causal", [False, True])
+def test_block_lengths_and_causal_slots(dtype, causal):
+    c = Case([65, 3, 0, 200], 7, 4, 2, 128, dtype, paged=False, layers=2, layer=1, seed=3)
+    blen = [7, 1, 4, 0]
+    bl = torch.tensor(blen, dtype=torch.int32, device="cuda")
+    out = torch.full_like(c.q, 77.0)
+    lse = torch.full((4, 7, 4), 55.0, device="cuda")
+    hdf.block_attention_kv4(c.q, c.kv4, 1, block_len=bl, causal=causal, out=(out, lse), **c.kw)
+    c.check(out, lse, causal=causal, blen=blen)
+    for s, b in enumerate(blen):        # slots behind a block's length
+        assert (out[s, b:] == 77.0).all() and (lse[s, b:] == 55.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_no_key_at_all(dtype):
+    c = Case([0, 70, 0], 3, 2, 1, 64, dtype, block=False, seed=4)
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    c.check(out, lse)
+    assert not out[0].any() and torch.isneginf(lse[0]).all()
+    none, l = hdf.block_attention_kv4(c.q, None, ctx_len=torch.zeros_like(c.kw["ctx_len"]), max_ctx=0)
+    assert not none.any() and torch.isneginf(l).all()
+    c.ctx, c.k, c.v, c.block = [0, 0, 0], [c.k[0]] * 3, [c.v[0]] * 3, True
+    out, lse = hdf.block_attention_kv4(c.q, None, ctx_len=torch.zeros_like(c.kw["ctx_len"]), max_ctx=0,
+                                       k_blk=c.kb, v_blk=c.vb)
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype,ctx", [(BF, [20000]), (F32, [9000]), (BF, [4000, 1, 2500])])
+def test_long_contexts_in_pieces(dtype, ctx):
+    c = Case(ctx, 2, 4, 2, 128, dtype, seed=5)
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    c.check(out, lse)
+    again, lse2 = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_sharp_scores_and_a_scale():
+    """Scores of a few hundred: one key takes nearly all of the weight."""
+    c = Case([300, 64], 4, 4, 4, 128, BF, spread=4.0, seed=6)
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, scale=0.7, **c.kw)
+    c.check(out, lse, scale=0.7)
+
+
+def test_pages_outside_the_pool_hold_no_keys():
+    c = Case([200], 4, 2, 2, 64, BF, seed=7)
+    pt = c.kw["page_table"]
+    pt[0, 1] = -5
+    pt[0, 3] = c.kv4.shape[2]
+    keep = np.r_[0:64, 128:192]
+    c.k[0], c.v[0] = c.k[0][keep], c.v[0][keep]
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    c.check(out, lse)
+
+
+def test_rows_that_are_no_numbers_reach_their_heads_alone():
+    c = Case([100, 50], 2, 4, 2, 64, BF, seed=8)
+    bad = torch.zeros(1, 2 * 64, dtype=BF, device="cuda")
+    bad[0, 70] = float("nan")           # of head 1
+    page = int(c.kw["page_table"][0, 1])
+    hdf.kv4_write_rows(c.kv4, 0, bad, None, row0=64 * page + 5)
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    assert torch.isnan(out[0, :, 2:]).all() and torch.isnan(lse[0, :, 2:]).all()
+    assert torch.isfinite(out[0, :, :2]).all() and torch.isfinite(out[1]).all()
+
+
+def test_a_larger_workspace_serves_and_lse_is_optional():
+    c = Case([3000, 10], 3, 4, 2, 128, BF, seed=9)
+    need = hdf.block_attention_kv4_workspace(2, 3, 4, 2, 128, 9000)
+    ws = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")
+    want, _ = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    got, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, want_lse=False, ws=ws, **c.kw)
+    assert lse is None and torch.equal(want, got)
