@@ -298,8 +298,8 @@ typedef struct {
  *   x_t = scale * q . K_t   over the context positions t < ctx_len[s] and the block's slots
  *                           t < block_len[s], with `causal` its slots t <= k only
  *   out = sum_t softmax(x)_t V_t,   lse = log sum_t exp(x_t)
- * with fp32 accumulation; bf16: probabilities carry 16 bits into the products; fp32: queries and
- * probabilities all 24.  A slot with no key at all gets zeros and an lse of -inf.  B = 1 is the
+ * with fp32 accumulation.  bf16: a context probability times its value's scale is rounded to 11 bits
+ * (an eighth of the output's own rounding); fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of -inf.  B = 1 is the
  * decoding of single tokens; without the block's keys, write a position to the cache before the
  * query that should see it.
  * q, k_blk, v_blk, out  row s*B + k, ld_* elements apart: [n_heads or n_kv_heads][head_dim]
@@ -312,7 +312,7 @@ typedef struct {
  * lse         [n_seq*B][n_heads] fp32 or NULL
  * ws          hdf_block_attention_kv4_workspace(...) bytes (may be 0, then NULL), 256-byte aligned;
  *             contents on entry do not matter.  The size serves smaller max_ctx too.
- * Limits: head_dim in {64, 128}; 1 <= B <= 64; n_kv_heads divides n_heads; n_seq, n_kv_heads and
+ * Limits: head_dim in {64, 128}; 1 <= B <= 64; max_ctx <= 2^30; n_kv_heads divides n_heads; n_seq, n_kv_heads and
  *         n_seq * ceil(n_heads / n_kv_heads * B / 16) below 65536; scale finite and positive; ld_*
  *         multiples of 16 bytes; tensors 16-byte aligned. */
 size_t hdf_block_attention_kv4_workspace(int n_seq, int B, int n_heads, int n_kv_heads,

@@ -632,6 +632,7 @@ static hdf_status kv4_attn_shape(const char* fn, int n_seq, int B, int n_heads, 
   const int64_t q_rows = int64_t(n_heads / n_kv_heads) * B;
   if (n_seq > 65535 || n_kv_heads > 65535 || int64_t(n_seq) * ((q_rows + 15) / 16) > 65535)
     return fail(HDF_E_UNSUPPORTED, "%s: more than 65535 sequences, heads or tiles of queries", fn);
+  if (max_ctx > 1 << 30) return fail(HDF_E_UNSUPPORTED, "%s: max_ctx beyond 2^30", fn);
   return HDF_OK;
 }
 

@@ -359,6 +359,8 @@ struct Kv4AttnArgs {
   float* lse;                // [n_seq * B][nh] or NULL
   float* part_o;             // n_chunks > 1: [n_seq][nkv][n_chunks][G * B][hd]
   float* part_ml;            // ... [2]
+  int G, n_groups;           // set by the launch: n_heads / n_kv_heads, workgroups' query groups a sequence
+  float inv_g;
 };
 // Chunks of the context and their length for these sizes (n_heads / n_kv_heads * B query rows a
 // head of keys), and the workspace bytes of every call up to max_ctx.

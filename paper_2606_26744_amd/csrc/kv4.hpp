@@ -24,6 +24,9 @@
 
 namespace hdf {
 
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
 // Bytes at which a tile's parts start, and its size.
 __host__ __device__ constexpr int kv4_values_at(int hd) { return 32 * hd; }
 __host__ __device__ constexpr int kv4_kscales_at(int hd) { return 64 * hd; }
@@ -62,6 +65,14 @@ __device__ __forceinline__ bf16x8_t kv4_bf16x8(uint32_t w, float scale) {
   const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
   const uint32_t d = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
   return __builtin_bit_cast(bf16x8_t, u32x4{a, b, c, d});
+}
+// ... as fp16 without a scale, exact (half the issue cycles of the bf16 conversion).
+__device__ __forceinline__ f16x8_t kv4_f16x8(uint32_t w) {
+  const f16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0);
+  const f16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1);
+  const f16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 2);
+  const f16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 3);
+  return f16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // Eight values as codes of x / scale (a power of two), to the nearest, ties to even, 6 at most.
 __device__ __forceinline__ uint32_t kv4_codes8(const float* x, float scale) {

@@ -17,10 +17,11 @@ namespace {
 constexpr int kTile = 64;
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * kWave;
-constexpr int kMaxTiles = 512;            // tiles of a chunk
+constexpr int kMaxTiles = kAttnWaves * kWave;   // tiles of a chunk: one a lane
 constexpr int kJoinThreads = 256;
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t to_bf2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
@@ -67,9 +68,6 @@ __device__ __forceinline__ void load8(const T* p, float* x) {
   }
 }
 
-__device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-
 // A tile of the cache as a wave's lanes hold it.
 template <int HD>
 struct Tile {
@@ -86,17 +84,24 @@ struct Tile {
   }
 };
 
+// The tile at p (the same for all lanes).  Buffer loads: one 32-bit offset a lane serves them all,
+// where 64-bit addresses of every part cost registers that the loop needs.  The codes are read once
+// a call, past the caches.
 template <int HD>
 __device__ __forceinline__ void load_tile(Tile<HD>& t, const char* p, int lane) {
   const int g = lane >> 4, ql = lane & 15;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, kv4_tile_bytes(HD), 0x00027000);
+  constexpr int NT = 2;   // non-temporal
 #pragma unroll
-  for (int l = 0; l < HD / 32; ++l) t.k[l] = ld_nt16(p + (l * 64 + lane) * 16);
+  for (int l = 0; l < HD / 32; ++l)
+    t.k[l] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16, 1024 * l, NT);
 #pragma unroll
-  for (int l = 0; l < HD / 32; ++l) t.v[l] = ld_nt16(p + kv4_values_at(HD) + (l * 64 + lane) * 16);
-  const int b = HD == 128 ? g : g >> 1;
-  t.ks = *reinterpret_cast<const uint32_t*>(p + kv4_kscales_at(HD) + (16 * b + ql) * 4);
-  t.vs[0] = ld16(p + kv4_vscales_at(HD) + 16 * g);
-  t.vs[1] = ld16(p + kv4_vscales_at(HD) + 64 + 16 * g);
+  for (int l = 0; l < HD / 32; ++l)
+    t.v[l] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16, kv4_values_at(HD) + 1024 * l, NT);
+  const int word = HD == 128 ? lane : (lane >> 5) * 16 + ql;   // block g, or g / 2, of row ql
+  t.ks = __builtin_amdgcn_raw_buffer_load_b32(rsrc, word * 4, kv4_kscales_at(HD), 0);
+  t.vs[0] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, g * 16, kv4_vscales_at(HD), 0);
+  t.vs[1] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, g * 16, kv4_vscales_at(HD) + 64, 0);
 }
 
 // Context chunks of a sequence of T positions.
@@ -110,25 +115,47 @@ __device__ __forceinline__ int block_of(const Kv4AttnArgs& a, int s) {
   return a.block_len != nullptr ? min(max(a.block_len[s], 0), a.B) : a.B;
 }
 
-// Running softmax of one 16-row query tile in a wave: lane (g, ql) keeps query ql.
+// Slot of query row r: r / G (rows are below 2^21, where this quotient is exact).
+__device__ __forceinline__ int slot_of(const Kv4AttnArgs& a, int r) {
+  return int((float(r) + 0.5f) * a.inv_g);
+}
+
+// Four dims of an output row: o / l, zeros where no key was seen.
+template <typename T>
+__device__ __forceinline__ void store_out(T* dst, f32x4_t o, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  else
+    *reinterpret_cast<uint2*>(dst) = make_uint2(to_bf2(o[0] * inv, o[1] * inv), to_bf2(o[2] * inv, o[3] * inv));
+}
+
+// Maximum over the four lane groups of a query.
+__device__ __forceinline__ float groups_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// Running softmax of one 16-row query tile in a wave: lane (g, ql) keeps query ql.  o and l are
+// relative to 2^m, m the greatest score (base 2) so far less `lift`.
 template <int HD>
 struct State {
   f32x4_t o[HD / 16];    // O^T: dim 16dt + 4g + e of query ql
-  float m, l;            // base-2 maximum; this lane group's part of the sum
+  float m, l;            // l: this lane group's part of the sum
 };
 
-// Scores of 64 keys (a lane's sixteen, -inf where masked) into the state's maximum and sum; sv
-// leaves as the probabilities relative to the new maximum.
+// Products of 64 keys (a lane's sixteen, -inf where masked) into the state's reference and sum; x
+// leaves as exp2(c * x - m).  The lift has fallen by `drop` since the last call.
 template <int HD>
-__device__ __forceinline__ void soft_step(State<HD>& st, float (&sv)[4][4]) {
-  float top = sv[0][0];
+__device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c, float lift, float drop) {
+  float top = x[0];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = fmaxf(top, sv[i][e]);
-  top = fmaxf(top, __shfl_xor(top, 16, kWave));
-  top = fmaxf(top, __shfl_xor(top, 32, kWave));
-  const float m = fmaxf(st.m, top);
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+  top = groups_max(top);
+  const float m = fmaxf(st.m + drop, fmaf(top, c, -lift));
   if (__any(m > st.m)) {
     const float alpha = m > st.m ? __builtin_amdgcn_exp2f(st.m - m) : 1.f;   // st.m -inf: 0
     st.l *= alpha;
@@ -138,229 +165,411 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&sv)[4][4]) {
       for (int e = 0; e < 4; ++e) st.o[dt][e] *= alpha;
     st.m = m;
   }
-  const float base = m == -INFINITY ? 0.f : m;   // no key yet
+  const float base = st.m == -INFINITY ? 0.f : st.m;   // no key yet
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sv[i][e] = __builtin_amdgcn_exp2f(sv[i][e] - base);
-      sum += sv[i][e];
-    }
+  for (int i = 0; i < 16; ++i) {
+    x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -base));
+    sum += x[i];
+  }
   st.l += sum;
 }
 
+// The lift of a wave's references.  A value's scale times its probability becomes one fp16 factor
+// of the products with the codes (bf16 queries): 11 bits, a rounding an eighth of the output's own.
+// So that it neither overflows nor loses small ones, probabilities are taken relative to 2^-lift,
+// lift = 15 - log2 of a power of two above the greatest scale so far: the factor is below 2^15, and
+// of full precision down to 2^-29 of the greatest probability times the greatest scale.  fp32:
+// three bf16 terms, no lift.
+struct Lift {
+  int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
+  __device__ __forceinline__ float value() const { return float(141 - top); }
+};
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// A query tile as the operand of the products with keys.
+// bf16 queries, heads of 128 dims: the scaled fp4 x fp8 product takes the keys as they lie in the
+// cache.  A bf16 has 8 significant bits, an e4m3 number 4: q = 2^e (hi + lo / 16), exact for the
+// elements from 2^-14 of the query's greatest on; smaller ones are off by 2^-23 of it at most.
+// Lane (g, ql): dims 16g .. and 64 + 16g .. of query ql.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kAttnThreads) kv4_attn_kernel(Kv4AttnArgs a) {
-  constexpr bool F32 = sizeof(T) == 4;
-  constexpr int QT = F32 ? 3 : 1;   // bf16 terms of a query's element
-  constexpr int PT = F32 ? 3 : 2;   // ... of a probability
-  constexpr int NJ = HD / 32;       // products over the dims of a score
-  constexpr int NDT = HD / 16;
-  __shared__ float red_o[kAttnWaves][16][HD + 1];
-  __shared__ float red_m[kAttnWaves][16], red_l[kAttnWaves][16];
-  __shared__ int32_t page[kMaxTiles];
-  const int chunk = blockIdx.z, hk = blockIdx.x;
-  const int G = a.nh / a.nkv, R = G * a.B;
-  const int nqt = (R + 15) / 16;
-  const int s = blockIdx.y / nqt, qt = blockIdx.y - s * nqt;
-  const int n_ctx = context_of(a, s);
-  if (chunk >= chunks_of(a, n_ctx)) return;
-  const int blen = block_of(a, s);
-  if (16 * qt >= G * blen) return;   // rows of no slot
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int g = lane >> 4, ql = lane & 15;
-  const int k_lo = min(n_ctx, chunk * a.chunk_len), k_hi = min(n_ctx, k_lo + a.chunk_len);
-  const int nct = (k_hi - k_lo + kTile - 1) / kTile;
-  const int nbk = a.kb != nullptr && chunk == 0 ? blen : 0;   // keys of the block
-
-  // The chunk's tiles; -1 for a page outside the pool, whose keys count as absent.
-  for (int j = threadIdx.x; j < nct; j += kAttnThreads) {
-    const int t = (k_lo >> 6) + j;
-    const int64_t p = a.page_table != nullptr ? int64_t(a.page_table[int64_t(s) * a.max_pages + t])
-                                              : int64_t(a.kv_offsets[s] >> 6) + t;
-    page[j] = p >= 0 && p < a.n_tiles ? int32_t(p) : -1;
-  }
-  __syncthreads();
-  const char* head = a.tiles + int64_t(hk) * a.n_tiles * kv4_tile_bytes(HD);
-
-  // Query operand: lane (g, ql) holds dims (HD/4)g + 8j .. of query ql.
-  const int row = 16 * qt + ql;
-  const int slot = row / G;
-  bf16x8_t qf[NJ][QT];
-  float qx[F32 ? NJ : 1][8];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (row < R)
-      load8(static_cast<const T*>(a.q) + (int64_t(s) * a.B + slot) * a.ld_q +
-                (int64_t(hk) * G + (row - slot * G)) * HD + (HD / 4) * g + 8 * j, x);
-    split8<QT>(x, qf[j]);
-    if constexpr (F32) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qx[j][e] = x[e];
-    }
-  }
-
-  State<HD> st;
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt) st.o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  st.m = -INFINITY;
-  st.l = 0.f;
-
-  Tile<HD> cur, nxt;
-  if (wid < nct) load_tile<HD>(cur, head + int64_t(max(page[wid], 0)) * kv4_tile_bytes(HD), lane);
-  for (int i = wid; i < nct; i += kAttnWaves) {
-    if (i + kAttnWaves < nct)
-      load_tile<HD>(nxt, head + int64_t(max(page[i + kAttnWaves], 0)) * kv4_tile_bytes(HD), lane);
-    const int nval = page[i] < 0 ? 0 : min(kTile, k_hi - k_lo - i * kTile);
-    float sv[4][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const float scale = __uint_as_float(((cur.ks >> (8 * t)) & 255u) << 23);
-      f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const bf16x8_t kf = kv4_bf16x8(cur.key_word(t, j), scale);
-#pragma unroll
-        for (int n = 0; n < QT; ++n)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j][n], acc, 0, 0, 0);
+struct Query {
+  static constexpr bool SCALED = sizeof(T) == 2 && HD == 128;
+  static constexpr int QT = sizeof(T) == 4 ? 3 : 1;   // bf16 terms of an element
+  static constexpr int NJ = HD / 32;
+  // Not scaled: lane (g, ql) holds dims (HD/4)g + 8j .. of query ql.
+  bf16x8_t f[SCALED ? 1 : NJ][QT];
+  i32x8_t hi, lo;
+  int e_hi, e_lo;
+  __device__ __forceinline__ void load(const T* p, int g) {   // p NULL: zeros
+    if constexpr (SCALED) {
+      u32x4 w[4] = {};
+      if (p != nullptr) {
+        w[0] = ld16(p + 16 * g);
+        w[1] = ld16(p + 16 * g + 8);
+        w[2] = ld16(p + 64 + 16 * g);
+        w[3] = ld16(p + 64 + 16 * g + 8);
       }
+      uint32_t m = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + e;
-        sv[t][e] = key < nval ? acc[e] * a.scale_log2 : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t b = w[i / 4][i % 4];
+        m = max(m, max(b & 0x7FFFu, (b >> 16) & 0x7FFFu));
       }
-    }
-    soft_step<HD>(st, sv);
+      m = max(m, uint32_t(__shfl_xor(m, 16, kWave)));
+      m = max(m, uint32_t(__shfl_xor(m, 32, kWave)));
+      // The greatest comes to lie in [128, 256).
+      const int e = max(int(m >> 7), 12) - 7;
+      const float unit = __uint_as_float(uint32_t(254 - e) << 23);
+      e_hi = m >= 0x7F80u ? 255 : e;
+      e_lo = m >= 0x7F80u ? 255 : e - 4;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t w = cur.vs[ks][e >> 1];
-        const float s_v = (e & 1) ? hi_bf(w) : lo_bf(w);
-        const float x = sv[2 * ks + (e >> 2)][e & 3];
-        p[e] = 32 * ks + 8 * g + e < nval ? x * s_v : 0.f;   // a scale of no row may be anything
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t b0 = w[i / 2][2 * (i % 2)], b1 = w[i / 2][2 * (i % 2) + 1];
+        const float y[4] = {lo_bf(b0) * unit, hi_bf(b0) * unit, lo_bf(b1) * unit, hi_bf(b1) * unit};
+        int h = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], h, true);
+        hi[i] = h;
+        const float r0 = (y[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0)) * 16.f;
+        const float r1 = (y[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1)) * 16.f;
+        const float r2 = (y[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2)) * 16.f;
+        const float r3 = (y[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3)) * 16.f;
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(r0, r1, 0, false);
+        lo[i] = __builtin_amdgcn_cvt_pk_fp8_f32(r2, r3, h, true);
       }
-      bf16x8_t pf[PT];
-      split8<PT>(p, pf);
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        const bf16x8_t vf = kv4_bf16x8(cur.value_word(ks, dt), 1.f);
-#pragma unroll
-        for (int n = 0; n < PT; ++n)
-          st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], st.o[dt], 0, 0, 0);
-      }
-    }
-    cur = nxt;
-  }
-
-  // The block's keys, by the wave that would take the next tile.
-  if (nbk > 0 && wid == nct % kAttnWaves) {
-    const T* kb = static_cast<const T*>(a.kb) + int64_t(s) * a.B * a.ld_kb + int64_t(hk) * HD;
-    const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
-    float sv[4][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int r = 32 * (t >> 1) + 8 * (ql >> 2) + 4 * (t & 1) + (ql & 3);   // this lane's key
-      f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (r < nbk) load8(kb + r * a.ld_kb + (HD / 4) * g + 8 * j, x);
-        if constexpr (F32) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], qx[j][e], acc, 0, 0, 0);
-        } else {
-          bf16x8_t kf[1];
-          split8<1>(x, kf);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qf[j][0], acc, 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 32 * (t >> 1) + 8 * g + 4 * (t & 1) + e;
-        const bool seen = key < nbk && (a.causal == 0 || key <= slot);
-        sv[t][e] = seen ? acc[e] * a.scale_log2 : -INFINITY;
+        if (p != nullptr) load8(p + (HD / 4) * g + 8 * j, x);
+        split8<QT>(x, f[j]);
       }
     }
-    soft_step<HD>(st, sv);
+  }
+};
+
+// Products of sub-tile ST's sixteen keys with the queries: lane (g, ql) gets keys 4g .. 4g+3.
+template <typename T, int HD, int ST>
+__device__ __forceinline__ f32x4_t score(const Tile<HD>& t, const Query<T, HD>& q) {
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (Query<T, HD>::SCALED) {
+    const i32x8_t k = {int(t.k[ST][0]), int(t.k[ST][1]), int(t.k[ST][2]), int(t.k[ST][3]), 0, 0, 0, 0};
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.hi, acc, 4, 0, ST, int(t.ks), 0, q.e_hi);
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.lo, acc, 4, 0, ST, int(t.ks), 0, q.e_lo);
+  } else {
+    const float scale = __uint_as_float(((t.ks >> (8 * ST)) & 255u) << 23);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      if (32 * ks >= nbk) break;
-      float p[8];
+    for (int j = 0; j < HD / 32; ++j) {
+      const bf16x8_t kf = kv4_bf16x8(t.key_word(ST, j), scale);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = sv[2 * ks + (e >> 2)][e & 3];
-      bf16x8_t pf[PT];
-      if constexpr (!F32) split8<PT>(p, pf);
+      for (int n = 0; n < Query<T, HD>::QT; ++n)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.f[j][n], acc, 0, 0, 0);
+    }
+  }
+  return acc;
+}
+
+// A tile of the cache into the states of NQ query tiles; nval of its 64 keys count.
+template <typename T, int HD, int NQ>
+__device__ __forceinline__ void tile_step(Tile<HD>& t, const Query<T, HD> (&q)[NQ], State<HD> (&st)[NQ],
+                                          Lift& lift, int nval, int g, float c) {
+  constexpr bool F32 = sizeof(T) == 4;
+  float x[NQ][16];
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        float x[8];
+  for (int n = 0; n < NQ; ++n) {
+    const f32x4_t s0 = score<T, HD, 0>(t, q[n]), s1 = score<T, HD, 1>(t, q[n]);
+    const f32x4_t s2 = score<T, HD, 2>(t, q[n]), s3 = score<T, HD, 3>(t, q[n]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int r = 32 * ks + 8 * g + e;
-          x[e] = r < nbk ? load1(vb + r * a.ld_vb + 16 * dt + ql) : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      x[n][e] = s0[e];
+      x[n][4 + e] = s1[e];
+      x[n][8 + e] = s2[e];
+      x[n][12 + e] = s3[e];
+    }
+  }
+  // x[i] is key 32 * (i/8) + 8g + i%8.  Behind the last key anything may stand, in the values'
+  // scales too.
+  if (nval < kTile) {
+    const int left = nval - 8 * g;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const bool off = 32 * (i >> 3) + (i & 7) >= left;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) x[n][i] = off ? -INFINITY : x[n][i];
+      const uint32_t w = t.vs[i >> 3][(i & 7) >> 1];
+      t.vs[i >> 3][(i & 7) >> 1] = off ? w & ((i & 1) ? 0x0000FFFFu : 0xFFFF0000u) : w;
+    }
+  }
+  float drop = 0.f;
+  if constexpr (!F32) {
+    u16x2_t w = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w = __builtin_elementwise_max(w, __builtin_bit_cast(u16x2_t, uint32_t(t.vs[i >> 2][i & 3])));
+    int top = max(w[0], w[1]) >> 7;
+    if (__any(top > lift.top)) {
+      top = max(top, __shfl_xor(top, 16, kWave));
+      top = max(top, __shfl_xor(top, 32, kWave));
+      drop = float(top - lift.top);
+      lift.top = top;
+    }
+  }
+  const float up = F32 ? 0.f : lift.value();
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) soft_step<HD>(st[n], x[n], c, up, drop);
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = (e & 1) ? hi_bf(t.vs[ks][e >> 1]) : lo_bf(t.vs[ks][e >> 1]);
+    if constexpr (F32) {
+      bf16x8_t pf[NQ][3];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = x[n][8 * ks + e] * s[e];
+        split8<3>(p, pf[n]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < HD / 16; ++dt) {
+        const bf16x8_t vf = kv4_bf16x8(t.value_word(ks, dt), 1.f);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            st[n].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][k], st[n].o[dt], 0, 0, 0);
+      }
+    } else {
+      f16x8_t pf[NQ];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const f16x2_t p = __builtin_convertvector(f32x2_t{x[n][8 * ks + e] * s[e], x[n][8 * ks + e + 1] * s[e + 1]}, f16x2_t);
+          pf[n][e] = p[0];
+          pf[n][e + 1] = p[1];
         }
+#pragma unroll
+      for (int dt = 0; dt < HD / 16; ++dt) {
+        const f16x8_t vf = kv4_f16x8(t.value_word(ks, dt));
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+          st[n].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n], st[n].o[dt], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// The block's own keys and values in LDS: rows of keys, values by dim, zeros behind the last row up
+// to a multiple of 32.
+template <typename T, int HD>
+struct BlockRows {
+  static constexpr int E = 16 / sizeof(T);   // elements of 16 bytes
+  T k[64][HD + E];
+  T v[HD][64 + E];
+};
+
+// nbk of them into the state of a query tile; a query sees those up to `last`.
+template <typename T, int HD>
+__device__ __forceinline__ void block_step(const T* qrow, const BlockRows<T, HD>& b, State<HD>& st, int nbk,
+                                           int last, int lane, float c) {
+  constexpr bool F32 = sizeof(T) == 4;
+  const int g = lane >> 4, ql = lane & 15;
+  float x[16];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    if (32 * (t >> 1) + 4 * (t & 1) < nbk) {
+      const T* kr = b.k[32 * (t >> 1) + 8 * (ql >> 2) + 4 * (t & 1) + (ql & 3)];   // this lane's key
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) {
+        float u[8], w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        load8(kr + (HD / 4) * g + 8 * j, u);
+        if (qrow != nullptr) load8(qrow + (HD / 4) * g + 8 * j, w);
         if constexpr (F32) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], p[e], st.o[dt], 0, 0, 0);
+          for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[e], w[e], acc, 0, 0, 0);
         } else {
-          bf16x8_t vf[1];
-          split8<1>(x, vf);
-#pragma unroll
-          for (int n = 0; n < PT; ++n)
-            st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[0], pf[n], st.o[dt], 0, 0, 0);
+          bf16x8_t kf[1], qf[1];
+          split8<1>(u, kf);
+          split8<1>(w, qf);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qf[0], acc, 0, 0, 0);
         }
       }
     }
+    const int left = min(nbk, last + 1) - 8 * g;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[4 * t + e] = 32 * (t >> 1) + 4 * (t & 1) + e < left ? acc[e] : -INFINITY;
+  }
+  soft_step<HD>(st, x, c, F32 ? 0.f : Lift().value(), 0.f);
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    if (32 * ks >= nbk) break;
+    bf16x8_t pf[2];
+    if constexpr (!F32) split8<2>(x + 8 * ks, pf);
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) {
+      const T* vr = b.v[16 * dt + ql] + 32 * ks + 8 * g;
+      if constexpr (F32) {
+        float v[8];
+        load8(vr, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], x[8 * ks + e], st.o[dt], 0, 0, 0);
+      } else {
+        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, ld16(vr));
+        st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[0], st.o[dt], 0, 0, 0);
+        st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[1], st.o[dt], 0, 0, 0);
+      }
+    }
+  }
+}
+
+template <typename T, int HD, int NQ>
+__global__ void __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2)))
+kv4_attn_kernel(Kv4AttnArgs a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int NDT = HD / 16;
+  // The block's keys and values, later the waves' states.
+  __shared__ __align__(16) union {
+    BlockRows<T, HD> blk;
+    float o[kAttnWaves][16][HD + 4];
+  } pool;
+  __shared__ float red_m[kAttnWaves][16], red_l[kAttnWaves][16];
+  const int chunk = blockIdx.z, hk = blockIdx.x;
+  const int G = a.G, R = G * a.B;
+  const int s = blockIdx.y / a.n_groups, row0 = 16 * NQ * (blockIdx.y - s * a.n_groups);
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, ql = lane & 15;
+
+  // Lane l keeps the place of the wave's l-th tile, tile wid + kAttnWaves * l of the chunk: read
+  // beside the lengths, not behind them.  -1 for a page outside the pool, whose keys count as absent.
+  const int t0 = chunk * (a.chunk_len >> 6);
+  int page = -1;
+  {
+    const int t = t0 + wid + kAttnWaves * lane;
+    if (a.page_table != nullptr) {
+      if (t < a.max_pages) page = a.page_table[int64_t(s) * a.max_pages + t];
+    } else if (a.kv_offsets != nullptr) {
+      page = int(min(int64_t(a.kv_offsets[s] >> 6) + t, int64_t(INT32_MAX)));
+    }
+    if (page >= a.n_tiles) page = -1;
+  }
+  const int n_ctx = context_of(a, s);
+  if (chunk >= chunks_of(a, n_ctx)) return;
+  const int blen = block_of(a, s);
+  if (row0 >= G * blen) return;   // rows of no slot
+  const int k_lo = min(n_ctx, t0 << 6), k_hi = min(n_ctx, k_lo + a.chunk_len);
+  const int nct = (k_hi - k_lo + kTile - 1) / kTile;
+  const int nbk = a.kb != nullptr && chunk == 0 ? blen : 0;   // keys of the block
+  const char* head = a.tiles + int64_t(hk) * a.n_tiles * kv4_tile_bytes(HD);
+
+  // Row of query ql of tile n (NULL behind the last).
+  auto q_row = [&](int n) -> const T* {
+    const int row = row0 + 16 * n + ql;
+    const int slot = slot_of(a, row);
+    return row < R ? static_cast<const T*>(a.q) + (int64_t(s) * a.B + slot) * a.ld_q +
+                         (int64_t(hk) * G + (row - slot * G)) * HD
+                   : nullptr;
+  };
+  auto tile_at = [&](int l) { return head + int64_t(max(__builtin_amdgcn_readlane(page, l), 0)) * kv4_tile_bytes(HD); };
+  Tile<HD> cur;
+  if (wid < nct) load_tile<HD>(cur, tile_at(0), lane);
+  Query<T, HD> q[NQ];
+  State<HD> st[NQ];
+  Lift lift;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    q[n].load(q_row(n), g);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) st[n].o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    st[n].m = -INFINITY;
+    st[n].l = 0.f;
+  }
+  // The block's rows into LDS, 16 bytes a thread, and into the state of the wave that has the fewest
+  // tiles, while the first tiles are on their way.
+  if (nbk > 0) {
+    constexpr int E = 16 / sizeof(T), P = HD / E;
+    const T* kb = static_cast<const T*>(a.kb) + int64_t(s) * a.B * a.ld_kb + int64_t(hk) * HD;
+    const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
+    const int rows = (nbk + 31) & ~31;
+    for (int e = threadIdx.x; e < 2 * rows * P; e += kAttnThreads) {
+      const int v = e >= rows * P, r = (e - v * rows * P) / P, i = (e - v * rows * P - r * P) * E;
+      u32x4 w = {0, 0, 0, 0};
+      if (r < nbk) w = ld16(v ? vb + r * a.ld_vb + i : kb + r * a.ld_kb + i);
+      if (v) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          if constexpr (F32)
+            pool.blk.v[i + k][r] = __uint_as_float(w[k]);
+          else
+            pool.blk.v[i + k][r] = T(w[k / 2] >> (16 * (k & 1)));
+        }
+      } else {
+        st16(&pool.blk.k[r][i], w);
+      }
+    }
+    __syncthreads();
+    if (wid == nct % kAttnWaves) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+        block_step<T, HD>(q_row(n), pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
+                          lane, a.scale_log2);
+    }
+  }
+  for (int i = wid, l = 0; i < nct; i += kAttnWaves, ++l) {
+    Tile<HD> nxt;
+    if (i + kAttnWaves < nct) load_tile<HD>(nxt, tile_at(l + 1), lane);
+    const int nval = __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, k_hi - k_lo - i * kTile);
+    tile_step<T, HD, NQ>(cur, q, st, lift, nval, g, a.scale_log2);
+    cur = nxt;
   }
 
-  // The waves' states side by side, then joined.
-  st.l += __shfl_xor(st.l, 16, kWave);
-  st.l += __shfl_xor(st.l, 32, kWave);
-  if (g == 0) {
-    red_m[wid][ql] = st.m;
-    red_l[wid][ql] = st.l;
-  }
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) red_o[wid][ql][16 * dt + 4 * g + e] = st.o[dt][e];
-  __syncthreads();
+  // The waves' states of a query tile side by side, then joined: four dims of a row a thread.
   const bool direct = a.n_chunks == 1;
-  for (int e = threadIdx.x; e < 16 * (HD / 2); e += kAttnThreads) {
-    const int qq = e / (HD / 2), dim = 2 * (e - qq * (HD / 2));
-    const int qr = 16 * qt + qq, k = qr / G;
-    if (k >= blen) continue;
-    float mm = red_m[0][qq];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) mm = fmaxf(mm, red_m[w][qq]);
-    float o0 = 0.f, o1 = 0.f, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-      const float f = red_m[w][qq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[w][qq] - mm);
-      o0 += f * red_o[w][qq][dim];
-      o1 += f * red_o[w][qq][dim + 1];
-      l += f * red_l[w][qq];
+  for (int n = 0; n < NQ; ++n) {
+    float l_sum = st[n].l;
+    l_sum += __shfl_xor(l_sum, 16, kWave);
+    l_sum += __shfl_xor(l_sum, 32, kWave);
+    if (n > 0 || nbk > 0) __syncthreads();
+    if (g == 0) {
+      red_m[wid][ql] = st[n].m;
+      red_l[wid][ql] = l_sum;
     }
-    if (direct) {
-      const int64_t orow = int64_t(s) * a.B + k;
-      const int h = hk * G + (qr - k * G);
-      const float inv = l == 0.f ? 0.f : 1.f / l;   // no key: zeros
-      T* dst = static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + dim;
-      if constexpr (F32)
-        *reinterpret_cast<float2*>(dst) = make_float2(o0 * inv, o1 * inv);
-      else
-        *reinterpret_cast<uint32_t*>(dst) = to_bf2(o0 * inv, o1 * inv);
-      if (dim == 0 && a.lse != nullptr)
-        a.lse[orow * a.nh + h] = (mm + __log2f(l)) * 0.6931471805599453f;
-    } else {
-      const int64_t p = ((int64_t(s) * a.nkv + hk) * a.n_chunks + chunk) * R + qr;
-      *reinterpret_cast<float2*>(a.part_o + p * HD + dim) = make_float2(o0, o1);
-      if (dim == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * p) = make_float2(mm, l);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4_t*>(&pool.o[wid][ql][16 * dt + 4 * g]) = st[n].o[dt];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * (HD / 4); e += kAttnThreads) {
+      const int qq = e / (HD / 4), dim = 4 * (e % (HD / 4));
+      const int qr = row0 + 16 * n + qq, k = slot_of(a, qr);
+      if (k >= blen) continue;
+      float mm = red_m[0][qq];
+#pragma unroll
+      for (int w = 1; w < kAttnWaves; ++w) mm = fmaxf(mm, red_m[w][qq]);
+      const float base = mm == -INFINITY ? 0.f : mm;
+      f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(red_m[w][qq] - base);
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&pool.o[w][qq][dim]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+        l = fmaf(f, red_l[w][qq], l);
+      }
+      if (direct) {
+        const int64_t orow = int64_t(s) * a.B + k;
+        const int h = hk * G + (qr - k * G);
+        store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + dim, o, l);
+        if (dim == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(l)) * 0.6931471805599453f;
+      } else {
+        const int64_t p = ((int64_t(s) * a.nkv + hk) * a.n_chunks + chunk) * R + qr;
+        *reinterpret_cast<f32x4_t*>(a.part_o + p * HD + dim) = o;
+        if (dim == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * p) = make_float2(mm, l);
+      }
     }
   }
 }
@@ -372,9 +581,9 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int Q = HD / 4, S = kJoinThreads / Q;
   __shared__ float4 so[S][Q];
   __shared__ float sm[S], sl[S];
-  const int G = a.nh / a.nkv, R = G * a.B;
+  const int G = a.G, R = G * a.B;
   const int qr = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
-  const int k = qr / G;
+  const int k = slot_of(a, qr);
   if (k >= block_of(a, s)) return;
   const int nc = chunks_of(a, context_of(a, s));
   const int d = threadIdx.x % Q, sl_ = threadIdx.x / Q;
@@ -417,22 +626,25 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
     o.z += f * so[w][d].z;
     o.w += f * so[w][d].w;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t orow = int64_t(s) * a.B + k;
   const int h = hk * G + (qr - k * G);
-  T* dst = static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + 4 * d;
-  if constexpr (sizeof(T) == 4)
-    *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  else
-    *reinterpret_cast<uint2*>(dst) = make_uint2(to_bf2(o.x * inv, o.y * inv), to_bf2(o.z * inv, o.w * inv));
+  store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + 4 * d,
+               f32x4_t{o.x, o.y, o.z, o.w}, sum);
   if (d == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(sum)) * 0.6931471805599453f;
 }
 
 template <typename T, int HD>
-hipError_t attn_t(const Kv4AttnArgs& a, hipStream_t s) {
-  const int R = a.nh / a.nkv * a.B;
-  const dim3 grid(a.nkv, unsigned(a.n_seq * ((R + 15) / 16)), a.n_chunks);
-  hipLaunchKernelGGL((kv4_attn_kernel<T, HD>), grid, dim3(kAttnThreads), 0, s, a);
+hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
+  const int R = a.G * a.B;
+  // Two query tiles a wave where there are two (32-bit heads of 128 dims would spill).
+  constexpr int MQ = sizeof(T) == 4 && HD == 128 ? 1 : 2;
+  const int nq = R > 16 ? MQ : 1;
+  a.n_groups = (R + 16 * nq - 1) / (16 * nq);
+  const dim3 grid(a.nkv, unsigned(a.n_seq * a.n_groups), a.n_chunks);
+  if (nq == 1)
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, 1>), grid, dim3(kAttnThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, MQ>), grid, dim3(kAttnThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
   hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3(R, a.nkv, a.n_seq), dim3(kJoinThreads), 0, s, a);
@@ -441,23 +653,33 @@ hipError_t attn_t(const Kv4AttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// Chunks of at most one round of workgroups over the card, of 2048 positions at least (four tiles a
+// wave; a chunk's lengths, queries and join take about 5 us beside its tiles, the second launch 4).
+// Measured, us a call by chunk length, 1024 to 16384: one query over 131072 positions of 8 heads 42,
+// 34, 30, 36, 52 (256 workgroups at 4096); 8 x 2048 positions of 32 heads 28, 18 (256 at 2048);
+// 64 contexts of up to 16384 609, 509, 443, 412, 368 (2048 workgroups at 16384).
+constexpr int kMinChunk = 2048;
+
+static int64_t chunks_wanted(int n_seq, int nkv, int64_t q_rows, int max_ctx) {
+  const int64_t wgs = std::max<int64_t>(1, int64_t(n_seq) * nkv * ((q_rows + 31) / 32));
+  const int64_t most = (int64_t(max_ctx) + kMinChunk - 1) / kMinChunk;
+  return std::max<int64_t>(1, std::min(int64_t(device_cu_count()) / wgs, most));
+}
+
 void kv4_attn_plan(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx, int* n_chunks,
                    int* chunk_len) {
-  const int64_t wgs = int64_t(n_seq) * nkv * ((q_rows + 15) / 16);
-  const int64_t want = std::max<int64_t>(1, 2 * int64_t(device_cu_count()) / std::max<int64_t>(1, wgs));
-  int64_t len = (std::max(max_ctx, 1) + want - 1) / want;
-  len = std::min<int64_t>(std::max<int64_t>((len + 511) / 512 * 512, 512), kMaxTiles * kTile);
+  const int64_t ctx = std::max(max_ctx, 1), want = chunks_wanted(n_seq, nkv, q_rows, max_ctx);
+  int64_t len = (ctx + want - 1) / want;
+  len = std::min<int64_t>((len + 511) / 512 * 512, kMaxTiles * kTile);
   *chunk_len = int(len);
-  *n_chunks = int((std::max(max_ctx, 1) + len - 1) / len);
+  *n_chunks = int((ctx + len - 1) / len);
 }
 
 size_t kv4_attn_ws_bytes(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx) {
-  // A shorter context has no more chunks: at most as many as fill the card, or one each 512 positions.
-  int n, len;
-  kv4_attn_plan(n_seq, nkv, q_rows, hd, max_ctx, &n, &len);
-  const int64_t wgs = int64_t(n_seq) * nkv * ((q_rows + 15) / 16);
-  const int64_t want = std::max<int64_t>(1, 2 * int64_t(device_cu_count()) / std::max<int64_t>(1, wgs));
-  const int64_t most = std::max<int64_t>(n, std::min<int64_t>(want, (int64_t(std::max(max_ctx, 1)) + 511) / 512));
+  // A shorter context takes as many chunks as are wanted for it, or as many of the greatest length
+  // as it needs: neither grows as it gets shorter.
+  const int64_t longest = (int64_t(max_ctx) + kMaxTiles * kTile - 1) / (kMaxTiles * kTile);
+  const int64_t most = std::max(chunks_wanted(n_seq, nkv, q_rows, max_ctx), longest);
   if (most <= 1) return 0;
   return size_t(n_seq) * nkv * size_t(most) * size_t(q_rows) * (hd + 2) * 4;
 }
@@ -465,7 +687,9 @@ size_t kv4_attn_ws_bytes(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx
 hipError_t launch_kv4_attention(bool bf16, int hd, const Kv4AttnArgs& args, void* ws, hipStream_t s) {
   Kv4AttnArgs a = args;
   if (a.n_seq <= 0) return hipSuccess;
-  const int64_t R = int64_t(a.nh / a.nkv) * a.B;
+  a.G = a.nh / a.nkv;
+  a.inv_g = 1.f / float(a.G);
+  const int64_t R = int64_t(a.G) * a.B;
   kv4_attn_plan(a.n_seq, a.nkv, R, hd, a.max_ctx, &a.n_chunks, &a.chunk_len);
   a.part_o = static_cast<float*>(ws);
   a.part_ml = a.part_o + size_t(a.n_seq) * a.nkv * a.n_chunks * R * hd;
