@@ -1075,26 +1075,24 @@ def kv4_alloc(n_layers: int, n_kv_heads: int, head_dim: int, kv_cap: int,
     return torch.zeros((n_layers, n_kv_heads, kv_cap // 64, tile), dtype=torch.uint8, device=device)
 
 
-def _kv4_dims(kv4: torch.Tensor):
-    """(n_layers, n_kv_heads, head_dim, kv_cap) of a cache tensor from kv4_alloc."""
-    if kv4.dtype != torch.uint8 or kv4.dim() != 4 or not kv4.is_contiguous():
+_KV4_HEAD_DIMS = {}
+
+
+def _kv4_dims(kv4: torch.Tensor, layer: int):
+    """(n_kv_heads, head_dim, kv_cap) of a cache tensor from kv4_alloc that holds `layer`."""
+    shape = kv4.shape
+    if len(shape) != 4 or kv4.dtype != torch.uint8 or not kv4.is_contiguous():
         raise ValueError("kv4 must be a contiguous uint8 [layers, heads, tiles, tile bytes] tensor")
-    L, nh, tiles, tile = kv4.shape
+    L, nh, tiles, tile = shape
     hd = _KV4_HEAD_DIMS.get(tile)
     if hd is None:
         hd = next((d for d in (64, 128) if int(lib().hdf_kv4_tile_bytes(d)) == tile), None)
         if hd is None:
             raise ValueError(f"tiles of {tile} bytes belong to no head_dim")
         _KV4_HEAD_DIMS[tile] = hd
-    return L, nh, hd, tiles * 64
-
-
-_KV4_HEAD_DIMS = {}
-
-
-def _kv4_layer(layer: int, L: int):
     if not 0 <= layer < L:
         raise ValueError(f"layer {layer} outside [0, {L})")
+    return nh, hd, tiles * 64
 
 
 def _kv4_rows_arg(rows: Optional[torch.Tensor], n: int, row0: int):
@@ -1105,13 +1103,28 @@ def _kv4_rows_arg(rows: Optional[torch.Tensor], n: int, row0: int):
         raise ValueError("row0 must be in [0, 2^31)")
 
 
-def _row_stride(t: Optional[torch.Tensor], n: int, width: int, what: str) -> int:
-    """Row stride of a [n, width] matrix with unit column stride."""
+def _row_stride(t: Optional[torch.Tensor], shape, what: str) -> int:
+    """Row stride of a matrix of that shape with unit column stride."""
     if t is None:
         return 0
-    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must be [{n}, {width}] with unit column stride")
-    return t.stride(0) if n > 1 else max(t.stride(0), width)
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {list(shape)}")
+    ld, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    return ld if shape[0] > 1 else max(ld, shape[1])
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_here(t: torch.Tensor, stream) -> Optional[int]:
+    """The current stream's handle where it is the one to use, None where _place has to be entered
+    first (a stream given, or another device than the current one)."""
+    device = t.get_device()
+    if stream is None and device >= 0 and device == _current_device():
+        return _current_raw_stream(device)
+    return None
 
 
 def kv4_write_rows(kv4: torch.Tensor, layer: int, k_rows: Optional[torch.Tensor],
@@ -1120,57 +1133,70 @@ def kv4_write_rows(kv4: torch.Tensor, layer: int, k_rows: Optional[torch.Tensor]
     """hdf_kv4_write_rows: row i of k_rows / v_rows [n, n_kv_heads*head_dim] (fp32 or bf16, any row
     stride of whole 16 bytes) quantised into cache row rows[i] (int32 device tensor, each row named
     once) or row0 + i of one layer.  Either of k_rows, v_rows may be None."""
-    L, nh, hd, cap = _kv4_dims(kv4)
+    nh, hd, cap = _kv4_dims(kv4, layer)
     src = k_rows if k_rows is not None else v_rows
     if src is None:
         raise ValueError("give keys or values")
-    n = src.shape[0]
-    _kv4_layer(layer, L)
-    _kv4_rows_arg(rows, n, row0)
-    ld_k = _row_stride(k_rows, n, nh * hd, "k_rows")
-    ld_v = _row_stride(v_rows, n, nh * hd, "v_rows")
-    if k_rows is not None and v_rows is not None and k_rows.dtype != v_rows.dtype:
+    shape = (src.shape[0], nh * hd)
+    _kv4_rows_arg(rows, shape[0], row0)
+    ld_k = _row_stride(k_rows, shape, "k_rows")
+    ld_v = _row_stride(v_rows, shape, "v_rows")
+    if v_rows is not None and v_rows.dtype != src.dtype:
         raise ValueError("k_rows and v_rows must be of one type")
-    with _place(kv4, stream):
-        _same_device(kv4, k_rows, v_rows, rows)
-        _check(lib().hdf_kv4_write_rows(_ptr(k_rows), ld_k, _ptr(v_rows), ld_v, n, _ptr(rows), row0,
-                                        layer, nh, hd, _dt(src), _ptr(kv4), cap, _stream()))
+    raw = _stream_here(kv4, stream)
+    if raw is None:
+        with _place(kv4, stream):
+            return kv4_write_rows(kv4, layer, k_rows, v_rows, row0=row0, rows=rows)
+    _same_device(kv4, k_rows, v_rows, rows)
+    _check(lib().hdf_kv4_write_rows(_ptr(k_rows), ld_k, _ptr(v_rows), ld_v, shape[0], _ptr(rows), row0,
+                                    layer, nh, hd, _dt(src), kv4.data_ptr(), cap, raw))
 
 
 def kv4_read_rows(kv4: torch.Tensor, layer: int, n: int, *, row0: int = 0,
                   rows: Optional[torch.Tensor] = None, dtype=torch.bfloat16, out=None, stream=None):
     """hdf_kv4_read_rows: cache rows rows[i] (or row0 + i), i < n, of one layer as row-major (keys,
     values), each [n, n_kv_heads*head_dim].  out: the same, preallocated (either may be None)."""
-    L, nh, hd, cap = _kv4_dims(kv4)
-    _kv4_layer(layer, L)
+    nh, hd, cap = _kv4_dims(kv4, layer)
     if not 0 <= n <= _INT_MAX:
         raise ValueError("n must be in [0, 2^31)")
     _kv4_rows_arg(rows, n, row0)
-    with _place(kv4, stream):
-        if out is None:
-            k = torch.empty((n, nh * hd), dtype=dtype, device=kv4.device)
-            out = k, torch.empty_like(k)
+    raw = _stream_here(kv4, stream)
+    if raw is None:
+        with _place(kv4, stream):
+            return kv4_read_rows(kv4, layer, n, row0=row0, rows=rows, dtype=dtype, out=out)
+    shape = (n, nh * hd)
+    if out is None:
+        k, v = torch.empty((2, *shape), dtype=dtype, device=kv4.device).unbind(0)
+        ld_k = ld_v = shape[1]
+        _same_device(kv4, rows)
+    else:
         k, v = out
-        src = k if k is not None else v
-        if src is None or (k is not None and v is not None and k.dtype != v.dtype):
-            raise ValueError("out must hold keys or values, of one type")
-        ld_k, ld_v = _row_stride(k, n, nh * hd, "keys"), _row_stride(v, n, nh * hd, "values")
+        ld_k, ld_v = _row_stride(k, shape, "keys"), _row_stride(v, shape, "values")
         _same_device(kv4, k, v, rows)
-        _check(lib().hdf_kv4_read_rows(_ptr(kv4), cap, layer, nh, hd, _dt(src), _ptr(rows), row0, n,
-                                       _ptr(k), ld_k, _ptr(v), ld_v, _stream()))
+    src = k if k is not None else v
+    if src is None or (v is not None and v.dtype != src.dtype):
+        raise ValueError("out must hold keys or values, of one type")
+    _check(lib().hdf_kv4_read_rows(kv4.data_ptr(), cap, layer, nh, hd, _dt(src), _ptr(rows), row0, n,
+                                   _ptr(k), ld_k, _ptr(v), ld_v, raw))
     return k, v
 
 
-def _block_stride(t: torch.Tensor, n_seq: int, B: int, what: str) -> int:
+def _block_stride(t: Optional[torch.Tensor], shape, what: str) -> int:
     """Row stride of a [n_seq, B, heads, head_dim] tensor whose rows (s, k) hold their heads
     contiguously and lie evenly, row s*B + k."""
-    _, _, H, hd = t.shape
+    if t is None:
+        return 0
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {list(shape)}")
+    n_seq, B, H, hd = shape
     s0, s1, s2, s3 = t.stride()
-    ok = (s3 == 1 or hd == 1) and (H == 1 or s2 == hd)
     ld = s1 if B > 1 else s0 if n_seq > 1 else H * hd
-    if not ok or (B > 1 and n_seq > 1 and s0 != B * ld):
+    if s3 != 1 or (H > 1 and s2 != hd) or (B > 1 and n_seq > 1 and s0 != B * ld):
         raise ValueError(f"{what} must hold a slot's heads contiguously and its slots evenly")
     return ld
+
+
+_KV4_WORKSPACES = {}
 
 
 def block_attention_kv4_workspace(n_seq: int, B: int, n_heads: int, n_kv_heads: int, head_dim: int,
@@ -1194,58 +1220,75 @@ def block_attention_kv4(q: torch.Tensor, kv4: Optional[torch.Tensor], layer: int
     or None).  ctx_len, block_len: int32 [n_seq]; scale: 1/sqrt(head_dim) if None; kv4 may be None
     with max_ctx = 0.  q, k_blk, v_blk, out may be columns of wider rows.  out: a preallocated (out,
     lse); outputs of slots from block_len on are left as they were."""
-    if q.dim() != 4:
+    shape = q.shape
+    if len(shape) != 4:
         raise ValueError("q must be [n_seq, B, n_heads, head_dim]")
-    n_seq, B, H, hd = q.shape
-    _int32(max(n_seq, H), "q's sequences and heads")
-    _int32(max_ctx, "max_ctx")
-    dt = _dt(q)
+    n_seq, B, H, hd = shape
+    if not 0 <= max_ctx <= _INT_MAX or n_seq > _INT_MAX or H > _INT_MAX:
+        raise ValueError("max_ctx and q's sizes must be in [0, 2^31)")
     if (k_blk is None) != (v_blk is None):
         raise ValueError("give k_blk and v_blk together")
+    cache = None
     if kv4 is not None:
-        L, nkv, hd_kv, cap = _kv4_dims(kv4)
-        _kv4_layer(layer, L)
+        nkv, hd_kv, cap = _kv4_dims(kv4, layer)
         if hd_kv != hd:
             raise ValueError("q and the cache disagree in head_dim")
-    elif k_blk is not None:
-        nkv = k_blk.shape[2] if k_blk.dim() == 4 else 0
-    else:
-        nkv = H
-    for t, what in ((k_blk, "k_blk"), (v_blk, "v_blk")):
-        if t is not None and (t.dtype != q.dtype or t.shape != (n_seq, B, nkv, hd)):
-            raise ValueError(f"{what} must be [n_seq, B, n_kv_heads, head_dim] of q's type")
-    if kv4 is not None and max_ctx > 0:
-        if (kv_offsets is None) == (page_table is None):
-            raise ValueError("give exactly one of kv_offsets and page_table")
-        if page_table is not None and (page_table.dtype != torch.int32 or page_table.dim() != 2 or
-                                       page_table.shape[0] != n_seq):
-            raise ValueError("page_table must be an int32 [n_seq, max_pages] tensor")
-    _typed(ctx_len, torch.int32, n_seq, "ctx_len")
-    _typed(block_len, torch.int32, n_seq, "block_len")
-    _typed(kv_offsets, torch.int32, n_seq + 1, "kv_offsets")
-    scale = hd ** -0.5 if scale is None else float(scale)
-    with _place(q, stream):
-        if out is None:
-            out = (torch.empty((n_seq, B, H, hd), dtype=q.dtype, device=q.device),
-                   torch.empty((n_seq, B, H), dtype=torch.float32, device=q.device)
-                   if want_lse else None)
-        o, lse = out
-        if o.shape != q.shape or o.dtype != q.dtype:
-            raise ValueError("out must have the shape and the type of q")
-        _typed(lse, torch.float32, n_seq * B * H, "lse")
-        _dev(ctx_len, block_len, kv_offsets, page_table, lse)
-        _same_device(q, kv4, ctx_len, block_len, kv_offsets, page_table, k_blk, v_blk, o, lse)
-        lds = [_block_stride(t, n_seq, B, what) if t is not None else 0
-               for t, what in ((q, "q"), (k_blk, "k_blk"), (v_blk, "v_blk"), (o, "out"))]
-        cache = None
-        if kv4 is not None and max_ctx > 0:
+        if max_ctx > 0:
+            if (kv_offsets is None) == (page_table is None):
+                raise ValueError("give exactly one of kv_offsets and page_table")
+            width = 0
+            if page_table is not None:
+                if page_table.dtype != torch.int32 or page_table.dim() != 2 or \
+                        page_table.shape[0] != n_seq:
+                    raise ValueError("page_table must be an int32 [n_seq, max_pages] tensor")
+                width = page_table.shape[1]
             cache = ctypes.byref(Kv4Cache(kv4.data_ptr(), cap, layer, _ptr(kv_offsets),
-                                          _ptr(page_table),
-                                          page_table.shape[1] if page_table is not None else 0))
-        need = block_attention_kv4_workspace(n_seq, B, H, nkv, hd, max_ctx) if nkv > 0 else 0
-        ws = _scratch(ws, need, q) if need else None
-        _check(lib().hdf_block_attention_kv4(
-            _ptr(q), lds[0], _ptr(k_blk), lds[1], _ptr(v_blk), lds[2], n_seq, B, H, nkv, hd, dt,
-            cache, _ptr(ctx_len), max_ctx, _ptr(block_len), int(causal), scale, _ptr(o), lds[3],
-            _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream()))
-    return o, lse
+                                          _ptr(page_table), width))
+    else:
+        nkv = k_blk.shape[2] if k_blk is not None and k_blk.dim() == 4 else H
+    dt = _dt(q)
+    ld_q = _block_stride(q, shape, "q")
+    ld_k = ld_v = 0
+    if k_blk is not None:
+        kv_shape = (n_seq, B, nkv, hd)
+        ld_k, ld_v = _block_stride(k_blk, kv_shape, "k_blk"), _block_stride(v_blk, kv_shape, "v_blk")
+        if k_blk.dtype != q.dtype or v_blk.dtype != q.dtype:
+            raise ValueError("k_blk and v_blk must be of q's type")
+    for t, numel, what in ((ctx_len, n_seq, "ctx_len"), (block_len, n_seq, "block_len"),
+                           (kv_offsets, n_seq + 1, "kv_offsets")):
+        if t is not None:
+            _typed(t, torch.int32, numel, what)
+    raw = _stream_here(q, stream)
+    if raw is None:
+        with _place(q, stream):
+            return block_attention_kv4(q, kv4, layer, ctx_len=ctx_len, max_ctx=max_ctx,
+                                       kv_offsets=kv_offsets, page_table=page_table, k_blk=k_blk,
+                                       v_blk=v_blk, block_len=block_len, causal=causal, scale=scale,
+                                       want_lse=want_lse, out=out, ws=ws)
+    if out is None:
+        out = (torch.empty(shape, dtype=q.dtype, device=q.device),
+               torch.empty(shape[:3], dtype=torch.float32, device=q.device) if want_lse else None)
+    o, lse = out
+    ld_o = _block_stride(o, shape, "out")
+    if o.dtype != q.dtype:
+        raise ValueError("out must have the type of q")
+    _typed(lse, torch.float32, n_seq * B * H, "lse")
+    _dev(ctx_len, block_len, kv_offsets, page_table, lse)
+    _same_device(q, kv4, ctx_len, block_len, kv_offsets, page_table, k_blk, v_blk, o, lse)
+    # The size depends on these numbers and the card's number of compute units alone.
+    key = (n_seq, B, H, nkv, hd, max_ctx, q.get_device())
+    need = _KV4_WORKSPACES.get(key)
+    if need is None:
+        if len(_KV4_WORKSPACES) > 4096:
+            _KV4_WORKSPACES.clear()
+        need = _KV4_WORKSPACES[key] = block_attention_kv4_workspace(*key[:6]) if nkv > 0 else 0
+    ws_bytes = 0
+    if need:
+        ws = _scratch(ws, need, q)
+        ws_bytes = ws.numel() * ws.element_size()
+    _check(lib().hdf_block_attention_kv4(
+        q.data_ptr(), ld_q, _ptr(k_blk), ld_k, _ptr(v_blk), ld_v, n_seq, B, H, nkv, hd, dt, cache,
+        ctx_len.data_ptr(), max_ctx, _ptr(block_len), 1 if causal else 0,
+        hd ** -0.5 if scale is None else scale, o.data_ptr(), ld_o, _ptr(lse),
+        ws.data_ptr() if need else None, ws_bytes, raw))
+    return out

@@ -128,8 +128,10 @@ def test_binding_refuses_tensors_of_other_shapes_and_types():
             hdf.block_attention_kv4(bad, kv4, 0, **ok)
     with pytest.raises(TypeError):
         hdf.block_attention_kv4(q.half(), kv4, 0, **ok)
-    with pytest.raises(ValueError):
-        hdf._block_stride(torch.zeros(2, 4, 2, 128)[..., :64], 2, 4, "q")
-    with pytest.raises(ValueError):
-        hdf._block_stride(torch.zeros(2, 5, 2, 64)[:, :4], 2, 4, "q")
-    assert hdf._block_stride(torch.zeros(2, 4, 512)[..., :128].view(2, 4, 2, 64), 2, 4, "q") == 512
+    for bad in (torch.zeros(2, 4, 2, 128)[..., :64], torch.zeros(2, 5, 2, 64)[:, :4],
+                torch.zeros(2, 4, 2, 128)[..., ::2]):
+        with pytest.raises(ValueError):
+            hdf._block_stride(bad, (2, 4, 2, 64), "q")
+    wide = torch.zeros(2, 4, 512)[..., :128].view(2, 4, 2, 64)
+    assert hdf._block_stride(wide, (2, 4, 2, 64), "q") == 512
+    assert hdf._block_stride(wide[:1, :1], (1, 1, 2, 64), "q") == 128
