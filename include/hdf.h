@@ -389,6 +389,21 @@ hdf_status hdf_draft_block_paged(const hdf_drafter* w, int n_seq, int B, const i
                                  const int32_t* tokens, void* hidden, void* ws, size_t ws_bytes,
                                  hdf_stream_t stream);
 
+/* The drafter step over a 4-bit cache (hdf_kv4_tile_bytes; n_kv_heads = n_heads): as
+ * hdf_draft_block (kv_offsets) or hdf_draft_block_paged (page_table, optionally new_counts), with
+ * the new rows' keys and values rounded to `dtype`, then quantised into kv4, and the block's own
+ * keys and values in `dtype`, as they are.  The new rows are in the cache before the block attends.
+ * Every other argument and limit is that of those calls and of hdf_block_attention_kv4; a page
+ * outside the cache counts as absent (its rows are not written, and not attended to). */
+size_t hdf_draft_block_kv4_workspace(const hdf_drafter* w, int n_seq, int B, int64_t n_new,
+                                     int max_ctx);
+hdf_status hdf_draft_block_kv4(const hdf_drafter* w, int n_seq, int B, const int32_t* ctx_len,
+                               int max_ctx, const void* y_new, const int32_t* new_offsets,
+                               const int32_t* new_counts, int64_t n_new,
+                               const int32_t* kv_offsets, const int32_t* page_table, int max_pages,
+                               void* kv4, int64_t kv_cap, const int32_t* tokens, void* hidden,
+                               void* ws, size_t ws_bytes, hdf_stream_t stream);
+
 /* ------------------------------------------------------------------------------
  * 3. LM head with fused greedy argmax (Sec. 2.3: z_k are the draft logits).
  *

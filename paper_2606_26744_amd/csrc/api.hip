@@ -103,6 +103,7 @@ hdf_status validate_drafter(const hdf_drafter* w) {
 
 struct DraftPlan {
   size_t plan_pos, plan_row, c, h, u, q, kb, vtb, parts, part_o, part_ml, attn, act, total;
+  size_t ctx_k, ctx_v;   // 4-bit cache: the context rows' keys and values before they are quantised
   int chunk_len;
 };
 
@@ -128,8 +129,9 @@ size_t parts_upto(int64_t rows, int64_t base, bool bf, size_t per_row, size_t fi
 }
 
 // upto: room for every call of at most n_new rows (the size that is reported), else for this one.
+// q4: over a 4-bit cache.
 DraftPlan plan_workspace(const hdf_drafter& w, int n_seq, int B, int64_t n_new, int max_ctx,
-                         bool upto) {
+                         bool upto, bool q4 = false) {
   DraftPlan P{};
   const bool bf = w.dtype == HDF_BF16;
   const size_t el = bf ? 2 : 4;
@@ -219,8 +221,14 @@ DraftPlan plan_workspace(const hdf_drafter& w, int n_seq, int B, int64_t n_new, 
   P.vtb = take(size_t(w.n_heads) * size_t(n_seq) * 64 * w.head_dim * el);
   P.parts = take(parts);
   const size_t pslots = size_t(n_seq) * w.n_heads * (n_chunks + 1) * QB;
-  P.part_o = take(pslots * w.head_dim * 4);
-  P.part_ml = take(pslots * 2 * 4);
+  if (q4) {
+    P.part_o = take(hdf::kv4_attn_ws_bytes(n_seq, w.n_heads, B, w.head_dim, max_ctx));
+    P.ctx_k = take(size_t(crow) * d * el);
+    P.ctx_v = take(size_t(crow) * d * el);
+  } else {
+    P.part_o = take(pslots * w.head_dim * 4);
+    P.part_ml = take(pslots * 2 * 4);
+  }
   P.attn = take(M * d * el);
   P.act = take(M * F * el);
   P.total = off;
@@ -706,8 +714,9 @@ size_t hdf_draft_block_workspace(const hdf_drafter* w, int n_seq, int B, int64_t
 }
 
 // Both cache forms: kv_offsets (contiguous slots) or page_table (pages of 64 rows; the
-// cache then holds kv_cap / 64 pages).
-static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const int32_t* ctx_len,
+// cache then holds kv_cap / 64 pages).  q4: kv_k is a 4-bit cache (hdf_kv4_*), kv_vt the same
+// pointer.
+static hdf_status draft_block_impl(bool q4, const hdf_drafter* w, int n_seq, int B, const int32_t* ctx_len,
                                    int max_ctx, const void* y_new, const int32_t* new_offsets,
                                    const int32_t* new_counts, int64_t n_new,
                                    const int32_t* kv_offsets,
@@ -741,7 +750,7 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
   if (!aligned16(hidden) || (y_new && !aligned16(y_new)) || (kv_k && !aligned16(kv_k)) ||
       (kv_vt && !aligned16(kv_vt)))
     return fail(HDF_E_INVALID, "draft_block: tensors must be 16-byte aligned");
-  const DraftPlan P = plan_workspace(*w, n_seq, B, n_new, max_ctx, false);
+  const DraftPlan P = plan_workspace(*w, n_seq, B, n_new, max_ctx, false, q4);
   if (ws == nullptr || ws_bytes < P.total)
     return fail(HDF_E_WORKSPACE, "draft_block: workspace of %zu bytes needed, %zu given", P.total,
                 ws_bytes);
@@ -801,6 +810,11 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
     ea.k = static_cast<char*>(kv_k) + l * layer_kv;
     ea.vt = static_cast<char*>(kv_vt) + l * layer_kv;
     ea.cap = kv_cap;
+    if (q4) {
+      ea.flat = 1;
+      ea.k = base + P.ctx_k;
+      ea.vt = base + P.ctx_v;
+    }
     return ea;
   };
   auto blk_epi = [&](int S, const float* pp) {
@@ -811,7 +825,17 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
     ea.d = d; ea.nh = nh; ea.hd = hd; ea.B = B;
     ea.ctx_len = ctx_len; ea.rope_cs = w->rope_cs;
     ea.q = q; ea.k = kb; ea.vt = vtb; ea.cap = capb;
+    ea.flat = q4 ? 1 : 0;
     return ea;
+  };
+  // 4-bit cache: the epilogue's context rows r0 .. quantised into the layer's tiles.
+  auto quantise = [&](int l, int64_t r0, int rows) {
+    hdf::Kv4RowArgs ra{};
+    ra.tiles = kv4_layer(kv_k, l, nh, hd, kv_cap);
+    ra.cap = kv_cap;
+    ra.k = base + P.ctx_k; ra.v = base + P.ctx_v; ra.ld_k = d; ra.ld_v = d;
+    ra.n = rows; ra.rows = plan_row + r0; ra.nh = nh;
+    return hdf::launch_kv4_rows(bf, true, hd, ra, s);
   };
   // Context rows projected in this call: with a bf16 drafter and at most kGroupRows of
   // them, each layer's context K/V share one GEMM launch and one epilogue launch with
@@ -828,7 +852,7 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
       // Rows d..3d-1 (W_k; W_v) of the packed W_qkv: d/128 whole row groups in.
       const char* wkv = static_cast<const char*>(w->w_qkv[l]) + size_t(d) * d * el;
       const hdf::GemmPlan Sp = hdf::gemm_plan(bf, rows, 2 * d, d);
-      if (bf && Sp.tn > 1 && Sp.splits == 1 && (hd == 64 || hd == 128) && d % 512 == 0) {
+      if (!q4 && bf && Sp.tn > 1 && Sp.splits == 1 && (hd == 64 || hd == 128) && d % 512 == 0) {
         // One K split: RoPE and the cache stores happen in the GEMM's epilogue, so the
         // fp32 rows never go through memory.
         HDF_TRY(hdf::launch_gemm_kv(cbuf, d, wkv, rows, d, hd, Sp, plan_pos + r0, plan_row + r0,
@@ -837,6 +861,7 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
       } else {
         HDF_TRY(hdf::launch_gemm_partial(bf, cbuf, d, wkv, rows, 2 * d, d, Sp, parts, s));
         HDF_TRY(hdf::launch_qkv_epilogue(bf, ctx_epi(l, r0, rows, Sp.splits, parts), s));
+        if (q4) HDF_TRY(quantise(l, r0, rows));
       }
     }
   }
@@ -844,7 +869,7 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
   const int n_chunks = std::max(1, (max_ctx + P.chunk_len - 1) / P.chunk_len);
   // With one attention workgroup per (sequence, head), the projection epilogue of the
   // shared launch runs inside the attention kernel (no launch of its own).
-  const bool fuse_epi = shared && n_chunks == 1 && B <= 16 && (hd == 64 || hd == 128);
+  const bool fuse_epi = !q4 && shared && n_chunks == 1 && B <= 16 && (hd == 64 || hd == 128);
   for (int l = 0; l < L; ++l) {
     hdf::QkvEpiArgs fused_ctx{}, fused_blk{};
     // Q, K_b, V_b with RoPE at T_s + k (and the context rows' K/V when grouped).
@@ -883,23 +908,41 @@ static hdf_status draft_block_impl(const hdf_drafter* w, int n_seq, int B, const
       HDF_TRY(hdf::launch_qkv_epilogue(bf, blk_epi(Sqp.splits, parts), s));
     }
 
-    hdf::AttnArgs aa{};
-    aa.q = q;
-    aa.kc = static_cast<char*>(kv_k) + l * layer_kv;
-    aa.vtc = static_cast<char*>(kv_vt) + l * layer_kv;
-    aa.cap = kv_cap; aa.kv_offsets = kv_offsets; aa.ctx_len = ctx_len;
-    aa.page_table = page_table; aa.max_pages = max_pages;
-    aa.kb = kb; aa.vtb = vtb; aa.capb = capb;
-    aa.n_seq = n_seq; aa.nh = nh; aa.hd = hd; aa.B = B; aa.QB = ((B + 15) / 16) * 16;
-    aa.n_chunks = n_chunks; aa.chunk_len = P.chunk_len;
-    aa.scale = float(1.0 / sqrt(double(hd)));
-    aa.scale_log2 = float(1.4426950408889634 / sqrt(double(hd)));
-    aa.part_o = part_o; aa.part_ml = part_ml;
-    aa.fuse_epi = fuse_epi ? 1 : 0;
-    aa.new_offsets = new_offsets;
-    aa.epi_ctx = fused_ctx;
-    aa.epi_blk = fused_blk;
-    HDF_TRY(hdf::launch_attention(bf, aa, attn, s));
+    if (q4) {
+      if (grouped) HDF_TRY(quantise(l, 0, int(n_new)));
+      hdf::Kv4AttnArgs ka{};
+      ka.q = q; ka.ld_q = d;
+      ka.kb = kb; ka.vb = vtb; ka.ld_kb = d; ka.ld_vb = d;
+      if (max_ctx > 0) {
+        ka.tiles = kv4_layer(kv_k, l, nh, hd, kv_cap);
+        ka.n_tiles = kv_cap / 64;
+        ka.kv_offsets = page_table != nullptr ? nullptr : kv_offsets;
+        ka.page_table = page_table; ka.max_pages = max_pages;
+      }
+      ka.ctx_len = ctx_len; ka.max_ctx = max_ctx;
+      ka.n_seq = n_seq; ka.B = B; ka.nh = nh; ka.nkv = nh;
+      ka.scale_log2 = float(1.4426950408889634 / sqrt(double(hd)));
+      ka.out = attn; ka.ld_out = d;
+      HDF_TRY(hdf::launch_kv4_attention(bf, hd, ka, part_o, s));
+    } else {
+      hdf::AttnArgs aa{};
+      aa.q = q;
+      aa.kc = static_cast<char*>(kv_k) + l * layer_kv;
+      aa.vtc = static_cast<char*>(kv_vt) + l * layer_kv;
+      aa.cap = kv_cap; aa.kv_offsets = kv_offsets; aa.ctx_len = ctx_len;
+      aa.page_table = page_table; aa.max_pages = max_pages;
+      aa.kb = kb; aa.vtb = vtb; aa.capb = capb;
+      aa.n_seq = n_seq; aa.nh = nh; aa.hd = hd; aa.B = B; aa.QB = ((B + 15) / 16) * 16;
+      aa.n_chunks = n_chunks; aa.chunk_len = P.chunk_len;
+      aa.scale = float(1.0 / sqrt(double(hd)));
+      aa.scale_log2 = float(1.4426950408889634 / sqrt(double(hd)));
+      aa.part_o = part_o; aa.part_ml = part_ml;
+      aa.fuse_epi = fuse_epi ? 1 : 0;
+      aa.new_offsets = new_offsets;
+      aa.epi_ctx = fused_ctx;
+      aa.epi_blk = fused_blk;
+      HDF_TRY(hdf::launch_attention(bf, aa, attn, s));
+    }
 
     // h += O Wo^T; u = RMSNorm(h) * mlp_norm.
     const hdf::GemmPlan Sop = hdf::gemm_plan(bf, M, d, d);
@@ -933,7 +976,7 @@ hdf_status hdf_draft_block(const hdf_drafter* w, int n_seq, int B, const int32_t
                            int64_t kv_cap, const int32_t* tokens, void* hidden, void* ws,
                            size_t ws_bytes, hdf_stream_t stream) {
   if (n_seq > 0 && kv_offsets == nullptr) return fail(HDF_E_INVALID, "draft_block: null kv_offsets");
-  return draft_block_impl(w, n_seq, B, ctx_len, max_ctx, y_new, new_offsets, nullptr, n_new,
+  return draft_block_impl(false, w, n_seq, B, ctx_len, max_ctx, y_new, new_offsets, nullptr, n_new,
                           kv_offsets, nullptr, 0, kv_k, kv_vt, kv_cap, tokens, hidden, ws,
                           ws_bytes, stream);
 }
@@ -951,9 +994,37 @@ hdf_status hdf_draft_block_paged(const hdf_drafter* w, int n_seq, int B, const i
   if (kv_pages < 0 || kv_pages > INT32_MAX / 64)
     return fail(HDF_E_INVALID, "draft_block_paged: kv_pages=%lld outside [0, 2^25)",
                 static_cast<long long>(kv_pages));
-  return draft_block_impl(w, n_seq, B, ctx_len, max_ctx, y_new, new_offsets, new_counts, n_new,
+  return draft_block_impl(false, w, n_seq, B, ctx_len, max_ctx, y_new, new_offsets, new_counts, n_new,
                           nullptr, page_table, max_pages, kv_k, kv_vt, kv_pages * 64, tokens,
                           hidden, ws, ws_bytes, stream);
+}
+
+size_t hdf_draft_block_kv4_workspace(const hdf_drafter* w, int n_seq, int B, int64_t n_new,
+                                     int max_ctx) {
+  if (validate_drafter(w) != HDF_OK || n_new < 0 ||
+      kv4_attn_shape("draft_block_kv4", n_seq, B, w->n_heads, w->n_heads, w->head_dim, max_ctx) != HDF_OK)
+    return 0;
+  return plan_workspace(*w, n_seq, B, n_new, max_ctx, true, true).total;
+}
+
+hdf_status hdf_draft_block_kv4(const hdf_drafter* w, int n_seq, int B, const int32_t* ctx_len,
+                               int max_ctx, const void* y_new, const int32_t* new_offsets,
+                               const int32_t* new_counts, int64_t n_new,
+                               const int32_t* kv_offsets, const int32_t* page_table, int max_pages,
+                               void* kv4, int64_t kv_cap, const int32_t* tokens, void* hidden,
+                               void* ws, size_t ws_bytes, hdf_stream_t stream) {
+  hdf_status st = validate_drafter(w);
+  if (st == HDF_OK)
+    st = kv4_attn_shape("draft_block_kv4", n_seq, B, w->n_heads, w->n_heads, w->head_dim, max_ctx);
+  if (st != HDF_OK) return st;
+  if (n_seq > 0 && (kv_offsets == nullptr) == (page_table == nullptr))
+    return fail(HDF_E_INVALID, "draft_block_kv4: give one of kv_offsets and page_table");
+  if (max_pages < 0) return fail(HDF_E_INVALID, "draft_block_kv4: max_pages < 0");
+  if (new_counts != nullptr && page_table == nullptr)
+    return fail(HDF_E_INVALID, "draft_block_kv4: new_counts goes with a paged cache");
+  return draft_block_impl(true, w, n_seq, B, ctx_len, max_ctx, y_new, new_offsets, new_counts, n_new,
+                          kv_offsets, page_table, max_pages, kv4, kv4, kv_cap, tokens, hidden, ws,
+                          ws_bytes, stream);
 }
 
 hdf_status hdf_advance_context(int n_seq, const int32_t* accept_len, int32_t* ctx_len,

@@ -149,6 +149,9 @@ struct QkvEpiArgs {
   void* k;                  // [nh][cap][hd]
   void* vt;                 // [nh][hd][cap]
   int64_t cap;
+  // flat (the stand-alone epilogue): q, k, vt are row-major [M][d] instead, row r of the set at row r
+  // (context rows that are not new are left out).
+  int flat;
 };
 
 struct PrepArgs {

@@ -75,7 +75,8 @@ __device__ __forceinline__ void epi_add4(float4& x, const float4 t) {
   x.x += t.x; x.y += t.y; x.z += t.z; x.w += t.w;
 }
 
-template <typename T, int HD>
+// FLAT: row-major destinations (QkvEpiArgs flat).
+template <typename T, int HD, bool FLAT = false>
 __device__ __forceinline__ void qkv_epi_tile(const QkvEpiArgs& a, int r0, int rows, int h,
                                              int tid, QkvEpiSmem<HD>& sm) {
   constexpr int HALF = HD / 2;
@@ -160,7 +161,11 @@ __device__ __forceinline__ void qkv_epi_tile(const QkvEpiArgs& a, int r0, int ro
         rope_rotate(y1[2 * j + 1], y2[2 * j + 1], cs[j].z, cs[j].w);
       }
     }
-    if (part == 0) {
+    if constexpr (FLAT) {
+      T* dst = static_cast<T*>(part == 0 ? a.q : a.k) + int64_t(r0 + rr) * a.d + h * HD;
+      epi_store8<T>(dst + i0, y1);
+      epi_store8<T>(dst + i0 + HALF, y2);
+    } else if (part == 0) {
       T* dst = static_cast<T*>(a.q) + ((int64_t(sm.seq[rr]) * a.nh + h) * a.B + sm.slot[rr]) * HD;
       epi_store8<T>(dst + i0, y1);
       epi_store8<T>(dst + i0 + HALF, y2);
@@ -170,6 +175,13 @@ __device__ __forceinline__ void qkv_epi_tile(const QkvEpiArgs& a, int r0, int ro
       epi_store8<T>(kh + kc_index(sm.drow[rr], i0, HD), y1);
       epi_store8<T>(kh + kc_index(sm.drow[rr], i0 + HALF, HD), y2);
     }
+  }
+  if constexpr (FLAT) {
+    if (has_v && sm.drow[rv] >= 0) {
+      const float y[8] = {xv[0].x, xv[0].y, xv[0].z, xv[0].w, xv[1].x, xv[1].y, xv[1].z, xv[1].w};
+      epi_store8<T>(static_cast<T*>(a.vt) + int64_t(r0 + rv) * a.d + h * HD + 8 * ov, y);
+    }
+    return;   // no tile to read back
   }
   if (has_v) {
     float* t = &sm.vt_tile[rv][8 * ov];

@@ -205,14 +205,14 @@ residual_norm_kernel(const float* __restrict__ parts, int S, int64_t M,
 
 // Projection epilogue: one workgroup per tile of kQkvRows rows x one head (qkv_epi.hpp);
 // the tiles of the first set of rows, then those of the optional second one.
-template <typename T, int HD>
+template <typename T, int HD, bool FLAT>
 __global__ void __launch_bounds__(kQkvThreads)
 qkv_epilogue_kernel(QkvEpiArgs a0, QkvEpiArgs a1, int nb0) {
   __shared__ QkvEpiSmem<HD> sm;
   const bool second = int(blockIdx.x) >= nb0;
   const QkvEpiArgs a = second ? a1 : a0;
   const int r0 = (second ? int(blockIdx.x) - nb0 : int(blockIdx.x)) * kQkvRows;
-  qkv_epi_tile<T, HD>(a, r0, min(kQkvRows, a.M - r0), int(blockIdx.y), int(threadIdx.x), sm);
+  qkv_epi_tile<T, HD, FLAT>(a, r0, min(kQkvRows, a.M - r0), int(blockIdx.y), int(threadIdx.x), sm);
 }
 
 template <typename T>
@@ -313,6 +313,22 @@ hipError_t launch_residual_norm(bool bf16, const float* parts, int S, const floa
   return hipGetLastError();
 }
 
+template <bool FLAT>
+static void qkv_epilogue_t(bool bf16, int hd, const dim3& grid, const QkvEpiArgs& a, const QkvEpiArgs& b,
+                           int nb0, hipStream_t s) {
+  if (bf16) {
+    if (hd == 128)
+      hipLaunchKernelGGL((qkv_epilogue_kernel<bf16_t, 128, FLAT>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
+    else
+      hipLaunchKernelGGL((qkv_epilogue_kernel<bf16_t, 64, FLAT>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
+  } else {
+    if (hd == 128)
+      hipLaunchKernelGGL((qkv_epilogue_kernel<float, 128, FLAT>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
+    else
+      hipLaunchKernelGGL((qkv_epilogue_kernel<float, 64, FLAT>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
+  }
+}
+
 hipError_t launch_qkv_epilogue2(bool bf16, const QkvEpiArgs& a, const QkvEpiArgs& b,
                                 hipStream_t s) {
   const int nb0 = a.M > 0 ? (a.M + kQkvRows - 1) / kQkvRows : 0;
@@ -320,17 +336,10 @@ hipError_t launch_qkv_epilogue2(bool bf16, const QkvEpiArgs& a, const QkvEpiArgs
   if (nb0 + nb1 == 0) return hipSuccess;
   const int nh = nb0 > 0 ? a.nh : b.nh, hd = nb0 > 0 ? a.hd : b.hd;
   const dim3 grid(unsigned(nb0 + nb1), unsigned(nh));
-  if (bf16) {
-    if (hd == 128)
-      hipLaunchKernelGGL((qkv_epilogue_kernel<bf16_t, 128>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
-    else
-      hipLaunchKernelGGL((qkv_epilogue_kernel<bf16_t, 64>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
-  } else {
-    if (hd == 128)
-      hipLaunchKernelGGL((qkv_epilogue_kernel<float, 128>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
-    else
-      hipLaunchKernelGGL((qkv_epilogue_kernel<float, 64>), grid, dim3(kQkvThreads), 0, s, a, b, nb0);
-  }
+  if (a.flat)
+    qkv_epilogue_t<true>(bf16, hd, grid, a, b, nb0, s);
+  else
+    qkv_epilogue_t<false>(bf16, hd, grid, a, b, nb0, s);
   return hipGetLastError();
 }
 

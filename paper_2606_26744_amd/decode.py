@@ -71,12 +71,13 @@ def pages_for(lengths, max_ctx: int) -> np.ndarray:
 
 
 class PagedDecoder:
-    """Decoding state of n_seq sequences: a paged KV cache, each sequence's pages and
-    context length, the block tokens (anchor + masks) and the step buffers."""
+    """Decoding state of n_seq sequences: a paged KV cache (kv_bits 4: held in 4 bits, kv_k
+    the cache and kv_vt None), each sequence's pages and context length, the block tokens
+    (anchor + masks) and the step buffers."""
 
     def __init__(self, handle: hdf.DrafterHandle, n_seq: int, B: int, max_ctx: int,
                  n_pages: int, max_new_rows: int, device="cuda",
-                 page_order: Optional[Sequence[int]] = None):
+                 page_order: Optional[Sequence[int]] = None, kv_bits: Optional[int] = None):
         if handle.w_lm is None:
             raise ValueError("the drafter handle carries no LM head")
         self.h, self.n_seq, self.B, self.max_ctx = handle, n_seq, B, max_ctx
@@ -84,12 +85,12 @@ class PagedDecoder:
         self.pool = PagePool(n_pages, page_order)
         self.pages: List[List[int]] = [[] for _ in range(n_seq)]
         self.ctx = np.zeros(n_seq, dtype=np.int64)          # T_s on the host
-        self.kv_k, self.kv_vt = handle.alloc_kv(n_pages * 64, device=device)
+        self.kv_k, self.kv_vt = handle.alloc_kv(n_pages * 64, device=device, kv_bits=kv_bits)
         dt, d = handle.torch_dtype, handle.d
         self.max_new_rows = max_new_rows
         self.Y = torch.empty((max(max_new_rows, 1), d), dtype=dt, device=device)
         self.hidden = torch.empty((n_seq * B, d), dtype=dt, device=device)
-        self.ws = torch.empty(max(handle.workspace_bytes(n_seq, B, max_new_rows, max_ctx), 1),
+        self.ws = torch.empty(max(handle.workspace_bytes(n_seq, B, max_new_rows, max_ctx, kv_bits), 1),
                               dtype=torch.uint8, device=device)
         self.lm_ws = torch.zeros(max(hdf.lm_head_workspace(n_seq * B, handle.V), 1),
                                  dtype=torch.uint8, device=device)

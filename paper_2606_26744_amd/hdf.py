@@ -37,7 +37,8 @@ EXPORTS = ("hdf_last_error", "hdf_version", "hdf_hc_reduce", "hdf_rope_table",
            "hdf_top_logits_workspace", "hdf_top_logits", "hdf_distill_saved_bytes",
            "hdf_distill_workspace", "hdf_distill_forward", "hdf_distill_backward",
            "hdf_kv4_tile_bytes", "hdf_kv4_cache_bytes", "hdf_kv4_write_rows", "hdf_kv4_read_rows",
-           "hdf_block_attention_kv4_workspace", "hdf_block_attention_kv4")
+           "hdf_block_attention_kv4_workspace", "hdf_block_attention_kv4",
+           "hdf_draft_block_kv4_workspace", "hdf_draft_block_kv4")
 
 
 class HdfError(RuntimeError):
@@ -191,6 +192,11 @@ def lib() -> ctypes.CDLL:
     L.hdf_block_attention_kv4.argtypes = [_P, _I64, _P, _I64, _P, _I64, _I, _I, _I, _I, _I, _I,
                                           ctypes.POINTER(Kv4Cache), _P, _I, _P, _I, _F, _P, _I64,
                                           _P, _P, _SZ, _P]
+    L.hdf_draft_block_kv4_workspace.restype = _SZ
+    L.hdf_draft_block_kv4_workspace.argtypes = [ctypes.POINTER(Drafter), _I, _I, _I64, _I]
+    L.hdf_draft_block_kv4.restype = _I
+    L.hdf_draft_block_kv4.argtypes = [ctypes.POINTER(Drafter), _I, _I, _P, _I, _P, _P, _P, _I64, _P,
+                                      _P, _I, _P, _I64, _P, _P, _P, _SZ, _P]
     _lib = L
     return L
 
@@ -897,25 +903,33 @@ class DrafterHandle:
     def kv_cache_bytes(self, kv_cap: int) -> int:
         return int(lib().hdf_kv_cache_bytes(ctypes.byref(self.s), kv_cap))
 
-    def workspace_bytes(self, n_seq: int, B: int, n_new: int, max_ctx: int) -> int:
-        return int(lib().hdf_draft_block_workspace(ctypes.byref(self.s), n_seq, B, n_new, max_ctx))
+    def workspace_bytes(self, n_seq: int, B: int, n_new: int, max_ctx: int,
+                        kv_bits: Optional[int] = None) -> int:
+        """Bytes of draft_block's workspace; kv_bits 4: over a 4-bit cache."""
+        f = lib().hdf_draft_block_workspace if not _is_kv4(kv_bits) else \
+            lib().hdf_draft_block_kv4_workspace
+        return int(f(ctypes.byref(self.s), n_seq, B, n_new, max_ctx))
 
-    def _workspace(self, n_seq, B, n_new, max_ctx, device) -> torch.Tensor:
-        return torch.empty(max(self.workspace_bytes(n_seq, B, n_new, max_ctx), 1), dtype=torch.uint8,
-                           device=device)
+    def _workspace(self, n_seq, B, n_new, max_ctx, device, kv_bits=None) -> torch.Tensor:
+        return torch.empty(max(self.workspace_bytes(n_seq, B, n_new, max_ctx, kv_bits), 1),
+                           dtype=torch.uint8, device=device)
 
-    def alloc_kv(self, kv_cap: int, device="cuda"):
-        """KV cache tensors in the library's layout: keys and values each
-        [L][nh][cap/64][64*hd], 64-position tiles in matrix-core operand order."""
+    def alloc_kv(self, kv_cap: int, device="cuda", kv_bits: Optional[int] = None):
+        """KV cache tensors (keys, values) in the library's layout, each
+        [L][nh][cap/64][64*hd], 64-position tiles in matrix-core operand order; kv_bits 4: the 4-bit
+        cache (kv4_alloc) in the place of the keys, and None."""
         if kv_cap % 64:
             raise ValueError("kv_cap must be a multiple of 64")
+        if _is_kv4(kv_bits):
+            return kv4_alloc(self.L, self.nh, self.hd, kv_cap, device=device), None
         shape = (self.L, self.nh, kv_cap // 64, 64 * self.hd)
         return (torch.zeros(shape, dtype=self.torch_dtype, device=device),
                 torch.zeros(shape, dtype=self.torch_dtype, device=device))
 
     def draft_block(self, *, ctx_len: torch.Tensor, max_ctx: int, y_new: torch.Tensor,
-                    new_offsets: torch.Tensor, kv_k: torch.Tensor, kv_vt: torch.Tensor,
-                    tokens: torch.Tensor, kv_offsets: Optional[torch.Tensor] = None,
+                    new_offsets: torch.Tensor, kv_k: torch.Tensor,
+                    kv_vt: Optional[torch.Tensor], tokens: torch.Tensor,
+                    kv_offsets: Optional[torch.Tensor] = None,
                     page_table: Optional[torch.Tensor] = None,
                     new_counts: Optional[torch.Tensor] = None,
                     hidden: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
@@ -923,7 +937,8 @@ class DrafterHandle:
         """hdf_draft_block over a contiguous cache (kv_offsets [n_seq+1]) or
         hdf_draft_block_paged over a paged one (page_table [n_seq][max_pages], optionally
         with device new_counts [n_seq]: only the first new_counts[s] rows of each
-        sequence's rows in y_new are new)."""
+        sequence's rows in y_new are new).  kv_k a 4-bit cache (alloc_kv(kv_bits=4)) and
+        kv_vt None: hdf_draft_block_kv4, over either."""
         if (kv_offsets is None) == (page_table is None):
             raise ValueError("give exactly one of kv_offsets and page_table")
         if new_counts is not None and page_table is None:
@@ -931,11 +946,18 @@ class DrafterHandle:
         n_seq, B = tokens.shape
         n_new = y_new.shape[0]
         dev = tokens.device
+        kv_bits = 4 if kv_k.dtype == torch.uint8 else None
+        if kv_bits == 4:
+            nkv, hd, kv_cap = _kv4_dims(kv_k, self.L - 1)
+            if kv_vt is not None or kv_k.shape[0] != self.L or (nkv, hd) != (self.nh, self.hd):
+                raise ValueError("a 4-bit cache of this drafter's layers and heads goes with kv_vt=None")
+        elif kv_vt is None:
+            raise ValueError("a cache of keys needs one of values")
         if hidden is None:
             hidden = torch.empty((n_seq * B, self.d), dtype=self.torch_dtype, device=dev)
         if ws is None or ((not ws.is_cuda or not ws.is_contiguous()) and
-                          ws.numel() < self.workspace_bytes(n_seq, B, n_new, max_ctx)):
-            ws = self._workspace(n_seq, B, n_new, max_ctx, dev)
+                          ws.numel() < self.workspace_bytes(n_seq, B, n_new, max_ctx, kv_bits)):
+            ws = self._workspace(n_seq, B, n_new, max_ctx, dev, kv_bits)
         if page_table is not None:
             if page_table.dtype != torch.int32 or page_table.dim() != 2 or \
                     page_table.shape[0] != n_seq or not page_table.is_contiguous():
@@ -943,8 +965,20 @@ class DrafterHandle:
             if new_counts is not None and (new_counts.dtype != torch.int32 or
                                            new_counts.numel() != n_seq):
                 raise ValueError("new_counts must be an int32 [n_seq] tensor")
+        if kv_bits == 4:
+            _dev(ctx_len, y_new, new_offsets, new_counts, kv_offsets, page_table, kv_k, tokens, hidden,
+                 ws)
+
+            def call(ws):
+                return lib().hdf_draft_block_kv4(
+                    ctypes.byref(self.s), n_seq, B, _ptr(ctx_len), max_ctx, _ptr(y_new),
+                    _ptr(new_offsets), _ptr(new_counts), n_new, _ptr(kv_offsets), _ptr(page_table),
+                    0 if page_table is None else page_table.shape[1], _ptr(kv_k), kv_cap,
+                    _ptr(tokens), _ptr(hidden), _ptr(ws), ws.numel(), _stream(stream))
+        elif page_table is not None:
             _dev(ctx_len, y_new, new_offsets, new_counts, page_table, kv_k, kv_vt, tokens, hidden,
                  ws)
+
             def call(ws):
                 return lib().hdf_draft_block_paged(
                     ctypes.byref(self.s), n_seq, B, _ptr(ctx_len), max_ctx, _ptr(y_new),
@@ -962,7 +996,7 @@ class DrafterHandle:
                     _stream(stream))
         st = call(ws)
         if st == HDF_E_WORKSPACE:   # a given workspace of fewer bytes than this call's
-            st = call(self._workspace(n_seq, B, n_new, max_ctx, dev))
+            st = call(self._workspace(n_seq, B, n_new, max_ctx, dev, kv_bits))
         _check(st)
         return hidden
 
@@ -1062,6 +1096,12 @@ def kv_slot_offsets(ctx_lens: Sequence[int]) -> list:
 
 
 # ------------------------------------------------------------------------- 4-bit cache
+
+def _is_kv4(kv_bits: Optional[int]) -> bool:
+    if kv_bits not in (None, 4):
+        raise ValueError(f"kv_bits must be 4 or None (the working type), not {kv_bits!r}")
+    return kv_bits == 4
+
 
 def kv4_alloc(n_layers: int, n_kv_heads: int, head_dim: int, kv_cap: int,
               device="cuda") -> torch.Tensor:

@@ -37,15 +37,16 @@ class SampledStepBuffers:
 
 
 class StepBuffers:
-    """Device buffers of one step, reused across steps (nothing is allocated per call)."""
+    """Device buffers of one step, reused across steps (nothing is allocated per call).
+    kv_bits 4: for steps over a 4-bit cache (kv_k, kv_vt from handle.alloc_kv(kv_bits=4))."""
 
     def __init__(self, handle: hdf.DrafterHandle, n_seq: int, B: int, n_new: int, max_ctx: int,
-                 m: int, device="cuda"):
+                 m: int, device="cuda", kv_bits: Optional[int] = None):
         dt = handle.torch_dtype
         d = handle.d
         self.Y = torch.empty((n_new, d), dtype=dt, device=device)
         self.hidden = torch.empty((n_seq * B, d), dtype=dt, device=device)
-        self.ws = torch.empty(max(handle.workspace_bytes(n_seq, B, n_new, max_ctx), 1),
+        self.ws = torch.empty(max(handle.workspace_bytes(n_seq, B, n_new, max_ctx, kv_bits), 1),
                               dtype=torch.uint8, device=device)
         self.lm_ws = torch.zeros(max(hdf.lm_head_workspace(n_seq * B, handle.V), 1),
                                  dtype=torch.uint8, device=device)   # zero before first use
@@ -56,7 +57,7 @@ class StepBuffers:
 def drafter_step(handle: hdf.DrafterHandle, bufs: StepBuffers, *, H_new: torch.Tensor,
                  W_g: torch.Tensor, b_g: torch.Tensor, new_offsets: torch.Tensor,
                  ctx_len: torch.Tensor, max_ctx: int, kv_offsets: torch.Tensor,
-                 kv_k: torch.Tensor, kv_vt: torch.Tensor, tokens: torch.Tensor,
+                 kv_k: torch.Tensor, kv_vt: Optional[torch.Tensor], tokens: torch.Tensor,
                  targets: Optional[torch.Tensor], reduce_kw: Optional[dict] = None,
                  stream=None, logits: bool = False, marks: Optional[list] = None):
     """Runs reduce -> draft block -> LM head argmax -> accept.  Returns a dict of device
@@ -104,7 +105,8 @@ def drafter_step(handle: hdf.DrafterHandle, bufs: StepBuffers, *, H_new: torch.T
 def drafter_step_sampled(handle: hdf.DrafterHandle, bufs: StepBuffers, sbufs: SampledStepBuffers,
                          *, H_new: torch.Tensor, W_g: torch.Tensor, b_g: torch.Tensor,
                          new_offsets: torch.Tensor, ctx_len: torch.Tensor, max_ctx: int,
-                         kv_offsets: torch.Tensor, kv_k: torch.Tensor, kv_vt: torch.Tensor,
+                         kv_offsets: torch.Tensor, kv_k: torch.Tensor,
+                         kv_vt: Optional[torch.Tensor],
                          tokens: torch.Tensor, target_logits: torch.Tensor,
                          temperature: float = 1.0, seed: int = 0, round_id: int = 0,
                          reduce_kw: Optional[dict] = None, stream=None):
@@ -161,7 +163,7 @@ def drafter_step_truncated(handle: hdf.DrafterHandle, bufs: StepBuffers,
                            tbufs: TruncatedStepBuffers, *, H_new: torch.Tensor, W_g: torch.Tensor,
                            b_g: torch.Tensor, new_offsets: torch.Tensor, ctx_len: torch.Tensor,
                            max_ctx: int, kv_offsets: torch.Tensor, kv_k: torch.Tensor,
-                           kv_vt: torch.Tensor, tokens: torch.Tensor, target_logits: torch.Tensor,
+                           kv_vt: Optional[torch.Tensor], tokens: torch.Tensor, target_logits: torch.Tensor,
                            draft_uniforms: torch.Tensor, accept_uniforms: torch.Tensor,
                            temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
                            reduce_kw: Optional[dict] = None, stream=None):

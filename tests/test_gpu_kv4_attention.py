@@ -177,3 +177,51 @@ def test_a_larger_workspace_serves_and_lse_is_optional():
     want, _ = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
     got, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, want_lse=False, ws=ws, **c.kw)
     assert lse is None and torch.equal(want, got)
+
+
+def test_written_and_attended_to_in_a_graph():
+    """A round (new rows into the cache, then the block) captured and replayed, with eager work and
+    other contents between the replays."""
+    c = Case([700, 3000], 4, 4, 2, 128, BF, seed=10)
+    nkv, hd = c.nkv, c.hd
+    rows = torch.cat([hdf.paged_rows(c.kw["page_table"][s].tolist(), t, "cuda")[-3:]
+                      for s, t in enumerate(c.ctx)]).contiguous()
+    k = torch.zeros(6, nkv * hd, dtype=BF, device="cuda")
+    v = torch.zeros_like(k)
+    out = (torch.zeros_like(c.q), torch.zeros(2, 4, 4, device="cuda"))
+    ws = torch.zeros(hdf.block_attention_kv4_workspace(2, 4, 4, nkv, hd, c.max_ctx), dtype=torch.uint8,
+                     device="cuda")
+
+    def step(o):
+        hdf.kv4_write_rows(c.kv4, 0, k, v, rows=rows)
+        hdf.block_attention_kv4(c.q, c.kv4, 0, out=o, ws=ws, **c.kw)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(out)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for i in range(4):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        k.copy_(torch.randn(k.shape, generator=g, device="cuda"))
+        v.copy_(torch.randn(v.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in out]
+        want = (torch.zeros_like(c.q), torch.zeros_like(out[1]))
+        step(want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_two_streams_at_once():
+    a, b = Case([2500], 4, 4, 4, 64, BF, seed=11), Case([90, 4000], 2, 8, 2, 128, F32, seed=12)
+    torch.cuda.synchronize()
+    sides = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [hdf.block_attention_kv4(c.q, c.kv4, 0, stream=s, **c.kw)
+           for _ in range(5) for c, s in zip((a, b), sides)][-2:]
+    for s in sides:
+        s.synchronize()
+    a.check(*got[0])
+    b.check(*got[1])

@@ -135,3 +135,30 @@ def test_binding_refuses_tensors_of_other_shapes_and_types():
     wide = torch.zeros(2, 4, 512)[..., :128].view(2, 4, 2, 64)
     assert hdf._block_stride(wide, (2, 4, 2, 64), "q") == 512
     assert hdf._block_stride(wide[:1, :1], (1, 1, 2, 64), "q") == 128
+
+
+def test_draft_block_validation():
+    from tests.test_abi import _fake_drafter
+    L = hdf.lib()
+    w, keep = _fake_drafter()
+
+    def call(n_seq=2, B=16, max_ctx=100, counts=None, n_new=8, offs=None, table=F, max_pages=4, kv4=F,
+             cap=640, ws=F, ws_bytes=1 << 40, hidden=F):
+        return _st(L.hdf_draft_block_kv4(ctypes.byref(w), n_seq, B, F, max_ctx, F, F, counts, n_new, offs,
+                                         table, max_pages, kv4, cap, F, hidden, ws, ws_bytes, None))
+    for bad in (dict(offs=F), dict(table=None), dict(table=None, offs=F, counts=F), dict(max_pages=1),
+                dict(max_pages=-1), dict(kv4=None), dict(cap=100), dict(cap=-64), dict(B=65), dict(B=0),
+                dict(n_seq=-1), dict(max_ctx=-1), dict(n_new=-1), dict(kv4=BAD), dict(hidden=None),
+                dict(ws=ctypes.c_void_p(4112))):
+        assert call(**bad) == "HDF_E_INVALID", bad
+    assert call(n_seq=70000) == "HDF_E_UNSUPPORTED"
+    assert call(ws=None, ws_bytes=0) == "HDF_E_WORKSPACE"
+    assert call(ws_bytes=1000) == "HDF_E_WORKSPACE"
+    assert call(n_seq=0) == "HDF_OK"
+    size = L.hdf_draft_block_kv4_workspace
+    last = 0
+    for n_new in list(range(0, 400, 13)) + [2048, 2049, 16384, 16385, 20000]:
+        need = size(ctypes.byref(w), 8, 16, n_new, 5000)
+        assert need >= last
+        last = need
+    assert size(ctypes.byref(w), 70000, 16, 0, 10) == 0 and size(None, 1, 1, 0, 10) == 0
