@@ -186,88 +186,39 @@ struct Lift {
   __device__ __forceinline__ float value() const { return float(141 - top); }
 };
 
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
-
-// A query tile as the operand of the products with keys.
-// bf16 queries, heads of 128 dims: the scaled fp4 x fp8 product takes the keys as they lie in the
-// cache.  A bf16 has 8 significant bits, an e4m3 number 4: q = 2^e (hi + lo / 16), exact for the
-// elements from 2^-14 of the query's greatest on; smaller ones are off by 2^-23 of it at most.
-// Lane (g, ql): dims 16g .. and 64 + 16g .. of query ql.
+// A query tile as the operand of the products with keys: lane (g, ql) holds dims (HD/4)g + 8j .. of
+// query ql, fp32 in three bf16 terms.  (The fp4 x fp8 products would take the keys as they lie and a
+// bf16 query as two e4m3 terms, exactly, but drop what is 2^-11 of an instruction's greatest product
+// or less, so that scores come out 2^-17 of sum |q k| off, and the log-sum-exps 1e-3.)
 template <typename T, int HD>
 struct Query {
-  static constexpr bool SCALED = sizeof(T) == 2 && HD == 128;
   static constexpr int QT = sizeof(T) == 4 ? 3 : 1;   // bf16 terms of an element
-  static constexpr int NJ = HD / 32;
-  // Not scaled: lane (g, ql) holds dims (HD/4)g + 8j .. of query ql.
-  bf16x8_t f[SCALED ? 1 : NJ][QT];
-  i32x8_t hi, lo;
-  int e_hi, e_lo;
+  bf16x8_t f[HD / 32][QT];
   __device__ __forceinline__ void load(const T* p, int g) {   // p NULL: zeros
-    if constexpr (SCALED) {
-      u32x4 w[4] = {};
-      if (p != nullptr) {
-        w[0] = ld16(p + 16 * g);
-        w[1] = ld16(p + 16 * g + 8);
-        w[2] = ld16(p + 64 + 16 * g);
-        w[3] = ld16(p + 64 + 16 * g + 8);
-      }
-      uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t b = w[i / 4][i % 4];
-        m = max(m, max(b & 0x7FFFu, (b >> 16) & 0x7FFFu));
-      }
-      m = max(m, uint32_t(__shfl_xor(m, 16, kWave)));
-      m = max(m, uint32_t(__shfl_xor(m, 32, kWave)));
-      // The greatest comes to lie in [128, 256).
-      const int e = max(int(m >> 7), 12) - 7;
-      const float unit = __uint_as_float(uint32_t(254 - e) << 23);
-      e_hi = m >= 0x7F80u ? 255 : e;
-      e_lo = m >= 0x7F80u ? 255 : e - 4;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t b0 = w[i / 2][2 * (i % 2)], b1 = w[i / 2][2 * (i % 2) + 1];
-        const float y[4] = {lo_bf(b0) * unit, hi_bf(b0) * unit, lo_bf(b1) * unit, hi_bf(b1) * unit};
-        int h = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-        h = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], h, true);
-        hi[i] = h;
-        const float r0 = (y[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0)) * 16.f;
-        const float r1 = (y[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1)) * 16.f;
-        const float r2 = (y[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2)) * 16.f;
-        const float r3 = (y[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3)) * 16.f;
-        h = __builtin_amdgcn_cvt_pk_fp8_f32(r0, r1, 0, false);
-        lo[i] = __builtin_amdgcn_cvt_pk_fp8_f32(r2, r3, h, true);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (p != nullptr) load8(p + (HD / 4) * g + 8 * j, x);
-        split8<QT>(x, f[j]);
-      }
+    for (int j = 0; j < HD / 32; ++j) {
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (p != nullptr) load8(p + (HD / 4) * g + 8 * j, x);
+      split8<QT>(x, f[j]);
     }
   }
 };
 
-// Products of sub-tile ST's sixteen keys with the queries: lane (g, ql) gets keys 4g .. 4g+3.
-template <typename T, int HD, int ST>
-__device__ __forceinline__ f32x4_t score(const Tile<HD>& t, const Query<T, HD>& q) {
-  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  if constexpr (Query<T, HD>::SCALED) {
-    const i32x8_t k = {int(t.k[ST][0]), int(t.k[ST][1]), int(t.k[ST][2]), int(t.k[ST][3]), 0, 0, 0, 0};
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.hi, acc, 4, 0, ST, int(t.ks), 0, q.e_hi);
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.lo, acc, 4, 0, ST, int(t.ks), 0, q.e_lo);
-  } else {
-    const float scale = __uint_as_float(((t.ks >> (8 * ST)) & 255u) << 23);
+// Products of sub-tile st's sixteen keys with the queries: lane (g, ql) gets keys 4g .. 4g+3.
+template <typename T, int HD, int NQ>
+__device__ __forceinline__ void score(const Tile<HD>& t, int st, const Query<T, HD> (&q)[NQ], f32x4_t (&acc)[NQ]) {
+  const float scale = __uint_as_float(((t.ks >> (8 * st)) & 255u) << 23);
 #pragma unroll
-    for (int j = 0; j < HD / 32; ++j) {
-      const bf16x8_t kf = kv4_bf16x8(t.key_word(ST, j), scale);
+  for (int n = 0; n < NQ; ++n) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int n = 0; n < Query<T, HD>::QT; ++n)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.f[j][n], acc, 0, 0, 0);
-    }
+  for (int j = 0; j < HD / 32; ++j) {
+    const bf16x8_t kf = kv4_bf16x8(t.key_word(st, j), scale);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int k = 0; k < Query<T, HD>::QT; ++k)
+        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[n].f[j][k], acc[n], 0, 0, 0);
   }
-  return acc;
 }
 
 // A tile of the cache into the states of NQ query tiles; nval of its 64 keys count.
@@ -277,16 +228,13 @@ __device__ __forceinline__ void tile_step(Tile<HD>& t, const Query<T, HD> (&q)[N
   constexpr bool F32 = sizeof(T) == 4;
   float x[NQ][16];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const f32x4_t s0 = score<T, HD, 0>(t, q[n]), s1 = score<T, HD, 1>(t, q[n]);
-    const f32x4_t s2 = score<T, HD, 2>(t, q[n]), s3 = score<T, HD, 3>(t, q[n]);
+  for (int i = 0; i < 4; ++i) {
+    f32x4_t acc[NQ];
+    score<T, HD, NQ>(t, i, q, acc);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[n][e] = s0[e];
-      x[n][4 + e] = s1[e];
-      x[n][8 + e] = s2[e];
-      x[n][12 + e] = s3[e];
-    }
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[n][4 * i + e] = acc[n][e];
   }
   // x[i] is key 32 * (i/8) + 8g + i%8.  Behind the last key anything may stand, in the values'
   // scales too.

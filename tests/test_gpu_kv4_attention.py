@@ -5,12 +5,10 @@ Bound of an output element, with A = sum p |v| (at least |out|):
   its argument), its probability by a factor 1 + d, the ratio of sums by 2 d; bf16: a probability
   times its value's scale is rounded to fp16, 2^-11 of itself, or 2^-25 in units of 2^-15 of the
   greatest probability (at most 1 of the sum) times twice the greatest scale, so 2^-39 max |v| a key;
-  a query's elements below 2^-14 of the greatest are off by 2^-23 of it, scale 2^-23 max|q| sum |k|
-  a score (within twice that of the fp32 sums for the normal queries here); fp32: a probability in
-  three bf16 terms, 2^-24, a query in three, 2^-24 more of its score; sums over T keys in fp32, each
-  at most T 2^-24; the result is rounded once, 2^-8 of itself (bf16) or 2^-24 (fp32).  What lies
-  below fp32's least normal number, 2^-126, may be 0: a key's probability relative to the greatest
-  and the lower term it is split into, so 2 * 2^-126 max |v| a key.
+  fp32: a probability in three bf16 terms, 2^-24, a query in three, 2^-24 more of its score; sums
+  over T keys in fp32, each at most T 2^-24; the result is rounded once, 2^-8 of itself (bf16) or
+  2^-24 (fp32).  What lies below fp32's least normal number, 2^-126, may be 0: a key's probability
+  relative to the greatest and the lower term it is split into, so 2 * 2^-126 max |v| a key.
 """
 import numpy as np
 import pytest
@@ -77,7 +75,7 @@ class Case:
             kb, vb = (_np(self.kb[s, :b]), _np(self.vb[s, :b])) if self.block else (None, None)
             o, l, mass, reach = ref.attend(_np(self.q[s, :b]), self.k[s], self.v[s], kb, vb,
                                            causal=causal, scale=scale)
-            d = (self.hd + 4) * 2.0 ** -24 * reach * (1 if f32 else 2) + 2.0 ** -22 + (2.0 ** -24 * reach if f32 else 0)
+            d = (self.hd + 4) * 2.0 ** -24 * reach + 2.0 ** -22 + (2.0 ** -24 * reach if f32 else 0)
             N = T + self.B
             tol = mass * (2 * d[..., None] + (2.0 ** -24 if f32 else 2.0 ** -11) + 2 * N * 2.0 ** -24)
             tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
