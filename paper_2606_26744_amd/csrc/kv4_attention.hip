@@ -84,13 +84,15 @@ struct Tile {
   }
 };
 
-// The tile at p (the same for all lanes).  Buffer loads: one 32-bit offset a lane serves them all,
-// where 64-bit addresses of every part cost registers that the loop needs.  The codes are read once
-// a call, past the caches.
+// The tile at p (the same for all lanes), or zeros, without a fetch, where there is none.  Buffer
+// loads: one 32-bit offset a lane serves them all, where 64-bit addresses of every part cost registers
+// that the loop needs; and a tile that is not there takes the same instructions, so that the waits
+// before a tile's use count exactly the loads behind it (behind a branch they wait for those too).
+// The codes are read once a call, past the caches.
 template <int HD>
-__device__ __forceinline__ void load_tile(Tile<HD>& t, const char* p, int lane) {
+__device__ __forceinline__ void load_tile(Tile<HD>& t, const char* p, bool there, int lane) {
   const int g = lane >> 4, ql = lane & 15;
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, kv4_tile_bytes(HD), 0x00027000);
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, there ? kv4_tile_bytes(HD) : 0, 0x00027000);
   constexpr int NT = 2;   // non-temporal
 #pragma unroll
   for (int l = 0; l < HD / 32; ++l)
@@ -197,9 +199,14 @@ struct Query {
   __device__ __forceinline__ void load(const T* p, int g) {   // p NULL: zeros
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (p != nullptr) load8(p + (HD / 4) * g + 8 * j, x);
-      split8<QT>(x, f[j]);
+      if constexpr (sizeof(T) == 2) {
+        f[j][0] = __builtin_bit_cast(bf16x8_t, u32x4{0, 0, 0, 0});
+        if (p != nullptr) f[j][0] = __builtin_bit_cast(bf16x8_t, ld16(p + (HD / 4) * g + 8 * j));
+      } else {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (p != nullptr) load8(p + (HD / 4) * g + 8 * j, x);
+        split8<QT>(x, f[j]);
+      }
     }
   }
 };
@@ -320,8 +327,8 @@ struct BlockRows {
 
 // nbk of them into the state of a query tile; a query sees those up to `last`.
 template <typename T, int HD>
-__device__ __forceinline__ void block_step(const T* qrow, const BlockRows<T, HD>& b, State<HD>& st, int nbk,
-                                           int last, int lane, float c) {
+__device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRows<T, HD>& b, State<HD>& st,
+                                           int nbk, int last, int lane, float c) {
   constexpr bool F32 = sizeof(T) == 4;
   const int g = lane >> 4, ql = lane & 15;
   float x[16];
@@ -332,17 +339,18 @@ __device__ __forceinline__ void block_step(const T* qrow, const BlockRows<T, HD>
       const T* kr = b.k[32 * (t >> 1) + 8 * (ql >> 2) + 4 * (t & 1) + (ql & 3)];   // this lane's key
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) {
-        float u[8], w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        load8(kr + (HD / 4) * g + 8 * j, u);
-        if (qrow != nullptr) load8(qrow + (HD / 4) * g + 8 * j, w);
         if constexpr (F32) {
+          float u[8];
+          load8(kr + (HD / 4) * g + 8 * j, u);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[e], w[e], acc, 0, 0, 0);
+          for (int e = 0; e < 8; ++e) {
+            // The three terms are the query's element.
+            const float w = (bf2f(q.f[j][0][e]) + bf2f(q.f[j][1][e])) + bf2f(q.f[j][2][e]);
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[e], w, acc, 0, 0, 0);
+          }
         } else {
-          bf16x8_t kf[1], qf[1];
-          split8<1>(u, kf);
-          split8<1>(w, qf);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qf[0], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8_t, ld16(kr + (HD / 4) * g + 8 * j)), q.f[j][0], acc, 0, 0, 0);
         }
       }
     }
@@ -422,57 +430,80 @@ kv4_attn_kernel(Kv4AttnArgs a) {
                          (int64_t(hk) * G + (row - slot * G)) * HD
                    : nullptr;
   };
-  auto tile_at = [&](int l) { return head + int64_t(max(__builtin_amdgcn_readlane(page, l), 0)) * kv4_tile_bytes(HD); };
-  Tile<HD> cur;
-  if (wid < nct) load_tile<HD>(cur, tile_at(0), lane);
+  // The block's rows, 16 bytes a thread and item, on their way before anything larger.
+  constexpr int E = 16 / sizeof(T), P = HD / E, NI = 64 * P / kAttnThreads;   // items of 64 rows
+  u32x4 bw[2][NI];
+  if (nbk > 0) {
+    const T* kb = static_cast<const T*>(a.kb) + int64_t(s) * a.B * a.ld_kb + int64_t(hk) * HD;
+    const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int e = n * kAttnThreads + threadIdx.x, r = e / P, i = (e % P) * E;
+      bw[0][n] = bw[1][n] = u32x4{0, 0, 0, 0};
+      if (r < nbk) {
+        bw[0][n] = ld16(kb + r * a.ld_kb + i);
+        bw[1][n] = ld16(vb + r * a.ld_vb + i);
+      }
+    }
+  }
   Query<T, HD> q[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) q[n].load(q_row(n), g);
+  // This wave's tiles, its l-th into t.
+  const int mine = (nct - wid + kAttnWaves - 1) / kAttnWaves;
+  auto fetch = [&](Tile<HD>& t, int l) {
+    const int at = l < mine ? __builtin_amdgcn_readlane(page, l) : -1;
+    load_tile<HD>(t, head + int64_t(max(at, 0)) * kv4_tile_bytes(HD), at >= 0, lane);
+  };
+  Tile<HD> even, odd;
+  fetch(even, 0);
   State<HD> st[NQ];
   Lift lift;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    q[n].load(q_row(n), g);
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) st[n].o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     st[n].m = -INFINITY;
     st[n].l = 0.f;
   }
-  // The block's rows into LDS, 16 bytes a thread, and into the state of the wave that has the fewest
-  // tiles, while the first tiles are on their way.
+  // Through LDS into the state of the wave that has the fewest tiles.
   if (nbk > 0) {
-    constexpr int E = 16 / sizeof(T), P = HD / E;
-    const T* kb = static_cast<const T*>(a.kb) + int64_t(s) * a.B * a.ld_kb + int64_t(hk) * HD;
-    const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
     const int rows = (nbk + 31) & ~31;
-    for (int e = threadIdx.x; e < 2 * rows * P; e += kAttnThreads) {
-      const int v = e >= rows * P, r = (e - v * rows * P) / P, i = (e - v * rows * P - r * P) * E;
-      u32x4 w = {0, 0, 0, 0};
-      if (r < nbk) w = ld16(v ? vb + r * a.ld_vb + i : kb + r * a.ld_kb + i);
-      if (v) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int e = n * kAttnThreads + threadIdx.x, r = e / P, i = (e % P) * E;
+      if (r < rows) {
+        st16(&pool.blk.k[r][i], bw[0][n]);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
           if constexpr (F32)
-            pool.blk.v[i + k][r] = __uint_as_float(w[k]);
+            pool.blk.v[i + k][r] = __uint_as_float(bw[1][n][k]);
           else
-            pool.blk.v[i + k][r] = T(w[k / 2] >> (16 * (k & 1)));
+            pool.blk.v[i + k][r] = T(bw[1][n][k / 2] >> (16 * (k & 1)));
         }
-      } else {
-        st16(&pool.blk.k[r][i], w);
       }
     }
-    __syncthreads();
+    lds_barrier();
     if (wid == nct % kAttnWaves) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
-        block_step<T, HD>(q_row(n), pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
+        block_step<T, HD>(q[n], pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
                           lane, a.scale_log2);
     }
   }
-  for (int i = wid, l = 0; i < nct; i += kAttnWaves, ++l) {
-    Tile<HD> nxt;
-    if (i + kAttnWaves < nct) load_tile<HD>(nxt, tile_at(l + 1), lane);
-    const int nval = __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, k_hi - k_lo - i * kTile);
-    tile_step<T, HD, NQ>(cur, q, st, lift, nval, g, a.scale_log2);
-    cur = nxt;
+  auto step = [&](Tile<HD>& t, int l) {
+    const int left = k_hi - k_lo - (wid + kAttnWaves * l) * kTile;
+    tile_step<T, HD, NQ>(t, q, st, lift, __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, left), g,
+                         a.scale_log2);
+  };
+  for (int l = 0; l < mine; l += 2) {   // the next tile always on its way
+    fetch(odd, l + 1);
+    __builtin_amdgcn_sched_barrier(0);   // loads first, not sunk between the products
+    step(even, l);
+    if (l + 1 >= mine) break;
+    fetch(even, l + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    step(odd, l + 1);
   }
 
   // The waves' states of a query tile side by side, then joined: four dims of a row a thread.
