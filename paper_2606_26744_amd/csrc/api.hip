@@ -574,7 +574,9 @@ size_t hdf_kv4_tile_bytes(int head_dim) {
 
 size_t hdf_kv4_cache_bytes(int n_layers, int n_kv_heads, int head_dim, int64_t kv_cap) {
   if (n_layers < 1 || n_kv_heads < 1 || kv_cap < 0 || kv_cap % 64 != 0 || kv_cap > INT32_MAX) return 0;
-  return size_t(n_layers) * size_t(n_kv_heads) * size_t(kv_cap / 64) * hdf_kv4_tile_bytes(head_dim);
+  const unsigned __int128 bytes = (unsigned __int128)(n_layers) * unsigned(n_kv_heads) * unsigned(kv_cap / 64) *
+                                  hdf_kv4_tile_bytes(head_dim);
+  return bytes <= SIZE_MAX / 2 ? size_t(bytes) : 0;
 }
 
 // A layer's tiles.
@@ -662,7 +664,9 @@ hdf_status hdf_block_attention_kv4(const void* q, int64_t ld_q, const void* k_bl
   if (dtype != HDF_F32 && dtype != HDF_BF16) return fail(HDF_E_INVALID, "%s: bad dtype", fn);
   const hdf_status st = kv4_attn_shape(fn, n_seq, B, n_heads, n_kv_heads, head_dim, max_ctx);
   if (st != HDF_OK) return st;
-  if (!(scale > 0.f) || !isfinite(scale)) return fail(HDF_E_INVALID, "%s: scale must be finite and positive", fn);
+  const float scale_log2 = float(1.4426950408889634 * double(scale));
+  if (!(scale > 0.f) || !isfinite(scale_log2))
+    return fail(HDF_E_INVALID, "%s: scale must be positive, and finite times log2(e)", fn);
   if (n_seq == 0) return ok();
   if (q == nullptr || out == nullptr || ctx_len == nullptr) return fail(HDF_E_INVALID, "%s: null pointer", fn);
   if ((k_blk == nullptr) != (v_blk == nullptr))
@@ -698,7 +702,7 @@ hdf_status hdf_block_attention_kv4(const void* q, int64_t ld_q, const void* k_bl
   a.kb = k_blk; a.vb = v_blk; a.ld_kb = ld_k; a.ld_vb = ld_v;
   a.ctx_len = ctx_len; a.max_ctx = max_ctx; a.block_len = block_len;
   a.n_seq = n_seq; a.B = B; a.nh = n_heads; a.nkv = n_kv_heads; a.causal = causal != 0 ? 1 : 0;
-  a.scale_log2 = float(1.4426950408889634 * double(scale));
+  a.scale_log2 = scale_log2;
   a.out = out; a.ld_out = ld_out; a.lse = lse;
   const hipError_t e = hdf::launch_kv4_attention(dtype == HDF_BF16, head_dim, a, ws,
                                                  reinterpret_cast<hipStream_t>(stream));

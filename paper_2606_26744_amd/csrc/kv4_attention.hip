@@ -141,6 +141,10 @@ __device__ __forceinline__ float groups_max(float x) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+// 2^(x/2), for a factor 2^x in two steps: references differ by their lifts too, up to 205, and a sum
+// may be as large as its lift, so that a factor below fp32's range still leaves a sum within it.
+__device__ __forceinline__ float half_power(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
+
 // Running softmax of one 16-row query tile in a wave: lane (g, ql) keeps query ql.  o and l are
 // relative to 2^m, m the greatest score (base 2) so far less `lift`.
 template <int HD>
@@ -159,12 +163,12 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
   top = groups_max(top);
   const float m = fmaxf(st.m + drop, fmaf(top, c, -lift));
   if (__any(m > st.m)) {
-    const float alpha = m > st.m ? __builtin_amdgcn_exp2f(st.m - m) : 1.f;   // st.m -inf: 0
-    st.l *= alpha;
+    const float h = m > st.m ? half_power(st.m - m) : 1.f;   // st.m -inf: 0
+    st.l = st.l * h * h;
 #pragma unroll
     for (int dt = 0; dt < HD / 16; ++dt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[dt][e] *= alpha;
+      for (int e = 0; e < 4; ++e) st.o[dt][e] = st.o[dt][e] * h * h;
     st.m = m;
   }
   const float base = st.m == -INFINITY ? 0.f : st.m;   // no key yet
@@ -180,9 +184,10 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // The lift of a wave's references.  A value's scale times its probability becomes one fp16 factor
 // of the products with the codes (bf16 queries): 11 bits, a rounding an eighth of the output's own.
 // So that it neither overflows nor loses small ones, probabilities are taken relative to 2^-lift,
-// lift = 15 - log2 of a power of two above the greatest scale so far: the factor is below 2^15, and
-// of full precision down to 2^-29 of the greatest probability times the greatest scale.  fp32:
-// three bf16 terms, no lift.
+// lift = 15 - log2 of a power of two above the greatest scale so far (2^-80 at least): the factor is
+// below 2^15, and of full precision down to 2^-29 of the greatest probability times the greatest
+// scale.  Sums stay within fp32: a probability is lost below 2^-126 - lift, 2^-40 even beside scales
+// of 2^100.  fp32 queries: three bf16 terms, no lift.
 struct Lift {
   int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
   __device__ __forceinline__ float value() const { return float(141 - top); }
@@ -533,11 +538,11 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       float l = 0.f;
 #pragma unroll
       for (int w = 0; w < kAttnWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(red_m[w][qq] - base);
+        const float f = half_power(red_m[w][qq] - base);
         const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&pool.o[w][qq][dim]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
-        l = fmaf(f, red_l[w][qq], l);
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i] * f, o[i]);
+        l = fmaf(f, red_l[w][qq] * f, l);
       }
       if (direct) {
         const int64_t orow = int64_t(s) * a.B + k;
@@ -558,7 +563,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int Q = HD / 4, S = kJoinThreads / Q;
-  __shared__ float4 so[S][Q];
+  __shared__ f32x4_t so[S][Q];
   __shared__ float sm[S], sl[S];
   const int G = a.G, R = G * a.B;
   const int qr = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
@@ -568,19 +573,17 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   const int d = threadIdx.x % Q, sl_ = threadIdx.x / Q;
   const int64_t base = (int64_t(s) * a.nkv + hk) * a.n_chunks;
   float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
   for (int c = sl_; c < nc; c += S) {
     const int64_t p = (base + c) * R + qr;
     const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * p);
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + p * HD + 4 * d);
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part_o + p * HD + 4 * d);
     const float mn = fmaxf(m, ml.x);
     const float b = mn == -INFINITY ? 0.f : mn;
-    const float f0 = __builtin_amdgcn_exp2f(m - b), f1 = __builtin_amdgcn_exp2f(ml.x - b);
-    l = l * f0 + ml.y * f1;
-    o.x = o.x * f0 + v.x * f1;
-    o.y = o.y * f0 + v.y * f1;
-    o.z = o.z * f0 + v.z * f1;
-    o.w = o.w * f0 + v.w * f1;
+    const float f0 = half_power(m - b), f1 = half_power(ml.x - b);
+    l = fmaf(l * f0, f0, ml.y * f1 * f1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i] * f0, f0, v[i] * f1 * f1);
     m = mn;
   }
   so[sl_][d] = o;
@@ -595,20 +598,18 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   for (int w = 1; w < S; ++w) mm = fmaxf(mm, sm[w]);
   const float b = mm == -INFINITY ? 0.f : mm;
   float sum = 0.f;
-  o = make_float4(0.f, 0.f, 0.f, 0.f);
+  o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int w = 0; w < S; ++w) {
-    const float f = __builtin_amdgcn_exp2f(sm[w] - b);
-    sum += f * sl[w];
-    o.x += f * so[w][d].x;
-    o.y += f * so[w][d].y;
-    o.z += f * so[w][d].z;
-    o.w += f * so[w][d].w;
+    const float f = half_power(sm[w] - b);
+    sum = fmaf(f, sl[w] * f, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, so[w][d][i] * f, o[i]);
   }
   const int64_t orow = int64_t(s) * a.B + k;
   const int h = hk * G + (qr - k * G);
   store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + 4 * d,
-               f32x4_t{o.x, o.y, o.z, o.w}, sum);
+               o, sum);
   if (d == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(sum)) * 0.6931471805599453f;
 }
 

@@ -81,6 +81,7 @@ class Case:
             tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
             top = max([np.abs(x).max() for x in (self.v[s], vb) if x is not None and x.size] or [0.0])
             tol += N * (2 * 2.0 ** -126 + (0 if f32 else 2.0 ** -39)) * top
+            tol += N * 6 * 2.0 ** -120
             err = np.abs(_np(out[s, :b]) - o)
             assert (err <= tol).all(), (s, T, float((err - tol).max()), np.argwhere(err > tol)[:3])
             if lse is not None:
@@ -144,6 +145,36 @@ def test_sharp_scores_and_a_scale():
     c = Case([300, 64], 4, 4, 4, 128, BF, spread=4.0, seed=6)
     out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, scale=0.7, **c.kw)
     c.check(out, lse, scale=0.7)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sizes", [(1e30, 1e-30), (1e-27, 1e-30), (2e33, 3e33), (1e-20, 1e20)])
+def test_values_of_any_size(dtype, sizes):
+    """Values far from 1, and of different sizes in one context: the factor that carries a value's
+    scale follows the greatest so far, in either order."""
+    c = Case([130, 200], 3, 2, 2, 64, dtype, seed=13, block=False)
+    for s, T in enumerate(c.ctx):
+        g = torch.Generator().manual_seed(s)
+        size = torch.where(torch.rand(T, 1, 1, generator=g) < 0.5, sizes[s], sizes[1 - s])
+        v = (torch.randn(T, 2, 64, generator=g) * size).to(dtype)
+        pages = c.kw["page_table"][s].tolist()
+        hdf.kv4_write_rows(c.kv4, 0, None, v.view(T, -1).cuda(), rows=hdf.paged_rows(pages, T, "cuda"))
+        c.v[s] = ref.quantise_values(_np(v))
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    c.check(out, lse)
+
+
+def test_a_cache_beyond_32_bits():
+    """Pages at the end of a cache of more than 4 GiB."""
+    c = Case([300], 4, 8, 8, 128, BF, seed=14)
+    tiles = 66000
+    kv4 = torch.zeros((1, 8, tiles, 8576), dtype=torch.uint8, device="cuda")
+    assert kv4.numel() > 1 << 32
+    n = c.kv4.shape[2]
+    kv4[:, :, tiles - n:] = c.kv4
+    c.kw["page_table"] = c.kw["page_table"] + (tiles - n)
+    out, lse = hdf.block_attention_kv4(c.q, kv4, 0, **c.kw)
+    c.check(out, lse)
 
 
 def test_pages_outside_the_pool_hold_no_keys():

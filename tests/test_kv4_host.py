@@ -20,7 +20,7 @@ def test_sizes():
     assert L.hdf_kv4_tile_bytes(96) == 0
     assert L.hdf_kv4_cache_bytes(2, 8, 128, 640) == 2 * 8 * 10 * 8576
     for bad in ((0, 8, 128, 64), (1, 0, 128, 64), (1, 1, 80, 64), (1, 1, 64, 100), (1, 1, 64, -64),
-                (1, 1, 64, 1 << 31)):
+                (1, 1, 64, 1 << 31), (1 << 30, 1 << 30, 64, 1 << 20)):
         assert L.hdf_kv4_cache_bytes(*bad) == 0, bad
     assert hdf.kv4_alloc(2, 3, 64, 128, device="cpu").shape == (2, 3, 2, 4352)
     for bad in ((1, 1, 96, 64), (1, 1, 64, 65)):
@@ -62,7 +62,7 @@ def _attend(n_seq=2, B=4, H=8, nkv=2, hd=64, dt=1, cache="paged", max_ctx=100, s
 
 @pytest.mark.parametrize("bad", [
     dict(dt=2), dict(n_seq=-1), dict(max_ctx=-1), dict(B=0), dict(B=65), dict(H=0), dict(nkv=0),
-    dict(nkv=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+    dict(nkv=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
     dict(q=None), dict(out=None), dict(ctx=None), dict(k=None), dict(v=None), dict(q=BAD), dict(k=BAD),
     dict(out=BAD), dict(ldq=511), dict(ldq=516), dict(ldo=504), dict(ldk=64), dict(ldv=132),
     dict(ldq=1 << 62), dict(cache="none"), dict(cache="both"), dict(cache="neither"), dict(kv4=None),
