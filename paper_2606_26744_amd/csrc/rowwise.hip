@@ -119,10 +119,14 @@ prep_kernel(PrepArgs a) {
     const bool valid = r < a.new_offsets[a.n_seq] && j < ns && pos >= 0 &&
                        (a.page_table == nullptr || (pos >> 6) < a.max_pages);
     a.plan_pos[r] = valid ? pos : -1;
-    a.plan_row[r] = !valid ? -1
-                    : a.page_table != nullptr
-                        ? a.page_table[int64_t(lo) * a.max_pages + (pos >> 6)] * 64 + (pos & 63)
-                        : a.kv_offsets[lo] + pos;
+    int row = -1;
+    if (valid && a.page_table != nullptr) {
+      const int page = a.page_table[int64_t(lo) * a.max_pages + (pos >> 6)];
+      if (page >= 0 && page < 1 << 25) row = page * 64 + (pos & 63);   // no pool holds more
+    } else if (valid) {
+      row = a.kv_offsets[lo] + pos;
+    }
+    a.plan_row[r] = row;
   }
   float* hrow = ctx ? nullptr : a.h + r * a.d;
   const float* gamma = ctx ? a.ctx_gamma : a.attn_gamma;

@@ -132,6 +132,53 @@ def test_block_over_a_4bit_cache(dtype, hd, B, ctx, new, paged):
     assert torch.equal(h.draft_block(ws=ws, **args), hidden)
 
 
+def test_a_prompt_longer_than_one_projection():
+    """More new rows than one launch projects (16384): the keys and values of the last ones."""
+    wl = dataclasses.replace(_workload("bf16", 64, 2), n_seq=1, ctx_lens=[16500])
+    dr, T = wl.drafter, 16500
+    w = synth.drafter_weights(wl, device="cuda", random_norms=True)
+    h = _handle(wl, w, T + 2)
+    kv4, _ = h.alloc_kv(64 * 260, kv_bits=4)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    y = synth.reduced_states(wl, T, device="cuda")
+    tokens = synth.block_tokens(wl, device="cuda")
+    args = dict(ctx_len=torch.tensor([T], **i32), max_ctx=T, new_offsets=torch.tensor([0, T], **i32),
+                kv_offsets=torch.tensor([0, 64 * 260], **i32), kv_k=kv4, kv_vt=None, tokens=tokens)
+    hidden = h.draft_block(y_new=y, **args)
+    assert torch.isfinite(hidden.float()).all()
+    W = _weights(wl, w)
+    at = np.r_[0:40, 16370:16400, 16480:16500]
+    fresh = context_kv(W, as_f64(bits(y[torch.from_numpy(at).cuda()])), at)
+    rows = torch.from_numpy(at.astype(np.int32)).cuda()
+    for l in range(dr.n_layers):
+        k, v = _read(kv4, l, rows)
+        _check_appended(k, fresh[l][0], 32, 3.5, "keys")
+        _check_appended(v, fresh[l][1], dr.head_dim, 6.0, "values")
+
+
+def test_pages_outside_the_pool_are_not_written():
+    """Page numbers whose rows lie beyond 32 bits too: nothing is written, nothing attended to."""
+    wl = dataclasses.replace(_workload("bf16", 64, 4), n_seq=2, ctx_lens=[70, 5])
+    w = synth.drafter_weights(wl, device="cuda")
+    h = _handle(wl, w, 80)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    y = synth.reduced_states(wl, 75, device="cuda")
+    tokens = synth.block_tokens(wl, device="cuda")
+    W = _weights(wl, w)
+    for page in (1 << 26, (1 << 31) - 1, 3, -1, -(1 << 26)):
+        kv4, _ = h.alloc_kv(3 * 64, kv_bits=4)
+        table = torch.tensor([[2, page], [1, -1]], **i32)
+        hidden = h.draft_block(ctx_len=torch.tensor([70, 5], **i32), max_ctx=70, y_new=y,
+                               new_offsets=torch.tensor([0, 70, 75], **i32), page_table=table,
+                               kv_k=kv4, kv_vt=None, tokens=tokens)
+        assert not kv4[:, :, 0].any(), page
+        for s, rows in ((0, range(128, 192)), (1, range(64, 69))):
+            kv = [_read(kv4, l, torch.tensor(list(rows), **i32)) for l in range(h.L)]
+            n = len(rows)
+            want = block_forward(W, kv, bits(tokens)[s], pos_shift=(70, 5)[s] - n)
+            _check_hidden(wl, bits(hidden[4 * s:4 * s + 4]), want, f"page {page}, sequence {s}")
+
+
 def _targets(drafts):
     """Copies the first draft, then differs."""
     n, K = drafts.shape
