@@ -11,6 +11,9 @@
  *      (hdf_sample_tokens, hdf_accept_sample: the same at temperature T > 0;
  *       hdf_sample_truncated, hdf_accept_truncated: with top-k, top-p and min-p as well;
  *       hdf_advance_context: the committed positions become the next round's context)
+ *   The cache that holds the context's keys and values may be in `dtype` (hdf_draft_block) or in 4
+ *   bits (hdf_draft_block_kv4); hdf_kv4_write_rows, hdf_kv4_read_rows and hdf_block_attention_kv4
+ *   work on the 4-bit cache alone, with heads of keys shared by several query heads too.
  *
  * For training: hdf_kl_forward, and hdf_distill_forward / hdf_distill_backward against a teacher's
  * stored top logits (hdf_top_logits).
@@ -266,9 +269,10 @@ size_t hdf_kv4_cache_bytes(int n_layers, int n_kv_heads, int head_dim, int64_t k
  * touches nothing else of the cache, a read nothing else of the outputs.  Writes to a row outside
  * [0, kv_cap) (from `rows`) are skipped, reads of one return zeros.  A read rounds code * scale
  * once to `dtype` (keys are exact in either type).
- * A row may be named once in a write: of a row named twice the codes and scales of either may
- * remain.  Writes to different rows may run at the same time on different streams only where the
- * rows lie in different groups of 8 (8j .. 8j+7), whose values share words.
+ * A row may be named once in a write: a row named twice is left with any codes and the scales of
+ * either (other rows are not touched by that).  Writes to different rows may run at the same time
+ * on different streams only where the rows lie in different groups of 8 (8j .. 8j+7), whose values
+ * share words.
  * Limits: head_dim in {64, 128}; kv_cap a positive multiple of 64 below 2^31; n_rows, row0 as
  *         there; ld_k, ld_v >= n_kv_heads*head_dim and multiples of 16 bytes; layer >= 0 (not
  *         checked against the cache); tensors 16-byte aligned. */
@@ -299,9 +303,10 @@ typedef struct {
  *                           t < block_len[s], with `causal` its slots t <= k only
  *   out = sum_t softmax(x)_t V_t,   lse = log sum_t exp(x_t)
  * with fp32 accumulation.  bf16: a context probability times its value's scale is rounded to 11 bits
- * (an eighth of the output's own rounding); fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of -inf.  B = 1 is the
- * decoding of single tokens; without the block's keys, write a position to the cache before the
- * query that should see it.
+ * (an eighth of the output's own rounding), or to a multiple of 2^-118 where every scale is below
+ * 2^-80; fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of -inf.
+ * B = 1 is the decoding of single tokens; without the block's keys, write a position to the cache
+ * before the query that should see it.
  * q, k_blk, v_blk, out  row s*B + k, ld_* elements apart: [n_heads or n_kv_heads][head_dim]
  *             contiguous, dtype; k_blk and v_blk may be NULL together (no keys of the block)
  * ctx_len     [n_seq] int32, 0 .. max_ctx (larger ones count as max_ctx)
@@ -312,9 +317,9 @@ typedef struct {
  * lse         [n_seq*B][n_heads] fp32 or NULL
  * ws          hdf_block_attention_kv4_workspace(...) bytes (may be 0, then NULL), 256-byte aligned;
  *             contents on entry do not matter.  The size serves smaller max_ctx too.
- * Limits: head_dim in {64, 128}; 1 <= B <= 64; max_ctx <= 2^30; n_kv_heads divides n_heads; n_seq, n_kv_heads and
- *         n_seq * ceil(n_heads / n_kv_heads * B / 16) below 65536; scale finite and positive; ld_*
- *         multiples of 16 bytes; tensors 16-byte aligned. */
+ * Limits: head_dim in {64, 128}; 1 <= B <= 64; max_ctx <= 2^30; n_kv_heads divides n_heads; n_seq,
+ *         n_kv_heads and n_seq * ceil(n_heads / n_kv_heads * B / 16) below 65536; scale finite and
+ *         positive; ld_* multiples of 16 bytes; tensors 16-byte aligned. */
 size_t hdf_block_attention_kv4_workspace(int n_seq, int B, int n_heads, int n_kv_heads,
                                          int head_dim, int max_ctx);
 hdf_status hdf_block_attention_kv4(const void* q, int64_t ld_q, const void* k_blk, int64_t ld_k,

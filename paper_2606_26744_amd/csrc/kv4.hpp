@@ -66,7 +66,7 @@ __device__ __forceinline__ bf16x8_t kv4_bf16x8(uint32_t w, float scale) {
   const uint32_t d = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
   return __builtin_bit_cast(bf16x8_t, u32x4{a, b, c, d});
 }
-// ... as fp16 without a scale, exact (half the issue cycles of the bf16 conversion).
+// ... as fp16 without a scale, exact.
 __device__ __forceinline__ f16x8_t kv4_f16x8(uint32_t w) {
   const f16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0);
   const f16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1);

@@ -900,7 +900,10 @@ class DrafterHandle:
         self.d, self.nh, self.hd, self.F, self.V = d, n_heads, head_dim, d_ff, vocab
         self.eps = eps
 
-    def kv_cache_bytes(self, kv_cap: int) -> int:
+    def kv_cache_bytes(self, kv_cap: int, kv_bits: Optional[int] = None) -> int:
+        """Bytes of the cache's keys, and of its values; kv_bits 4: of the whole 4-bit cache."""
+        if _is_kv4(kv_bits):
+            return int(lib().hdf_kv4_cache_bytes(self.L, self.nh, self.hd, kv_cap))
         return int(lib().hdf_kv_cache_bytes(ctypes.byref(self.s), kv_cap))
 
     def workspace_bytes(self, n_seq: int, B: int, n_new: int, max_ctx: int,

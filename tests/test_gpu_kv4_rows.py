@@ -176,3 +176,21 @@ def test_tiles_beyond_32_bits():
     for x, w in zip(hdf.kv4_read_rows(kv4, 0, 70, row0=cap - 70), _expect(k, v, nh, hd, BF)):
         _same(x, w)
     assert not kv4[:, :, :cap // 64 - 2].any()
+
+
+def test_a_row_named_twice_disturbs_no_other():
+    """What that row then holds is open; its neighbours, whose values share its words, keep theirs."""
+    nh, hd, cap = 2, 128, 64
+    kv4 = hdf.kv4_alloc(1, nh, hd, cap)
+    k0, v0 = _rows(cap, nh * hd, BF, 13), _rows(cap, nh * hd, BF, 14)
+    hdf.kv4_write_rows(kv4, 0, k0, v0)
+    before = hdf.kv4_read_rows(kv4, 0, cap)
+    rows = [3, 3] + list(range(20, 28)) + [3, 40, 3]       # in one wave's eight rows, and in another's
+    k, v = _rows(len(rows), nh * hd, BF, 15), _rows(len(rows), nh * hd, BF, 16)
+    hdf.kv4_write_rows(kv4, 0, k, v, rows=torch.tensor(rows, dtype=torch.int32, device="cuda"))
+    once = [i for i, r in enumerate(rows) if r != 3]
+    want = _expect(k[once], v[once], nh, hd, BF)
+    for got, old, w in zip(hdf.kv4_read_rows(kv4, 0, cap), before, want):
+        _same(got[[rows[i] for i in once]], w)
+        rest = [r for r in range(cap) if r not in rows]
+        assert torch.equal(got[rest], old[rest])
