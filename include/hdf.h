@@ -303,7 +303,7 @@ typedef struct {
  *                           t < block_len[s], with `causal` its slots t <= k only
  *   out = sum_t softmax(x)_t V_t,   lse = log sum_t exp(x_t)
  * with fp32 accumulation.  bf16: a context probability times its value's scale is rounded to 11 bits
- * (an eighth of the output's own rounding), or to a multiple of 2^-118 where every scale is below
+ * (an eighth of the output's own rounding), or to a multiple of 2^-114 where every scale is below
  * 2^-80; fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of -inf.
  * B = 1 is the decoding of single tokens; without the block's keys, write a position to the cache
  * before the query that should see it.

@@ -146,7 +146,10 @@ __device__ __forceinline__ float groups_max(float x) {
 __device__ __forceinline__ float half_power(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
 
 // Running softmax of one 16-row query tile in a wave: lane (g, ql) keeps query ql.  o and l are
-// relative to 2^m, m the greatest score (base 2) so far less `lift`.
+// relative to 2^m, m a score (base 2) less `lift`: the greatest so far, or one that the greatest is
+// at most kSlack above.  Moving the reference costs a product an element of o, and with 16 queries a
+// tile some query's greatest rises in most tiles, by little.
+constexpr int kSlack = 4;
 template <int HD>
 struct State {
   f32x4_t o[HD / 16];    // O^T: dim 16dt + 4g + e of query ql
@@ -161,8 +164,9 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
   top = groups_max(top);
-  const float m = fmaxf(st.m + drop, fmaf(top, c, -lift));
-  if (__any(m > st.m)) {
+  const float seen = fmaf(top, c, -lift);
+  if (__any(drop > 0.f || seen > st.m + float(kSlack))) {
+    const float m = fmaxf(st.m + drop, seen);
     const float h = m > st.m ? half_power(st.m - m) : 1.f;   // st.m -inf: 0
     st.l = st.l * h * h;
 #pragma unroll
@@ -184,13 +188,13 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // The lift of a wave's references.  A value's scale times its probability becomes one fp16 factor
 // of the products with the codes (bf16 queries): 11 bits, a rounding an eighth of the output's own.
 // So that it neither overflows nor loses small ones, probabilities are taken relative to 2^-lift,
-// lift = 15 - log2 of a power of two above the greatest scale so far (2^-80 at least): the factor is
-// below 2^15, and of full precision down to 2^-29 of the greatest probability times the greatest
-// scale.  Sums stay within fp32: a probability is lost below 2^-126 - lift, 2^-40 even beside scales
-// of 2^100.  fp32 queries: three bf16 terms, no lift.
+// lift = 15 - kSlack - log2 of a power of two above the greatest scale so far (2^-80 at least): the
+// factor is below 2^15, and of full precision down to 2^-25 of the greatest probability times the
+// greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-37 even
+// beside scales of 2^100.  fp32 queries: three bf16 terms, no lift.
 struct Lift {
   int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
-  __device__ __forceinline__ float value() const { return float(141 - top); }
+  __device__ __forceinline__ float value() const { return float(141 - kSlack - top); }
 };
 
 // A query tile as the operand of the products with keys: lane (g, ql) holds dims (HD/4)g + 8j .. of
@@ -419,7 +423,8 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     if (page >= a.n_tiles) page = -1;
   }
   const int n_ctx = context_of(a, s);
-  if (chunk >= chunks_of(a, n_ctx)) return;
+  const int nc = chunks_of(a, n_ctx);
+  if (chunk >= nc) return;
   const int blen = block_of(a, s);
   if (row0 >= G * blen) return;   // rows of no slot
   const int k_lo = min(n_ctx, t0 << 6), k_hi = min(n_ctx, k_lo + a.chunk_len);
@@ -512,7 +517,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   }
 
   // The waves' states of a query tile side by side, then joined: four dims of a row a thread.
-  const bool direct = a.n_chunks == 1;
+  const bool direct = nc == 1;   // nothing to join
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     float l_sum = st[n].l;
@@ -558,19 +563,21 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   }
 }
 
-// The chunks' partial outputs of a query row joined: a workgroup a row, its threads (slice of the
-// chunks, four dims).
-template <typename T, int HD>
+// The chunks' partial outputs of a query row joined, where the sequence has more than one: threads
+// (row, slice of the row's chunks, four dims), S slices a row and as many rows a workgroup as fit.
+template <typename T, int HD, int S>
 __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
-  constexpr int Q = HD / 4, S = kJoinThreads / Q;
-  __shared__ f32x4_t so[S][Q];
-  __shared__ float sm[S], sl[S];
+  constexpr int Q = HD / 4, N = kJoinThreads / (Q * S);
+  __shared__ f32x4_t so[N * S][Q];
+  __shared__ float sm[N * S], sl[N * S];
   const int G = a.G, R = G * a.B;
-  const int qr = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
-  const int k = slot_of(a, qr);
-  if (k >= block_of(a, s)) return;
+  const int hk = blockIdx.y, s = blockIdx.z;
   const int nc = chunks_of(a, context_of(a, s));
-  const int d = threadIdx.x % Q, sl_ = threadIdx.x / Q;
+  if (nc == 1) return;
+  const int d = threadIdx.x % Q, at = threadIdx.x / Q, sl_ = at % S;
+  const int qr = min(int(blockIdx.x) * N + at / S, R - 1);   // rows behind the last: the last's again
+  const int k = slot_of(a, qr);
+  if (N == 1 && k >= block_of(a, s)) return;
   const int64_t base = (int64_t(s) * a.nkv + hk) * a.n_chunks;
   float m = -INFINITY, l = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
@@ -586,25 +593,25 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
     for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i] * f0, f0, v[i] * f1 * f1);
     m = mn;
   }
-  so[sl_][d] = o;
+  so[at][d] = o;
   if (d == 0) {
-    sm[sl_] = m;
-    sl[sl_] = l;
+    sm[at] = m;
+    sl[at] = l;
   }
   __syncthreads();
-  if (sl_ != 0) return;
-  float mm = sm[0];
+  if (sl_ != 0 || k >= block_of(a, s)) return;
+  float mm = sm[at];
 #pragma unroll
-  for (int w = 1; w < S; ++w) mm = fmaxf(mm, sm[w]);
+  for (int w = 1; w < S; ++w) mm = fmaxf(mm, sm[at + w]);
   const float b = mm == -INFINITY ? 0.f : mm;
   float sum = 0.f;
   o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int w = 0; w < S; ++w) {
-    const float f = half_power(sm[w] - b);
-    sum = fmaf(f, sl[w] * f, sum);
+    const float f = half_power(sm[at + w] - b);
+    sum = fmaf(f, sl[at + w] * f, sum);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, so[w][d][i] * f, o[i]);
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, so[at + w][d][i] * f, o[i]);
   }
   const int64_t orow = int64_t(s) * a.B + k;
   const int h = hk * G + (qr - k * G);
@@ -627,7 +634,15 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
     hipLaunchKernelGGL((kv4_attn_kernel<T, HD, MQ>), grid, dim3(kAttnThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
-  hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3(R, a.nkv, a.n_seq), dim3(kJoinThreads), 0, s, a);
+  // Two slices for up to eight chunks (four rows a workgroup at 128 dims), else a workgroup a row: the
+  // call takes 32.1 us in the place of 33.3 for 2 contexts of 8192 positions, 32 heads over 8, B = 64
+  // (2048 rows of two chunks), 22.7 in the place of 23.0 for 4 contexts, B = 16.
+  constexpr int Q = HD / 4, most = kJoinThreads / Q, few = 2;
+  const dim3 rows((R + most / few - 1) / (most / few), a.nkv, a.n_seq);
+  if (a.n_chunks <= 8)
+    hipLaunchKernelGGL((kv4_join_kernel<T, HD, few>), rows, dim3(kJoinThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((kv4_join_kernel<T, HD, most>), dim3(R, a.nkv, a.n_seq), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -3,8 +3,9 @@
 Bound of an output element, with A = sum p |v| (at least |out|):
   a score is off by d <= (hd + 4) 2^-24 scale sum |q k| + 2^-22 (fp32 sums; the exponential and
   its argument), its probability by a factor 1 + d, the ratio of sums by 2 d; bf16: a probability
-  times its value's scale is rounded to fp16, 2^-11 of itself, or 2^-25 in units of 2^-15 of the
-  greatest probability (at most 1 of the sum) times twice the greatest scale, so 2^-39 max |v| a key;
+  times its value's scale is rounded to fp16, 2^-11 of itself, or 2^-25 in units of 2^-11 of the
+  greatest probability (at most 1 of the sum) times twice the greatest scale, so 2^-35 max |v| a key
+  (the reference of the probabilities is at most 2^4 below the greatest, and their factor's top 2^15);
   fp32: a probability in three bf16 terms, 2^-24, a query in three, 2^-24 more of its score; sums
   over T keys in fp32, each at most T 2^-24; the result is rounded once, 2^-8 of itself (bf16) or
   2^-24 (fp32).  What lies below fp32's least normal number, 2^-126, may be 0: a key's probability
@@ -80,7 +81,7 @@ class Case:
             tol = mass * (2 * d[..., None] + (2.0 ** -24 if f32 else 2.0 ** -11) + 2 * N * 2.0 ** -24)
             tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
             top = max([np.abs(x).max() for x in (self.v[s], vb) if x is not None and x.size] or [0.0])
-            tol += N * (2 * 2.0 ** -126 + (0 if f32 else 2.0 ** -39)) * top
+            tol += N * (2 * 2.0 ** -126 + (0 if f32 else 2.0 ** -35)) * top
             tol += N * 6 * 2.0 ** -120
             err = np.abs(_np(out[s, :b]) - o)
             assert (err <= tol).all(), (s, T, float((err - tol).max()), np.argwhere(err > tol)[:3])
