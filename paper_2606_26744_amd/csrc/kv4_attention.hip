@@ -648,15 +648,25 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
 
 }  // namespace
 
-// Chunks of at most one round of workgroups over the card, of 2048 positions at least (four tiles a
-// wave; a chunk's lengths, queries and join take about 5 us beside its tiles, the second launch 4).
-// Measured, us a call by chunk length, 1024 to 16384: one query over 131072 positions of 8 heads 42,
-// 34, 30, 36, 52 (256 workgroups at 4096); 8 x 2048 positions of 32 heads 28, 18 (256 at 2048);
-// 64 contexts of up to 16384 609, 509, 443, 412, 368 (2048 workgroups at 16384).
-constexpr int kMinChunk = 2048;
+// Chunks: as many as leave one round of workgroups over the card, of 512 positions at least (a tile a
+// wave), and none for contexts of up to 1536.  us a call by chunk length, whole context last:
+//   1 query, 32 heads over 8        512    1024   2048   whole
+//     1024 positions                9.1                  8.4
+//     1500                          9.4    10.5          9.7
+//     4096                          9.5    10.5   13.2   16.8
+//     16384 (256 workgroups: 512)  11.3    11.8   13.6   49.7
+//   16 queries, 32 heads, 1 context
+//     1024                          9.9                  9.1
+//     4096 (256: 512)              12.2    12.1   14.1   17.3
+//     16384 (256: 2048)            32.8    23.5   17.5   50.4
+// More than a round pays nowhere: 64 contexts of up to 16384 take 607, 493, 423, 389, 361 us in chunks
+// of 1024, 2048, 4096, 8192, 16384 (2048 workgroups), 16 of 512 to 8192 in 256 workgroups 39, in twice
+// and four times as many 45 and 48.
+constexpr int kMinChunk = 512, kWholeCtx = 1536;
 
 static int64_t chunks_wanted(int n_seq, int nkv, int64_t q_rows, int max_ctx) {
   const int64_t wgs = std::max<int64_t>(1, int64_t(n_seq) * nkv * ((q_rows + 31) / 32));
+  if (max_ctx <= kWholeCtx) return 1;
   const int64_t most = (int64_t(max_ctx) + kMinChunk - 1) / kMinChunk;
   return std::max<int64_t>(1, std::min(int64_t(device_cu_count()) / wgs, most));
 }
