@@ -38,7 +38,7 @@ namespace hdf {
 
 namespace {
 
-constexpr int kWriteWaves = 4, kReadWaves = 16;   // heads a workgroup, at most
+constexpr int kWaves = 4, kWideWaves = 16;   // heads a workgroup, at most
 constexpr int kGroupRows = 8;
 
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
@@ -160,7 +160,7 @@ __device__ __forceinline__ void place_row(const Kv4RowArgs& a, int64_t g, int i,
 }
 
 template <typename T, int HD, bool LIST>
-__global__ void __launch_bounds__(kWriteWaves * kWave) kv4_write_kernel(Kv4RowArgs a) {
+__global__ void __launch_bounds__(kWaves * kWave) kv4_write_kernel(Kv4RowArgs a) {
   constexpr int H = HD / 64;       // eights of dims a lane
   constexpr int TB = kv4_tile_bytes(HD);
   const int lane = threadIdx.x & 63, i = lane >> 3, j = lane & 7;
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kWriteWaves * kWave) kv4_write_kernel(Kv4RowAr
 }
 
 template <typename T, int HD, bool LIST>
-__global__ void __launch_bounds__(kReadWaves * kWave) kv4_read_kernel(Kv4RowArgs a) {
+__global__ void __launch_bounds__(kWideWaves * kWave) kv4_read_kernel(Kv4RowArgs a) {
   constexpr int H = HD / 64, TB = kv4_tile_bytes(HD);
   const int lane = threadIdx.x & 63, i = lane >> 3, j = lane & 7;
   const int h = blockIdx.x * (blockDim.x / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -378,9 +378,12 @@ __global__ void __launch_bounds__(kReadWaves * kWave) kv4_read_kernel(Kv4RowArgs
 
 template <typename T, int HD, bool LIST>
 hipError_t rows_t(bool write, const Kv4RowArgs& a, hipStream_t s) {
-  // Heads of a group by workgroup.  65536 rows of 32 x 128 in bf16, 4, 8, 16 heads: written 221, 234,
-  // 240 us, read back 266, 260, 249; 4096 rows 17.7, 18.1, 18.7 and 19.5, 20.2, 20.3.
-  const int most = write ? kWriteWaves : kReadWaves, wgs = (a.nh + most - 1) / most;
+  // Heads of a group by workgroup, 32 heads of 128 in bf16, 4 heads, 8, 16: written 65536 rows 221 us,
+  // 234, 240; read back 65536 rows 266, 260, 249; 4096 rows 19.5, 20.2, 20.3; 40 listed rows 4.2 and 6.2
+  // (16), 129 of 64 dims 3.7 and 5.0.  16384 rows read back: 68, 67, 65 from memory, 56 and 60 (16) right
+  // after they were written, so more than four from twice their number on.
+  const bool wide = !write && a.groups * a.nh > 131072;
+  const int most = wide ? kWideWaves : kWaves, wgs = (a.nh + most - 1) / most;
   const dim3 grid(wgs, unsigned(a.groups < 65535 ? a.groups : 65535)), block((a.nh + wgs - 1) / wgs * kWave);
   if (write)
     hipLaunchKernelGGL((kv4_write_kernel<T, HD, LIST>), grid, block, 0, s, a);
