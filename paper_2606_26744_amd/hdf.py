@@ -1121,18 +1121,20 @@ def kv4_alloc(n_layers: int, n_kv_heads: int, head_dim: int, kv_cap: int,
 _KV4_HEAD_DIMS = {}
 
 
+def _kv4_head_dim(tile: int) -> int:
+    for hd in (64, 128):
+        _KV4_HEAD_DIMS[int(lib().hdf_kv4_tile_bytes(hd))] = hd
+    if tile not in _KV4_HEAD_DIMS:
+        raise ValueError(f"tiles of {tile} bytes belong to no head_dim")
+    return _KV4_HEAD_DIMS[tile]
+
+
 def _kv4_dims(kv4: torch.Tensor, layer: int):
     """(n_kv_heads, head_dim, kv_cap) of a cache tensor from kv4_alloc that holds `layer`."""
-    shape = kv4.shape
-    if len(shape) != 4 or kv4.dtype != torch.uint8 or not kv4.is_contiguous():
+    if kv4.dim() != 4 or kv4.dtype is not torch.uint8 or not kv4.is_contiguous():
         raise ValueError("kv4 must be a contiguous uint8 [layers, heads, tiles, tile bytes] tensor")
-    L, nh, tiles, tile = shape
-    hd = _KV4_HEAD_DIMS.get(tile)
-    if hd is None:
-        hd = next((d for d in (64, 128) if int(lib().hdf_kv4_tile_bytes(d)) == tile), None)
-        if hd is None:
-            raise ValueError(f"tiles of {tile} bytes belong to no head_dim")
-        _KV4_HEAD_DIMS[tile] = hd
+    L, nh, tiles, tile = kv4.shape
+    hd = _KV4_HEAD_DIMS.get(tile) or _kv4_head_dim(tile)
     if not 0 <= layer < L:
         raise ValueError(f"layer {layer} outside [0, {L})")
     return nh, hd, tiles * 64
@@ -1155,7 +1157,7 @@ def _row_stride(t: Optional[torch.Tensor], shape, what: str) -> int:
     ld, one = t.stride()
     if one != 1:
         raise ValueError(f"{what} must have unit column stride")
-    return ld if shape[0] > 1 else max(ld, shape[1])
+    return ld if ld > shape[1] or shape[0] > 1 else shape[1]
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -1209,7 +1211,8 @@ def kv4_read_rows(kv4: torch.Tensor, layer: int, n: int, *, row0: int = 0,
             return kv4_read_rows(kv4, layer, n, row0=row0, rows=rows, dtype=dtype, out=out)
     shape = (n, nh * hd)
     if out is None:
-        k, v = torch.empty((2, *shape), dtype=dtype, device=kv4.device).unbind(0)
+        k = kv4.new_empty(shape, dtype=dtype)
+        v = torch.empty_like(k)
         ld_k = ld_v = shape[1]
         _same_device(kv4, rows)
     else:
