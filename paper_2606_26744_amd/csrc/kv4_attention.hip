@@ -4,6 +4,29 @@
 //   O = softmax(scale * Q [K, K_b]^T) [V, V_b],   lse = log of the softmax's sum
 // G = n_heads / n_kv_heads query heads share a head of keys, so a (sequence, head of keys) has
 // G * B query rows, row k * G + j being slot k of its j-th head.
+//
+// A workgroup of eight waves (or four: few_waves) takes 16 query rows, or 32 as two tiles a wave, of
+// a (sequence, head of keys) over a chunk of the context; a wave takes every eighth of its 64-row
+// tiles and keeps its own running maximum and sum, so the loop has no barrier and no LDS, and the
+// waves' states are joined once.  The products are S^T = K Q^T and O^T = V^T P^T: the keys of a 64-row tile are laid
+// out so that the lane that has a score has its probability where the second product wants it.
+// Codes go from their 16-byte loads through the conversion instructions into the matrix
+// instructions.  Keys become bf16 (exactly, scale and all); values fp16 codes, their scales in the
+// probabilities (struct Lift); 32-bit queries and probabilities are three bf16 terms.
+//
+// Bound by the memory where a workgroup has enough tiles: 64 contexts of 1024 to 16384 positions, 32
+// heads, B = 16, 361 us for 2.32 GB (6.4 TB/s; vector issue 53% of the cycles, matrix cores 18%);
+// 8 x 2048 positions 13 to 15 us for 70 MB, 3 of them start and join.  Bound by instruction
+// issue where 32 queries share a head of keys: a tile takes a wave about 430 vector and 64 matrix
+// instructions, 3100 cycles beside the SIMD's other wave, so 16 contexts of 512 to 8192 positions, 32
+// heads over 8, B = 16, take 39 us, the time of the longest's workgroups (2.0 TB/s on average).
+// A conversion costs what any vector instruction does (4.6 cycles; to fp16 as to bf16), an
+// exponential two, a matrix instruction 16 of the matrix core and about half of them of the issue.
+// Measured and not kept: products of fp4 keys with two fp8 terms of a query (products 2^-11 below an
+// instruction's greatest are dropped: log-sum-exps 1e-3 off); loads for the next tile behind a branch
+// (the waits then cover them too: 17 us for 14.7 in the 8 x 2048 case); barriers a round or priorities
+// so that a SIMD's waves alternate (42 for 41 us, 40 for 40); 2, 6, 12 or 16 waves a workgroup;
+// the block's keys read by its wave from memory, without LDS (no gain, and the 32-bit form spills).
 #include <algorithm>
 #include <type_traits>
 
@@ -15,9 +38,7 @@ namespace hdf {
 namespace {
 
 constexpr int kTile = 64;
-constexpr int kAttnWaves = 8;
-constexpr int kAttnThreads = kAttnWaves * kWave;
-constexpr int kMaxTiles = kAttnWaves * kWave;   // tiles of a chunk: one a lane
+constexpr int kWaves = 8, kFewWaves = 4;    // of a workgroup (attn_t)
 constexpr int kJoinThreads = 256;
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
@@ -392,29 +413,29 @@ __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRow
   }
 }
 
-template <typename T, int HD, int NQ>
-__global__ void __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2)))
+template <typename T, int HD, int NQ, int W>
+__global__ void __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 kv4_attn_kernel(Kv4AttnArgs a) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int NDT = HD / 16;
+  constexpr int NDT = HD / 16, kThreads = W * kWave;
   // The block's keys and values, later the waves' states.
   __shared__ __align__(16) union {
     BlockRows<T, HD> blk;
-    float o[kAttnWaves][16][HD + 4];
+    float o[W][16][HD + 4];
   } pool;
-  __shared__ float red_m[kAttnWaves][16], red_l[kAttnWaves][16];
+  __shared__ float red_m[W][16], red_l[W][16];
   const int chunk = blockIdx.z, hk = blockIdx.x;
   const int G = a.G, R = G * a.B;
   const int s = blockIdx.y / a.n_groups, row0 = 16 * NQ * (blockIdx.y - s * a.n_groups);
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, ql = lane & 15;
 
-  // Lane l keeps the place of the wave's l-th tile, tile wid + kAttnWaves * l of the chunk: read
+  // Lane l keeps the place of the wave's l-th tile, tile wid + W * l of the chunk: read
   // beside the lengths, not behind them.  -1 for a page outside the pool, whose keys count as absent.
   const int t0 = chunk * (a.chunk_len >> 6);
   int page = -1;
   {
-    const int t = t0 + wid + kAttnWaves * lane;
+    const int t = t0 + wid + W * lane;
     if (a.page_table != nullptr) {
       if (t < a.max_pages) page = a.page_table[int64_t(s) * a.max_pages + t];
     } else if (a.kv_offsets != nullptr) {
@@ -441,14 +462,14 @@ kv4_attn_kernel(Kv4AttnArgs a) {
                    : nullptr;
   };
   // The block's rows, 16 bytes a thread and item, on their way before anything larger.
-  constexpr int E = 16 / sizeof(T), P = HD / E, NI = 64 * P / kAttnThreads;   // items of 64 rows
+  constexpr int E = 16 / sizeof(T), P = HD / E, NI = 64 * P / kThreads;   // items of 64 rows
   u32x4 bw[2][NI];
   if (nbk > 0) {
     const T* kb = static_cast<const T*>(a.kb) + int64_t(s) * a.B * a.ld_kb + int64_t(hk) * HD;
     const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int e = n * kAttnThreads + threadIdx.x, r = e / P, i = (e % P) * E;
+      const int e = n * kThreads + threadIdx.x, r = e / P, i = (e % P) * E;
       bw[0][n] = bw[1][n] = u32x4{0, 0, 0, 0};
       if (r < nbk) {
         bw[0][n] = ld16(kb + r * a.ld_kb + i);
@@ -460,7 +481,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
 #pragma unroll
   for (int n = 0; n < NQ; ++n) q[n].load(q_row(n), g);
   // This wave's tiles, its l-th into t.
-  const int mine = (nct - wid + kAttnWaves - 1) / kAttnWaves;
+  const int mine = (nct - wid + W - 1) / W;
   auto fetch = [&](Tile<HD>& t, int l) {
     const int at = l < mine ? __builtin_amdgcn_readlane(page, l) : -1;
     load_tile<HD>(t, head + int64_t(max(at, 0)) * kv4_tile_bytes(HD), at >= 0, lane);
@@ -481,7 +502,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     const int rows = (nbk + 31) & ~31;
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int e = n * kAttnThreads + threadIdx.x, r = e / P, i = (e % P) * E;
+      const int e = n * kThreads + threadIdx.x, r = e / P, i = (e % P) * E;
       if (r < rows) {
         st16(&pool.blk.k[r][i], bw[0][n]);
 #pragma unroll
@@ -494,7 +515,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       }
     }
     lds_barrier();
-    if (wid == nct % kAttnWaves) {
+    if (wid == nct % W) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
         block_step<T, HD>(q[n], pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
@@ -502,7 +523,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     }
   }
   auto step = [&](Tile<HD>& t, int l) {
-    const int left = k_hi - k_lo - (wid + kAttnWaves * l) * kTile;
+    const int left = k_hi - k_lo - (wid + W * l) * kTile;
     tile_step<T, HD, NQ>(t, q, st, lift, __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, left), g,
                          a.scale_log2);
   };
@@ -531,18 +552,18 @@ kv4_attn_kernel(Kv4AttnArgs a) {
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4_t*>(&pool.o[wid][ql][16 * dt + 4 * g]) = st[n].o[dt];
     __syncthreads();
-    for (int e = threadIdx.x; e < 16 * (HD / 4); e += kAttnThreads) {
+    for (int e = threadIdx.x; e < 16 * (HD / 4); e += kThreads) {
       const int qq = e / (HD / 4), dim = 4 * (e % (HD / 4));
       const int qr = row0 + 16 * n + qq, k = slot_of(a, qr);
       if (k >= blen) continue;
       float mm = red_m[0][qq];
 #pragma unroll
-      for (int w = 1; w < kAttnWaves; ++w) mm = fmaxf(mm, red_m[w][qq]);
+      for (int w = 1; w < W; ++w) mm = fmaxf(mm, red_m[w][qq]);
       const float base = mm == -INFINITY ? 0.f : mm;
       f32x4_t o = {0.f, 0.f, 0.f, 0.f};
       float l = 0.f;
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = half_power(red_m[w][qq] - base);
         const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&pool.o[w][qq][dim]);
 #pragma unroll
@@ -620,6 +641,21 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   if (d == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(sum)) * 0.6931471805599453f;
 }
 
+// Four waves a workgroup, of which a CU holds two so that one's start and join pass beside the other's
+// tiles, where there is more than a round of eight waves' and contexts are short; long ones of
+// unequal lengths leave CUs with one workgroup for longer.  us a call with eight and four, bf16, 16
+// queries, 32 heads of 128 with keys of their own, lengths from a tenth on:
+//   up to               300          2000         4000          8000          16384
+//   12 contexts (1.5)                19, 17       28, 32        49, 53
+//   16          (2)     13, 10       20, 16       36, 33        64, 65
+//   24          (3)     19, 14       32, 24       45, 44        97, 100
+//   64          (8)     52, 33 (500) 68, 50       127, 114      221, 209      363, 383
+// and all of one length: 16 of 2000 31, 26, of 8000 100, 97; 12 of 8000 80, 79.
+bool few_waves(int64_t wgs, int max_ctx) {
+  const int64_t rounds = wgs / device_cu_count();
+  return wgs > device_cu_count() && max_ctx <= 2048 * std::min<int64_t>(rounds, 4);
+}
+
 template <typename T, int HD>
 hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
   const int R = a.G * a.B;
@@ -628,19 +664,25 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
   const int nq = R > 16 ? MQ : 1;
   a.n_groups = (R + 16 * nq - 1) / (16 * nq);
   const dim3 grid(a.nkv, unsigned(a.n_seq * a.n_groups), a.n_chunks);
-  if (nq == 1)
-    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, 1>), grid, dim3(kAttnThreads), 0, s, a);
+  const bool few = few_waves(int64_t(grid.x) * grid.y * grid.z, a.max_ctx);
+  const dim3 block((few ? kFewWaves : kWaves) * kWave);
+  if (nq == 1 && few)
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, 1, kFewWaves>), grid, block, 0, s, a);
+  else if (nq == 1)
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, 1, kWaves>), grid, block, 0, s, a);
+  else if (few)
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, MQ, kFewWaves>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, MQ>), grid, dim3(kAttnThreads), 0, s, a);
+    hipLaunchKernelGGL((kv4_attn_kernel<T, HD, MQ, kWaves>), grid, block, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
   // Two slices for up to eight chunks (four rows a workgroup at 128 dims), else a workgroup a row: the
   // call takes 32.1 us in the place of 33.3 for 2 contexts of 8192 positions, 32 heads over 8, B = 64
   // (2048 rows of two chunks), 22.7 in the place of 23.0 for 4 contexts, B = 16.
-  constexpr int Q = HD / 4, most = kJoinThreads / Q, few = 2;
-  const dim3 rows((R + most / few - 1) / (most / few), a.nkv, a.n_seq);
+  constexpr int Q = HD / 4, most = kJoinThreads / Q, two = 2;
+  const dim3 rows((R + most / two - 1) / (most / two), a.nkv, a.n_seq);
   if (a.n_chunks <= 8)
-    hipLaunchKernelGGL((kv4_join_kernel<T, HD, few>), rows, dim3(kJoinThreads), 0, s, a);
+    hipLaunchKernelGGL((kv4_join_kernel<T, HD, two>), rows, dim3(kJoinThreads), 0, s, a);
   else
     hipLaunchKernelGGL((kv4_join_kernel<T, HD, most>), dim3(R, a.nkv, a.n_seq), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
@@ -663,6 +705,7 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
 // of 1024, 2048, 4096, 8192, 16384 (2048 workgroups), 16 of 512 to 8192 in 256 workgroups 39, in twice
 // and four times as many 45 and 48.
 constexpr int kMinChunk = 512, kWholeCtx = 1536;
+constexpr int kMaxChunk = kWaves * kWave * kTile;   // a lane keeps the place of one tile
 
 static int64_t chunks_wanted(int n_seq, int nkv, int64_t q_rows, int max_ctx) {
   const int64_t wgs = std::max<int64_t>(1, int64_t(n_seq) * nkv * ((q_rows + 31) / 32));
@@ -675,7 +718,7 @@ void kv4_attn_plan(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx, int*
                    int* chunk_len) {
   const int64_t ctx = std::max(max_ctx, 1), want = chunks_wanted(n_seq, nkv, q_rows, max_ctx);
   int64_t len = (ctx + want - 1) / want;
-  len = std::min<int64_t>((len + 511) / 512 * 512, kMaxTiles * kTile);
+  len = std::min<int64_t>((len + 511) / 512 * 512, kMaxChunk);
   *chunk_len = int(len);
   *n_chunks = int((ctx + len - 1) / len);
 }
@@ -683,7 +726,7 @@ void kv4_attn_plan(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx, int*
 size_t kv4_attn_ws_bytes(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx) {
   // A shorter context takes as many chunks as are wanted for it, or as many of the greatest length
   // as it needs: neither grows as it gets shorter.
-  const int64_t longest = (int64_t(max_ctx) + kMaxTiles * kTile - 1) / (kMaxTiles * kTile);
+  const int64_t longest = (int64_t(max_ctx) + kMaxChunk - 1) / kMaxChunk;
   const int64_t most = std::max(chunks_wanted(n_seq, nkv, q_rows, max_ctx), longest);
   if (most <= 1) return 0;
   return size_t(n_seq) * nkv * size_t(most) * size_t(q_rows) * (hd + 2) * 4;

@@ -104,6 +104,25 @@ def test_blocks_over_ragged_contexts(hd, dtype, B, H, nkv):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("dtype,hd,B,H,nkv", [(BF, 128, 3, 8, 8), (BF, 64, 16, 16, 8), (BF, 128, 5, 56, 8),
+                                              (BF, 64, 1, 32, 32), (F32, 128, 2, 16, 8), (F32, 64, 17, 8, 8)])
+@pytest.mark.parametrize("long", [130, 700])
+def test_many_short_contexts(dtype, hd, B, H, nkv, long):
+    """More workgroups than the card has compute units, for which smaller ones are taken."""
+    print(f"[kv4 attention] many, hd={hd} {dtype} B={B} H={H}/{nkv} long={long}", flush=True)
+    n = 44 if nkv == 8 else 11
+    ctx = ([0, 1, 63, 64, 65, 127, 128, 129, long, 2, 100] * 4)[:n]
+    c = Case(ctx, B, H, nkv, hd, dtype, seed=20 + B)
+    blen = [s % (B + 1) for s in range(n)]
+    bl = torch.tensor(blen, dtype=torch.int32, device="cuda")
+    out = torch.full_like(c.q, 77.0)
+    lse = torch.full((n, B, H), 55.0, device="cuda")
+    hdf.block_attention_kv4(c.q, c.kv4, 0, block_len=bl, causal=True, out=(out, lse), **c.kw)
+    c.check(out, lse, causal=True, blen=blen)
+    for s, b in enumerate(blen):
+        assert (out[s, b:] == 77.0).all() and (lse[s, b:] == 55.0).all()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("causal", [False, True])
 def test_block_lengths_and_causal_slots(dtype, causal):
