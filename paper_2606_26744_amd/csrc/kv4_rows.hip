@@ -26,7 +26,7 @@
 // does not matter.
 //
 // Bound by the memory: 65536 rows of 32 heads of 128 in bf16, 1.36 GB, are written in 221 us (6.1 TB/s,
-// four parts read to one written) and read back in 249 (5.4 TB/s, one part read to four written); a copy
+// four parts read to one written) and read back in 239 (5.7 TB/s, one part read to four written); a copy
 // of 4 GiB moves 4.7 TB/s.  Rows that a call reads back are stored through the caches: past them takes
 // the same time, and a few rows are what the next kernel reads.
 #include <type_traits>
@@ -38,7 +38,7 @@ namespace hdf {
 
 namespace {
 
-constexpr int kWaves = 4, kWideWaves = 16;   // heads a workgroup, at most
+constexpr int kHeads = 4, kReadGroups = 4;   // of a workgroup, at most: a wave each
 constexpr int kGroupRows = 8;
 
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
@@ -160,11 +160,11 @@ __device__ __forceinline__ void place_row(const Kv4RowArgs& a, int64_t g, int i,
 }
 
 template <typename T, int HD, bool LIST>
-__global__ void __launch_bounds__(kWaves * kWave) kv4_write_kernel(Kv4RowArgs a) {
+__global__ void __launch_bounds__(kHeads * kWave) kv4_write_kernel(Kv4RowArgs a) {
   constexpr int H = HD / 64;       // eights of dims a lane
   constexpr int TB = kv4_tile_bytes(HD);
   const int lane = threadIdx.x & 63, i = lane >> 3, j = lane & 7;
-  const int h = blockIdx.x * (blockDim.x / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x * kHeads + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (h >= a.nh) return;
   Place pl;
   pl.head = a.tiles + int64_t(h) * (a.cap >> 6) * TB;
@@ -298,14 +298,15 @@ __global__ void __launch_bounds__(kWaves * kWave) kv4_write_kernel(Kv4RowArgs a)
 }
 
 template <typename T, int HD, bool LIST>
-__global__ void __launch_bounds__(kWideWaves * kWave) kv4_read_kernel(Kv4RowArgs a) {
+__global__ void __launch_bounds__(kHeads * kReadGroups * kWave) kv4_read_kernel(Kv4RowArgs a) {
   constexpr int H = HD / 64, TB = kv4_tile_bytes(HD);
   const int lane = threadIdx.x & 63, i = lane >> 3, j = lane & 7;
-  const int h = blockIdx.x * (blockDim.x / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x * kHeads + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (h >= a.nh) return;
   Place pl;
   pl.head = a.tiles + int64_t(h) * (a.cap >> 6) * TB;
-  for (int64_t g = blockIdx.y; g < a.groups; g += gridDim.y) {
+  const int in_wg = __builtin_amdgcn_readfirstlane(threadIdx.y), gw = blockDim.y;
+  for (int64_t g = int64_t(blockIdx.y) * gw + in_wg; g < a.groups; g += int64_t(gridDim.y) * gw) {
     place_row<LIST>(a, g, i, pl);
     const bool live = pl.row >= 0;
     const int r = live ? int(pl.row & 63) : 0;
@@ -378,13 +379,13 @@ __global__ void __launch_bounds__(kWideWaves * kWave) kv4_read_kernel(Kv4RowArgs
 
 template <typename T, int HD, bool LIST>
 hipError_t rows_t(bool write, const Kv4RowArgs& a, hipStream_t s) {
-  // Heads of a group by workgroup, 32 heads of 128 in bf16, 4 heads, 8, 16: written 65536 rows 221 us,
-  // 234, 240; read back 65536 rows 266, 260, 249; 4096 rows 19.5, 20.2, 20.3; 40 listed rows 4.2 and 6.2
-  // (16), 129 of 64 dims 3.7 and 5.0.  16384 rows read back: 68, 67, 65 from memory, 56 and 60 (16) right
-  // after they were written, so more than four from twice their number on.
-  const bool wide = !write && a.groups * a.nh > 131072;
-  const int most = wide ? kWideWaves : kWaves, wgs = (a.nh + most - 1) / most;
-  const dim3 grid(wgs, unsigned(a.groups < 65535 ? a.groups : 65535)), block((a.nh + wgs - 1) / wgs * kWave);
+  // Four heads of a group a workgroup; in long reads of four neighbouring groups, which share lines of
+  // the cache's tiles (the keys of 8 rows lie in runs of 64 bytes): (heads, groups) (4, 1), (16, 1),
+  // (2, 8), (4, 4) read 65536 rows of 32 x 128 in bf16 back in 266 us, 248, 249, 239, and 16384 in 68.8,
+  // 66.5, 67.1, 64.6; 4096 rows take 20 in all.  Written by 4, 8, 16 heads: 65536 rows 221, 234, 240.
+  const int gw = !write && a.groups * a.nh > 32768 ? kReadGroups : 1;
+  const int64_t gy = (a.groups + gw - 1) / gw;
+  const dim3 grid((a.nh + kHeads - 1) / kHeads, unsigned(gy < 65535 ? gy : 65535)), block(kHeads * kWave, gw);
   if (write)
     hipLaunchKernelGGL((kv4_write_kernel<T, HD, LIST>), grid, block, 0, s, a);
   else

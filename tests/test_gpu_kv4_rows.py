@@ -194,3 +194,25 @@ def test_a_row_named_twice_disturbs_no_other():
         _same(got[[rows[i] for i in once]], w)
         rest = [r for r in range(cap) if r not in rows]
         assert torch.equal(got[rest], old[rest])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_long_reads_are_those_of_their_pieces(hd, dtype):
+    """Long reads go by larger workgroups: runs and lists of rows, odd heads, rows outside the cache."""
+    nh, n = 33, 8209
+    cap = 64 * 130
+    kv4 = hdf.kv4_alloc(1, nh, hd, cap)
+    hdf.kv4_write_rows(kv4, 0, _rows(cap, nh * hd, dtype, 17), _rows(cap, nh * hd, dtype, 18))
+    order = torch.randperm(cap, generator=torch.Generator().manual_seed(3))[:n].int()
+    order[::1000] = -1
+    order[5::1000] = cap
+    order[80:96] = torch.arange(80, 96, dtype=torch.int32)
+    order = order.cuda()
+    for kw in (dict(row0=13), dict(rows=order)):
+        got = hdf.kv4_read_rows(kv4, 0, n, dtype=dtype, **kw)
+        for lo in range(0, n, 1000):
+            m = min(1000, n - lo)
+            part = dict(row0=13 + lo) if "row0" in kw else dict(rows=order[lo:lo + m].contiguous())
+            for x, y in zip(got, hdf.kv4_read_rows(kv4, 0, m, dtype=dtype, **part)):
+                assert torch.equal(x[lo:lo + m], y), lo
