@@ -212,10 +212,13 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // lift = 15 - kSlack - log2 of a power of two above the greatest scale so far (2^-80 at least): the
 // factor is below 2^15, and of full precision down to 2^-25 of the greatest probability times the
 // greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-37 even
-// beside scales of 2^100.  fp32 queries: three bf16 terms, no lift.
+// beside scales of 2^100.  The block's values are not split off their probabilities: so that 64
+// products with values below 2^e stay within fp32, the lift is 116 - e where that is less.  fp32 queries: three bf16 terms, no lift.
 struct Lift {
   int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
   __device__ __forceinline__ float value() const { return float(141 - kSlack - top); }
+  // The block's values have biased exponents of up to `e`: below 2^(e - 126).
+  __device__ __forceinline__ void for_block(int e) { top = max(top, e - (242 - (141 - kSlack))); }
 };
 
 // A query tile as the operand of the products with keys: lane (g, ql) holds dims (HD/4)g + 8j .. of
@@ -358,7 +361,7 @@ struct BlockRows {
 // nbk of them into the state of a query tile; a query sees those up to `last`.
 template <typename T, int HD>
 __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRows<T, HD>& b, State<HD>& st,
-                                           int nbk, int last, int lane, float c) {
+                                           int nbk, int last, int lane, float c, float lift) {
   constexpr bool F32 = sizeof(T) == 4;
   const int g = lane >> 4, ql = lane & 15;
   float x[16];
@@ -389,7 +392,7 @@ __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRow
     for (int e = 0; e < 4; ++e)
       x[4 * t + e] = 32 * (t >> 1) + 4 * (t & 1) + e < left ? acc[e] : -INFINITY;
   }
-  soft_step<HD>(st, x, c, F32 ? 0.f : Lift().value(), 0.f);
+  soft_step<HD>(st, x, c, lift, 0.f);
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
     if (32 * ks >= nbk) break;
@@ -424,6 +427,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     float o[W][16][HD + 4];
   } pool;
   __shared__ float red_m[W][16], red_l[W][16];
+  __shared__ int blk_top[W];   // greatest biased exponent of the block's values, by wave
   const int chunk = blockIdx.z, hk = blockIdx.x;
   const int G = a.G, R = G * a.B;
   const int s = blockIdx.y / a.n_groups, row0 = 16 * NQ * (blockIdx.y - s * a.n_groups);
@@ -514,12 +518,32 @@ kv4_attn_kernel(Kv4AttnArgs a) {
         }
       }
     }
+    if constexpr (!F32) {
+      u16x2_t w = {0, 0};
+#pragma unroll
+      for (int n = 0; n < NI; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w = __builtin_elementwise_max(w, __builtin_bit_cast(u16x2_t, uint32_t(bw[1][n][k] & 0x7FFF7FFFu)));
+      int top = max(w[0], w[1]) >> 7;
+      if (__any(top > 152)) {   // below, for_block changes nothing
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) top = max(top, __shfl_xor(top, d, kWave));
+      }
+      if (lane == 0) blk_top[wid] = top;
+    }
     lds_barrier();
     if (wid == nct % W) {
+      if constexpr (!F32) {
+        int top = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = max(top, blk_top[w]);
+        lift.for_block(top);
+      }
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
         block_step<T, HD>(q[n], pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
-                          lane, a.scale_log2);
+                          lane, a.scale_log2, F32 ? 0.f : lift.value());
     }
   }
   auto step = [&](Tile<HD>& t, int l) {

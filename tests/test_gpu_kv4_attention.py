@@ -184,6 +184,19 @@ def test_values_of_any_size(dtype, sizes):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [1e-30, 1e8, 1e12, 1e30, 1e36])
+@pytest.mark.parametrize("ctx", [[0, 40], [700, 130]])
+def test_block_values_of_any_size(dtype, size, ctx):
+    """Values of the block far from 1, alone and beside a context of ordinary ones."""
+    c = Case(ctx, 7, 4, 2, 128, dtype, seed=15)
+    c.vb.mul_(size)
+    c.vb[1, 3, 1, 5] *= 16
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
+    assert torch.isfinite(out.float()).all()
+    c.check(out, lse)
+
+
 def test_a_cache_beyond_32_bits():
     """Pages at the end of a cache of more than 4 GiB."""
     c = Case([300], 4, 8, 8, 128, BF, seed=14)
