@@ -416,6 +416,53 @@ __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRow
   }
 }
 
+// Greatest biased exponent of a thread's items of the block's values (255: one is no number).
+template <bool F32, int NI>
+__device__ __forceinline__ int block_top(const u32x4 (&v)[NI]) {
+  u16x2_t w = {0, 0};
+  uint32_t u = 0;
+#pragma unroll
+  for (int n = 0; n < NI; ++n)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (F32)
+        u = max(u, uint32_t(v[n][k] & 0x7FFFFFFFu));
+      else
+        w = __builtin_elementwise_max(w, __builtin_bit_cast(u16x2_t, uint32_t(v[n][k] & 0x7FFF7FFFu)));
+    }
+  return F32 ? int(u >> 23) : max(w[0], w[1]) >> 7;
+}
+template <bool F32, int NI>
+__device__ __forceinline__ void numbers_only(u32x4 (&v)[NI]) {
+#pragma unroll
+  for (int n = 0; n < NI; ++n)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w = v[n][k];
+      if ((w & 0x7F800000u) == 0x7F800000u) w &= F32 ? 0u : 0xFFFFu;
+      if (!F32 && (w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+      v[n][k] = w;
+    }
+}
+// The block's values (rows of v) that are no numbers into the state of a query tile: a query's sums
+// become what those that it sees, up to slot `last`, make of them.
+template <typename T, int HD>
+__device__ __forceinline__ void no_numbers(State<HD>& st, const T* v, int64_t ld, int last, int nbk, int g) {
+  for (int r = 0; r < nbk; ++r)
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x;
+        if constexpr (sizeof(T) == 2)
+          x = bf2f(v[r * ld + 16 * dt + 4 * g + e]);
+        else
+          x = v[r * ld + 16 * dt + 4 * g + e];
+        const bool number = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+        st.o[dt][e] += number || r > last ? 0.f : x;
+      }
+}
+
 template <typename T, int HD, int NQ, int W>
 __global__ void __launch_bounds__(W * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 kv4_attn_kernel(Kv4AttnArgs a) {
@@ -504,6 +551,15 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   // Through LDS into the state of the wave that has the fewest tiles.
   if (nbk > 0) {
     const int rows = (nbk + 31) & ~31;
+    // What is no number among the values leaves as 0: a product with a masked probability's 0 would be NaN.
+    const int top = block_top<F32, NI>(bw[1]);
+    if (__any(top == 255)) numbers_only<F32, NI>(bw[1]);
+    int all = top;
+    if (__any(top > 152)) {   // below, for_block changes nothing
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) all = max(all, __shfl_xor(all, d, kWave));
+    }
+    if (lane == 0) blk_top[wid] = all;
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
       const int e = n * kThreads + threadIdx.x, r = e / P, i = (e % P) * E;
@@ -518,32 +574,23 @@ kv4_attn_kernel(Kv4AttnArgs a) {
         }
       }
     }
-    if constexpr (!F32) {
-      u16x2_t w = {0, 0};
-#pragma unroll
-      for (int n = 0; n < NI; ++n)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          w = __builtin_elementwise_max(w, __builtin_bit_cast(u16x2_t, uint32_t(bw[1][n][k] & 0x7FFF7FFFu)));
-      int top = max(w[0], w[1]) >> 7;
-      if (__any(top > 152)) {   // below, for_block changes nothing
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) top = max(top, __shfl_xor(top, d, kWave));
-      }
-      if (lane == 0) blk_top[wid] = top;
-    }
     lds_barrier();
     if (wid == nct % W) {
-      if constexpr (!F32) {
-        int top = 0;
+      int most = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = max(top, blk_top[w]);
-        lift.for_block(top);
-      }
+      for (int w = 0; w < W; ++w) most = max(most, blk_top[w]);
+      most = __builtin_amdgcn_readfirstlane(most);
+      if constexpr (!F32) lift.for_block(most);
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
         block_step<T, HD>(q[n], pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
                           lane, a.scale_log2, F32 ? 0.f : lift.value());
+      if (most == 255) {
+        const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+          no_numbers<T, HD>(st[n], vb, a.ld_vb, min(nbk - 1, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B), nbk, g);
+      }
     }
   }
   auto step = [&](Tile<HD>& t, int l) {

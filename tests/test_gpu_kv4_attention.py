@@ -2,7 +2,8 @@
 
 Bound of an output element, with A = sum p |v| (at least |out|):
   a score is off by d <= (hd + 4) 2^-24 scale sum |q k| + 2^-22 (fp32 sums; the exponential and
-  its argument), its probability by a factor 1 + d, the ratio of sums by 2 d; bf16: a probability
+  its argument; bf16: the argument holds a power of two of up to 2^94, half a step 2^-18), its
+  probability by a factor 1 + d, the ratio of sums by 2 d; bf16: a probability
   times its value's scale is rounded to fp16, 2^-11 of itself, or 2^-25 in units of 2^-11 of the
   greatest probability (at most 1 of the sum) times twice the greatest scale, so 2^-35 max |v| a key
   (the reference of the probabilities is at most 2^4 below the greatest, and their factor's top 2^15);
@@ -76,7 +77,7 @@ class Case:
             kb, vb = (_np(self.kb[s, :b]), _np(self.vb[s, :b])) if self.block else (None, None)
             o, l, mass, reach = ref.attend(_np(self.q[s, :b]), self.k[s], self.v[s], kb, vb,
                                            causal=causal, scale=scale)
-            d = (self.hd + 4) * 2.0 ** -24 * reach + 2.0 ** -22 + (2.0 ** -24 * reach if f32 else 0)
+            d = (self.hd + 4) * 2.0 ** -24 * reach + 2.0 ** -22 + (2.0 ** -24 * reach if f32 else 2.0 ** -18)
             N = T + self.B
             tol = mass * (2 * d[..., None] + (2.0 ** -24 if f32 else 2.0 ** -11) + 2 * N * 2.0 ** -24)
             tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
@@ -195,6 +196,37 @@ def test_block_values_of_any_size(dtype, size, ctx):
     out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, **c.kw)
     assert torch.isfinite(out.float()).all()
     c.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype,hd,B,H", [(BF, 128, 9, 4), (BF, 64, 6, 2), (F32, 128, 9, 2), (F32, 64, 9, 4)])
+def test_what_is_no_number_in_masked_slots(dtype, hd, B, H):
+    """A causal slot does not see the slots after it, whatever they hold, nor any slot those from
+    the block's length on."""
+    c = Case([100, 0], B, H, 2, hd, dtype, seed=16)
+    blen = [B, 4]
+    kw = dict(c.kw, block_len=torch.tensor(blen, dtype=torch.int32, device="cuda"))
+    want, lse0 = hdf.block_attention_kv4(c.q, c.kv4, 0, causal=True, **kw)
+    nan, inf = float("nan"), float("inf")
+    c.vb[0, 5, 0, 3] = nan                # seen from slot 5 on
+    c.vb[0, 4, 1, 7], c.vb[0, 5, 1, 7] = inf, -inf
+    c.vb[0, 3, 1, 9] = -inf
+    c.kb[0, 5, 0, 0] = nan                # the scores of head 0 from slot 5 on
+    c.kb[1, 4:], c.vb[1, 4:] = nan, inf
+    out, lse = hdf.block_attention_kv4(c.q, c.kv4, 0, causal=True, **kw)
+    G = H // 2
+    assert torch.equal(out[1, :4], want[1, :4]) and torch.equal(lse[1, :4], lse0[1, :4])
+    # A value that is no number moves the power of two that probabilities are taken relative to, and
+    # with it the rounding of the exponentials' arguments (2^-18 each side) and of what follows.
+    tol = 2.0 ** -7 if dtype == BF else 2.0 ** -16
+    near = lambda a, b: torch.allclose(a.float(), b.float(), rtol=tol, atol=tol * float(want.abs().max()))
+    assert near(out[0, :5, :G], want[0, :5, :G]) and near(lse[0, :5], lse0[0, :5])
+    assert torch.isnan(out[0, 5:, :G]).all() and torch.isnan(lse[0, 5:, :G]).all()
+    assert near(lse[0, :, G:], lse0[0, :, G:])
+    got, ref_ = out[0, :, G:].clone(), want[0, :, G:].clone()
+    assert (got[3:, :, 9] == -inf).all() and (got[4, :, 7] == inf).all() and torch.isnan(got[5:, :, 7]).all()
+    got[3:, :, 9] = ref_[3:, :, 9]
+    got[4:, :, 7] = ref_[4:, :, 7]
+    assert near(got, ref_)
 
 
 def test_a_cache_beyond_32_bits():
