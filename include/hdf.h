@@ -304,9 +304,11 @@ typedef struct {
  *   out = sum_t softmax(x)_t V_t,   lse = log sum_t exp(x_t)
  * with fp32 accumulation.  bf16: a context probability times its value's scale is rounded to 11 bits
  * (an eighth of the output's own rounding), or to a multiple of 2^-114 where every scale is below
- * 2^-80; fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of -inf.
- * B = 1 is the decoding of single tokens; without the block's keys, write a position to the cache
- * before the query that should see it.
+ * 2^-80, and beside a scale of 2^e (e > 10) probabilities below 2^(e - 136) of the greatest may count
+ * as 0; fp32: queries and probabilities keep 24.  A slot with no key at all gets zeros and an lse of
+ * -inf; what a slot does not see does not reach it, whatever it holds.  B = 1 is the decoding of
+ * single tokens; without the block's keys, write a position to the cache before the query that
+ * should see it.
  * q, k_blk, v_blk, out  row s*B + k, ld_* elements apart: [n_heads or n_kv_heads][head_dim]
  *             contiguous, dtype; k_blk and v_blk may be NULL together (no keys of the block)
  * ctx_len     [n_seq] int32, 0 .. max_ctx (larger ones count as max_ctx)
