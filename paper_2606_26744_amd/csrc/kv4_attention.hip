@@ -8,8 +8,9 @@
 // A workgroup of eight waves (or four: few_waves) takes 16 query rows, or 32 as two tiles a wave, of
 // a (sequence, head of keys) over a chunk of the context; a wave takes every eighth of its 64-row
 // tiles and keeps its own running maximum and sum, so the loop has no barrier and no LDS, and the
-// waves' states are joined once.  The products are S^T = K Q^T and O^T = V^T P^T: the keys of a 64-row tile are laid
-// out so that the lane that has a score has its probability where the second product wants it.
+// waves' states are joined once.  The products are S^T = K Q^T and O^T = V^T P^T: the keys of a 64-row
+// tile are laid out so that the lane that has a score has its probability where the second product
+// wants it.
 // Codes go from their 16-byte loads through the conversion instructions into the matrix
 // instructions.  Keys become bf16 (exactly, scale and all); values fp16 codes, their scales in the
 // probabilities (struct Lift); 32-bit queries and probabilities are three bf16 terms.
@@ -211,9 +212,10 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // So that it neither overflows nor loses small ones, probabilities are taken relative to 2^-lift,
 // lift = 15 - kSlack - log2 of a power of two above the greatest scale so far (2^-80 at least): the
 // factor is below 2^15, and of full precision down to 2^-25 of the greatest probability times the
-// greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-37 even
+// greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-36 even
 // beside scales of 2^100.  The block's values are not split off their probabilities: so that 64
-// products with values below 2^e stay within fp32, the lift is 116 - e where that is less.  fp32 queries: three bf16 terms, no lift.
+// products with values below 2^e stay within fp32, the lift is 116 - e where that is less.  fp32
+// queries: three bf16 terms, no lift.
 struct Lift {
   int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
   __device__ __forceinline__ float value() const { return float(141 - kSlack - top); }
@@ -589,7 +591,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
         const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
-          no_numbers<T, HD>(st[n], vb, a.ld_vb, min(nbk - 1, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B), nbk, g);
+          no_numbers<T, HD>(st[n], vb, a.ld_vb, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B, nbk, g);
       }
     }
   }
