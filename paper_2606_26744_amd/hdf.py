@@ -1264,8 +1264,10 @@ def block_attention_kv4(q: torch.Tensor, kv4: Optional[torch.Tensor], layer: int
     (kv_offsets [n_seq+1] or page_table [n_seq, max_pages], int32) and, where given, the block's
     own k_blk, v_blk [n_seq, B, n_kv_heads, head_dim] -> (out like q, lse [n_seq, B, n_heads] fp32
     or None).  ctx_len, block_len: int32 [n_seq]; scale: 1/sqrt(head_dim) if None; kv4 may be None
-    with max_ctx = 0.  q, k_blk, v_blk, out may be columns of wider rows.  out: a preallocated (out,
-    lse); outputs of slots from block_len on are left as they were."""
+    with max_ctx = 0.  max_ctx may be beyond the table (a bound that a loop keeps while it trims its
+    tables): positions behind the table's pages have no keys.  q, k_blk, v_blk, out may be columns of
+    wider rows.  out: a preallocated (out, lse); outputs of slots from block_len on are left as they
+    were."""
     shape = q.shape
     if len(shape) != 4:
         raise ValueError("q must be [n_seq, B, n_heads, head_dim]")
@@ -1288,6 +1290,7 @@ def block_attention_kv4(q: torch.Tensor, kv4: Optional[torch.Tensor], layer: int
                         page_table.shape[0] != n_seq:
                     raise ValueError("page_table must be an int32 [n_seq, max_pages] tensor")
                 width = page_table.shape[1]
+                max_ctx = min(max_ctx, 64 * width)   # no pages, so no keys, behind the table
             cache = ctypes.byref(Kv4Cache(kv4.data_ptr(), cap, layer, _ptr(kv_offsets),
                                           _ptr(page_table), width))
     else:
