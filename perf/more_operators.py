@@ -205,7 +205,7 @@ def prepare(case, seed):
         m = (T + 63) // 64
         table[i, :m] = order[at:at + m].int()
         at += m
-    s.update(ctx=ctx, blk=blk, max_ctx=max(ctx), page_table=table.to(DEV),
+    s.update(ctx=ctx, blk=blk, max_ctx=c["ctx_hi"], page_table=table.to(DEV),
              ctx_len=torch.tensor(ctx, dtype=torch.int32, device=DEV),
              block_len=torch.tensor(blk, dtype=torch.int32, device=DEV)
              if c["block"] == "causal_ragged" else None)
