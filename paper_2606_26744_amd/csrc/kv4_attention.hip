@@ -176,6 +176,12 @@ template <int HD>
 struct State {
   f32x4_t o[HD / 16];    // O^T: dim 16dt + 4g + e of query ql
   float m, l;            // l: this lane group's part of the sum
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
 };
 
 // Products of 64 keys (a lane's sixteen, -inf where masked) into the state's reference and sum; x
@@ -214,7 +220,7 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // factor is below 2^15, and of full precision down to 2^-25 of the greatest probability times the
 // greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-36 even
 // beside scales of 2^100.  The block's values are not split off their probabilities: so that 64
-// products with values below 2^e stay within fp32, the lift is 116 - e where that is less.  fp32
+// products with values below 2^e stay within fp32, its lift is 116 - e where that is less.  fp32
 // queries: three bf16 terms, no lift.
 struct Lift {
   int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
@@ -476,7 +482,10 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     float o[W][16][HD + 4];
   } pool;
   __shared__ float red_m[W][16], red_l[W][16];
-  __shared__ int blk_top[W];   // greatest biased exponent of the block's values, by wave
+  // The block's states, joined like a wave's: its keys and values take no part in a context's references.
+  __shared__ __align__(16) float blk_o[NQ][16][HD + 4];
+  __shared__ float blk_m[NQ][16], blk_l[NQ][16];
+  __shared__ int blk_top[W];   // greatest biased exponent of the block's numbers; 256: not all are, by wave
   const int chunk = blockIdx.z, hk = blockIdx.x;
   const int G = a.G, R = G * a.B;
   const int s = blockIdx.y / a.n_groups, row0 = 16 * NQ * (blockIdx.y - s * a.n_groups);
@@ -541,26 +550,34 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   };
   Tile<HD> even, odd;
   fetch(even, 0);
-  State<HD> st[NQ];
-  Lift lift;
+  // A query tile's state to LDS.
+  auto keep = [&](const State<HD>& b, float (&o)[16][HD + 4], float (&m)[16], float (&l)[16]) {
+    float l_sum = b.l;
+    l_sum += __shfl_xor(l_sum, 16, kWave);
+    l_sum += __shfl_xor(l_sum, 32, kWave);
+    if (g == 0) {
+      m[ql] = b.m;
+      l[ql] = l_sum;
+    }
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) st[n].o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    st[n].m = -INFINITY;
-    st[n].l = 0.f;
-  }
-  // Through LDS into the state of the wave that has the fewest tiles.
+    for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4_t*>(&o[ql][16 * dt + 4 * g]) = b.o[dt];
+  };
+  // Through LDS into states by the wave that has the fewest tiles.
   if (nbk > 0) {
     const int rows = (nbk + 31) & ~31;
     // What is no number among the values leaves as 0: a product with a masked probability's 0 would be NaN.
-    const int top = block_top<F32, NI>(bw[1]);
-    if (__any(top == 255)) numbers_only<F32, NI>(bw[1]);
+    int top = block_top<F32, NI>(bw[1]), odd_ones = 0;
+    if (__any(top == 255)) {
+      odd_ones = 256;
+      numbers_only<F32, NI>(bw[1]);
+      top = block_top<F32, NI>(bw[1]);
+    }
     int all = top;
     if (__any(top > 152)) {   // below, for_block changes nothing
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) all = max(all, __shfl_xor(all, d, kWave));
     }
+    all |= odd_ones;
     if (lane == 0) blk_top[wid] = all;
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
@@ -578,23 +595,32 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     }
     lds_barrier();
     if (wid == nct % W) {
-      int most = 0;
+      int most = 0, odd = 0;
 #pragma unroll
-      for (int w = 0; w < W; ++w) most = max(most, blk_top[w]);
+      for (int w = 0; w < W; ++w) {
+        most = max(most, blk_top[w] & 255);
+        odd |= blk_top[w] & 256;
+      }
       most = __builtin_amdgcn_readfirstlane(most);
+      odd = __builtin_amdgcn_readfirstlane(odd);
+      Lift lift;
       if constexpr (!F32) lift.for_block(most);
+      const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-        block_step<T, HD>(q[n], pool.blk, st[n], nbk, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B,
-                          lane, a.scale_log2, F32 ? 0.f : lift.value());
-      if (most == 255) {
-        const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-          no_numbers<T, HD>(st[n], vb, a.ld_vb, a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B, nbk, g);
+      for (int n = 0; n < NQ; ++n) {
+        const int last = a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B;
+        State<HD> b;
+        b.clear();
+        block_step<T, HD>(q[n], pool.blk, b, nbk, last, lane, a.scale_log2, F32 ? 0.f : lift.value());
+        if (odd != 0) no_numbers<T, HD>(b, vb, a.ld_vb, last, nbk, g);
+        keep(b, blk_o[n], blk_m[n], blk_l[n]);
       }
     }
   }
+  State<HD> st[NQ];
+  Lift lift;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) st[n].clear();
   auto step = [&](Tile<HD>& t, int l) {
     const int left = k_hi - k_lo - (wid + W * l) * kTile;
     tile_step<T, HD, NQ>(t, q, st, lift, __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, left), g,
@@ -614,16 +640,8 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   const bool direct = nc == 1;   // nothing to join
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    float l_sum = st[n].l;
-    l_sum += __shfl_xor(l_sum, 16, kWave);
-    l_sum += __shfl_xor(l_sum, 32, kWave);
     if (n > 0 || nbk > 0) __syncthreads();
-    if (g == 0) {
-      red_m[wid][ql] = st[n].m;
-      red_l[wid][ql] = l_sum;
-    }
-#pragma unroll
-    for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4_t*>(&pool.o[wid][ql][16 * dt + 4 * g]) = st[n].o[dt];
+    keep(st[n], pool.o[wid], red_m[wid], red_l[wid]);
     __syncthreads();
     for (int e = threadIdx.x; e < 16 * (HD / 4); e += kThreads) {
       const int qq = e / (HD / 4), dim = 4 * (e % (HD / 4));
@@ -632,17 +650,20 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       float mm = red_m[0][qq];
 #pragma unroll
       for (int w = 1; w < W; ++w) mm = fmaxf(mm, red_m[w][qq]);
+      if (nbk > 0) mm = fmaxf(mm, blk_m[n][qq]);
       const float base = mm == -INFINITY ? 0.f : mm;
       f32x4_t o = {0.f, 0.f, 0.f, 0.f};
       float l = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float f = half_power(red_m[w][qq] - base);
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&pool.o[w][qq][dim]);
+      auto join = [&](float m, float lw, const float* from) {
+        const float f = half_power(m - base);
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(from);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i] * f, o[i]);
-        l = fmaf(f, red_l[w][qq] * f, l);
-      }
+        l = fmaf(f, lw * f, l);
+      };
+#pragma unroll
+      for (int w = 0; w < W; ++w) join(red_m[w][qq], red_l[w][qq], &pool.o[w][qq][dim]);
+      if (nbk > 0) join(blk_m[n][qq], blk_l[n][qq], &blk_o[n][qq][dim]);
       if (direct) {
         const int64_t orow = int64_t(s) * a.B + k;
         const int h = hk * G + (qr - k * G);
