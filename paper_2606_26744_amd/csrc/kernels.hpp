@@ -361,7 +361,7 @@ struct Kv4AttnArgs {
   int64_t ld_out;
   float* lse;                // [n_seq * B][nh] or NULL
   float* part_o;             // n_chunks > 1: [n_seq][nkv][n_chunks][G * B][hd]
-  float* part_ml;            // ... [2]
+  float* part_ml;            // ... [4]: reference, sum, part_o's power of two
   int G, n_groups;           // set by the launch: n_heads / n_kv_heads, workgroups' query groups a sequence
   float inv_g;
 };

@@ -12,8 +12,8 @@
 // tile are laid out so that the lane that has a score has its probability where the second product
 // wants it.
 // Codes go from their 16-byte loads through the conversion instructions into the matrix
-// instructions.  Keys become bf16 (exactly, scale and all); values fp16 codes, their scales in the
-// probabilities (struct Lift); 32-bit queries and probabilities are three bf16 terms.
+// instructions.  Keys become bf16 (exactly, scale and all); values fp16 or bf16 codes, their scales in
+// the probabilities (struct Unit); 32-bit queries and probabilities are three bf16 terms.
 //
 // Bound by the memory where a workgroup has enough tiles: 64 contexts of 1024 to 16384 positions, 32
 // heads, B = 16, 361 us for 2.32 GB (6.4 TB/s; vector issue 53% of the cycles, matrix cores 18%);
@@ -144,10 +144,13 @@ __device__ __forceinline__ int slot_of(const Kv4AttnArgs& a, int r) {
   return int((float(r) + 0.5f) * a.inv_g);
 }
 
-// Four dims of an output row: o / l, zeros where no key was seen.
+// 2^k, |k| <= 126.
+__device__ __forceinline__ float power(int k) { return __uint_as_float(uint32_t(127 + k) << 23); }
+
+// Four dims of an output row: o / l, o held times 2^k; zeros where no key was seen.
 template <typename T>
-__device__ __forceinline__ void store_out(T* dst, f32x4_t o, float l) {
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+__device__ __forceinline__ void store_out(T* dst, f32x4_t o, float l, int k) {
+  const float inv = l == 0.f ? 0.f : power(-k) / l;
   if constexpr (sizeof(T) == 4)
     *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   else
@@ -163,18 +166,14 @@ __device__ __forceinline__ float groups_max(float x) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
-// 2^(x/2), for a factor 2^x in two steps: references differ by their lifts too, up to 205, and a sum
-// may be as large as its lift, so that a factor below fp32's range still leaves a sum within it.
-__device__ __forceinline__ float half_power(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
-
 // Running softmax of one 16-row query tile in a wave: lane (g, ql) keeps query ql.  o and l are
-// relative to 2^m, m a score (base 2) less `lift`: the greatest so far, or one that the greatest is
-// at most kSlack above.  Moving the reference costs a product an element of o, and with 16 queries a
-// tile some query's greatest rises in most tiles, by little.
+// relative to 2^m, m a score (base 2): the greatest so far, or one that the greatest is at most kSlack
+// above.  Moving the reference costs a product an element of o, and with 16 queries a tile some query's
+// greatest rises in most tiles, by little.
 constexpr int kSlack = 4;
 template <int HD>
 struct State {
-  f32x4_t o[HD / 16];    // O^T: dim 16dt + 4g + e of query ql
+  f32x4_t o[HD / 16];    // O^T: dim 16dt + 4g + e of query ql, times 2^k (struct Unit)
   float m, l;            // l: this lane group's part of the sum
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -182,25 +181,39 @@ struct State {
     m = -INFINITY;
     l = 0.f;
   }
-};
-
-// Products of 64 keys (a lane's sixteen, -inf where masked) into the state's reference and sum; x
-// leaves as exp2(c * x - m).  The lift has fallen by `drop` since the last call.
-template <int HD>
-__device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c, float lift, float drop) {
-  float top = x[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-  top = groups_max(top);
-  const float seen = fmaf(top, c, -lift);
-  if (__any(drop > 0.f || seen > st.m + float(kSlack))) {
-    const float m = fmaxf(st.m + drop, seen);
-    const float h = m > st.m ? half_power(st.m - m) : 1.f;   // st.m -inf: 0
-    st.l = st.l * h * h;
+  __device__ __forceinline__ void scale(float f) {
 #pragma unroll
     for (int dt = 0; dt < HD / 16; ++dt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[dt][e] = st.o[dt][e] * h * h;
+      for (int e = 0; e < 4; ++e) o[dt][e] *= f;
+  }
+  // Another state of the same queries; the sums are then held times the lesser unit.
+  __device__ __forceinline__ void join(const State& b, int k, int kb) {
+    const float m1 = fmaxf(m, b.m), base = m1 == -INFINITY ? 0.f : m1;
+    const float f = __builtin_amdgcn_exp2f(m - base), fb = __builtin_amdgcn_exp2f(b.m - base);
+    const float u = power(min(k, kb) - k), ub = power(min(k, kb) - kb);
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(o[dt][e] * f, u, b.o[dt][e] * fb * ub);
+    l = fmaf(l, f, b.l * fb);
+    m = m1;
+  }
+};
+
+// Products of 64 keys (a lane's sixteen, -inf where masked) into the state's reference and sum; x
+// leaves as exp2(c * x - m).
+template <int HD>
+__device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+  const float seen = groups_max(top) * c;
+  if (__any(seen > st.m + float(kSlack))) {
+    const float m = fmaxf(st.m, seen);
+    const float f = m > st.m ? __builtin_amdgcn_exp2f(st.m - m) : 1.f;   // st.m -inf: 0
+    st.l *= f;
+    st.scale(f);
     st.m = m;
   }
   const float base = st.m == -INFINITY ? 0.f : st.m;   // no key yet
@@ -213,21 +226,37 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
   st.l += sum;
 }
 
-// The lift of a wave's references.  A value's scale times its probability becomes one fp16 factor
-// of the products with the codes (bf16 queries): 11 bits, a rounding an eighth of the output's own.
-// So that it neither overflows nor loses small ones, probabilities are taken relative to 2^-lift,
-// lift = 15 - kSlack - log2 of a power of two above the greatest scale so far (2^-80 at least): the
-// factor is below 2^15, and of full precision down to 2^-25 of the greatest probability times the
-// greatest scale.  Sums stay within fp32: a probability is lost below 2^(-126 - lift), 2^-36 even
-// beside scales of 2^100.  The block's values are not split off their probabilities: so that 64
-// products with values below 2^e stay within fp32, its lift is 116 - e where that is less.  fp32
-// queries: three bf16 terms, no lift.
-struct Lift {
-  int top = 47;          // biased exponent of the greatest scale, 2^-80 at least
-  __device__ __forceinline__ float value() const { return float(141 - kSlack - top); }
-  // The block's values have biased exponents of up to `e`: below 2^(e - 126).
-  __device__ __forceinline__ void for_block(int e) { top = max(top, e - (242 - (141 - kSlack))); }
+// Sums of values are held times a unit 2^k, |k| <= kMost.  With bf16 queries a context factor, a
+// probability times its value's scale, is fp16 in tiles whose scales are all within [2^kLow, 2^kHigh) in
+// that unit: 11 bits, a rounding an eighth of the output's own, in one product with the codes.  With the
+// reference's slack a factor is below 2^15, and the greatest probability's at least 2^kLow, so that
+// the half step of fp16's subnormals, 2^-25, is 2^-23 of that one or less.
+// Tiles whose scales lie further apart, or elsewhere, are left out and go into a state of their own
+// behind the others, with factors of two bf16 terms, 16 bits of any size: a row of large values may have
+// no weight, one of small values all of it, and 2^-23 of another's scale is then no small part of the
+// output.  Those tiles are fetched twice: a context of nothing else takes 1.5 to 2.6 times as long (16 x 16
+// queries over 512 to 8192 positions, 32 heads over 8: 98 us for 38.8).  Two terms in every tile took
+// 47 us there, and 385 for 364 in the 64 contexts above.
+constexpr int kMost = 40, kLow = -2, kHigh = 11, kWindow = (kHigh - kLow) << 7;   // kWindow: in steps of bf16
+struct Unit {
+  int k = kMost;
+  uint32_t low = 0;      // bits of the window's first scale, in both halves
 };
+
+// The window that a tile of nval rows sets: 16 times above the greatest scale of its first eight rows
+// (the first row's, where there are fewer) it ends.
+template <int HD>
+__device__ __forceinline__ Unit window_of(const Tile<HD>& t, int nval) {
+  u16x2_t m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, uint32_t(t.vs[0][i])));
+  const int eight = __builtin_amdgcn_readfirstlane(max(m[0], m[1]));
+  const int one = __builtin_amdgcn_readfirstlane(int(t.vs[0][0])) & 0xFFFF;
+  Unit u;
+  u.k = min(max(kHigh - 5 - (((nval < 8 ? one : eight) >> 7) - 127), -kMost), kMost);
+  u.low = uint32_t(127 + kLow - u.k) * 0x00800080u;
+  return u;
+}
 
 // A query tile as the operand of the products with keys: lane (g, ql) holds dims (HD/4)g + 8j .. of
 // query ql, fp32 in three bf16 terms.  (The fp4 x fp8 products would take the keys as they lie and a
@@ -269,10 +298,31 @@ __device__ __forceinline__ void score(const Tile<HD>& t, int st, const Query<T, 
   }
 }
 
-// A tile of the cache into the states of NQ query tiles; nval of its 64 keys count.
-template <typename T, int HD, int NQ>
-__device__ __forceinline__ void tile_step(Tile<HD>& t, const Query<T, HD> (&q)[NQ], State<HD> (&st)[NQ],
-                                          Lift& lift, int nval, int g, float c) {
+// Values of a tile times factors p, in NT bf16 terms, into the sums.
+template <int NT, int HD, int NQ>
+__device__ __forceinline__ void values_bf16(const Tile<HD>& t, const float (&p)[NQ][16], State<HD> (&st)[NQ]) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    bf16x8_t pf[NQ][NT];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) split8<NT>(p[n] + 8 * ks, pf[n]);
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) {
+      const bf16x8_t vf = kv4_bf16x8(t.value_word(ks, dt), 1.f);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+          st[n].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][k], st[n].o[dt], 0, 0, 0);
+    }
+  }
+}
+
+// A tile of the cache into the states of NQ query tiles; nval of its 64 keys count.  NARROW: factors of
+// fp16; false, and the states as they were, where the tile does not take them.
+template <typename T, int HD, int NQ, bool NARROW>
+__device__ __forceinline__ bool tile_step(Tile<HD>& t, const Query<T, HD> (&q)[NQ], State<HD> (&st)[NQ],
+                                          Unit& unit, int nval, int g, float c) {
   constexpr bool F32 = sizeof(T) == 4;
   float x[NQ][16];
 #pragma unroll
@@ -285,64 +335,70 @@ __device__ __forceinline__ void tile_step(Tile<HD>& t, const Query<T, HD> (&q)[N
       for (int e = 0; e < 4; ++e) x[n][4 * i + e] = acc[n][e];
   }
   // x[i] is key 32 * (i/8) + 8g + i%8.  Behind the last key anything may stand, in the values'
-  // scales too.
-  if (nval < kTile) {
+  // scales too: they become the window's first.
+  auto hide = [&](int nval) {
     const int left = nval - 8 * g;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const bool off = 32 * (i >> 3) + (i & 7) >= left;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) x[n][i] = off ? -INFINITY : x[n][i];
-      const uint32_t w = t.vs[i >> 3][(i & 7) >> 1];
-      t.vs[i >> 3][(i & 7) >> 1] = off ? w & ((i & 1) ? 0x0000FFFFu : 0xFFFF0000u) : w;
+      const uint32_t w = t.vs[i >> 3][(i & 7) >> 1], keep = (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+      t.vs[i >> 3][(i & 7) >> 1] = off ? (w & keep) | (unit.low & ~keep) : w;
+    }
+  };
+  if (nval < kTile) hide(nval);
+  bool in = true;
+  u16x2_t scale[8], most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    scale[i] = __builtin_bit_cast(u16x2_t, uint32_t(t.vs[i >> 2][i & 3]));
+    if constexpr (NARROW) scale[i] -= __builtin_bit_cast(u16x2_t, unit.low);   // those below the window wrap
+    most = __builtin_elementwise_max(most, scale[i]);
+  }
+  if constexpr (NARROW) {
+    in = !__any(max(most[0], most[1]) >= kWindow);
+    if (!in) {
+      hide(0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) scale[i] = u16x2_t{0, 0};
+    }
+  } else if constexpr (!F32) {
+    if (__any((max(most[0], most[1]) >> 7) - 127 >= kMost) && unit.k > 0) {   // sums of 2^30 such values: below 2^122
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) st[n].scale(power(-2 * kMost));
+      unit.k = -kMost;
     }
   }
-  float drop = 0.f;
-  if constexpr (!F32) {
-    u16x2_t w = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w = __builtin_elementwise_max(w, __builtin_bit_cast(u16x2_t, uint32_t(t.vs[i >> 2][i & 3])));
-    int top = max(w[0], w[1]) >> 7;
-    if (__any(top > lift.top)) {
-      top = max(top, __shfl_xor(top, 16, kWave));
-      top = max(top, __shfl_xor(top, 32, kWave));
-      drop = float(top - lift.top);
-      lift.top = top;
+  for (int n = 0; n < NQ; ++n) soft_step<HD>(st[n], x[n], c);
+  const float up = power(unit.k);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    constexpr unsigned short kFirst = (127 + kLow) << 7;   // the window's first scale, in its unit
+    const uint32_t w = __builtin_bit_cast(uint32_t, NARROW ? u16x2_t(scale[i] + u16x2_t{kFirst, kFirst}) : scale[i]);
+    float s0 = lo_bf(w), s1 = hi_bf(w);
+    if constexpr (!NARROW && !F32) {
+      s0 *= up;
+      s1 *= up;
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      x[n][2 * i] *= s0;
+      x[n][2 * i + 1] *= s1;
     }
   }
-  const float up = F32 ? 0.f : lift.value();
+  if constexpr (!NARROW) {
+    values_bf16<F32 ? 3 : 2, HD, NQ>(t, x, st);
+  } else {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) soft_step<HD>(st[n], x[n], c, up, drop);
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    float s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = (e & 1) ? hi_bf(t.vs[ks][e >> 1]) : lo_bf(t.vs[ks][e >> 1]);
-    if constexpr (F32) {
-      bf16x8_t pf[NQ][3];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = x[n][8 * ks + e] * s[e];
-        split8<3>(p, pf[n]);
-      }
-#pragma unroll
-      for (int dt = 0; dt < HD / 16; ++dt) {
-        const bf16x8_t vf = kv4_bf16x8(t.value_word(ks, dt), 1.f);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int k = 0; k < 3; ++k)
-            st[n].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][k], st[n].o[dt], 0, 0, 0);
-      }
-    } else {
+    for (int ks = 0; ks < 2; ++ks) {
       f16x8_t pf[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const f16x2_t p = __builtin_convertvector(f32x2_t{x[n][8 * ks + e] * s[e], x[n][8 * ks + e + 1] * s[e + 1]}, f16x2_t);
+          const f16x2_t p = __builtin_convertvector(f32x2_t{x[n][8 * ks + e], x[n][8 * ks + e + 1]}, f16x2_t);
           pf[n][e] = p[0];
           pf[n][e + 1] = p[1];
         }
@@ -355,6 +411,7 @@ __device__ __forceinline__ void tile_step(Tile<HD>& t, const Query<T, HD> (&q)[N
       }
     }
   }
+  return in;
 }
 
 // The block's own keys and values in LDS: rows of keys, values by dim, zeros behind the last row up
@@ -366,10 +423,11 @@ struct BlockRows {
   T v[HD][64 + E];
 };
 
-// nbk of them into the state of a query tile; a query sees those up to `last`.
+// nbk of them into the state of a query tile, whose sums are held times `unit`; a query sees those up
+// to `last`.
 template <typename T, int HD>
 __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRows<T, HD>& b, State<HD>& st,
-                                           int nbk, int last, int lane, float c, float lift) {
+                                           int nbk, int last, int lane, float c, float unit) {
   constexpr bool F32 = sizeof(T) == 4;
   const int g = lane >> 4, ql = lane & 15;
   float x[16];
@@ -400,7 +458,11 @@ __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRow
     for (int e = 0; e < 4; ++e)
       x[4 * t + e] = 32 * (t >> 1) + 4 * (t & 1) + e < left ? acc[e] : -INFINITY;
   }
-  soft_step<HD>(st, x, c, lift, 0.f);
+  soft_step<HD>(st, x, c);
+  if constexpr (!F32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= unit;
+  }
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
     if (32 * ks >= nbk) break;
@@ -482,9 +544,12 @@ kv4_attn_kernel(Kv4AttnArgs a) {
     float o[W][16][HD + 4];
   } pool;
   __shared__ float red_m[W][16], red_l[W][16];
-  // The block's states, joined like a wave's: its keys and values take no part in a context's references.
+  __shared__ int red_k[W];
+  // The block's states, joined like a wave's: its keys and values take no part in a context's reference
+  // or unit.
   __shared__ __align__(16) float blk_o[NQ][16][HD + 4];
   __shared__ float blk_m[NQ][16], blk_l[NQ][16];
+  __shared__ int blk_k;
   __shared__ int blk_top[W];   // greatest biased exponent of the block's numbers; 256: not all are, by wave
   const int chunk = blockIdx.z, hk = blockIdx.x;
   const int G = a.G, R = G * a.B;
@@ -573,7 +638,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       top = block_top<F32, NI>(bw[1]);
     }
     int all = top;
-    if (__any(top > 152)) {   // below, for_block changes nothing
+    if (__any(top - 127 >= kMost)) {   // below, the unit is the least value's
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) all = max(all, __shfl_xor(all, d, kWave));
     }
@@ -603,37 +668,40 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       }
       most = __builtin_amdgcn_readfirstlane(most);
       odd = __builtin_amdgcn_readfirstlane(odd);
-      Lift lift;
-      if constexpr (!F32) lift.for_block(most);
+      const int k = F32 ? 0 : most - 127 >= kMost ? -kMost : kMost;
+      if (lane == 0) blk_k = k;
       const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         const int last = a.causal != 0 ? slot_of(a, row0 + 16 * n + ql) : a.B;
         State<HD> b;
         b.clear();
-        block_step<T, HD>(q[n], pool.blk, b, nbk, last, lane, a.scale_log2, F32 ? 0.f : lift.value());
+        block_step<T, HD>(q[n], pool.blk, b, nbk, last, lane, a.scale_log2, power(k));
         if (odd != 0) no_numbers<T, HD>(b, vb, a.ld_vb, last, nbk, g);
         keep(b, blk_o[n], blk_m[n], blk_l[n]);
       }
     }
   }
   State<HD> st[NQ];
-  Lift lift;
+  Unit unit;
+  if constexpr (F32) unit.k = 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) st[n].clear();
-  auto step = [&](Tile<HD>& t, int l) {
-    const int left = k_hi - k_lo - (wid + W * l) * kTile;
-    tile_step<T, HD, NQ>(t, q, st, lift, __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, left), g,
-                         a.scale_log2);
+  auto valid = [&](int l) {   // keys of the wave's l-th tile
+    return __builtin_amdgcn_readlane(page, l) < 0 ? 0 : min(kTile, k_hi - k_lo - (wid + W * l) * kTile);
   };
-  for (int l = 0; l < mine; l += 2) {   // the next tile always on its way
-    fetch(odd, l + 1);
-    __builtin_amdgcn_sched_barrier(0);   // loads first, not sunk between the products
-    step(even, l);
+  uint64_t left = 0;   // tiles that fp16 factors do not take
+  fetch(odd, 1);                       // the next tile always on its way
+  __builtin_amdgcn_sched_barrier(0);   // loads first, not sunk between the products
+  if constexpr (!F32) unit = window_of<HD>(even, mine > 0 ? valid(0) : 0);
+  for (int l = 0; l < mine; l += 2) {
+    if (!tile_step<T, HD, NQ, !F32>(even, q, st, unit, valid(l), g, a.scale_log2)) left |= uint64_t(1) << l;
     if (l + 1 >= mine) break;
     fetch(even, l + 2);
     __builtin_amdgcn_sched_barrier(0);
-    step(odd, l + 1);
+    if (!tile_step<T, HD, NQ, !F32>(odd, q, st, unit, valid(l + 1), g, a.scale_log2)) left |= uint64_t(2) << l;
+    fetch(odd, l + 3);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // The waves' states of a query tile side by side, then joined: four dims of a row a thread.
@@ -642,37 +710,79 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   for (int n = 0; n < NQ; ++n) {
     if (n > 0 || nbk > 0) __syncthreads();
     keep(st[n], pool.o[wid], red_m[wid], red_l[wid]);
+    int k = unit.k;
+    if constexpr (!F32) {
+      // The tiles that were left out, a query tile at a time, while this one's state lies in LDS: both at
+      // once would spill in the loop above.
+      if (left != 0) {
+        const Query<T, HD> one[1] = {q[n]};
+        State<HD> own[1], rest;
+        own[0].clear();
+        Unit wide;
+        uint64_t todo = left;
+        auto next = [&]() {   // kTile: none
+          const int l = todo != 0 ? __builtin_ctzll(todo) : kTile;
+          todo &= todo - 1;
+          return l;
+        };
+        int l = next();
+        fetch(even, l);
+        while (l < kTile) {
+          const int l1 = next();
+          fetch(odd, l1);
+          __builtin_amdgcn_sched_barrier(0);
+          tile_step<T, HD, 1, false>(even, one, own, wide, valid(l), g, a.scale_log2);
+          even = odd;
+          l = l1;
+        }
+        asm volatile("" ::: "memory");   // read back, not kept in registers
+        rest.m = st[n].m;
+        rest.l = st[n].l;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) rest.o[dt] = *reinterpret_cast<const f32x4_t*>(&pool.o[wid][ql][16 * dt + 4 * g]);
+        own[0].join(rest, wide.k, k);
+        keep(own[0], pool.o[wid], red_m[wid], red_l[wid]);
+        k = min(k, wide.k);
+      }
+    }
+    if (lane == 0) red_k[wid] = k;
     __syncthreads();
     for (int e = threadIdx.x; e < 16 * (HD / 4); e += kThreads) {
       const int qq = e / (HD / 4), dim = 4 * (e % (HD / 4));
-      const int qr = row0 + 16 * n + qq, k = slot_of(a, qr);
-      if (k >= blen) continue;
+      const int qr = row0 + 16 * n + qq, slot = slot_of(a, qr);
+      if (slot >= blen) continue;
       float mm = red_m[0][qq];
 #pragma unroll
       for (int w = 1; w < W; ++w) mm = fmaxf(mm, red_m[w][qq]);
-      if (nbk > 0) mm = fmaxf(mm, blk_m[n][qq]);
+      int k_min = red_k[0];        // the sums' unit: the least
+#pragma unroll
+      for (int w = 1; w < W; ++w) k_min = min(k_min, red_k[w]);
+      if (nbk > 0) {
+        mm = fmaxf(mm, blk_m[n][qq]);
+        k_min = min(k_min, blk_k);
+      }
       const float base = mm == -INFINITY ? 0.f : mm;
       f32x4_t o = {0.f, 0.f, 0.f, 0.f};
       float l = 0.f;
-      auto join = [&](float m, float lw, const float* from) {
-        const float f = half_power(m - base);
+      auto join = [&](float m, float lw, int kw, const float* from) {
+        const float f = __builtin_amdgcn_exp2f(m - base), u = power(k_min - kw);
         const f32x4_t v = *reinterpret_cast<const f32x4_t*>(from);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i] * f, o[i]);
-        l = fmaf(f, lw * f, l);
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i] * f, u, o[i]);
+        l = fmaf(f, lw, l);
       };
 #pragma unroll
-      for (int w = 0; w < W; ++w) join(red_m[w][qq], red_l[w][qq], &pool.o[w][qq][dim]);
-      if (nbk > 0) join(blk_m[n][qq], blk_l[n][qq], &blk_o[n][qq][dim]);
+      for (int w = 0; w < W; ++w) join(red_m[w][qq], red_l[w][qq], red_k[w], &pool.o[w][qq][dim]);
+      if (nbk > 0) join(blk_m[n][qq], blk_l[n][qq], blk_k, &blk_o[n][qq][dim]);
       if (direct) {
-        const int64_t orow = int64_t(s) * a.B + k;
-        const int h = hk * G + (qr - k * G);
-        store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + dim, o, l);
+        const int64_t orow = int64_t(s) * a.B + slot;
+        const int h = hk * G + (qr - slot * G);
+        store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + dim, o, l, k_min);
         if (dim == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(l)) * 0.6931471805599453f;
       } else {
         const int64_t p = ((int64_t(s) * a.nkv + hk) * a.n_chunks + chunk) * R + qr;
         *reinterpret_cast<f32x4_t*>(a.part_o + p * HD + dim) = o;
-        if (dim == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * p) = make_float2(mm, l);
+        if (dim == 0) *reinterpret_cast<float4*>(a.part_ml + 4 * p) = make_float4(mm, l, float(k_min), 0.f);
       }
     }
   }
@@ -685,6 +795,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int Q = HD / 4, N = kJoinThreads / (Q * S);
   __shared__ f32x4_t so[N * S][Q];
   __shared__ float sm[N * S], sl[N * S];
+  __shared__ int sk[N * S];
   const int G = a.G, R = G * a.B;
   const int hk = blockIdx.y, s = blockIdx.z;
   const int nc = chunks_of(a, context_of(a, s));
@@ -695,43 +806,52 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
   if (N == 1 && k >= block_of(a, s)) return;
   const int64_t base = (int64_t(s) * a.nkv + hk) * a.n_chunks;
   float m = -INFINITY, l = 0.f;
+  int ko = kMost;              // o is held times 2^ko, the least of the chunks'
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
   for (int c = sl_; c < nc; c += S) {
     const int64_t p = (base + c) * R + qr;
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * p);
+    const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + 4 * p);
     const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part_o + p * HD + 4 * d);
     const float mn = fmaxf(m, ml.x);
     const float b = mn == -INFINITY ? 0.f : mn;
-    const float f0 = half_power(m - b), f1 = half_power(ml.x - b);
-    l = fmaf(l * f0, f0, ml.y * f1 * f1);
+    const int kc = int(ml.z), kn = min(ko, kc);
+    const float f0 = __builtin_amdgcn_exp2f(m - b), f1 = __builtin_amdgcn_exp2f(ml.x - b);
+    const float u0 = power(kn - ko), u1 = power(kn - kc);
+    l = fmaf(l, f0, ml.y * f1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i] * f0, f0, v[i] * f1 * f1);
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i] * f0, u0, v[i] * f1 * u1);
     m = mn;
+    ko = kn;
   }
   so[at][d] = o;
   if (d == 0) {
     sm[at] = m;
     sl[at] = l;
+    sk[at] = ko;
   }
   __syncthreads();
   if (sl_ != 0 || k >= block_of(a, s)) return;
   float mm = sm[at];
+  ko = sk[at];
 #pragma unroll
-  for (int w = 1; w < S; ++w) mm = fmaxf(mm, sm[at + w]);
+  for (int w = 1; w < S; ++w) {
+    mm = fmaxf(mm, sm[at + w]);
+    ko = min(ko, sk[at + w]);
+  }
   const float b = mm == -INFINITY ? 0.f : mm;
   float sum = 0.f;
   o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int w = 0; w < S; ++w) {
-    const float f = half_power(sm[at + w] - b);
-    sum = fmaf(f, sl[at + w] * f, sum);
+    const float f = __builtin_amdgcn_exp2f(sm[at + w] - b), u = power(ko - sk[at + w]);
+    sum = fmaf(f, sl[at + w], sum);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, so[at + w][d][i] * f, o[i]);
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(so[at + w][d][i] * f, u, o[i]);
   }
   const int64_t orow = int64_t(s) * a.B + k;
   const int h = hk * G + (qr - k * G);
   store_out<T>(static_cast<T*>(a.out) + orow * a.ld_out + int64_t(h) * HD + 4 * d,
-               o, sum);
+               o, sum, ko);
   if (d == 0 && a.lse != nullptr) a.lse[orow * a.nh + h] = (mm + __log2f(sum)) * 0.6931471805599453f;
 }
 
@@ -823,7 +943,7 @@ size_t kv4_attn_ws_bytes(int n_seq, int nkv, int64_t q_rows, int hd, int max_ctx
   const int64_t longest = (int64_t(max_ctx) + kMaxChunk - 1) / kMaxChunk;
   const int64_t most = std::max(chunks_wanted(n_seq, nkv, q_rows, max_ctx), longest);
   if (most <= 1) return 0;
-  return size_t(n_seq) * nkv * size_t(most) * size_t(q_rows) * (hd + 2) * 4;
+  return size_t(n_seq) * nkv * size_t(most) * size_t(q_rows) * (hd + 4) * 4;
 }
 
 hipError_t launch_kv4_attention(bool bf16, int hd, const Kv4AttnArgs& args, void* ws, hipStream_t s) {

@@ -13,7 +13,7 @@ of a key's whole head:
   in fp32, each at most N 2^-24, of outputs and of weights; the result is rounded once, 2^-8 of itself
   (bf16) or 2^-24 (fp32).  Below fp32's least normal number may be 0: a probability relative to the
   greatest and the lower term it is split into, 2 * 2^-126 max |v| a key; a sum in its unit, which is
-  2^-86 beside values of 2^69 and more.
+  2^-86 beside values of 2^40 and more.
 """
 import numpy as np
 import pytest
@@ -87,7 +87,7 @@ def _check(c, out, lse, *, causal=False, slots=None):
         N = T + B
         tol = mass * (2 * d[..., None] + (2.0 ** -24 if f32 else 2.0 ** -11) + 2 * N * 2.0 ** -24)
         tol += np.abs(o) * (2.0 ** -24 if f32 else 2.0 ** -8)
-        least = 2 * 2.0 ** -126 * top + np.where(top >= 2.0 ** 69, 6 * 2.0 ** -86, 6 * 2.0 ** -126)
+        least = 2 * 2.0 ** -126 * top + np.where(top >= 2.0 ** 40, 6 * 2.0 ** -86, 6 * 2.0 ** -126)
         tol += N * (least + (0.0 if f32 else 2.0 ** -23 * W))[..., None]
         err = np.abs(_np(out[s, :B]) - o)
         worst = float((err / np.maximum(mass, 1e-300)).max(initial=0.0))
@@ -102,10 +102,10 @@ FORMS = [(BF, 128, 9, 4), (BF, 64, 6, 2), (BF, 128, 9, 8), (F32, 128, 9, 2), (F3
 
 @pytest.mark.parametrize("dtype,hd,B,H", FORMS)
 @pytest.mark.parametrize("size", [1.0, 0.02, 1e-3])
-@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 3e38, 2.0 ** 70])
 def test_unseen_slots_leave_the_others_as_they_are(dtype, hd, B, H, size, bad):
-    """Contexts of 10 to 63 tiles under a causal block whose later slots hold what is no number; a
-    dim of a slot that sees it keeps its precision in the others."""
+    """Contexts of 10 to 63 tiles under a causal block whose later slots hold what is no number, or
+    nearly none; a dim of a slot that sees it keeps its precision in the others."""
     print(f"[kv4 ranges] unseen {dtype} hd={hd} B={B} H={H} size={size} bad={bad}", flush=True)
     c = Case([1030, 600, 4000, 0], B, H, 2, hd, dtype, size, 41)
     clean, lse0 = c(causal=True)
@@ -115,3 +115,66 @@ def test_unseen_slots_leave_the_others_as_they_are(dtype, hd, B, H, size, bad):
     assert torch.equal(out[:, :5], clean[:, :5]) and torch.equal(lse, lse0)
     others = [d for d in range(hd) if d != 3]
     assert torch.equal(out[..., others], clean[..., others])
+
+
+@pytest.mark.parametrize("dtype,hd,B,H", FORMS)
+@pytest.mark.parametrize("big", [2.0 ** 14, 2.0 ** 26, 1e10, 2.0 ** 40, 1e20, 1e30])
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+def test_a_row_of_large_values_and_no_weight(dtype, hd, B, H, big, where):
+    """Ordinary rows beside one whose values are far larger and whose probability is 2^-100 or so."""
+    print(f"[kv4 ranges] large {dtype} hd={hd} B={B} H={H} big={big} {where}", flush=True)
+    c = Case([700, 1500, 4000], B, H, 2, hd, dtype, 0.02, 42)
+    c.q[..., 0] = 8.0
+    for s, T in enumerate(c.ctx):
+        k, v = torch.zeros(1, 2, hd), torch.randn(1, 2, hd, generator=torch.Generator().manual_seed(7))
+        k[0, :, 0] = -8.75 * hd ** 0.5           # a score of -70, about 2^-100
+        c.put(s, {"first": 1, "middle": T // 2, "last": T - 2}[where], k, v * big)
+    out, lse = c()
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hd,B,H", FORMS)
+@pytest.mark.parametrize("small", [0.0, 1e-30, 2.0 ** -30, 2.0 ** -14])
+@pytest.mark.parametrize("where", ["first", "last", "block"])
+def test_a_row_of_small_values_and_all_the_weight(dtype, hd, B, H, small, where):
+    """Rows of about 2^-40 of the weight beside one that has the rest and the smallest values, in the
+    context or in the block: the output is of the size of either part's."""
+    print(f"[kv4 ranges] small {dtype} hd={hd} B={B} H={H} small={small} {where}", flush=True)
+    c = Case([700, 1500, 4000], B, H, 2, hd, dtype, 1.0, 43)
+    c.q[..., 0] = 8.0
+    k, v = torch.zeros(1, 2, hd), torch.randn(1, 2, hd, generator=torch.Generator().manual_seed(8)) * small
+    k[0, :, 0] = 3.5 * hd ** 0.5                 # a score of 28, about 2^40
+    if where == "block":
+        c.kb[:, 2:3], c.vb[:, 2:3] = k.to(c.dtype).cuda(), v.to(c.dtype).cuda()
+    else:
+        for s, T in enumerate(c.ctx):
+            c.put(s, 3 if where == "first" else T - 3, k, v)
+    out, lse = c()
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hd,B,H", FORMS)
+@pytest.mark.parametrize("spread", [1.0, 4.0, 10.0])
+def test_values_of_sizes_that_vary(dtype, hd, B, H, spread):
+    """Sizes of rows from a log-normal distribution: a factor of 2 either way to one of 2^10."""
+    print(f"[kv4 ranges] spread {dtype} hd={hd} B={B} H={H} spread={spread}", flush=True)
+    c = Case([700, 1500, 4000], B, H, 2, hd, dtype, 1.0, 44)
+    for s, T in enumerate(c.ctx):
+        g = torch.Generator().manual_seed(s)
+        size = torch.exp2(spread * torch.randn(T, 2, 1, generator=g))
+        c.put(s, 0, None, torch.randn(T, 2, hd, generator=g) * size)
+    out, lse = c()
+    _check(c, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hd", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("ctx", [700, 5000])
+def test_log_sum_exp_of_equal_scores(dtype, hd, ctx):
+    """Queries of zeros: the sum is the number of keys, exactly, and its logarithm off by the
+    logarithm's last place and a product's rounding, whatever the values are."""
+    c = Case([ctx], 4, 2, 1, hd, dtype, 1e-28, 46)
+    c.q.zero_()
+    out, lse = c()
+    want = np.log(ctx + 4.0)
+    assert (np.abs(_np(lse) - want) <= 2.0 ** -22 * (1 + want)).all()
+    _check(c, out, lse)
