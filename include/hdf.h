@@ -306,7 +306,7 @@ typedef struct {
  * (an eighth of the output's own rounding) or to 2^-23 of the greatest such product, where the scales of
  * 64 rows are within 2^13 of one another; else to 16 bits.  fp32: queries and probabilities keep 24.
  * Probabilities below 2^-126 of the greatest may count as 0, and sums of values below 2^-86 beside
- * values of 2^40 and more.  A slot with no key at all gets zeros and an lse of
+ * values of 2^40 (fp32: 2^80) and more.  A slot with no key at all gets zeros and an lse of
  * -inf; what a slot does not see does not reach it, whatever it holds.  B = 1 is the decoding of
  * single tokens; without the block's keys, write a position to the cache before the query that
  * should see it.

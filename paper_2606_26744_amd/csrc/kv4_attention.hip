@@ -226,7 +226,11 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
   st.l += sum;
 }
 
-// Sums of values are held times a unit 2^k, |k| <= kMost.  With bf16 queries a context factor, a
+// Sums of values are held times a unit 2^k, |k| <= kMost, so that they stay within fp32 where their
+// quotients do: k is -kMost from values on that are beyond 2^kTop in the unit at the start, so that sums
+// of 2^30 keys at 2^kSlack are below 2^123.
+//
+// With bf16 queries a context factor, a
 // probability times its value's scale, is fp16 in tiles whose scales are all within [2^kLow, 2^kHigh) in
 // that unit: 11 bits, a rounding an eighth of the output's own, in one product with the codes.  With the
 // reference's slack a factor is below 2^15, and the greatest probability's at least 2^kLow, so that
@@ -237,9 +241,11 @@ __device__ __forceinline__ void soft_step(State<HD>& st, float (&x)[16], float c
 // output.  Those tiles are fetched twice: a context of nothing else takes 1.5 to 2.6 times as long (16 x 16
 // queries over 512 to 8192 positions, 32 heads over 8: 98 us for 38.8).  Two terms in every tile took
 // 47 us there, and 385 for 364 in the 64 contexts above.
-constexpr int kMost = 40, kLow = -2, kHigh = 11, kWindow = (kHigh - kLow) << 7;   // kWindow: in steps of bf16
+constexpr int kMost = 40, kTop = 80, kLow = -2, kHigh = 11, kWindow = (kHigh - kLow) << 7;   // kWindow: in steps of bf16
+template <typename T>
+constexpr int kStart = sizeof(T) == 4 ? 0 : kMost;
 struct Unit {
-  int k = kMost;
+  int k;
   uint32_t low = 0;      // bits of the window's first scale, in both halves
 };
 
@@ -363,10 +369,10 @@ __device__ __forceinline__ bool tile_step(Tile<HD>& t, const Query<T, HD> (&q)[N
 #pragma unroll
       for (int i = 0; i < 8; ++i) scale[i] = u16x2_t{0, 0};
     }
-  } else if constexpr (!F32) {
-    if (__any((max(most[0], most[1]) >> 7) - 127 >= kMost) && unit.k > 0) {   // sums of 2^30 such values: below 2^122
+  } else {
+    if (__any((max(most[0], most[1]) >> 7) - 127 + unit.k >= kTop) && unit.k > -kMost) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) st[n].scale(power(-2 * kMost));
+      for (int n = 0; n < NQ; ++n) st[n].scale(power(-kMost - unit.k));
       unit.k = -kMost;
     }
   }
@@ -378,7 +384,7 @@ __device__ __forceinline__ bool tile_step(Tile<HD>& t, const Query<T, HD> (&q)[N
     constexpr unsigned short kFirst = (127 + kLow) << 7;   // the window's first scale, in its unit
     const uint32_t w = __builtin_bit_cast(uint32_t, NARROW ? u16x2_t(scale[i] + u16x2_t{kFirst, kFirst}) : scale[i]);
     float s0 = lo_bf(w), s1 = hi_bf(w);
-    if constexpr (!NARROW && !F32) {
+    if constexpr (!NARROW) {
       s0 *= up;
       s1 *= up;
     }
@@ -459,10 +465,8 @@ __device__ __forceinline__ void block_step(const Query<T, HD>& q, const BlockRow
       x[4 * t + e] = 32 * (t >> 1) + 4 * (t & 1) + e < left ? acc[e] : -INFINITY;
   }
   soft_step<HD>(st, x, c);
-  if constexpr (!F32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= unit;
-  }
+  for (int i = 0; i < 16; ++i) x[i] *= unit;
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
     if (32 * ks >= nbk) break;
@@ -638,7 +642,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       top = block_top<F32, NI>(bw[1]);
     }
     int all = top;
-    if (__any(top - 127 >= kMost)) {   // below, the unit is the least value's
+    if (__any(top - 127 + kStart<T> >= kTop)) {   // below, the unit stays what it is
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) all = max(all, __shfl_xor(all, d, kWave));
     }
@@ -668,7 +672,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
       }
       most = __builtin_amdgcn_readfirstlane(most);
       odd = __builtin_amdgcn_readfirstlane(odd);
-      const int k = F32 ? 0 : most - 127 >= kMost ? -kMost : kMost;
+      const int k = most - 127 + kStart<T> >= kTop ? -kMost : kStart<T>;
       if (lane == 0) blk_k = k;
       const T* vb = static_cast<const T*>(a.vb) + int64_t(s) * a.B * a.ld_vb + int64_t(hk) * HD;
 #pragma unroll
@@ -684,7 +688,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
   }
   State<HD> st[NQ];
   Unit unit;
-  if constexpr (F32) unit.k = 0;
+  unit.k = kStart<T>;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) st[n].clear();
   auto valid = [&](int l) {   // keys of the wave's l-th tile
@@ -719,6 +723,7 @@ kv4_attn_kernel(Kv4AttnArgs a) {
         State<HD> own[1], rest;
         own[0].clear();
         Unit wide;
+        wide.k = kStart<T>;
         uint64_t todo = left;
         auto next = [&]() {   // kTile: none
           const int l = todo != 0 ? __builtin_ctzll(todo) : kTile;

@@ -167,6 +167,24 @@ def test_values_of_sizes_that_vary(dtype, hd, B, H, spread):
     _check(c, out, lse)
 
 
+@pytest.mark.parametrize("dtype,hd", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("size", [1e30, 1e36, 5e37])
+def test_sums_of_large_values(dtype, hd, size):
+    """Many keys of nearly the same score whose values' sum is beyond the type while their mean is
+    not, in the context and in the block."""
+    print(f"[kv4 ranges] sums {dtype} hd={hd} size={size}", flush=True)
+    c = Case([4096, 300, 0], 64, 2, 1, hd, dtype, 1.0, 45)
+    for s, T in enumerate(c.ctx):
+        if T:
+            g = torch.Generator().manual_seed(s)
+            c.put(s, 0, None, torch.rand(T, 1, hd, generator=g) * size)
+    c.vb.copy_(torch.rand(c.vb.shape, generator=torch.Generator().manual_seed(9)) * size)
+    c.q.mul_(0.01)
+    out, lse = c()
+    assert torch.isfinite(out.float()).all()
+    _check(c, out, lse)
+
+
 @pytest.mark.parametrize("dtype,hd", [(BF, 128), (F32, 64)])
 @pytest.mark.parametrize("ctx", [700, 5000])
 def test_log_sum_exp_of_equal_scores(dtype, hd, ctx):
