@@ -196,3 +196,34 @@ def test_log_sum_exp_of_equal_scores(dtype, hd, ctx):
     want = np.log(ctx + 4.0)
     assert (np.abs(_np(lse) - want) <= 2.0 ** -22 * (1 + want)).all()
     _check(c, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hd,B,H", [(BF, 128, 3, 8), (BF, 128, 9, 16), (BF, 64, 16, 16), (F32, 64, 9, 16)])
+def test_many_short_contexts_of_sizes_that_vary(dtype, hd, B, H):
+    """More workgroups than the card has compute units, for which smaller ones are taken: sizes of a
+    factor of 2^10 either way, causal, NaN in the last slot."""
+    print(f"[kv4 ranges] many {dtype} hd={hd} B={B} H={H}", flush=True)
+    c = Case(([0, 1, 64, 65, 130, 300, 513, 700] * 5)[:36], B, H, 8, hd, dtype, 1.0, 47)
+    for s, T in enumerate(c.ctx):
+        if T:
+            g = torch.Generator().manual_seed(s)
+            size = torch.exp2(10 * torch.randn(T, 8, 1, generator=g))
+            c.put(s, 0, None, torch.randn(T, 8, hd, generator=g) * size)
+    c.vb[:, B - 1] = float("nan")
+    out, lse = c(causal=True)
+    _check(c, out, lse, causal=True, slots=[B - 1] * len(c.ctx))
+    assert torch.isnan(out[:, B - 1]).all()
+
+
+@pytest.mark.parametrize("place", ["first", "last", "all"])
+def test_a_chunk_of_as_many_tiles_as_a_workgroup_takes(place):
+    """32768 positions in one chunk, 64 tiles a wave: large values without weight in the first or the
+    last tile of a wave, or in every second one."""
+    c = Case([32768] + [0] * 32, 1, 8, 8, 64, BF, 0.02, 48)
+    c.q[..., 0] = 8.0
+    k, v = torch.zeros(1, 8, 64), torch.randn(1, 8, 64, generator=torch.Generator().manual_seed(7)) * 1e10
+    k[0, :, 0] = -8.75 * 8                       # a score of -70
+    for t in {"first": [0], "last": [511], "all": range(0, 512, 2)}[place]:
+        c.put(0, 64 * t + 63, k, v)
+    out, lse = c()
+    _check(c, out, lse)
