@@ -16,11 +16,12 @@
 // the probabilities (struct Unit); 32-bit queries and probabilities are three bf16 terms.
 //
 // Bound by the memory where a workgroup has enough tiles: 64 contexts of 1024 to 16384 positions, 32
-// heads, B = 16, 361 us for 2.32 GB (6.4 TB/s; vector issue 53% of the cycles, matrix cores 18%);
-// 8 x 2048 positions 13 to 15 us for 70 MB, 3 of them start and join.  Bound by instruction
-// issue where 32 queries share a head of keys: a tile takes a wave about 430 vector and 64 matrix
-// instructions, 3100 cycles beside the SIMD's other wave, so 16 contexts of 512 to 8192 positions, 32
-// heads over 8, B = 16, take 39 us, the time of the longest's workgroups (2.0 TB/s on average).
+// heads, B = 16, 363 us for 2.32 GB (6.4 TB/s; vector issue 51% of the cycles, matrix cores 17%);
+// 8 x 2048 positions 14 to 15.5 us for 70 MB, 3 of them start and join.  Bound by instruction issue where 32
+// queries share a head of keys: 16 contexts of one length, 32 heads over 8, B = 16 (256 workgroups), take
+// 10 us and 2.4 for every tile a wave, 5800 cycles in which the SIMD's two waves have a tile each, about
+// 4300 of them vector issue (500 instructions a tile) and 2050 of the matrix cores (64).  Contexts of 512 to
+// 8192 positions take 39 us (2.0 TB/s on average) where the longest has 6656, 13 tiles a wave: 41 by that.
 // A conversion costs what any vector instruction does (4.6 cycles; to fp16 as to bf16), an
 // exponential two, a matrix instruction 16 of the matrix core and about half of them of the issue.
 // Measured and not kept: products of fp4 keys with two fp8 terms of a query (products 2^-11 below an
@@ -870,6 +871,12 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4AttnArgs a) {
 //   24          (3)     19, 14       32, 24       45, 44        97, 100
 //   64          (8)     52, 33 (500) 68, 50       127, 114      221, 209      363, 383
 // and all of one length: 16 of 2000 31, 26, of 8000 100, 97; 12 of 8000 80, 79.
+// The other forms, 16 queries, up to 300, 1000, 2000, 8000 positions, eight / four:
+//   bf16, heads of 64, 32 heads, 16 contexts    8 / 7    10 / 9    13 / 13   34 / 34
+//   fp32, heads of 64, 32 heads, 16 contexts   13 / 9    16 / 13   21 / 18   47 / 50
+//   fp32, 32 heads, 16 contexts                21 / 14   26 / 20   33 / 28   77 / 78
+//   bf16, 32 heads over 8, 32 contexts         21 / 14   25 / 20   32 / 27   69 / 73
+//   bf16, 32 heads over 8, 128 contexts        79 / 47   97 / 63  120 / 83  252 / 235
 bool few_waves(int64_t wgs, int max_ctx) {
   const int64_t rounds = wgs / device_cu_count();
   return wgs > device_cu_count() && max_ctx <= 2048 * std::min<int64_t>(rounds, 4);
@@ -920,6 +927,9 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
 //     1024                          9.9                  9.1
 //     4096 (256: 512)              12.2    12.1   14.1   17.3
 //     16384 (256: 2048)            32.8    23.5   17.5   50.4
+// From 1024 to 1536 positions chunks of 512 and the whole context are within 0.6 us of one another, now
+// the one ahead and now the other (1 query, in a graph: 1024 9.4 and 9.0, 1300 9.8 and 10.4, 1500 9.9 and
+// 10.4; 16 queries: 10.6 and 9.8, 11.2 and 11.3, 11.1 and 11.2); whole ones need no workspace.
 // More than a round pays nowhere: 64 contexts of up to 16384 take 607, 493, 423, 389, 361 us in chunks
 // of 1024, 2048, 4096, 8192, 16384 (2048 workgroups), 16 of 512 to 8192 in 256 workgroups 39, in twice
 // and four times as many 45 and 48.
