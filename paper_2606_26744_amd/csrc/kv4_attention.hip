@@ -927,7 +927,7 @@ hipError_t attn_t(Kv4AttnArgs a, hipStream_t s) {
 //     1024                          9.9                  9.1
 //     4096 (256: 512)              12.2    12.1   14.1   17.3
 //     16384 (256: 2048)            32.8    23.5   17.5   50.4
-// From 1024 to 1536 positions chunks of 512 and the whole context are within 0.6 us of one another, now
+// From 1024 to 1536 positions chunks of 512 and the whole context are within 0.8 us of one another, now
 // the one ahead and now the other (1 query, in a graph: 1024 9.4 and 9.0, 1300 9.8 and 10.4, 1500 9.9 and
 // 10.4; 16 queries: 10.6 and 9.8, 11.2 and 11.3, 11.1 and 11.2); whole ones need no workspace.
 // More than a round pays nowhere: 64 contexts of up to 16384 take 607, 493, 423, 389, 361 us in chunks
